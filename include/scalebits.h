@@ -416,6 +416,97 @@ int  sbits_mp_gemm(sbits_plan *plan, int mat, const void *x_bf16, int64_t ld_x, 
                    const uint8_t *level, const int64_t *byte_off, const uint8_t *codes,
                    const float *scale, const float *zero, float *y, void *ws);
 
+/* ---- layers with 4-bit floating point weights ------------------------------------
+ * The microscaled form: a row's values in blocks of 32; a block has a power of two,
+ * 2^(byte - 127), and each value a code of 4 bits, sign and magnitude 0, 0.5, 1, 1.5,
+ * 2, 3, 4 or 6 (codes 0 .. 7; 8 .. 15 negative).  A byte of 255 makes its block NaN.
+ * codes: row i at i * ld_codes bytes, element j in byte j / 2, even ones in the low
+ * half; scales: row i at i * ld_scales bytes, one byte a block.  cols a multiple of
+ * 32; codes 16-byte aligned, ld_codes >= cols / 2 and a multiple of 16; scales 4-byte
+ * aligned, ld_scales a multiple of 4 and >= sbits_mx_scale_pitch(cols).  Bytes of a row behind
+ * its last block may hold anything.  These calls take a context, not a plan; NaN
+ * and infinities are honoured in all of them.                                     */
+typedef struct {
+    void *codes, *scales;                      /* DEVICE                              */
+    int64_t rows, cols, ld_codes, ld_scales;   /* pitches in bytes                    */
+} sbits_mx;
+int64_t sbits_mx_scale_pitch(int64_t cols);    /* cols / 32 up to a multiple of 4     */
+int64_t sbits_mx_out_pitch(int64_t rows);      /* rows up to a multiple of 8          */
+
+/* element types of arguments below */
+#define SBITS_TYPE_FP32 0
+#define SBITS_TYPE_BF16 1
+
+/* x to the microscaled form: the power of two is that of the block's largest
+ * magnitude less 2 (at least 2^-125), so that the largest magnitude is below 8 times it;
+ * quotients round to the nearest value, ties to the even code, above 6 to 6.  A block with
+ * a NaN or an infinity gets the byte 255 and codes 0.  x: [q->rows][ld_x] of x_type,
+ * 16-byte aligned, ld_x >= cols and a multiple of 8 (bf16) or 4 (fp32).  values_bf16
+ * (may be NULL): [rows][ld_values], what the codes stand for, rounded to bfloat16;
+ * 16-byte aligned, ld_values >= cols and a multiple of 8.  rows may be 0.          */
+int  sbits_mx_quantize(sbits_ctx *ctx, const void *x, int x_type, int64_t ld_x, const sbits_mx *q,
+                       void *values_bf16, int64_t ld_values);
+
+/* y[b][i] = sum_j W[i][j] x[b][j], or with `gated` y[b][i] = silu(g) * u, where g and u
+ * are those sums for rows i and w->rows / 2 + i (silu(g) = g / (1 + e^-g)).  x comes
+ * either as x_bf16 ([batch][ld_x], 16-byte aligned, ld_x >= cols and a multiple of 8)
+ * or, already quantised, as x_mx (rows >= batch, the same cols): exactly one is not NULL.
+ * y: [batch][ld_y] of y_type, 16-byte aligned, ld_y >= the outputs of a row and a multiple
+ * of 8; elements of a row behind those are left as they are.  Sums are taken in fp32 on the matrix
+ * cores and rounded once; a call gives the same bits again.  With x_bf16 a value of W beyond
+ * bfloat16's range (possible with the bytes 253 and 254 only) counts as infinite.  batch may be 0.  ws: 256-byte
+ * aligned, sbits_mx_gemm_ws_bytes() bytes (which may be 0).                        */
+size_t sbits_mx_gemm_ws_bytes(const sbits_ctx *ctx, const sbits_mx *w, int64_t batch, int four_bit, int gated);
+int  sbits_mx_gemm(sbits_ctx *ctx, const sbits_mx *w, const void *x_bf16, int64_t ld_x, const sbits_mx *x_mx, int64_t batch,
+                   int gated, void *y, int y_type, int64_t ld_y, void *ws, size_t ws_bytes);
+
+/* The choice of experts.  p = softmax(logits) or sigmoid(logits); score = p + bias (bias
+ * may be NULL: p).  With groups > 1 the experts form groups of experts / groups consecutive
+ * ones, a group counts the sum of its two best scores (SBITS_ROUTE_GROUP_TOP2) or its best
+ * (SBITS_ROUTE_GROUP_MAX), and only the top_groups best groups stay.  ids: the top_k best
+ * scores, descending, ties to the lower index, groups too; weights: their p, divided by
+ * their sum if `renormalize`.  Logits that are not finite are experts that are not there
+ * (p = 0, never chosen), and an expert with a bias that is not finite is never chosen; where
+ * none is left the id is -1 and the weight 0.  Scores that decide are computed in 64 bits.  */
+#define SBITS_ROUTE_SOFTMAX 0
+#define SBITS_ROUTE_SIGMOID 1
+#define SBITS_ROUTE_GROUP_TOP2 0
+#define SBITS_ROUTE_GROUP_MAX  1
+typedef struct {
+    int32_t experts;       /* 1 .. 512, a multiple of groups                              */
+    int32_t top_k;         /* 1 .. 32, at most top_groups * experts / groups              */
+    int32_t scoring;       /* SBITS_ROUTE_SOFTMAX, SBITS_ROUTE_SIGMOID                    */
+    int32_t groups;        /* 1 .. 64                                                     */
+    int32_t top_groups;    /* 1 .. groups                                                 */
+    int32_t group_score;   /* SBITS_ROUTE_GROUP_TOP2, SBITS_ROUTE_GROUP_MAX               */
+    int32_t renormalize;   /* 0, 1                                                        */
+} sbits_router;
+/* logits: [tokens][ld_logits] of logits_type; bias: float32[experts] or NULL; ids,
+ * weights: [tokens][top_k].  tokens may be 0, in the next call, too.               */
+int  sbits_route(sbits_ctx *ctx, const sbits_router *r, const void *logits, int logits_type, int64_t ld_logits,
+                 const float *bias, int64_t tokens, int32_t *ids, float *weights);
+/* d_logits[tokens][ld_d], float32: the gradient with respect to the logits, given the one
+ * with respect to the weights, d_weights[tokens][top_k]; the choice counts as fixed.  ids:
+ * as sbits_route gave them, distinct in a row; those outside 0 .. experts - 1 are skipped.  */
+int  sbits_route_backward(sbits_ctx *ctx, const sbits_router *r, const void *logits, int logits_type, int64_t ld_logits,
+                          const int32_t *ids, const float *d_weights, int64_t tokens, float *d_logits, int64_t ld_d);
+
+/* A layer of experts: sbits_route, then out[t] = sum over t's experts e of
+ * weight * down_e (silu(g) * u), (g, u) = up_e x[t].  up: experts * 2 * inner rows (of expert e
+ * first inner rows of g, then as many of u) by hidden columns; down: experts * hidden
+ * rows by inner columns.  h = silu(g) * u is rounded to bfloat16, and the experts' outputs are,
+ * before the weighted sum, which is taken in fp32 in the order of the ids.  four_bit: x and h
+ * enter the products in the microscaled form.  x_bf16: [tokens][ld_x] as in sbits_mx_gemm;
+ * out_bf16: [tokens][ld_out], 16-byte aligned, ld_out >= hidden and a multiple of 8; ids,
+ * weights: written as by sbits_route.  tokens >= 0, tokens * top_k < 2^30.  A token
+ * without an expert gets zeros.  ws: 256-byte aligned, sbits_expert_layer_ws_bytes().  */
+size_t sbits_expert_layer_ws_bytes(const sbits_ctx *ctx, const sbits_router *r, int64_t tokens, const sbits_mx *up,
+                                   const sbits_mx *down, int four_bit);
+int  sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits, int logits_type, int64_t ld_logits,
+                        const float *bias, const void *x_bf16, int64_t ld_x, int64_t tokens, const sbits_mx *up,
+                        const sbits_mx *down, void *out_bf16, int64_t ld_out, int32_t *ids, float *weights, int four_bit,
+                        void *ws, size_t ws_bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,6 +16,9 @@ OK = 0
 ERR_INVALID_ARG, ERR_BAD_SHAPE, ERR_BAD_BITWIDTHS, ERR_INFEASIBLE_BUDGET = -1, -2, -3, -4
 DIM_INDEPENDENT, DIM_FIXED = -1, -2
 ERR_WORKSPACE, ERR_MAX_ITERS, ERR_HIP, ERR_UNIMPLEMENTED, ERR_CAPACITY, ERR_INTERNAL = -5, -6, -7, -8, -9, -10
+TYPE_FP32, TYPE_BF16 = 0, 1
+ROUTE_SOFTMAX, ROUTE_SIGMOID = 0, 1
+ROUTE_GROUP_TOP2, ROUTE_GROUP_MAX = 0, 1
 OFFSETS_STATIC_MAX_BLOCKS = 8388608          # SBITS_OFFSETS_STATIC_MAX_BLOCKS of the header
 
 EXPORTS = [
@@ -27,6 +30,8 @@ EXPORTS = [
     "sbits_gather_cost_supported", "sbits_gather_cost_all", "sbits_gather_pack_all",
     "sbits_reorder_coupled_all", "sbits_surrogates_all",
     "sbits_allocate", "sbits_propose", "sbits_offsets", "sbits_offsets_static", "sbits_pack", "sbits_search", "sbits_search_coupled", "sbits_mp_gemm", "sbits_dequant",
+    "sbits_mx_scale_pitch", "sbits_mx_out_pitch", "sbits_mx_quantize", "sbits_mx_gemm_ws_bytes", "sbits_mx_gemm",
+    "sbits_route", "sbits_route_backward", "sbits_expert_layer_ws_bytes", "sbits_expert_layer",
 ]
 
 
@@ -74,6 +79,21 @@ class Outputs(C.Structure):
                 ("scale", C.c_void_p), ("zero", C.c_void_p)]
 
 
+class Mx(C.Structure):
+    """A matrix in the microscaled 4-bit form (see mx())."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ld_codes", C.c_int64), ("ld_scales", C.c_int64)]
+
+
+class Router(C.Structure):
+    """How experts are chosen (sbits_router)."""
+    _fields_ = [("experts", C.c_int32), ("top_k", C.c_int32), ("scoring", C.c_int32), ("groups", C.c_int32),
+                ("top_groups", C.c_int32), ("group_score", C.c_int32), ("renormalize", C.c_int32)]
+
+    def __init__(self, experts, top_k, scoring=ROUTE_SOFTMAX, groups=1, top_groups=1, group_score=ROUTE_GROUP_TOP2, renormalize=True):
+        super().__init__(experts, top_k, scoring, groups, top_groups, group_score, 1 if renormalize else 0)
+
+
 class SbitsError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -99,6 +119,18 @@ def load():
             lib.sbits_workspace_bytes.restype = C.c_size_t
             lib.sbits_codes_bytes_bound.restype = C.c_int64
             lib.sbits_codes_bytes_bound.argtypes = [C.c_void_p, C.c_double]
+            # calls of a few microseconds: with their types given here, addresses and numbers go in as they are
+            p, i, n, z = C.c_void_p, C.c_int, C.c_int64, C.c_size_t
+            for name, types in (("mx_scale_pitch", [n]), ("mx_out_pitch", [n]), ("mx_quantize", [p, p, i, n, p, p, n]),
+                                ("mx_gemm_ws_bytes", [p, p, n, i, i]), ("mx_gemm", [p, p, p, n, p, n, i, p, i, n, p, z]),
+                                ("route", [p, p, p, i, n, p, n, p, p]), ("route_backward", [p, p, p, i, n, p, p, n, p, n]),
+                                ("expert_layer_ws_bytes", [p, p, n, p, p, i]),
+                                ("expert_layer", [p, p, p, i, n, p, p, n, n, p, p, p, n, p, p, i, p, z])):
+                getattr(lib, "sbits_" + name).argtypes = types
+            for name in ("sbits_mx_scale_pitch", "sbits_mx_out_pitch"):
+                getattr(lib, name).restype = n
+            for name in ("sbits_mx_gemm_ws_bytes", "sbits_expert_layer_ws_bytes"):
+                getattr(lib, name).restype = z
             _loaded[LIB_PATH] = lib
         _lib = _loaded[LIB_PATH]
     return _lib
@@ -154,6 +186,45 @@ def matrix(w, s) -> Matrix:
     return d
 
 
+def mx_scale_pitch(cols: int) -> int:
+    """Bytes between rows of a dense array of scales."""
+    return load().sbits_mx_scale_pitch(cols)
+
+
+def mx_out_pitch(rows: int) -> int:
+    """Elements between rows of a dense output with so many of them to a row."""
+    return load().sbits_mx_out_pitch(rows)
+
+
+def mx(codes, scales, cols: int) -> Mx:
+    """Descriptor of a matrix in the microscaled form: uint8 tensors of codes [rows, >= cols / 2] and scales [rows, >= pitch]."""
+    d = Mx(codes.data_ptr(), scales.data_ptr(), codes.shape[0], cols, _pitch(codes), _pitch(scales))
+    d.codes_tensor, d.scales_tensor = codes, scales       # (also keeps them alive as long as the descriptor lives)
+    return d
+
+
+def _pitch(t) -> int:
+    """Elements between the rows of a matrix whose rows are dense."""
+    row, element = t.stride()
+    if element != 1 and t.shape[1] > 1:
+        raise ValueError("rows of a tensor have to be dense")
+    return row
+
+
+def _type(t) -> int:
+    name = str(t.dtype)
+    if name == "torch.bfloat16":
+        return TYPE_BF16
+    if name == "torch.float32":
+        return TYPE_FP32
+    raise TypeError("bfloat16 or float32 expected, not " + name)
+
+
+def _is(t, name, what):
+    if str(t.dtype) != name:
+        raise TypeError("%s: %s expected, not %s" % (what, name, t.dtype))
+
+
 class Context:
     def __init__(self, device: int = 0, stream: int = 0):
         self.h = C.c_void_p()
@@ -166,6 +237,86 @@ class Context:
 
     def last_hip_error(self) -> int:
         return load().sbits_last_hip_error(self.h)
+
+    # ---- layers with 4-bit floating point weights (see scalebits.h) ---------------------
+    def mx_quantize(self, x, q: Mx, values=None):
+        """x (bf16 or fp32) to q's codes and scales; values (bf16, may be None): what they stand for."""
+        if tuple(x.shape) != (q.rows, q.cols) or (values is not None and values.shape != x.shape):
+            raise ValueError("x, q and values differ in shape")
+        if values is not None:
+            _is(values, "torch.bfloat16", "values")
+        return _check(load().sbits_mx_quantize(self.h, x.data_ptr(), _type(x), _pitch(x), C.addressof(q),
+                                               values.data_ptr() if values is not None else None,
+                                               _pitch(values) if values is not None else 0), "sbits_mx_quantize")
+
+    def mx_gemm_ws_bytes(self, w: Mx, batch: int, four_bit: bool = False, gated: bool = False) -> int:
+        return load().sbits_mx_gemm_ws_bytes(self.h, C.addressof(w), batch, 1 if four_bit else 0, 1 if gated else 0)
+
+    def mx_gemm(self, w: Mx, x, y, ws, gated: bool = False):
+        """y[b][i] = sum_j W[i][j] x[b][j] (gated: silu of the first half of W's rows times the second); x: bf16 tensor or Mx,
+        y: bf16 or fp32 [batch, rows]."""
+        batch = y.shape[0]
+        if y.shape[1] != (w.rows // 2 if gated else w.rows):
+            raise ValueError("y has %d columns, %d rows in W" % (y.shape[1], w.rows))
+        if isinstance(x, Mx):
+            bf16, ld, four = None, 0, C.addressof(x)
+        else:
+            _is(x, "torch.bfloat16", "x")
+            if tuple(x.shape) != (batch, w.cols):
+                raise ValueError("x is not [%d, %d]" % (batch, w.cols))
+            bf16, ld, four = x.data_ptr(), _pitch(x), None
+        return _check(load().sbits_mx_gemm(self.h, C.addressof(w), bf16, ld, four, batch, 1 if gated else 0, y.data_ptr(), _type(y), _pitch(y),
+                                           ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0),
+                      "sbits_mx_gemm")
+
+    def route(self, router: Router, logits, bias, ids, weights):
+        """ids (int32) and weights (fp32) [tokens, top_k] of the chosen experts; logits: bf16 or fp32 [tokens, experts], bias: fp32 or None."""
+        tokens = _routed(router, logits, bias, ids, weights)
+        return _check(load().sbits_route(self.h, C.addressof(router), logits.data_ptr(), _type(logits), _pitch(logits),
+                                         bias.data_ptr() if bias is not None else None, tokens, ids.data_ptr(), weights.data_ptr()),
+                      "sbits_route")
+
+    def route_backward(self, router: Router, logits, ids, d_weights, d_logits):
+        """d_logits (fp32 [tokens, experts]) from the gradient of the weights."""
+        tokens = _routed(router, logits, None, ids, d_weights)
+        _is(d_logits, "torch.float32", "d_logits")
+        if d_logits.shape != logits.shape:
+            raise ValueError("d_logits and logits differ in shape")
+        return _check(load().sbits_route_backward(self.h, C.addressof(router), logits.data_ptr(), _type(logits), _pitch(logits),
+                                                  ids.data_ptr(), d_weights.data_ptr(), tokens, d_logits.data_ptr(), _pitch(d_logits)),
+                      "sbits_route_backward")
+
+    def expert_layer_ws_bytes(self, router: Router, tokens: int, up: Mx, down: Mx, four_bit: bool = False) -> int:
+        return load().sbits_expert_layer_ws_bytes(self.h, C.addressof(router), tokens, C.addressof(up), C.addressof(down), 1 if four_bit else 0)
+
+    def expert_layer(self, router: Router, logits, bias, x, up: Mx, down: Mx, out, ids, weights, ws, four_bit: bool = False):
+        """out (bf16 [tokens, hidden]) = the weighted sum of the chosen experts' outputs; ids, weights: as route() writes them."""
+        tokens = _routed(router, logits, bias, ids, weights)
+        _is(x, "torch.bfloat16", "x")
+        _is(out, "torch.bfloat16", "out")
+        if tuple(x.shape) != (tokens, up.cols) or x.shape != out.shape:
+            raise ValueError("x and out are not [%d, %d]" % (tokens, up.cols))
+        return _check(load().sbits_expert_layer(self.h, C.addressof(router), logits.data_ptr(), _type(logits), _pitch(logits),
+                                                bias.data_ptr() if bias is not None else None, x.data_ptr(), _pitch(x), tokens,
+                                                C.addressof(up), C.addressof(down), out.data_ptr(), _pitch(out), ids.data_ptr(),
+                                                weights.data_ptr(), 1 if four_bit else 0, ws.data_ptr() if ws is not None else None,
+                                                ws.numel() if ws is not None else 0), "sbits_expert_layer")
+
+
+def _routed(router, logits, bias, ids, weights) -> int:
+    """Checks of what the calls around a router share; the number of tokens."""
+    tokens, experts = logits.shape
+    if experts != router.experts or ids.shape != weights.shape or tuple(ids.shape) != (tokens, router.top_k):
+        raise ValueError("logits, ids or weights do not fit the router")
+    if not (ids.is_contiguous() and weights.is_contiguous()):
+        raise ValueError("ids and weights have to be contiguous")
+    _is(ids, "torch.int32", "ids")
+    _is(weights, "torch.float32", "weights")
+    if bias is not None:
+        _is(bias, "torch.float32", "bias")
+        if tuple(bias.shape) != (experts,) or not bias.is_contiguous():
+            raise ValueError("bias is not [experts]")
+    return tokens
 
 
 class Plan:

@@ -27,7 +27,10 @@ TEST_VARIANTS = {"impatient": ["-DSBITS_SPIN_LIMIT=0"],
                  "masked": ["-DSBITS_D16_ZERO_FILL=0"],
                  "noretry": ["-DSBITS_SECOND_TRY=0"]}
 ONLY = {v: ["api.hip" if v == "masked" else "alloc.hip"] for v in TEST_VARIANTS}       # sources a variant compiles anew; the rest are the default build's objects
-SOURCES = ["api.hip", "reorder.hip", "cost.hip", "fused.hip", "fused_copies.hip", "fused_wide.hip", "alloc.hip", "pack.hip", "mpgemm.hip", "dequant.hip"]
+SOURCES = ["api.hip", "reorder.hip", "cost.hip", "fused.hip", "fused_copies.hip", "fused_wide.hip", "alloc.hip", "pack.hip", "mpgemm.hip", "dequant.hip",
+           "mx.hip", "mxgemm.hip", "route.hip", "layers.hip"]
+# sources whose inputs may hold NaN
+HONOR_NANS = {"mx.hip", "mxgemm.hip", "route.hip", "layers.hip"}
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -51,7 +54,8 @@ def _compile(src: str, force: bool, variant: str) -> str:
     deps.append(os.path.join(INCLUDE, "scalebits.h"))
     if not force and os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(d) for d in deps):
         return obj
-    cmd = [HIPCC, *FLAGS, *{**VARIANTS, **TEST_VARIANTS}[variant], "-c", os.path.join(CSRC, src), "-o", obj]
+    nans = ["-Xarch_device", "-fhonor-nans"] if src in HONOR_NANS else []
+    cmd = [HIPCC, *FLAGS, *nans, *{**VARIANTS, **TEST_VARIANTS}[variant], "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:
         sys.stderr.write(r.stdout)

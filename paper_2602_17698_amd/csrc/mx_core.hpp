@@ -1,0 +1,102 @@
+// Layers with 4-bit floating point weights: declarations shared by their kernels (mx.hip, mxgemm.hip, route.hip) and entry points
+// (layers.hip), and device helpers.  These sources are compiled with NaN and infinities honoured.
+#pragma once
+
+#include "sbits_internal.hpp"
+
+namespace sbits {
+
+constexpr int MX_BLOCK = 32;                 // values that share a power of two
+constexpr int MAX_EXPERTS = 512, MAX_TOP_K = 32, MAX_GROUPS = 64;
+constexpr int64_t MX_MAX_COLS = 1 << 24;     // a row's bytes and a tile's stay within 32-bit offsets
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+
+// fp32 to bf16, nearest even, NaN stays NaN
+__device__ __forceinline__ uint32_t bf16_round(float v)
+{
+    const __bf16 h = (__bf16)v;
+    return __builtin_bit_cast(unsigned short, h);
+}
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b)
+{
+    const bf16x2 h = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, h);
+}
+
+// The power of two of a block from the bits of its largest magnitude: 2^(exponent - 2), at least 2^-125; 255 for a block
+// that is not finite (its bits, as a whole number, are then the largest of the block).
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t largest)
+{
+    const uint32_t e = largest >> 23;
+    return e >= 255 ? 255u : (e < 4 ? 4u : e) - 2u;
+}
+// Codes of 8 values.  The conversion divides by the power of two, rounds to nearest even and saturates, subnormal values included
+// (checked for every power and for all borders between codes).
+__device__ __forceinline__ uint32_t mx_codes8(const float (&v)[8], uint32_t byte)
+{
+    const float scale = __uint_as_float(byte << 23);
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+    return byte == 255 ? 0u : c;
+}
+// The values of 8 codes in bf16, exact but below 2^-133 (the conversion takes the exponent's bits of the scale: 0 is 2^-127, 255 NaN).
+__device__ __forceinline__ u32x4 mx_values8(uint32_t codes, float scale)
+{
+    u32x4 v;
+    v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+    v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+    v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+    v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    return v;
+}
+
+__device__ __forceinline__ float silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+
+// One set of rows of x against one matrix of a stack: rows first .. first + count - 1 of the sorted list, matrix `expert`.
+struct MxTile { int expert, first, count, pad_; };
+
+struct MxGemm {
+    const uint8_t *w, *ws;          // codes and scales of the (first) matrix
+    int64_t ld_w, ld_ws;            // pitches in bytes
+    int64_t w_rows;                 // rows of one matrix (of both halves where gated)
+    int outs;                       // outputs of a row: w_rows, or half of them
+    int cols;
+    const void *x;                  // bf16, or codes
+    const uint8_t *xs;              // scales of x, or null
+    int64_t ld_x, ld_xs;            // pitches in bytes
+    void *y;
+    int64_t ld_y;                   // elements
+    int y_bf16, gated;
+    int64_t batch;
+    // a stack of matrices: tiles (n_tiles of them at most, with count 0 where there are none), the rows of x (x_row[s] / x_div) and of y
+    // (y_row[s]) of a place in the sorted list; null: the place itself
+    const MxTile *tiles;
+    int n_tiles, tile_rows;
+    const int *x_row, *y_row;
+    int x_div;
+};
+
+}  // namespace sbits
+
+// ---- launchers --------------------------------------------------------------
+int sbits_launch_mx_quantize(sbits_ctx *ctx, const void *x, bool bf16, int64_t ld_x, const sbits_mx &q, int64_t rows, void *values, int64_t ld_v);
+int sbits_mx_tile_rows(const sbits_ctx *ctx, int64_t rows_per_matrix, bool four_bit);
+int sbits_launch_mx_gemm(sbits_ctx *ctx, const sbits::MxGemm &g);
+int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const float *bias, int64_t tokens,
+                       int32_t *ids, float *weights);
+int sbits_launch_route_backward(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const int32_t *ids,
+                                const float *d_weights, int64_t tokens, float *d_logits, int64_t ld_d);
+int sbits_launch_expert_lists(sbits_ctx *ctx, const int32_t *ids, int n, int experts, int tile_rows, int max_tiles, int *sorted,
+                              sbits::MxTile *tiles);
+int sbits_launch_combine(sbits_ctx *ctx, const void *y, int64_t ld_y, const int32_t *ids, const float *weights, int64_t tokens, int top_k,
+                         int hidden, void *out, int64_t ld_out);

@@ -1,0 +1,213 @@
+"""Microscaled 4-bit form on the GPU: quantisation bit for bit, products against 64 bits."""
+import math
+
+import pytest
+import torch
+
+import mx_plain as mp
+from paper_2602_17698_amd import binding as sb
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = sb.Context(0, torch.cuda.current_stream().cuda_stream)
+    yield c
+    c.close()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def quantise_on_gpu(ctx, x, with_values=True, extra=0):
+    rows, cols = x.shape
+    codes = torch.full((rows, cols // 2 + 16 * extra), 0xa5, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows, sb.mx_scale_pitch(cols) + 4 * extra), 0xa5, dtype=torch.uint8, device="cuda")
+    values = torch.zeros(rows, cols + 8 * extra, dtype=torch.bfloat16, device="cuda")[:, :cols] if with_values else None
+    q = sb.mx(codes, scales, cols)
+    ctx.mx_quantize(x, q, values)
+    torch.cuda.synchronize()
+    assert bool((codes[:, cols // 2:] == 0xa5).all()) and bool((scales[:, cols // 32:] == 0xa5).all())
+    return codes[:, :cols // 2].cpu(), scales[:, :cols // 32].cpu(), values.cpu() if with_values else None
+
+
+def check_quantised(ctx, x, **k):
+    codes, bytes_, values = quantise_on_gpu(ctx, x, **k)
+    code, byte = mp.quantise(x.cpu())
+    assert torch.equal(bytes_, byte)
+    assert torch.equal(mp.unpack(codes), code)
+    if values is not None:
+        want = mp.values(code, byte).to(torch.bfloat16)
+        assert torch.equal(torch.nan_to_num(values.float(), nan=7e37), torch.nan_to_num(want.float(), nan=7e37))
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols,extra", [(1, 32, 0), (1, 4096, 0), (3, 96, 1), (37, 1056, 2), (257, 160, 0), (5, 28672, 0)])
+def test_quantise_rows(ctx, rows, cols, extra, kind):
+    x = (torch.randn(rows, cols + 8 * extra, generator=gen(rows)) * torch.exp(3 * torch.randn(rows, 1, generator=gen(cols)))).to(kind).cuda()
+    check_quantised(ctx, x[:, :cols], extra=extra)
+    check_quantised(ctx, x[:, :cols], with_values=False)
+
+
+def test_quantise_borders_and_broken_blocks(ctx):
+    """Every border between codes at many powers of two, both neighbours of each; subnormal blocks, zeros of both signs, blocks with NaN, infinities
+    and the largest numbers."""
+    rows = []
+    for power in (-149, -140, -128, -126, -125, -124, -100, -3, 0, 5, 60, 124, 125):
+        edge = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 7.9, 4.0, 0.5, 1.0, 1.5, 2.0, 3.0], dtype=torch.float64) * 2.0 ** power
+        edge = edge.clamp(max=3.0e38).float()
+        up, down = torch.nextafter(edge, torch.tensor(math.inf)), torch.nextafter(edge, torch.tensor(0.0))
+        for v in (edge, up, down):
+            lead = torch.tensor(min(7.5 * 2.0 ** power, 3.3e38))
+            block = torch.cat((lead[None], v[:15], -v))
+            rows.append(torch.where(torch.isfinite(block), block, 1.0))
+    plain = torch.linspace(-4, 4, 32)
+    for at, v in ((0, math.nan), (31, math.nan), (7, math.inf), (8, -math.inf), (16, 3.4028234663852886e38), (5, 1e-45)):
+        b = plain.clone()
+        b[at] = v
+        rows.append(b)
+    rows += [torch.zeros(32), -torch.zeros(32), torch.full((32,), 1e-45), torch.full((32,), -0.0)]
+    x = torch.stack(rows).cuda()
+    check_quantised(ctx, x)
+    check_quantised(ctx, x.flatten().view(1, -1))
+    check_quantised(ctx, x.to(torch.bfloat16))
+
+
+# ---- products --------------------------------------------------------------------------------------
+# batches on both sides of the lines between kernels and tiles, outputs that end inside a tile, runs of columns that end inside one
+SHAPES = [(1, 8, 32), (1, 250, 256), (2, 33, 96), (15, 64, 128), (16, 31, 160), (17, 100, 512), (31, 257, 288), (33, 64, 1056), (48, 130, 544), (64, 96, 2080),
+          (65, 250, 320), (97, 256, 576), (128, 514, 256), (129, 300, 352), (200, 129, 1120), (255, 513, 64), (256, 256, 32), (257, 258, 608), (300, 700, 800)]
+
+
+def check_product(ctx, batch, rows, cols, four, gated, out, extra=0, seed=0, spread=3):
+    g = gen(seed + 31 * batch + rows)
+    code, byte = mp.random_matrix(rows * (2 if gated else 1), cols, g, spread)
+    x = torch.randn(batch, cols + 8 * extra, generator=g).to(torch.bfloat16)
+    w = sb.mx(*mp.stored(code, byte, "cuda", extra))
+    if four:
+        xc, xb = mp.quantise(x[:, :cols])
+        xs, xd = mp.values(xc, xb), sb.mx(*mp.stored(xc, xb, "cuda", extra))
+    else:
+        xs, xd = x[:, :cols].double(), x.cuda()[:, :cols]
+    y = torch.full((batch, sb.mx_out_pitch(rows) + 8 * extra), 7.0, dtype=out, device="cuda")
+    ws = torch.full((max(256, ctx.mx_gemm_ws_bytes(w, batch, four, gated)),), 0xff, dtype=torch.uint8, device="cuda")
+    print("[case]", batch, rows, cols, four, gated, out, flush=True)
+    ctx.mx_gemm(w, xd, y[:, :rows], ws, gated=gated)
+    torch.cuda.synchronize()
+    want, off = mp.product(xs, mp.values(code, byte), gated)
+    if out == torch.bfloat16:
+        off = off + 2.0 ** -8 * (want.abs() + off)
+    else:
+        off = off + 2.0 ** -24 * (want.abs() + off)
+    got = y.cpu().double()
+    assert bool(((got[:, :rows] - want).abs() <= off).all()), float(((got[:, :rows] - want).abs() / off).max())
+    assert bool((got[:, rows:] == 7.0).all())
+    first = y.clone()
+    ctx.mx_gemm(w, xd, y[:, :rows], ws, gated=gated)
+    assert torch.equal(first, y)                                     # the same bits again
+
+
+@pytest.mark.parametrize("batch,rows,cols", SHAPES)
+@pytest.mark.parametrize("four,gated,out", [(False, False, torch.float32), (False, True, torch.bfloat16), (True, False, torch.bfloat16),
+                                            (True, True, torch.float32)])
+def test_product(ctx, batch, rows, cols, four, gated, out):
+    check_product(ctx, batch, rows, cols, four, gated, out)
+
+
+@pytest.mark.parametrize("batch", [1, 20, 70, 260])
+@pytest.mark.parametrize("four", [False, True])
+def test_product_of_strided_matrices(ctx, batch, four):
+    check_product(ctx, batch, 120, 352, four, True, torch.bfloat16, extra=1, seed=1)
+    check_product(ctx, batch, 520, 96, four, False, torch.float32, extra=3, seed=2)
+
+
+@pytest.mark.parametrize("batch", [3, 300])
+@pytest.mark.parametrize("four", [False, True])
+def test_product_with_far_powers(ctx, batch, four):
+    """Powers of two from 2^-67 to 2^53 side by side: products far apart in size, none beyond fp32."""
+    check_product(ctx, batch, 70, 256, four, False, torch.float32, seed=3, spread=60)
+
+
+@pytest.mark.parametrize("batch", [2, 300])
+@pytest.mark.parametrize("four", [False, True])
+def test_broken_blocks_stay_in_their_outputs(ctx, batch, four):
+    """A block of W with the byte 255 makes its output row NaN, an infinite x or a broken block of x its row of y; the others are as without."""
+    rows, cols = 300, 416
+    g = gen(5)
+    code, byte = mp.random_matrix(rows, cols, g)
+    x = torch.randn(batch, cols, generator=g).to(torch.bfloat16)
+    def run(byte, x):
+        w = sb.mx(*mp.stored(code, byte, "cuda"))
+        xd = sb.mx(*mp.stored(*mp.quantise(x), "cuda")) if four else x.cuda()
+        y = torch.empty(batch, sb.mx_out_pitch(rows), device="cuda")
+        ctx.mx_gemm(w, xd, y[:, :rows], None)
+        return y[:, :rows].cpu()
+    good = run(byte, x)
+    byte2, x2 = byte.clone(), x.clone()
+    byte2[17, 12], byte2[299, 0], x2[1, 415] = 255, 255, math.nan
+    bad = run(byte2, x2)
+    hit = torch.zeros(batch, rows, dtype=torch.bool)
+    hit[:, 17] = hit[:, 299] = True
+    hit[1] = True
+    assert bool(torch.isnan(bad[hit]).all())
+    assert torch.equal(bad[~hit], good[~hit])
+
+
+@pytest.mark.parametrize("byte", [0, 1, 254])
+def test_product_at_the_ends_of_the_powers(ctx, byte):
+    """2^-127, 2^-126 and 2^127 with x that brings the products back into range; values beyond bfloat16's range count as infinite."""
+    code = torch.arange(32 * 32).view(32, 32).remainder(16).to(torch.uint8)
+    b = torch.full((32, 1), byte, dtype=torch.uint8)
+    x = (torch.randn(4, 32, generator=gen(0)) * 2.0 ** (60 if byte < 2 else -100)).to(torch.bfloat16)
+    y = torch.empty(4, 32, device="cuda")
+    ctx.mx_gemm(sb.mx(*mp.stored(code, b, "cuda")), x.cuda(), y, None)
+    want, off = mp.product(x.double(), mp.values(code, b).to(torch.bfloat16).double(), False)
+    got, fine = y.cpu().double(), torch.isfinite(want)
+    assert bool(((got - want).abs() <= off)[fine].all())
+    assert torch.equal(torch.nan_to_num(got[~fine], nan=5.0), torch.nan_to_num(want[~fine], nan=5.0)) and bool(fine.all()) == (byte < 2)
+
+
+def test_product_and_quantisation_in_a_graph(ctx):
+    """Captured on a stream of their own, replayed with eager calls in between, each replay as the eager call."""
+    side = torch.cuda.Stream()
+    own = sb.Context(0, side.cuda_stream)
+    g = gen(9)
+    jobs = []
+    for batch, rows, cols in ((3, 100, 256), (40, 96, 544), (300, 300, 288)):
+        code, byte = mp.random_matrix(rows, cols, g)
+        w = sb.mx(*mp.stored(code, byte, "cuda"))
+        x = torch.randn(batch, cols, generator=g).to(torch.bfloat16).cuda()
+        q = sb.mx(torch.empty(batch, cols // 2, dtype=torch.uint8, device="cuda"),
+                  torch.empty(batch, sb.mx_scale_pitch(cols), dtype=torch.uint8, device="cuda"), cols)
+        ws = torch.empty(max(256, own.mx_gemm_ws_bytes(w, batch, True)) + own.mx_gemm_ws_bytes(w, batch), dtype=torch.uint8, device="cuda")
+        jobs.append((w, x, q, ws, torch.empty(batch, sb.mx_out_pitch(rows), device="cuda")[:, :rows],
+                     torch.empty(batch, sb.mx_out_pitch(rows), device="cuda")[:, :rows]))
+    def calls(c):
+        for w, x, q, ws, y4, y16 in jobs:
+            c.mx_quantize(x, q)
+            c.mx_gemm(w, q, y4, ws)
+            c.mx_gemm(w, x, y16, ws)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        calls(own)
+        graph = torch.cuda.CUDAGraph()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            calls(own)
+    for turn in range(4):
+        for w, x, q, ws, y4, y16 in jobs:
+            x.copy_(torch.randn(x.shape, generator=g).to(torch.bfloat16))
+            y4.zero_(), y16.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [(a.clone(), b.clone()) for *_, a, b in jobs]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            calls(own)
+        torch.cuda.synchronize()
+        for (a, b), (*_, y4, y16) in zip(replayed, jobs):
+            assert torch.equal(a, y4) and torch.equal(b, y16), turn
+    own.close()
