@@ -1,4 +1,6 @@
 // C-ABI entry points of the layers with 4-bit floating point weights: argument validation, the workspace's layout, the sequence of kernels.
+#include <algorithm>
+
 #include "mx_core.hpp"
 
 using namespace sbits;
@@ -47,22 +49,25 @@ struct LayerSpace {
     int64_t codes_x, scales_x, codes_h, scales_h;                  // pitches
     size_t sorted, tiles, h, y, xq, xs, hq, hs, bytes;
 };
-static LayerSpace layer_space(const sbits_ctx *ctx, const sbits_router &r, int64_t tokens, const sbits_mx &up, const sbits_mx &down, bool four)
+static LayerSpace layer_space(const sbits_router &r, int64_t tokens, const sbits_mx &up, const sbits_mx &down, bool four, int64_t ld_x)
 {
     LayerSpace s;
     s.tokens = tokens;
     s.places = tokens * r.top_k;
     s.hidden = up.cols;
     s.inner = down.cols;
-    s.tile_rows = sbits_mx_tile_rows(ctx, (s.places + r.experts - 1) / r.experts, four);
-    const int64_t tiles = r.experts + s.places / s.tile_rows;
-    s.max_tiles = (int)(tiles < s.places ? tiles : s.places);
+    // (space for as many tiles as there are at most, however far apart the rows of x lie)
+    const int64_t rows = (s.places + r.experts - 1) / r.experts;
+    s.tile_rows = sbits_mx_tile_rows(rows, std::max(2 * s.inner * std::max(up.ld_codes, up.ld_scales), s.hidden * std::max(down.ld_codes, down.ld_scales)),
+                                     std::max(tokens * ld_x, 512 * s.inner));
+    auto tiles = [&](int tile_rows) { return std::min(r.experts + s.places / tile_rows, s.places); };
+    s.max_tiles = (int)tiles(s.tile_rows);
     s.codes_x = s.hidden / 2; s.scales_x = sbits_mx_scale_pitch(s.hidden);
     s.codes_h = s.inner / 2; s.scales_h = sbits_mx_scale_pitch(s.inner);
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)up_to(bytes, 256); return here; };
     s.sorted = take(s.places * 4);
-    s.tiles = take((int64_t)s.max_tiles * (int64_t)sizeof(MxTile));
+    s.tiles = take(tiles(std::min(s.tile_rows, 64)) * (int64_t)sizeof(MxTile));
     s.h = take(s.places * s.inner * 2);
     s.y = take(s.places * s.hidden * 2);
     s.xq = take(four ? tokens * s.codes_x : 0);
@@ -134,7 +139,7 @@ int sbits_mx_gemm(sbits_ctx *ctx, const sbits_mx *w, const void *x_bf16, int64_t
     g.ld_xs = x_mx ? x_mx->ld_scales : 0;
     g.y = y; g.ld_y = ld_y; g.y_bf16 = y_type == SBITS_TYPE_BF16; g.gated = gated;
     g.batch = batch;
-    g.tile_rows = sbits_mx_tile_rows(ctx, batch, x_mx != nullptr);
+    g.tile_rows = sbits_mx_tile_rows(batch, w->rows * std::max(w->ld_codes, w->ld_scales), 256 * std::max(g.ld_x, g.ld_xs));
     return sbits_launch_mx_gemm(ctx, g);
 }
 
@@ -167,7 +172,7 @@ int sbits_route_backward(sbits_ctx *ctx, const sbits_router *r, const void *logi
 size_t sbits_expert_layer_ws_bytes(const sbits_ctx *ctx, const sbits_router *r, int64_t tokens, const sbits_mx *up, const sbits_mx *down,
                                    int four_bit)
 {
-    return check_layer(ctx, r, tokens, up, down) ? 0 : layer_space(ctx, *r, tokens, *up, *down, four_bit != 0).bytes;
+    return check_layer(ctx, r, tokens, up, down) ? 0 : layer_space(*r, tokens, *up, *down, four_bit != 0, 0).bytes;
 }
 
 int sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits, int logits_type, int64_t ld_logits, const float *bias,
@@ -181,7 +186,7 @@ int sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits
     if ((bias && !aligned(bias, 4)) || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(x_bf16, 16) || !pitch(ld_x, up->cols, 8) ||
         !aligned(out_bf16, 16) || !pitch(ld_out, up->cols, 8))
         return SBITS_ERR_INVALID_ARG;
-    const LayerSpace s = layer_space(ctx, *r, tokens, *up, *down, four_bit != 0);
+    const LayerSpace s = layer_space(*r, tokens, *up, *down, four_bit != 0, four_bit ? up->cols / 2 : 2 * ld_x);
     if (!ws_ok(ws, ws_bytes, s.bytes)) return SBITS_ERR_WORKSPACE;
     if ((rc = need_device(ctx))) return rc;
     char *const base = static_cast<char *>(ws);

@@ -90,8 +90,9 @@ struct MxGemm {
 
 // ---- launchers --------------------------------------------------------------
 int sbits_launch_mx_quantize(sbits_ctx *ctx, const void *x, bool bf16, int64_t ld_x, const sbits_mx &q, int64_t rows, void *values, int64_t ld_v);
-int sbits_mx_tile_rows(const sbits_ctx *ctx, int64_t rows_per_matrix, bool four_bit);
+int sbits_mx_tile_rows(int64_t rows_per_matrix, int64_t w_bytes, int64_t x_bytes);
 int sbits_launch_mx_gemm(sbits_ctx *ctx, const sbits::MxGemm &g);
+int sbits_launch_mx_gemm_many(sbits_ctx *ctx, const sbits::MxGemm &g);
 int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const float *bias, int64_t tokens,
                        int32_t *ids, float *weights);
 int sbits_launch_route_backward(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const int32_t *ids,

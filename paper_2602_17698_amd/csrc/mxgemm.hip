@@ -118,9 +118,12 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx_gemm_few_kernel(MxGemm g)
 
 using namespace sbits;
 
-// rows of x to a tile, for so many rows to a matrix (on average)
-int sbits_mx_tile_rows(const sbits_ctx *, int64_t rows_per_matrix, bool)
+// Rows of x to a tile, for so many rows to a matrix (on average), and the bytes that offsets of a tile have to span: from the first row of a
+// matrix to its last, and from the first row of x that a tile may read to the last.  The kernel of many rows has offsets of 31 bits.
+int sbits_mx_tile_rows(int64_t rows_per_matrix, int64_t w_bytes, int64_t x_bytes)
 {
+    const bool near = w_bytes < ((int64_t)1 << 31) && x_bytes < ((int64_t)1 << 31);
+    if (near && rows_per_matrix > 64) return rows_per_matrix > 128 ? 256 : 128;
     return rows_per_matrix <= 16 ? 16 : rows_per_matrix <= 32 ? 32 : 64;
 }
 
@@ -132,6 +135,7 @@ static auto few_instance(int rows)
 
 int sbits_launch_mx_gemm(sbits_ctx *ctx, const MxGemm &g)
 {
+    if (g.tile_rows > 64) return sbits_launch_mx_gemm_many(ctx, g);
     const bool x4 = g.xs != nullptr;
     const int tiles = g.tiles ? g.n_tiles : (int)((g.batch + g.tile_rows - 1) / g.tile_rows);
     auto fn = x4 ? (g.gated ? few_instance<true, true>(g.tile_rows) : few_instance<true, false>(g.tile_rows))
