@@ -1,15 +1,18 @@
 // Products of many rows of x with matrices in the microscaled 4-bit form (see mxgemm.hip), by tiles that fill a CU.
 //
-// A workgroup of 4 waves takes 64 MT rows of x and 64 NT rows of W, a wave MT x NT tiles of 32 x 32.  Both operands come into LDS by
-// direct loads, 16 bytes a lane, several steps ahead of their use; a step is 128 columns with x in 4 bits and 64 with x in bf16.  The first
-// operands of a step are read from LDS during the one before, so that the matrix cores go on across the barrier between them.
+// A workgroup of 4 waves takes 64 MT rows of x and 64 NT rows of W, a wave MT x NT tiles of 32 x 32.  A step is 256 columns with x in 4 bits, 64 with
+// x in bf16, 128 bytes of a row of x either way; four phases of MT NT matrix instructions.  W comes in chunks of 256 columns, 128 bytes of a
+// row, too: a load of fewer neighbouring bytes is a request to L2 all the same, and requests were the bound (8192 x 14336 x 4096 in 4 bits, 64 bytes
+// a row and step: 346 us).  Both go to LDS by direct loads, two buffers each, and scales for 1024 columns at a time.
+// The barrier of a step is ahead of its last phase: the operands of that phase are in registers by then, so the step's buffers may be
+// filled again, the next step is there, and its first operands are read during the last phase.
 //
 // Order of the columns: lane l of an instruction has row l % 32 of a tile and, by h = l / 32, one of two halves of the columns.  Any order will do
-// that both operands share; here the halves are whole blocks (x in 4 bits: blocks 2 h + ks of the step in instruction ks; x in bf16: block h,
-// 8 columns an instruction), so that a lane's scales are neighbours.
+// that both operands share; here phase q has piece 4 h + q of the 8 pieces of 16 bytes of a step (x in 4 bits: a block; x in bf16: 8 columns), so
+// that a lane's scales are neighbours.
 // Order of W's rows: tile t of a wave has rows NT n + t, n = l % 32, so that a lane's outputs for a row of x are NT neighbours, a wave's 32 NT.
 // With gated products tiles 2 p and 2 p + 1 are rows NT / 2 n + p of both halves of W.
-// LDS: the 16-byte pieces of a row are permuted (xor) by bits of the row's number, so that 16 rows of one piece lie in different banks.
+// LDS: the pieces of a row are permuted (xor) by bits of the row's number, so that 16 rows of one piece lie in different banks.
 #include "mx_core.hpp"
 
 namespace sbits {
@@ -17,11 +20,13 @@ namespace sbits {
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 constexpr uint32_t NOWHERE = 0x80000000u;          // an offset that is out of every buffer's range: zeros are loaded
 
-// 16 bytes a lane to LDS, at lds + 16 * lane.  (The builtin for it makes the compiler wait for all of them before any read of LDS;
-// the waits are this file's own.  Nothing else here uses m0.)
-__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t at, rsrc_t from, uint32_t plus)
+// 16 bytes a lane to LDS, at m0 + OFF + 16 * lane, from the buffer at OFF + at + plus.  (The builtin for it makes the compiler wait for all of
+// them before any read of LDS; the waits are this file's own.  Nothing else here uses m0.)
+__device__ __forceinline__ void set_m0(uint32_t lds) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(lds) : "memory"); }
+template <int OFF>
+__device__ __forceinline__ void load_to_lds(uint32_t at, rsrc_t from, uint32_t plus)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(at), "s"(from), "s"(plus) : "memory");
+    asm volatile("buffer_load_dwordx4 %0, %1, %2 offen offset:%3 lds" ::"v"(at), "s"(from), "s"(plus), "n"(OFF) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_and_meet()
@@ -29,35 +34,26 @@ __device__ __forceinline__ void wait_and_meet()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-template <bool X4>
-struct Step {
-    static constexpr int COLS = X4 ? 128 : 64;                     // columns
-    static constexpr int XB = X4 ? 64 : 128, WB = COLS / 2;        // bytes of a row
-    static constexpr int XP = XB / 16, WP = WB / 16;               // pieces of a row
-    static constexpr int DEEP = X4 ? 4 : 3;                        // steps in LDS
-    static constexpr int RUN = 512 / COLS;                         // steps that 16 bytes of scales are for
-    // where piece p of a row lies
-    static __device__ __forceinline__ int x_piece(int slot, int p) { return X4 ? p ^ (slot >> 2 & 3) : p ^ (slot >> 1 & 7); }
-    static __device__ __forceinline__ int w_piece(int slot, int p) { return X4 ? p ^ (slot >> 2 & 3) : p ^ (slot >> 3 & 1); }
-};
+constexpr int CHUNK = 256, RUN = 1024;             // columns of a chunk of W, of a run of scales
+constexpr int ROW = 128, PIECES = 8;               // bytes, pieces of a row of a step of x or a chunk of W
+constexpr int SCALE_ROW = RUN / MX_BLOCK;          // bytes of a row of scales
+__device__ __forceinline__ int piece_at(int slot, int p) { return p ^ (slot >> 1 & 7); }       // where piece p of a row lies, and what lies there
 
 template <bool X4, int MT, int NT>
-constexpr int many_lds()
-{
-    using S = Step<X4>;
-    return S::DEEP * 64 * (MT * S::XB + NT * S::WB) + 2 * 64 * 16 * (NT + (X4 ? MT : 0));
-}
+constexpr int many_lds() { return 2 * 64 * ((MT + NT) * ROW + (NT + (X4 ? MT : 0)) * SCALE_ROW); }
 
 template <bool X4, bool GATED, int MT, int NT>
 __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
 {
-    using S = Step<X4>;
+    constexpr int COLS = X4 ? 256 : 64;                            // of a step
     constexpr int XROWS = 64 * MT, WROWS = 64 * NT, OUTS = GATED ? WROWS / 2 : WROWS;
-    constexpr int XBYTES = XROWS * S::XB, WBYTES = WROWS * S::WB, BUFFER = XBYTES + WBYTES;
-    constexpr int XL = XBYTES / 4096, WL = WBYTES / 4096;          // a wave's loads of a step
+    constexpr int XBYTES = XROWS * ROW, WBYTES = WROWS * ROW;
+    constexpr int WSTEPS = CHUNK / COLS;                           // steps of a chunk of W
+    constexpr int XL = XBYTES / 4096, WL = WBYTES / 4096, LOADS = XL + WL / WSTEPS;        // a wave's loads of a step of x, of a chunk of W; in a step
     constexpr int SROWS = WROWS + (X4 ? XROWS : 0);                // rows with scales: W's, then x's
-    constexpr int SLOADS = SROWS / 64, SL = (SLOADS + 3) / 4;      // loads of them, for a run of steps; a wave's
-    static_assert(XBYTES % 4096 == 0 && WBYTES % 4096 == 0 && SROWS % 64 == 0, "whole loads");
+    constexpr int SLOADS = SROWS * SCALE_ROW / 1024, SL = (SLOADS + 3) / 4;                // loads of a run of them; a wave's
+    constexpr int W_AT = 2 * XBYTES, S_AT = W_AT + 2 * WBYTES;     // in LDS, behind two buffers of x
+    static_assert(WL % WSTEPS == 0, "as many loads in every step");
     extern __shared__ unsigned char smem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -81,10 +77,12 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     const int out0 = wt * OUTS;
 
     // Where a lane's loads come from: offsets into buffers that begin at the tile's first row of x (with a list of rows: at the first of
-    // all) and at the matrix.  Rows and columns that are not there: NOWHERE.
+    // all) and at the matrix.  Rows and columns that are not there: NOWHERE.  Four loads share an address in LDS and have offsets 0 .. LAST, which count for
+    // the memory's address, too: buffers begin LAST bytes ahead, and the offsets here take the load's own away.
+    constexpr int LAST = 3 * 1024;
     const int64_t x_first = g.x_row ? 0 : t.first, w_first = (int64_t)t.expert * g.w_rows;
-    const rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(static_cast<const uint8_t *>(g.x) + x_first * g.ld_x), 0, 0x7fffffff, 0x00027000);
-    const rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.w + w_first * g.ld_w), 0, 0x7fffffff, 0x00027000);
+    const rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(static_cast<const uint8_t *>(g.x) + x_first * g.ld_x - LAST), 0, 0x7fffffff, 0x00027000);
+    const rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.w + w_first * g.ld_w - LAST), 0, 0x7fffffff, 0x00027000);
     const uint8_t *const scales_w = g.ws + w_first * g.ld_ws;
     const uint8_t *const scales_x = X4 ? g.xs + x_first * g.ld_xs : nullptr;
     auto x_row = [&](int slot) -> int { return slot >= t.count ? -1 : g.x_row ? g.x_row[t.first + slot] / g.x_div : slot; };
@@ -93,73 +91,74 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
         const int out = out0 + (GATED ? w * 16 * NT + n * (NT / 2) + tile / 2 : w * 32 * NT + n * NT + tile);
         return out >= g.outs ? -1 : GATED && (tile & 1) ? g.outs + out : out;
     };
-    auto x_slot = [&](int i) { return (wave * XL + i) * (64 / S::XP) + lane / S::XP; };
-    auto w_slot = [&](int i) { return (wave * WL + i) * (64 / S::WP) + lane / S::WP; };
+    auto x_slot = [&](int i) { return (wave * XL + i) * 8 + lane / 8; };
+    auto w_slot = [&](int i) { return (wave * WL + i) * 8 + lane / 8; };
     uint32_t x_at[XL], w_at[WL], s_at[SL];
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
         const int row = x_row(x_slot(i));
-        x_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * g.ld_x) + 16 * S::x_piece(x_slot(i), lane % S::XP);
+        x_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * g.ld_x) + 16 * piece_at(x_slot(i), lane % 8) + LAST - 1024 * (i & 3);
     }
 #pragma unroll
     for (int i = 0; i < WL; ++i) {
         const int row = w_row(w_slot(i));
-        w_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * g.ld_w) + 16 * S::w_piece(w_slot(i), lane % S::WP);
+        w_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * g.ld_w) + 16 * piece_at(w_slot(i), lane % 8) + LAST - 1024 * (i & 3);
     }
+    auto s_slot = [&](int i) { return (wave + 4 * i) * 32 + lane / 2; };
 #pragma unroll
     for (int i = 0; i < SL; ++i) {
-        const int slot = (wave + 4 * i) * 64 + lane;
+        const int slot = s_slot(i);
         const int row = slot < WROWS ? w_row(slot) : slot < SROWS ? x_row(slot - WROWS) : -1;
-        s_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * (slot < WROWS ? g.ld_ws : g.ld_xs));
+        s_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * (slot < WROWS ? g.ld_ws : g.ld_xs)) + 16 * (lane % 2);
     }
-    const int steps = (g.cols + S::COLS - 1) / S::COLS;
+    const int steps = (g.cols + COLS - 1) / COLS;
 
-    auto fetch = [&](int step) {                                   // (as many loads in every step, also behind the last)
-        const uint32_t to = lds + (uint32_t)(step % S::DEEP) * BUFFER + (uint32_t)wave * (XL * 1024);
-        const uint32_t to_w = lds + (uint32_t)(step % S::DEEP) * BUFFER + XBYTES + (uint32_t)wave * (WL * 1024);
-        const int left = g.cols - step * S::COLS;
-        if (left >= S::COLS) {
-#pragma unroll
-            for (int i = 0; i < XL; ++i) load_to_lds(to + 1024 * i, x_at[i], xr, (uint32_t)step * S::XB);
-#pragma unroll
-            for (int i = 0; i < WL; ++i) load_to_lds(to_w + 1024 * i, w_at[i], wr, (uint32_t)step * S::WB);
-        } else {
-            constexpr int XC = S::COLS / S::XP, WC = S::COLS / S::WP;                       // columns of a piece
-#pragma unroll
-            for (int i = 0; i < XL; ++i)
-                load_to_lds(to + 1024 * i, S::x_piece(x_slot(i), lane % S::XP) * XC < left ? x_at[i] : NOWHERE, xr, (uint32_t)step * S::XB);
-#pragma unroll
-            for (int i = 0; i < WL; ++i)
-                load_to_lds(to_w + 1024 * i, S::w_piece(w_slot(i), lane % S::WP) * WC < left ? w_at[i] : NOWHERE, wr, (uint32_t)step * S::WB);
-        }
+    // Loads of a step, the first XL x's, then the step's share of the next chunk of W.  Pieces behind the last column go NOWHERE: a comparison with
+    // every load, as a branch would part the matrix instructions around it.
+    static_assert(XL % 2 == 0 && WL % 2 == 0, "a lane's piece goes by the load's number's lowest bit");
+    const int piece[2] = {piece_at(lane / 8, lane % 8), piece_at(8 + lane / 8, lane % 8)};
+    // (begin: the first of the four, or of a phase's)
+    auto fetch_x = [&](int step, auto i_, bool begin) {
+        constexpr int i = decltype(i_)::value;
+        const uint32_t at = piece[i & 1] * (COLS / PIECES) < g.cols - step * COLS ? x_at[i] : NOWHERE;
+        if (begin || i % 4 == 0) set_m0(lds + (uint32_t)(step & 1) * XBYTES + (uint32_t)wave * (XL * 1024) + i / 4 * 4096);
+        load_to_lds<1024 * (i & 3)>(at, xr, (uint32_t)step * ROW);
     };
-    auto fetch_scales = [&](int run) {                             // of 512 columns
-        const int left = g.cols / MX_BLOCK - 16 * run;             // blocks
-        const uint32_t to = S::DEEP * BUFFER + (uint32_t)(run & 1) * (SROWS * 16);
-        if (left >= 16) {
+    auto fetch_w = [&](int chunk, auto i_, bool begin) {
+        constexpr int i = decltype(i_)::value;
+        const uint32_t at = piece[i & 1] * (CHUNK / PIECES) < g.cols - chunk * CHUNK ? w_at[i] : NOWHERE;
+        if (begin || i % 4 == 0) set_m0(lds + W_AT + (uint32_t)(chunk & 1) * WBYTES + (uint32_t)wave * (WL * 1024) + i / 4 * 4096);
+        load_to_lds<1024 * (i & 3)>(at, wr, (uint32_t)chunk * ROW);
+    };
+    auto fetch_scales = [&](int run) {
+        const int left = g.cols / MX_BLOCK - SCALE_ROW * run;      // blocks
+        const uint32_t to = S_AT + (uint32_t)(run & 1) * (SROWS * SCALE_ROW);
+        if (left >= SCALE_ROW) {
             const rsrc_t sw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(scales_w), 0, 0x7fffffff, 0x00027000);
             const rsrc_t sx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(X4 ? scales_x : scales_w), 0, 0x7fffffff, 0x00027000);
 #pragma unroll
             for (int i = 0; i < SL; ++i)
-                if (wave + 4 * i < SLOADS)
-                    load_to_lds(lds + to + (uint32_t)(wave + 4 * i) * 1024, s_at[i], (wave + 4 * i) * 64 < WROWS ? sw : sx, (uint32_t)run * 16);
+                if (wave + 4 * i < SLOADS) {
+                    set_m0(lds + to + (uint32_t)(wave + 4 * i) * 1024);
+                    load_to_lds<0>(s_at[i], (wave + 4 * i) * 32 < WROWS ? sw : sx, (uint32_t)(run * SCALE_ROW));
+                }
         } else if (left > 0) {                                     // the last bytes of a row, and 1 for what is behind them
 #pragma unroll
             for (int i = 0; i < SL; ++i) {
-                const int slot = (wave + 4 * i) * 64 + lane;
+                const int slot = s_slot(i);
                 if (slot >= SROWS) continue;
                 u32x4 v;
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
                     uint32_t b = 0x7f7f7f7fu;
-                    const int here = left - 4 * d;
+                    const int here = left - 16 * (lane % 2) - 4 * d;
                     if (here > 0 && s_at[i] != NOWHERE) {
-                        b = *reinterpret_cast<const uint32_t *>((slot < WROWS ? scales_w : scales_x) + s_at[i] + 16 * run + 4 * d);
+                        b = *reinterpret_cast<const uint32_t *>((slot < WROWS ? scales_w : scales_x) + s_at[i] + run * SCALE_ROW + 4 * d);
                         if (here < 4) b = (b & ((1u << 8 * here) - 1u)) | 0x7f7f7f7fu << 8 * here;
                     }
                     v[d] = b;
                 }
-                *reinterpret_cast<u32x4 *>(smem + to + slot * 16) = v;
+                *reinterpret_cast<u32x4 *>(smem + to + (wave + 4 * i) * 1024 + lane * 16) = v;
             }
         }
     };
@@ -168,14 +167,15 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     const int wx = wave >> 1, ww = wave & 1, n = lane & 31, h = lane >> 5;
     auto x_frag = [&](int step, int m, int p) {
         const int slot = wx * 32 * MT + m * 32 + n;
-        return *reinterpret_cast<const u32x4 *>(smem + (step % S::DEEP) * BUFFER + slot * S::XB + 16 * S::x_piece(slot, p));
+        return *reinterpret_cast<const u32x4 *>(smem + (step & 1) * XBYTES + slot * ROW + 16 * piece_at(slot, p));
     };
-    auto w_frag = [&](int step, int k, int p) {
+    auto w_frag = [&](int chunk, int k, int p) {
         const int slot = ww * 32 * NT + k * 32 + n;
-        return *reinterpret_cast<const u32x4 *>(smem + (step % S::DEEP) * BUFFER + XBYTES + slot * S::WB + 16 * S::w_piece(slot, p));
+        return *reinterpret_cast<const u32x4 *>(smem + W_AT + (chunk & 1) * WBYTES + slot * ROW + 16 * piece_at(slot, p));
     };
     auto scale_at = [&](int step, int slot) {
-        return smem + S::DEEP * BUFFER + (step / S::RUN & 1) * (SROWS * 16) + slot * 16 + (step % S::RUN) * (S::COLS / MX_BLOCK);
+        constexpr int STEPS = RUN / COLS;
+        return smem + S_AT + (step / STEPS & 1) * (SROWS * SCALE_ROW) + slot * SCALE_ROW + step % STEPS * (COLS / MX_BLOCK);
     };
 
     f32x16 acc[MT][NT];
@@ -186,127 +186,147 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[m][k][r] = 0.0f;
 
-    fetch_scales(0);
-#pragma unroll
-    for (int s = 0; s < S::DEEP - 1; ++s) fetch(s);
-    wait_and_meet<(S::DEEP - 2) * (XL + WL)>();
-    if constexpr (X4) {
-        u32x4 xa[2][MT], wa[2][NT];
-        uint32_t xb[MT], wb[NT];
-        auto operands = [&](int set, int step, int ks) {
-#pragma unroll
-            for (int m = 0; m < MT; ++m) xa[set][m] = x_frag(step, m, 2 * h + ks);
-#pragma unroll
-            for (int k = 0; k < NT; ++k) wa[set][k] = w_frag(step, k, 2 * h + ks);
-        };
-        auto scales = [&](int step) {                              // of both instructions of the step
-#pragma unroll
-            for (int m = 0; m < MT; ++m) xb[m] = *reinterpret_cast<const uint16_t *>(scale_at(step, WROWS + wx * 32 * MT + m * 32 + n) + 2 * h);
-#pragma unroll
-            for (int k = 0; k < NT; ++k) wb[k] = *reinterpret_cast<const uint16_t *>(scale_at(step, ww * 32 * NT + k * 32 + n) + 2 * h);
-        };
-        operands(0, 0, 0);
-        scales(0);
-        for (int s = 0; s < steps; ++s) {
-            wait_and_meet<(S::DEEP - 3) * (XL + WL)>();            // the next step is there, too, and the one before is done with
-            if (s % S::RUN == 0) fetch_scales(s / S::RUN + 1);
-            fetch(s + S::DEEP - 1);
-            operands(1, s, 1);
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int k = 0; k < NT; ++k) {
-                    const i32x8 a = {(int)xa[0][m].x, (int)xa[0][m].y, (int)xa[0][m].z, (int)xa[0][m].w, 0, 0, 0, 0};
-                    const i32x8 b = {(int)wa[0][k].x, (int)wa[0][k].y, (int)wa[0][k].z, (int)wa[0][k].w, 0, 0, 0, 0};
-                    acc[m][k] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[m][k], 4, 4, 0, (int)xb[m], 0, (int)wb[k]);
-                }
-            operands(0, s + 1, 0);
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int k = 0; k < NT; ++k) {
-                    const i32x8 a = {(int)xa[1][m].x, (int)xa[1][m].y, (int)xa[1][m].z, (int)xa[1][m].w, 0, 0, 0, 0};
-                    const i32x8 b = {(int)wa[1][k].x, (int)wa[1][k].y, (int)wa[1][k].z, (int)wa[1][k].w, 0, 0, 0, 0};
-                    acc[m][k] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc[m][k], 4, 4, 1, (int)xb[m], 1, (int)wb[k]);
-                }
-            scales(s + 1);
+    // the loads behind the barrier of a step: x of the step after the next, a share of the chunk of W after the one of the next (after: the step's
+    // place, and the next one's, in its chunk)
+    auto load = [&](int step, auto next_, auto i_, bool begin) {
+        constexpr int i = decltype(i_)::value, next = decltype(next_)::value;
+        if constexpr (i < XL) fetch_x(step + 2, i_, begin);
+        else fetch_w((step + 1) / WSTEPS + 1, std::integral_constant<int, next * (WL / WSTEPS) + i - XL>{}, begin || i == XL);
+    };
+    constexpr int EARLY = LOADS / 2;                               // loads in the last phase; the others are in the first of the next step
+    int zero = 0;
+    asm volatile("" : "+s"(zero));                                 // (offsets in registers, also where they are known)
+    fetch_scales(zero);
+    static_for<0, XL>([&](auto i) { fetch_x(zero, i, false); });
+    static_for<0, WL>([&](auto i) { fetch_w(zero, i, false); });
+    static_for<0, EARLY>([&](auto i) { load(zero - 1, std::integral_constant<int, 0>{}, i, false); });
+    wait_and_meet<EARLY>();
+
+    // The loop's instructions stay in the order of the source: one wave to a SIMD, so what is issued between two matrix instructions has to fit
+    // the time of one of them.  Left to itself the compiler reads operands just before their use (8192 x 14336 x 4096 in 4 bits: 426 us instead of 346).
+    constexpr int TILES = MT * NT;
+    u32x4 xa[2][MT], wa[2][NT];                                    // x in bf16: wa[0] has the codes of a step
+    uint32_t xb[MT], wb[NT], ahead[MT + NT];                       // scales of a step, of the next
+    bf16x8 b[2][NT];
+    auto operand = [&](int step, int q, int i) {                   // i of MT + NT, or of MT
+        if (i < MT) xa[q & 1][i] = x_frag(step, i, 4 * h + q);
+        else wa[q & 1][i - MT] = w_frag(step, i - MT, 4 * h + q);
+    };
+    auto codes = [&](int step, int k) { wa[0][k] = w_frag(step / WSTEPS, k, step % WSTEPS * 2 + h); };
+    auto scale = [&](int step, int i) {                            // i of MT + NT, or of NT
+        if constexpr (X4) {
+            const int slot = i < MT ? WROWS + wx * 32 * MT + i * 32 + n : ww * 32 * NT + (i - MT) * 32 + n;
+            ahead[i] = *reinterpret_cast<const uint32_t *>(scale_at(step, slot) + 4 * h);
+        } else {
+            wb[i] = (uint32_t)scale_at(step, ww * 32 * NT + i * 32 + n)[h] << 23;
         }
-    } else {
-        u32x4 xa[2][MT], wc[NT];
-        float sc[NT];
-        auto codes = [&](int step) {
-#pragma unroll
-            for (int k = 0; k < NT; ++k) {
-                wc[k] = w_frag(step, k, h);
-                sc[k] = __uint_as_float((uint32_t)scale_at(step, ww * 32 * NT + k * 32 + n)[h] << 23);
-            }
-        };
-        auto operands = [&](int set, int step, int q) {
-#pragma unroll
-            for (int m = 0; m < MT; ++m) xa[set][m] = x_frag(step, m, 4 * h + q);
-        };
-        operands(0, 0, 0);
-        codes(0);
-        for (int s = 0; s < steps; ++s) {
-            wait_and_meet<(S::DEEP - 3) * (XL + WL)>();
-            if (s % S::RUN == 0) fetch_scales(s / S::RUN + 1);
-            fetch(s + S::DEEP - 1);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (q < 3) operands((q + 1) & 1, s, q + 1);
-                else operands(0, s + 1, 0);
-                bf16x8 b[NT];
-#pragma unroll
-                for (int k = 0; k < NT; ++k) b[k] = __builtin_bit_cast(bf16x8, mx_values8(wc[k][q], sc[k]));
-                if (q == 3) codes(s + 1);
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int k = 0; k < NT; ++k)
-                        acc[m][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, xa[q & 1][m]), b[k], acc[m][k], 0, 0, 0);
-            }
+    };
+    auto convert = [&](int q, int k) { b[q & 1][k] = __builtin_bit_cast(bf16x8, mx_values8(wa[0][k][q], __uint_as_float(wb[k]))); };
+    auto multiply = [&](auto q_, int j) {
+        constexpr int Q = decltype(q_)::value;
+        const int m = j / NT, k = j % NT;
+        if constexpr (X4) {
+            const u32x4 x = xa[Q & 1][m], w = wa[Q & 1][k];
+            const i32x8 xv = {(int)x.x, (int)x.y, (int)x.z, (int)x.w, 0, 0, 0, 0}, wv = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
+            acc[m][k] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(xv, wv, acc[m][k], 4, 4, Q, (int)xb[m], Q, (int)wb[k]);
+        } else {
+            acc[m][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, xa[Q & 1][m]), b[Q & 1][k], acc[m][k], 0, 0, 0);
         }
+    };
+    constexpr int READS = X4 ? MT + NT : MT, SCALES = X4 ? MT + NT : NT, CODES = X4 ? 0 : NT, CONVERTS = X4 ? 0 : NT;
+#pragma unroll
+    for (int i = 0; i < SCALES; ++i) scale(0, i);
+#pragma unroll
+    for (int i = 0; i < CODES; ++i) codes(0, i);
+#pragma unroll
+    for (int i = 0; i < READS; ++i) operand(0, 0, i);
+#pragma unroll
+    for (int i = 0; i < CONVERTS; ++i) convert(0, i);
+    auto do_step = [&](const int s, auto u_) {                     // u: the step's place in its chunk
+        constexpr int u = decltype(u_)::value;
+        if constexpr (X4) {
+#pragma unroll
+            for (int i = 0; i < READS; ++i) (i < MT ? xb[i] : wb[i - MT]) = ahead[i];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        static_for<0, 4>([&](auto q_) {
+            constexpr int q = decltype(q_)::value;
+            if constexpr (q == 3) {
+                wait_and_meet<0>();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // what is done behind the products of a phase: reads of the next one's operands (ahead of a step, of scales and codes, too),
+            // conversions, and loads, spread over two phases: 4 waves that ask for 16 KB each in one phase wait for each other
+            constexpr int LOAD0 = q == 0 ? EARLY : 0, LOAD1 = q == 3 ? EARLY : q == 0 ? LOADS : 0;
+            constexpr int A = q == 3 ? CODES + SCALES : 0, B = A + READS, C = B + LOAD1 - LOAD0, OPS = C + CONVERTS;
+            constexpr int SPREAD = OPS > TILES ? OPS : TILES;
+            static_for<0, TILES>([&](auto j_) {
+                constexpr int j = decltype(j_)::value;
+                multiply(q_, j);
+                static_for<j * SPREAD / TILES, (j + 1) * SPREAD / TILES>([&](auto o_) {
+                    constexpr int o = decltype(o_)::value;
+                    if constexpr (o < CODES && o < A) codes(s + 1, o);
+                    else if constexpr (o < A) scale(s + 1, o - CODES);
+                    else if constexpr (o < B) operand(q == 3 ? s + 1 : s, (q + 1) & 3, o - A);
+                    else if constexpr (o < C)
+                        load(q == 3 ? s : s - 1, std::integral_constant<int, q == 3 ? (u + 1) % WSTEPS : u>{}, std::integral_constant<int, LOAD0 + o - B>{}, o == B);
+                    else if constexpr (o < OPS) convert((q + 1) & 3, o - C);
+                });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+    };
+    for (int s = 0; s < steps; s += WSTEPS) {                      // whole chunks: what is behind the last column is 0
+        // (what branches is here: the compiler moves matrix instructions across a branch among them, behind what they are to hide)
+        if (s % (RUN / COLS) == 0) fetch_scales(s / (RUN / COLS) + 1);
+        static_for<0, WSTEPS>([&](auto u) { do_step(s + decltype(u)::value, u); });
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // (the loads behind the last step, before LDS goes to another workgroup)
 
     // D layout: W's row lane % 32 of a tile, x's row 8 (r / 4) + 4 h + r % 4
     constexpr int HAS = GATED ? NT / 2 : NT;                       // outputs of a lane, neighbours, for a row of x
-    const int out = out0 + ww * 32 * HAS + n * HAS;
-    if (out >= g.outs) return;
+    const int out = out0 + ww * 32 * HAS + n * HAS, b0 = wx * 32 * MT + 4 * h;
+    auto put = [&](auto bf16, auto whole, auto listed) {
+        constexpr bool BF16 = decltype(bf16)::value, WHOLE = decltype(whole)::value, LISTED = decltype(listed)::value;
+        const int64_t size = BF16 ? 2 : 4, ld = g.ld_y * size;
+        char *const y0 = static_cast<char *>(g.y) + out * size + (LISTED ? 0 : (t.first + b0) * ld);
+        if (!WHOLE && out >= g.outs) return;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int b = wx * 32 * MT + m * 32 + 8 * (r / 4) + 4 * h + r % 4;
-            if (b >= t.count) continue;
-            float v[HAS];
+            for (int r = 0; r < 16; ++r) {
+                const int b = m * 32 + 8 * (r / 4) + r % 4;
+                if (!WHOLE && b0 + b >= t.count) continue;
+                char *const y = y0 + (LISTED ? g.y_row[t.first + b0 + b] : b) * ld;
+                float v[HAS];
 #pragma unroll
-            for (int k = 0; k < HAS; ++k) v[k] = GATED ? silu_mul(acc[m][2 * k][r], acc[m][2 * k + 1][r]) : acc[m][k][r];
-            const int64_t place = t.first + b, at = (g.y_row ? g.y_row[place] : place) * g.ld_y + out;
-            if (g.y_bf16) {
-                uint16_t *const y = static_cast<uint16_t *>(g.y) + at;
-                if (out + HAS <= g.outs) {
-                    if constexpr (HAS == 4) *reinterpret_cast<u32x2 *>(y) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-                    else if constexpr (HAS == 2) *reinterpret_cast<uint32_t *>(y) = bf16_pair(v[0], v[1]);
-                    else y[0] = (uint16_t)bf16_round(v[0]);
+                for (int k = 0; k < HAS; ++k) v[k] = GATED ? silu_mul(acc[m][2 * k][r], acc[m][2 * k + 1][r]) : acc[m][k][r];
+                if (WHOLE || out + HAS <= g.outs) {
+                    if constexpr (BF16) {
+                        if constexpr (HAS == 4) *reinterpret_cast<u32x2 *>(y) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+                        else *reinterpret_cast<uint32_t *>(y) = bf16_pair(v[0], v[1]);
+                    } else {
+                        if constexpr (HAS == 4) *reinterpret_cast<f32x4 *>(y) = f32x4{v[0], v[1], v[2], v[3]};
+                        else *reinterpret_cast<float2 *>(y) = make_float2(v[0], v[1]);
+                    }
                 } else {
 #pragma unroll
                     for (int k = 0; k < HAS; ++k)
-                        if (out + k < g.outs) y[k] = (uint16_t)bf16_round(v[k]);
-                }
-            } else {
-                float *const y = static_cast<float *>(g.y) + at;
-                if (out + HAS <= g.outs) {
-                    if constexpr (HAS == 4) *reinterpret_cast<f32x4 *>(y) = f32x4{v[0], v[1], v[2], v[3]};
-                    else if constexpr (HAS == 2) *reinterpret_cast<float2 *>(y) = make_float2(v[0], v[1]);
-                    else y[0] = v[0];
-                } else {
-#pragma unroll
-                    for (int k = 0; k < HAS; ++k)
-                        if (out + k < g.outs) y[k] = v[k];
+                        if (out + k < g.outs) {
+                            if constexpr (BF16) reinterpret_cast<uint16_t *>(y)[k] = (uint16_t)bf16_round(v[k]);
+                            else reinterpret_cast<float *>(y)[k] = v[k];
+                        }
                 }
             }
-        }
+    };
+    const bool whole = t.count == XROWS && out0 + OUTS <= g.outs;
+    auto typed = [&](auto bf16) {
+        if (!GATED && g.y_row) put(bf16, std::false_type{}, std::true_type{});
+        else if (whole) put(bf16, std::true_type{}, std::false_type{});
+        else put(bf16, std::false_type{}, std::false_type{});
+    };
+    if (g.y_bf16) typed(std::true_type{});
+    else typed(std::false_type{});
 }
 
 }  // namespace sbits
