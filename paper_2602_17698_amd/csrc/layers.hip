@@ -87,6 +87,15 @@ static int check_layer(const sbits_ctx *ctx, const sbits_router *r, int64_t toke
     return SBITS_OK;
 }
 
+// how a product is cut up (x_pitch: bytes between rows of x), and the workspace of its parts
+static void product_shape(const sbits_ctx *ctx, const sbits_mx &w, int64_t batch, int64_t x_pitch, MxGemm &g)
+{
+    g.w_rows = w.rows; g.cols = (int)w.cols; g.batch = batch;
+    g.tile_rows = sbits_mx_tile_rows(batch, w.rows * std::max(w.ld_codes, w.ld_scales), 256 * x_pitch);
+    sbits_mx_split(ctx, g);
+}
+static size_t product_space(const MxGemm &g) { return g.n_split == 1 ? 0 : (size_t)g.n_split * g.batch * g.ld_part * 4; }
+
 extern "C" {
 
 int64_t sbits_mx_scale_pitch(int64_t cols) { return up_to((cols + MX_BLOCK - 1) / MX_BLOCK, 4); }
@@ -106,8 +115,11 @@ int sbits_mx_quantize(sbits_ctx *ctx, const void *x, int x_type, int64_t ld_x, c
 
 size_t sbits_mx_gemm_ws_bytes(const sbits_ctx *ctx, const sbits_mx *w, int64_t batch, int four_bit, int gated)
 {
-    (void)ctx; (void)w; (void)batch; (void)four_bit; (void)gated;
-    return 0;
+    if (!ctx || check_mx(w) || batch <= 0 || batch > INT32_MAX) return 0;
+    (void)gated;
+    MxGemm g = {};
+    product_shape(ctx, *w, batch, four_bit ? w->cols / 2 : 2 * w->cols, g);      // (rows of x far apart: no parts)
+    return product_space(g);
 }
 
 int sbits_mx_gemm(sbits_ctx *ctx, const sbits_mx *w, const void *x_bf16, int64_t ld_x, const sbits_mx *x_mx, int64_t batch,
@@ -127,19 +139,19 @@ int sbits_mx_gemm(sbits_ctx *ctx, const sbits_mx *w, const void *x_bf16, int64_t
         return SBITS_ERR_INVALID_ARG;
     }
     if (!aligned(y, 16) || !pitch(ld_y, outs, 8)) return SBITS_ERR_INVALID_ARG;
-    if (!ws_ok(ws, ws_bytes, sbits_mx_gemm_ws_bytes(ctx, w, batch, x_mx != nullptr, gated))) return SBITS_ERR_WORKSPACE;
-    if ((rc = need_device(ctx))) return rc;
     MxGemm g = {};
+    product_shape(ctx, *w, batch, x_mx ? std::max(x_mx->ld_codes, x_mx->ld_scales) : 2 * ld_x, g);
+    if (!ws_ok(ws, ws_bytes, product_space(g))) return SBITS_ERR_WORKSPACE;
+    if ((rc = need_device(ctx))) return rc;
+    g.part = static_cast<float *>(ws);
     g.w = static_cast<const uint8_t *>(w->codes); g.ws = static_cast<const uint8_t *>(w->scales);
     g.ld_w = w->ld_codes; g.ld_ws = w->ld_scales;
-    g.w_rows = w->rows; g.outs = (int)outs; g.cols = (int)w->cols;
+    g.outs = (int)outs;
     g.x = x_mx ? x_mx->codes : x_bf16;
     g.xs = x_mx ? static_cast<const uint8_t *>(x_mx->scales) : nullptr;
     g.ld_x = x_mx ? x_mx->ld_codes : 2 * ld_x;
     g.ld_xs = x_mx ? x_mx->ld_scales : 0;
     g.y = y; g.ld_y = ld_y; g.y_bf16 = y_type == SBITS_TYPE_BF16; g.gated = gated;
-    g.batch = batch;
-    g.tile_rows = sbits_mx_tile_rows(batch, w->rows * std::max(w->ld_codes, w->ld_scales), 256 * std::max(g.ld_x, g.ld_xs));
     return sbits_launch_mx_gemm(ctx, g);
 }
 
@@ -195,6 +207,7 @@ int sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits
     if ((rc = sbits_launch_route(ctx, *r, logits, logits_type == SBITS_TYPE_BF16, ld_logits, bias, tokens, ids, weights))) return rc;
     if ((rc = sbits_launch_expert_lists(ctx, ids, (int)s.places, r->experts, s.tile_rows, s.max_tiles, sorted, tiles))) return rc;
     MxGemm g = {};
+    g.n_split = 1;
     g.tiles = tiles; g.n_tiles = s.max_tiles; g.tile_rows = s.tile_rows;
     g.batch = s.places;
     // h = silu(g) * u of the sorted list's rows

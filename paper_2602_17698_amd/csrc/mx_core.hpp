@@ -84,6 +84,10 @@ struct MxGemm {
     int n_tiles, tile_rows;
     const int *x_row, *y_row;
     int x_div;
+    // the columns in n_split parts of `chunks` chunks of 256 each, whose sums (fp32, [n_split][batch][ld_part]) a second kernel adds; 1: no parts
+    int n_split, chunks;
+    float *part;
+    int64_t ld_part;
 };
 
 }  // namespace sbits
@@ -91,6 +95,7 @@ struct MxGemm {
 // ---- launchers --------------------------------------------------------------
 int sbits_launch_mx_quantize(sbits_ctx *ctx, const void *x, bool bf16, int64_t ld_x, const sbits_mx &q, int64_t rows, void *values, int64_t ld_v);
 int sbits_mx_tile_rows(int64_t rows_per_matrix, int64_t w_bytes, int64_t x_bytes);
+void sbits_mx_split(const sbits_ctx *ctx, sbits::MxGemm &g);
 int sbits_launch_mx_gemm(sbits_ctx *ctx, const sbits::MxGemm &g);
 int sbits_launch_mx_gemm_many(sbits_ctx *ctx, const sbits::MxGemm &g);
 int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const float *bias, int64_t tokens,

@@ -8,106 +8,136 @@
 namespace sbits {
 
 // ---- few rows of x -----------------------------------------------------------------
-// A workgroup takes 2 tiles of 16 rows of W (gated: one of each half) and NB tiles of 16 rows of x; its 4 waves take every fourth
-// run of 128 columns and add up in LDS.  Lane l has row l % 16 of a tile and block l / 16 of the run: 16 bytes of codes, one of scales.
+// A workgroup takes T tiles of 16 rows of W (gated: half of them of each half) and one of up to 16 rows of x; its 8 waves take a group of U runs of
+// 128 columns in turn and add up in LDS.  Lane l has row l % 16 of a tile and block l / 16 of a run: 16 bytes of codes.  The codes of a group are asked
+// for ahead of the products of the one before.
 // D layout: W's row l % 16, x's row 4 (l / 16) + r.
-constexpr int FEW_WAVES = 4;
+constexpr int FEW_WAVES = 8;
 
-template <bool X4, bool GATED, int NB>
-__global__ __launch_bounds__(64 * FEW_WAVES) void mx_gemm_few_kernel(MxGemm g)
+template <int T, int U>
+struct FewGroup { u32x4 codes[T][U], scales[T]; };    // scales: of the row's 4 U blocks in the group, a byte each
+
+template <bool X4, bool GATED, int T, int U>
+__global__ __launch_bounds__(64 * FEW_WAVES, T * U > 4 ? 2 : 4) void mx_gemm_few_kernel(MxGemm g)
 {
-    __shared__ float red[FEW_WAVES][2][NB][4][64];
-    MxTile t = {0, (int)blockIdx.y * 16 * NB, 0, 0};
+    __shared__ float red[FEW_WAVES][T][4][64];
+    MxTile t = {0, (int)blockIdx.y * 16, 0, 0};
     if (g.tiles) {
         t = g.tiles[blockIdx.y];
         if (t.count == 0) return;
     } else {
-        t.count = (int)(g.batch - t.first < 16 * NB ? g.batch - t.first : 16 * NB);
+        t.count = (int)(g.batch - t.first < 16 ? g.batch - t.first : 16);
     }
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, q = lane >> 4;
-    constexpr int OUTS = GATED ? 16 : 32;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, q = lane >> 4;
+    constexpr int OUTS = GATED ? 8 * T : 16 * T, HALF = GATED ? T / 2 : T, COLS = 128 * U;
+    static_assert(!GATED || T % 2 == 0, "tiles of both halves");
     const int out0 = blockIdx.x * OUTS;
-    const uint8_t *w[2], *ws[2];
+    const uint8_t *w[T], *ws[T];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        int row = out0 + (GATED ? n : 16 * k + n);
+    for (int k = 0; k < T; ++k) {
+        int row = out0 + 16 * (k % HALF) + n;
         if (row >= g.outs) row = g.outs - 1;                    // (its sums go nowhere)
-        const int64_t at = (int64_t)t.expert * g.w_rows + (GATED && k ? g.outs : 0) + row;
+        const int64_t at = (int64_t)t.expert * g.w_rows + (k >= HALF ? g.outs : 0) + row;
         w[k] = g.w + at * g.ld_w + 16 * q;
-        ws[k] = g.ws + at * g.ld_ws + q;
+        ws[k] = g.ws + at * g.ld_ws;
     }
-    const uint8_t *x[NB], *xs[NB];
-    bool there[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const int place = 16 * b + n;
-        there[b] = place < t.count;
-        int64_t row = t.first + (there[b] ? place : 0);
-        if (g.x_row) row = g.x_row[row] / g.x_div;
-        x[b] = static_cast<const uint8_t *>(g.x) + row * g.ld_x + (X4 ? 16 : 64) * q;
-        xs[b] = X4 ? g.xs + row * g.ld_xs + q : nullptr;
-    }
+    const bool there = n < t.count;
+    int64_t x_row = t.first + (there ? n : 0);
+    if (g.x_row) x_row = g.x_row[x_row] / g.x_div;
+    const uint8_t *const x = static_cast<const uint8_t *>(g.x) + x_row * g.ld_x + (X4 ? 16 : 64) * q;
+    const uint8_t *const xs = X4 ? g.xs + x_row * g.ld_xs : nullptr;
     const u32x4 zero = {0, 0, 0, 0};
-    f32x4 acc[2][NB];
+
+    // the bytes of 4 U blocks from block `at` on; behind the last block 127
+    auto load_scales = [&](const uint8_t *row, int at, bool whole) {
+        u32x4 v = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+        if (whole) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int b = 0; b < NB; ++b) acc[k][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int runs = (g.cols + 127) / 128;
-    for (int c = wave; c < runs; c += FEW_WAVES) {
-        const bool ok = 128 * c + 32 * q < g.cols;              // behind the last block: codes 0, scale 1
-        u32x4 code[2];
-        uint32_t byte[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            code[k] = ok ? *reinterpret_cast<const u32x4 *>(w[k] + 64 * (int64_t)c) : zero;
-            byte[k] = ok ? ws[k][4 * (int64_t)c] : 127u;
-        }
-        if constexpr (X4) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const u32x4 xc = ok && there[b] ? *reinterpret_cast<const u32x4 *>(x[b] + 64 * (int64_t)c) : zero;
-                const uint32_t xb = ok && there[b] ? xs[b][4 * (int64_t)c] : 127u;
-                const i32x8 xa = {(int)xc.x, (int)xc.y, (int)xc.z, (int)xc.w, 0, 0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const i32x8 wb = {(int)code[k].x, (int)code[k].y, (int)code[k].z, (int)code[k].w, 0, 0, 0, 0};
-                    acc[k][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xa, wb, acc[k][b], 4, 4, 0, (int)xb, 0, (int)byte[k]);
-                }
-            }
+            for (int u = 0; u < U; ++u) v[u] = reinterpret_cast<const uint32_t *>(row + at)[u];
         } else {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                bf16x8 wv[2];
+            for (int u = 0; u < U; ++u) {
+                const int left = g.cols / MX_BLOCK - at - 4 * u;
+                if (left <= 0) continue;
+                const uint32_t b = reinterpret_cast<const uint32_t *>(row + at)[u];
+                v[u] = left >= 4 ? b : (b & ((1u << 8 * left) - 1u)) | 0x7f7f7f7fu << 8 * left;
+            }
+        }
+        return v;
+    };
+    auto load = [&](int group, FewGroup<T, U> &f) {
+        const int64_t c = (int64_t)group * COLS;
+        const bool whole = c + COLS <= g.cols;                  // (the same for the whole wave)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) wv[k] = __builtin_bit_cast(bf16x8, mx_values8(code[k][s], __uint_as_float(byte[k] << 23)));
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const u32x4 xv = ok && there[b] ? *reinterpret_cast<const u32x4 *>(x[b] + 256 * (int64_t)c + 16 * s) : zero;
+            for (int k = 0; k < T; ++k)
+                f.codes[k][u] = whole || c + 128 * u + 32 * q < g.cols ? *reinterpret_cast<const u32x4 *>(w[k] + c / 2 + 64 * u) : zero;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        acc[k][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv), wv[k], acc[k][b], 0, 0, 0);
+        for (int k = 0; k < T; ++k) f.scales[k] = load_scales(ws[k], (int)(c / MX_BLOCK), whole);
+    };
+    f32x4 acc[T];
+#pragma unroll
+    for (int k = 0; k < T; ++k) acc[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto multiply = [&](int group, const FewGroup<T, U> &f) {
+        const int64_t c = (int64_t)group * COLS;
+        const bool whole = c + COLS <= g.cols;
+        u32x4 xv[U][X4 ? 1 : 4], xb = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
+        if (X4 && there) xb = load_scales(xs, (int)(c / MX_BLOCK), whole);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool ok = there && (whole || c + 128 * u + 32 * q < g.cols);
+#pragma unroll
+            for (int s = 0; s < (X4 ? 1 : 4); ++s)
+                xv[u][s] = ok ? *reinterpret_cast<const u32x4 *>(x + (X4 ? c / 2 + 64 * u : 2 * c + 256 * u + 16 * s)) : zero;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if constexpr (X4) {
+                const i32x8 xa = {(int)xv[u][0].x, (int)xv[u][0].y, (int)xv[u][0].z, (int)xv[u][0].w, 0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < T; ++k) {
+                    const u32x4 w_ = f.codes[k][u];
+                    const i32x8 wb = {(int)w_.x, (int)w_.y, (int)w_.z, (int)w_.w, 0, 0, 0, 0};
+                    acc[k] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(xa, wb, acc[k], 4, 4, 0, (int)(xb[u] >> 8 * q), 0, (int)(f.scales[k][u] >> 8 * q));
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < T; ++k) {
+                    const float scale = __uint_as_float((f.scales[k][u] >> 8 * q & 255u) << 23);
+#pragma unroll
+                    for (int s = 0; s < 4; ++s)
+                        acc[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[u][s]),
+                                                                        __builtin_bit_cast(bf16x8, mx_values8(f.codes[k][u][s], scale)), acc[k], 0, 0, 0);
                 }
             }
         }
+    };
+    const int groups = (g.cols + COLS - 1) / COLS;
+    if (wave < groups) {
+        FewGroup<T, U> now, next;
+        load(wave, now);
+        for (int c = wave; c < groups; c += FEW_WAVES) {
+            if (c + FEW_WAVES < groups) load(c + FEW_WAVES, next);
+            multiply(c, now);
+            now = next;
+        }
     }
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < T; ++k)
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) red[wave][k][b][r][lane] = acc[k][b][r];
+        for (int r = 0; r < 4; ++r) red[wave][k][r][lane] = acc[k][r];
     __syncthreads();
-    const int i = tid % OUTS;
-    if (out0 + i >= g.outs) return;
-    for (int b = tid / OUTS; b < t.count; b += 64 * FEW_WAVES / OUTS) {
+    for (int p = tid; p < OUTS * t.count; p += 64 * FEW_WAVES) {
+        const int i = p % OUTS, b = p / OUTS;
+        if (out0 + i >= g.outs) continue;
         auto sum = [&](int k, int n_) {
-            float v = red[0][k][b >> 4][b & 3][(b >> 2 & 3) * 16 + n_];
+            float v = red[0][k][b & 3][(b >> 2) * 16 + n_];
 #pragma unroll
-            for (int w_ = 1; w_ < FEW_WAVES; ++w_) v += red[w_][k][b >> 4][b & 3][(b >> 2 & 3) * 16 + n_];
+            for (int w_ = 1; w_ < FEW_WAVES; ++w_) v += red[w_][k][b & 3][(b >> 2) * 16 + n_];
             return v;
         };
-        const float v = GATED ? silu_mul(sum(0, i), sum(1, i)) : sum(i >> 4, i & 15);
+        const float v = GATED ? silu_mul(sum(i >> 4, i & 15), sum(HALF + (i >> 4), i & 15)) : sum(i >> 4, i & 15);
         const int64_t place = t.first + b, at = (g.y_row ? g.y_row[place] : place) * g.ld_y + out0 + i;
         if (g.y_bf16) static_cast<uint16_t *>(g.y)[at] = (uint16_t)bf16_round(v);
         else static_cast<float *>(g.y)[at] = v;
@@ -123,24 +153,42 @@ using namespace sbits;
 int sbits_mx_tile_rows(int64_t rows_per_matrix, int64_t w_bytes, int64_t x_bytes)
 {
     const bool near = w_bytes < ((int64_t)1 << 31) && x_bytes < ((int64_t)1 << 31);
-    if (near && rows_per_matrix > 64) return rows_per_matrix > 128 ? 256 : 128;
-    return rows_per_matrix <= 16 ? 16 : rows_per_matrix <= 32 ? 32 : 64;
+    if (rows_per_matrix <= 16 || !near) return 16;
+    return rows_per_matrix <= 64 ? 64 : rows_per_matrix <= 128 ? 128 : 256;
 }
 
-template <bool X4, bool GATED>
-static auto few_instance(int rows)
+// Tiles of W to a workgroup: 4, if the CUs are three quarters busy with that, else 2 or 1.  One token, bf16: 14336 x 4096 with 1, 2, 4 tiles 12.0, 10.6,
+// 9.9 us, with 16 rows of x 22.4, 16.3, 12.6 (x is read once for every workgroup); 4096 x 14336 10.2, 14.5, 28.8, with 16 rows 19.5, 23.0, 36.6.
+// Runs to a group: 4, or as many as leave a group for each wave.
+template <bool X4, bool GATED, int T>
+static auto few_runs(int cols)
 {
-    return rows == 16 ? mx_gemm_few_kernel<X4, GATED, 1> : rows == 32 ? mx_gemm_few_kernel<X4, GATED, 2> : mx_gemm_few_kernel<X4, GATED, 4>;
+    const int runs = (cols + 127) / 128;
+    return runs <= FEW_WAVES ? mx_gemm_few_kernel<X4, GATED, T, 1> : runs <= 2 * FEW_WAVES ? mx_gemm_few_kernel<X4, GATED, T, 2> : mx_gemm_few_kernel<X4, GATED, T, 4>;
+}
+template <bool X4, bool GATED>
+static auto few_instance(const sbits_ctx *ctx, const MxGemm &g, int tiles, int &outs)
+{
+    const int64_t enough = (int64_t)sbits_cus(ctx) * 3 / 4, rows = (int64_t)g.w_rows * tiles;
+    outs = 64 / (GATED ? 2 : 1);
+    if (rows >= 64 * enough) return few_runs<X4, GATED, 4>(g.cols);
+    outs /= 2;
+    if constexpr (!GATED)
+        if (rows < 32 * enough) {
+            outs = 16;
+            return few_runs<X4, GATED, 1>(g.cols);
+        }
+    return few_runs<X4, GATED, 2>(g.cols);
 }
 
 int sbits_launch_mx_gemm(sbits_ctx *ctx, const MxGemm &g)
 {
-    if (g.tile_rows > 64) return sbits_launch_mx_gemm_many(ctx, g);
+    if (g.tile_rows > 16) return sbits_launch_mx_gemm_many(ctx, g);
     const bool x4 = g.xs != nullptr;
     const int tiles = g.tiles ? g.n_tiles : (int)((g.batch + g.tile_rows - 1) / g.tile_rows);
-    auto fn = x4 ? (g.gated ? few_instance<true, true>(g.tile_rows) : few_instance<true, false>(g.tile_rows))
-                 : (g.gated ? few_instance<false, true>(g.tile_rows) : few_instance<false, false>(g.tile_rows));
-    const int outs = g.gated ? 16 : 32;
+    int outs;
+    auto fn = x4 ? (g.gated ? few_instance<true, true>(ctx, g, tiles, outs) : few_instance<true, false>(ctx, g, tiles, outs))
+                 : (g.gated ? few_instance<false, true>(ctx, g, tiles, outs) : few_instance<false, false>(ctx, g, tiles, outs));
     for (int first = 0; first < tiles; first += 65535) {
         MxGemm part = g;
         const int n = tiles - first < 65535 ? tiles - first : 65535;

@@ -75,16 +75,18 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
         t.count = (int)(g.batch - t.first < XROWS ? g.batch - t.first : XROWS);
     }
     const int out0 = wt * OUTS;
+    const int chunk0 = (int)blockIdx.y * g.chunks;                 // the part of the columns
+    const int cols = g.n_split == 1 || g.cols - chunk0 * CHUNK < g.chunks * CHUNK ? g.cols - chunk0 * CHUNK : g.chunks * CHUNK;
 
     // Where a lane's loads come from: offsets into buffers that begin at the tile's first row of x (with a list of rows: at the first of
     // all) and at the matrix.  Rows and columns that are not there: NOWHERE.  Four loads share an address in LDS and have offsets 0 .. LAST, which count for
     // the memory's address, too: buffers begin LAST bytes ahead, and the offsets here take the load's own away.
     constexpr int LAST = 3 * 1024;
     const int64_t x_first = g.x_row ? 0 : t.first, w_first = (int64_t)t.expert * g.w_rows;
-    const rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(static_cast<const uint8_t *>(g.x) + x_first * g.ld_x - LAST), 0, 0x7fffffff, 0x00027000);
-    const rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.w + w_first * g.ld_w - LAST), 0, 0x7fffffff, 0x00027000);
-    const uint8_t *const scales_w = g.ws + w_first * g.ld_ws;
-    const uint8_t *const scales_x = X4 ? g.xs + x_first * g.ld_xs : nullptr;
+    const rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(static_cast<const uint8_t *>(g.x) + x_first * g.ld_x + (int64_t)chunk0 * (X4 ? ROW : 2 * CHUNK) - LAST), 0, 0x7fffffff, 0x00027000);
+    const rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.w + w_first * g.ld_w + (int64_t)chunk0 * ROW - LAST), 0, 0x7fffffff, 0x00027000);
+    const uint8_t *const scales_w = g.ws + w_first * g.ld_ws + chunk0 * (CHUNK / MX_BLOCK);
+    const uint8_t *const scales_x = X4 ? g.xs + x_first * g.ld_xs + chunk0 * (CHUNK / MX_BLOCK) : nullptr;
     auto x_row = [&](int slot) -> int { return slot >= t.count ? -1 : g.x_row ? g.x_row[t.first + slot] / g.x_div : slot; };
     auto w_row = [&](int slot) -> int {
         const int w = slot / (32 * NT), tile = slot / 32 % NT, n = slot % 32;
@@ -111,7 +113,7 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
         const int row = slot < WROWS ? w_row(slot) : slot < SROWS ? x_row(slot - WROWS) : -1;
         s_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * (slot < WROWS ? g.ld_ws : g.ld_xs)) + 16 * (lane % 2);
     }
-    const int steps = (g.cols + COLS - 1) / COLS;
+    const int steps = (cols + COLS - 1) / COLS;
 
     // Loads of a step, the first XL x's, then the step's share of the next chunk of W.  Pieces behind the last column go NOWHERE: a comparison with
     // every load, as a branch would part the matrix instructions around it.
@@ -120,18 +122,18 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     // (begin: the first of the four, or of a phase's)
     auto fetch_x = [&](int step, auto i_, bool begin) {
         constexpr int i = decltype(i_)::value;
-        const uint32_t at = piece[i & 1] * (COLS / PIECES) < g.cols - step * COLS ? x_at[i] : NOWHERE;
+        const uint32_t at = piece[i & 1] * (COLS / PIECES) < cols - step * COLS ? x_at[i] : NOWHERE;
         if (begin || i % 4 == 0) set_m0(lds + (uint32_t)(step & 1) * XBYTES + (uint32_t)wave * (XL * 1024) + i / 4 * 4096);
         load_to_lds<1024 * (i & 3)>(at, xr, (uint32_t)step * ROW);
     };
     auto fetch_w = [&](int chunk, auto i_, bool begin) {
         constexpr int i = decltype(i_)::value;
-        const uint32_t at = piece[i & 1] * (CHUNK / PIECES) < g.cols - chunk * CHUNK ? w_at[i] : NOWHERE;
+        const uint32_t at = piece[i & 1] * (CHUNK / PIECES) < cols - chunk * CHUNK ? w_at[i] : NOWHERE;
         if (begin || i % 4 == 0) set_m0(lds + W_AT + (uint32_t)(chunk & 1) * WBYTES + (uint32_t)wave * (WL * 1024) + i / 4 * 4096);
         load_to_lds<1024 * (i & 3)>(at, wr, (uint32_t)chunk * ROW);
     };
     auto fetch_scales = [&](int run) {
-        const int left = g.cols / MX_BLOCK - SCALE_ROW * run;      // blocks
+        const int left = cols / MX_BLOCK - SCALE_ROW * run;      // blocks
         const uint32_t to = S_AT + (uint32_t)(run & 1) * (SROWS * SCALE_ROW);
         if (left >= SCALE_ROW) {
             const rsrc_t sw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(scales_w), 0, 0x7fffffff, 0x00027000);
@@ -286,10 +288,13 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     // D layout: W's row lane % 32 of a tile, x's row 8 (r / 4) + 4 h + r % 4
     constexpr int HAS = GATED ? NT / 2 : NT;                       // outputs of a lane, neighbours, for a row of x
     const int out = out0 + ww * 32 * HAS + n * HAS, b0 = wx * 32 * MT + 4 * h;
-    auto put = [&](auto bf16, auto whole, auto listed) {
-        constexpr bool BF16 = decltype(bf16)::value, WHOLE = decltype(whole)::value, LISTED = decltype(listed)::value;
-        const int64_t size = BF16 ? 2 : 4, ld = g.ld_y * size;
-        char *const y0 = static_cast<char *>(g.y) + out * size + (LISTED ? 0 : (t.first + b0) * ld);
+    const bool whole = t.count == XROWS && out0 + OUTS <= g.outs, parts = g.n_split > 1;
+    char *const y_base = parts ? reinterpret_cast<char *>(g.part + (int64_t)blockIdx.y * g.batch * g.ld_part) : static_cast<char *>(g.y);
+    const int64_t ld_y = parts ? g.ld_part : g.ld_y;
+    auto put = [&](auto bf16, auto whole_, auto listed) {
+        constexpr bool BF16 = decltype(bf16)::value, WHOLE = decltype(whole_)::value, LISTED = decltype(listed)::value;
+        const int64_t size = BF16 ? 2 : 4, ld = ld_y * size;
+        char *const y0 = y_base + out * size + (LISTED ? 0 : (t.first + b0) * ld);
         if (!WHOLE && out >= g.outs) return;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -319,14 +324,63 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
                 }
             }
     };
-    const bool whole = t.count == XROWS && out0 + OUTS <= g.outs;
     auto typed = [&](auto bf16) {
         if (!GATED && g.y_row) put(bf16, std::false_type{}, std::true_type{});
         else if (whole) put(bf16, std::true_type{}, std::false_type{});
         else put(bf16, std::false_type{}, std::false_type{});
     };
-    if (g.y_bf16) typed(std::true_type{});
+    if (g.y_bf16 && !parts) typed(std::true_type{});
     else typed(std::false_type{});
+}
+
+// the parts' sums, in the order of the columns, then what the kernel above does with a sum
+struct MxJoin {
+    const float *part;
+    void *y;
+    int64_t ld_part, ld_y, batch;
+    int n_split, outs;
+};
+template <bool GATED, bool BF16>
+__global__ __launch_bounds__(256) void mx_join_kernel(MxJoin a)
+{
+    const int out = 4 * (int)(blockIdx.x * 256 + threadIdx.x);
+    if (out >= a.outs) return;
+    const int64_t b = blockIdx.y;
+    const float *p = a.part + b * a.ld_part + out;
+    float v[4], u[4];
+    auto add = [&](const float *from, float (&sum)[4], bool first) {
+        if (!GATED || out + 4 <= a.outs) {                         // (rows of sums are a multiple of 8 long)
+            const f32x4 f = *reinterpret_cast<const f32x4 *>(from);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = first ? f[i] : sum[i] + f[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float f = out + i < a.outs ? from[i] : 0.0f;
+                sum[i] = first ? f : sum[i] + f;
+            }
+        }
+    };
+    for (int s = 0; s < a.n_split; ++s, p += a.batch * a.ld_part) {
+        add(p, v, s == 0);
+        if (GATED) {
+            if (a.outs % 4 == 0) add(p + a.outs, u, s == 0);
+            else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float f = out + i < a.outs ? p[a.outs + i] : 0.0f;
+                    u[i] = s == 0 ? f : u[i] + f;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (GATED) v[i] = silu_mul(v[i], u[i]);
+        if (out + i >= a.outs) continue;
+        if constexpr (BF16) static_cast<uint16_t *>(a.y)[b * a.ld_y + out + i] = (uint16_t)bf16_round(v[i]);
+        else static_cast<float *>(a.y)[b * a.ld_y + out + i] = v[i];
+    }
 }
 
 }  // namespace sbits
@@ -342,20 +396,55 @@ static int launch(sbits_ctx *ctx, const MxGemm &g)
     MxGemm a = g;
     if (!g.tiles) a.n_tiles = (int)((g.batch + 64 * MT - 1) / (64 * MT));
     const int64_t all = (int64_t)a.n_tiles * ((g.outs + outs - 1) / outs);
-    hipLaunchKernelGGL(fn, dim3((unsigned)all), dim3(256), lds, ctx->stream, a);
+    hipLaunchKernelGGL(fn, dim3((unsigned)all, (unsigned)a.n_split), dim3(256), lds, ctx->stream, a);
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;
 }
 
-int sbits_launch_mx_gemm_many(sbits_ctx *ctx, const MxGemm &g)
+#ifndef MANY_NT
+#define MANY_NT 4
+#endif
+// Parts of the columns where there are fewer tiles than CUs.
+void sbits_mx_split(const sbits_ctx *ctx, MxGemm &g)
+{
+    const int chunks = (g.cols + CHUNK - 1) / CHUNK, rows = (int)g.w_rows;
+    g.n_split = 1;
+    g.chunks = chunks;
+    g.ld_part = (g.w_rows + 7) / 8 * 8;
+    if (g.tiles || g.tile_rows <= 16) return;
+    const int64_t tiles = ((g.batch + g.tile_rows - 1) / g.tile_rows) * ((rows + 64 * MANY_NT - 1) / (64 * MANY_NT));
+    const int most = (int)(sbits_cus(ctx) / tiles);
+    if (most < 2 || chunks < 2) return;
+    g.chunks = (chunks + most - 1) / most;
+    g.n_split = (chunks + g.chunks - 1) / g.chunks;
+}
+
+static int launch_tile(sbits_ctx *ctx, const MxGemm &g)
 {
     const bool x4 = g.xs != nullptr;
     switch (g.tile_rows) {
 #define MANY(MT, NT) (x4 ? (g.gated ? launch<true, true, MT, NT>(ctx, g) : launch<true, false, MT, NT>(ctx, g)) \
                          : (g.gated ? launch<false, true, MT, NT>(ctx, g) : launch<false, false, MT, NT>(ctx, g)))
-    case 256: return MANY(4, 4);
-    case 128: return MANY(2, 4);
+    case 256: return MANY(4, MANY_NT);
+    case 128: return MANY(2, MANY_NT);
+    case 64: return MANY(1, MANY_NT);
     default: return SBITS_ERR_INTERNAL;
 #undef MANY
     }
+}
+
+int sbits_launch_mx_gemm_many(sbits_ctx *ctx, const MxGemm &g)
+{
+    if (g.n_split == 1) return launch_tile(ctx, g);
+    MxGemm part = g;
+    part.outs = (int)g.w_rows;
+    part.gated = 0;
+    const int rc = launch_tile(ctx, part);
+    if (rc) return rc;
+    const MxJoin j = {g.part, g.y, g.ld_part, g.ld_y, g.batch, g.n_split, g.outs};
+    auto fn = g.gated ? (g.y_bf16 ? mx_join_kernel<true, true> : mx_join_kernel<true, false>)
+                      : (g.y_bf16 ? mx_join_kernel<false, true> : mx_join_kernel<false, false>);
+    hipLaunchKernelGGL(fn, dim3((unsigned)((g.outs + 1023) / 1024), (unsigned)g.batch), dim3(256), 0, ctx->stream, j);
+    SBITS_HIP(ctx, hipGetLastError());
+    return SBITS_OK;
 }

@@ -81,6 +81,10 @@ SHAPES = [(1, 8, 32), (1, 250, 256), (2, 33, 96), (15, 64, 128), (16, 31, 160), 
           (65, 250, 320), (97, 256, 576), (128, 514, 256), (129, 300, 352), (200, 129, 1120), (255, 513, 64), (256, 256, 32), (257, 258, 608), (300, 700, 800)]
 
 
+def workspace(ctx, w, batch, four, gated=False):
+    return torch.full((max(256, ctx.mx_gemm_ws_bytes(w, batch, four, gated)),), 0xff, dtype=torch.uint8, device="cuda")
+
+
 def check_product(ctx, batch, rows, cols, four, gated, out, extra=0, seed=0, spread=3):
     g = gen(seed + 31 * batch + rows)
     code, byte = mp.random_matrix(rows * (2 if gated else 1), cols, g, spread)
@@ -92,7 +96,7 @@ def check_product(ctx, batch, rows, cols, four, gated, out, extra=0, seed=0, spr
     else:
         xs, xd = x[:, :cols].double(), x.cuda()[:, :cols]
     y = torch.full((batch, sb.mx_out_pitch(rows) + 8 * extra), 7.0, dtype=out, device="cuda")
-    ws = torch.full((max(256, ctx.mx_gemm_ws_bytes(w, batch, four, gated)),), 0xff, dtype=torch.uint8, device="cuda")
+    ws = workspace(ctx, w, batch, four, gated)
     print("[case]", batch, rows, cols, four, gated, out, flush=True)
     ctx.mx_gemm(w, xd, y[:, :rows], ws, gated=gated)
     torch.cuda.synchronize()
@@ -142,7 +146,7 @@ def test_broken_blocks_stay_in_their_outputs(ctx, batch, four):
         w = sb.mx(*mp.stored(code, byte, "cuda"))
         xd = sb.mx(*mp.stored(*mp.quantise(x), "cuda")) if four else x.cuda()
         y = torch.empty(batch, sb.mx_out_pitch(rows), device="cuda")
-        ctx.mx_gemm(w, xd, y[:, :rows], None)
+        ctx.mx_gemm(w, xd, y[:, :rows], workspace(ctx, w, batch, four))
         return y[:, :rows].cpu()
     good = run(byte, x)
     byte2, x2 = byte.clone(), x.clone()
