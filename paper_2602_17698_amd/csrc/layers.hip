@@ -47,7 +47,7 @@ struct LayerSpace {
     int64_t tokens, places, hidden, inner;
     int tile_rows, max_tiles;
     int64_t codes_x, scales_x, codes_h, scales_h;                  // pitches
-    size_t sorted, tiles, h, y, xq, xs, hq, hs, bytes;
+    size_t sorted, token, tiles, h, y, xq, xs, hq, hs, bytes;
 };
 static LayerSpace layer_space(const sbits_router &r, int64_t tokens, const sbits_mx &up, const sbits_mx &down, bool four, int64_t ld_x)
 {
@@ -67,6 +67,7 @@ static LayerSpace layer_space(const sbits_router &r, int64_t tokens, const sbits
     size_t at = 0;
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)up_to(bytes, 256); return here; };
     s.sorted = take(s.places * 4);
+    s.token = take(s.places * 4);
     s.tiles = take(tiles(std::min(s.tile_rows, 64)) * (int64_t)sizeof(MxTile));
     s.h = take(s.places * s.inner * 2);
     s.y = take(s.places * s.hidden * 2);
@@ -202,10 +203,10 @@ int sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits
     if (!ws_ok(ws, ws_bytes, s.bytes)) return SBITS_ERR_WORKSPACE;
     if ((rc = need_device(ctx))) return rc;
     char *const base = static_cast<char *>(ws);
-    int *const sorted = reinterpret_cast<int *>(base + s.sorted);
+    int *const sorted = reinterpret_cast<int *>(base + s.sorted), *const token = reinterpret_cast<int *>(base + s.token);
     MxTile *const tiles = reinterpret_cast<MxTile *>(base + s.tiles);
     if ((rc = sbits_launch_route(ctx, *r, logits, logits_type == SBITS_TYPE_BF16, ld_logits, bias, tokens, ids, weights))) return rc;
-    if ((rc = sbits_launch_expert_lists(ctx, ids, (int)s.places, r->experts, s.tile_rows, s.max_tiles, sorted, tiles))) return rc;
+    if ((rc = sbits_launch_expert_lists(ctx, ids, (int)s.places, r->experts, r->top_k, s.tile_rows, s.max_tiles, sorted, token, tiles))) return rc;
     MxGemm g = {};
     g.n_split = 1;
     g.tiles = tiles; g.n_tiles = s.max_tiles; g.tile_rows = s.tile_rows;
@@ -215,7 +216,7 @@ int sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits
     g.ld_w = up->ld_codes; g.ld_ws = up->ld_scales;
     g.w_rows = 2 * s.inner; g.outs = (int)s.inner; g.cols = (int)s.hidden;
     g.x = x_bf16; g.ld_x = 2 * ld_x;
-    g.x_row = sorted; g.x_div = r->top_k;
+    g.x_row = token;
     g.y = base + s.h; g.ld_y = s.inner; g.y_bf16 = 1; g.gated = 1;
     if (four_bit) {
         const sbits_mx q = {base + s.xq, base + s.xs, tokens, s.hidden, s.codes_x, s.scales_x};
@@ -229,7 +230,7 @@ int sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits
     g.ld_w = down->ld_codes; g.ld_ws = down->ld_scales;
     g.w_rows = s.hidden; g.outs = (int)s.hidden; g.cols = (int)s.inner;
     g.x = base + s.h; g.ld_x = 2 * s.inner;
-    g.x_row = nullptr; g.x_div = 1; g.y_row = sorted;
+    g.x_row = nullptr; g.y_row = sorted;
     g.y = base + s.y; g.ld_y = s.hidden; g.gated = 0;
     if (four_bit) {
         const sbits_mx q = {base + s.hq, base + s.hs, s.places, s.inner, s.codes_h, s.scales_h};

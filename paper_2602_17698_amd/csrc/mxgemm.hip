@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, T * U > 4 ? 2 : 4) void mx_gemm_few
     }
     const bool there = n < t.count;
     int64_t x_row = t.first + (there ? n : 0);
-    if (g.x_row) x_row = g.x_row[x_row] / g.x_div;
+    if (g.x_row) x_row = g.x_row[x_row];
     const uint8_t *const x = static_cast<const uint8_t *>(g.x) + x_row * g.ld_x + (X4 ? 16 : 64) * q;
     const uint8_t *const xs = X4 ? g.xs + x_row * g.ld_xs : nullptr;
     const u32x4 zero = {0, 0, 0, 0};

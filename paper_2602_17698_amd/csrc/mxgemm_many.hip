@@ -87,31 +87,33 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     const rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.w + w_first * g.ld_w + (int64_t)chunk0 * ROW - LAST), 0, 0x7fffffff, 0x00027000);
     const uint8_t *const scales_w = g.ws + w_first * g.ld_ws + chunk0 * (CHUNK / MX_BLOCK);
     const uint8_t *const scales_x = X4 ? g.xs + x_first * g.ld_xs + chunk0 * (CHUNK / MX_BLOCK) : nullptr;
-    auto x_row = [&](int slot) -> int { return slot >= t.count ? -1 : g.x_row ? g.x_row[t.first + slot] / g.x_div : slot; };
+    auto x_row = [&](int slot) -> int { return slot >= t.count ? -1 : g.x_row ? g.x_row[t.first + slot] : slot; };
     auto w_row = [&](int slot) -> int {
         const int w = slot / (32 * NT), tile = slot / 32 % NT, n = slot % 32;
         const int out = out0 + (GATED ? w * 16 * NT + n * (NT / 2) + tile / 2 : w * 32 * NT + n * NT + tile);
         return out >= g.outs ? -1 : GATED && (tile & 1) ? g.outs + out : out;
     };
+    // (32 bits: the caller sees to it that what a tile spans is below 2^31)
+    const uint32_t ld_x = (uint32_t)g.ld_x, ld_w = (uint32_t)g.ld_w, ld_xs = (uint32_t)g.ld_xs, ld_ws = (uint32_t)g.ld_ws;
     auto x_slot = [&](int i) { return (wave * XL + i) * 8 + lane / 8; };
     auto w_slot = [&](int i) { return (wave * WL + i) * 8 + lane / 8; };
     uint32_t x_at[XL], w_at[WL], s_at[SL];
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
         const int row = x_row(x_slot(i));
-        x_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * g.ld_x) + 16 * piece_at(x_slot(i), lane % 8) + LAST - 1024 * (i & 3);
+        x_at[i] = row < 0 ? NOWHERE : row * ld_x + 16 * piece_at(x_slot(i), lane % 8) + LAST - 1024 * (i & 3);
     }
 #pragma unroll
     for (int i = 0; i < WL; ++i) {
         const int row = w_row(w_slot(i));
-        w_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * g.ld_w) + 16 * piece_at(w_slot(i), lane % 8) + LAST - 1024 * (i & 3);
+        w_at[i] = row < 0 ? NOWHERE : row * ld_w + 16 * piece_at(w_slot(i), lane % 8) + LAST - 1024 * (i & 3);
     }
     auto s_slot = [&](int i) { return (wave + 4 * i) * 32 + lane / 2; };
 #pragma unroll
     for (int i = 0; i < SL; ++i) {
-        const int slot = s_slot(i);
-        const int row = slot < WROWS ? w_row(slot) : slot < SROWS ? x_row(slot - WROWS) : -1;
-        s_at[i] = row < 0 ? NOWHERE : (uint32_t)(row * (slot < WROWS ? g.ld_ws : g.ld_xs)) + 16 * (lane % 2);
+        const bool of_w = (wave + 4 * i) * 32 < WROWS;             // (the same for the whole wave)
+        const int row = of_w ? w_row(s_slot(i)) : (wave + 4 * i) * 32 < SROWS ? x_row(s_slot(i) - WROWS) : -1;
+        s_at[i] = row < 0 ? NOWHERE : row * (of_w ? ld_ws : ld_xs) + 16 * (lane % 2);
     }
     const int steps = (cols + COLS - 1) / COLS;
 
@@ -287,50 +289,60 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
 
     // D layout: W's row lane % 32 of a tile, x's row 8 (r / 4) + 4 h + r % 4
     constexpr int HAS = GATED ? NT / 2 : NT;                       // outputs of a lane, neighbours, for a row of x
-    const int out = out0 + ww * 32 * HAS + n * HAS, b0 = wx * 32 * MT + 4 * h;
-    const bool whole = t.count == XROWS && out0 + OUTS <= g.outs, parts = g.n_split > 1;
+    const int out = out0 + ww * 32 * HAS + n * HAS, b0 = wx * 32 * MT;
+    const bool rows_whole = t.count == XROWS, outs_whole = out0 + OUTS <= g.outs, parts = g.n_split > 1;
     char *const y_base = parts ? reinterpret_cast<char *>(g.part + (int64_t)blockIdx.y * g.batch * g.ld_part) : static_cast<char *>(g.y);
     const int64_t ld_y = parts ? g.ld_part : g.ld_y;
-    auto put = [&](auto bf16, auto whole_, auto listed) {
-        constexpr bool BF16 = decltype(bf16)::value, WHOLE = decltype(whole_)::value, LISTED = decltype(listed)::value;
-        const int64_t size = BF16 ? 2 : 4, ld = ld_y * size;
-        char *const y0 = y_base + out * size + (LISTED ? 0 : (t.first + b0) * ld);
-        if (!WHOLE && out >= g.outs) return;
+    auto value = [&](int m, int r, int k) { return GATED ? silu_mul(acc[m][2 * k][r], acc[m][2 * k + 1][r]) : acc[m][k][r]; };
+    auto put = [&](auto bf16, auto listed, auto rest) {            // rest: of lanes that have some of their outputs only
+        constexpr bool BF16 = decltype(bf16)::value, LISTED = decltype(listed)::value, REST = decltype(rest)::value;
+        const int64_t ld = ld_y * (BF16 ? 2 : 4);
+        char *const y0 = y_base + (int64_t)out * (BF16 ? 2 : 4) + (LISTED ? 0 : (t.first + b0 + 4 * h) * ld);
+        int rows[MT];                                              // (of all lanes: they are read across lanes below)
+        if (LISTED)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) rows[m] = b0 + 32 * m + n < t.count ? g.y_row[t.first + b0 + 32 * m + n] : 0;
+        if (REST ? out >= g.outs || out + HAS <= g.outs : !outs_whole && out + HAS > g.outs) return;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int b = m * 32 + 8 * (r / 4) + r % 4;
-                if (!WHOLE && b0 + b >= t.count) continue;
-                char *const y = y0 + (LISTED ? g.y_row[t.first + b0 + b] : b) * ld;
-                float v[HAS];
-#pragma unroll
-                for (int k = 0; k < HAS; ++k) v[k] = GATED ? silu_mul(acc[m][2 * k][r], acc[m][2 * k + 1][r]) : acc[m][k][r];
-                if (WHOLE || out + HAS <= g.outs) {
-                    if constexpr (BF16) {
-                        if constexpr (HAS == 4) *reinterpret_cast<u32x2 *>(y) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-                        else *reinterpret_cast<uint32_t *>(y) = bf16_pair(v[0], v[1]);
-                    } else {
-                        if constexpr (HAS == 4) *reinterpret_cast<f32x4 *>(y) = f32x4{v[0], v[1], v[2], v[3]};
-                        else *reinterpret_cast<float2 *>(y) = make_float2(v[0], v[1]);
-                    }
+                constexpr int H = 4;
+                const int b = 32 * m + 8 * (r / 4) + r % 4;
+                if (!rows_whole && b0 + b + H * h >= t.count) continue;
+                char *y;
+                if constexpr (LISTED) {
+                    const int row0 = __builtin_amdgcn_readlane(rows[m], b % 32), row1 = __builtin_amdgcn_readlane(rows[m], b % 32 + H);
+                    y = y0 + (h ? row1 : row0) * ld;
                 } else {
+                    y = y0 + b * ld;
+                }
+                if constexpr (REST) {
 #pragma unroll
                     for (int k = 0; k < HAS; ++k)
                         if (out + k < g.outs) {
-                            if constexpr (BF16) reinterpret_cast<uint16_t *>(y)[k] = (uint16_t)bf16_round(v[k]);
-                            else reinterpret_cast<float *>(y)[k] = v[k];
+                            if constexpr (BF16) reinterpret_cast<uint16_t *>(y)[k] = (uint16_t)bf16_round(value(m, r, k));
+                            else reinterpret_cast<float *>(y)[k] = value(m, r, k);
                         }
+                } else if constexpr (BF16) {
+                    if constexpr (HAS == 4) *reinterpret_cast<u32x2 *>(y) = u32x2{bf16_pair(value(m, r, 0), value(m, r, 1)), bf16_pair(value(m, r, 2), value(m, r, 3))};
+                    else *reinterpret_cast<uint32_t *>(y) = bf16_pair(value(m, r, 0), value(m, r, 1));
+                } else {
+                    if constexpr (HAS == 4) *reinterpret_cast<f32x4 *>(y) = f32x4{value(m, r, 0), value(m, r, 1), value(m, r, 2), value(m, r, 3)};
+                    else *reinterpret_cast<float2 *>(y) = make_float2(value(m, r, 0), value(m, r, 1));
                 }
             }
     };
-    auto typed = [&](auto bf16) {
-        if (!GATED && g.y_row) put(bf16, std::false_type{}, std::true_type{});
-        else if (whole) put(bf16, std::true_type{}, std::false_type{});
-        else put(bf16, std::false_type{}, std::false_type{});
+    auto typed = [&](auto listed, auto rest) {
+        if (g.y_bf16 && !parts) put(std::true_type{}, listed, rest);
+        else put(std::false_type{}, listed, rest);
     };
-    if (g.y_bf16 && !parts) typed(std::true_type{});
-    else typed(std::false_type{});
+    if (GATED || !g.y_row) {
+        typed(std::false_type{}, std::false_type{});
+        if (!outs_whole && g.outs % HAS) typed(std::false_type{}, std::true_type{});
+    } else {                                                       // (rows of a multiple of 32 outputs)
+        put(std::true_type{}, std::true_type{}, std::false_type{});
+    }
 }
 
 // the parts' sums, in the order of the columns, then what the kernel above does with a sum

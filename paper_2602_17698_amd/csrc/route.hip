@@ -219,22 +219,37 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
 }
 
 // ---- lists by expert ---------------------------------------------------------------
-// sorted: the places (token * top_k + j) of all choices, expert after expert, ascending inside one; tiles: pieces of at most tile_rows of an
-// expert's list, expert after expert, then entries with count 0.  A workgroup an expert: it counts the choices of all experts
-// in LDS (whole numbers: any order gives the same), and so knows where its own list and tiles begin.
-__global__ __launch_bounds__(256) void expert_lists_kernel(const int32_t *ids, int n, int experts, int tile_rows, int max_tiles, int *sorted,
-                                                           MxTile *tiles)
+// sorted: the places (token * top_k + j) of all choices, expert after expert, ascending inside one; token_of: their tokens; tiles: pieces of at most
+// tile_rows of an expert's list, expert after expert, then entries with count 0.  A workgroup an expert.  Its waves take consecutive runs
+// of the choices; a wave's first pass counts those of its own expert (by ballots), and of all experts (in LDS, whole numbers: any order
+// gives the same), so the workgroup knows where its list and its tiles begin, a wave where its part does.
+// Bound by the latency of the two passes over the ids, which come from L2: 16384 choices of 32 experts, one id a lane and 256 threads: 42 us.
+constexpr int LIST_WAVES = 16, LIST_STEP = 8;                  // ids of a lane and step
+__global__ __launch_bounds__(64 * LIST_WAVES) void expert_lists_kernel(const int32_t *ids, int n, int experts, int top_k, int tile_rows, int max_tiles,
+                                                                      int *sorted, int *token_of, MxTile *tiles)
 {
     __shared__ int counts[MAX_EXPERTS];
-    __shared__ int found[4];
+    __shared__ int found[LIST_WAVES];
     __shared__ int begin_, tile_;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, mine = blockIdx.x;
-    for (int e = tid; e < experts; e += 256) counts[e] = 0;
+    for (int e = tid; e < experts; e += 64 * LIST_WAVES) counts[e] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += 256) {
-        const int id = ids[i];
-        if (id >= 0 && id < experts) atomicAdd(&counts[id], 1);
+    const int run = (n + 64 * LIST_WAVES - 1) / (64 * LIST_WAVES) * 64, from = wave * run, to = from + run < n ? from + run : n;
+    int own = 0;
+    for (int i0 = from; i0 < to; i0 += 64 * LIST_STEP) {
+        int id[LIST_STEP];
+#pragma unroll
+        for (int k = 0; k < LIST_STEP; ++k) {
+            const int i = i0 + 64 * k + lane;
+            id[k] = i < to ? ids[i] : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < LIST_STEP; ++k) {
+            own += __popcll(__ballot(id[k] == mine));
+            if (id[k] >= 0 && id[k] < experts) atomicAdd(&counts[id[k]], 1);
+        }
     }
+    if (lane == 0) found[wave] = own;
     __syncthreads();
     if (wave == 0) {
         int before = 0, tiles_before = 0;
@@ -249,28 +264,34 @@ __global__ __launch_bounds__(256) void expert_lists_kernel(const int32_t *ids, i
         if (lane == 0) { begin_ = before; tile_ = tiles_before; }
     }
     __syncthreads();
-    const int begin = begin_, count = counts[mine];
-    const int own = (count + tile_rows - 1) / tile_rows;
-    for (int t = tid; t < own; t += 256) {
+    const int begin = begin_, count = counts[mine], pieces = (count + tile_rows - 1) / tile_rows;
+    for (int t = tid; t < pieces; t += 64 * LIST_WAVES) {
         const int first = t * tile_rows, left = count - first;
         tiles[tile_ + t] = {mine, begin + first, left < tile_rows ? left : tile_rows, 0};
     }
     if (mine == experts - 1)
-        for (int t = tile_ + own + tid; t < max_tiles; t += 256) tiles[t] = {0, 0, 0, 0};
+        for (int t = tile_ + pieces + tid; t < max_tiles; t += 64 * LIST_WAVES) tiles[t] = {0, 0, 0, 0};
+    if (own == 0) return;
     int place = begin;
-    for (int i0 = 0; i0 < n && place < begin + count; i0 += 256) {
-        const int i = i0 + tid;
-        const bool hit = i < n && ids[i] == mine;
-        const uint64_t who = __ballot(hit);
-        if (lane == 0) found[wave] = __popcll(who);
-        __syncthreads();
-        int at = place + __popcll(who & ((1ull << lane) - 1));
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) at += found[w];
-            place += found[w];
+    for (int w = 0; w < wave; ++w) place += found[w];
+    for (int i0 = from; i0 < to; i0 += 64 * LIST_STEP) {
+        int id[LIST_STEP];
+#pragma unroll
+        for (int k = 0; k < LIST_STEP; ++k) {
+            const int i = i0 + 64 * k + lane;
+            id[k] = i < to ? ids[i] : -1;
         }
-        if (hit) sorted[at] = i;
-        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < LIST_STEP; ++k) {
+            const int i = i0 + 64 * k + lane;
+            const uint64_t who = __ballot(id[k] == mine);
+            if (id[k] == mine) {
+                const int at = place + __popcll(who & ((1ull << lane) - 1));
+                sorted[at] = i;
+                token_of[at] = i / top_k;
+            }
+            place += __popcll(who);
+        }
     }
 }
 
@@ -346,9 +367,11 @@ int sbits_launch_route_backward(sbits_ctx *ctx, const sbits_router &r, const voi
     return SBITS_OK;
 }
 
-int sbits_launch_expert_lists(sbits_ctx *ctx, const int32_t *ids, int n, int experts, int tile_rows, int max_tiles, int *sorted, MxTile *tiles)
+int sbits_launch_expert_lists(sbits_ctx *ctx, const int32_t *ids, int n, int experts, int top_k, int tile_rows, int max_tiles, int *sorted, int *tokens,
+                              MxTile *tiles)
 {
-    hipLaunchKernelGGL(expert_lists_kernel, dim3((unsigned)experts), dim3(256), 0, ctx->stream, ids, n, experts, tile_rows, max_tiles, sorted, tiles);
+    hipLaunchKernelGGL(expert_lists_kernel, dim3((unsigned)experts), dim3(64 * LIST_WAVES), 0, ctx->stream, ids, n, experts, top_k, tile_rows, max_tiles, sorted,
+                       tokens, tiles);
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;
 }
