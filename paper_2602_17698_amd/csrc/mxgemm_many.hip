@@ -13,6 +13,8 @@
 // Order of W's rows: tile t of a wave has rows NT n + t, n = l % 32, so that a lane's outputs for a row of x are NT neighbours, a wave's 32 NT.
 // With gated products tiles 2 p and 2 p + 1 are rows NT / 2 n + p of both halves of W.
 // LDS: the pieces of a row are permuted (xor) by bits of the row's number, so that 16 rows of one piece lie in different banks.
+#include <algorithm>
+
 #include "mx_core.hpp"
 
 namespace sbits {
@@ -39,8 +41,11 @@ constexpr int ROW = 128, PIECES = 8;               // bytes, pieces of a row of 
 constexpr int SCALE_ROW = RUN / MX_BLOCK;          // bytes of a row of scales
 __device__ __forceinline__ int piece_at(int slot, int p) { return p ^ (slot >> 1 & 7); }       // where piece p of a row lies, and what lies there
 
+// Buffers of x and of W: two where tiles fill LDS; with 64 rows of x, whose steps are shorter than a load takes, more.
+template <bool X4, int MT> constexpr int x_buffers() { return MT > 1 ? 2 : X4 ? 3 : 4; }
+template <bool X4, int MT> constexpr int w_buffers() { return MT > 1 ? 2 : 3; }
 template <bool X4, int MT, int NT>
-constexpr int many_lds() { return 2 * 64 * ((MT + NT) * ROW + (NT + (X4 ? MT : 0)) * SCALE_ROW); }
+constexpr int many_lds() { return 64 * ((x_buffers<X4, MT>() * MT + w_buffers<X4, MT>() * NT) * ROW + 2 * (NT + (X4 ? MT : 0)) * SCALE_ROW); }
 
 template <bool X4, bool GATED, int MT, int NT>
 __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
@@ -52,7 +57,8 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     constexpr int XL = XBYTES / 4096, WL = WBYTES / 4096, LOADS = XL + WL / WSTEPS;        // a wave's loads of a step of x, of a chunk of W; in a step
     constexpr int SROWS = WROWS + (X4 ? XROWS : 0);                // rows with scales: W's, then x's
     constexpr int SLOADS = SROWS * SCALE_ROW / 1024, SL = (SLOADS + 3) / 4;                // loads of a run of them; a wave's
-    constexpr int W_AT = 2 * XBYTES, S_AT = W_AT + 2 * WBYTES;     // in LDS, behind two buffers of x
+    constexpr int XD = x_buffers<X4, MT>(), WD = w_buffers<X4, MT>();
+    constexpr int W_AT = XD * XBYTES, S_AT = W_AT + WD * WBYTES;   // in LDS, behind the buffers of x
     static_assert(WL % WSTEPS == 0, "as many loads in every step");
     extern __shared__ unsigned char smem[];
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
@@ -122,17 +128,17 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     static_assert(XL % 2 == 0 && WL % 2 == 0, "a lane's piece goes by the load's number's lowest bit");
     const int piece[2] = {piece_at(lane / 8, lane % 8), piece_at(8 + lane / 8, lane % 8)};
     // (begin: the first of the four, or of a phase's)
-    auto fetch_x = [&](int step, auto i_, bool begin) {
+    auto fetch_x = [&](uint32_t step, auto i_, bool begin) {
         constexpr int i = decltype(i_)::value;
-        const uint32_t at = piece[i & 1] * (COLS / PIECES) < cols - step * COLS ? x_at[i] : NOWHERE;
-        if (begin || i % 4 == 0) set_m0(lds + (uint32_t)(step & 1) * XBYTES + (uint32_t)wave * (XL * 1024) + i / 4 * 4096);
-        load_to_lds<1024 * (i & 3)>(at, xr, (uint32_t)step * ROW);
+        const uint32_t at = piece[i & 1] * (COLS / PIECES) < cols - (int)step * COLS ? x_at[i] : NOWHERE;
+        if (begin || i % 4 == 0) set_m0(lds + (uint32_t)(step % XD) * XBYTES + (uint32_t)wave * (XL * 1024) + i / 4 * 4096);
+        load_to_lds<1024 * (i & 3)>(at, xr, step * ROW);
     };
-    auto fetch_w = [&](int chunk, auto i_, bool begin) {
+    auto fetch_w = [&](uint32_t chunk, auto i_, bool begin) {
         constexpr int i = decltype(i_)::value;
-        const uint32_t at = piece[i & 1] * (CHUNK / PIECES) < cols - chunk * CHUNK ? w_at[i] : NOWHERE;
-        if (begin || i % 4 == 0) set_m0(lds + W_AT + (uint32_t)(chunk & 1) * WBYTES + (uint32_t)wave * (WL * 1024) + i / 4 * 4096);
-        load_to_lds<1024 * (i & 3)>(at, wr, (uint32_t)chunk * ROW);
+        const uint32_t at = piece[i & 1] * (CHUNK / PIECES) < cols - (int)chunk * CHUNK ? w_at[i] : NOWHERE;
+        if (begin || i % 4 == 0) set_m0(lds + W_AT + (uint32_t)(chunk % WD) * WBYTES + (uint32_t)wave * (WL * 1024) + i / 4 * 4096);
+        load_to_lds<1024 * (i & 3)>(at, wr, chunk * ROW);
     };
     auto fetch_scales = [&](int run) {
         const int left = cols / MX_BLOCK - SCALE_ROW * run;      // blocks
@@ -171,11 +177,11 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     const int wx = wave >> 1, ww = wave & 1, n = lane & 31, h = lane >> 5;
     auto x_frag = [&](int step, int m, int p) {
         const int slot = wx * 32 * MT + m * 32 + n;
-        return *reinterpret_cast<const u32x4 *>(smem + (step & 1) * XBYTES + slot * ROW + 16 * piece_at(slot, p));
+        return *reinterpret_cast<const u32x4 *>(smem + (uint32_t)step % XD * XBYTES + slot * ROW + 16 * piece_at(slot, p));
     };
     auto w_frag = [&](int chunk, int k, int p) {
         const int slot = ww * 32 * NT + k * 32 + n;
-        return *reinterpret_cast<const u32x4 *>(smem + W_AT + (chunk & 1) * WBYTES + slot * ROW + 16 * piece_at(slot, p));
+        return *reinterpret_cast<const u32x4 *>(smem + W_AT + (uint32_t)chunk % WD * WBYTES + slot * ROW + 16 * piece_at(slot, p));
     };
     auto scale_at = [&](int step, int slot) {
         constexpr int STEPS = RUN / COLS;
@@ -190,21 +196,28 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[m][k][r] = 0.0f;
 
-    // the loads behind the barrier of a step: x of the step after the next, a share of the chunk of W after the one of the next (after: the step's
-    // place, and the next one's, in its chunk)
+    // the loads behind the barrier of a step: x of step + XD, a share of the chunk of W that is WD - 1 after the next step's (next: the next
+    // step's place in its chunk)
     auto load = [&](int step, auto next_, auto i_, bool begin) {
         constexpr int i = decltype(i_)::value, next = decltype(next_)::value;
-        if constexpr (i < XL) fetch_x(step + 2, i_, begin);
-        else fetch_w((step + 1) / WSTEPS + 1, std::integral_constant<int, next * (WL / WSTEPS) + i - XL>{}, begin || i == XL);
+        if constexpr (i < XL) fetch_x(step + XD, i_, begin);
+        else fetch_w((step + 1) / WSTEPS + WD - 1, std::integral_constant<int, next * (WL / WSTEPS) + i - XL>{}, begin || i == XL);
     };
     constexpr int EARLY = LOADS / 2;                               // loads in the last phase; the others are in the first of the next step
+    // How many loads may be under way at a step's barrier: those of the steps behind the one that brought x of the next, and of those behind the one
+    // that brought the last share of its chunk.  (At the start: behind x and W of step 1 as many were asked for, or more.)
+    constexpr int FLYING = std::min(XD - 2, WSTEPS * (WD - 2)) * LOADS;
+    static_assert((WD - 2) * WL + (XD > 3 ? (XD - 3) * XL : 0) + LOADS >= FLYING && (WD == 2) == (XD == 2), "the first waits");
     int zero = 0;
     asm volatile("" : "+s"(zero));                                 // (offsets in registers, also where they are known)
     fetch_scales(zero);
     static_for<0, XL>([&](auto i) { fetch_x(zero, i, false); });
     static_for<0, WL>([&](auto i) { fetch_w(zero, i, false); });
+    if constexpr (XD > 2) static_for<0, XL>([&](auto i) { fetch_x(zero + 1, i, false); });
+    static_for<1, WD - 1>([&](auto c) { static_for<0, WL>([&](auto i) { fetch_w(zero + decltype(c)::value, i, false); }); });
+    static_for<2, XD - 1>([&](auto s) { static_for<0, XL>([&](auto i) { fetch_x(zero + decltype(s)::value, i, false); }); });
     static_for<0, EARLY>([&](auto i) { load(zero - 1, std::integral_constant<int, 0>{}, i, false); });
-    wait_and_meet<EARLY>();
+    wait_and_meet<(XD - 2) * XL + (WD - 2) * WL + EARLY>();
 
     // The loop's instructions stay in the order of the source: one wave to a SIMD, so what is issued between two matrix instructions has to fit
     // the time of one of them.  Left to itself the compiler reads operands just before their use (8192 x 14336 x 4096 in 4 bits: 426 us instead of 346).
@@ -256,7 +269,7 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
         static_for<0, 4>([&](auto q_) {
             constexpr int q = decltype(q_)::value;
             if constexpr (q == 3) {
-                wait_and_meet<0>();
+                wait_and_meet<FLYING>();
                 __builtin_amdgcn_sched_barrier(0);
             }
             // what is done behind the products of a phase: reads of the next one's operands (ahead of a step, of scales and codes, too),
