@@ -8,19 +8,17 @@
 namespace sbits {
 
 // ---- few rows of x -----------------------------------------------------------------
-// A workgroup takes T tiles of 16 rows of W (gated: half of them of each half) and one of up to 16 rows of x; its 8 waves take a group of U runs of
-// 128 columns in turn and add up in LDS.  Lane l has row l % 16 of a tile and block l / 16 of a run: 16 bytes of codes.  The codes of a group are asked
+// A workgroup takes T tiles of 16 rows of W (gated: half of them of each half) and one of up to 16 rows of x; its WAVES waves take a group of U runs
+// of 128 columns in turn and add up in LDS.  Lane l has row l % 16 of a tile and block l / 16 of a run: 16 bytes of codes.  The codes of a group are asked
 // for ahead of the products of the one before.
 // D layout: W's row l % 16, x's row 4 (l / 16) + r.
-constexpr int FEW_WAVES = 8;
-
 template <int T, int U>
 struct FewGroup { u32x4 codes[T][U], scales[T]; };    // scales: of the row's 4 U blocks in the group, a byte each
 
-template <bool X4, bool GATED, int T, int U>
-__global__ __launch_bounds__(64 * FEW_WAVES, T * U > 4 ? 2 : 4) void mx_gemm_few_kernel(MxGemm g)
+template <bool X4, bool GATED, int WAVES, int T, int U>
+__global__ __launch_bounds__(64 * WAVES, T * U > 8 ? 2 : 3) void mx_gemm_few_kernel(MxGemm g)
 {
-    __shared__ float red[FEW_WAVES][T][4][64];
+    __shared__ float red[WAVES][T][4][64];
     MxTile t = {0, (int)blockIdx.y * 16, 0, 0};
     if (g.tiles) {
         t = g.tiles[blockIdx.y];
@@ -117,8 +115,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, T * U > 4 ? 2 : 4) void mx_gemm_few
     if (wave < groups) {
         FewGroup<T, U> now, next;
         load(wave, now);
-        for (int c = wave; c < groups; c += FEW_WAVES) {
-            if (c + FEW_WAVES < groups) load(c + FEW_WAVES, next);
+        for (int c = wave; c < groups; c += WAVES) {
+            if (c + WAVES < groups) load(c + WAVES, next);
             multiply(c, now);
             now = next;
         }
@@ -128,13 +126,13 @@ __global__ __launch_bounds__(64 * FEW_WAVES, T * U > 4 ? 2 : 4) void mx_gemm_few
 #pragma unroll
         for (int r = 0; r < 4; ++r) red[wave][k][r][lane] = acc[k][r];
     __syncthreads();
-    for (int p = tid; p < OUTS * t.count; p += 64 * FEW_WAVES) {
+    for (int p = tid; p < OUTS * t.count; p += 64 * WAVES) {
         const int i = p % OUTS, b = p / OUTS;
         if (out0 + i >= g.outs) continue;
         auto sum = [&](int k, int n_) {
             float v = red[0][k][b & 3][(b >> 2) * 16 + n_];
 #pragma unroll
-            for (int w_ = 1; w_ < FEW_WAVES; ++w_) v += red[w_][k][b & 3][(b >> 2) * 16 + n_];
+            for (int w_ = 1; w_ < WAVES; ++w_) v += red[w_][k][b & 3][(b >> 2) * 16 + n_];
             return v;
         };
         const float v = GATED ? silu_mul(sum(i >> 4, i & 15), sum(HALF + (i >> 4), i & 15)) : sum(i >> 4, i & 15);
@@ -159,26 +157,23 @@ int sbits_mx_tile_rows(int64_t rows_per_matrix, int64_t w_bytes, int64_t x_bytes
 
 // Tiles of W to a workgroup: 4, if the CUs are three quarters busy with that, else 2 or 1.  One token, bf16: 14336 x 4096 with 1, 2, 4 tiles 12.0, 10.6,
 // 9.9 us, with 16 rows of x 22.4, 16.3, 12.6 (x is read once for every workgroup); 4096 x 14336 10.2, 14.5, 28.8, with 16 rows 19.5, 23.0, 36.6.
-// Runs to a group: 4, or as many as leave a group for each wave.
-template <bool X4, bool GATED, int T>
-static auto few_runs(int cols)
-{
-    const int runs = (cols + 127) / 128;
-    return runs <= FEW_WAVES ? mx_gemm_few_kernel<X4, GATED, T, 1> : runs <= 2 * FEW_WAVES ? mx_gemm_few_kernel<X4, GATED, T, 2> : mx_gemm_few_kernel<X4, GATED, T, 4>;
-}
+// Rows of up to 2048 columns by 4 waves with 2 runs to a group, wider ones by 8 with 4: 110 products of 2048 x 2048 with a row or two of x each 28.7 and
+// 37.0 us, one of 14336 x 4096 12.4 and 10.2.
 template <bool X4, bool GATED>
-static auto few_instance(const sbits_ctx *ctx, const MxGemm &g, int tiles, int &outs)
+static auto few_instance(const sbits_ctx *ctx, const MxGemm &g, int tiles, int &outs, int &waves)
 {
     const int64_t enough = (int64_t)sbits_cus(ctx) * 3 / 4, rows = (int64_t)g.w_rows * tiles;
+    const bool narrow = g.cols <= 2048;
+    waves = narrow ? 4 : 8;
     outs = 64 / (GATED ? 2 : 1);
-    if (rows >= 64 * enough) return few_runs<X4, GATED, 4>(g.cols);
+    if (rows >= 64 * enough) return narrow ? mx_gemm_few_kernel<X4, GATED, 4, 4, 2> : mx_gemm_few_kernel<X4, GATED, 8, 4, 4>;
     outs /= 2;
     if constexpr (!GATED)
         if (rows < 32 * enough) {
             outs = 16;
-            return few_runs<X4, GATED, 1>(g.cols);
+            return narrow ? mx_gemm_few_kernel<X4, GATED, 4, 1, 2> : mx_gemm_few_kernel<X4, GATED, 8, 1, 4>;
         }
-    return few_runs<X4, GATED, 2>(g.cols);
+    return narrow ? mx_gemm_few_kernel<X4, GATED, 4, 2, 2> : mx_gemm_few_kernel<X4, GATED, 8, 2, 4>;
 }
 
 int sbits_launch_mx_gemm(sbits_ctx *ctx, const MxGemm &g)
@@ -186,9 +181,9 @@ int sbits_launch_mx_gemm(sbits_ctx *ctx, const MxGemm &g)
     if (g.tile_rows > 16) return sbits_launch_mx_gemm_many(ctx, g);
     const bool x4 = g.xs != nullptr;
     const int tiles = g.tiles ? g.n_tiles : (int)((g.batch + g.tile_rows - 1) / g.tile_rows);
-    int outs;
-    auto fn = x4 ? (g.gated ? few_instance<true, true>(ctx, g, tiles, outs) : few_instance<true, false>(ctx, g, tiles, outs))
-                 : (g.gated ? few_instance<false, true>(ctx, g, tiles, outs) : few_instance<false, false>(ctx, g, tiles, outs));
+    int outs, waves;
+    auto fn = x4 ? (g.gated ? few_instance<true, true>(ctx, g, tiles, outs, waves) : few_instance<true, false>(ctx, g, tiles, outs, waves))
+                 : (g.gated ? few_instance<false, true>(ctx, g, tiles, outs, waves) : few_instance<false, false>(ctx, g, tiles, outs, waves));
     for (int first = 0; first < tiles; first += 65535) {
         MxGemm part = g;
         const int n = tiles - first < 65535 ? tiles - first : 65535;
@@ -201,7 +196,7 @@ int sbits_launch_mx_gemm(sbits_ctx *ctx, const MxGemm &g)
             part.y = static_cast<char *>(g.y) + skip * g.ld_y * (g.y_bf16 ? 2 : 4);
             part.batch = g.batch - skip;
         }
-        hipLaunchKernelGGL(fn, dim3((unsigned)((g.outs + outs - 1) / outs), (unsigned)n), dim3(64 * FEW_WAVES), 0, ctx->stream, part);
+        hipLaunchKernelGGL(fn, dim3((unsigned)((g.outs + outs - 1) / outs), (unsigned)n), dim3(64 * waves), 0, ctx->stream, part);
         SBITS_HIP(ctx, hipGetLastError());
     }
     return SBITS_OK;

@@ -4,13 +4,19 @@
 namespace sbits {
 
 // ---- the choice ------------------------------------------------------------------
+// A wave a token.  Groups lie in `lanes` = 2^k neighbouring lanes each (64 without groups): expert i of group g is in lane g * lanes + i % lanes,
+// register i / lanes.
+//
+// Which experts are taken is decided as with scores in 64 bits, but scores are computed in fp32 first, with a bound on how far each
+// may be off; only where the bounds leave the choice or its order open (a token in some hundred) the wave goes on to 64 bits.  In 64 bits for every
+// token 16384 x 256 took 52 us.  Instruction issue bounds it: top_k searches of the largest key, some 30 instructions each.
 struct RouteArgs {
     const void *logits;
     const float *bias;
     int32_t *ids;
     float *weights;
     int64_t ld, tokens;
-    int experts, top_k, groups, top_groups, each;   // each: experts of a group
+    int experts, top_k, groups, top_groups, each, log_lanes;   // each: experts of a group
     int sigmoid, best_only, renormalize;
 };
 
@@ -20,93 +26,107 @@ __device__ __forceinline__ float logit_at(const void *p, int64_t at)
     if constexpr (BF16) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[at] << 16);
     else return static_cast<const float *>(p)[at];
 }
-__device__ __forceinline__ double wave_sum(double v)
+
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+// all lanes get f over the 2^LOG lanes of their run (f commutative and associative; sums: by pairs)
+template <int LOG, class V, class F>
+__device__ __forceinline__ V over_lanes(V v, F f)
 {
-    for (int s = 1; s < 64; s <<= 1) v += __shfl_xor(v, s);
+    auto bits = [](V x) { return __builtin_bit_cast(int, x); };
+    auto back = [](int x) { return __builtin_bit_cast(V, x); };
+    if constexpr (LOG >= 1) v = f(v, back(dpp<DPP_XOR1>(bits(v))));
+    if constexpr (LOG >= 2) v = f(v, back(dpp<DPP_XOR2>(bits(v))));
+    if constexpr (LOG >= 3) v = f(v, back(dpp<DPP_HALF_MIRROR>(bits(v))));
+    if constexpr (LOG >= 4) v = f(v, back(dpp<DPP_MIRROR>(bits(v))));
+    if constexpr (LOG >= 5) {
+        auto w = __builtin_amdgcn_permlane16_swap(bits(v), bits(v), false, false);
+        v = f(back((int)w[0]), back((int)w[1]));
+    }
+    if constexpr (LOG >= 6) {
+        auto w = __builtin_amdgcn_permlane32_swap(bits(v), bits(v), false, false);
+        v = f(back((int)w[0]), back((int)w[1]));
+    }
     return v;
 }
-__device__ __forceinline__ float wave_max(float v)
+struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
+struct Largest { __device__ __forceinline__ int operator()(int a, int b) const { return max(a, b); } };
+struct Smallest { __device__ __forceinline__ int operator()(int a, int b) const { return min(a, b); } };
+
+// whole numbers in the order of the numbers (0 and -0 the same)
+constexpr int NONE = INT32_MIN;                                 // below every number's
+__device__ __forceinline__ int ordered(float v)
 {
-    for (int s = 1; s < 64; s <<= 1) v = fmaxf(v, __shfl_xor(v, s));
-    return v;
+    const int b = __float_as_int(v + 0.0f);
+    return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float unordered(int o) { return __int_as_float(o ^ ((o >> 31) & 0x7fffffff)); }
+
+// e^v, off by 2 units in the last place at most (see silu_mul)
+__device__ __forceinline__ float exp_of(float v)
+{
+    constexpr float LOG2E = 0x1.715476p+0f, LOG2E_REST = 0x1.4ae0cp-26f, LN2 = 0x1.62e43p-1f;
+    const float t = v * LOG2E, rest = fmaf(v, LOG2E_REST, fmaf(v, LOG2E, -t)), e = __builtin_amdgcn_exp2f(t);
+    return t > 120.0f ? e : fmaf(e, rest * LN2, e);
 }
 
-// A wave a token; lane l has experts l * PER .. l * PER + PER - 1.
-template <bool BF16, int PER>
-__global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
+// The choice in 64 bits: lane j < top_k gets the j-th expert, or -1, and its p.
+template <int PER>
+__device__ __forceinline__ void choose_exactly(const RouteArgs &a, int lane, const float (&x)[PER], const float (&b)[PER], const bool (&fine)[PER], float top,
+                                                         int &id, float &p_of)
 {
-    __shared__ double scores[4][64 * PER];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t token = (int64_t)blockIdx.x * 4 + wave;
-    if (token >= a.tokens) return;
     const double none = -HUGE_VAL;
-    float x[PER];
-    double p[PER], key[PER];
-    bool fine[PER];
-    float top = -HUGE_VALF;
+    const int lanes = 1 << a.log_lanes, first = (lane >> a.log_lanes) * a.each + (lane & (lanes - 1));
+    double p[PER], key[PER], sum = 0.0;
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
-        const int e = lane * PER + r;
-        x[r] = e < a.experts ? logit_at<BF16>(a.logits, token * a.ld + e) : -HUGE_VALF;
-        fine[r] = fabsf(x[r]) < HUGE_VALF;
-        if (fine[r]) top = fmaxf(top, x[r]);
+        const bool there = fabsf(x[r]) < HUGE_VALF;
+        p[r] = !there ? 0.0 : a.sigmoid ? 1.0 / (1.0 + exp(-(double)x[r])) : exp((double)x[r] - (double)top);
+        sum += p[r];
     }
-    top = wave_max(top);
-    if (a.sigmoid) {
+    for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
 #pragma unroll
-        for (int r = 0; r < PER; ++r) p[r] = fine[r] ? 1.0 / (1.0 + exp(-(double)x[r])) : 0.0;
-    } else {
-        double sum = 0.0;
+    for (int r = 0; r < PER; ++r) {
+        if (!a.sigmoid) p[r] = sum > 0.0 ? p[r] / sum : 0.0;
+        key[r] = fine[r] ? p[r] + (double)b[r] : none;
+    }
+    if (a.groups > 1) {
+        double best = none, second = none;
 #pragma unroll
         for (int r = 0; r < PER; ++r) {
-            p[r] = fine[r] ? exp((double)x[r] - (double)top) : 0.0;
-            sum += p[r];
+            if (key[r] > best) { second = best; best = key[r]; }
+            else if (key[r] > second) second = key[r];
         }
-        sum = wave_sum(sum);
-#pragma unroll
-        for (int r = 0; r < PER; ++r) p[r] = fine[r] ? p[r] / sum : 0.0;
-    }
-#pragma unroll
-    for (int r = 0; r < PER; ++r) {
-        const int e = lane * PER + r;
-        const float b = a.bias && e < a.experts ? a.bias[e] : 0.0f;
-        fine[r] = fine[r] && fabsf(b) < HUGE_VALF;
-        // (without a bias the logits have the same order, also where scores round to the same)
-        key[r] = !fine[r] ? none : a.bias ? p[r] + (double)b : (double)x[r];
-        if (a.groups > 1) scores[wave][e] = !fine[r] ? none : a.bias ? key[r] : p[r];
-    }
-    if (a.groups > 1) {                                   // (a wave's own part of LDS: in order without a barrier)
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        double g = none;
-        if (lane < a.groups) {
-            double first = none, second = none;
-            for (int i = 0; i < a.each; ++i) {
-                const double s = scores[wave][lane * a.each + i];
-                if (s > first) { second = first; first = s; }
-                else if (s > second) second = s;
-            }
-            g = a.best_only || second == none ? first : first + second;
+        for (int s = 1; s < lanes; s <<= 1) {
+            const double o1 = __shfl_xor(best, s), o2 = __shfl_xor(second, s);
+            second = fmax(fmin(best, o1), fmax(second, o2));
+            best = fmax(best, o1);
         }
+        const double worth = a.best_only || second == none ? best : best + second;
         int rank = 0;
+        const int mine = lane >> a.log_lanes;
         for (int o = 0; o < a.groups; ++o) {
-            const double other = __shfl(g, o);
-            rank += other > g || (other == g && o < lane);
+            const double other = __shfl(worth, o << a.log_lanes);
+            rank += other > worth || (other == worth && o < mine);
         }
-        const uint64_t open = __ballot(lane < a.groups && rank < a.top_groups);
 #pragma unroll
         for (int r = 0; r < PER; ++r) {
-            const int e = lane * PER + r;
-            if (e < a.experts && !(open >> (e / a.each) & 1)) key[r] = none;
+            if (rank >= a.top_groups) key[r] = none;
+            else if (!a.bias && fine[r]) key[r] = (double)x[r];
         }
-    }
-    int my_id = -1;
-    double my_p = 0.0, total = 0.0;
-    for (int j = 0; j < a.top_k; ++j) {
-        double best = key[0];
-        int at = lane * PER;
+    } else if (!a.bias) {
 #pragma unroll
-        for (int r = 1; r < PER; ++r)
-            if (key[r] > best) { best = key[r]; at = lane * PER + r; }
+        for (int r = 0; r < PER; ++r)
+            if (fine[r]) key[r] = (double)x[r];
+    }
+    id = -1;
+    p_of = 0.0f;
+    for (int j = 0; j < a.top_k; ++j) {
+        double best = none;
+        int at = INT32_MAX;
+#pragma unroll
+        for (int r = 0; r < PER; ++r)
+            if (key[r] > best) { best = key[r]; at = first + r * lanes; }
         for (int s = 1; s < 64; s <<= 1) {
             const double other = __shfl_xor(best, s);
             const int o = __shfl_xor(at, s);
@@ -116,15 +136,139 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
         double w = 0.0;
 #pragma unroll
         for (int r = 0; r < PER; ++r)
-            if (lane * PER + r == at) { w = p[r]; key[r] = none; }
-        w = __shfl(w, at / PER);
-        total += w;
-        if (lane == j) { my_id = at; my_p = w; }
+            if (key[r] > none && first + r * lanes == at) { w = p[r]; key[r] = none; }
+        for (int s = 1; s < 64; s <<= 1) w += __shfl_xor(w, s);
+        if (lane == j) { id = at; p_of = (float)w; }
     }
+}
+
+template <bool BF16, int PER>
+__global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t token = (int64_t)blockIdx.x * 4 + wave;
+    if (token >= a.tokens) return;
+    const int lanes = 1 << a.log_lanes, group = lane >> a.log_lanes, in_group = lane & (lanes - 1), first = group * a.each + in_group;
+    float x[PER], b[PER], p[PER];
+    bool fine[PER];
+    int key[PER], top_key = NONE;
+#pragma unroll
+    for (int r = 0; r < PER; ++r) {
+        const bool there = group < a.groups && r * lanes + in_group < a.each;
+        x[r] = there ? logit_at<BF16>(a.logits, token * a.ld + first + r * lanes) : -HUGE_VALF;
+        b[r] = a.bias && there ? a.bias[first + r * lanes] : 0.0f;
+    }
+#pragma unroll
+    for (int r = 0; r < PER; ++r) {
+        const bool there = fabsf(x[r]) < HUGE_VALF;
+        fine[r] = there && fabsf(b[r]) < HUGE_VALF;
+        if (there) top_key = max(top_key, ordered(x[r]));
+    }
+    top_key = over_lanes<6>(top_key, Largest{});
+    const float top = top_key == NONE ? 0.0f : unordered(top_key);
+    if (a.sigmoid) {
+#pragma unroll
+        for (int r = 0; r < PER; ++r) p[r] = fabsf(x[r]) < HUGE_VALF ? __builtin_amdgcn_rcpf(1.0f + exp_of(-x[r])) : 0.0f;
+    } else {
+        float sum = 0.0f;
+#pragma unroll
+        for (int r = 0; r < PER; ++r) {
+            p[r] = fabsf(x[r]) < HUGE_VALF ? exp_of(x[r] - top) : 0.0f;
+            sum += p[r];
+        }
+        const float one_by = __builtin_amdgcn_rcpf(fmaxf(over_lanes<6>(sum, Add{}), 1e-30f));
+#pragma unroll
+        for (int r = 0; r < PER; ++r) p[r] *= one_by;
+    }
+    // Scores p + b, each off by less than 2^-18 p + 2^-22 |b|: exp and reciprocal 4 units in the last place, an argument x - top that was rounded
+    // (2^-24 |x - top|: p is below e^-|x - top|, and 16 p (1 + log 1 / p) 2^-24 is the same bound for all but p < e^-60), a sum of PER + 6 additions; the
+    // addition of b another 2^-24 (p + |b|).
+    auto off = [&](int r) { return fmaf(0x1p-18f, p[r], 0x1p-22f * fabsf(b[r])); };
+    bool open = false;                                          // whether fp32 leaves the choice open
+#pragma unroll
+    for (int r = 0; r < PER; ++r) key[r] = !fine[r] ? NONE : ordered(a.bias ? p[r] + b[r] : x[r]);
+    if (a.groups > 1) {
+        int best = NONE, second = NONE;
+        float most_off = 0.0f;
+#pragma unroll
+        for (int r = 0; r < PER; ++r) {
+            const int v = !fine[r] ? NONE : a.bias ? key[r] : ordered(p[r]);
+            second = max(second, min(best, v));
+            best = max(best, v);
+            if (fine[r]) most_off = fmaxf(most_off, off(r));
+        }
+        // (lane by lane within a group; of a run of lanes, all get the same)
+        for (int s = 1; s < lanes; s <<= 1) {
+            const int o1 = __shfl_xor(best, s), o2 = __shfl_xor(second, s);
+            second = max(min(best, o1), max(second, o2));
+            best = max(best, o1);
+        }
+        most_off = __int_as_float(over_lanes<6>(__float_as_int(most_off), Largest{}));      // (not negative: in the order of the bits)
+        const float worth = best == NONE ? -HUGE_VALF : a.best_only || second == NONE ? unordered(best) : unordered(best) + unordered(second);
+        int rank = 0;
+        float least_in = HUGE_VALF, most_out = -HUGE_VALF;
+        for (int o = 0; o < a.groups; ++o) {
+            const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(worth), o << a.log_lanes));
+            rank += other > worth || (other == worth && o < group);
+        }
+        const bool in = rank < a.top_groups;
+        if (group < a.groups && worth > -HUGE_VALF) (in ? least_in : most_out) = worth;
+        least_in = unordered(over_lanes<6>(ordered(least_in), Smallest{}));
+        most_out = unordered(over_lanes<6>(ordered(most_out), Largest{}));
+        open = least_in - most_out <= 4.0f * most_off + 0x1p-22f * fabsf(least_in);         // (false where either is infinite)
+#pragma unroll
+        for (int r = 0; r < PER; ++r)
+            if (!in) key[r] = NONE;
+    }
+    int my_id = -1, my_key = NONE;
+    float my_p = 0.0f, my_off = 0.0f;
+    for (int j = 0; j < a.top_k; ++j) {
+        int best = key[0];
+#pragma unroll
+        for (int r = 1; r < PER; ++r) best = max(best, key[r]);
+        const int all = over_lanes<6>(best, Largest{});
+        if (all == NONE) break;
+        // the lowest expert with this key: the lane's lowest, then, if there is more than one lane, the lowest of the lanes
+        int at = INT32_MAX;
+        float pw = 0.0f, ow = 0.0f;
+#pragma unroll
+        for (int r = PER - 1; r >= 0; --r)
+            if (key[r] == all) { at = first + r * lanes; pw = p[r]; ow = off(r); }
+        const uint64_t who = __ballot(best == all);
+        int winner = __ffsll((unsigned long long)who) - 1;
+        if (who & (who - 1)) {
+            const int lowest = over_lanes<6>(at, Smallest{});
+            winner = __ffsll((unsigned long long)__ballot(at == lowest)) - 1;
+        }
+#pragma unroll
+        for (int r = 0; r < PER; ++r)
+            if (lane == winner && at == first + r * lanes) key[r] = NONE;
+        const int id = __builtin_amdgcn_readlane(at, winner);
+        const float pj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(pw), winner));
+        const float oj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ow), winner));
+        if (lane == j) { my_id = id; my_p = pj; my_key = all; my_off = oj; }
+    }
+    if (a.bias) {                                               // (without a bias keys are the logits themselves)
+        // each chosen score against the next, the last against all that are left
+        const uint64_t some = __ballot(my_id >= 0);
+        const int n = __popcll(some);
+        const float v = unordered(my_key);
+        const float next = __shfl_down(v, 1), next_off = __shfl_down(my_off, 1);
+        bool close = lane + 1 < n && v - next <= my_off + next_off;
+        if (n > 0) {
+            const float last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v - my_off), n - 1));
+#pragma unroll
+            for (int r = 0; r < PER; ++r)
+                if (key[r] != NONE && unordered(key[r]) + off(r) >= last) close = true;
+        }
+        open = open || __ballot(close) != 0;
+    }
+    if (open) choose_exactly<PER>(a, lane, x, b, fine, top, my_id, my_p);
+    const float total = a.renormalize ? over_lanes<6>(my_p, Add{}) : 1.0f;
     if (lane < a.top_k) {
-        if (a.renormalize) my_p = total > 0.0 ? my_p / total : 0.0;
+        if (a.renormalize) my_p = total > 0.0f ? my_p / total : 0.0f;
         a.ids[token * a.top_k + lane] = my_id;
-        a.weights[token * a.top_k + lane] = (float)my_p;
+        a.weights[token * a.top_k + lane] = my_p;
     }
 }
 
@@ -143,11 +287,7 @@ struct RouteBackArgs {
     int experts, top_k, sigmoid, renormalize;
 };
 
-__device__ __forceinline__ float wave_sum(float v)
-{
-    for (int s = 1; s < 64; s <<= 1) v += __shfl_xor(v, s);
-    return v;
-}
+__device__ __forceinline__ float wave_sum(float v) { return over_lanes<6>(v, Add{}); }
 
 template <bool BF16, int PER>
 __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
@@ -163,7 +303,7 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
         x[r] = e < a.experts ? logit_at<BF16>(a.logits, token * a.ld + e) : -HUGE_VALF;
         if (fabsf(x[r]) < HUGE_VALF) top = fmaxf(top, x[r]);
     }
-    top = wave_max(top);
+    top = unordered(over_lanes<6>(ordered(top), Largest{}));
     int id = -1;
     float d = 0.0f, c = 0.0f;                                  // lane j < top_k: the j-th chosen expert, its e^x or p
     if (lane < a.top_k) {
@@ -331,9 +471,9 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a)
 using namespace sbits;
 
 template <bool BF16>
-static auto route_instance(int experts)
+static auto route_instance(int per)
 {
-    return experts <= 64 ? route_kernel<BF16, 1> : experts <= 128 ? route_kernel<BF16, 2> : experts <= 256 ? route_kernel<BF16, 4> : route_kernel<BF16, 8>;
+    return per <= 1 ? route_kernel<BF16, 1> : per <= 2 ? route_kernel<BF16, 2> : per <= 4 ? route_kernel<BF16, 4> : per <= 8 ? route_kernel<BF16, 8> : route_kernel<BF16, 16>;
 }
 template <bool BF16>
 static auto route_backward_instance(int experts)
@@ -349,7 +489,10 @@ int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits
     a.logits = logits; a.bias = bias; a.ids = ids; a.weights = weights; a.ld = ld; a.tokens = tokens;
     a.experts = r.experts; a.top_k = r.top_k; a.groups = r.groups; a.top_groups = r.top_groups; a.each = r.experts / r.groups;
     a.sigmoid = r.scoring == SBITS_ROUTE_SIGMOID; a.best_only = r.group_score == SBITS_ROUTE_GROUP_MAX; a.renormalize = r.renormalize;
-    auto fn = bf16 ? route_instance<true>(r.experts) : route_instance<false>(r.experts);
+    a.log_lanes = 0;
+    while (r.groups << (a.log_lanes + 1) <= 64) ++a.log_lanes;
+    const int per = (a.each + (1 << a.log_lanes) - 1) >> a.log_lanes;                    // at most 15: at least 33 lanes are in use
+    auto fn = bf16 ? route_instance<true>(per) : route_instance<false>(per);
     hipLaunchKernelGGL(fn, dim3((unsigned)((tokens + 3) / 4)), dim3(256), 0, ctx->stream, a);
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;
