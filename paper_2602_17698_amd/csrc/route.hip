@@ -72,12 +72,20 @@ __device__ __forceinline__ float exp_of(float v)
 
 // The choice in 64 bits: lane j < top_k gets the j-th expert, or -1, and its p.
 template <int PER>
-__device__ __forceinline__ void choose_exactly(const RouteArgs &a, int lane, const float (&x)[PER], const float (&b)[PER], const bool (&fine)[PER], float top,
-                                                         int &id, float &p_of)
+__device__ __forceinline__ void choose_exactly(const RouteArgs &a, int lane, const float (&x)[PER], const float (&b)[PER], int &id, float &p_of)
 {
     const double none = -HUGE_VAL;
     const int lanes = 1 << a.log_lanes, first = (lane >> a.log_lanes) * a.each + (lane & (lanes - 1));
     double p[PER], key[PER], sum = 0.0;
+    int top_key = NONE;
+    bool fine[PER];
+#pragma unroll
+    for (int r = 0; r < PER; ++r) {
+        fine[r] = fabsf(x[r]) < HUGE_VALF && fabsf(b[r]) < HUGE_VALF;
+        if (fabsf(x[r]) < HUGE_VALF) top_key = max(top_key, ordered(x[r]));
+    }
+    top_key = over_lanes<6>(top_key, Largest{});
+    const float top = top_key == NONE ? 0.0f : unordered(top_key);
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
         const bool there = fabsf(x[r]) < HUGE_VALF;
@@ -150,7 +158,6 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
     if (token >= a.tokens) return;
     const int lanes = 1 << a.log_lanes, group = lane >> a.log_lanes, in_group = lane & (lanes - 1), first = group * a.each + in_group;
     float x[PER], b[PER], p[PER];
-    bool fine[PER];
     int key[PER], top_key = NONE;
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
@@ -158,44 +165,41 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
         x[r] = there ? logit_at<BF16>(a.logits, token * a.ld + first + r * lanes) : -HUGE_VALF;
         b[r] = a.bias && there ? a.bias[first + r * lanes] : 0.0f;
     }
+    float top = 0.0f, one_by = 1.0f;
+    if (!a.sigmoid) {
 #pragma unroll
-    for (int r = 0; r < PER; ++r) {
-        const bool there = fabsf(x[r]) < HUGE_VALF;
-        fine[r] = there && fabsf(b[r]) < HUGE_VALF;
-        if (there) top_key = max(top_key, ordered(x[r]));
-    }
-    top_key = over_lanes<6>(top_key, Largest{});
-    const float top = top_key == NONE ? 0.0f : unordered(top_key);
-    if (a.sigmoid) {
-#pragma unroll
-        for (int r = 0; r < PER; ++r) p[r] = fabsf(x[r]) < HUGE_VALF ? __builtin_amdgcn_rcpf(1.0f + exp_of(-x[r])) : 0.0f;
-    } else {
+        for (int r = 0; r < PER; ++r)
+            if (fabsf(x[r]) < HUGE_VALF) top_key = max(top_key, ordered(x[r]));
+        top_key = over_lanes<6>(top_key, Largest{});
+        top = top_key == NONE ? 0.0f : unordered(top_key);
         float sum = 0.0f;
 #pragma unroll
         for (int r = 0; r < PER; ++r) {
             p[r] = fabsf(x[r]) < HUGE_VALF ? exp_of(x[r] - top) : 0.0f;
             sum += p[r];
         }
-        const float one_by = __builtin_amdgcn_rcpf(fmaxf(over_lanes<6>(sum, Add{}), 1e-30f));
-#pragma unroll
-        for (int r = 0; r < PER; ++r) p[r] *= one_by;
+        one_by = __builtin_amdgcn_rcpf(fmaxf(over_lanes<6>(sum, Add{}), 1e-30f));
     }
-    // Scores p + b, each off by less than 2^-18 p + 2^-22 |b|: exp and reciprocal 4 units in the last place, an argument x - top that was rounded
-    // (2^-24 |x - top|: p is below e^-|x - top|, and 16 p (1 + log 1 / p) 2^-24 is the same bound for all but p < e^-60), a sum of PER + 6 additions; the
-    // addition of b another 2^-24 (p + |b|).
-    auto off = [&](int r) { return fmaf(0x1p-18f, p[r], 0x1p-22f * fabsf(b[r])); };
+    auto chance = [&](float v) { return a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + exp_of(-v)) : exp_of(v - top) * one_by; };
+    // Scores p + b, each off by less than by_p * p + 2^-22 |p + b|.  by_p: of a sigmoid 2^-21 (exp and reciprocal 4 units in the last place), of softmax
+    // 2^-18 (also an argument x - top that was rounded, 2^-24 |x - top|: p is below e^-|x - top|, and 16 p (1 + log 1 / p) 2^-24 is the same bound
+    // for all but p < e^-60; a sum of PER + 6 additions).
+    const float by_p = a.sigmoid ? 0x1p-21f : 0x1p-18f;
     bool open = false;                                          // whether fp32 leaves the choice open
-#pragma unroll
-    for (int r = 0; r < PER; ++r) key[r] = !fine[r] ? NONE : ordered(a.bias ? p[r] + b[r] : x[r]);
-    if (a.groups > 1) {
-        int best = NONE, second = NONE;
-        float most_off = 0.0f;
+    if (a.bias || a.groups > 1) {
 #pragma unroll
         for (int r = 0; r < PER; ++r) {
-            const int v = !fine[r] ? NONE : a.bias ? key[r] : ordered(p[r]);
-            second = max(second, min(best, v));
-            best = max(best, v);
-            if (fine[r]) most_off = fmaxf(most_off, off(r));
+            p[r] = !(fabsf(x[r]) < HUGE_VALF) ? 0.0f : a.sigmoid ? chance(x[r]) : p[r] * one_by;
+            const float v = a.bias ? p[r] + b[r] : p[r];
+            key[r] = fabsf(x[r]) < HUGE_VALF && fabsf(v) < HUGE_VALF ? ordered(v) : NONE;
+        }
+    }
+    if (a.groups > 1) {
+        int best = NONE, second = NONE;
+#pragma unroll
+        for (int r = 0; r < PER; ++r) {
+            second = max(second, min(best, key[r]));
+            best = max(best, key[r]);
         }
         // (lane by lane within a group; of a run of lanes, all get the same)
         for (int s = 1; s < lanes; s <<= 1) {
@@ -203,25 +207,27 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
             second = max(min(best, o1), max(second, o2));
             best = max(best, o1);
         }
-        most_off = __int_as_float(over_lanes<6>(__float_as_int(most_off), Largest{}));      // (not negative: in the order of the bits)
-        const float worth = best == NONE ? -HUGE_VALF : a.best_only || second == NONE ? unordered(best) : unordered(best) + unordered(second);
+        const float v1 = unordered(best), v2 = unordered(second);
+        const float worth = best == NONE ? -HUGE_VALF : a.best_only || second == NONE ? v1 : v1 + v2;
+        // two groups' sums are certain to be as they seem if they are further apart than both may be off: four scores, two of them of this group
+        // (twice as far where the other two are as large; no p is above one_by, that of the largest logit)
+        const float tolerance = 4.0f * by_p * one_by + 0x1p-20f * (fabsf(v1) + (second == NONE ? 0.0f : fabsf(v2)));
         int rank = 0;
-        float least_in = HUGE_VALF, most_out = -HUGE_VALF;
         for (int o = 0; o < a.groups; ++o) {
             const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(worth), o << a.log_lanes));
             rank += other > worth || (other == worth && o < group);
+            open = open || (o != group && fabsf(other - worth) <= tolerance);           // (not where one of them is infinite)
         }
-        const bool in = rank < a.top_groups;
-        if (group < a.groups && worth > -HUGE_VALF) (in ? least_in : most_out) = worth;
-        least_in = unordered(over_lanes<6>(ordered(least_in), Smallest{}));
-        most_out = unordered(over_lanes<6>(ordered(most_out), Largest{}));
-        open = least_in - most_out <= 4.0f * most_off + 0x1p-22f * fabsf(least_in);         // (false where either is infinite)
+        open = a.top_groups < a.groups && group < a.groups && open;
 #pragma unroll
         for (int r = 0; r < PER; ++r)
-            if (!in) key[r] = NONE;
+            if (rank >= a.top_groups) key[r] = NONE;
+    }
+    if (!a.bias) {                                              // the logits have the order of the scores, also where those round to the same
+#pragma unroll
+        for (int r = 0; r < PER; ++r) key[r] = fabsf(x[r]) < HUGE_VALF && (a.groups == 1 || key[r] != NONE) ? ordered(x[r]) : NONE;
     }
     int my_id = -1, my_key = NONE;
-    float my_p = 0.0f, my_off = 0.0f;
     for (int j = 0; j < a.top_k; ++j) {
         int best = key[0];
 #pragma unroll
@@ -229,41 +235,40 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
         const int all = over_lanes<6>(best, Largest{});
         if (all == NONE) break;
         // the lowest expert with this key: the lane's lowest, then, if there is more than one lane, the lowest of the lanes
-        int at = INT32_MAX;
-        float pw = 0.0f, ow = 0.0f;
+        int reg = PER - 1;
 #pragma unroll
-        for (int r = PER - 1; r >= 0; --r)
-            if (key[r] == all) { at = first + r * lanes; pw = p[r]; ow = off(r); }
+        for (int r = PER - 2; r >= 0; --r) reg = key[r] == all ? r : reg;
         const uint64_t who = __ballot(best == all);
         int winner = __ffsll((unsigned long long)who) - 1;
+        const int at = first + reg * lanes;
         if (who & (who - 1)) {
-            const int lowest = over_lanes<6>(at, Smallest{});
-            winner = __ffsll((unsigned long long)__ballot(at == lowest)) - 1;
+            const int lowest = over_lanes<6>(best == all ? at : INT32_MAX, Smallest{});
+            winner = __ffsll((unsigned long long)__ballot(best == all && at == lowest)) - 1;
         }
+        const int taken = lane == winner ? reg : -1;
 #pragma unroll
-        for (int r = 0; r < PER; ++r)
-            if (lane == winner && at == first + r * lanes) key[r] = NONE;
+        for (int r = 0; r < PER; ++r) key[r] = taken == r ? NONE : key[r];
         const int id = __builtin_amdgcn_readlane(at, winner);
-        const float pj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(pw), winner));
-        const float oj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ow), winner));
-        if (lane == j) { my_id = id; my_p = pj; my_key = all; my_off = oj; }
+        if (lane == j) { my_id = id; my_key = all; }
     }
+    float my_p = 0.0f;
+    if (my_id >= 0) my_p = chance(logit_at<BF16>(a.logits, token * a.ld + my_id));
     if (a.bias) {                                               // (without a bias keys are the logits themselves)
         // each chosen score against the next, the last against all that are left
-        const uint64_t some = __ballot(my_id >= 0);
-        const int n = __popcll(some);
-        const float v = unordered(my_key);
-        const float next = __shfl_down(v, 1), next_off = __shfl_down(my_off, 1);
-        bool close = lane + 1 < n && v - next <= my_off + next_off;
+        const int n = __popcll(__ballot(my_id >= 0));
+        const float v = unordered(my_key), my_off = fmaf(by_p, my_p, 0x1p-22f * fabsf(v));
+        bool close = lane + 1 < n && v - my_off <= __shfl_down(v + my_off, 1);
         if (n > 0) {
             const float last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v - my_off), n - 1));
 #pragma unroll
-            for (int r = 0; r < PER; ++r)
-                if (key[r] != NONE && unordered(key[r]) + off(r) >= last) close = true;
+            for (int r = 0; r < PER; ++r) {
+                const float u = unordered(key[r]);
+                close = close || (key[r] != NONE && fmaf(by_p, p[r], fmaf(0x1p-22f, fabsf(u), u)) >= last);
+            }
         }
-        open = open || __ballot(close) != 0;
+        open = open || close;
     }
-    if (open) choose_exactly<PER>(a, lane, x, b, fine, top, my_id, my_p);
+    if (__ballot(open) != 0) choose_exactly<PER>(a, lane, x, b, my_id, my_p);
     const float total = a.renormalize ? over_lanes<6>(my_p, Add{}) : 1.0f;
     if (lane < a.top_k) {
         if (a.renormalize) my_p = total > 0.0f ? my_p / total : 0.0f;
