@@ -62,12 +62,12 @@ __device__ __forceinline__ int ordered(float v)
 }
 __device__ __forceinline__ float unordered(int o) { return __int_as_float(o ^ ((o >> 31) & 0x7fffffff)); }
 
-// e^v, off by 2 units in the last place at most (see silu_mul)
+// e^v, off by 2 units in the last place at most (see silu_mul) for |v| < 83, by 2^-17 below, 0 at -infinity
 __device__ __forceinline__ float exp_of(float v)
 {
     constexpr float LOG2E = 0x1.715476p+0f, LOG2E_REST = 0x1.4ae0cp-26f, LN2 = 0x1.62e43p-1f;
     const float t = v * LOG2E, rest = fmaf(v, LOG2E_REST, fmaf(v, LOG2E, -t)), e = __builtin_amdgcn_exp2f(t);
-    return t > 120.0f ? e : fmaf(e, rest * LN2, e);
+    return fabsf(t) < 120.0f ? fmaf(e, rest * LN2, e) : e;
 }
 
 // The choice in 64 bits: lane j < top_k gets the j-th expert, or -1, and its p.
@@ -165,17 +165,19 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
         x[r] = there ? logit_at<BF16>(a.logits, token * a.ld + first + r * lanes) : -HUGE_VALF;
         b[r] = a.bias && there ? a.bias[first + r * lanes] : 0.0f;
     }
+#pragma unroll
+    for (int r = 0; r < PER; ++r) x[r] = fabsf(x[r]) < HUGE_VALF ? x[r] : -HUGE_VALF;         // (p = 0 below, without a branch)
     float top = 0.0f, one_by = 1.0f;
     if (!a.sigmoid) {
 #pragma unroll
         for (int r = 0; r < PER; ++r)
-            if (fabsf(x[r]) < HUGE_VALF) top_key = max(top_key, ordered(x[r]));
-        top_key = over_lanes<6>(top_key, Largest{});
-        top = top_key == NONE ? 0.0f : unordered(top_key);
+            top_key = max(top_key, ordered(x[r]));
+        top = unordered(over_lanes<6>(top_key, Largest{}));
+        if (top == -HUGE_VALF) top = 0.0f;
         float sum = 0.0f;
 #pragma unroll
         for (int r = 0; r < PER; ++r) {
-            p[r] = fabsf(x[r]) < HUGE_VALF ? exp_of(x[r] - top) : 0.0f;
+            p[r] = exp_of(x[r] - top);
             sum += p[r];
         }
         one_by = __builtin_amdgcn_rcpf(fmaxf(over_lanes<6>(sum, Add{}), 1e-30f));
@@ -189,9 +191,10 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
     if (a.bias || a.groups > 1) {
 #pragma unroll
         for (int r = 0; r < PER; ++r) {
-            p[r] = !(fabsf(x[r]) < HUGE_VALF) ? 0.0f : a.sigmoid ? chance(x[r]) : p[r] * one_by;
-            const float v = a.bias ? p[r] + b[r] : p[r];
-            key[r] = fabsf(x[r]) < HUGE_VALF && fabsf(v) < HUGE_VALF ? ordered(v) : NONE;
+            if (a.sigmoid) p[r] = __builtin_amdgcn_rcpf(1.0f + exp_of(-x[r]));
+            else p[r] *= one_by;
+            const float v = p[r] + b[r];
+            key[r] = x[r] > -HUGE_VALF && fabsf(v) < HUGE_VALF ? ordered(v) : NONE;
         }
     }
     if (a.groups > 1) {
@@ -225,7 +228,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
     }
     if (!a.bias) {                                              // the logits have the order of the scores, also where those round to the same
 #pragma unroll
-        for (int r = 0; r < PER; ++r) key[r] = fabsf(x[r]) < HUGE_VALF && (a.groups == 1 || key[r] != NONE) ? ordered(x[r]) : NONE;
+        for (int r = 0; r < PER; ++r) key[r] = x[r] > -HUGE_VALF && (a.groups == 1 || key[r] != NONE) ? ordered(x[r]) : NONE;
     }
     int my_id = -1, my_key = NONE;
     for (int j = 0; j < a.top_k; ++j) {
@@ -306,9 +309,11 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
     for (int r = 0; r < PER; ++r) {
         const int e = r * 64 + lane;
         x[r] = e < a.experts ? logit_at<BF16>(a.logits, token * a.ld + e) : -HUGE_VALF;
-        if (fabsf(x[r]) < HUGE_VALF) top = fmaxf(top, x[r]);
+        x[r] = fabsf(x[r]) < HUGE_VALF ? x[r] : -HUGE_VALF;
+        top = fmaxf(top, x[r]);
     }
     top = unordered(over_lanes<6>(ordered(top), Largest{}));
+    if (top == -HUGE_VALF) top = 0.0f;
     int id = -1;
     float d = 0.0f, c = 0.0f;                                  // lane j < top_k: the j-th chosen expert, its e^x or p
     if (lane < a.top_k) {
@@ -317,20 +322,20 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
         if (id >= 0) {
             d = a.d_weights[token * a.top_k + lane];
             const float v = logit_at<BF16>(a.logits, token * a.ld + id);
-            if (fabsf(v) < HUGE_VALF) c = a.sigmoid ? 1.0f / (1.0f + expf(-v)) : expf(v - top);
+            if (fabsf(v) < HUGE_VALF) c = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + exp_of(-v)) : exp_of(v - top);
         }
     }
-    float all = 1.0f;
+    float all = 1.0f;                                          // 1 / sum e^(x - top)
     float e[PER];
     if (!a.sigmoid && !a.renormalize) {
         float sum = 0.0f;
 #pragma unroll
         for (int r = 0; r < PER; ++r) {
-            e[r] = fabsf(x[r]) < HUGE_VALF ? expf(x[r] - top) : 0.0f;
+            e[r] = exp_of(x[r] - top);
             sum += e[r];
         }
-        all = wave_sum(sum);
-        c = all > 0.0f ? c / all : 0.0f;
+        all = __builtin_amdgcn_rcpf(fmaxf(wave_sum(sum), 1e-30f));
+        c *= all;
     }
     float g;                                                   // of the chosen experts
     float dot = 0.0f;
@@ -349,8 +354,8 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
 #pragma unroll
     for (int r = 0; r < PER; ++r) spread[r] = 0.0f;
     for (int j = 0; j < a.top_k; ++j) {
-        const int at = __shfl(id, j);
-        const float v = __shfl(g, j);
+        const int at = __builtin_amdgcn_readlane(id, j);
+        const float v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), j));
 #pragma unroll
         for (int r = 0; r < PER; ++r)
             if (at == r * 64 + lane) spread[r] = v;
@@ -358,7 +363,7 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
         const int i = r * 64 + lane;
-        if (!a.sigmoid && !a.renormalize) spread[r] = all > 0.0f ? e[r] / all * (spread[r] - dot) : 0.0f;
+        if (!a.sigmoid && !a.renormalize) spread[r] = e[r] * all * (spread[r] - dot);
         if (i < a.experts) a.d_logits[token * a.ld_d + i] = spread[r];
     }
 }
