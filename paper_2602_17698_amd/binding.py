@@ -211,18 +211,27 @@ def _pitch(t) -> int:
     return row
 
 
+_types = {}                     # torch.dtype -> its number here (filled on first use: the search's calls do not import torch)
+_INT32 = 100
+
+
+def _kind(t) -> int:
+    if not _types:
+        import torch
+        _types.update({torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16, torch.int32: _INT32})
+    return _types.get(t.dtype, -1)
+
+
 def _type(t) -> int:
-    name = str(t.dtype)
-    if name == "torch.bfloat16":
-        return TYPE_BF16
-    if name == "torch.float32":
-        return TYPE_FP32
-    raise TypeError("bfloat16 or float32 expected, not " + name)
+    kind = _kind(t)
+    if kind != TYPE_BF16 and kind != TYPE_FP32:
+        raise TypeError("bfloat16 or float32 expected, not %s" % t.dtype)
+    return kind
 
 
-def _is(t, name, what):
-    if str(t.dtype) != name:
-        raise TypeError("%s: %s expected, not %s" % (what, name, t.dtype))
+def _is(t, kind, what):
+    if _kind(t) != kind:
+        raise TypeError("%s may not be in %s" % (what, t.dtype))
 
 
 class Context:
@@ -241,10 +250,10 @@ class Context:
     # ---- layers with 4-bit floating point weights (see scalebits.h) ---------------------
     def mx_quantize(self, x, q: Mx, values=None):
         """x (bf16 or fp32) to q's codes and scales; values (bf16, may be None): what they stand for."""
-        if tuple(x.shape) != (q.rows, q.cols) or (values is not None and values.shape != x.shape):
+        if x.shape != (q.rows, q.cols) or (values is not None and values.shape != x.shape):
             raise ValueError("x, q and values differ in shape")
         if values is not None:
-            _is(values, "torch.bfloat16", "values")
+            _is(values, TYPE_BF16, "values")
         return _check(load().sbits_mx_quantize(self.h, x.data_ptr(), _type(x), _pitch(x), C.addressof(q),
                                                values.data_ptr() if values is not None else None,
                                                _pitch(values) if values is not None else 0), "sbits_mx_quantize")
@@ -261,8 +270,8 @@ class Context:
         if isinstance(x, Mx):
             bf16, ld, four = None, 0, C.addressof(x)
         else:
-            _is(x, "torch.bfloat16", "x")
-            if tuple(x.shape) != (batch, w.cols):
+            _is(x, TYPE_BF16, "x")
+            if x.shape != (batch, w.cols):
                 raise ValueError("x is not [%d, %d]" % (batch, w.cols))
             bf16, ld, four = x.data_ptr(), _pitch(x), None
         return _check(load().sbits_mx_gemm(self.h, C.addressof(w), bf16, ld, four, batch, 1 if gated else 0, y.data_ptr(), _type(y), _pitch(y),
@@ -279,7 +288,7 @@ class Context:
     def route_backward(self, router: Router, logits, ids, d_weights, d_logits):
         """d_logits (fp32 [tokens, experts]) from the gradient of the weights."""
         tokens = _routed(router, logits, None, ids, d_weights)
-        _is(d_logits, "torch.float32", "d_logits")
+        _is(d_logits, TYPE_FP32, "d_logits")
         if d_logits.shape != logits.shape:
             raise ValueError("d_logits and logits differ in shape")
         return _check(load().sbits_route_backward(self.h, C.addressof(router), logits.data_ptr(), _type(logits), _pitch(logits),
@@ -292,9 +301,9 @@ class Context:
     def expert_layer(self, router: Router, logits, bias, x, up: Mx, down: Mx, out, ids, weights, ws, four_bit: bool = False):
         """out (bf16 [tokens, hidden]) = the weighted sum of the chosen experts' outputs; ids, weights: as route() writes them."""
         tokens = _routed(router, logits, bias, ids, weights)
-        _is(x, "torch.bfloat16", "x")
-        _is(out, "torch.bfloat16", "out")
-        if tuple(x.shape) != (tokens, up.cols) or x.shape != out.shape:
+        _is(x, TYPE_BF16, "x")
+        _is(out, TYPE_BF16, "out")
+        if x.shape != (tokens, up.cols) or x.shape != out.shape:
             raise ValueError("x and out are not [%d, %d]" % (tokens, up.cols))
         return _check(load().sbits_expert_layer(self.h, C.addressof(router), logits.data_ptr(), _type(logits), _pitch(logits),
                                                 bias.data_ptr() if bias is not None else None, x.data_ptr(), _pitch(x), tokens,
@@ -306,15 +315,15 @@ class Context:
 def _routed(router, logits, bias, ids, weights) -> int:
     """Checks of what the calls around a router share; the number of tokens."""
     tokens, experts = logits.shape
-    if experts != router.experts or ids.shape != weights.shape or tuple(ids.shape) != (tokens, router.top_k):
+    if experts != router.experts or ids.shape != weights.shape or ids.shape != (tokens, router.top_k):
         raise ValueError("logits, ids or weights do not fit the router")
     if not (ids.is_contiguous() and weights.is_contiguous()):
         raise ValueError("ids and weights have to be contiguous")
-    _is(ids, "torch.int32", "ids")
-    _is(weights, "torch.float32", "weights")
+    _is(ids, _INT32, "ids")
+    _is(weights, TYPE_FP32, "weights")
     if bias is not None:
-        _is(bias, "torch.float32", "bias")
-        if tuple(bias.shape) != (experts,) or not bias.is_contiguous():
+        _is(bias, TYPE_FP32, "bias")
+        if bias.shape != (experts,) or not bias.is_contiguous():
             raise ValueError("bias is not [experts]")
     return tokens
 

@@ -307,26 +307,32 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     char *const y_base = parts ? reinterpret_cast<char *>(g.part + (int64_t)blockIdx.y * g.batch * g.ld_part) : static_cast<char *>(g.y);
     const int64_t ld_y = parts ? g.ld_part : g.ld_y;
     auto value = [&](int m, int r, int k) { return GATED ? silu_mul(acc[m][2 * k][r], acc[m][2 * k + 1][r]) : acc[m][k][r]; };
-    auto put = [&](auto bf16, auto listed, auto rest) {            // rest: of lanes that have some of their outputs only
-        constexpr bool BF16 = decltype(bf16)::value, LISTED = decltype(listed)::value, REST = decltype(rest)::value;
+    // whole: all rows and outputs of the tile are there; rest: of lanes that have some of their outputs only.  (Checks of a row's own are a branch each:
+    // none in whole tiles.)
+    auto put = [&](auto bf16, auto listed, auto whole, auto rest) {
+        constexpr bool BF16 = decltype(bf16)::value, LISTED = decltype(listed)::value, WHOLE = decltype(whole)::value, REST = decltype(rest)::value;
         const int64_t ld = ld_y * (BF16 ? 2 : 4);
         char *const y0 = y_base + (int64_t)out * (BF16 ? 2 : 4) + (LISTED ? 0 : (t.first + b0 + 4 * h) * ld);
         int rows[MT];                                              // (of all lanes: they are read across lanes below)
-        if (LISTED)
+        if (LISTED) {
 #pragma unroll
             for (int m = 0; m < MT; ++m) rows[m] = b0 + 32 * m + n < t.count ? g.y_row[t.first + b0 + 32 * m + n] : 0;
-        if (REST ? out >= g.outs || out + HAS <= g.outs : !outs_whole && out + HAS > g.outs) return;
+            // (waited for here: in the branches below the compiler would wait for the stores of the branch before, too)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) asm volatile("s_waitcnt vmcnt(0)" : "+v"(rows[m]));
+        }
+        if (REST ? out >= g.outs || out + HAS <= g.outs : !WHOLE && out + HAS > g.outs) return;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 constexpr int H = 4;
                 const int b = 32 * m + 8 * (r / 4) + r % 4;
-                if (!rows_whole && b0 + b + H * h >= t.count) continue;
+                if (!WHOLE && b0 + b + H * h >= t.count) continue;
                 char *y;
                 if constexpr (LISTED) {
                     const int row0 = __builtin_amdgcn_readlane(rows[m], b % 32), row1 = __builtin_amdgcn_readlane(rows[m], b % 32 + H);
-                    y = y0 + (h ? row1 : row0) * ld;
+                    y = y0 + (uint64_t)(uint32_t)(h ? row1 : row0) * (uint32_t)ld;
                 } else {
                     y = y0 + b * ld;
                 }
@@ -346,15 +352,20 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
                 }
             }
     };
-    auto typed = [&](auto listed, auto rest) {
-        if (g.y_bf16 && !parts) put(std::true_type{}, listed, rest);
-        else put(std::false_type{}, listed, rest);
-    };
-    if (GATED || !g.y_row) {
-        typed(std::false_type{}, std::false_type{});
-        if (!outs_whole && g.outs % HAS) typed(std::false_type{}, std::true_type{});
-    } else {                                                       // (rows of a multiple of 32 outputs)
-        put(std::true_type{}, std::true_type{}, std::false_type{});
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    const bool whole = rows_whole && outs_whole;
+    if (!GATED && g.y_row) {                                       // (bf16, rows of a multiple of 32 outputs, below 2^32 bytes)
+        if (whole) put(yes, yes, yes, no);
+        else put(yes, yes, no, no);
+    } else if (g.y_bf16 && !parts) {
+        if (whole) put(yes, no, yes, no);
+        else put(yes, no, no, no);
+        if (!outs_whole && g.outs % HAS) put(yes, no, no, yes);
+    } else {
+        if (whole) put(no, no, yes, no);
+        else put(no, no, no, no);
+        if (!outs_whole && g.outs % HAS) put(no, no, no, yes);
     }
 }
 
