@@ -68,7 +68,7 @@ static LayerSpace layer_space(const sbits_router &r, int64_t tokens, const sbits
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)up_to(bytes, 256); return here; };
     s.sorted = take(s.places * 4);
     s.token = take(s.places * 4);
-    s.tiles = take(tiles(std::min(s.tile_rows, 64)) * (int64_t)sizeof(MxTile));
+    s.tiles = take((tiles(std::min(s.tile_rows, 16)) + 1) * (int64_t)sizeof(MxTile));
     s.h = take(s.places * s.inner * 2);
     s.y = take(s.places * s.hidden * 2);
     s.xq = take(four ? tokens * s.codes_x : 0);

@@ -89,7 +89,7 @@ struct MxGemm {
     int64_t ld_y;                   // elements
     int y_bf16, gated;
     int64_t batch;
-    // a stack of matrices: tiles (n_tiles of them at most, with count 0 where there are none), the rows of x (x_row[s]) and of y (y_row[s])
+    // a stack of matrices: tiles (n_tiles of them at most, with count 0 where there are none, and an entry whose count is how many there are), the rows of x (x_row[s]) and of y (y_row[s])
     // of a place in the sorted list; null: the place itself.  With y_row, y is in bf16 and outs a multiple of 32
     const MxTile *tiles;
     int n_tiles, tile_rows;

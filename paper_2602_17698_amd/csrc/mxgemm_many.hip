@@ -65,63 +65,65 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     // Tiles in an order for the 8 dies: workgroups go to them in turn, and each gets a run of neighbours, 8 tiles of W by as many of x as
-    // follow (what the 32 CUs of a die work on at a time then comes from 8 + 4 tiles).
-    const int wtiles = (g.outs + OUTS - 1) / OUTS, all = wtiles * g.n_tiles;
-    const int die = blockIdx.x & 7, each = all >> 3, more = all & 7;
-    const int id = die * each + (die < more ? die : more) + (int)(blockIdx.x >> 3);
-    const int band = id / (8 * g.n_tiles), in_band = id - band * 8 * g.n_tiles;
-    const int wide = wtiles - 8 * band < 8 ? wtiles - 8 * band : 8;
-    const int xt = in_band / wide, wt = 8 * band + (in_band - xt * wide);
-
-    MxTile t = {0, xt * XROWS, 0, 0};
-    if (g.tiles) {
-        t = g.tiles[xt];
-        if (t.count == 0) return;
-    } else {
-        t.count = (int)(g.batch - t.first < XROWS ? g.batch - t.first : XROWS);
-    }
-    const int out0 = wt * OUTS;
+    // follow (what the 32 CUs of a die work on at a time then comes from 8 + 4 tiles).  A workgroup takes every gridDim.x-th.
+    const int n_tiles = g.tiles ? g.tiles[g.n_tiles].count : g.n_tiles;                    // (of a list, as many as there are)
+    const int wtiles = (g.outs + OUTS - 1) / OUTS, all = wtiles * n_tiles;
     const int chunk0 = (int)blockIdx.y * g.chunks;                 // the part of the columns
     const int cols = g.n_split == 1 || g.cols - chunk0 * CHUNK < g.chunks * CHUNK ? g.cols - chunk0 * CHUNK : g.chunks * CHUNK;
+    const int steps = (cols + COLS - 1) / COLS;
 
     // Where a lane's loads come from: offsets into buffers that begin at the tile's first row of x (with a list of rows: at the first of
     // all) and at the matrix.  Rows and columns that are not there: NOWHERE.  Four loads share an address in LDS and have offsets 0 .. LAST, which count for
     // the memory's address, too: buffers begin LAST bytes ahead, and the offsets here take the load's own away.
-    constexpr int LAST = 3 * 1024;
-    const int64_t x_first = g.x_row ? 0 : t.first, w_first = (int64_t)t.expert * g.w_rows;
-    const rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(static_cast<const uint8_t *>(g.x) + x_first * g.ld_x + (int64_t)chunk0 * (X4 ? ROW : 2 * CHUNK) - LAST), 0, 0x7fffffff, 0x00027000);
-    const rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(g.w + w_first * g.ld_w + (int64_t)chunk0 * ROW - LAST), 0, 0x7fffffff, 0x00027000);
-    const uint8_t *const scales_w = g.ws + w_first * g.ld_ws + chunk0 * (CHUNK / MX_BLOCK);
-    const uint8_t *const scales_x = X4 ? g.xs + x_first * g.ld_xs + chunk0 * (CHUNK / MX_BLOCK) : nullptr;
-    auto x_row = [&](int slot) -> int { return slot >= t.count ? -1 : g.x_row ? g.x_row[t.first + slot] : slot; };
-    auto w_row = [&](int slot) -> int {
-        const int w = slot / (32 * NT), tile = slot / 32 % NT, n = slot % 32;
-        const int out = out0 + (GATED ? w * 16 * NT + n * (NT / 2) + tile / 2 : w * 32 * NT + n * NT + tile);
-        return out >= g.outs ? -1 : GATED && (tile & 1) ? g.outs + out : out;
-    };
     // (32 bits: the caller sees to it that what a tile spans is below 2^31)
+    constexpr int LAST = 3 * 1024;
     const uint32_t ld_x = (uint32_t)g.ld_x, ld_w = (uint32_t)g.ld_w, ld_xs = (uint32_t)g.ld_xs, ld_ws = (uint32_t)g.ld_ws;
-    auto x_slot = [&](int i) { return (wave * XL + i) * 8 + lane / 8; };
-    auto w_slot = [&](int i) { return (wave * WL + i) * 8 + lane / 8; };
+    MxTile t;
+    int out0;
+    const uint8_t *xp, *wp, *scales_w, *scales_x;
     uint32_t x_at[XL], w_at[WL], s_at[SL];
-#pragma unroll
-    for (int i = 0; i < XL; ++i) {
-        const int row = x_row(x_slot(i));
-        x_at[i] = row < 0 ? NOWHERE : row * ld_x + 16 * piece_at(x_slot(i), lane % 8) + LAST - 1024 * (i & 3);
-    }
-#pragma unroll
-    for (int i = 0; i < WL; ++i) {
-        const int row = w_row(w_slot(i));
-        w_at[i] = row < 0 ? NOWHERE : row * ld_w + 16 * piece_at(w_slot(i), lane % 8) + LAST - 1024 * (i & 3);
-    }
+    auto buffer = [](const uint8_t *from) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(from), 0, 0x7fffffff, 0x00027000); };
     auto s_slot = [&](int i) { return (wave + 4 * i) * 32 + lane / 2; };
+    auto set_up = [&](int number) {
+        const int die = number & 7, each = all >> 3, more = all & 7;
+        const int id = die * each + (die < more ? die : more) + (number >> 3);
+        const int band = id / (8 * n_tiles), in_band = id - band * 8 * n_tiles;
+        const int wide = wtiles - 8 * band < 8 ? wtiles - 8 * band : 8;
+        const int xt = in_band / wide;
+        out0 = (8 * band + (in_band - xt * wide)) * OUTS;
+        t = {0, xt * XROWS, 0, 0};
+        if (g.tiles) t = g.tiles[xt];
+        else t.count = (int)(g.batch - t.first < XROWS ? g.batch - t.first : XROWS);
+        const int64_t x_first = g.x_row ? 0 : t.first, w_first = (int64_t)t.expert * g.w_rows;
+        xp = static_cast<const uint8_t *>(g.x) + x_first * g.ld_x + (int64_t)chunk0 * (X4 ? ROW : 2 * CHUNK) - LAST;
+        wp = g.w + w_first * g.ld_w + (int64_t)chunk0 * ROW - LAST;
+        scales_w = g.ws + w_first * g.ld_ws + chunk0 * (CHUNK / MX_BLOCK);
+        scales_x = X4 ? g.xs + x_first * g.ld_xs + chunk0 * (CHUNK / MX_BLOCK) : nullptr;
+        auto x_row = [&](int slot) -> int { return slot >= t.count ? -1 : g.x_row ? g.x_row[t.first + slot] : slot; };
+        auto w_row = [&](int slot) -> int {
+            const int w = slot / (32 * NT), tile = slot / 32 % NT, n = slot % 32;
+            const int out = out0 + (GATED ? w * 16 * NT + n * (NT / 2) + tile / 2 : w * 32 * NT + n * NT + tile);
+            return out >= g.outs ? -1 : GATED && (tile & 1) ? g.outs + out : out;
+        };
+        auto x_slot = [&](int i) { return (wave * XL + i) * 8 + lane / 8; };
+        auto w_slot = [&](int i) { return (wave * WL + i) * 8 + lane / 8; };
 #pragma unroll
-    for (int i = 0; i < SL; ++i) {
-        const bool of_w = (wave + 4 * i) * 32 < WROWS;             // (the same for the whole wave)
-        const int row = of_w ? w_row(s_slot(i)) : (wave + 4 * i) * 32 < SROWS ? x_row(s_slot(i) - WROWS) : -1;
-        s_at[i] = row < 0 ? NOWHERE : row * (of_w ? ld_ws : ld_xs) + 16 * (lane % 2);
-    }
-    const int steps = (cols + COLS - 1) / COLS;
+        for (int i = 0; i < XL; ++i) {
+            const int row = x_row(x_slot(i));
+            x_at[i] = row < 0 ? NOWHERE : row * ld_x + 16 * piece_at(x_slot(i), lane % 8) + LAST - 1024 * (i & 3);
+        }
+#pragma unroll
+        for (int i = 0; i < WL; ++i) {
+            const int row = w_row(w_slot(i));
+            w_at[i] = row < 0 ? NOWHERE : row * ld_w + 16 * piece_at(w_slot(i), lane % 8) + LAST - 1024 * (i & 3);
+        }
+#pragma unroll
+        for (int i = 0; i < SL; ++i) {
+            const bool of_w = (wave + 4 * i) * 32 < WROWS;         // (the same for the whole wave)
+            const int row = of_w ? w_row(s_slot(i)) : (wave + 4 * i) * 32 < SROWS ? x_row(s_slot(i) - WROWS) : -1;
+            s_at[i] = row < 0 ? NOWHERE : row * (of_w ? ld_ws : ld_xs) + 16 * (lane % 2);
+        }
+    };
 
     // Loads of a step, the first XL x's, then the step's share of the next chunk of W.  Pieces behind the last column go NOWHERE: a comparison with
     // every load, as a branch would part the matrix instructions around it.
@@ -132,25 +134,23 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
         constexpr int i = decltype(i_)::value;
         const uint32_t at = piece[i & 1] * (COLS / PIECES) < cols - (int)step * COLS ? x_at[i] : NOWHERE;
         if (begin || i % 4 == 0) set_m0(lds + (uint32_t)(step % XD) * XBYTES + (uint32_t)wave * (XL * 1024) + i / 4 * 4096);
-        load_to_lds<1024 * (i & 3)>(at, xr, step * ROW);
+        load_to_lds<1024 * (i & 3)>(at, buffer(xp), step * ROW);
     };
     auto fetch_w = [&](uint32_t chunk, auto i_, bool begin) {
         constexpr int i = decltype(i_)::value;
         const uint32_t at = piece[i & 1] * (CHUNK / PIECES) < cols - (int)chunk * CHUNK ? w_at[i] : NOWHERE;
         if (begin || i % 4 == 0) set_m0(lds + W_AT + (uint32_t)(chunk % WD) * WBYTES + (uint32_t)wave * (WL * 1024) + i / 4 * 4096);
-        load_to_lds<1024 * (i & 3)>(at, wr, chunk * ROW);
+        load_to_lds<1024 * (i & 3)>(at, buffer(wp), chunk * ROW);
     };
     auto fetch_scales = [&](int run) {
         const int left = cols / MX_BLOCK - SCALE_ROW * run;      // blocks
         const uint32_t to = S_AT + (uint32_t)(run & 1) * (SROWS * SCALE_ROW);
         if (left >= SCALE_ROW) {
-            const rsrc_t sw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(scales_w), 0, 0x7fffffff, 0x00027000);
-            const rsrc_t sx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(X4 ? scales_x : scales_w), 0, 0x7fffffff, 0x00027000);
 #pragma unroll
             for (int i = 0; i < SL; ++i)
                 if (wave + 4 * i < SLOADS) {
                     set_m0(lds + to + (uint32_t)(wave + 4 * i) * 1024);
-                    load_to_lds<0>(s_at[i], (wave + 4 * i) * 32 < WROWS ? sw : sx, (uint32_t)(run * SCALE_ROW));
+                    load_to_lds<0>(s_at[i], buffer((wave + 4 * i) * 32 < WROWS ? scales_w : scales_x), (uint32_t)(run * SCALE_ROW));
                 }
         } else if (left > 0) {                                     // the last bytes of a row, and 1 for what is behind them
 #pragma unroll
@@ -189,12 +189,6 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     };
 
     f32x16 acc[MT][NT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int k = 0; k < NT; ++k)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[m][k][r] = 0.0f;
 
     // the loads behind the barrier of a step: x of step + XD, a share of the chunk of W that is WD - 1 after the next step's (next: the next
     // step's place in its chunk)
@@ -208,16 +202,18 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     // that brought the last share of its chunk.  (At the start: behind x and W of step 1 as many were asked for, or more.)
     constexpr int FLYING = std::min(XD - 2, WSTEPS * (WD - 2)) * LOADS;
     static_assert((WD - 2) * WL + (XD > 3 ? (XD - 3) * XL : 0) + LOADS >= FLYING && (WD == 2) == (XD == 2), "the first waits");
-    int zero = 0;
-    asm volatile("" : "+s"(zero));                                 // (offsets in registers, also where they are known)
-    fetch_scales(zero);
-    static_for<0, XL>([&](auto i) { fetch_x(zero, i, false); });
-    static_for<0, WL>([&](auto i) { fetch_w(zero, i, false); });
-    if constexpr (XD > 2) static_for<0, XL>([&](auto i) { fetch_x(zero + 1, i, false); });
-    static_for<1, WD - 1>([&](auto c) { static_for<0, WL>([&](auto i) { fetch_w(zero + decltype(c)::value, i, false); }); });
-    static_for<2, XD - 1>([&](auto s) { static_for<0, XL>([&](auto i) { fetch_x(zero + decltype(s)::value, i, false); }); });
-    static_for<0, EARLY>([&](auto i) { load(zero - 1, std::integral_constant<int, 0>{}, i, false); });
-    wait_and_meet<(XD - 2) * XL + (WD - 2) * WL + EARLY>();
+    auto start = [&]() {
+        int zero = 0;
+        asm volatile("" : "+s"(zero));                                 // (offsets in registers, also where they are known)
+        fetch_scales(zero);
+        static_for<0, XL>([&](auto i) { fetch_x(zero, i, false); });
+        static_for<0, WL>([&](auto i) { fetch_w(zero, i, false); });
+        if constexpr (XD > 2) static_for<0, XL>([&](auto i) { fetch_x(zero + 1, i, false); });
+        static_for<1, WD - 1>([&](auto c) { static_for<0, WL>([&](auto i) { fetch_w(zero + decltype(c)::value, i, false); }); });
+        static_for<2, XD - 1>([&](auto s) { static_for<0, XL>([&](auto i) { fetch_x(zero + decltype(s)::value, i, false); }); });
+        static_for<0, EARLY>([&](auto i) { load(zero - 1, std::integral_constant<int, 0>{}, i, false); });
+    };
+    constexpr int BEHIND = (XD - 2) * XL + (WD - 2) * WL + EARLY;  // loads behind those of the first step
 
     // The loop's instructions stay in the order of the source: one wave to a SIMD, so what is issued between two matrix instructions has to fit
     // the time of one of them.  Left to itself the compiler reads operands just before their use (8192 x 14336 x 4096 in 4 bits: 426 us instead of 346).
@@ -251,14 +247,6 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
         }
     };
     constexpr int READS = X4 ? MT + NT : MT, SCALES = X4 ? MT + NT : NT, CODES = X4 ? 0 : NT, CONVERTS = X4 ? 0 : NT;
-#pragma unroll
-    for (int i = 0; i < SCALES; ++i) scale(0, i);
-#pragma unroll
-    for (int i = 0; i < CODES; ++i) codes(0, i);
-#pragma unroll
-    for (int i = 0; i < READS; ++i) operand(0, 0, i);
-#pragma unroll
-    for (int i = 0; i < CONVERTS; ++i) convert(0, i);
     auto do_step = [&](const int s, auto u_) {                     // u: the step's place in its chunk
         constexpr int u = decltype(u_)::value;
         if constexpr (X4) {
@@ -293,79 +281,122 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
             });
         });
     };
-    for (int s = 0; s < steps; s += WSTEPS) {                      // whole chunks: what is behind the last column is 0
-        // (what branches is here: the compiler moves matrix instructions across a branch among them, behind what they are to hide)
-        if (s % (RUN / COLS) == 0) fetch_scales(s / (RUN / COLS) + 1);
-        static_for<0, WSTEPS>([&](auto u) { do_step(s + decltype(u)::value, u); });
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // (the loads behind the last step, before LDS goes to another workgroup)
-
     // D layout: W's row lane % 32 of a tile, x's row 8 (r / 4) + 4 h + r % 4
     constexpr int HAS = GATED ? NT / 2 : NT;                       // outputs of a lane, neighbours, for a row of x
-    const int out = out0 + ww * 32 * HAS + n * HAS, b0 = wx * 32 * MT;
-    const bool rows_whole = t.count == XROWS, outs_whole = out0 + OUTS <= g.outs, parts = g.n_split > 1;
-    char *const y_base = parts ? reinterpret_cast<char *>(g.part + (int64_t)blockIdx.y * g.batch * g.ld_part) : static_cast<char *>(g.y);
-    const int64_t ld_y = parts ? g.ld_part : g.ld_y;
-    auto value = [&](int m, int r, int k) { return GATED ? silu_mul(acc[m][2 * k][r], acc[m][2 * k + 1][r]) : acc[m][k][r]; };
-    // whole: all rows and outputs of the tile are there; rest: of lanes that have some of their outputs only.  (Checks of a row's own are a branch each:
-    // none in whole tiles.)
-    auto put = [&](auto bf16, auto listed, auto whole, auto rest) {
-        constexpr bool BF16 = decltype(bf16)::value, LISTED = decltype(listed)::value, WHOLE = decltype(whole)::value, REST = decltype(rest)::value;
-        const int64_t ld = ld_y * (BF16 ? 2 : 4);
-        char *const y0 = y_base + (int64_t)out * (BF16 ? 2 : 4) + (LISTED ? 0 : (t.first + b0 + 4 * h) * ld);
-        int rows[MT];                                              // (of all lanes: they are read across lanes below)
-        if (LISTED) {
+    auto store = [&](const MxTile t, const int out0) {
+        const int out = out0 + ww * 32 * HAS + n * HAS, b0 = wx * 32 * MT;
+        const bool rows_whole = t.count == XROWS, outs_whole = out0 + OUTS <= g.outs, parts = g.n_split > 1;
+        char *const y_base = parts ? reinterpret_cast<char *>(g.part + (int64_t)blockIdx.y * g.batch * g.ld_part) : static_cast<char *>(g.y);
+        const int64_t ld_y = parts ? g.ld_part : g.ld_y;
+        // (taken out of its register here: conversions that several variants of what follows share would be made ahead of them, all at once)
+        auto sum = [&](int m, int r, int k) {
+            float v = acc[m][k][r];
+            asm volatile("" : "+v"(v));
+            return v;
+        };
+        auto value = [&](int m, int r, int k) { return GATED ? silu_mul(sum(m, r, 2 * k), sum(m, r, 2 * k + 1)) : sum(m, r, k); };
+        // whole: all rows and outputs of the tile are there; rest: of lanes that have some of their outputs only.  (Checks of a row's own are a branch each:
+        // none in whole tiles.)
+        auto put = [&](auto bf16, auto listed, auto whole, auto rest) {
+            constexpr bool BF16 = decltype(bf16)::value, LISTED = decltype(listed)::value, WHOLE = decltype(whole)::value, REST = decltype(rest)::value;
+            const int64_t ld = ld_y * (BF16 ? 2 : 4);
+            char *const y0 = y_base + (int64_t)out * (BF16 ? 2 : 4) + (LISTED ? 0 : (t.first + b0 + 4 * h) * ld);
+            int rows[MT];                                              // (of all lanes: they are read across lanes below)
+            if (LISTED) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) rows[m] = b0 + 32 * m + n < t.count ? g.y_row[t.first + b0 + 32 * m + n] : 0;
-            // (waited for here: in the branches below the compiler would wait for the stores of the branch before, too)
+                for (int m = 0; m < MT; ++m) rows[m] = b0 + 32 * m + n < t.count ? g.y_row[t.first + b0 + 32 * m + n] : 0;
+                // (waited for here: in the branches below the compiler would wait for the stores of the branch before, too)
 #pragma unroll
-            for (int m = 0; m < MT; ++m) asm volatile("s_waitcnt vmcnt(0)" : "+v"(rows[m]));
+                for (int m = 0; m < MT; ++m) asm volatile("s_waitcnt vmcnt(0)" : "+v"(rows[m]));
+            }
+            if (REST ? out >= g.outs || out + HAS <= g.outs : !WHOLE && out + HAS > g.outs) return;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    constexpr int H = 4;
+                    const int b = 32 * m + 8 * (r / 4) + r % 4;
+                    if (!WHOLE && b0 + b + H * h >= t.count) continue;
+                    char *y;
+                    if constexpr (LISTED) {
+                        const int row0 = __builtin_amdgcn_readlane(rows[m], b % 32), row1 = __builtin_amdgcn_readlane(rows[m], b % 32 + H);
+                        y = y0 + (uint64_t)(uint32_t)(h ? row1 : row0) * (uint32_t)ld;
+                    } else {
+                        y = y0 + b * ld;
+                    }
+                    if constexpr (REST) {
+#pragma unroll
+                        for (int k = 0; k < HAS; ++k)
+                            if (out + k < g.outs) {
+                                if constexpr (BF16) reinterpret_cast<uint16_t *>(y)[k] = (uint16_t)bf16_round(value(m, r, k));
+                                else reinterpret_cast<float *>(y)[k] = value(m, r, k);
+                            }
+                    } else if constexpr (BF16) {
+                        if constexpr (HAS == 4) *reinterpret_cast<u32x2 *>(y) = u32x2{bf16_pair(value(m, r, 0), value(m, r, 1)), bf16_pair(value(m, r, 2), value(m, r, 3))};
+                        else *reinterpret_cast<uint32_t *>(y) = bf16_pair(value(m, r, 0), value(m, r, 1));
+                    } else {
+                        if constexpr (HAS == 4) *reinterpret_cast<f32x4 *>(y) = f32x4{value(m, r, 0), value(m, r, 1), value(m, r, 2), value(m, r, 3)};
+                        else *reinterpret_cast<float2 *>(y) = make_float2(value(m, r, 0), value(m, r, 1));
+                    }
+                    __builtin_amdgcn_sched_barrier(0);             // (else the addresses of all rows are made ahead, in registers that are not there)
+                }
+        };
+        constexpr std::true_type yes;
+        constexpr std::false_type no;
+        const bool whole = rows_whole && outs_whole;
+        if (!GATED && g.y_row) {                                       // (bf16, rows of a multiple of 32 outputs, below 2^32 bytes)
+            if (whole) put(yes, yes, yes, no);
+            else put(yes, yes, no, no);
+        } else if (g.y_bf16 && !parts) {
+            if (whole) put(yes, no, yes, no);
+            else put(yes, no, no, no);
+            if (!outs_whole && g.outs % HAS) put(yes, no, no, yes);
+        } else {
+            if (whole) put(no, no, yes, no);
+            else put(no, no, no, no);
+            if (!outs_whole && g.outs % HAS) put(no, no, no, yes);
         }
-        if (REST ? out >= g.outs || out + HAS <= g.outs : !WHOLE && out + HAS > g.outs) return;
+    };
+
+    // The next tile's first loads are asked for ahead of the stores of the one before.
+    bool any = false;
+    MxTile done = {};
+    int done_out = 0;
+    for (int number = blockIdx.x;; number += gridDim.x) {
+        const bool next = number < all;
+        if (next) {
+            set_up(number);
+            start();
+        }
+        if (any) store(done, done_out);
+        if (!next) break;
+        // (a whole tile has a store for each of a wave's rows behind the loads; else the stores are waited for, too)
+        if (any && done.count == XROWS && done_out + OUTS <= g.outs) wait_and_meet<std::min(63, BEHIND + 16 * MT)>();
+        else wait_and_meet<BEHIND>();
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                constexpr int H = 4;
-                const int b = 32 * m + 8 * (r / 4) + r % 4;
-                if (!WHOLE && b0 + b + H * h >= t.count) continue;
-                char *y;
-                if constexpr (LISTED) {
-                    const int row0 = __builtin_amdgcn_readlane(rows[m], b % 32), row1 = __builtin_amdgcn_readlane(rows[m], b % 32 + H);
-                    y = y0 + (uint64_t)(uint32_t)(h ? row1 : row0) * (uint32_t)ld;
-                } else {
-                    y = y0 + b * ld;
-                }
-                if constexpr (REST) {
+            for (int k = 0; k < NT; ++k)
 #pragma unroll
-                    for (int k = 0; k < HAS; ++k)
-                        if (out + k < g.outs) {
-                            if constexpr (BF16) reinterpret_cast<uint16_t *>(y)[k] = (uint16_t)bf16_round(value(m, r, k));
-                            else reinterpret_cast<float *>(y)[k] = value(m, r, k);
-                        }
-                } else if constexpr (BF16) {
-                    if constexpr (HAS == 4) *reinterpret_cast<u32x2 *>(y) = u32x2{bf16_pair(value(m, r, 0), value(m, r, 1)), bf16_pair(value(m, r, 2), value(m, r, 3))};
-                    else *reinterpret_cast<uint32_t *>(y) = bf16_pair(value(m, r, 0), value(m, r, 1));
-                } else {
-                    if constexpr (HAS == 4) *reinterpret_cast<f32x4 *>(y) = f32x4{value(m, r, 0), value(m, r, 1), value(m, r, 2), value(m, r, 3)};
-                    else *reinterpret_cast<float2 *>(y) = make_float2(value(m, r, 0), value(m, r, 1));
-                }
-            }
-    };
-    constexpr std::true_type yes;
-    constexpr std::false_type no;
-    const bool whole = rows_whole && outs_whole;
-    if (!GATED && g.y_row) {                                       // (bf16, rows of a multiple of 32 outputs, below 2^32 bytes)
-        if (whole) put(yes, yes, yes, no);
-        else put(yes, yes, no, no);
-    } else if (g.y_bf16 && !parts) {
-        if (whole) put(yes, no, yes, no);
-        else put(yes, no, no, no);
-        if (!outs_whole && g.outs % HAS) put(yes, no, no, yes);
-    } else {
-        if (whole) put(no, no, yes, no);
-        else put(no, no, no, no);
-        if (!outs_whole && g.outs % HAS) put(no, no, no, yes);
+                for (int r = 0; r < 16; ++r) acc[m][k][r] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) scale(0, i);
+#pragma unroll
+        for (int i = 0; i < CODES; ++i) codes(0, i);
+#pragma unroll
+        for (int i = 0; i < READS; ++i) operand(0, 0, i);
+#pragma unroll
+        for (int i = 0; i < CONVERTS; ++i) convert(0, i);
+        for (int s = 0; s < steps; s += WSTEPS) {                      // whole chunks: what is behind the last column is 0
+            // (what branches is here: the compiler moves matrix instructions across a branch among them, behind what they are to hide)
+            if (s % (RUN / COLS) == 0) fetch_scales(s / (RUN / COLS) + 1);
+            static_for<0, WSTEPS>([&](auto u) { do_step(s + decltype(u)::value, u); });
+        }
+        // (the loads behind the last step, ahead of others to the same places, or of LDS for another workgroup)
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        any = true;
+        done = t;
+        done_out = out0;
     }
 }
 
@@ -431,7 +462,9 @@ static int launch(sbits_ctx *ctx, const MxGemm &g)
     SBITS_HIP(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
     MxGemm a = g;
     if (!g.tiles) a.n_tiles = (int)((g.batch + 64 * MT - 1) / (64 * MT));
-    const int64_t all = (int64_t)a.n_tiles * ((g.outs + outs - 1) / outs);
+    // a workgroup for each CU at most, each on the die of its tiles
+    int64_t all = (int64_t)a.n_tiles * ((g.outs + outs - 1) / outs);
+    if (a.n_split == 1) all = std::min(all, (int64_t)std::max(sbits_cus(ctx) / 8 * 8, 8));
     hipLaunchKernelGGL(fn, dim3((unsigned)all, (unsigned)a.n_split), dim3(256), lds, ctx->stream, a);
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;

@@ -370,7 +370,7 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
 
 // ---- lists by expert ---------------------------------------------------------------
 // sorted: the places (token * top_k + j) of all choices, expert after expert, ascending inside one; token_of: their tokens; tiles: pieces of at most
-// tile_rows of an expert's list, expert after expert, then entries with count 0.  A workgroup an expert.  Its waves take consecutive runs
+// tile_rows of an expert's list, expert after expert, then entries with count 0 up to max_tiles, then one whose count is that of the pieces.  A workgroup an expert.  Its waves take consecutive runs
 // of the choices; a wave's first pass counts those of its own expert (by ballots), and of all experts (in LDS, whole numbers: any order
 // gives the same), so the workgroup knows where its list and its tiles begin, a wave where its part does.
 // Bound by the latency of the two passes over the ids, which come from L2: 16384 choices of 32 experts, one id a lane and 256 threads: 42 us.
@@ -419,8 +419,10 @@ __global__ __launch_bounds__(64 * LIST_WAVES) void expert_lists_kernel(const int
         const int first = t * tile_rows, left = count - first;
         tiles[tile_ + t] = {mine, begin + first, left < tile_rows ? left : tile_rows, 0};
     }
-    if (mine == experts - 1)
+    if (mine == experts - 1) {
         for (int t = tile_ + pieces + tid; t < max_tiles; t += 64 * LIST_WAVES) tiles[t] = {0, 0, 0, 0};
+        if (tid == 0) tiles[max_tiles] = {0, 0, tile_ + pieces, 0};
+    }
     if (own == 0) return;
     int place = begin;
     for (int w = 0; w < wave; ++w) place += found[w];
