@@ -42,6 +42,8 @@ static int need_device(sbits_ctx *ctx)
     return SBITS_OK;
 }
 
+static bool near_2gb(int64_t bytes) { return bytes < ((int64_t)1 << 31); }
+
 // the workspace of a layer of experts, as offsets
 struct LayerSpace {
     int64_t tokens, places, hidden, inner;
@@ -49,17 +51,15 @@ struct LayerSpace {
     int64_t codes_x, scales_x, codes_h, scales_h;                  // pitches
     size_t sorted, token, tiles, h, y, xq, xs, hq, hs, bytes;
 };
-static LayerSpace layer_space(const sbits_router &r, int64_t tokens, const sbits_mx &up, const sbits_mx &down, bool four, int64_t ld_x)
+static LayerSpace layer_space(const sbits_ctx *ctx, const sbits_router &r, int64_t tokens, const sbits_mx &up, const sbits_mx &down, bool four, int64_t ld_x)
 {
     LayerSpace s;
     s.tokens = tokens;
     s.places = tokens * r.top_k;
     s.hidden = up.cols;
     s.inner = down.cols;
-    // (space for as many tiles as there are at most, however far apart the rows of x lie)
-    const int64_t rows = (s.places + r.experts - 1) / r.experts;
-    s.tile_rows = sbits_mx_tile_rows(rows, std::max(2 * s.inner * std::max(up.ld_codes, up.ld_scales), s.hidden * std::max(down.ld_codes, down.ld_scales)),
-                                     std::max(tokens * ld_x, 512 * s.inner));
+    const int64_t w_bytes = std::max(2 * s.inner * std::max(up.ld_codes, up.ld_scales), s.hidden * std::max(down.ld_codes, down.ld_scales));
+    s.tile_rows = sbits_mx_cut_layer(ctx, four, near_2gb(w_bytes) && near_2gb(std::max(tokens * ld_x, 512 * s.inner)), r.experts, s.places, s.hidden, s.inner);
     auto tiles = [&](int tile_rows) { return std::min(r.experts + s.places / tile_rows, s.places); };
     s.max_tiles = (int)tiles(s.tile_rows);
     s.codes_x = s.hidden / 2; s.scales_x = sbits_mx_scale_pitch(s.hidden);
@@ -68,7 +68,7 @@ static LayerSpace layer_space(const sbits_router &r, int64_t tokens, const sbits
     auto take = [&](int64_t bytes) { const size_t here = at; at += (size_t)up_to(bytes, 256); return here; };
     s.sorted = take(s.places * 4);
     s.token = take(s.places * 4);
-    s.tiles = take((tiles(std::min(s.tile_rows, 16)) + 1) * (int64_t)sizeof(MxTile));
+    s.tiles = take((tiles(16) + 1) * (int64_t)sizeof(MxTile));            // (for as many as there may be, however far apart the rows of x lie)
     s.h = take(s.places * s.inner * 2);
     s.y = take(s.places * s.hidden * 2);
     s.xq = take(four ? tokens * s.codes_x : 0);
@@ -89,11 +89,10 @@ static int check_layer(const sbits_ctx *ctx, const sbits_router *r, int64_t toke
 }
 
 // how a product is cut up (x_pitch: bytes between rows of x), and the workspace of its parts
-static void product_shape(const sbits_ctx *ctx, const sbits_mx &w, int64_t batch, int64_t x_pitch, MxGemm &g)
+static void product_shape(const sbits_ctx *ctx, const sbits_mx &w, int64_t batch, bool four, int64_t x_pitch, MxGemm &g)
 {
     g.w_rows = w.rows; g.cols = (int)w.cols; g.batch = batch;
-    g.tile_rows = sbits_mx_tile_rows(batch, w.rows * std::max(w.ld_codes, w.ld_scales), 256 * x_pitch);
-    sbits_mx_split(ctx, g);
+    sbits_mx_cut(ctx, four, near_2gb(w.rows * std::max(w.ld_codes, w.ld_scales)) && near_2gb(256 * x_pitch), g);
 }
 static size_t product_space(const MxGemm &g) { return g.n_split == 1 ? 0 : (size_t)g.n_split * g.batch * g.ld_part * 4; }
 
@@ -119,7 +118,7 @@ size_t sbits_mx_gemm_ws_bytes(const sbits_ctx *ctx, const sbits_mx *w, int64_t b
     if (!ctx || check_mx(w) || batch <= 0 || batch > INT32_MAX) return 0;
     (void)gated;
     MxGemm g = {};
-    product_shape(ctx, *w, batch, four_bit ? w->cols / 2 : 2 * w->cols, g);      // (rows of x far apart: no parts)
+    product_shape(ctx, *w, batch, four_bit != 0, four_bit ? w->cols / 2 : 2 * w->cols, g);      // (rows of x far apart: no parts)
     return product_space(g);
 }
 
@@ -141,7 +140,7 @@ int sbits_mx_gemm(sbits_ctx *ctx, const sbits_mx *w, const void *x_bf16, int64_t
     }
     if (!aligned(y, 16) || !pitch(ld_y, outs, 8)) return SBITS_ERR_INVALID_ARG;
     MxGemm g = {};
-    product_shape(ctx, *w, batch, x_mx ? std::max(x_mx->ld_codes, x_mx->ld_scales) : 2 * ld_x, g);
+    product_shape(ctx, *w, batch, x_mx != nullptr, x_mx ? std::max(x_mx->ld_codes, x_mx->ld_scales) : 2 * ld_x, g);
     if (!ws_ok(ws, ws_bytes, product_space(g))) return SBITS_ERR_WORKSPACE;
     if ((rc = need_device(ctx))) return rc;
     g.part = static_cast<float *>(ws);
@@ -185,7 +184,7 @@ int sbits_route_backward(sbits_ctx *ctx, const sbits_router *r, const void *logi
 size_t sbits_expert_layer_ws_bytes(const sbits_ctx *ctx, const sbits_router *r, int64_t tokens, const sbits_mx *up, const sbits_mx *down,
                                    int four_bit)
 {
-    return check_layer(ctx, r, tokens, up, down) ? 0 : layer_space(*r, tokens, *up, *down, four_bit != 0, 0).bytes;
+    return check_layer(ctx, r, tokens, up, down) ? 0 : layer_space(ctx, *r, tokens, *up, *down, four_bit != 0, 0).bytes;
 }
 
 int sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits, int logits_type, int64_t ld_logits, const float *bias,
@@ -199,7 +198,7 @@ int sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits
     if ((bias && !aligned(bias, 4)) || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(x_bf16, 16) || !pitch(ld_x, up->cols, 8) ||
         !aligned(out_bf16, 16) || !pitch(ld_out, up->cols, 8))
         return SBITS_ERR_INVALID_ARG;
-    const LayerSpace s = layer_space(*r, tokens, *up, *down, four_bit != 0, four_bit ? up->cols / 2 : 2 * ld_x);
+    const LayerSpace s = layer_space(ctx, *r, tokens, *up, *down, four_bit != 0, four_bit ? up->cols / 2 : 2 * ld_x);
     if (!ws_ok(ws, ws_bytes, s.bytes)) return SBITS_ERR_WORKSPACE;
     if ((rc = need_device(ctx))) return rc;
     char *const base = static_cast<char *>(ws);

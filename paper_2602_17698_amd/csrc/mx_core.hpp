@@ -104,8 +104,10 @@ struct MxGemm {
 
 // ---- launchers --------------------------------------------------------------
 int sbits_launch_mx_quantize(sbits_ctx *ctx, const void *x, bool bf16, int64_t ld_x, const sbits_mx &q, int64_t rows, void *values, int64_t ld_v);
-int sbits_mx_tile_rows(int64_t rows_per_matrix, int64_t w_bytes, int64_t x_bytes);
-void sbits_mx_split(const sbits_ctx *ctx, sbits::MxGemm &g);
+// how a product is cut up: tile_rows, n_split, chunks and ld_part from w_rows, cols and batch; near: offsets in its matrices are below 2^31
+void sbits_mx_cut(const sbits_ctx *ctx, bool x4, bool near, sbits::MxGemm &g);
+// tile_rows of both products of a layer of experts with so many choices
+int sbits_mx_cut_layer(const sbits_ctx *ctx, bool x4, bool near, int experts, int64_t places, int64_t hidden, int64_t inner);
 int sbits_launch_mx_gemm(sbits_ctx *ctx, const sbits::MxGemm &g);
 int sbits_launch_mx_gemm_many(sbits_ctx *ctx, const sbits::MxGemm &g);
 int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const float *bias, int64_t tokens,

@@ -3,6 +3,9 @@
 //
 // Activations in 4 bits go to the matrix cores as they are: an instruction multiplies blocks of 32 codes and applies both powers of two.
 // With bf16 activations the codes become bf16, exactly (the power of two included), two to an instruction.
+#include <algorithm>
+#include <cmath>
+
 #include "mx_core.hpp"
 
 namespace sbits {
@@ -146,13 +149,59 @@ __global__ __launch_bounds__(64 * WAVES, T * U > 8 ? 2 : 3) void mx_gemm_few_ker
 
 using namespace sbits;
 
-// Rows of x to a tile, for so many rows to a matrix (on average), and the bytes that offsets of a tile have to span: from the first row of a
-// matrix to its last, and from the first row of x that a tile may read to the last.  The kernel of many rows has offsets of 31 bits.
-int sbits_mx_tile_rows(int64_t rows_per_matrix, int64_t w_bytes, int64_t x_bytes)
+// ---- which kernel, and how -----------------------------------------------------------
+// Estimates in microseconds, from products of 4096 x 4096, 14336 x 4096 and 4096 x 14336 with 17 .. 512 rows of x, each with tiles of 16, 64, 128 and 256 rows.
+// Tiles of 64 and more: 8 for a launch, its first loads and stores; then for every 256 columns, while all CUs have a tile, what CHUNK_US says.
+// Parts of the columns cost a second kernel, 5, and their sums are written and read at 5 TB/s.
+// Tiles of 16 rows: 4, and W is read again for each, at 3 TB/s.
+static const double CHUNK_US[2][3] = {{2.1, 3.2, 6.1}, {0.9, 1.4, 2.2}};       // [x in 4 bits][64, 128, 256 rows]
+static double many_us(const sbits_ctx *ctx, bool x4, int size, double tiles, int64_t w_rows, int chunks)
 {
-    const bool near = w_bytes < ((int64_t)1 << 31) && x_bytes < ((int64_t)1 << 31);
-    if (rows_per_matrix <= 16 || !near) return 16;
-    return rows_per_matrix <= 64 ? 64 : rows_per_matrix <= 128 ? 128 : 256;
+    return 8.0 + std::ceil(tiles * (double)((w_rows + 255) / 256) / sbits_cus(ctx)) * chunks * CHUNK_US[x4][size];
+}
+static double few_us(double tiles, int64_t w_rows, int64_t cols) { return 4.0 + tiles * (double)w_rows * (double)cols * (17.0 / 32.0) / 3e6; }
+
+void sbits_mx_cut(const sbits_ctx *ctx, bool x4, bool near, MxGemm &g)
+{
+    const int chunks = (g.cols + 255) / 256;
+    g.tile_rows = 16;
+    g.n_split = 1;
+    g.chunks = chunks;
+    g.ld_part = (g.w_rows + 7) / 8 * 8;
+    if (!near || g.batch <= 16) return;
+    double best = few_us((double)((g.batch + 15) / 16), g.w_rows, g.cols);
+    for (int size = 0; size < 3; ++size) {
+        const int rows = 64 << size;
+        const int64_t x_tiles = (g.batch + rows - 1) / rows, tiles = x_tiles * ((g.w_rows + 255) / 256);
+        // each number of parts that leaves a CU for each, and no more of them than there are chunks for
+        for (int split = 1; split <= chunks && (split == 1 || split * tiles <= sbits_cus(ctx)); ++split) {
+            const int per = (chunks + split - 1) / split, parts = (chunks + per - 1) / per;
+            if (parts != split) continue;
+            double us = many_us(ctx, x4, size, (double)x_tiles, g.w_rows, per);
+            if (parts > 1) us += 5.0 + (double)parts * (double)g.batch * (double)g.ld_part * 8.0 / 5e6;
+            if (us < best) {
+                best = us;
+                g.tile_rows = rows; g.n_split = parts; g.chunks = per;
+            }
+        }
+    }
+}
+
+// Of an expert's rows a last tile is on average half full.
+int sbits_mx_cut_layer(const sbits_ctx *ctx, bool x4, bool near, int experts, int64_t places, int64_t hidden, int64_t inner)
+{
+    const double each = (double)places / experts;
+    auto tiles = [&](int rows) { return std::min((double)experts * (each / rows + (each > 1.0 ? 0.5 : 0.0)) + 1.0, (double)places); };
+    int best_rows = 16;
+    if (!near) return best_rows;
+    double best = few_us(tiles(16), 2 * inner, hidden) + few_us(tiles(16), hidden, inner);
+    for (int size = 0; size < 3; ++size) {
+        const int rows = 64 << size;
+        const double n = std::max(tiles(rows), std::min((double)experts, (double)places));
+        const double us = many_us(ctx, x4, size, n, 2 * inner, (int)((hidden + 255) / 256)) + many_us(ctx, x4, size, n, hidden, (int)((inner + 255) / 256));
+        if (us < best) { best = us; best_rows = rows; }
+    }
+    return best_rows;
 }
 
 // Tiles of W to a workgroup: 4, if the CUs are three quarters busy with that, else 2 or 1.  One token, bf16: 14336 x 4096 with 1, 2, 4 tiles 12.0, 10.6,

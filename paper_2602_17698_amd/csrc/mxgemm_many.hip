@@ -470,33 +470,15 @@ static int launch(sbits_ctx *ctx, const MxGemm &g)
     return SBITS_OK;
 }
 
-#ifndef MANY_NT
-#define MANY_NT 4
-#endif
-// Parts of the columns where there are fewer tiles than CUs.
-void sbits_mx_split(const sbits_ctx *ctx, MxGemm &g)
-{
-    const int chunks = (g.cols + CHUNK - 1) / CHUNK, rows = (int)g.w_rows;
-    g.n_split = 1;
-    g.chunks = chunks;
-    g.ld_part = (g.w_rows + 7) / 8 * 8;
-    if (g.tiles || g.tile_rows <= 16) return;
-    const int64_t tiles = ((g.batch + g.tile_rows - 1) / g.tile_rows) * ((rows + 64 * MANY_NT - 1) / (64 * MANY_NT));
-    const int most = (int)(sbits_cus(ctx) / tiles);
-    if (most < 2 || chunks < 2) return;
-    g.chunks = (chunks + most - 1) / most;
-    g.n_split = (chunks + g.chunks - 1) / g.chunks;
-}
-
 static int launch_tile(sbits_ctx *ctx, const MxGemm &g)
 {
     const bool x4 = g.xs != nullptr;
     switch (g.tile_rows) {
 #define MANY(MT, NT) (x4 ? (g.gated ? launch<true, true, MT, NT>(ctx, g) : launch<true, false, MT, NT>(ctx, g)) \
                          : (g.gated ? launch<false, true, MT, NT>(ctx, g) : launch<false, false, MT, NT>(ctx, g)))
-    case 256: return MANY(4, MANY_NT);
-    case 128: return MANY(2, MANY_NT);
-    case 64: return MANY(1, MANY_NT);
+    case 256: return MANY(4, 4);
+    case 128: return MANY(2, 4);
+    case 64: return MANY(1, 4);
     default: return SBITS_ERR_INTERNAL;
 #undef MANY
     }
