@@ -153,13 +153,29 @@ using namespace sbits;
 // Estimates in microseconds, from products of 4096 x 4096, 14336 x 4096 and 4096 x 14336 with 17 .. 512 rows of x, each with tiles of 16, 64, 128 and 256 rows.
 // Tiles of 64 and more: 8 for a launch, its first loads and stores; then for every 256 columns, while all CUs have a tile, what CHUNK_US says.
 // Parts of the columns cost a second kernel, 5, and their sums are written and read at 5 TB/s.
-// Tiles of 16 rows: 4, and W is read again for each, at 3 TB/s.
+// Tiles of 16 rows: 4, and W is read again for each, at 3 TB/s; with more than 2048 columns, where a CU has one workgroup at a time, at least 1.0, 1.4, 2.2 ns a
+// column for each time that all CUs get one with 1, 2, 4 tiles of W.
 static const double CHUNK_US[2][3] = {{2.1, 3.2, 6.1}, {0.9, 1.4, 2.2}};       // [x in 4 bits][64, 128, 256 rows]
 static double many_us(const sbits_ctx *ctx, bool x4, int size, double tiles, int64_t w_rows, int chunks)
 {
     return 8.0 + std::ceil(tiles * (double)((w_rows + 255) / 256) / sbits_cus(ctx)) * chunks * CHUNK_US[x4][size];
 }
-static double few_us(double tiles, int64_t w_rows, int64_t cols) { return 4.0 + tiles * (double)w_rows * (double)cols * (17.0 / 32.0) / 3e6; }
+// Tiles of W to a workgroup of the kernel of few rows: 4, if the CUs are three quarters busy with that, else 2 or 1.  One token, bf16: 14336 x 4096 with 1,
+// 2, 4 tiles 12.0, 10.6, 9.9 us, with 16 rows of x 22.4, 16.3, 12.6 (x is read once for every workgroup); 4096 x 14336 10.2, 14.5, 28.8, with 16
+// rows 19.5, 23.0, 36.6.
+static int few_tiles(const sbits_ctx *ctx, double rows)            // rows of W, once for each tile of x
+{
+    const double enough = sbits_cus(ctx) * 0.75;
+    return rows >= 64 * enough ? 4 : rows >= 32 * enough ? 2 : 1;
+}
+static double few_us(const sbits_ctx *ctx, double tiles, int64_t w_rows, int64_t cols)
+{
+    const double read = tiles * (double)w_rows * (double)cols * (17.0 / 32.0) / 3e6;
+    if (cols <= 2048) return 4.0 + read;
+    const int t = few_tiles(ctx, (double)w_rows * tiles);
+    const double rounds = std::ceil((double)((w_rows + 16 * t - 1) / (16 * t)) * tiles / sbits_cus(ctx));
+    return 4.0 + std::max(read, rounds * (double)cols * (t == 4 ? 2.2e-3 : t == 2 ? 1.4e-3 : 1.0e-3));
+}
 
 void sbits_mx_cut(const sbits_ctx *ctx, bool x4, bool near, MxGemm &g)
 {
@@ -169,7 +185,7 @@ void sbits_mx_cut(const sbits_ctx *ctx, bool x4, bool near, MxGemm &g)
     g.chunks = chunks;
     g.ld_part = (g.w_rows + 7) / 8 * 8;
     if (!near || g.batch <= 16) return;
-    double best = few_us((double)((g.batch + 15) / 16), g.w_rows, g.cols);
+    double best = few_us(ctx, (double)((g.batch + 15) / 16), g.w_rows, g.cols);
     for (int size = 0; size < 3; ++size) {
         const int rows = 64 << size;
         const int64_t x_tiles = (g.batch + rows - 1) / rows, tiles = x_tiles * ((g.w_rows + 255) / 256);
@@ -194,7 +210,7 @@ int sbits_mx_cut_layer(const sbits_ctx *ctx, bool x4, bool near, int experts, in
     auto tiles = [&](int rows) { return std::min((double)experts * (each / rows + (each > 1.0 ? 0.5 : 0.0)) + 1.0, (double)places); };
     int best_rows = 16;
     if (!near) return best_rows;
-    double best = few_us(tiles(16), 2 * inner, hidden) + few_us(tiles(16), hidden, inner);
+    double best = few_us(ctx, tiles(16), 2 * inner, hidden) + few_us(ctx, tiles(16), hidden, inner);
     for (int size = 0; size < 3; ++size) {
         const int rows = 64 << size;
         const double n = std::max(tiles(rows), std::min((double)experts, (double)places));
@@ -204,24 +220,18 @@ int sbits_mx_cut_layer(const sbits_ctx *ctx, bool x4, bool near, int experts, in
     return best_rows;
 }
 
-// Tiles of W to a workgroup: 4, if the CUs are three quarters busy with that, else 2 or 1.  One token, bf16: 14336 x 4096 with 1, 2, 4 tiles 12.0, 10.6,
-// 9.9 us, with 16 rows of x 22.4, 16.3, 12.6 (x is read once for every workgroup); 4096 x 14336 10.2, 14.5, 28.8, with 16 rows 19.5, 23.0, 36.6.
 // Rows of up to 2048 columns by 4 waves with 2 runs to a group, wider ones by 8 with 4: 110 products of 2048 x 2048 with a row or two of x each 28.7 and
 // 37.0 us, one of 14336 x 4096 12.4 and 10.2.
 template <bool X4, bool GATED>
 static auto few_instance(const sbits_ctx *ctx, const MxGemm &g, int tiles, int &outs, int &waves)
 {
-    const int64_t enough = (int64_t)sbits_cus(ctx) * 3 / 4, rows = (int64_t)g.w_rows * tiles;
     const bool narrow = g.cols <= 2048;
+    const int t = few_tiles(ctx, (double)g.w_rows * tiles);
     waves = narrow ? 4 : 8;
-    outs = 64 / (GATED ? 2 : 1);
-    if (rows >= 64 * enough) return narrow ? mx_gemm_few_kernel<X4, GATED, 4, 4, 2> : mx_gemm_few_kernel<X4, GATED, 8, 4, 4>;
-    outs /= 2;
+    outs = (GATED ? 8 : 16) * (GATED && t == 1 ? 2 : t);
+    if (t == 4) return narrow ? mx_gemm_few_kernel<X4, GATED, 4, 4, 2> : mx_gemm_few_kernel<X4, GATED, 8, 4, 4>;
     if constexpr (!GATED)
-        if (rows < 32 * enough) {
-            outs = 16;
-            return narrow ? mx_gemm_few_kernel<X4, GATED, 4, 1, 2> : mx_gemm_few_kernel<X4, GATED, 8, 1, 4>;
-        }
+        if (t == 1) return narrow ? mx_gemm_few_kernel<X4, GATED, 4, 1, 2> : mx_gemm_few_kernel<X4, GATED, 8, 1, 4>;
     return narrow ? mx_gemm_few_kernel<X4, GATED, 4, 2, 2> : mx_gemm_few_kernel<X4, GATED, 8, 2, 4>;
 }
 

@@ -400,7 +400,8 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     }
 }
 
-// the parts' sums, in the order of the columns, then what the kernel above does with a sum
+// The parts' sums, added in the order of the columns (four waves a quarter each, then the quarters), and what the kernel above does with a sum.  Bound by the
+// latency of sums that other dies have just written: 8 of them at a time; one after the other 56 parts of 60 x 250 outputs took 14 us, by one wave 10.
 struct MxJoin {
     const float *part;
     void *y;
@@ -410,44 +411,51 @@ struct MxJoin {
 template <bool GATED, bool BF16>
 __global__ __launch_bounds__(256) void mx_join_kernel(MxJoin a)
 {
-    const int out = 4 * (int)(blockIdx.x * 256 + threadIdx.x);
-    if (out >= a.outs) return;
+    __shared__ f32x4 quarter[4][GATED ? 2 : 1][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, out = 4 * (int)(blockIdx.x * 64 + lane);
     const int64_t b = blockIdx.y;
-    const float *p = a.part + b * a.ld_part + out;
-    float v[4], u[4];
-    auto add = [&](const float *from, float (&sum)[4], bool first) {
-        if (!GATED || out + 4 <= a.outs) {                         // (rows of sums are a multiple of 8 long)
-            const f32x4 f = *reinterpret_cast<const f32x4 *>(from);
+    const int each = (a.n_split + 3) / 4, first = wave * each, last = first + each < a.n_split ? first + each : a.n_split;
+    auto join = [&](const float *p) {
+        const bool aligned = (reinterpret_cast<uintptr_t>(p) & 15) == 0 && out + 4 <= a.outs;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = first; s < last; s += 8) {
+            f32x4 f[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = first ? f[i] : sum[i] + f[i];
-        } else {
+            for (int k = 0; k < 8; ++k) {
+                f[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                if (s + k >= last) continue;
+                const float *from = p + (s + k) * a.batch * a.ld_part;
+                if (aligned) {
+                    f[k] = *reinterpret_cast<const f32x4 *>(from);
+                } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float f = out + i < a.outs ? from[i] : 0.0f;
-                sum[i] = first ? f : sum[i] + f;
-            }
-        }
-    };
-    for (int s = 0; s < a.n_split; ++s, p += a.batch * a.ld_part) {
-        add(p, v, s == 0);
-        if (GATED) {
-            if (a.outs % 4 == 0) add(p + a.outs, u, s == 0);
-            else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float f = out + i < a.outs ? p[a.outs + i] : 0.0f;
-                    u[i] = s == 0 ? f : u[i] + f;
+                    for (int i = 0; i < 4; ++i)
+                        if (out + i < a.outs) f[k][i] = from[i];
                 }
             }
-        }
-    }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (GATED) v[i] = silu_mul(v[i], u[i]);
-        if (out + i >= a.outs) continue;
-        if constexpr (BF16) static_cast<uint16_t *>(a.y)[b * a.ld_y + out + i] = (uint16_t)bf16_round(v[i]);
-        else static_cast<float *>(a.y)[b * a.ld_y + out + i] = v[i];
-    }
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] += f[k][i];
+        }
+        return sum;
+    };
+    const float *const p = a.part + b * a.ld_part + out;
+    quarter[wave][0][lane] = join(p);
+    if constexpr (GATED) quarter[wave][1][lane] = join(p + a.outs);
+    __syncthreads();
+    // (a thread an output: 64 lanes' 4)
+    const int i = threadIdx.x, o = (int)blockIdx.x * 256 + i;
+    if (o >= a.outs) return;
+    auto whole = [&](int half) {
+        const float *q = reinterpret_cast<const float *>(&quarter[0][half][0]);
+        constexpr int NEXT = (GATED ? 2 : 1) * 256;
+        return ((q[i] + q[NEXT + i]) + q[2 * NEXT + i]) + q[3 * NEXT + i];
+    };
+    float v = whole(0);
+    if constexpr (GATED) v = silu_mul(v, whole(1));
+    if constexpr (BF16) static_cast<uint16_t *>(a.y)[b * a.ld_y + o] = (uint16_t)bf16_round(v);
+    else static_cast<float *>(a.y)[b * a.ld_y + o] = v;
 }
 
 }  // namespace sbits
@@ -495,7 +503,7 @@ int sbits_launch_mx_gemm_many(sbits_ctx *ctx, const MxGemm &g)
     const MxJoin j = {g.part, g.y, g.ld_part, g.ld_y, g.batch, g.n_split, g.outs};
     auto fn = g.gated ? (g.y_bf16 ? mx_join_kernel<true, true> : mx_join_kernel<true, false>)
                       : (g.y_bf16 ? mx_join_kernel<false, true> : mx_join_kernel<false, false>);
-    hipLaunchKernelGGL(fn, dim3((unsigned)((g.outs + 1023) / 1024), (unsigned)g.batch), dim3(256), 0, ctx->stream, j);
+    hipLaunchKernelGGL(fn, dim3((unsigned)((g.outs + 255) / 256), (unsigned)g.batch), dim3(256), 0, ctx->stream, j);
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;
 }
