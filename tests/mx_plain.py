@@ -13,17 +13,21 @@ def quantise(x):
     fine = torch.isfinite(b).all(-1)
     power = torch.frexp(torch.where(fine, top, 1.0))[1] - 3
     power = torch.where(top == 0, -125, power).clamp(min=-125)
-    size = b.abs() * torch.exp2(-power.double())[..., None]
+    size = (b.abs() * torch.exp2(-power.double())[..., None]).nan_to_num(posinf=9.0)
     # the nearest of the grid; of two the one whose code is even
-    away = (size[..., None] - GRID[:8]).abs()
-    code = (away * 16 + (torch.arange(8) % 2) * 1e-9).argmin(-1) + 8 * torch.signbit(b)
-    code = torch.where(fine[..., None], code, 0)
+    code = torch.zeros_like(size, dtype=torch.int64)
+    least = size.clone()
+    for k in range(1, 8):
+        away = (size - GRID[k].item()).abs()
+        nearer = (away < least) | (away == least) & (k % 2 == 0)
+        code, least = torch.where(nearer, k, code), torch.where(nearer, away, least)
+    code = torch.where(fine[..., None], code + 8 * torch.signbit(b), 0)
     return code.flatten(1).to(torch.uint8), torch.where(fine, power + 127, 255).to(torch.uint8)
 
 
 def values(code, byte):
     scale = torch.where(byte == 255, math.nan, torch.exp2(byte.double() - 127))
-    return (GRID[code.long()].reshape(code.shape[0], -1, 32) * scale[..., None]).flatten(1)
+    return (GRID.to(code.device)[code.long()].reshape(code.shape[0], -1, 32) * scale[..., None]).flatten(1)
 
 
 def pack(code):
@@ -118,26 +122,25 @@ def chosen_weights(r, x, ids):
 
 
 def layer(r, logits, bias, x, up, down, four):
-    """(ids, weights, out, how far out may be off); up, down: lists of matrices in 64 bits, x bf16."""
+    """(ids, weights, out, how far out may be off); up, down: lists of matrices in 64 bits, x bf16, where the products are to be computed."""
     ids, w = route(r, logits, bias)
     xs = values(*quantise(x)) if four else x.double()
-    hidden, d = x.shape[1], 2.0 ** -7                       # h: rounded to bf16, perhaps to the other side
-    out, off = torch.zeros(x.shape[0], hidden, dtype=torch.float64), torch.zeros(x.shape[0], hidden, dtype=torch.float64)
-    for t in range(x.shape[0]):
-        for j in range(r.top_k):
-            e = int(ids[t, j])
-            if e < 0:
-                continue
-            h, dh = product(xs[t:t + 1], up[e], True)
-            dh = dh + d * h.abs()
-            h = h.to(torch.bfloat16).double()
-            if four:
-                q = values(*quantise(h))
-                ends = [values(*quantise(h + s * dh)) for s in (-1, 1)]
-                dh = torch.stack([(v - q).abs() for v in ends]).amax(0)
-                h = q
-            y, dy = product(h, down[e], False)
-            dy = dy + dh @ down[e].abs().T + 2.0 ** -8 * y.abs()
-            out[t] += w[t, j] * y[0]
-            off[t] += w[t, j] * (dy[0] + 2.0 ** -22 * y[0].abs())
+    tokens, hidden, d = x.shape[0], x.shape[1], 2.0 ** -7   # h: rounded to bf16, perhaps to the other side
+    each, each_off = (torch.zeros(tokens, r.top_k, hidden, dtype=torch.float64, device=x.device) for _ in range(2))
+    for e in range(r.experts):
+        t, j = (i.to(x.device) for i in torch.nonzero(ids == e, as_tuple=True))
+        if len(t) == 0:
+            continue
+        h, dh = product(xs[t], up[e], True)
+        dh = dh + d * h.abs()
+        h = h.to(torch.bfloat16).double()
+        if four:
+            q = values(*quantise(h))
+            ends = [values(*quantise(h + s * dh)) for s in (-1, 1)]
+            dh = torch.stack([(v - q).abs() for v in ends]).amax(0)
+            h = q
+        y, dy = product(h, down[e], False)
+        each[t, j], each_off[t, j] = y, dy + dh @ down[e].abs().T + (2.0 ** -8 + 2.0 ** -22) * y.abs()
+    weight = w.to(x.device)[..., None]
+    out, off = (each * weight).sum(1), (each_off * weight).sum(1)
     return ids, w, out, off + 2.0 ** -8 * (out.abs() + off)

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import mx_plain as mp
+from mx_shapes import LARGE_LAYERS, LAYERS
 from paper_2602_17698_amd import binding as sb
 
 pytestmark = pytest.mark.gpu
@@ -123,14 +124,7 @@ def make_layer(experts, hidden, inner, seed, extra=0):
     return descs, mp.values(*up).view(experts, 2 * inner, hidden), mp.values(*down).view(experts, hidden, inner)
 
 
-LAYERS = [(1, 4, 1, 32, 32), (3, 8, 2, 96, 64), (20, 8, 4, 160, 96), (33, 16, 4, 512, 256), (70, 4, 2, 288, 544), (300, 8, 2, 128, 160), (150, 2, 2, 256, 288),
-          (600, 4, 2, 64, 32)]
-
-
-@pytest.mark.parametrize("tokens,experts,top_k,hidden,inner", LAYERS)
-@pytest.mark.parametrize("four", [False, True])
-@pytest.mark.parametrize("biased", [False, True])
-def test_layer(ctx, tokens, experts, top_k, hidden, inner, four, biased):
+def check_layer(ctx, tokens, experts, top_k, hidden, inner, four, biased, where):
     r = sb.Router(experts=experts, top_k=top_k, scoring=1 if biased else 0, renormalize=not biased)
     (up, down), up64, down64 = make_layer(experts, hidden, inner, tokens, extra=1 if biased else 0)
     logits = make_logits(tokens, experts, torch.float32, tokens)
@@ -145,15 +139,28 @@ def test_layer(ctx, tokens, experts, top_k, hidden, inner, four, biased):
     print("[case]", tokens, experts, top_k, hidden, inner, four, biased, flush=True)
     args = (r, logits.cuda(), bias.cuda() if biased else None, x.cuda(), up, down)
     ctx.expert_layer(*args, out[:, :hidden], ids, weights, ws, four_bit=four)
-    want_ids, want_w, want, off = mp.layer(r, logits, bias, x, up64, down64, four)
+    want_ids, want_w, want, off = mp.layer(r, logits, bias, x.to(where), up64.to(where), down64.to(where), four)
     assert torch.equal(ids.cpu(), want_ids)
     assert bool(((weights.cpu().double() - want_w).abs() <= 64 * 2.0 ** -24 * want_w).all())
-    got = out[:, :hidden].cpu().double()
+    got = out[:, :hidden].to(where).double()
     assert bool(((got - want).abs() <= off).all()), float(((got - want).abs() / off.clamp(min=1e-30)).max())
     assert bool((out[:, hidden:] == 7.0).all())
     first = out.clone()
     ctx.expert_layer(*args, out[:, :hidden], ids, weights, ws, four_bit=four)
     assert torch.equal(first, out)
+
+
+@pytest.mark.parametrize("tokens,experts,top_k,hidden,inner", LAYERS)
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("biased", [False, True])
+def test_layer(ctx, tokens, experts, top_k, hidden, inner, four, biased):
+    check_layer(ctx, tokens, experts, top_k, hidden, inner, four, biased, "cpu")
+
+
+@pytest.mark.parametrize("tokens,experts,top_k,hidden,inner", [k[:5] for k in LARGE_LAYERS])
+@pytest.mark.parametrize("four", [False, True])
+def test_layer_by_large_tiles(ctx, tokens, experts, top_k, hidden, inner, four):
+    check_layer(ctx, tokens, experts, top_k, hidden, inner, four, tokens % 400 != 0, "cuda")
 
 
 def test_layer_without_any_choice(ctx):

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import mx_plain as mp
+from mx_shapes import LARGE, SHAPES
 from paper_2602_17698_amd import binding as sb
 
 pytestmark = pytest.mark.gpu
@@ -76,36 +77,31 @@ def test_quantise_borders_and_broken_blocks(ctx):
 
 
 # ---- products --------------------------------------------------------------------------------------
-# batches on both sides of the lines between kernels and tiles, outputs that end inside a tile, runs of columns that end inside one
-SHAPES = [(1, 8, 32), (1, 250, 256), (2, 33, 96), (15, 64, 128), (16, 31, 160), (17, 100, 512), (31, 257, 288), (33, 64, 1056), (48, 130, 544), (64, 96, 2080),
-          (65, 250, 320), (97, 256, 576), (128, 514, 256), (129, 300, 352), (200, 129, 1120), (255, 513, 64), (256, 256, 32), (257, 258, 608), (300, 700, 800)]
-
-
 def workspace(ctx, w, batch, four, gated=False):
     return torch.full((max(256, ctx.mx_gemm_ws_bytes(w, batch, four, gated)),), 0xff, dtype=torch.uint8, device="cuda")
 
 
-def check_product(ctx, batch, rows, cols, four, gated, out, extra=0, seed=0, spread=3):
+def check_product(ctx, batch, rows, cols, four, gated, out, extra=0, seed=0, spread=3, where="cpu"):
     g = gen(seed + 31 * batch + rows)
     code, byte = mp.random_matrix(rows * (2 if gated else 1), cols, g, spread)
     x = torch.randn(batch, cols + 8 * extra, generator=g).to(torch.bfloat16)
     w = sb.mx(*mp.stored(code, byte, "cuda", extra))
     if four:
-        xc, xb = mp.quantise(x[:, :cols])
-        xs, xd = mp.values(xc, xb), sb.mx(*mp.stored(xc, xb, "cuda", extra))
+        xc, xb = mp.quantise(x[:, :cols].to(where))
+        xs, xd = mp.values(xc, xb), sb.mx(*mp.stored(xc.cpu(), xb.cpu(), "cuda", extra))
     else:
-        xs, xd = x[:, :cols].double(), x.cuda()[:, :cols]
+        xs, xd = x[:, :cols].double().to(where), x.cuda()[:, :cols]
     y = torch.full((batch, sb.mx_out_pitch(rows) + 8 * extra), 7.0, dtype=out, device="cuda")
     ws = workspace(ctx, w, batch, four, gated)
     print("[case]", batch, rows, cols, four, gated, out, flush=True)
     ctx.mx_gemm(w, xd, y[:, :rows], ws, gated=gated)
     torch.cuda.synchronize()
-    want, off = mp.product(xs, mp.values(code, byte), gated)
+    want, off = mp.product(xs, mp.values(code.to(where), byte.to(where)), gated)
     if out == torch.bfloat16:
         off = off + 2.0 ** -8 * (want.abs() + off)
     else:
         off = off + 2.0 ** -24 * (want.abs() + off)
-    got = y.cpu().double()
+    got = y.to(where).double()
     assert bool(((got[:, :rows] - want).abs() <= off).all()), float(((got[:, :rows] - want).abs() / off).max())
     assert bool((got[:, rows:] == 7.0).all())
     first = y.clone()
@@ -118,6 +114,19 @@ def check_product(ctx, batch, rows, cols, four, gated, out, extra=0, seed=0, spr
                                             (True, True, torch.float32)])
 def test_product(ctx, batch, rows, cols, four, gated, out):
     check_product(ctx, batch, rows, cols, four, gated, out)
+
+
+@pytest.mark.parametrize("batch,rows,cols", [k[:3] for k in LARGE])
+@pytest.mark.parametrize("four,gated,out", [(False, False, torch.bfloat16), (False, True, torch.float32), (True, False, torch.float32),
+                                            (True, True, torch.bfloat16)])
+def test_product_by_large_tiles(ctx, batch, rows, cols, four, gated, out):
+    check_product(ctx, batch, rows // 2 if gated else rows, cols, four, gated, out, where="cuda")
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(700, 2050, 800), (4000, 1030, 288), (2000, 4100, 288), (300, 250, 14336)])
+@pytest.mark.parametrize("four", [False, True])
+def test_product_of_strided_large_matrices(ctx, batch, rows, cols, four):
+    check_product(ctx, batch, rows, cols, four, False, torch.bfloat16, extra=2, seed=4, where="cuda")
 
 
 @pytest.mark.parametrize("batch", [1, 20, 70, 260])
@@ -134,11 +143,10 @@ def test_product_with_far_powers(ctx, batch, four):
     check_product(ctx, batch, 70, 256, four, False, torch.float32, seed=3, spread=60)
 
 
-@pytest.mark.parametrize("batch", [2, 300])
+@pytest.mark.parametrize("batch,rows,cols", [(2, 300, 416), (300, 300, 416), (700, 2050, 416), (4000, 1030, 416), (3000, 4100, 416)])
 @pytest.mark.parametrize("four", [False, True])
-def test_broken_blocks_stay_in_their_outputs(ctx, batch, four):
+def test_broken_blocks_stay_in_their_outputs(ctx, batch, rows, cols, four):
     """A block of W with the byte 255 makes its output row NaN, an infinite x or a broken block of x its row of y; the others are as without."""
-    rows, cols = 300, 416
     g = gen(5)
     code, byte = mp.random_matrix(rows, cols, g)
     x = torch.randn(batch, cols, generator=g).to(torch.bfloat16)
@@ -179,7 +187,7 @@ def test_product_and_quantisation_in_a_graph(ctx):
     own = sb.Context(0, side.cuda_stream)
     g = gen(9)
     jobs = []
-    for batch, rows, cols in ((3, 100, 256), (40, 96, 544), (300, 300, 288)):
+    for batch, rows, cols in ((3, 100, 256), (60, 250, 14336), (700, 2050, 288), (2000, 4100, 96)):
         code, byte = mp.random_matrix(rows, cols, g)
         w = sb.mx(*mp.stored(code, byte, "cuda"))
         x = torch.randn(batch, cols, generator=g).to(torch.bfloat16).cuda()
