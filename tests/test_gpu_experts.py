@@ -210,3 +210,15 @@ def test_layer_in_a_graph(ctx, four):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(kept, (out, ids, weights))), turn
     own.close()
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_the_example_quantises_runs_and_balances(capsys, four):
+    import json
+    from paper_2602_17698_amd import experts
+    assert experts.main(["--hidden", "512", "--inner", "256", "--experts", "16", "--top-k", "4", "--tokens", "512", "--json"] + ["--four-bit"] * four) == 0
+    lines = [json.loads(line) for line in capsys.readouterr().out.splitlines()]
+    # 4-bit weights of normal distributions are off by some 11 % each, activations as much
+    assert [line["stage"] for line in lines] == ["prompt", "16 tokens", "one token", "balance", "balance"]
+    assert all(0.02 < line["error"] < 0.5 for line in lines[:3])
+    assert lines[4]["variation"] < 0.7 * lines[3]["variation"]

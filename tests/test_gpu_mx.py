@@ -223,3 +223,27 @@ def test_product_and_quantisation_in_a_graph(ctx):
         for (a, b), (*_, y4, y16) in zip(replayed, jobs):
             assert torch.equal(a, y4) and torch.equal(b, y16), turn
     own.close()
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_rows_further_apart_than_32_bits_reach(ctx, four):
+    """Rows of W and of x 8 MiB apart: the last ones begin 2.4 GB behind the first."""
+    rows, cols, batch, far = 300, 96, 290, 1 << 23
+    g = gen(21)
+    code, byte = mp.random_matrix(rows, cols, g)
+    xc, xb = mp.random_matrix(batch, cols, g)
+    space = torch.empty(rows, far, dtype=torch.uint8, device="cuda")
+    space[:, :cols // 2] = mp.pack(code).cuda()
+    w = sb.mx(space, mp.stored(code, byte, "cuda")[1], cols)
+    x = torch.randn(batch, cols, generator=g).to(torch.bfloat16)
+    if four:
+        space[:batch, 4096:4096 + cols // 2] = mp.pack(xc).cuda()
+        xs, xd = mp.values(xc, xb), sb.mx(space[:batch, 4096:], mp.stored(xc, xb, "cuda")[1], cols)
+    else:
+        wide = space.view(torch.bfloat16)[:batch, 4096:4096 + cols]
+        wide.copy_(x.cuda())
+        xs, xd = x.double(), wide
+    y = torch.empty(batch, sb.mx_out_pitch(rows), device="cuda")
+    ctx.mx_gemm(w, xd, y[:, :rows], workspace(ctx, w, batch, four))
+    want, off = mp.product(xs, mp.values(code, byte), False)
+    assert bool(((y[:, :rows].cpu().double() - want).abs() <= off).all())
