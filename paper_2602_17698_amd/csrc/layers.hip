@@ -204,8 +204,9 @@ int sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logits
     char *const base = static_cast<char *>(ws);
     int *const sorted = reinterpret_cast<int *>(base + s.sorted), *const token = reinterpret_cast<int *>(base + s.token);
     MxTile *const tiles = reinterpret_cast<MxTile *>(base + s.tiles);
-    if ((rc = sbits_launch_route(ctx, *r, logits, logits_type == SBITS_TYPE_BF16, ld_logits, bias, tokens, ids, weights))) return rc;
-    if ((rc = sbits_launch_expert_lists(ctx, ids, (int)s.places, r->experts, r->top_k, s.tile_rows, s.max_tiles, sorted, token, tiles))) return rc;
+    if ((rc = sbits_launch_route_and_list(ctx, *r, logits, logits_type == SBITS_TYPE_BF16, ld_logits, bias, tokens, ids, weights, s.tile_rows,
+                                          s.max_tiles, sorted, token, tiles)))
+        return rc;
     MxGemm g = {};
     g.n_split = 1;
     g.tiles = tiles; g.n_tiles = s.max_tiles; g.tile_rows = s.tile_rows;

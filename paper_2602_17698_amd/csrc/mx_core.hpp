@@ -114,7 +114,8 @@ int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits
                        int32_t *ids, float *weights);
 int sbits_launch_route_backward(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const int32_t *ids,
                                 const float *d_weights, int64_t tokens, float *d_logits, int64_t ld_d);
-int sbits_launch_expert_lists(sbits_ctx *ctx, const int32_t *ids, int n, int experts, int top_k, int tile_rows, int max_tiles,
-                              int *sorted, int *tokens, sbits::MxTile *tiles);
+// the choice, and the choices' places and tokens by expert with the tiles of their lists
+int sbits_launch_route_and_list(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const float *bias, int64_t tokens,
+                                int32_t *ids, float *weights, int tile_rows, int max_tiles, int *sorted, int *token_of, sbits::MxTile *tiles);
 int sbits_launch_combine(sbits_ctx *ctx, const void *y, int64_t ld_y, const int32_t *ids, const float *weights, int64_t tokens, int top_k,
                          int hidden, void *out, int64_t ld_out);

@@ -150,12 +150,11 @@ __device__ __forceinline__ void choose_exactly(const RouteArgs &a, int lane, con
     }
 }
 
+// One token: lane j < top_k gets the j-th expert, or -1, and its weight; both are written.
 template <bool BF16, int PER>
-__global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
+__device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, int lane, int &my_id)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t token = (int64_t)blockIdx.x * 4 + wave;
-    if (token >= a.tokens) return;
+    float my_p;
     const int lanes = 1 << a.log_lanes, group = lane >> a.log_lanes, in_group = lane & (lanes - 1), first = group * a.each + in_group;
     float x[PER], b[PER], p[PER];
     int key[PER], top_key = NONE;
@@ -230,7 +229,8 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
 #pragma unroll
         for (int r = 0; r < PER; ++r) key[r] = x[r] > -HUGE_VALF && (a.groups == 1 || key[r] != NONE) ? ordered(x[r]) : NONE;
     }
-    int my_id = -1, my_key = NONE;
+    int my_key = NONE;
+    my_id = -1;
     for (int j = 0; j < a.top_k; ++j) {
         int best = key[0];
 #pragma unroll
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
         const int id = __builtin_amdgcn_readlane(at, winner);
         if (lane == j) { my_id = id; my_key = all; }
     }
-    float my_p = 0.0f;
+    my_p = 0.0f;
     if (my_id >= 0) my_p = chance(logit_at<BF16>(a.logits, token * a.ld + my_id));
     if (a.bias) {                                               // (without a bias keys are the logits themselves)
         // each chosen score against the next, the last against all that are left
@@ -278,6 +278,16 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
         a.ids[token * a.top_k + lane] = my_id;
         a.weights[token * a.top_k + lane] = my_p;
     }
+}
+
+template <bool BF16, int PER>
+__global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t token = (int64_t)blockIdx.x * 4 + wave;
+    if (token >= a.tokens) return;
+    int id;
+    route_token<BF16, PER>(a, token, lane, id);
 }
 
 // ---- its gradient ----------------------------------------------------------------
@@ -447,6 +457,66 @@ __global__ __launch_bounds__(64 * LIST_WAVES) void expert_lists_kernel(const int
     }
 }
 
+// The choice and the lists of up to HERE tokens in one launch, by one workgroup.  A layer of 64 experts, 8 to a token, in a graph, in one launch and in
+// two: 1 token 19.5 and 20.9 us, 8 tokens 22.8 and 24.0, 16 tokens 25.2 and 24.4 (one CU issues the choices of all tokens).
+constexpr int HERE = 8, LISTED_HERE = HERE * MAX_TOP_K;
+template <bool BF16, int PER>
+__global__ __launch_bounds__(1024) void route_and_list_kernel(RouteArgs a, int tile_rows, int max_tiles, int *sorted, int *token_of, MxTile *tiles)
+{
+    __shared__ __align__(16) int ids[LISTED_HERE];
+    __shared__ int counts[MAX_EXPERTS], before[MAX_EXPERTS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = (int)a.tokens * a.top_k;
+    for (int e = tid; e < MAX_EXPERTS; e += 1024) counts[e] = 0;
+    __syncthreads();
+    if (wave < a.tokens) {
+        const int token = wave;
+        int id;
+        route_token<BF16, PER>(a, token, lane, id);
+        if (lane < a.top_k) {
+            ids[token * a.top_k + lane] = id;
+            if (id >= 0) atomicAdd(&counts[id], 1);
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {
+        // lane l: experts 8 l .. 8 l + 7
+        int c[8], own = 0, own_tiles = 0;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            c[r] = counts[8 * lane + r];
+            own += c[r];
+            own_tiles += (c[r] + tile_rows - 1) / tile_rows;
+        }
+        int upto = own, tiles_upto = own_tiles;
+        for (int s = 1; s < 64; s <<= 1) {
+            const int o = __shfl_up(upto, s), ot = __shfl_up(tiles_upto, s);
+            if (lane >= s) { upto += o; tiles_upto += ot; }
+        }
+        int at = upto - own, tile = tiles_upto - own_tiles;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            before[8 * lane + r] = at;
+            for (int first = 0; first < c[r]; first += tile_rows)
+                tiles[tile++] = {8 * lane + r, at + first, c[r] - first < tile_rows ? c[r] - first : tile_rows, 0};
+            at += c[r];
+        }
+        const int all = __shfl(tiles_upto, 63);
+        for (int t = all + lane; t < max_tiles; t += 64) tiles[t] = {0, 0, 0, 0};
+        if (lane == 0) tiles[max_tiles] = {0, 0, all, 0};
+    }
+    __syncthreads();
+    if (tid < n && ids[tid] >= 0) {
+        const int id = ids[tid];
+        int at = before[id];
+        for (int i = 0; i < tid; i += 4) {                      // (four to a read; those behind this one do not count)
+            const int4 v = *reinterpret_cast<const int4 *>(&ids[i]);
+            at += (v.x == id) + (v.y == id && i + 1 < tid) + (v.z == id && i + 2 < tid) + (v.w == id && i + 3 < tid);
+        }
+        sorted[at] = tid;
+        token_of[at] = tid / a.top_k;
+    }
+}
+
 // ---- the weighted sum --------------------------------------------------------------
 // out[t] = sum_j weights[t][j] * y[t * top_k + j], in fp32, in the order of j; places without an expert are not read.
 struct CombineArgs {
@@ -457,25 +527,36 @@ struct CombineArgs {
     int64_t ld_y, ld_out;
     int top_k, hidden;
 };
+// Memory bounds it; 8 rows are asked for at a time (one after the other 16 tokens of 2048 columns, 8 rows each, took 5.7 us).
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a)
 {
     const int64_t token = blockIdx.x;
-    for (int c = threadIdx.x * 8; c < a.hidden; c += 2048) {
-        float sum[8];
-        for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-        for (int j = 0; j < a.top_k; ++j) {
-            const int64_t at = token * a.top_k + j;
-            if (a.ids[at] < 0) continue;
-            const float w = a.weights[at];
-            float v[8];
-            unpack8(gload_u4(a.y + at * a.ld_y + c), v);
+    const int c = (int)(blockIdx.y * 256 + threadIdx.x) * 8;
+    if (c >= a.hidden) return;
+    float sum[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+    for (int j0 = 0; j0 < a.top_k; j0 += 8) {
+        float w[8];
+        uint4 y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t at = token * a.top_k + j0 + j;
+            const bool there = j0 + j < a.top_k && a.ids[at] >= 0;
+            w[j] = there ? a.weights[at] : 0.0f;
+            y[j] = there ? gload_u4(a.y + at * a.ld_y + c) : make_uint4(0, 0, 0, 0);
         }
-        u32x4 o;
-        o.x = bf16_pair(sum[0], sum[1]); o.y = bf16_pair(sum[2], sum[3]); o.z = bf16_pair(sum[4], sum[5]); o.w = bf16_pair(sum[6], sum[7]);
-        *reinterpret_cast<u32x4 *>(a.out + token * a.ld_out + c) = o;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float v[8];
+            unpack8(y[j], v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[j], v[i], sum[i]);
+        }
     }
+    u32x4 o;
+    o.x = bf16_pair(sum[0], sum[1]); o.y = bf16_pair(sum[2], sum[3]); o.z = bf16_pair(sum[4], sum[5]); o.w = bf16_pair(sum[6], sum[7]);
+    *reinterpret_cast<u32x4 *>(a.out + token * a.ld_out + c) = o;
 }
 
 }  // namespace sbits
@@ -488,24 +569,53 @@ static auto route_instance(int per)
     return per <= 1 ? route_kernel<BF16, 1> : per <= 2 ? route_kernel<BF16, 2> : per <= 4 ? route_kernel<BF16, 4> : per <= 8 ? route_kernel<BF16, 8> : route_kernel<BF16, 16>;
 }
 template <bool BF16>
+static auto route_and_list_instance(int per)
+{
+    return per <= 1 ? route_and_list_kernel<BF16, 1> : per <= 2 ? route_and_list_kernel<BF16, 2> : route_and_list_kernel<BF16, 4>;
+}
+template <bool BF16>
 static auto route_backward_instance(int experts)
 {
     return experts <= 64 ? route_backward_kernel<BF16, 1> : experts <= 128 ? route_backward_kernel<BF16, 2>
          : experts <= 256 ? route_backward_kernel<BF16, 4> : route_backward_kernel<BF16, 8>;
 }
 
-int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const float *bias, int64_t tokens,
-                       int32_t *ids, float *weights)
+// the arguments; returns the registers of a lane: at most 15, as at least 33 lanes are in use
+static int route_args(const sbits_router &r, const void *logits, int64_t ld, const float *bias, int64_t tokens, int32_t *ids, float *weights, RouteArgs &a)
 {
-    RouteArgs a;
     a.logits = logits; a.bias = bias; a.ids = ids; a.weights = weights; a.ld = ld; a.tokens = tokens;
     a.experts = r.experts; a.top_k = r.top_k; a.groups = r.groups; a.top_groups = r.top_groups; a.each = r.experts / r.groups;
     a.sigmoid = r.scoring == SBITS_ROUTE_SIGMOID; a.best_only = r.group_score == SBITS_ROUTE_GROUP_MAX; a.renormalize = r.renormalize;
     a.log_lanes = 0;
     while (r.groups << (a.log_lanes + 1) <= 64) ++a.log_lanes;
-    const int per = (a.each + (1 << a.log_lanes) - 1) >> a.log_lanes;                    // at most 15: at least 33 lanes are in use
+    return (a.each + (1 << a.log_lanes) - 1) >> a.log_lanes;
+}
+
+int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const float *bias, int64_t tokens,
+                       int32_t *ids, float *weights)
+{
+    RouteArgs a;
+    const int per = route_args(r, logits, ld, bias, tokens, ids, weights, a);
     auto fn = bf16 ? route_instance<true>(per) : route_instance<false>(per);
     hipLaunchKernelGGL(fn, dim3((unsigned)((tokens + 3) / 4)), dim3(256), 0, ctx->stream, a);
+    SBITS_HIP(ctx, hipGetLastError());
+    return SBITS_OK;
+}
+
+int sbits_launch_route_and_list(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const float *bias, int64_t tokens,
+                                int32_t *ids, float *weights, int tile_rows, int max_tiles, int *sorted, int *token_of, MxTile *tiles)
+{
+    RouteArgs a;
+    const int per = route_args(r, logits, ld, bias, tokens, ids, weights, a);
+    if (tokens > HERE || per > 4) {                             // (more registers than 16 waves have)
+        const int rc = sbits_launch_route(ctx, r, logits, bf16, ld, bias, tokens, ids, weights);
+        if (rc) return rc;
+        hipLaunchKernelGGL(expert_lists_kernel, dim3((unsigned)r.experts), dim3(64 * LIST_WAVES), 0, ctx->stream, ids, (int)(tokens * r.top_k), r.experts,
+                           r.top_k, tile_rows, max_tiles, sorted, token_of, tiles);
+    } else {
+        auto fn = bf16 ? route_and_list_instance<true>(per) : route_and_list_instance<false>(per);
+        hipLaunchKernelGGL(fn, dim3(1), dim3(1024), 0, ctx->stream, a, tile_rows, max_tiles, sorted, token_of, tiles);
+    }
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;
 }
@@ -522,22 +632,13 @@ int sbits_launch_route_backward(sbits_ctx *ctx, const sbits_router &r, const voi
     return SBITS_OK;
 }
 
-int sbits_launch_expert_lists(sbits_ctx *ctx, const int32_t *ids, int n, int experts, int top_k, int tile_rows, int max_tiles, int *sorted, int *tokens,
-                              MxTile *tiles)
-{
-    hipLaunchKernelGGL(expert_lists_kernel, dim3((unsigned)experts), dim3(64 * LIST_WAVES), 0, ctx->stream, ids, n, experts, top_k, tile_rows, max_tiles, sorted,
-                       tokens, tiles);
-    SBITS_HIP(ctx, hipGetLastError());
-    return SBITS_OK;
-}
-
 int sbits_launch_combine(sbits_ctx *ctx, const void *y, int64_t ld_y, const int32_t *ids, const float *weights, int64_t tokens, int top_k,
                          int hidden, void *out, int64_t ld_out)
 {
     CombineArgs a;
     a.y = static_cast<const uint16_t *>(y); a.ids = ids; a.weights = weights; a.out = static_cast<uint16_t *>(out);
     a.ld_y = ld_y; a.ld_out = ld_out; a.top_k = top_k; a.hidden = hidden;
-    hipLaunchKernelGGL(combine_kernel, dim3((unsigned)tokens), dim3(256), 0, ctx->stream, a);
+    hipLaunchKernelGGL(combine_kernel, dim3((unsigned)tokens, (unsigned)((hidden + 2047) / 2048)), dim3(256), 0, ctx->stream, a);
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;
 }
