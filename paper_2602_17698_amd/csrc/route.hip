@@ -214,10 +214,10 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
         // two groups' sums are certain to be as they seem if they are further apart than both may be off: four scores, two of them of this group
         // (twice as far where the other two are as large; no p is above one_by, that of the largest logit)
         const float tolerance = 4.0f * by_p * one_by + 0x1p-20f * (fabsf(v1) + (second == NONE ? 0.0f : fabsf(v2)));
-        int rank = 0;
+        int rank = 0;                                           // (of groups that are the same: the choice is open, or they are empty)
         for (int o = 0; o < a.groups; ++o) {
             const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(worth), o << a.log_lanes));
-            rank += other > worth || (other == worth && o < group);
+            rank += other > worth;
             open = open || (o != group && fabsf(other - worth) <= tolerance);           // (not where one of them is infinite)
         }
         open = a.top_groups < a.groups && group < a.groups && open;
@@ -229,30 +229,46 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
 #pragma unroll
         for (int r = 0; r < PER; ++r) key[r] = x[r] > -HUGE_VALF && (a.groups == 1 || key[r] != NONE) ? ordered(x[r]) : NONE;
     }
+    // a lane's keys, the largest first, of equal ones the lower expert's
+    int reg[PER];
+#pragma unroll
+    for (int r = 0; r < PER; ++r) reg[r] = r;
+#pragma unroll
+    for (int pass = 0; pass < PER; ++pass)
+#pragma unroll
+        for (int r = pass & 1; r + 1 < PER; r += 2) {
+            const bool swap = key[r + 1] > key[r];
+            const int k = max(key[r], key[r + 1]), i = swap ? reg[r + 1] : reg[r];
+            key[r + 1] = min(key[r], key[r + 1]);
+            reg[r + 1] = swap ? reg[r] : reg[r + 1];
+            key[r] = k;
+            reg[r] = i;
+        }
     int my_key = NONE;
     my_id = -1;
     for (int j = 0; j < a.top_k; ++j) {
-        int best = key[0];
-#pragma unroll
-        for (int r = 1; r < PER; ++r) best = max(best, key[r]);
-        const int all = over_lanes<6>(best, Largest{});
+        const int all = __builtin_amdgcn_readfirstlane(over_lanes<6>(key[0], Largest{}));
         if (all == NONE) break;
-        // the lowest expert with this key: the lane's lowest, then, if there is more than one lane, the lowest of the lanes
-        int reg = PER - 1;
-#pragma unroll
-        for (int r = PER - 2; r >= 0; --r) reg = key[r] == all ? r : reg;
-        const uint64_t who = __ballot(best == all);
-        int winner = __ffsll((unsigned long long)who) - 1;
-        const int at = first + reg * lanes;
+        // the lowest expert with this key: of several lanes' the lowest
+        const uint64_t who = __ballot(key[0] == all);
+        int winner = __builtin_ctzll(who);
+        const int at = first + reg[0] * lanes;
         if (who & (who - 1)) {
-            const int lowest = over_lanes<6>(best == all ? at : INT32_MAX, Smallest{});
-            winner = __ffsll((unsigned long long)__ballot(best == all && at == lowest)) - 1;
+            const int lowest = __builtin_amdgcn_readfirstlane(over_lanes<6>(key[0] == all ? at : INT32_MAX, Smallest{}));
+            winner = __builtin_ctzll(__ballot(key[0] == all && at == lowest));
         }
-        const int taken = lane == winner ? reg : -1;
-#pragma unroll
-        for (int r = 0; r < PER; ++r) key[r] = taken == r ? NONE : key[r];
         const int id = __builtin_amdgcn_readlane(at, winner);
-        if (lane == j) { my_id = id; my_key = all; }
+        my_id = lane == j ? id : my_id;
+        my_key = lane == j ? all : my_key;
+        const bool mine = lane == winner;
+#pragma unroll
+        for (int r = 0; r + 1 < PER; ++r) {
+            int k = key[r + 1], i = reg[r + 1];
+            asm("" : "+v"(k), "+v"(i));                         // (else this becomes an array with an index, of a select for each entry)
+            key[r] = mine ? k : key[r];
+            reg[r] = mine ? i : reg[r];
+        }
+        key[PER - 1] = mine ? NONE : key[PER - 1];
     }
     my_p = 0.0f;
     if (my_id >= 0) my_p = chance(logit_at<BF16>(a.logits, token * a.ld + my_id));
@@ -262,12 +278,9 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
         const float v = unordered(my_key), my_off = fmaf(by_p, my_p, 0x1p-22f * fabsf(v));
         bool close = lane + 1 < n && v - my_off <= __shfl_down(v + my_off, 1);
         if (n > 0) {
-            const float last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v - my_off), n - 1));
-#pragma unroll
-            for (int r = 0; r < PER; ++r) {
-                const float u = unordered(key[r]);
-                close = close || (key[r] != NONE && fmaf(by_p, p[r], fmaf(0x1p-22f, fabsf(u), u)) >= last);
-            }
+            // (what is left of a lane is below its first key; off by no more than any p of its own may be, one_by at most)
+            const float last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v - my_off), n - 1)), u = unordered(key[0]);
+            close = close || (key[0] != NONE && fmaf(by_p, one_by, fmaf(0x1p-22f, fabsf(u), u)) >= last);
         }
         open = open || close;
     }
