@@ -332,11 +332,12 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
                                 else reinterpret_cast<float *>(y)[k] = value(m, r, k);
                             }
                     } else if constexpr (BF16) {
-                        if constexpr (HAS == 4) *reinterpret_cast<u32x2 *>(y) = u32x2{bf16_pair(value(m, r, 0), value(m, r, 1)), bf16_pair(value(m, r, 2), value(m, r, 3))};
-                        else *reinterpret_cast<uint32_t *>(y) = bf16_pair(value(m, r, 0), value(m, r, 1));
+                        // (past the caches: nothing here reads it, and what lies there at a kernel's end is written back then)
+                        if constexpr (HAS == 4) __builtin_nontemporal_store(u32x2{bf16_pair(value(m, r, 0), value(m, r, 1)), bf16_pair(value(m, r, 2), value(m, r, 3))}, reinterpret_cast<u32x2 *>(y));
+                        else __builtin_nontemporal_store(bf16_pair(value(m, r, 0), value(m, r, 1)), reinterpret_cast<uint32_t *>(y));
                     } else {
-                        if constexpr (HAS == 4) *reinterpret_cast<f32x4 *>(y) = f32x4{value(m, r, 0), value(m, r, 1), value(m, r, 2), value(m, r, 3)};
-                        else *reinterpret_cast<float2 *>(y) = make_float2(value(m, r, 0), value(m, r, 1));
+                        if constexpr (HAS == 4) __builtin_nontemporal_store(f32x4{value(m, r, 0), value(m, r, 1), value(m, r, 2), value(m, r, 3)}, reinterpret_cast<f32x4 *>(y));
+                        else __builtin_nontemporal_store(f32x2{value(m, r, 0), value(m, r, 1)}, reinterpret_cast<f32x2 *>(y));
                     }
                     __builtin_amdgcn_sched_barrier(0);             // (else the addresses of all rows are made ahead, in registers that are not there)
                 }
