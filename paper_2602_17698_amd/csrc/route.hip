@@ -1,15 +1,19 @@
 // Routing to experts: the choice with its weights, the gradient, the lists by expert, the weighted sum.
+#include <type_traits>
+
 #include "mx_core.hpp"
 
 namespace sbits {
 
 // ---- the choice ------------------------------------------------------------------
-// A wave a token.  Groups lie in `lanes` = 2^k neighbouring lanes each (64 without groups): expert i of group g is in lane g * lanes + i % lanes,
-// register i / lanes.
+// A wave a token, or half of one.  Groups lie in `lanes` = 2^k neighbouring lanes each (all without groups): expert i of group g is in lane
+// g * lanes + i % lanes, register i / lanes.
 //
 // Which experts are taken is decided as with scores in 64 bits, but scores are computed in fp32 first, with a bound on how far each
-// may be off; only where the bounds leave the choice or its order open (a token in some hundred) the wave goes on to 64 bits.  In 64 bits for every
-// token 16384 x 256 took 52 us.  Instruction issue bounds it: top_k searches of the largest key, some 30 instructions each.
+// may be off.  Where the bounds leave only the order of the chosen ones open, these are computed in 64 bits and put in order (a token in some hundred with
+// sigmoid scores and a bias); only where they leave the choice open (one in a thousand) all are.  In 64 bits for every token 16384 x 256 took 52 us.
+// 16384 tokens of 256 experts, 8 groups, a bias, the best 8: 21 us, 0.8 TB/s.  Instruction issue bounds it: a wave has some 450 of 4 cycles for a token, half of them
+// in the top_k searches of the largest key.  Without groups, bias and sigmoid 15 us; 2048 tokens 7.
 struct RouteArgs {
     const void *logits;
     const float *bias;
@@ -33,24 +37,33 @@ __device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0
 template <int LOG, class V, class F>
 __device__ __forceinline__ V over_lanes(V v, F f)
 {
-    auto bits = [](V x) { return __builtin_bit_cast(int, x); };
-    auto back = [](int x) { return __builtin_bit_cast(V, x); };
-    if constexpr (LOG >= 1) v = f(v, back(dpp<DPP_XOR1>(bits(v))));
-    if constexpr (LOG >= 2) v = f(v, back(dpp<DPP_XOR2>(bits(v))));
-    if constexpr (LOG >= 3) v = f(v, back(dpp<DPP_HALF_MIRROR>(bits(v))));
-    if constexpr (LOG >= 4) v = f(v, back(dpp<DPP_MIRROR>(bits(v))));
-    if constexpr (LOG >= 5) {
-        auto w = __builtin_amdgcn_permlane16_swap(bits(v), bits(v), false, false);
-        v = f(back((int)w[0]), back((int)w[1]));
-    }
-    if constexpr (LOG >= 6) {
-        auto w = __builtin_amdgcn_permlane32_swap(bits(v), bits(v), false, false);
-        v = f(back((int)w[0]), back((int)w[1]));
-    }
+    struct Words { int w[sizeof(V) / 4]; };
+    auto with = [&](auto other) {
+        Words a = __builtin_bit_cast(Words, v);
+        for (int &w : a.w) w = other(w);
+        v = f(v, __builtin_bit_cast(V, a));
+    };
+    auto halves = [&](auto swap) {
+        Words a = __builtin_bit_cast(Words, v), b = a;
+        for (unsigned i = 0; i < sizeof(V) / 4; ++i) {
+            auto both = swap(a.w[i]);
+            a.w[i] = (int)both[0]; b.w[i] = (int)both[1];
+        }
+        v = f(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b));
+    };
+    if constexpr (LOG >= 1) with([](int w) { return dpp<DPP_XOR1>(w); });
+    if constexpr (LOG >= 2) with([](int w) { return dpp<DPP_XOR2>(w); });
+    if constexpr (LOG >= 3) with([](int w) { return dpp<DPP_HALF_MIRROR>(w); });
+    if constexpr (LOG >= 4) with([](int w) { return dpp<DPP_MIRROR>(w); });
+    if constexpr (LOG >= 5) halves([](int w) { return __builtin_amdgcn_permlane16_swap(w, w, false, false); });
+    if constexpr (LOG >= 6) halves([](int w) { return __builtin_amdgcn_permlane32_swap(w, w, false, false); });
     return v;
 }
-struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
-struct Largest { __device__ __forceinline__ int operator()(int a, int b) const { return max(a, b); } };
+struct Add { template <class V> __device__ __forceinline__ V operator()(V a, V b) const { return a + b; } };
+struct Largest {
+    __device__ __forceinline__ int operator()(int a, int b) const { return max(a, b); }
+    __device__ __forceinline__ double operator()(double a, double b) const { return fmax(a, b); }
+};
 struct Smallest { __device__ __forceinline__ int operator()(int a, int b) const { return min(a, b); } };
 
 // whole numbers in the order of the numbers (0 and -0 the same)
@@ -71,7 +84,7 @@ __device__ __forceinline__ float exp_of(float v)
 }
 
 // The choice in 64 bits: lane j < top_k gets the j-th expert, or -1, and its p.
-template <int PER>
+template <int PER, int LOG>
 __device__ __forceinline__ void choose_exactly(const RouteArgs &a, int lane, const float (&x)[PER], const float (&b)[PER], int &id, float &p_of)
 {
     const double none = -HUGE_VAL;
@@ -84,7 +97,7 @@ __device__ __forceinline__ void choose_exactly(const RouteArgs &a, int lane, con
         fine[r] = fabsf(x[r]) < HUGE_VALF && fabsf(b[r]) < HUGE_VALF;
         if (fabsf(x[r]) < HUGE_VALF) top_key = max(top_key, ordered(x[r]));
     }
-    top_key = over_lanes<6>(top_key, Largest{});
+    top_key = over_lanes<LOG>(top_key, Largest{});
     const float top = top_key == NONE ? 0.0f : unordered(top_key);
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
@@ -92,7 +105,7 @@ __device__ __forceinline__ void choose_exactly(const RouteArgs &a, int lane, con
         p[r] = !there ? 0.0 : a.sigmoid ? 1.0 / (1.0 + exp(-(double)x[r])) : exp((double)x[r] - (double)top);
         sum += p[r];
     }
-    for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
+    sum = over_lanes<LOG>(sum, Add{});
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
         if (!a.sigmoid) p[r] = sum > 0.0 ? p[r] / sum : 0.0;
@@ -114,7 +127,7 @@ __device__ __forceinline__ void choose_exactly(const RouteArgs &a, int lane, con
         int rank = 0;
         const int mine = lane >> a.log_lanes;
         for (int o = 0; o < a.groups; ++o) {
-            const double other = __shfl(worth, o << a.log_lanes);
+            const double other = __shfl(worth, o << a.log_lanes, 1 << LOG);
             rank += other > worth || (other == worth && o < mine);
         }
 #pragma unroll
@@ -131,47 +144,66 @@ __device__ __forceinline__ void choose_exactly(const RouteArgs &a, int lane, con
     p_of = 0.0f;
     for (int j = 0; j < a.top_k; ++j) {
         double best = none;
+        float w = 0.0f;
         int at = INT32_MAX;
 #pragma unroll
         for (int r = 0; r < PER; ++r)
-            if (key[r] > best) { best = key[r]; at = first + r * lanes; }
-        for (int s = 1; s < 64; s <<= 1) {
-            const double other = __shfl_xor(best, s);
-            const int o = __shfl_xor(at, s);
-            if (other > best || (other == best && o < at)) { best = other; at = o; }
-        }
-        if (best == none) break;
-        double w = 0.0;
+            if (key[r] > best) { best = key[r]; w = (float)p[r]; at = first + r * lanes; }
+        const double all = over_lanes<LOG>(best, Largest{});
+        if (__ballot(all != none) == 0) break;
+        const int lowest = over_lanes<LOG>(best == all ? at : INT32_MAX, Smallest{});
+        const bool mine = at == lowest;
+        // (one lane's, the others' 0)
+        const float p_at = over_lanes<LOG>(mine ? w : 0.0f, Add{});
 #pragma unroll
         for (int r = 0; r < PER; ++r)
-            if (key[r] > none && first + r * lanes == at) { w = p[r]; key[r] = none; }
-        for (int s = 1; s < 64; s <<= 1) w += __shfl_xor(w, s);
-        if (lane == j) { id = at; p_of = (float)w; }
+            if (mine && first + r * lanes == at) key[r] = none;
+        if (lane == j && all != none) { id = lowest; p_of = p_at; }
     }
 }
 
-// One token: lane j < top_k gets the j-th expert, or -1, and its weight; both are written.
-template <bool BF16, int PER>
+// One token, by 2^LOG lanes: lane j < top_k gets the j-th expert, or -1, and its weight; both are written.
+template <bool BF16, int PER, int LOG>
 __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, int lane, int &my_id)
 {
     float my_p;
+    constexpr int LANES = 1 << LOG;
+    const int base = (int)(threadIdx.x & 63 & -LANES);          // the wave's lane that is this token's first
+    auto ballot = [&](bool v) -> uint64_t {                     // of the token's lanes
+        const uint64_t all = __ballot(v);
+        if constexpr (LOG == 6) return all;
+        return (uint32_t)(base ? all >> 32 : all);
+    };
+    // the value of the token's lane `from`, the same for all of them
+    auto of_lane = [&](int v, int from) {
+        if constexpr (LOG == 6) return __builtin_amdgcn_readlane(v, from);
+        return __builtin_amdgcn_ds_bpermute(4 * (base + from), v);
+    };
+    auto uniform = [](int v) { return LOG == 6 ? __builtin_amdgcn_readfirstlane(v) : v; };
     const int lanes = 1 << a.log_lanes, group = lane >> a.log_lanes, in_group = lane & (lanes - 1), first = group * a.each + in_group;
     float x[PER], b[PER], p[PER];
     int key[PER], top_key = NONE;
+    const int64_t row = token * a.ld;
+    // (all lanes load, without a branch: those without an expert the first one's)
+    bool there[PER];
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
-        const bool there = group < a.groups && r * lanes + in_group < a.each;
-        x[r] = there ? logit_at<BF16>(a.logits, token * a.ld + first + r * lanes) : -HUGE_VALF;
-        b[r] = a.bias && there ? a.bias[first + r * lanes] : 0.0f;
+        there[r] = group < a.groups && r * lanes + in_group < a.each;
+        x[r] = logit_at<BF16>(a.logits, row + (there[r] ? first + r * lanes : 0));
+        b[r] = 0.0f;
+    }
+    if (a.bias) {
+#pragma unroll
+        for (int r = 0; r < PER; ++r) b[r] = a.bias[there[r] ? first + r * lanes : 0];
     }
 #pragma unroll
-    for (int r = 0; r < PER; ++r) x[r] = fabsf(x[r]) < HUGE_VALF ? x[r] : -HUGE_VALF;         // (p = 0 below, without a branch)
+    for (int r = 0; r < PER; ++r) x[r] = there[r] & (fabsf(x[r]) < HUGE_VALF) ? x[r] : -HUGE_VALF;         // (p = 0 below, without a branch)
     float top = 0.0f, one_by = 1.0f;
     if (!a.sigmoid) {
 #pragma unroll
         for (int r = 0; r < PER; ++r)
             top_key = max(top_key, ordered(x[r]));
-        top = unordered(over_lanes<6>(top_key, Largest{}));
+        top = unordered(over_lanes<LOG>(top_key, Largest{}));
         if (top == -HUGE_VALF) top = 0.0f;
         float sum = 0.0f;
 #pragma unroll
@@ -179,7 +211,7 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
             p[r] = exp_of(x[r] - top);
             sum += p[r];
         }
-        one_by = __builtin_amdgcn_rcpf(fmaxf(over_lanes<6>(sum, Add{}), 1e-30f));
+        one_by = __builtin_amdgcn_rcpf(fmaxf(over_lanes<LOG>(sum, Add{}), 1e-30f));
     }
     auto chance = [&](float v) { return a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + exp_of(-v)) : exp_of(v - top) * one_by; };
     // Scores p + b, each off by less than by_p * p + 2^-22 |p + b|.  by_p: of a sigmoid 2^-21 (exp and reciprocal 4 units in the last place), of softmax
@@ -188,12 +220,17 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
     const float by_p = a.sigmoid ? 0x1p-21f : 0x1p-18f;
     bool open = false;                                          // whether fp32 leaves the choice open
     if (a.bias || a.groups > 1) {
+        if (a.sigmoid) {
+#pragma unroll
+            for (int r = 0; r < PER; ++r) p[r] = __builtin_amdgcn_rcpf(1.0f + exp_of(-x[r]));
+        } else {
+#pragma unroll
+            for (int r = 0; r < PER; ++r) p[r] *= one_by;
+        }
 #pragma unroll
         for (int r = 0; r < PER; ++r) {
-            if (a.sigmoid) p[r] = __builtin_amdgcn_rcpf(1.0f + exp_of(-x[r]));
-            else p[r] *= one_by;
             const float v = p[r] + b[r];
-            key[r] = x[r] > -HUGE_VALF && fabsf(v) < HUGE_VALF ? ordered(v) : NONE;
+            key[r] = (x[r] > -HUGE_VALF) & (fabsf(v) < HUGE_VALF) ? ordered(v) : NONE;
         }
     }
     if (a.groups > 1) {
@@ -211,16 +248,16 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
         }
         const float v1 = unordered(best), v2 = unordered(second);
         const float worth = best == NONE ? -HUGE_VALF : a.best_only || second == NONE ? v1 : v1 + v2;
-        // two groups' sums are certain to be as they seem if they are further apart than both may be off: four scores, two of them of this group
-        // (twice as far where the other two are as large; no p is above one_by, that of the largest logit)
-        const float tolerance = 4.0f * by_p * one_by + 0x1p-20f * (fabsf(v1) + (second == NONE ? 0.0f : fabsf(v2)));
-        int rank = 0;                                           // (of groups that are the same: the choice is open, or they are empty)
-        for (int o = 0; o < a.groups; ++o) {
-            const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(worth), o << a.log_lanes));
-            rank += other > worth;
-            open = open || (o != group && fabsf(other - worth) <= tolerance);           // (not where one of them is infinite)
-        }
-        open = a.top_groups < a.groups && group < a.groups && open;
+        int rank = 0;                                           // (of groups that are the same: the lowest)
+        for (int o = 0; o < a.groups; ++o) rank += __int_as_float(of_lane(__float_as_int(worth), o << a.log_lanes)) > worth;
+        // open, unless as many are taken as should be, and the lowest of them less what it may be off (two scores, whose p are below that of the largest
+        // logit, one_by, and their sum) is above the highest of the others; groups without a score do not count
+        const float off = 2.0f * by_p * one_by + 0x1p-21f * (fabsf(v1) + (second == NONE ? 0.0f : fabsf(v2)));
+        const bool counts = group < a.groups && best != NONE, taken = rank < a.top_groups;
+        const int lowest = over_lanes<LOG>(counts && taken ? ordered(worth - off) : INT32_MAX, Smallest{});
+        const int highest = over_lanes<LOG>(counts && !taken ? ordered(worth + off) : NONE, Largest{});
+        const int n = __popcll(ballot(counts && in_group == 0)), n_taken = __popcll(ballot(counts && taken && in_group == 0));
+        open = lowest <= highest || n_taken != min(n, a.top_groups) || (counts && !(fabsf(worth) < HUGE_VALF));
 #pragma unroll
         for (int r = 0; r < PER; ++r)
             if (rank >= a.top_groups) key[r] = NONE;
@@ -244,48 +281,75 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
             key[r] = k;
             reg[r] = i;
         }
+    // the registers they came from, the first one's in the lowest bits
+    typedef typename std::conditional<(PER > 8), uint64_t, uint32_t>::type Order;
+    Order order = 0;
+#pragma unroll
+    for (int r = 0; r < PER; ++r) order |= (Order)reg[r] << 4 * r;
     int my_key = NONE;
     my_id = -1;
     for (int j = 0; j < a.top_k; ++j) {
-        const int all = __builtin_amdgcn_readfirstlane(over_lanes<6>(key[0], Largest{}));
-        if (all == NONE) break;
+        const int all = uniform(over_lanes<LOG>(key[0], Largest{}));
+        if (LOG == 6 ? all == NONE : __ballot(all != NONE) == 0) break;
         // the lowest expert with this key: of several lanes' the lowest
-        const uint64_t who = __ballot(key[0] == all);
-        int winner = __builtin_ctzll(who);
-        const int at = first + reg[0] * lanes;
-        if (who & (who - 1)) {
-            const int lowest = __builtin_amdgcn_readfirstlane(over_lanes<6>(key[0] == all ? at : INT32_MAX, Smallest{}));
-            winner = __builtin_ctzll(__ballot(key[0] == all && at == lowest));
+        uint64_t who = ballot(key[0] == all);
+        const int at = first + (int)(order & 15) * lanes;
+        if (LOG == 6 ? __popcll(who) > 1 : __ballot((who & (who - 1)) != 0) != 0) {
+            const int lowest = over_lanes<LOG>(key[0] == all ? at : INT32_MAX, Smallest{});
+            who = ballot(key[0] == all && at == lowest);
         }
-        const int id = __builtin_amdgcn_readlane(at, winner);
+        const int winner = __builtin_ctzll(who), id = LOG < 6 && all == NONE ? -1 : of_lane(at, winner);
         my_id = lane == j ? id : my_id;
         my_key = lane == j ? all : my_key;
-        const bool mine = lane == winner;
+        int mine = lane == winner ? -1 : 0;
+        asm("" : "+v"(mine));                                   // (else the keys become an array with an index, of a select for each entry)
 #pragma unroll
-        for (int r = 0; r + 1 < PER; ++r) {
-            int k = key[r + 1], i = reg[r + 1];
-            asm("" : "+v"(k), "+v"(i));                         // (else this becomes an array with an index, of a select for each entry)
-            key[r] = mine ? k : key[r];
-            reg[r] = mine ? i : reg[r];
-        }
-        key[PER - 1] = mine ? NONE : key[PER - 1];
+        for (int r = 0; r + 1 < PER; ++r) key[r] = (key[r] & ~mine) | (key[r + 1] & mine);
+        key[PER - 1] = (key[PER - 1] & ~mine) | (NONE & mine);
+        order >>= 4 & mine;
     }
     my_p = 0.0f;
     if (my_id >= 0) my_p = chance(logit_at<BF16>(a.logits, token * a.ld + my_id));
+    bool unordered_ones = false;                                // whether fp32 leaves only the order of the chosen ones open
     if (a.bias) {                                               // (without a bias keys are the logits themselves)
         // each chosen score against the next, the last against all that are left
-        const int n = __popcll(__ballot(my_id >= 0));
+        const int n = __popcll(ballot(my_id >= 0));
         const float v = unordered(my_key), my_off = fmaf(by_p, my_p, 0x1p-22f * fabsf(v));
-        bool close = lane + 1 < n && v - my_off <= __shfl_down(v + my_off, 1);
+        const float next = __shfl_down(v + my_off, 1);          // (of all lanes: not behind a condition)
+        unordered_ones = lane + 1 < n && v - my_off <= next;
         if (n > 0) {
             // (what is left of a lane is below its first key; off by no more than any p of its own may be, one_by at most)
-            const float last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v - my_off), n - 1)), u = unordered(key[0]);
-            close = close || (key[0] != NONE && fmaf(by_p, one_by, fmaf(0x1p-22f, fabsf(u), u)) >= last);
+            const float last = __int_as_float(of_lane(__float_as_int(v - my_off), n - 1)), u = unordered(key[0]);
+            open = open || (key[0] != NONE && fmaf(by_p, one_by, fmaf(0x1p-22f, fabsf(u), u)) >= last);
         }
-        open = open || close;
+        if (!a.sigmoid) open = open || unordered_ones;          // (a sum over all experts is needed)
     }
-    if (__ballot(open) != 0) choose_exactly<PER>(a, lane, x, b, my_id, my_p);
-    const float total = a.renormalize ? over_lanes<6>(my_p, Add{}) : 1.0f;
+    // (a token's result does not depend on its neighbour's)
+    const bool exactly = ballot(open) != 0, sort = a.sigmoid && !exactly && ballot(unordered_ones) != 0;
+    if (__ballot(exactly) != 0) {
+        int id;
+        float p_of;
+        choose_exactly<PER, LOG>(a, lane, x, b, id, p_of);
+        if (exactly) { my_id = id; my_p = p_of; }
+    }
+    if (__ballot(sort) != 0) {
+        double p_of = 0.0, score = -HUGE_VAL;
+        if (my_id >= 0) {
+            p_of = 1.0 / (1.0 + exp(-(double)logit_at<BF16>(a.logits, row + my_id)));
+            score = p_of + (double)a.bias[my_id];
+        }
+        int place = 0;
+        for (int j = 0; j < a.top_k; ++j) {
+            const double other = __shfl(score, j, LANES);
+            const int its_id = __shfl(my_id, j, LANES);
+            place += (other > score) | ((other == score) & (its_id < my_id));
+        }
+        if (my_id < 0 || !sort) place = lane;
+        const float p_new = __int_as_float(__builtin_amdgcn_ds_permute(4 * (base + place), __float_as_int(sort ? (float)p_of : my_p)));
+        my_id = __builtin_amdgcn_ds_permute(4 * (base + place), my_id);
+        my_p = p_new;
+    }
+    const float total = a.renormalize ? over_lanes<LOG>(my_p, Add{}) : 1.0f;
     if (lane < a.top_k) {
         if (a.renormalize) my_p = total > 0.0f ? my_p / total : 0.0f;
         a.ids[token * a.top_k + lane] = my_id;
@@ -293,14 +357,13 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
     }
 }
 
-template <bool BF16, int PER>
+template <bool BF16, int PER, int LOG>
 __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t token = (int64_t)blockIdx.x * 4 + wave;
+    const int64_t token = (int64_t)blockIdx.x * (256 >> LOG) + (threadIdx.x >> LOG);
     if (token >= a.tokens) return;
     int id;
-    route_token<BF16, PER>(a, token, lane, id);
+    route_token<BF16, PER, LOG>(a, token, (int)(threadIdx.x & ((1 << LOG) - 1)), id);
 }
 
 // ---- its gradient ----------------------------------------------------------------
@@ -484,7 +547,7 @@ __global__ __launch_bounds__(1024) void route_and_list_kernel(RouteArgs a, int t
     if (wave < a.tokens) {
         const int token = wave;
         int id;
-        route_token<BF16, PER>(a, token, lane, id);
+        route_token<BF16, PER, 6>(a, token, lane, id);
         if (lane < a.top_k) {
             ids[token * a.top_k + lane] = id;
             if (id >= 0) atomicAdd(&counts[id], 1);
@@ -577,9 +640,11 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a)
 using namespace sbits;
 
 template <bool BF16>
-static auto route_instance(int per)
+static auto route_instance(int per, int log)
 {
-    return per <= 1 ? route_kernel<BF16, 1> : per <= 2 ? route_kernel<BF16, 2> : per <= 4 ? route_kernel<BF16, 4> : per <= 8 ? route_kernel<BF16, 8> : route_kernel<BF16, 16>;
+    if (log == 5) return per <= 1 ? route_kernel<BF16, 1, 5> : per <= 2 ? route_kernel<BF16, 2, 5> : route_kernel<BF16, 4, 5>;
+    return per <= 1 ? route_kernel<BF16, 1, 6> : per <= 2 ? route_kernel<BF16, 2, 6> : per <= 4 ? route_kernel<BF16, 4, 6>
+         : per <= 8 ? route_kernel<BF16, 8, 6> : route_kernel<BF16, 16, 6>;
 }
 template <bool BF16>
 static auto route_and_list_instance(int per)
@@ -593,24 +658,37 @@ static auto route_backward_instance(int experts)
          : experts <= 256 ? route_backward_kernel<BF16, 4> : route_backward_kernel<BF16, 8>;
 }
 
-// the arguments; returns the registers of a lane: at most 15, as at least 33 lanes are in use
-static int route_args(const sbits_router &r, const void *logits, int64_t ld, const float *bias, int64_t tokens, int32_t *ids, float *weights, RouteArgs &a)
+// the arguments; returns the registers of a lane: at most 15, as more than half of the 2^log lanes are in use
+static int route_args(const sbits_router &r, int log, const void *logits, int64_t ld, const float *bias, int64_t tokens, int32_t *ids, float *weights, RouteArgs &a)
 {
     a.logits = logits; a.bias = bias; a.ids = ids; a.weights = weights; a.ld = ld; a.tokens = tokens;
     a.experts = r.experts; a.top_k = r.top_k; a.groups = r.groups; a.top_groups = r.top_groups; a.each = r.experts / r.groups;
     a.sigmoid = r.scoring == SBITS_ROUTE_SIGMOID; a.best_only = r.group_score == SBITS_ROUTE_GROUP_MAX; a.renormalize = r.renormalize;
     a.log_lanes = 0;
-    while (r.groups << (a.log_lanes + 1) <= 64) ++a.log_lanes;
+    while (r.groups << (a.log_lanes + 1) <= 1 << log) ++a.log_lanes;
     return (a.each + (1 << a.log_lanes) - 1) >> a.log_lanes;
+}
+
+// Two tokens to a wave, where that leaves 4 waves to each SIMD, and 4 registers of keys are enough.  16384 tokens of 32, 64, 128 and 256 experts by one to a wave
+// 11.5, 11.2, 12.6 and 21.2 us, by two 7.8, 9.0, 10.8 and (8 registers, whose order takes 28 exchanges) 26.5; 5000 tokens of 32 experts 6.0 and 5.3.
+static bool two_a_wave(const sbits_ctx *ctx, const sbits_router &r, int64_t tokens)
+{
+    return r.groups <= 32 && tokens >= 16 * (int64_t)sbits_cus(ctx);
 }
 
 int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits, bool bf16, int64_t ld, const float *bias, int64_t tokens,
                        int32_t *ids, float *weights)
 {
     RouteArgs a;
-    const int per = route_args(r, logits, ld, bias, tokens, ids, weights, a);
-    auto fn = bf16 ? route_instance<true>(per) : route_instance<false>(per);
-    hipLaunchKernelGGL(fn, dim3((unsigned)((tokens + 3) / 4)), dim3(256), 0, ctx->stream, a);
+    int log = 6, per = route_args(r, 6, logits, ld, bias, tokens, ids, weights, a);
+    if (two_a_wave(ctx, r, tokens)) {
+        RouteArgs half;
+        const int more = route_args(r, 5, logits, ld, bias, tokens, ids, weights, half);
+        if (more <= 4) { a = half; log = 5; per = more; }
+    }
+    auto fn = bf16 ? route_instance<true>(per, log) : route_instance<false>(per, log);
+    const int each = 256 >> log;
+    hipLaunchKernelGGL(fn, dim3((unsigned)((tokens + each - 1) / each)), dim3(256), 0, ctx->stream, a);
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;
 }
@@ -619,7 +697,7 @@ int sbits_launch_route_and_list(sbits_ctx *ctx, const sbits_router &r, const voi
                                 int32_t *ids, float *weights, int tile_rows, int max_tiles, int *sorted, int *token_of, MxTile *tiles)
 {
     RouteArgs a;
-    const int per = route_args(r, logits, ld, bias, tokens, ids, weights, a);
+    const int per = route_args(r, 6, logits, ld, bias, tokens, ids, weights, a);
     if (tokens > HERE || per > 4) {                             // (more registers than 16 waves have)
         const int rc = sbits_launch_route(ctx, r, logits, bf16, ld, bias, tokens, ids, weights);
         if (rc) return rc;

@@ -66,6 +66,31 @@ def test_route(ctx, router, kind, biased, tokens):
 
 
 @pytest.mark.parametrize("router", ROUTERS, ids=lambda r: "-".join("%s%d" % i for i in r.items()))
+@pytest.mark.parametrize("kind,biased", [(torch.float32, True), (torch.bfloat16, False)])
+def test_route_of_many_tokens(ctx, router, kind, biased):
+    """More tokens than waves have room for one by one; pairs of which one alone leaves the choice open, and an odd last one."""
+    test_route(ctx, router, kind, biased, 16 * torch.cuda.get_device_properties(0).multi_processor_count + 1)
+
+
+@pytest.mark.parametrize("router", [dict(experts=32, top_k=4, groups=4, top_groups=2, scoring=1), dict(experts=256, top_k=8, groups=8, top_groups=4, scoring=1),
+                                    dict(experts=96, top_k=6, scoring=1), dict(experts=128, top_k=8, groups=4, top_groups=2, group_score=1),
+                                    dict(experts=64, top_k=8)], ids=lambda r: "-".join("%s%d" % i for i in r.items()))
+@pytest.mark.parametrize("apart,bias_apart,tokens", [(a, b, 301) for a in (1e-7, 1e-6, 1e-5, 1e-4) for b in (0.0, 1e-6, 0.05)] + [(1e-5, 1e-6, 4301), (1e-5, 0.05, 4301)])
+def test_route_of_scores_close_to_each_other(ctx, router, apart, bias_apart, tokens):
+    """Scores about as far apart as fp32 can tell: eight logits, repeated with small changes; the choice is that of 64 bits."""
+    r, g = sb.Router(**router), gen(tokens)
+    logits = torch.randn(tokens, 8, generator=g).repeat(1, r.experts // 8)
+    logits += apart * torch.randn(tokens, r.experts, generator=g)
+    bias = bias_apart * torch.randn(r.experts, generator=g) if bias_apart else None
+    ids = torch.empty(tokens, r.top_k, dtype=torch.int32, device="cuda")
+    weights = torch.empty(tokens, r.top_k, device="cuda")
+    ctx.route(r, logits.cuda(), bias.cuda() if bias_apart else None, ids, weights)
+    want, w = mp.route(r, logits, bias)
+    assert torch.equal(ids.cpu(), want)
+    assert bool(((weights.cpu().double() - w).abs() <= 64 * 2.0 ** -24 * w).all())
+
+
+@pytest.mark.parametrize("router", ROUTERS, ids=lambda r: "-".join("%s%d" % i for i in r.items()))
 @pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("tokens", [1, 29])
 def test_route_backward(ctx, router, kind, tokens):
