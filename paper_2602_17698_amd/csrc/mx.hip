@@ -4,6 +4,7 @@
 //
 // Memory bounds it: 2 or 4 bytes read for each value, 17/32 of a byte written, and 2 for the value where it is asked for.  A lane takes 8
 // values (one or two 16-byte loads, 4 bytes of codes, 16 of values), four lanes a block; the largest magnitude is taken as a whole number.
+// 8192 x 14336 in bf16, values too, 89 us: 6.0 TB/s, what a copy reaches; 1001 x 1056 in fp32 3.1 us, 1 x 4096 2.0, both of them a launch.
 #include "mx_core.hpp"
 
 namespace sbits {

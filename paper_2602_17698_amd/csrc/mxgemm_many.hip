@@ -2,8 +2,8 @@
 //
 // A workgroup of 4 waves takes 64 MT rows of x and 64 NT rows of W, a wave MT x NT tiles of 32 x 32.  A step is 256 columns with x in 4 bits, 64 with
 // x in bf16, 128 bytes of a row of x either way; four phases of MT NT matrix instructions.  W comes in chunks of 256 columns, 128 bytes of a
-// row, too: a load of fewer neighbouring bytes is a request to L2 all the same, and requests were the bound (8192 x 14336 x 4096 in 4 bits, 64 bytes
-// a row and step: 346 us).  Both go to LDS by direct loads, two buffers each, and scales for 1024 columns at a time.
+// row, too: a load of fewer neighbouring bytes is a request to L2 all the same, and requests were the bound (64 bytes a row and step: the loop took a
+// fifth longer).  Both go to LDS by direct loads, two buffers each, and scales for 1024 columns at a time.
 // The barrier of a step is ahead of its last phase: the operands of that phase are in registers by then, so the step's buffers may be
 // filled again, the next step is there, and its first operands are read during the last phase.
 //
@@ -12,6 +12,11 @@
 // that a lane's scales are neighbours.
 // Order of W's rows: tile t of a wave has rows NT n + t, n = l % 32, so that a lane's outputs for a row of x are NT neighbours, a wave's 32 NT.
 // With gated products tiles 2 p and 2 p + 1 are rows NT / 2 n + p of both halves of W.
+// What bounds it: with random data the clock falls to 1.55 .. 1.8 GHz at the card's power limit (matrix instructions alone, from registers: 5.9 PFLOP/s in 4 bits,
+// 1.5 in bf16); of a step of 256 columns in 4 bits a quarter is not hidden behind them (operands from LDS and loads to it take 2.0 us where they take 1.5).
+// 8192 x 14336 x 4096, x in 4 bits, 249 us: 3.9 PFLOP/s; 1000 rows of x in bf16, gated, 28672 x 4096, 190 us: 1.24 PFLOP/s (448 tiles on 256 CUs, 7/8 of two
+// rounds); 37 rows in bf16, 4096 x 14336, the columns in 14 parts, 17 us and 4 to join them; 16384 places of 32 experts, 4096 x 4096, gated, 4 bits, 205 .. 240 us,
+// 4096 x 2048 120 .. 140 (2.7 .. 2.0 PFLOP/s: rows by lists, tiles that an expert's rows do not fill).
 // LDS: the pieces of a row are permuted (xor) by bits of the row's number, so that 16 rows of one piece lie in different banks.
 #include <algorithm>
 
@@ -216,7 +221,7 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     constexpr int BEHIND = (XD - 2) * XL + (WD - 2) * WL + EARLY;  // loads behind those of the first step
 
     // The loop's instructions stay in the order of the source: one wave to a SIMD, so what is issued between two matrix instructions has to fit
-    // the time of one of them.  Left to itself the compiler reads operands just before their use (8192 x 14336 x 4096 in 4 bits: 426 us instead of 346).
+    // the time of one of them.  Left to itself the compiler reads operands just before their use, and the loop takes a quarter longer.
     constexpr int TILES = MT * NT;
     u32x4 xa[2][MT], wa[2][NT];                                    // x in bf16: wa[0] has the codes of a step
     uint32_t xb[MT], wb[NT], ahead[MT + NT];                       // scales of a step, of the next
@@ -402,7 +407,8 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
 }
 
 // The parts' sums, added in the order of the columns (four waves a quarter each, then the quarters), and what the kernel above does with a sum.  Bound by the
-// latency of sums that other dies have just written: 8 of them at a time; one after the other 56 parts of 60 x 250 outputs took 14 us, by one wave 10.
+// latency of sums that other dies have just written: 8 of them at a time; one after the other 56 parts of 60 x 250 outputs took 14 us, by one wave 10.  14 parts
+// of 37 x 4096: 3.9 us.
 struct MxJoin {
     const float *part;
     void *y;

@@ -372,6 +372,8 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
 //   softmax, renormalised d_x[i] = s[i] (d[i] - sum_c d s), s = p / sum_c p = e^x / sum_c e^x;   0 elsewhere
 //   sigmoid               d_x[i] = d[i] p[i] (1 - p[i])
 //   sigmoid, renormalised d_x[i] = s[i] (d[i] - sum_c d s) (1 - p[i])
+// A wave a token; a chosen expert's value reaches its lane by top_k comparisons (no atomics, no order).  16384 x 128 in bf16, top 8: 9.0 us, 12.6 MB, 1.4 TB/s:
+// bound by issue, some 200 instructions a token.
 struct RouteBackArgs {
     const void *logits;
     const int32_t *ids;
@@ -456,10 +458,10 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
 
 // ---- lists by expert ---------------------------------------------------------------
 // sorted: the places (token * top_k + j) of all choices, expert after expert, ascending inside one; token_of: their tokens; tiles: pieces of at most
-// tile_rows of an expert's list, expert after expert, then entries with count 0 up to max_tiles, then one whose count is that of the pieces.  A workgroup an expert.  Its waves take consecutive runs
-// of the choices; a wave's first pass counts those of its own expert (by ballots), and of all experts (in LDS, whole numbers: any order
+// tile_rows of an expert's list, expert after expert, then entries with count 0 up to max_tiles, then one whose count is that of the pieces.
+// A workgroup an expert.  Its waves take consecutive runs of the choices; a wave's first pass counts those of its own expert (by ballots), and of all experts (in LDS, whole numbers: any order
 // gives the same), so the workgroup knows where its list and its tiles begin, a wave where its part does.
-// Bound by the latency of the two passes over the ids, which come from L2: 16384 choices of 32 experts, one id a lane and 256 threads: 42 us.
+// Bound by the latency of the two passes over the ids, which come from L2: 16384 choices of 32 experts 9 .. 11 us; with one id a lane and 256 threads 42.
 constexpr int LIST_WAVES = 16, LIST_STEP = 8;                  // ids of a lane and step
 __global__ __launch_bounds__(64 * LIST_WAVES) void expert_lists_kernel(const int32_t *ids, int n, int experts, int top_k, int tile_rows, int max_tiles,
                                                                       int *sorted, int *token_of, MxTile *tiles)
@@ -603,7 +605,8 @@ struct CombineArgs {
     int64_t ld_y, ld_out;
     int top_k, hidden;
 };
-// Memory bounds it; 8 rows are asked for at a time (one after the other 16 tokens of 2048 columns, 8 rows each, took 5.7 us).
+// Memory bounds it: 4096 tokens of 4096 columns, 4 rows each, 28 us, 6.0 TB/s.  8 rows are asked for at a time: 16 tokens of 2048 columns, 8 rows each, 3.9 us, one
+// after the other 5.7.
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a)
 {
     const int64_t token = blockIdx.x;
