@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
 
     // Tiles in an order for the 8 dies: workgroups go to them in turn, and each gets a run of neighbours, 8 tiles of W by as many of x as
     // follow (what the 32 CUs of a die work on at a time then comes from 8 + 4 tiles).  A workgroup takes every gridDim.x-th.
-    const int n_tiles = g.tiles ? g.tiles[g.n_tiles].count : g.n_tiles;                    // (of a list, as many as there are)
+    const int n_tiles = g.tiles ? __builtin_amdgcn_readfirstlane(g.tiles[g.n_tiles].count) : g.n_tiles;          // (of a list, as many as there are)
     const int wtiles = (g.outs + OUTS - 1) / OUTS, all = wtiles * n_tiles;
     const int chunk0 = (int)blockIdx.y * g.chunks;                 // the part of the columns
     const int cols = g.n_split == 1 || g.cols - chunk0 * CHUNK < g.chunks * CHUNK ? g.cols - chunk0 * CHUNK : g.chunks * CHUNK;
@@ -97,7 +97,10 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
         const int xt = in_band / wide;
         out0 = (8 * band + (in_band - xt * wide)) * OUTS;
         t = {0, xt * XROWS, 0, 0};
-        if (g.tiles) t = g.tiles[xt];
+        if (g.tiles) {
+            const MxTile l = g.tiles[xt];                          // (the same for all lanes, which the compiler is not always able to see)
+            t = {__builtin_amdgcn_readfirstlane(l.expert), __builtin_amdgcn_readfirstlane(l.first), __builtin_amdgcn_readfirstlane(l.count), 0};
+        }
         else t.count = (int)(g.batch - t.first < XROWS ? g.batch - t.first : XROWS);
         const int64_t x_first = g.x_row ? 0 : t.first, w_first = (int64_t)t.expert * g.w_rows;
         xp = static_cast<const uint8_t *>(g.x) + x_first * g.ld_x + (int64_t)chunk0 * (X4 ? ROW : 2 * CHUNK) - LAST;

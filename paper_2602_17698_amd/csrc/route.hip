@@ -12,8 +12,8 @@ namespace sbits {
 // Which experts are taken is decided as with scores in 64 bits, but scores are computed in fp32 first, with a bound on how far each
 // may be off.  Where the bounds leave only the order of the chosen ones open, these are computed in 64 bits and put in order (a token in some hundred with
 // sigmoid scores and a bias); only where they leave the choice open (one in a thousand) all are.  In 64 bits for every token 16384 x 256 took 52 us.
-// 16384 tokens of 256 experts, 8 groups, a bias, the best 8: 21 us, 0.8 TB/s.  Instruction issue bounds it: a wave has some 450 of 4 cycles for a token, half of them
-// in the top_k searches of the largest key.  Without groups, bias and sigmoid 15 us; 2048 tokens 7.
+// 16384 tokens of 256 experts, 8 groups, a bias, the best 8: 21 us, 0.8 TB/s.  Instruction issue bounds it: 640 vector instructions of 4 cycles a token, a
+// third of them in the top_k searches of the largest key.  Without groups, bias and sigmoid 15 us; 2048 tokens 7.
 struct RouteArgs {
     const void *logits;
     const float *bias;
