@@ -155,8 +155,9 @@ using namespace sbits;
 // Estimates in microseconds, from products of 4096 x 4096, 14336 x 4096 and 4096 x 14336 with 17 .. 512 rows of x, each with tiles of 16, 64, 128 and 256 rows.
 // Tiles of 64 and more: 8 for a launch, its first loads and stores; then for every 256 columns, while all CUs have a tile, what CHUNK_US says.
 // Parts of the columns cost a second kernel, 5, and their sums are written and read at 5 TB/s.
-// Tiles of 16 rows: 4, and W is read again for each, at 3 TB/s; with more than 2048 columns, where a CU has one workgroup at a time, at least 1.0, 1.4, 2.2 ns a
-// column for each time that all CUs get one with 1, 2, 4 tiles of W.
+// Tiles of 16 rows: 4, and W is read again for each, at 3 TB/s; with more than 2048 columns at least 1.0, 1.4, 2.2 ns a
+// column for each time that all CUs get a workgroup with 1, 2, 4 tiles of W (of 8 waves; those of 4 take up to a third less, but with 17 rows of x and more
+// the tiles of 64 were then as fast: 10240 x 4096, 20 rows, 18.0 us and 20.2 by workgroups of 4 waves).
 static const double CHUNK_US[2][3] = {{2.1, 3.2, 6.1}, {0.9, 1.4, 2.2}};       // [x in 4 bits][64, 128, 256 rows]
 static double many_us(const sbits_ctx *ctx, bool x4, int size, double tiles, int64_t w_rows, int chunks)
 {
@@ -170,12 +171,19 @@ static int few_tiles(const sbits_ctx *ctx, double rows)            // rows of W,
     const double enough = sbits_cus(ctx) * 0.75;
     return rows >= 64 * enough ? 4 : rows >= 32 * enough ? 2 : 1;
 }
+// Waves to its workgroup: 8, with 4 runs to a group, for rows of more than 2048 columns where all workgroups are at work at a time, else 4, with 2: of those a
+// CU has three, one of which starts or ends while the others read.  us by 8 and by 4, one row of x in bf16: 14336 x 4096 10.6, 12.5; 20480 x 4096 18.9, 18.7;
+// 57344 x 4096 39.2, 33.3; 57344 x 8192 82, 61; 110 products of 2048 x 2048 with a row or two each 37.0, 28.7.
+static int few_waves(const sbits_ctx *ctx, double rows, int64_t cols)
+{
+    return cols <= 2048 || rows > 16.0 * few_tiles(ctx, rows) * sbits_cus(ctx) ? 4 : 8;
+}
 static double few_us(const sbits_ctx *ctx, double tiles, int64_t w_rows, int64_t cols)
 {
-    const double read = tiles * (double)w_rows * (double)cols * (17.0 / 32.0) / 3e6;
+    const double rows = tiles * (double)w_rows, read = rows * (double)cols * (17.0 / 32.0) / 3e6;
     if (cols <= 2048) return 4.0 + read;
-    const int t = few_tiles(ctx, (double)w_rows * tiles);
-    const double rounds = std::ceil((double)((w_rows + 16 * t - 1) / (16 * t)) * tiles / sbits_cus(ctx));
+    const int t = few_tiles(ctx, rows);
+    const double rounds = std::ceil(std::ceil((double)w_rows / (16 * t)) * tiles / sbits_cus(ctx));
     return 4.0 + std::max(read, rounds * (double)cols * (t == 4 ? 2.2e-3 : t == 2 ? 1.4e-3 : 1.0e-3));
 }
 
@@ -222,14 +230,12 @@ int sbits_mx_cut_layer(const sbits_ctx *ctx, bool x4, bool near, int experts, in
     return best_rows;
 }
 
-// Rows of up to 2048 columns by 4 waves with 2 runs to a group, wider ones by 8 with 4: 110 products of 2048 x 2048 with a row or two of x each 28.7 and
-// 37.0 us, one of 14336 x 4096 12.4 and 10.2.
 template <bool X4, bool GATED>
 static auto few_instance(const sbits_ctx *ctx, const MxGemm &g, int tiles, int &outs, int &waves)
 {
-    const bool narrow = g.cols <= 2048;
     const int t = few_tiles(ctx, (double)g.w_rows * tiles);
-    waves = narrow ? 4 : 8;
+    waves = few_waves(ctx, (double)g.w_rows * tiles, g.cols);
+    const bool narrow = waves == 4;
     outs = (GATED ? 8 : 16) * (GATED && t == 1 ? 2 : t);
     if (t == 4) return narrow ? mx_gemm_few_kernel<X4, GATED, 4, 4, 2> : mx_gemm_few_kernel<X4, GATED, 8, 4, 4>;
     if constexpr (!GATED)

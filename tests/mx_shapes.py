@@ -3,7 +3,7 @@
 # few rows, or small matrices: outputs that end inside a tile, runs of columns that end inside one
 SHAPES = [(1, 8, 32), (1, 250, 256), (2, 33, 96), (15, 64, 128), (16, 31, 160), (17, 100, 512), (31, 257, 288), (33, 64, 1056), (48, 130, 544), (64, 96, 2080),
           (65, 250, 320), (97, 256, 576), (128, 514, 256), (129, 300, 352), (200, 129, 1120), (255, 513, 64), (256, 256, 32), (257, 258, 608), (300, 700, 800),
-          (16, 4100, 4128), (1, 16500, 2176), (9, 20000, 544), (5, 8200, 2080)]
+          (16, 4100, 4128), (1, 16500, 2176), (2, 14000, 2176), (9, 20000, 544), (5, 8200, 2080), (3, 8000, 2208)]
 
 # (batch, rows, cols, rows of x to a tile, whether the columns are in parts: with x in bf16, in 4 bits)
 LARGE = [(700, 2050, 800, 64, (False, False)), (2100, 514, 2336, 64, (True, False)), (60, 250, 14336, 64, (True, True)), (300, 250, 14336, 64, (True, True)),
