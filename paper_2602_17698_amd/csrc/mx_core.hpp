@@ -62,16 +62,17 @@ __device__ __forceinline__ u32x4 mx_values8(uint32_t codes, float scale)
 }
 
 // g / (1 + e^-g) * u.  e^-g as 2^t with t = -g log2(e), what t's rounding took away put back (t has an error of 2^-24 |t|, which is one of
-// e^-g's); the hardware's power of two and reciprocal are off by a unit in the last place at most.  Half the instructions of expf and a quotient,
-// which were 9 us of a tile of 256 x 128 outputs.
+// e^-g's); the hardware's power of two and reciprocal are off by a unit in the last place at most.  From |t| = 128 on the power is 0 or infinite, and what
+// is to be put back may be NaN.  The reciprocal is that of a quarter of 1 + e^-g, as one of numbers above 2^126 would be 0.  Half the instructions of expf and
+// a quotient, which were 9 us of a tile of 256 x 128 outputs.
 __device__ __forceinline__ float silu_mul(float g, float u)
 {
     constexpr float LOG2E = 0x1.715476p+0f, LOG2E_REST = 0x1.4ae0cp-26f, LN2 = 0x1.62e43p-1f;
     const float t = -g * LOG2E;
     const float rest = fmaf(-g, LOG2E_REST, fmaf(-g, LOG2E, -t));
     float e = __builtin_amdgcn_exp2f(t);
-    e = t > 120.0f ? e : fmaf(e, rest * LN2, e);               // (above, e may be infinite; the quotient is 0 or next to it)
-    return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
+    e = fabsf(t) < 128.0f ? fmaf(e, rest * LN2, e) : e;
+    return 0.25f * g * __builtin_amdgcn_rcpf(fmaf(e, 0.25f, 0.25f)) * u;
 }
 
 // One set of rows of x against one matrix of a stack: rows first .. first + count - 1 of the sorted list, matrix `expert`.
