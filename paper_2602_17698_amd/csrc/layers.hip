@@ -42,7 +42,8 @@ static int need_device(sbits_ctx *ctx)
     return SBITS_OK;
 }
 
-static bool near_2gb(int64_t bytes) { return bytes < ((int64_t)1 << 31); }
+// whether the product of many rows can address so many bytes
+static bool near_2gb(int64_t bytes) { return bytes <= MX_REACH - MX_LEAD; }
 
 // the workspace of a layer of experts, as offsets
 struct LayerSpace {

@@ -9,6 +9,8 @@ namespace sbits {
 constexpr int MX_BLOCK = 32;                 // values that share a power of two
 constexpr int MAX_EXPERTS = 512, MAX_TOP_K = 32, MAX_GROUPS = 64;
 constexpr int64_t MX_MAX_COLS = 1 << 24;     // a row's bytes and a tile's stay within 32-bit offsets
+constexpr int MX_LEAD = 3 * 1024;            // bytes that the buffers of the product of many rows begin ahead of what they are for
+constexpr int MX_REACH = 0x7fffffff;         // and their length: MX_LEAD and what is read have to fit
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -106,7 +108,7 @@ struct MxGemm {
 
 // ---- launchers --------------------------------------------------------------
 int sbits_launch_mx_quantize(sbits_ctx *ctx, const void *x, bool bf16, int64_t ld_x, const sbits_mx &q, int64_t rows, void *values, int64_t ld_v);
-// how a product is cut up: tile_rows, n_split, chunks and ld_part from w_rows, cols and batch; near: offsets in its matrices are below 2^31
+// how a product is cut up: tile_rows, n_split, chunks and ld_part from w_rows, cols and batch; near: what a tile reads ends within MX_REACH - MX_LEAD bytes of its buffers' begin
 void sbits_mx_cut(const sbits_ctx *ctx, bool x4, bool near, sbits::MxGemm &g);
 // tile_rows of both products of a layer of experts with so many choices
 int sbits_mx_cut_layer(const sbits_ctx *ctx, bool x4, bool near, int experts, int64_t places, int64_t hidden, int64_t inner);

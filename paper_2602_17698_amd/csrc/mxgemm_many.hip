@@ -80,14 +80,15 @@ __global__ __launch_bounds__(256, 1) void mx_gemm_many_kernel(MxGemm g)
     // Where a lane's loads come from: offsets into buffers that begin at the tile's first row of x (with a list of rows: at the first of
     // all) and at the matrix.  Rows and columns that are not there: NOWHERE.  Four loads share an address in LDS and have offsets 0 .. LAST, which count for
     // the memory's address, too: buffers begin LAST bytes ahead, and the offsets here take the load's own away.
-    // (32 bits: the caller sees to it that what a tile spans is below 2^31)
-    constexpr int LAST = 3 * 1024;
+    // (32 bits: the caller sees to it that what a tile spans, and LAST, are within a buffer's length)
+    constexpr int LAST = MX_LEAD;
+    static_assert(LAST == 3 * 1024, "the largest of four loads' offsets");
     const uint32_t ld_x = (uint32_t)g.ld_x, ld_w = (uint32_t)g.ld_w, ld_xs = (uint32_t)g.ld_xs, ld_ws = (uint32_t)g.ld_ws;
     MxTile t;
     int out0;
     const uint8_t *xp, *wp, *scales_w, *scales_x;
     uint32_t x_at[XL], w_at[WL], s_at[SL];
-    auto buffer = [](const uint8_t *from) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(from), 0, 0x7fffffff, 0x00027000); };
+    auto buffer = [](const uint8_t *from) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(from), 0, MX_REACH, 0x00027000); };
     auto s_slot = [&](int i) { return (wave + 4 * i) * 32 + lane / 2; };
     auto set_up = [&](int number) {
         const int die = number & 7, each = all >> 3, more = all & 7;
