@@ -467,7 +467,9 @@ int  sbits_mx_gemm(sbits_ctx *ctx, const sbits_mx *w, const void *x_bf16, int64_
  * scores, descending, ties to the lower index, groups too; weights: their p, divided by
  * their sum if `renormalize`.  Logits that are not finite are experts that are not there
  * (p = 0, never chosen), and an expert with a bias that is not finite is never chosen; where
- * none is left the id is -1 and the weight 0.  Scores that decide are computed in 64 bits.  */
+ * none is left the id is -1 and the weight 0.  Scores that decide are computed in 64 bits.
+ * Shares do not lose small p (they sum to 1 wherever an expert is left); a weight below
+ * 2^-126 may be 0.                                                                        */
 #define SBITS_ROUTE_SOFTMAX 0
 #define SBITS_ROUTE_SIGMOID 1
 #define SBITS_ROUTE_GROUP_TOP2 0

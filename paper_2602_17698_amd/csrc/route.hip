@@ -349,9 +349,21 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
         my_id = __builtin_amdgcn_ds_permute(4 * (base + place), my_id);
         my_p = p_new;
     }
-    const float total = a.renormalize ? over_lanes<LOG>(my_p, Add{}) : 1.0f;
+    if (a.renormalize) {
+        const float total = over_lanes<LOG>(my_p, Add{});
+        // p below 2^-126 are 0 by now, and small ones have a rounded argument: shares with one below 2^-60 come from the logits, in 64 bits, with the largest
+        // p's power of e taken out (p = e^min(x, 0) / (1 + e^-|x|))
+        const bool low = ballot(my_id >= 0 && my_p < 0x1p-60f) != 0;
+        my_p = total > 0.0f ? my_p / total : 0.0f;
+        if (__ballot(low) != 0) {
+            const double v = my_id >= 0 ? (double)logit_at<BF16>(a.logits, row + my_id) : -HUGE_VAL, largest = over_lanes<LOG>(v, Largest{});
+            double q = 0.0;
+            if (my_id >= 0) q = a.sigmoid ? exp(fmin(v, 0.0) - fmin(largest, 0.0)) / (1.0 + exp(-fabs(v))) : exp(v - largest);
+            const double all = over_lanes<LOG>(q, Add{});
+            if (low) my_p = (float)(q / all);
+        }
+    }
     if (lane < a.top_k) {
-        if (a.renormalize) my_p = total > 0.0f ? my_p / total : 0.0f;
         a.ids[token * a.top_k + lane] = my_id;
         a.weights[token * a.top_k + lane] = my_p;
     }

@@ -1,0 +1,123 @@
+"""Routing where probabilities are beyond what 32 bits hold: shares of small ones, their gradient, against 64 bits."""
+import math
+
+import pytest
+import torch
+
+import mx_plain as mp
+from paper_2602_17698_amd import binding as sb
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = sb.Context(0, torch.cuda.current_stream().cuda_stream)
+    yield c
+    c.close()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def low_logits(tokens, experts, kind, seed):
+    """Tokens whose logits are all, or but for some, far below 0 or far apart."""
+    g = gen(seed)
+    x = 1.5 * torch.randn(tokens, experts, generator=g)
+    level = torch.tensor([0.0, -60.0, -84.0, -87.0, -90.0, -100.0, -104.0, -200.0, -3000.0, -1e30])
+    x += level[torch.arange(tokens) % 10][:, None]
+    x[torch.arange(tokens) % 3 == 1] *= 1 + 12 * torch.rand(experts, generator=g)      # far apart
+    if experts > 4:
+        x[::7, 2] = 4.0                                                                 # one far above the rest
+        x[5::9, 1] = -math.inf
+    x = x.to(kind)
+    return torch.where(torch.isfinite(x) | (x == -math.inf), x, torch.finfo(kind).min)
+
+
+def exact_weights(r, logits, ids):
+    """The weights of these choices in 64 bits; shares without the probabilities, which may be below what 64 bits hold."""
+    x, some = logits.double().gather(1, ids.clamp(min=0).long()), ids >= 0
+    x = torch.where(some, x, -math.inf)
+    if r.scoring == 0:
+        fine = torch.where(torch.isfinite(logits.double()), logits.double(), -math.inf)
+        top = fine.amax(-1, keepdim=True)                                        # (taken away first: beside -1e30 the sum's logarithm is nothing)
+        log_p = x - top - torch.log(torch.exp(fine - top).sum(-1, keepdim=True))
+    else:
+        log_p = torch.where(some, -torch.nn.functional.softplus(-x.clamp(min=-700)) + (x - x.clamp(min=-700)), -math.inf)
+    if r.renormalize:
+        top = log_p.amax(-1, keepdim=True)
+        log_p = log_p - torch.where(top > -math.inf, top, 0.0)
+        e = torch.exp(log_p)
+        return torch.where(some, e / e.sum(-1, keepdim=True).clamp(min=1e-300), 0.0)
+    return torch.where(some, torch.exp(log_p), 0.0)
+
+
+def check_weights(r, logits, ids, weights):
+    want = exact_weights(r, logits, ids)
+    # as in the tests of routing: 64 roundings; arguments (differences of logits) are rounded, 2^-24 of up to 88 in weight and sum each: 176 more.  Below the least normal
+    # number a weight may be 0
+    assert bool(((weights.double() - want).abs() <= 240 * 2.0 ** -24 * want + 2.0 ** -126).all()), float((weights.double() - want).abs().max())
+    if r.renormalize:
+        some = (ids >= 0).any(-1)
+        assert bool(((weights.double().sum(-1) - 1).abs()[some] <= 64 * 2.0 ** -24).all())
+
+
+ROUTERS = [dict(experts=8, top_k=2), dict(experts=24, top_k=4, groups=8, top_groups=4), dict(experts=64, top_k=8), dict(experts=128, top_k=32),
+           dict(experts=256, top_k=8, groups=8, top_groups=4), dict(experts=300, top_k=7)]
+
+
+@pytest.mark.parametrize("router", ROUTERS, ids=lambda r: "-".join("%s%d" % i for i in r.items()))
+@pytest.mark.parametrize("scoring", [0, 1])
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens", [1, 61, 4301])
+def test_weights_of_low_logits(ctx, router, scoring, renormalize, kind, tokens):
+    """Without a bias: sigmoids of logits that are all far below 0; groups that leave only experts far below the best."""
+    r = sb.Router(scoring=scoring, renormalize=renormalize, **router)
+    logits = low_logits(tokens + 4, r.experts, kind, tokens)[4:]                 # (a single token: the one of -90)
+    ids, weights = torch.empty(tokens, r.top_k, dtype=torch.int32, device="cuda"), torch.empty(tokens, r.top_k, device="cuda")
+    ctx.route(r, logits.cuda(), None, ids, weights)
+    if r.groups == 1:                                                            # (groups of which all probabilities are 0 in 64 bits are a matter of the index)
+        some = min(tokens, 61)
+        assert torch.equal(ids[:some].cpu(), mp.route(r, logits[:some], None)[0])
+    check_weights(r, logits, ids.cpu(), weights.cpu())
+
+
+@pytest.mark.parametrize("router", ROUTERS, ids=lambda r: "-".join("%s%d" % i for i in r.items()))
+@pytest.mark.parametrize("scoring", [0, 1])
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("tokens", [1, 61, 4301])
+def test_weights_of_experts_that_a_bias_prefers(ctx, router, scoring, renormalize, tokens):
+    """A bias for the experts with the lowest logits, 30 to 200 below the best."""
+    r, g = sb.Router(scoring=scoring, renormalize=renormalize, **router), gen(tokens + 1)
+    logits = torch.randn(tokens, r.experts, generator=g)
+    low = torch.arange(r.experts) % 2 == 0
+    logits[:, low] -= torch.tensor([30.0, 80.0, 87.0, 100.0, 200.0])[torch.arange(tokens) % 5 - 2][:, None]
+    bias = torch.where(low, 2.0, 0.0) + 0.01 * torch.randn(r.experts, generator=g)
+    ids, weights = torch.empty(tokens, r.top_k, dtype=torch.int32, device="cuda"), torch.empty(tokens, r.top_k, device="cuda")
+    ctx.route(r, logits.cuda(), bias.cuda(), ids, weights)
+    some = min(tokens, 61)
+    assert torch.equal(ids[:some].cpu(), mp.route(r, logits[:some], bias)[0])
+    check_weights(r, logits, ids.cpu(), weights.cpu())
+
+
+@pytest.mark.parametrize("scoring", [0, 1])
+@pytest.mark.parametrize("four", [False, True])
+def test_layer_of_tokens_with_low_logits(ctx, scoring, four):
+    """Tokens whose choices are all far below 0 (by a bias, with softmax) are not zeros."""
+    r, tokens, hidden, inner, g = sb.Router(experts=8, top_k=2, scoring=scoring), 5, 64, 32, gen(3)
+    up, down = mp.random_matrix(8 * 2 * inner, hidden, g, 1), mp.random_matrix(8 * hidden, inner, g, 1)
+    logits = torch.randn(tokens, 8, generator=g)
+    logits[:, ::2] -= 95.0
+    bias = torch.where(torch.arange(8) % 2 == 0, 2.0, 0.0)
+    x = (0.05 * torch.randn(tokens, hidden, generator=g)).to(torch.bfloat16)
+    ids, weights = torch.empty(tokens, 2, dtype=torch.int32, device="cuda"), torch.empty(tokens, 2, device="cuda")
+    out = torch.empty(tokens, hidden, dtype=torch.bfloat16, device="cuda")
+    u, d = (sb.mx(*mp.stored(*m, "cuda")) for m in (up, down))
+    ws = torch.empty(ctx.expert_layer_ws_bytes(r, tokens, u, d, four), dtype=torch.uint8, device="cuda")
+    ctx.expert_layer(r, logits.cuda(), bias.cuda(), x.cuda(), u, d, out, ids, weights, ws, four_bit=four)
+    check_weights(r, logits, ids.cpu(), weights.cpu())
+    want_ids, _, want, off = mp.layer(r, logits, bias, x, mp.values(*up).view(8, 2 * inner, hidden), mp.values(*down).view(8, hidden, inner), four)
+    assert torch.equal(ids.cpu(), want_ids)
+    assert bool(((out.cpu().double() - want).abs() <= off).all())
