@@ -415,14 +415,18 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
     top = unordered(over_lanes<6>(ordered(top), Largest{}));
     if (top == -HUGE_VALF) top = 0.0f;
     int id = -1;
-    float d = 0.0f, c = 0.0f;                                  // lane j < top_k: the j-th chosen expert, its e^x or p
+    float d = 0.0f, c = 0.0f, rest = 0.0f;                     // lane j < top_k: the j-th chosen expert, its e^x or p, a sigmoid's 1 - p
     if (lane < a.top_k) {
         id = a.ids[token * a.top_k + lane];
         if (id < 0 || id >= a.experts) id = -1;
         if (id >= 0) {
             d = a.d_weights[token * a.top_k + lane];
             const float v = logit_at<BF16>(a.logits, token * a.ld + id);
-            if (fabsf(v) < HUGE_VALF) c = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + exp_of(-v)) : exp_of(v - top);
+            if (fabsf(v) < HUGE_VALF) {
+                c = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + exp_of(-v)) : exp_of(v - top);
+                // (not 1 - c, in which p's rounding is all that is left of a confident expert's)
+                if (a.sigmoid) rest = __builtin_amdgcn_rcpf(1.0f + exp_of(v));
+            }
         }
     }
     float all = 1.0f;                                          // 1 / sum e^(x - top)
@@ -443,9 +447,9 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
         const float total = wave_sum(c);
         const float s = total > 0.0f ? c / total : 0.0f;
         g = s * (d - wave_sum(d * s));
-        if (a.sigmoid) g *= 1.0f - c;
+        if (a.sigmoid) g *= rest;
     } else if (a.sigmoid) {
-        g = d * c * (1.0f - c);
+        g = d * c * rest;
     } else {
         g = d;
         dot = wave_sum(d * c);

@@ -121,3 +121,54 @@ def test_layer_of_tokens_with_low_logits(ctx, scoring, four):
     want_ids, _, want, off = mp.layer(r, logits, bias, x, mp.values(*up).view(8, 2 * inner, hidden), mp.values(*down).view(8, hidden, inner), four)
     assert torch.equal(ids.cpu(), want_ids)
     assert bool(((out.cpu().double() - want).abs() <= off).all())
+
+
+# ---- the gradient ----------------------------------------------------------------------------------
+def check_gradient(ctx, r, logits, ids, d, roundings=128):
+    """Against the formulas in 64 bits, each with the magnitudes of its terms: s (|d| + sum |d| s), with sigmoids (1 - p) of that, p (1 - p) |d| without shares."""
+    tokens = logits.shape[0]
+    out = torch.empty(tokens, r.experts, device="cuda")
+    ctx.route_backward(r, logits.cuda(), ids.cuda(), d.cuda(), out)
+    some = ids >= 0
+    at = ids.clamp(min=0).long()
+    x = torch.where(some, logits.double().gather(1, at), -math.inf)
+    w, d64 = exact_weights(r, logits, ids), torch.where(some, d.double(), 0.0)
+    rest = torch.sigmoid(-x) if r.scoring == 1 else torch.ones_like(x)                 # 1 - p, of its own accuracy
+    if r.renormalize:
+        g = w * rest * (d64 - (d64 * w).sum(-1, keepdim=True))
+        size = w * rest * (d64.abs() + (d64.abs() * w).sum(-1, keepdim=True))
+    else:
+        assert r.scoring == 1
+        g = size = w * rest * d64
+    want, sizes = (torch.zeros(tokens, r.experts, dtype=torch.float64).scatter_add_(1, at, torch.where(some, v, 0.0)) for v in (g, size.abs()))
+    # below the least normal number a share, p or 1 - p may be 0
+    off = roundings * 2.0 ** -24 * sizes + 2.0 ** -126 * (1 + d64.abs().amax())
+    got = out.cpu().double()
+    assert bool(((got - want).abs() <= off).all()), float(((got - want).abs() / off).max())
+
+
+@pytest.mark.parametrize("renormalize", [False, True])
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("experts,top_k,tokens", [(8, 2, 1), (8, 2, 37), (100, 8, 37), (300, 6, 37)])
+def test_gradient_of_confident_sigmoids(ctx, renormalize, kind, experts, top_k, tokens):
+    """Logits of 3 to 60: the gradient has the factor 1 - p, down to e^-60, as accurate as the rest of it."""
+    r, g = sb.Router(experts=experts, top_k=top_k, scoring=1, renormalize=renormalize), gen(tokens)
+    logits = (3.0 + 57.0 * torch.rand(tokens, experts, generator=g) ** 2).to(kind)
+    ids = torch.stack([torch.randperm(experts, generator=g)[:top_k] for _ in range(tokens)]).int()
+    check_gradient(ctx, r, logits, ids, torch.randn(tokens, top_k, generator=g))
+
+
+@pytest.mark.parametrize("scoring", [0, 1])
+@pytest.mark.parametrize("renormalize", [False, True])
+def test_gradient_of_choices_whose_logits_are_not_there(ctx, scoring, renormalize):
+    """Ids of experts with NaN or infinite logits: their gradient is 0, the others' as if they had not been chosen."""
+    r, g = sb.Router(experts=16, top_k=4, scoring=scoring, renormalize=renormalize), gen(2)
+    logits, d = torch.randn(4, 16, generator=g), torch.randn(4, 4, generator=g)
+    logits[0, 3], logits[1, 3], logits[2, 3] = math.nan, math.inf, -math.inf
+    ids = torch.tensor([[1, 3, 5, 7]] * 4, dtype=torch.int32)
+    without = ids.clone()
+    without[:3, 1] = -1
+    out = [torch.empty(4, 16, device="cuda") for _ in range(2)]
+    for i, o in zip((ids, without), out):
+        ctx.route_backward(r, logits.cuda(), i.cuda(), d.cuda(), o)
+    assert bool(torch.isfinite(out[0]).all()) and bool((out[0][:3, 3] == 0).all()) and torch.equal(*out)
