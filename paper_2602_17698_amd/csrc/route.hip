@@ -404,30 +404,37 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteBackArgs a)
     const int64_t token = (int64_t)blockIdx.x * 4 + wave;
     if (token >= a.tokens) return;
     float x[PER];
-    float top = -HUGE_VALF;
+    float most = -HUGE_VALF;
 #pragma unroll
     for (int r = 0; r < PER; ++r) {
         const int e = r * 64 + lane;
         x[r] = e < a.experts ? logit_at<BF16>(a.logits, token * a.ld + e) : -HUGE_VALF;
         x[r] = fabsf(x[r]) < HUGE_VALF ? x[r] : -HUGE_VALF;
-        top = fmaxf(top, x[r]);
+        most = fmaxf(most, x[r]);
     }
-    top = unordered(over_lanes<6>(ordered(top), Largest{}));
-    if (top == -HUGE_VALF) top = 0.0f;
     int id = -1;
-    float d = 0.0f, c = 0.0f, rest = 0.0f;                     // lane j < top_k: the j-th chosen expert, its e^x or p, a sigmoid's 1 - p
+    float v = -HUGE_VALF, d = 0.0f;                            // lane j < top_k: the j-th chosen expert, its logit
     if (lane < a.top_k) {
         id = a.ids[token * a.top_k + lane];
         if (id < 0 || id >= a.experts) id = -1;
         if (id >= 0) {
             d = a.d_weights[token * a.top_k + lane];
-            const float v = logit_at<BF16>(a.logits, token * a.ld + id);
-            if (fabsf(v) < HUGE_VALF) {
-                c = a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + exp_of(-v)) : exp_of(v - top);
-                // (not 1 - c, in which p's rounding is all that is left of a confident expert's)
-                if (a.sigmoid) rest = __builtin_amdgcn_rcpf(1.0f + exp_of(v));
-            }
+            v = logit_at<BF16>(a.logits, token * a.ld + id);
+            v = fabsf(v) < HUGE_VALF ? v : -HUGE_VALF;
         }
+    }
+    // the largest logit, of the chosen experts where only these count: shares of small p do not vanish
+    float top = unordered(over_lanes<6>(ordered(a.renormalize ? v : most), Largest{}));
+    if (top == -HUGE_VALF) top = 0.0f;
+    // c: e^(x - top); of sigmoids p, for shares with the largest p's power of e taken out (p = e^min(x, 0) / (1 + e^-|x|)); rest: 1 - p (not 1 - c, in
+    // which p's rounding is all that is left of a confident expert's)
+    float c, rest = 0.0f;
+    if (a.sigmoid) {
+        const float least = a.renormalize ? fminf(top, 0.0f) : 0.0f;
+        c = exp_of(fminf(v, 0.0f) - least) * __builtin_amdgcn_rcpf(1.0f + exp_of(-fabsf(v)));
+        rest = __builtin_amdgcn_rcpf(1.0f + exp_of(v));
+    } else {
+        c = exp_of(v - top);
     }
     float all = 1.0f;                                          // 1 / sum e^(x - top)
     float e[PER];

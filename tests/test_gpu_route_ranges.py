@@ -172,3 +172,18 @@ def test_gradient_of_choices_whose_logits_are_not_there(ctx, scoring, renormaliz
     for i, o in zip((ids, without), out):
         ctx.route_backward(r, logits.cuda(), i.cuda(), d.cuda(), o)
     assert bool(torch.isfinite(out[0]).all()) and bool((out[0][:3, 3] == 0).all()) and torch.equal(*out)
+
+
+@pytest.mark.parametrize("router", ROUTERS, ids=lambda r: "-".join("%s%d" % i for i in r.items()))
+@pytest.mark.parametrize("scoring", [0, 1])
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tokens", [1, 61])
+def test_gradient_of_low_shares(ctx, router, scoring, kind, tokens):
+    """Shares among choices that are all far below 0, or below the best: as large as any."""
+    r, g = sb.Router(scoring=scoring, **router), gen(tokens + 2)
+    logits = low_logits(tokens + 4, r.experts, kind, tokens)[4:]
+    ids = mp.route(r, logits, torch.where(torch.arange(r.experts) % 2 == 0, 2.0, 0.0))[0]      # the best, and those that a bias prefers
+    if tokens > 8:
+        ids[7, -1] = -1
+    # (arguments are rounded as in check_weights, of a share and of those it is compared with)
+    check_gradient(ctx, r, logits, ids, torch.randn(tokens, r.top_k, generator=g), 2 * 240)
