@@ -75,12 +75,12 @@ __device__ __forceinline__ int ordered(float v)
 }
 __device__ __forceinline__ float unordered(int o) { return __int_as_float(o ^ ((o >> 31) & 0x7fffffff)); }
 
-// e^v, off by 2 units in the last place at most (see silu_mul) for |v| < 83, by 2^-17 below, 0 at -infinity
+// e^v, off by 2 units in the last place at most (see silu_mul); 0 below 2^-126
 __device__ __forceinline__ float exp_of(float v)
 {
     constexpr float LOG2E = 0x1.715476p+0f, LOG2E_REST = 0x1.4ae0cp-26f, LN2 = 0x1.62e43p-1f;
     const float t = v * LOG2E, rest = fmaf(v, LOG2E_REST, fmaf(v, LOG2E, -t)), e = __builtin_amdgcn_exp2f(t);
-    return fabsf(t) < 120.0f ? fmaf(e, rest * LN2, e) : e;
+    return fabsf(t) < 128.0f ? fmaf(e, rest * LN2, e) : e;
 }
 
 // The choice in 64 bits: lane j < top_k gets the j-th expert, or -1, and its p.
@@ -214,9 +214,10 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
         one_by = __builtin_amdgcn_rcpf(fmaxf(over_lanes<LOG>(sum, Add{}), 1e-30f));
     }
     auto chance = [&](float v) { return a.sigmoid ? __builtin_amdgcn_rcpf(1.0f + exp_of(-v)) : exp_of(v - top) * one_by; };
-    // Scores p + b, each off by less than by_p * p + 2^-22 |p + b|.  by_p: of a sigmoid 2^-21 (exp and reciprocal 4 units in the last place), of softmax
-    // 2^-18 (also an argument x - top that was rounded, 2^-24 |x - top|: p is below e^-|x - top|, and 16 p (1 + log 1 / p) 2^-24 is the same bound
-    // for all but p < e^-60; a sum of PER + 6 additions).
+    // Scores p + b, each off by less than by_p p + 2^-22 |p + b| + 2^-125 (p below 2^-126 are 0).  by_p: of a sigmoid 2^-21 (exp and reciprocal 4 units in the
+    // last place, a sum).  Of softmax, with D = top - x: the argument's rounding 2^-24 D, exp, PER + 6 additions, the other terms' errors (of the sum 9 2^-24),
+    // reciprocal, product: (D + 38) 2^-24, below 2^-18 for D < 26, which holds from p = 2^-36 on, and below 2^-17 for all.  p is below one_by e^-D, so
+    // 2^-18 one_by bounds the error of any p.
     const float by_p = a.sigmoid ? 0x1p-21f : 0x1p-18f;
     bool open = false;                                          // whether fp32 leaves the choice open
     if (a.bias || a.groups > 1) {
@@ -314,7 +315,8 @@ __device__ __forceinline__ void route_token(const RouteArgs &a, int64_t token, i
     if (a.bias) {                                               // (without a bias keys are the logits themselves)
         // each chosen score against the next, the last against all that are left
         const int n = __popcll(ballot(my_id >= 0));
-        const float v = unordered(my_key), my_off = fmaf(by_p, my_p, 0x1p-22f * fabsf(v));
+        const float v = unordered(my_key), by = a.sigmoid || my_p >= 0x1p-36f ? by_p : 0x1p-17f;
+        const float my_off = fmaf(by, my_p, fmaf(0x1p-22f, fabsf(v), 0x1p-125f));
         const float next = __shfl_down(v + my_off, 1);          // (of all lanes: not behind a condition)
         unordered_ones = lane + 1 < n && v - my_off <= next;
         if (n > 0) {

@@ -187,3 +187,44 @@ def test_gradient_of_low_shares(ctx, router, scoring, kind, tokens):
         ids[7, -1] = -1
     # (arguments are rounded as in check_weights, of a share and of those it is compared with)
     check_gradient(ctx, r, logits, ids, torch.randn(tokens, r.top_k, generator=g), 2 * 240)
+
+
+@pytest.mark.parametrize("router", [dict(experts=32, top_k=4, scoring=1), dict(experts=64, top_k=8, scoring=1), dict(experts=256, top_k=8, scoring=1),
+                                    dict(experts=64, top_k=8), dict(experts=96, top_k=6, groups=4, top_groups=2, scoring=1)],
+                         ids=lambda r: "-".join("%s%d" % i for i in r.items()))
+@pytest.mark.parametrize("level", [-30.0, -60.0, -84.0, -86.0, -87.3, -90.0])
+@pytest.mark.parametrize("bias", [0.0, 1e-37])
+def test_order_of_low_scores(ctx, router, level, bias):
+    """Scores that are small probabilities and little else, of logits a unit or some in the last place apart."""
+    r, tokens = sb.Router(**router), 67
+    g = gen(int(-level))
+    step = 2.0 ** -17 if level < -64 else 2.0 ** -19
+    logits = torch.full((tokens, r.experts), level) + step * torch.randint(-20, 21, (tokens, r.experts), generator=g)
+    logits[:, 0] = 0.0 if r.scoring == 0 else level                              # (softmax: far below the best)
+    b = bias * torch.rand(r.experts, generator=g)
+    b[0] = -1.0
+    ids, weights = torch.empty(tokens, r.top_k, dtype=torch.int32, device="cuda"), torch.empty(tokens, r.top_k, device="cuda")
+    ctx.route(r, logits.cuda(), b.cuda(), ids, weights)
+    assert torch.equal(ids.cpu(), mp.route(r, logits, b)[0])
+    check_weights(r, logits, ids.cpu(), weights.cpu())
+
+
+@pytest.mark.parametrize("router", [dict(experts=64, top_k=8, scoring=1), dict(experts=256, top_k=8, scoring=1), dict(experts=64, top_k=8),
+                                    dict(experts=3, top_k=3, scoring=1), dict(experts=3, top_k=3), dict(experts=6, top_k=2, groups=3, top_groups=1, scoring=1),
+                                    dict(experts=96, top_k=6, groups=4, top_groups=2, scoring=1)], ids=lambda r: "-".join("%s%d" % i for i in r.items()))
+@pytest.mark.parametrize("level", [-5.0, -30.0, -60.0, -83.7, -85.0, -86.3])
+@pytest.mark.parametrize("apart", [0.0, 2.0 ** -21, 2.0 ** -19, 2.0 ** -17])
+def test_order_of_low_scores_that_a_bias_evens_out(ctx, router, level, apart):
+    """p + bias the same for all experts, to some units in the last place of either."""
+    r, g = sb.Router(**router), gen(int(-level))
+    logits = (level + 0.4 * torch.rand(1, r.experts, generator=g)).repeat(401, 1)
+    logits[:, 0] = 0.3 if r.scoring == 0 else level
+    logits[1:] += 2.0 ** (math.frexp(level)[1] - 24) * torch.randint(-1, 2, (400, r.experts), generator=g)
+    p = torch.softmax(logits[0].double(), -1) if r.scoring == 0 else torch.sigmoid(logits[0].double())
+    most = p[1:].max()
+    b = ((2 * most - p) * (1 + apart * torch.randn(r.experts, generator=g).double())).float()
+    b[0] = -1.0
+    ids, weights = torch.empty(401, r.top_k, dtype=torch.int32, device="cuda"), torch.empty(401, r.top_k, device="cuda")
+    ctx.route(r, logits.cuda(), b.cuda(), ids, weights)
+    assert torch.equal(ids.cpu(), mp.route(r, logits, b)[0])
+    check_weights(r, logits, ids.cpu(), weights.cpu())
