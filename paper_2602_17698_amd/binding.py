@@ -198,7 +198,13 @@ def mx_out_pitch(rows: int) -> int:
 
 def mx(codes, scales, cols: int) -> Mx:
     """Descriptor of a matrix in the microscaled form: uint8 tensors of codes [rows, >= cols / 2] and scales [rows, >= pitch]."""
-    d = Mx(codes.data_ptr(), scales.data_ptr(), codes.shape[0], cols, _pitch(codes), _pitch(scales))
+    _is(codes, _UINT8, "codes")
+    _is(scales, _UINT8, "scales")
+    rows, width = codes.shape
+    # (the blocks' bytes are read in fours: rows of scales up to a multiple of 4)
+    if 2 * width < cols or scales.shape[0] != rows or scales.shape[1] < (cols + 127) // 128 * 4:
+        raise ValueError("codes %s and scales %s do not hold %d columns" % (tuple(codes.shape), tuple(scales.shape), cols))
+    d = Mx(codes.data_ptr(), scales.data_ptr(), rows, cols, _pitch(codes), _pitch(scales))
     d.codes_tensor, d.scales_tensor = codes, scales       # (also keeps them alive as long as the descriptor lives)
     return d
 
@@ -212,13 +218,13 @@ def _pitch(t) -> int:
 
 
 _types = {}                     # torch.dtype -> its number here (filled on first use: the search's calls do not import torch)
-_INT32 = 100
+_INT32, _UINT8 = 100, 101
 
 
 def _kind(t) -> int:
     if not _types:
         import torch
-        _types.update({torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16, torch.int32: _INT32})
+        _types.update({torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16, torch.int32: _INT32, torch.uint8: _UINT8})
     return _types.get(t.dtype, -1)
 
 
