@@ -210,11 +210,12 @@ def mx(codes, scales, cols: int) -> Mx:
 
 
 def _pitch(t) -> int:
-    """Elements between the rows of a matrix whose rows are dense."""
+    """Elements between the rows of a matrix whose rows are dense; of a single row its length, up to what every call takes."""
     row, element = t.stride()
-    if element != 1 and t.shape[1] > 1:
+    rows, cols = t.shape
+    if element != 1 and cols > 1:
         raise ValueError("rows of a tensor have to be dense")
-    return row
+    return row if rows != 1 else (cols + 15) // 16 * 16
 
 
 _types = {}                     # torch.dtype -> its number here (filled on first use: the search's calls do not import torch)
