@@ -282,7 +282,7 @@ class Context:
                 raise ValueError("x is not [%d, %d]" % (batch, w.cols))
             bf16, ld, four = x.data_ptr(), _pitch(x), None
         return _check(load().sbits_mx_gemm(self.h, C.addressof(w), bf16, ld, four, batch, 1 if gated else 0, y.data_ptr(), _type(y), _pitch(y),
-                                           ws.data_ptr() if ws is not None else None, ws.numel() if ws is not None else 0),
+                                           ws.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0),
                       "sbits_mx_gemm")
 
     def route(self, router: Router, logits, bias, ids, weights):
@@ -316,7 +316,7 @@ class Context:
                                                 bias.data_ptr() if bias is not None else None, x.data_ptr(), _pitch(x), tokens,
                                                 C.addressof(up), C.addressof(down), out.data_ptr(), _pitch(out), ids.data_ptr(),
                                                 weights.data_ptr(), 1 if four_bit else 0, ws.data_ptr() if ws is not None else None,
-                                                ws.numel() if ws is not None else 0), "sbits_expert_layer")
+                                                ws.nbytes if ws is not None else 0), "sbits_expert_layer")
 
 
 def _routed(router, logits, bias, ids, weights) -> int:
