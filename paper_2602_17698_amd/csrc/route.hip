@@ -1,4 +1,5 @@
 // Routing to experts: the choice with its weights, the gradient, the lists by expert, the weighted sum.
+#include <algorithm>
 #include <type_traits>
 
 #include "mx_core.hpp"
@@ -667,6 +668,8 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a)
 
 using namespace sbits;
 
+constexpr int64_t MOST_TOKENS = 1 << 25;       // of a launch, 64 threads each: a grid has fewer than 2^32 threads along an axis
+
 template <bool BF16>
 static auto route_instance(int per, int log)
 {
@@ -716,8 +719,14 @@ int sbits_launch_route(sbits_ctx *ctx, const sbits_router &r, const void *logits
     }
     auto fn = bf16 ? route_instance<true>(per, log) : route_instance<false>(per, log);
     const int each = 256 >> log;
-    hipLaunchKernelGGL(fn, dim3((unsigned)((tokens + each - 1) / each)), dim3(256), 0, ctx->stream, a);
-    SBITS_HIP(ctx, hipGetLastError());
+    for (int64_t first = 0; first < tokens; first += MOST_TOKENS) {
+        a.tokens = std::min(tokens - first, MOST_TOKENS);
+        a.logits = static_cast<const char *>(logits) + first * ld * (bf16 ? 2 : 4);
+        a.ids = ids + first * r.top_k;
+        a.weights = weights + first * r.top_k;
+        hipLaunchKernelGGL(fn, dim3((unsigned)((a.tokens + each - 1) / each)), dim3(256), 0, ctx->stream, a);
+        SBITS_HIP(ctx, hipGetLastError());
+    }
     return SBITS_OK;
 }
 
@@ -743,11 +752,18 @@ int sbits_launch_route_backward(sbits_ctx *ctx, const sbits_router &r, const voi
                                 const float *d_weights, int64_t tokens, float *d_logits, int64_t ld_d)
 {
     RouteBackArgs a;
-    a.logits = logits; a.ids = ids; a.d_weights = d_weights; a.d_logits = d_logits; a.ld = ld; a.ld_d = ld_d; a.tokens = tokens;
+    a.ld = ld; a.ld_d = ld_d;
     a.experts = r.experts; a.top_k = r.top_k; a.sigmoid = r.scoring == SBITS_ROUTE_SIGMOID; a.renormalize = r.renormalize;
     auto fn = bf16 ? route_backward_instance<true>(r.experts) : route_backward_instance<false>(r.experts);
-    hipLaunchKernelGGL(fn, dim3((unsigned)((tokens + 3) / 4)), dim3(256), 0, ctx->stream, a);
-    SBITS_HIP(ctx, hipGetLastError());
+    for (int64_t first = 0; first < tokens; first += MOST_TOKENS) {
+        a.tokens = std::min(tokens - first, MOST_TOKENS);
+        a.logits = static_cast<const char *>(logits) + first * ld * (bf16 ? 2 : 4);
+        a.ids = ids + first * r.top_k;
+        a.d_weights = d_weights + first * r.top_k;
+        a.d_logits = d_logits + first * ld_d;
+        hipLaunchKernelGGL(fn, dim3((unsigned)((a.tokens + 3) / 4)), dim3(256), 0, ctx->stream, a);
+        SBITS_HIP(ctx, hipGetLastError());
+    }
     return SBITS_OK;
 }
 
@@ -755,9 +771,15 @@ int sbits_launch_combine(sbits_ctx *ctx, const void *y, int64_t ld_y, const int3
                          int hidden, void *out, int64_t ld_out)
 {
     CombineArgs a;
-    a.y = static_cast<const uint16_t *>(y); a.ids = ids; a.weights = weights; a.out = static_cast<uint16_t *>(out);
     a.ld_y = ld_y; a.ld_out = ld_out; a.top_k = top_k; a.hidden = hidden;
-    hipLaunchKernelGGL(combine_kernel, dim3((unsigned)tokens, (unsigned)((hidden + 2047) / 2048)), dim3(256), 0, ctx->stream, a);
-    SBITS_HIP(ctx, hipGetLastError());
+    constexpr int64_t most = MOST_TOKENS / 4;                  // (a workgroup a token)
+    for (int64_t first = 0; first < tokens; first += most) {
+        a.y = static_cast<const uint16_t *>(y) + first * top_k * ld_y;
+        a.ids = ids + first * top_k;
+        a.weights = weights + first * top_k;
+        a.out = static_cast<uint16_t *>(out) + first * ld_out;
+        hipLaunchKernelGGL(combine_kernel, dim3((unsigned)std::min(tokens - first, most), (unsigned)((hidden + 2047) / 2048)), dim3(256), 0, ctx->stream, a);
+        SBITS_HIP(ctx, hipGetLastError());
+    }
     return SBITS_OK;
 }
