@@ -84,7 +84,7 @@ struct MxGemm {
     const uint8_t *w, *ws;          // codes and scales of the (first) matrix
     int64_t ld_w, ld_ws;            // pitches in bytes
     int64_t w_rows;                 // rows of one matrix (of both halves where gated)
-    int outs;                       // outputs of a row: w_rows, or half of them
+    int outs;                       // outputs of a row: w_rows, or half of them (in a launch for a part of them what is left of those)
     int cols;
     const void *x;                  // bf16, or codes
     const uint8_t *xs;              // scales of x, or null

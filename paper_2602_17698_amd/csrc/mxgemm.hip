@@ -40,7 +40,7 @@ __global__ __launch_bounds__(64 * WAVES, T * U > 8 ? 2 : 3) void mx_gemm_few_ker
     for (int k = 0; k < T; ++k) {
         int row = out0 + 16 * (k % HALF) + n;
         if (row >= g.outs) row = g.outs - 1;                    // (its sums go nowhere)
-        const int64_t at = (int64_t)t.expert * g.w_rows + (k >= HALF ? g.outs : 0) + row;
+        const int64_t at = (int64_t)t.expert * g.w_rows + (k >= HALF ? g.w_rows / 2 : 0) + row;
         w[k] = g.w + at * g.ld_w + 16 * q;
         ws[k] = g.ws + at * g.ld_ws;
     }
@@ -263,8 +263,16 @@ int sbits_launch_mx_gemm(sbits_ctx *ctx, const MxGemm &g)
             part.y = static_cast<char *>(g.y) + skip * g.ld_y * (g.y_bf16 ? 2 : 4);
             part.batch = g.batch - skip;
         }
-        hipLaunchKernelGGL(fn, dim3((unsigned)((g.outs + outs - 1) / outs), (unsigned)n), dim3(64 * waves), 0, ctx->stream, part);
-        SBITS_HIP(ctx, hipGetLastError());
+        // (a grid has fewer than 2^32 threads along an axis, and a tile's rows count in 31 bits)
+        constexpr int most = 1 << 22;
+        for (int64_t out = 0; out < g.outs; out += (int64_t)most * outs) {
+            part.w = g.w + out * g.ld_w;
+            part.ws = g.ws + out * g.ld_ws;
+            part.outs = (int)(g.outs - out);
+            hipLaunchKernelGGL(fn, dim3((unsigned)std::min((part.outs - 1) / outs + 1, most), (unsigned)n), dim3(64 * waves), 0, ctx->stream, part);
+            SBITS_HIP(ctx, hipGetLastError());
+            part.y = static_cast<char *>(part.y) + (int64_t)most * outs * (g.y_bf16 ? 2 : 4);
+        }
     }
     return SBITS_OK;
 }

@@ -58,3 +58,22 @@ def test_layer_of_more_tokens_than_a_launch_of_the_sum_takes(ctx):
                                           mp.values(*down).view(experts, hidden, inner), False)
         assert torch.equal(ids[part].cpu(), want_ids)
         assert bool(((out[part].cpu().double() - want).abs() <= off).all())
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_product_with_more_rows_of_w_than_a_launch_takes(ctx, gated):
+    border, cols = (32 if gated else 64) << 22, 32
+    outs = border + 77
+    rows = outs * (2 if gated else 1)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    codes = torch.randint(0, 256, (rows, cols // 2), dtype=torch.uint8, device="cuda", generator=g)
+    scales = torch.randint(118, 124, (rows, 4), dtype=torch.uint8, device="cuda", generator=g)
+    x = torch.randn(1, cols, device="cuda", generator=g).to(torch.bfloat16)
+    y = torch.full((1, sb.mx_out_pitch(outs)), 7.0, device="cuda")
+    print("[case]", rows, flush=True)
+    ctx.mx_gemm(sb.mx(codes, scales, cols), x, y[:, :outs], None, gated=gated)
+    assert bool((y[:, outs:] == 7.0).all())
+    for first, last in ((0, 50), (border - 50, outs)):
+        part = torch.cat([torch.arange(first, last) + half * outs for half in range(2 if gated else 1)]).cuda()
+        want, off = mp.product(x.cpu().double(), mp.values(mp.unpack(codes[part].cpu()), scales[part, :1].cpu()), gated)
+        assert bool(((y[:, first:last].cpu().double() - want).abs() <= off + 2.0 ** -24 * (want.abs() + off)).all())
