@@ -198,11 +198,13 @@ def mx_out_pitch(rows: int) -> int:
 
 def mx(codes, scales, cols: int) -> Mx:
     """Descriptor of a matrix in the microscaled form: uint8 tensors of codes [rows, >= cols / 2] and scales [rows, >= pitch]."""
-    _is(codes, _UINT8, "codes")
-    _is(scales, _UINT8, "scales")
+    if not (codes.dtype is scales.dtype is _uint8):
+        _is(codes, _UINT8, "codes")
+        _is(scales, _UINT8, "scales")
     rows, width = codes.shape
+    of, bytes_ = scales.shape
     # (the blocks' bytes are read in fours: rows of scales up to a multiple of 4)
-    if 2 * width < cols or scales.shape[0] != rows or scales.shape[1] < (cols + 127) // 128 * 4:
+    if 2 * width < cols or of != rows or bytes_ < (cols + 127) // 128 * 4:
         raise ValueError("codes %s and scales %s do not hold %d columns" % (tuple(codes.shape), tuple(scales.shape), cols))
     d = Mx(codes.data_ptr(), scales.data_ptr(), rows, cols, _pitch(codes), _pitch(scales))
     d.codes_tensor, d.scales_tensor = codes, scales       # (also keeps them alive as long as the descriptor lives)
@@ -212,19 +214,25 @@ def mx(codes, scales, cols: int) -> Mx:
 def _pitch(t) -> int:
     """Elements between the rows of a matrix whose rows are dense; of a single row its length, up to what every call takes."""
     row, element = t.stride()
-    rows, cols = t.shape
-    if element != 1 and cols > 1:
-        raise ValueError("rows of a tensor have to be dense")
-    return row if rows != 1 else (cols + 15) // 16 * 16
+    if element != 1 or row & 15:
+        rows, cols = t.shape
+        if element != 1 and cols > 1:
+            raise ValueError("rows of a tensor have to be dense")
+        if rows == 1:
+            return (cols + 15) // 16 * 16
+    return row
 
 
 _types = {}                     # torch.dtype -> its number here (filled on first use: the search's calls do not import torch)
 _INT32, _UINT8 = 100, 101
+_uint8 = None                   # torch.uint8, once _types is filled
 
 
 def _kind(t) -> int:
+    global _uint8
     if not _types:
         import torch
+        _uint8 = torch.uint8
         _types.update({torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16, torch.int32: _INT32, torch.uint8: _UINT8})
     return _types.get(t.dtype, -1)
 
