@@ -455,7 +455,8 @@ int  sbits_mx_quantize(sbits_ctx *ctx, const void *x, int x_type, int64_t ld_x, 
  * of 8; elements of a row behind those are left as they are.  Sums are taken in fp32 on the matrix
  * cores and rounded once; a call gives the same bits again.  With x_bf16 a value of W beyond
  * bfloat16's range (possible with the bytes 253 and 254 only) counts as infinite.  batch may be 0.  ws: 256-byte
- * aligned, sbits_mx_gemm_ws_bytes() bytes (which may be 0).                        */
+ * aligned, sbits_mx_gemm_ws_bytes() bytes (which may be 0), asked for with the call's own arguments (both
+ * kinds of product are cut up alike, so `gated` makes no difference to it).        */
 size_t sbits_mx_gemm_ws_bytes(const sbits_ctx *ctx, const sbits_mx *w, int64_t batch, int four_bit, int gated);
 int  sbits_mx_gemm(sbits_ctx *ctx, const sbits_mx *w, const void *x_bf16, int64_t ld_x, const sbits_mx *x_mx, int64_t batch,
                    int gated, void *y, int y_type, int64_t ld_y, void *ws, size_t ws_bytes);

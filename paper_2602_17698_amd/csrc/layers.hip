@@ -114,10 +114,9 @@ int sbits_mx_quantize(sbits_ctx *ctx, const void *x, int x_type, int64_t ld_x, c
     return sbits_launch_mx_quantize(ctx, x, x_type == SBITS_TYPE_BF16, ld_x, *q, q->rows, values_bf16, ld_values);
 }
 
-size_t sbits_mx_gemm_ws_bytes(const sbits_ctx *ctx, const sbits_mx *w, int64_t batch, int four_bit, int gated)
+size_t sbits_mx_gemm_ws_bytes(const sbits_ctx *ctx, const sbits_mx *w, int64_t batch, int four_bit, int /*gated*/)
 {
     if (!ctx || check_mx(w) || batch <= 0 || batch > INT32_MAX) return 0;
-    (void)gated;
     MxGemm g = {};
     product_shape(ctx, *w, batch, four_bit != 0, four_bit ? w->cols / 2 : 2 * w->cols, g);      // (rows of x far apart: no parts)
     return product_space(g);

@@ -16,7 +16,7 @@ namespace sbits {
 // for ahead of the products of the one before.
 // D layout: W's row l % 16, x's row 4 (l / 16) + r.
 // Reading W bounds it, at what so many loads under way allow: one row of x, bf16, through 14336 x 4096 10.4 us (3.0 TB/s: 224 workgroups, one a CU, whose start
-// and LDS sum are a third of it), 128 rows through 64 matrices of 2048 x 2048, a row or two each, 28.6 us (4.1 TB/s; a plain read reaches 6).
+// and LDS sum are a third of it), 128 rows through 64 matrices of 2048 x 2048, a row or two each, 28.6 us (4.1 TB/s; a plain read reaches 7.2).
 template <int T, int U>
 struct FewGroup { u32x4 codes[T][U], scales[T]; };    // scales: of the row's 4 U blocks in the group, a byte each
 

@@ -12,10 +12,10 @@
 // that a lane's scales are neighbours.
 // Order of W's rows: tile t of a wave has rows NT n + t, n = l % 32, so that a lane's outputs for a row of x are NT neighbours, a wave's 32 NT.
 // With gated products tiles 2 p and 2 p + 1 are rows NT / 2 n + p of both halves of W.
-// What bounds it: with random data the clock falls to 1.55 .. 1.8 GHz at the card's power limit (matrix instructions alone, from registers: 5.9 PFLOP/s in 4 bits,
-// 1.5 in bf16); of a step of 256 columns in 4 bits a quarter is not hidden behind them (operands from LDS and loads to it take 2.0 us where they take 1.5).
-// 8192 x 14336 x 4096, x in 4 bits, 249 us: 3.9 PFLOP/s; 1000 rows of x in bf16, gated, 28672 x 4096, 190 us: 1.24 PFLOP/s (448 tiles on 256 CUs, 7/8 of two
-// rounds); 37 rows in bf16, 4096 x 14336, the columns in 14 parts, 17 us and 4 to join them; 16384 places of 32 experts, 4096 x 4096, gated, 4 bits, 205 .. 240 us,
+// What bounds it: with random data the clock falls to 1.55 .. 1.8 GHz at the card's power limit (matrix instructions alone, from registers: 6.0 PFLOP/s in 4 bits,
+// 1.8 in bf16); of a step of 256 columns in 4 bits a quarter is not hidden behind them (operands from LDS and loads to it take 2.0 us where they take 1.5).
+// 8192 x 14336 x 4096, x in 4 bits, 243 .. 282 us (the clock decides): 4.0 .. 3.4 PFLOP/s; 1000 rows of x in bf16, gated, 28672 x 4096, 187 us, after a pause 200 and
+// more: 1.25 PFLOP/s (448 tiles on 256 CUs, 7/8 of two rounds); 37 rows in bf16, 4096 x 14336, the columns in 14 parts, 17 us and 4 to join them; 16384 places of 32 experts, 4096 x 4096, gated, 4 bits, 205 .. 240 us,
 // 4096 x 2048 120 .. 140 (2.7 .. 2.0 PFLOP/s: rows by lists, tiles that an expert's rows do not fill).
 // LDS: the pieces of a row are permuted (xor) by bits of the row's number, so that 16 rows of one piece lie in different banks.
 #include <algorithm>

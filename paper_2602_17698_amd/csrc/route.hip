@@ -13,8 +13,10 @@ namespace sbits {
 // Which experts are taken is decided as with scores in 64 bits, but scores are computed in fp32 first, with a bound on how far each
 // may be off.  Where the bounds leave only the order of the chosen ones open, these are computed in 64 bits and put in order (a token in some hundred with
 // sigmoid scores and a bias); only where they leave the choice open (one in a thousand) all are.  In 64 bits for every token 16384 x 256 took 52 us.
-// 16384 tokens of 256 experts, 8 groups, a bias, the best 8: 21 us, 0.8 TB/s.  Instruction issue bounds it: 640 vector instructions of 4 cycles a token, a
-// third of them in the top_k searches of the largest key.  Without groups, bias and sigmoid 15 us; 2048 tokens 7.
+// 16384 tokens of 256 experts, 8 groups, a bias, the best 8: 21 us, 0.8 TB/s.  Instruction issue bounds it: 650 vector instructions of 4 cycles a token, a
+// third of them in the top_k searches of the largest key.  Weights are fp32's p, off by up
+// to what `by_p` below says, 5e-8 in the root mean square where the rounding of those of 64 bits is off by 2.8e-8: these were the 52 us.  Without groups, bias and
+// sigmoid 15 us; 2048 tokens 7.
 struct RouteArgs {
     const void *logits;
     const float *bias;
@@ -388,7 +390,7 @@ __global__ __launch_bounds__(256) void route_kernel(RouteArgs a)
 //   sigmoid               d_x[i] = d[i] p[i] (1 - p[i])
 //   sigmoid, renormalised d_x[i] = s[i] (d[i] - sum_c d s) (1 - p[i])
 // A wave a token; a chosen expert's value reaches its lane by top_k comparisons (no atomics, no order).  16384 x 128 in bf16, top 8: 9.0 us, 12.6 MB, 1.4 TB/s:
-// bound by issue, some 200 instructions a token.
+// bound by issue, some 210 instructions a token.
 struct RouteBackArgs {
     const void *logits;
     const int32_t *ids;
