@@ -19,12 +19,12 @@ for rows, cols, batch in %r:
 answer(out)
 """
 
-# (rows of the last matrix below the border, columns, rows of x): codes end 3072 bytes ahead of 2 GiB, or the row's pitch further ahead
+# (rows of the last matrix below the border, columns, rows of x): codes end 3 KiB ahead of 2 GiB, or up to a row further ahead
 BORDER = [(299592, 14336, 700), (1048574, 4096, 4000), (16777191, 256, 70)]
 
 
 def test_matrices_at_the_border_of_31_bits(tmp_path):
-    lead = 3072                                                 # bytes that the kernel's buffers begin ahead
+    lead = 3 * 1024                                             # bytes that the kernel's buffers begin ahead
     cases = [(rows + more, cols, batch) for rows, cols, batch in BORDER for more in (0, 1)]
     for rows, cols, four, rc, names in record(tmp_path, PRODUCTS % (cases,)):
         inside = rows * (cols // 2) + lead <= 2 ** 31 - 1
