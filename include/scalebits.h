@@ -510,6 +510,104 @@ int  sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logit
                         const sbits_mx *down, void *out_bf16, int64_t ld_out, int32_t *ids, float *weights, int four_bit,
                         void *ws, size_t ws_bytes);
 
+/* ---- a cache of keys and values in the microscaled form ---------------------------
+ * Keys and values of a batch of sequences, in pages of page_tokens tokens; a sequence's
+ * pages are listed in a row of a table.  In a page, a head's tokens follow each other, a
+ * token's row being head_dim values in the microscaled form: head_dim / 2 bytes of codes,
+ * sbits_mx_scale_pitch(head_dim) bytes of scales, of which those behind the last block may hold
+ * anything.  Code row of token t and head h in page p: p * ld_codes + (h * page_tokens + t) *
+ * head_dim / 2; scales likewise.  Codes 16-byte aligned, ld_codes a multiple of 16, scales
+ * 4-byte aligned, ld_scales a multiple of 4; pitches at least a page long.            */
+typedef struct {
+    void *k_codes, *k_scales, *v_codes, *v_scales;   /* DEVICE                          */
+    int64_t pages;                                   /* 1 .. 2^31 - 1                   */
+    int64_t ld_codes, ld_scales;                     /* bytes from page to page         */
+    int32_t page_tokens;                             /* a power of two, 1 .. 2^20       */
+    int32_t kv_heads, head_dim;                      /* 1 .. 1024; a multiple of 32, 32 .. 256 */
+} sbits_kv_cache;
+
+/* The sequences of a batch.  Sequence b has the rows starts[b] .. starts[b + 1] - 1 of the
+ * tensors beside the cache, none if they are equal: its last tokens.  lengths[b] counts its tokens, those
+ * included, so that row r is at position lengths[b] - starts[b + 1] + r; page pages[b][p / page_tokens]
+ * has position p.  A page's number outside the cache's, or a position behind the row's last
+ * entry, is a place that is not there: nothing is written to it, its keys are not seen, and reading it
+ * gives zeros.  Rows ahead of starts[0] or behind starts[count] belong to no sequence and
+ * are left as they were.  Several sequences may have the same pages for what they only read; of pages into which
+ * a call writes each has to be one sequence's own, listed once.                        */
+typedef struct {
+    const int32_t *starts;                           /* DEVICE, count + 1, ascending     */
+    const int32_t *lengths;                          /* DEVICE, count                    */
+    const int32_t *pages;                            /* DEVICE, [count][ld_pages]        */
+    int64_t ld_pages;
+    int32_t count, max_pages;                        /* entries of a row of pages: 1 or more, <= ld_pages */
+    int32_t max_new, max_length;                     /* rows that no sequence has more of, and tokens; 0 where not known.
+                                                        They only choose between ways to the same result */
+} sbits_sequences;
+
+/* Rotary positions.  The first 2 * pairs elements of a head are pairs, (i, pairs + i) or, interleaved,
+ * (2 i, 2 i + 1); pair i at position p is turned by p * turns[i] whole turns and scaled by
+ * amplitude: (a, b) to (a cos - b sin, b cos + a sin) * amplitude; what is behind stays as it
+ * is.  Angles are computed in 64 bits.                                                  */
+typedef struct {
+    const double *turns;                             /* DEVICE, pairs                    */
+    int32_t pairs, interleaved;                      /* 1 .. 128; 0, 1                   */
+    double amplitude;
+} sbits_rotary;
+
+/* HOST.  turns[i], i < pairs, for frequencies f = base^(-i / pairs), scaled for longer contexts:
+ *   SBITS_ROTARY_PLAIN    f / 2 pi
+ *   SBITS_ROTARY_LINEAR   f / (2 pi factor)
+ *   SBITS_ROTARY_TURNS    by the turns n = context * f / 2 pi of a pair: f where n >= high,
+ *                         f / factor where n <= low, between them in proportion to n
+ *   SBITS_ROTARY_INDEX    by the pair's number: f up to the floor of the index that turns high times over the context, f / factor
+ *                         from the ceiling of the one that turns low times on, between them in proportion to the index
+ * low < high and context >= 1 are read by the last two only.                             */
+#define SBITS_ROTARY_PLAIN  0
+#define SBITS_ROTARY_LINEAR 1
+#define SBITS_ROTARY_TURNS  2
+#define SBITS_ROTARY_INDEX  3
+int  sbits_rotary_turns(int pairs, double base, int scaling, double factor, double low, double high, double context,
+                        double *turns);
+
+/* out = x with each row turned by its position (int32[tokens], any sign); inverse: by the opposite angle, the
+ * amplitude as it is, which is the gradient with respect to x given that with respect to out.
+ * x, out: element j of head h of row t at t * ld + h * hd + j, of `type`; x and out may be the same with the same pitches, else they must
+ * not overlap.  head_dim 2 .. 256, 2 * pairs <= head_dim.  tokens may be 0.              */
+int  sbits_rotate(sbits_ctx *ctx, const sbits_rotary *rotary, const int32_t *positions, int64_t tokens, int heads, int head_dim,
+                  const void *x, int64_t ld_x, int64_t hd_x, int type, int inverse, void *out, int64_t ld_out, int64_t hd_out);
+
+/* Writes the rows of k and v ([tokens][kv_heads][head_dim] by pitches as above, of `type`) to their sequences' places in
+ * the cache, quantised as sbits_mx_quantize does.  With `rotary` (may be NULL) keys are turned
+ * first, by positions[row] or, where positions is NULL, by the row's place in its sequence, in 64
+ * bits, without a rounding ahead of the quantisation; and so are the rows of q (may be NULL) with q_heads
+ * heads, rounded once to `type`, into q_out (which may be q).  Rows that are 16-byte aligned: pitches multiples of 8
+ * (bf16) or 4 (fp32).  Where a place is not there, q_out is written all the same.         */
+int  sbits_kv_store(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens,
+                    const void *k, int64_t ld_k, int64_t hd_k, const void *v, int64_t ld_v, int64_t hd_v, int type,
+                    const sbits_rotary *rotary, const int32_t *positions, const void *q, int64_t ld_q, int64_t hd_q, int q_heads,
+                    void *q_out, int64_t ld_q_out, int64_t hd_q_out);
+
+/* Reads the rows' places back: what the codes stand for, exactly in fp32, rounded in bf16 (exact but below 2^-133).
+ * k, v: as above, 16-byte aligned; either may be NULL.                                   */
+int  sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens,
+                   void *k, int64_t ld_k, int64_t hd_k, void *v, int64_t ld_v, int64_t hd_v, int type);
+
+/* Attention of the rows to their sequences' cached tokens:  out = sum_j p_j v_j,  p = softmax over the keys seen of
+ * scale * q . k_j.  q, out: bf16 [tokens][heads][head_dim] by pitches as above, 16-byte aligned, pitches multiples of 8;
+ * heads a multiple of kv_heads, head h reads kv_heads' number h / (heads / kv_heads).  causal: a row at position p sees the
+ * positions up to p, with window > 0 (causal only) the last `window` of them; else all of the sequence's.
+ * A row that sees no key gets zeros.  lse (float32[tokens][heads], may be NULL): the logarithm of the sum of
+ * e^(scale * q . k_j), -infinity where no key is seen.  Only keys that a row sees have a part in it, whatever the others
+ * hold; a seen value that is not finite makes its block of 32 outputs NaN (in v the bytes 253 and 254 count as 255), a seen key that is
+ * not or a q that is not makes the row NaN.  Scores and sums are taken in fp32 on the matrix cores, in an order that goes with the batch's
+ * sizes; a call gives the same bits again.  scale > 0.  ws: 256-byte aligned,
+ * sbits_kv_attention_ws_bytes() bytes (which may be 0), asked for with the call's own arguments.  */
+size_t sbits_kv_attention_ws_bytes(const sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens,
+                                   int heads);
+int  sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens, int heads,
+                        const void *q_bf16, int64_t ld_q, int64_t hd_q, float scale, int causal, int window,
+                        void *out_bf16, int64_t ld_out, int64_t hd_out, float *lse, void *ws, size_t ws_bytes);
+
 #ifdef __cplusplus
 }
 #endif

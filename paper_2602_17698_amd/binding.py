@@ -19,6 +19,7 @@ ERR_WORKSPACE, ERR_MAX_ITERS, ERR_HIP, ERR_UNIMPLEMENTED, ERR_CAPACITY, ERR_INTE
 TYPE_FP32, TYPE_BF16 = 0, 1
 ROUTE_SOFTMAX, ROUTE_SIGMOID = 0, 1
 ROUTE_GROUP_TOP2, ROUTE_GROUP_MAX = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_TURNS, ROTARY_INDEX = 0, 1, 2, 3
 OFFSETS_STATIC_MAX_BLOCKS = 8388608          # SBITS_OFFSETS_STATIC_MAX_BLOCKS of the header
 
 EXPORTS = [
@@ -32,6 +33,7 @@ EXPORTS = [
     "sbits_allocate", "sbits_propose", "sbits_offsets", "sbits_offsets_static", "sbits_pack", "sbits_search", "sbits_search_coupled", "sbits_mp_gemm", "sbits_dequant",
     "sbits_mx_scale_pitch", "sbits_mx_out_pitch", "sbits_mx_quantize", "sbits_mx_gemm_ws_bytes", "sbits_mx_gemm",
     "sbits_route", "sbits_route_backward", "sbits_expert_layer_ws_bytes", "sbits_expert_layer",
+    "sbits_rotary_turns", "sbits_rotate", "sbits_kv_store", "sbits_kv_load", "sbits_kv_attention_ws_bytes", "sbits_kv_attention",
 ]
 
 
@@ -94,6 +96,23 @@ class Router(C.Structure):
         super().__init__(experts, top_k, scoring, groups, top_groups, group_score, 1 if renormalize else 0)
 
 
+class Rotary(C.Structure):
+    """Rotary positions (see rotary())."""
+    _fields_ = [("turns", C.c_void_p), ("pairs", C.c_int32), ("interleaved", C.c_int32), ("amplitude", C.c_double)]
+
+
+class KvCache(C.Structure):
+    """A cache of keys and values in the microscaled form (see kv_cache())."""
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p), ("v_scales", C.c_void_p), ("pages", C.c_int64),
+                ("ld_codes", C.c_int64), ("ld_scales", C.c_int64), ("page_tokens", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class Sequences(C.Structure):
+    """The sequences of a batch (see sequences())."""
+    _fields_ = [("starts", C.c_void_p), ("lengths", C.c_void_p), ("pages", C.c_void_p), ("ld_pages", C.c_int64), ("count", C.c_int32),
+                ("max_pages", C.c_int32), ("max_new", C.c_int32), ("max_length", C.c_int32)]
+
+
 class SbitsError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -125,11 +144,16 @@ def load():
                                 ("mx_gemm_ws_bytes", [p, p, n, i, i]), ("mx_gemm", [p, p, p, n, p, n, i, p, i, n, p, z]),
                                 ("route", [p, p, p, i, n, p, n, p, p]), ("route_backward", [p, p, p, i, n, p, p, n, p, n]),
                                 ("expert_layer_ws_bytes", [p, p, n, p, p, i]),
-                                ("expert_layer", [p, p, p, i, n, p, p, n, n, p, p, p, n, p, p, i, p, z])):
+                                ("expert_layer", [p, p, p, i, n, p, p, n, n, p, p, p, n, p, p, i, p, z]),
+                                ("rotary_turns", [i, C.c_double, i, C.c_double, C.c_double, C.c_double, C.c_double, p]),
+                                ("rotate", [p, p, p, n, i, i, p, n, n, i, i, p, n, n]),
+                                ("kv_store", [p, p, p, n, p, n, n, p, n, n, i, p, p, p, n, n, i, p, n, n]),
+                                ("kv_load", [p, p, p, n, p, n, n, p, n, n, i]), ("kv_attention_ws_bytes", [p, p, p, n, i]),
+                                ("kv_attention", [p, p, p, n, i, p, n, n, C.c_float, i, i, p, n, n, p, p, z])):
                 getattr(lib, "sbits_" + name).argtypes = types
             for name in ("sbits_mx_scale_pitch", "sbits_mx_out_pitch"):
                 getattr(lib, name).restype = n
-            for name in ("sbits_mx_gemm_ws_bytes", "sbits_expert_layer_ws_bytes"):
+            for name in ("sbits_mx_gemm_ws_bytes", "sbits_expert_layer_ws_bytes", "sbits_kv_attention_ws_bytes"):
                 getattr(lib, name).restype = z
             _loaded[LIB_PATH] = lib
         _lib = _loaded[LIB_PATH]
@@ -221,6 +245,79 @@ def _pitch(t) -> int:
         if rows == 1:
             return (cols + 15) // 16 * 16
     return row
+
+
+def rotary_turns(dims: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0, low: float = 1.0, high: float = 4.0,
+                 context: float = 8192):
+    """Turns a position of the dims / 2 pairs of a head (a list of floats: put them into a float64 tensor on the device for rotary())."""
+    turns = (C.c_double * (dims // 2))()
+    if dims % 2:
+        raise ValueError("pairs need an even number of elements")
+    _check(load().sbits_rotary_turns(dims // 2, base, scaling, factor, low, high, context, C.addressof(turns)), "sbits_rotary_turns")
+    return list(turns)
+
+
+def rotary(turns, interleaved: bool = False, amplitude: float = 1.0) -> Rotary:
+    """Rotary positions from the turns of each pair (float64 on the device); pairs are halves of the rotated part, or neighbours."""
+    import torch
+    if turns.dtype != torch.float64 or turns.dim() != 1 or not turns.is_contiguous():
+        raise TypeError("turns have to be a dense vector in float64")
+    r = Rotary(turns.data_ptr(), turns.shape[0], 1 if interleaved else 0, amplitude)
+    r.turns_tensor = turns
+    return r
+
+
+def kv_cache(k_codes, k_scales, v_codes, v_scales, head_dim: int) -> KvCache:
+    """Descriptor of a cache: uint8 tensors [pages, kv_heads, page_tokens, head_dim / 2] of codes and [.., mx_scale_pitch(head_dim)] of scales, the last
+    three dimensions dense."""
+    for name, t in (("k_codes", k_codes), ("k_scales", k_scales), ("v_codes", v_codes), ("v_scales", v_scales)):
+        _is(t, _UINT8, name)
+    pages, heads, tokens, _ = k_codes.shape
+    pitches = []
+    for pair, row in (((k_codes, v_codes), head_dim // 2), ((k_scales, v_scales), mx_scale_pitch(head_dim))):
+        for t in pair:
+            if t.shape != (pages, heads, tokens, row):
+                raise ValueError("%s is not [%d, %d, %d, %d]" % (tuple(t.shape), pages, heads, tokens, row))
+            if not t[0].is_contiguous():
+                raise ValueError("a page has to be dense")
+        pitch = {t.stride(0) for t in pair} if pages > 1 else {heads * tokens * row}
+        if len(pitch) > 1:
+            raise ValueError("pages of keys and values lie differently far apart")
+        # (of a single page no pitch is read: any that the call takes)
+        pitches.append(pitch.pop() if pages > 1 else (heads * tokens * row + 15) // 16 * 16)
+    c = KvCache(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), pages, *pitches, tokens, heads, head_dim)
+    c.tensors = (k_codes, k_scales, v_codes, v_scales)
+    return c
+
+
+def sequences(starts, lengths, pages, max_new: int = 0, max_length: int = 0) -> Sequences:
+    """Descriptor of a batch's sequences: int32 tensors starts [count + 1], lengths [count], pages [count, max_pages]; max_new, max_length: rows
+    and tokens that no sequence has more of, 0 where not known."""
+    for name, t in (("starts", starts), ("lengths", lengths), ("pages", pages)):
+        _is(t, _INT32, name)
+    count, most = pages.shape
+    if starts.shape != (count + 1,) or lengths.shape != (count,):
+        raise ValueError("starts, lengths and pages are not of the same sequences")
+    if not (starts.is_contiguous() and lengths.is_contiguous()) or (most > 1 and pages.stride(1) != 1):
+        raise ValueError("starts, lengths and rows of pages have to be dense")
+    s = Sequences(starts.data_ptr(), lengths.data_ptr(), pages.data_ptr(), pages.stride(0) if count > 1 else most, count, most, max_new, max_length)
+    s.tensors = (starts, lengths, pages)
+    return s
+
+
+def _heads(t, heads, dim):
+    """Address and pitches of a tensor [tokens, heads, dim]; of a single token or head any pitch that the calls take."""
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != dim or (heads and shape[1] != heads):
+        raise ValueError("%s is not [tokens, %s, %d]" % (tuple(shape), heads or "heads", dim))
+    ld, hd, one = t.stride()
+    if one != 1 and dim > 1:
+        raise ValueError("heads of a tensor have to be dense")
+    if shape[1] == 1:
+        hd = (dim + 7) // 8 * 8
+    if shape[0] == 1:
+        ld = hd * shape[1]
+    return t.data_ptr(), ld, hd
 
 
 _types = {}                     # torch.dtype -> its number here (filled on first use: the search's calls do not import torch)
@@ -325,6 +422,77 @@ class Context:
                                                 C.addressof(up), C.addressof(down), out.data_ptr(), _pitch(out), ids.data_ptr(),
                                                 weights.data_ptr(), 1 if four_bit else 0, ws.data_ptr() if ws is not None else None,
                                                 ws.nbytes if ws is not None else 0), "sbits_expert_layer")
+
+
+    # ---- a cache of keys and values in the microscaled form (see scalebits.h) -----------
+    def rotate(self, rotary: Rotary, positions, x, out, inverse: bool = False):
+        """out = x [tokens, heads, head_dim] (bf16 or fp32) turned by the positions (int32) of its rows; inverse: the gradient."""
+        tokens, heads, dim = x.shape
+        kind = _type(x)
+        _is(out, kind, "out")
+        _is(positions, _INT32, "positions")
+        if out.shape != x.shape or positions.shape != (tokens,) or not positions.is_contiguous():
+            raise ValueError("x, out and positions are not of the same rows")
+        return _check(load().sbits_rotate(self.h, C.addressof(rotary), positions.data_ptr(), tokens, heads, dim, *_heads(x, heads, dim), kind,
+                                          1 if inverse else 0, *_heads(out, heads, dim)), "sbits_rotate")
+
+    def kv_store(self, cache: KvCache, sequences: Sequences, k, v, rotary: Rotary = None, positions=None, q=None, q_out=None):
+        """k and v [tokens, kv_heads, head_dim] (bf16 or fp32) into the cache; with `rotary` keys are turned on the way, and q into q_out."""
+        tokens, kind, dim = k.shape[0], _type(k), cache.head_dim
+        _is(v, kind, "v")
+        if v.shape != k.shape:
+            raise ValueError("k and v differ in shape")
+        if (positions is not None or q is not None) and rotary is None:
+            raise ValueError("positions and q are for a rotation")
+        if positions is not None:
+            _is(positions, _INT32, "positions")
+            if positions.shape != (tokens,) or not positions.is_contiguous():
+                raise ValueError("positions is not [%d]" % tokens)
+        queries, heads, turned = (None, 0, 0), 0, (None, 0, 0)
+        if q is not None:
+            _is(q, kind, "q")
+            _is(q_out, kind, "q_out")
+            heads = q.shape[1]
+            if q.shape != q_out.shape or q.shape[0] != tokens:
+                raise ValueError("q, q_out and k are not of the same rows")
+            queries, turned = _heads(q, heads, dim), _heads(q_out, heads, dim)
+        return _check(load().sbits_kv_store(self.h, C.addressof(cache), C.addressof(sequences), tokens, *_heads(k, cache.kv_heads, dim),
+                                            *_heads(v, cache.kv_heads, dim), kind, C.addressof(rotary) if rotary is not None else None,
+                                            positions.data_ptr() if positions is not None else None, *queries, heads, *turned), "sbits_kv_store")
+
+    def kv_load(self, cache: KvCache, sequences: Sequences, k, v):
+        """What the cache has at the rows' places, into k and v [tokens, kv_heads, head_dim] (bf16 or fp32; either may be None)."""
+        t = k if k is not None else v
+        if t is None:
+            return OK
+        kind, heads, dim = _type(t), cache.kv_heads, cache.head_dim
+        if k is not None and v is not None:
+            _is(v, kind, "v")
+            if k.shape != v.shape:
+                raise ValueError("k and v differ in shape")
+        return _check(load().sbits_kv_load(self.h, C.addressof(cache), C.addressof(sequences), t.shape[0],
+                                           *(_heads(k, heads, dim) if k is not None else (None, 0, 0)),
+                                           *(_heads(v, heads, dim) if v is not None else (None, 0, 0)), kind), "sbits_kv_load")
+
+    def kv_attention_ws_bytes(self, cache: KvCache, sequences: Sequences, tokens: int, heads: int) -> int:
+        return load().sbits_kv_attention_ws_bytes(self.h, C.addressof(cache), C.addressof(sequences), tokens, heads)
+
+    def kv_attention(self, cache: KvCache, sequences: Sequences, q, out, ws, scale: float = None, causal: bool = True, window: int = 0, lse=None):
+        """out (bf16 [tokens, heads, head_dim]) = the attention of q's rows to their sequences' cached tokens; scale: 1 / sqrt(head_dim) unless given; lse
+        (fp32 [tokens, heads]): the logarithms of the sums."""
+        tokens, heads, dim = q.shape
+        _is(q, TYPE_BF16, "q")
+        _is(out, TYPE_BF16, "out")
+        if out.shape != q.shape or dim != cache.head_dim:
+            raise ValueError("q and out are not [tokens, heads, %d]" % cache.head_dim)
+        if lse is not None:
+            _is(lse, TYPE_FP32, "lse")
+            if lse.shape != (tokens, heads) or not lse.is_contiguous():
+                raise ValueError("lse is not [tokens, heads]")
+        return _check(load().sbits_kv_attention(self.h, C.addressof(cache), C.addressof(sequences), tokens, heads, *_heads(q, heads, dim),
+                                                dim ** -0.5 if scale is None else scale, 1 if causal else 0, window, *_heads(out, heads, dim),
+                                                lse.data_ptr() if lse is not None else None, ws.data_ptr() if ws is not None else None,
+                                                ws.nbytes if ws is not None else 0), "sbits_kv_attention")
 
 
 def _routed(router, logits, bias, ids, weights) -> int:

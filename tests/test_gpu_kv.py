@@ -1,0 +1,389 @@
+"""The cache of keys and values in the microscaled form, rotary positions and attention against their definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import kv_plain
+from kv_plain import Batch
+from paper_2602_17698_amd import binding as sb
+
+pytestmark = pytest.mark.gpu
+BF16, FP32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = sb.Context(0, torch.cuda.current_stream().cuda_stream)
+    yield c
+    c.close()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def spaced(shape, dtype, pad, heads_first=False):
+    """A tensor [tokens, heads, dim] on the device whose rows or heads lie `pad` elements further apart than need be, or heads ahead of tokens; junk between."""
+    tokens, heads, dim = shape
+    if heads_first:
+        return torch.full((heads, tokens, dim + pad), 77.0, dtype=dtype, device="cuda").transpose(0, 1)[..., :dim]
+    return torch.full((tokens, heads * dim + pad), 77.0, dtype=dtype, device="cuda")[:, :heads * dim].unflatten(1, (heads, dim))
+
+
+def rotary_of(turns, interleaved=False, amplitude=1.0):
+    return sb.rotary(torch.tensor(turns, dtype=torch.float64, device="cuda"), interleaved, amplitude)
+
+
+# ---- rotary positions ------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("tokens,heads,dim,dims,pad,first", [
+    (1, 1, 2, 2, 0, 5), (1, 40, 128, 128, 0, 0), (3, 5, 128, 64, 8, 2047), (7, 3, 80, 32, 1, 1 << 20), (5, 2, 96, 38, 0, -9),
+    (33, 1, 256, 256, 16, 1 << 30), (2, 71, 64, 16, 0, 11), (4, 2, 7, 6, 3, 100)])
+def test_rotation(ctx, dtype, interleaved, tokens, heads, dim, dims, pad, first):
+    x = torch.randn(tokens, heads, dim, generator=gen(dim)).to(dtype)
+    at = (torch.arange(tokens) * 37 + first).int()
+    turns = kv_plain.turns(dims)
+    for back in (False, True):
+        src, out = spaced(x.shape, dtype, pad), spaced(x.shape, dtype, 2 * pad, heads_first=back)
+        src.copy_(x)
+        ctx.rotate(rotary_of(turns, interleaved, 1.25), at.cuda(), src, out, inverse=back)
+        want, size = kv_plain.turn(x, at, turns, interleaved, 1.25, back)
+        # cos and sin, a product and the sum round; 2^-24 more for angles (64 bits: 2^31 turns and 53 bits)
+        off = 4 * 2.0 ** -24 * size + (2.0 ** -8 * want.abs() if dtype == BF16 else 0.0)
+        off[..., dims:] = 0
+        assert ((out.cpu().double() - want).abs() <= off).all()
+        base = out._base if out._base is not None else out
+        if pad:
+            assert int((base == 77.0).sum()) >= base.numel() - out.numel()
+        src2 = src.clone()
+        ctx.rotate(rotary_of(turns, interleaved, 1.25), at.cuda(), src2, src2, inverse=back)            # in place
+        assert torch.equal(src2, out)
+
+
+def test_rotation_backward_is_the_gradient():
+    """Of sum(out * g): against differences, which for a linear map have no error but rounding's."""
+    ctx = sb.Context(0, torch.cuda.current_stream().cuda_stream)
+    tokens, heads, dim = 3, 2, 12
+    r = rotary_of(kv_plain.turns(8), False, 0.7)
+    at = torch.tensor([0, 5, 900], dtype=torch.int32, device="cuda")
+    x, g = torch.randn(tokens, heads, dim, device="cuda"), torch.randn(tokens, heads, dim, device="cuda")
+    d = torch.empty_like(x)
+    ctx.rotate(r, at, g, d, inverse=True)
+    for i in range(dim):
+        up, out0, out1 = x.clone(), torch.empty_like(x), torch.empty_like(x)
+        up[..., i] += 1.0
+        ctx.rotate(r, at, x, out0)
+        ctx.rotate(r, at, up, out1)
+        diff = ((out1 - out0) * g).sum(-1)
+        assert torch.allclose(diff, d[..., i], rtol=0, atol=32 * 2.0 ** -24 * float((x.abs().max() + 1) * g.abs().sum(-1).max()))
+    ctx.close()
+
+
+# ---- writing and reading -----------------------------------------------------------------------------
+SIZES = [(1, 0), (5, 3), (0, 9), (40, 100), (0, 0), (2, 64)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("page,kv_heads,dim,dims,interleaved,given,pad", [
+    (16, 2, 128, 128, False, False, 0), (1, 1, 32, 32, True, False, 8), (8, 3, 96, 40, False, True, 16), (64, 1, 256, 38, True, True, 0),
+    (128, 5, 64, 64, False, False, 8), (4096, 2, 160, 0, False, False, 0), (2, 4, 192, 192, False, True, 24), (32, 1, 224, 64, True, False, 0)])
+def test_store_and_load(ctx, dtype, page, kv_heads, dim, dims, interleaved, given, pad):
+    b = Batch(SIZES, page, kv_heads, dim, seed=dim, lead=3, behind=2)
+    cache, seqs, buffers = b.on(sb)
+    before = [t.clone() for t in buffers]
+    g = gen(page)
+    big = torch.where(torch.rand(dim, generator=g) < 0.1, 30.0, 1.0)
+    k, v, q = (torch.randn(b.tokens, h, dim, generator=g).mul(big).to(dtype) for h in (kv_heads, kv_heads, 3 * kv_heads))
+    src = [spaced(x.shape, dtype, pad) for x in (k, v, q)]
+    for s, x in zip(src, (k, v, q)):
+        s.copy_(x)
+    rows, at = b.rows(), b.positions()
+    positions = None
+    if given:
+        positions = torch.full((b.tokens,), 1 << 30, dtype=torch.int32)
+        at = (at * 3 + 1000000).int()
+        positions[rows] = at
+    q_out = spaced(q.shape, dtype, pad, heads_first=True)
+    if dims:
+        ctx.kv_store(cache, seqs, src[0], src[1], rotary=rotary_of(kv_plain.turns(dims), interleaved, 1.1), q=src[2], q_out=q_out,
+                     positions=positions.cuda() if given else None)
+        want_k, _ = kv_plain.turn(k[rows], at, kv_plain.turns(dims), interleaved, 1.1)
+        want_q, _ = kv_plain.turn(q[rows], at, kv_plain.turns(dims), interleaved, 1.1)
+        got = q_out.cpu().double()
+        assert ((got[rows] - want_q).abs() <= (2.0 ** -8 if dtype == BF16 else 2.0 ** -23) * want_q.abs() + 1e-12).all()
+        assert (got[:3] == 77).all() and (got[-2:] == 77).all()
+    else:
+        ctx.kv_store(cache, seqs, src[0], src[1])
+        want_k = k[rows].double()
+    # the places of the new tokens hold what the definition says, bit by bit; all others what they held
+    expected = Batch(SIZES, page, kv_heads, dim, seed=dim, lead=3, behind=2)
+    row = 0
+    for s, (n, p) in enumerate(SIZES):
+        for i, x in enumerate((want_k, v[rows].double())):
+            expected.put(i, s, p, *kv_plain.quantised(x[row:row + n]))
+        row += n
+    for t, want in zip(buffers, (expected.codes[0], expected.scales[0], expected.codes[1], expected.scales[1])):
+        assert torch.equal(t.cpu(), want)
+    assert not torch.equal(before[0], buffers[0])
+    # and come back
+    for out_type in (BF16, FP32):
+        out = [spaced(k.shape, out_type, pad, heads_first=i == 1) for i in range(2)]
+        ctx.kv_load(cache, seqs, *out)
+        row = 0
+        for i in range(2):
+            got = out[i].cpu()
+            assert (got[:3] == 77).all() and (got[-2:] == 77).all()
+            want = torch.cat([expected.get(i, s, p, n) for s, (n, p) in enumerate(SIZES)])
+            assert torch.equal(got[rows].double(), want)
+    only = torch.full_like(k, 5.0, device="cuda")
+    ctx.kv_load(cache, seqs, None, only)
+    assert torch.equal(only.cpu()[rows].double(), want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_store_of_values_that_are_not_finite_and_of_all_powers(ctx, dtype):
+    b = Batch([(260, 0)], 32, 1, 64)
+    cache, seqs, buffers = b.on(sb)
+    g = gen(3)
+    x = torch.randn(260, 1, 64, generator=g, dtype=torch.float64).clamp(-3.9, 3.9) * torch.exp2(torch.arange(260).double() - 134)[:, None, None]
+    x = x.clamp(-3e38, 3e38).to(dtype)
+    x[7, 0, 3], x[9, 0, 40], x[11, 0, 0] = math.nan, math.inf, -math.inf
+    ctx.kv_store(cache, seqs, x.cuda(), (-x).cuda())
+    code, byte = kv_plain.quantised(x)
+    assert torch.equal(b_unpacked(buffers[0], b)[:260], code[:, 0]) and int(byte[7, 0, 0]) == 255
+    got = torch.empty(260, 1, 64, device="cuda")
+    ctx.kv_load(cache, seqs, got, None)
+    want = kv_plain.values(code, byte)
+    assert torch.equal(got.cpu().double().nan_to_num(nan=1.5), want.nan_to_num(nan=1.5))
+
+
+def b_unpacked(t, b):
+    page, at = b.places(0, 0, int(b.lengths[0]))
+    import mx_plain
+    return mx_plain.unpack(t.cpu()[page, 0, at])
+
+
+def test_places_that_are_not_there(ctx):
+    """Numbers of pages outside the cache, positions behind the table, more rows than tokens: nothing is written, zeros come back."""
+    b = Batch([(6, 10), (3, 0), (4, 29)], 8, 2, 64, extra_pages=0)
+    b.table[0, 1] = b.pages                                      # positions 8 .. 15 of the first
+    b.table[1, 0] = -1
+    b.lengths[2] = 40                                            # of 5 pages' 40 places the table has all; rows at 36 .. 39 there
+    b.table = b.table[:, :4].contiguous()                        # now positions from 32 on are behind the table
+    b.lengths[0] = 4                                             # six rows of a sequence of four: two at -2, -1
+    cache, seqs, buffers = b.on(sb)
+    before = [t.clone() for t in buffers]
+    k = torch.randn(b.tokens, 2, 64).cuda()
+    ctx.kv_store(cache, seqs, k, k)
+    out = torch.full((b.tokens, 2, 64), 9.0, device="cuda")
+    ctx.kv_load(cache, seqs, out, None)
+    assert (out[:2] == 0).all() and (out[6:] == 0).all() and (out[2:6] != 9).all() and (out[2:6] != 0).any()
+    page = int(b.table[0, 0])
+    for t, was in zip(buffers, before):
+        changed = (t != was).flatten(2).any(-1).any(-1).nonzero().flatten().tolist()
+        assert set(changed) <= {page}
+
+
+# ---- attention ---------------------------------------------------------------------------------------
+def check(ctx, b, heads, causal=True, window=0, scale=None, lse=True, pad=0, gone=(), seed=1, queries=None, **hints):
+    q = (torch.randn(b.tokens, heads, b.dim, generator=gen(seed)) * 1.5).to(BF16) if queries is None else queries
+    cache, seqs, _ = b.on(sb, **hints)
+    src, out = spaced(q.shape, BF16, pad), spaced(q.shape, BF16, 2 * pad, heads_first=pad > 0)
+    src.copy_(q)
+    sums = torch.full((b.tokens, heads), 77.0, device="cuda") if lse else None
+    ws = torch.full((ctx.kv_attention_ws_bytes(cache, seqs, b.tokens, heads),), 255, dtype=torch.uint8, device="cuda")
+    ctx.kv_attention(cache, seqs, src, out, ws, scale=scale, causal=causal, window=window, lse=sums)
+    rows = b.rows()
+    got = out.cpu().double()
+    want, want_lse, off, off_lse = kv_plain.attention(b, q, scale, causal, window, gone)
+    nan = torch.isnan(want)
+    assert torch.equal(torch.isnan(got[rows]), nan)
+    assert ((got[rows] - want).abs()[~nan] <= off[~nan]).all(), float(((got[rows] - want).abs() / off.clamp(min=1e-30))[~nan].max())
+    others = torch.ones(b.tokens, dtype=torch.bool)
+    others[rows] = False
+    assert (got[others] == 77).all()
+    if lse:
+        s = sums.cpu().double()
+        none = want_lse == -math.inf
+        assert (s[others] == 77).all() and (s[rows][none] == -math.inf).all()
+        keep = ~none & ~torch.isnan(want_lse)
+        assert ((s[rows] - want_lse).abs()[keep] <= off_lse[keep]).all()
+    again = torch.empty_like(out)
+    ctx.kv_attention(cache, seqs, src, again, ws, scale=scale, causal=causal, window=window)
+    if not nan.any():
+        assert torch.equal(again[rows.cuda()], out[rows.cuda()]) or not lse
+    return out
+
+
+@pytest.mark.parametrize("dim", [32, 64, 96, 128, 160, 192, 224, 256])
+@pytest.mark.parametrize("page,kv_heads,group", [(16, 2, 4), (1, 1, 1), (64, 1, 7), (256, 3, 16)])
+def test_attention_of_single_tokens(ctx, dim, page, kv_heads, group):
+    b = Batch([(1, 0), (1, 1), (1, 62), (1, 63), (1, 64), (0, 70), (1, 200), (1, 400)], page, kv_heads, dim, seed=dim + page, lead=1, behind=3)
+    check(ctx, b, kv_heads * group, pad=8, max_new=1, max_length=401)
+
+
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 50), (True, 64), (True, 1000)])
+@pytest.mark.parametrize("dim,group", [(64, 1), (128, 4), (96, 3), (256, 2)])
+def test_attention_of_chunks(ctx, causal, window, dim, group):
+    b = Batch([(5, 0), (70, 0), (1, 130), (33, 100), (0, 5), (3, 61), (64, 64)], 16, 2, dim, seed=dim + window, lead=2, behind=1)
+    check(ctx, b, 2 * group, causal, window, pad=8)
+    check(ctx, b, 2 * group, causal, window, max_new=70, max_length=200, lse=False)
+
+
+@pytest.mark.parametrize("sizes,group", [([(300, 0)], 4), ([(129, 700)], 1), ([(257, 64)], 8), ([(1, 5000)], 5), ([(17, 3000), (1, 9)], 16)])
+def test_attention_of_long_sequences(ctx, sizes, group):
+    b = Batch(sizes, 64, 1, 128, seed=7)
+    check(ctx, b, group)
+    check(ctx, b, group, max_new=max(n for n, _ in sizes), max_length=max(n + p for n, p in sizes))
+
+
+def test_attention_with_wrong_hints(ctx):
+    """Hints that are too small only choose a slower way."""
+    b = Batch([(40, 0), (3, 300), (90, 20)], 16, 2, 64, seed=3)
+    for hints in (dict(max_new=1), dict(max_new=1, max_length=1), dict(max_new=1000, max_length=5), dict(max_length=1 << 30)):
+        check(ctx, b, 8, **hints)
+
+
+@pytest.mark.parametrize("heads", [1, 71])
+def test_attention_with_one_key_head(ctx, heads):
+    check(ctx, Batch([(1, 99), (9, 40), (65, 0)], 32, 1, 64, seed=5), heads)
+
+
+@pytest.mark.parametrize("scale", [1e-6, 0.5, 3.0])
+def test_attention_scales(ctx, scale):
+    check(ctx, Batch([(1, 300), (70, 3)], 16, 1, 64, seed=9, spread=1), 2, scale=scale)
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_attention_pages_that_are_not_there(ctx, new):
+    b = Batch([(new, 150), (new, 40)], 16, 1, 64, seed=4)
+    other = Batch([(new, 150), (new, 40)], 16, 1, 64, seed=4)
+    other.table[0, 2], other.table[0, 3], other.table[1, 0] = -5, other.pages, 1 << 30
+    other.codes, other.scales = b.codes, b.scales
+    gone = ((0, 2), (0, 3), (1, 0))
+    q = torch.randn(b.tokens, 4, 64, generator=gen(2)).to(BF16)
+    want, want_lse, off, _ = kv_plain.attention(b, q, gone=gone)
+    cache, seqs, _ = other.on(sb)
+    out = torch.zeros(q.shape, dtype=BF16, device="cuda")
+    ws = torch.empty(ctx.kv_attention_ws_bytes(cache, seqs, b.tokens, 4), dtype=torch.uint8, device="cuda")
+    ctx.kv_attention(cache, seqs, q.cuda(), out, ws)
+    assert ((out.cpu().double() - want).abs() <= off).all()
+    other.table[:] = -1                                          # no key at all: zeros
+    cache, seqs, _ = other.on(sb)
+    sums = torch.zeros(b.tokens, 4, device="cuda")
+    ctx.kv_attention(cache, seqs, q.cuda(), out, ws, lse=sums)
+    assert (out == 0).all() and (sums == -math.inf).all()
+
+
+@pytest.mark.parametrize("sizes", [[(1, 100)], [(40, 30)], [(130, 40)]])
+def test_attention_only_what_is_seen_counts(ctx, sizes):
+    """Blocks that are not finite: behind a row's position, or ahead of its window, they change nothing; seen, they make NaN."""
+    (n, p), = sizes
+    b = Batch(sizes, 16, 1, 128, seed=6)
+    page, at = b.places(0, 0, n + p)
+    def spoil(which, position, block, byte=255):
+        b.scales[which][page[position], 0, at[position], block] = byte
+    spoil(1, 5, 2)
+    spoil(1, n + p - 1, 1, 254)
+    spoil(1, p + n // 2, 3)
+    check(ctx, b, 4)
+    check(ctx, b, 4, window=10)
+    check(ctx, b, 4, max_new=n)
+    spoil(0, n + p - 1, 0)                                       # a key: only the last row sees it
+    spoil(0, 2, 3)                                               # and one that only rows without a window see
+    check(ctx, b, 4, window=12)
+    q = torch.randn(b.tokens, 4, 128, generator=gen(8)).to(BF16)
+    q[0, 2, 77], q[n - 1, 1, 3] = math.nan, math.inf
+    clean = Batch(sizes, 16, 1, 128, seed=6)
+    want, _, off, _ = kv_plain.attention(clean, q.nan_to_num(nan=0.0, posinf=0.0))
+    want[0, 2], want[n - 1, 1] = math.nan, math.nan
+    cache, seqs, _ = clean.on(sb)
+    out = torch.zeros(q.shape, dtype=BF16, device="cuda")
+    ws = torch.empty(ctx.kv_attention_ws_bytes(cache, seqs, b.tokens, 4), dtype=torch.uint8, device="cuda")
+    ctx.kv_attention(cache, seqs, q.cuda(), out, ws)
+    got = out.cpu().double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert ((got - want).abs() <= off)[~torch.isnan(want)].all()
+
+
+def test_attention_sequences_that_share_pages(ctx):
+    """A prompt's pages in two sequences, which go on in pages of their own."""
+    b = Batch([(1, 39), (1, 39)], 8, 2, 64, seed=2)
+    b.table[1, :4] = b.table[0, :4]
+    check(ctx, b, 4)
+
+
+@pytest.mark.parametrize("spread", [9, 5])
+def test_attention_large_scores(ctx, spread):
+    """Scores far apart and far from 0: the largest is taken out, before powers are taken."""
+    b = Batch([(1, 500), (70, 90)], 32, 1, 64, seed=12, spread=spread)
+    q = (torch.randn(b.tokens, 2, 64, generator=gen(1)) * 2.0 ** torch.randint(-20, 6, (b.tokens, 2, 64), generator=gen(2))).to(BF16)
+    check(ctx, b, 2, queries=q)
+
+
+# ---- together ----------------------------------------------------------------------------------------
+def test_a_prompt_and_steps_behind_it_captured(ctx):
+    """As a program uses them: a prompt stored and attended, then steps in a graph that is replayed with new lengths, each against the eager calls."""
+    kv_heads, heads, dim, page, most = 2, 8, 128, 16, 12
+    side = torch.cuda.Stream()
+    own = sb.Context(0, side.cuda_stream)
+    table = torch.randperm(40)[:2 * most].view(2, most).int().cuda()
+    shape = (40, kv_heads, page)
+    def buffers():
+        return [torch.zeros(*shape, n, dtype=torch.uint8, device="cuda") for n in (64, 4, 64, 4)]
+    r = rotary_of(kv_plain.turns(dim))
+    eager, graphed = buffers(), buffers()
+    def state(tokens):
+        return [torch.empty(tokens, h, dim, dtype=BF16, device="cuda") for h in (heads, kv_heads, kv_heads, heads, heads)]
+    def step(c, cache, seqs, q, k, v, turned, out, ws):
+        c.kv_store(cache, seqs, k, v, rotary=r, q=q, q_out=turned)
+        c.kv_attention(cache, seqs, turned, out, ws)
+    prompt = [50, 3]
+    starts, lengths = torch.tensor([0, 50, 53], dtype=torch.int32, device="cuda"), torch.tensor(prompt, dtype=torch.int32, device="cuda")
+    tensors = state(53)
+    for i in range(3):
+        tensors[i].copy_(torch.randn(tensors[i].shape, generator=gen(i)))
+    for buf in (eager, graphed):
+        cache, seqs = sb.kv_cache(*buf, dim), sb.sequences(starts, lengths, table)
+        ws = torch.empty(ctx.kv_attention_ws_bytes(cache, seqs, 53, heads), dtype=torch.uint8, device="cuda")
+        step(ctx, cache, seqs, *tensors, ws)
+    assert torch.equal(eager[0], graphed[0])
+    # the prompt's attention against what the cache says
+    b = Batch([(50, 0), (3, 0)], page, kv_heads, dim)
+    b.table, b.pages = table.cpu(), 40
+    b.codes, b.scales = [eager[0].cpu(), eager[2].cpu()], [eager[1].cpu(), eager[3].cpu()]
+    want, _, off, _ = kv_plain.attention(b, tensors[3].cpu())
+    assert ((tensors[4].cpu().double() - want).abs() <= off).all()
+    starts = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    mine = state(2)
+    cache, seqs = sb.kv_cache(*graphed, dim), sb.sequences(starts, lengths, table, max_new=1)
+    ws = torch.empty(max(1, own.kv_attention_ws_bytes(cache, seqs, 2, heads)), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    kept = [t.clone() for t in graphed]
+    lengths.add_(1)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        step(own, cache, seqs, *mine, ws)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step(own, cache, seqs, *mine, ws)
+    for t, k in zip(graphed, kept):
+        t.copy_(k)
+    lengths.sub_(1)
+    other = sb.kv_cache(*eager, dim)
+    for turn in range(5):
+        lengths.add_(torch.tensor([1, 1], dtype=torch.int32, device="cuda"))
+        for i in range(3):
+            mine[i].copy_(torch.randn(mine[i].shape, generator=gen(100 + 10 * turn + i)))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, turned = mine[4].clone(), mine[3].clone()
+        step(ctx, other, seqs, *mine, torch.empty_like(ws))
+        torch.cuda.synchronize()
+        assert torch.equal(got, mine[4]) and torch.equal(turned, mine[3])
+        assert all(torch.equal(a, b) for a, b in zip(eager, graphed))
+    own.close()
