@@ -162,12 +162,14 @@ int sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_seque
 size_t sbits_kv_attention_ws_bytes(const sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens, int heads)
 {
     if (!ctx || check_cache(cache) || check_sequences(sequences) || !tokens_ok(tokens) || heads < 1 || heads > KV_MAX_QUERY_HEADS || heads % cache->kv_heads) return 0;
-    return 0;
+    if (tokens == 0 || sequences->count == 0) return 0;
+    AttentionArgs a;
+    return sbits_kv_attention_cut(ctx, *cache, *sequences, tokens, heads, a);
 }
 
 int sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens, int heads, const void *q_bf16,
                        int64_t ld_q, int64_t hd_q, float scale, int causal, int window, void *out_bf16, int64_t ld_out, int64_t hd_out, float *lse,
-                       void * /*ws*/, size_t /*ws_bytes*/)
+                       void *ws, size_t ws_bytes)
 {
     if (!ctx || !tokens_ok(tokens) || (causal & ~1) || window < 0 || (window && !causal) || !(scale > 0.0f) || !isfinite(scale)) return SBITS_ERR_INVALID_ARG;
     int rc;
@@ -176,15 +178,18 @@ int sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_
     if (tokens == 0 || sequences->count == 0) return SBITS_OK;
     if (!heads_ok(q_bf16, ld_q, hd_q, SBITS_TYPE_BF16, 0) || !heads_ok(out_bf16, ld_out, hd_out, SBITS_TYPE_BF16, cache->head_dim) || (lse && !aligned(lse, 4)))
         return SBITS_ERR_INVALID_ARG;
-    if ((rc = need_device(ctx))) return rc;
     AttentionArgs a;
+    const size_t need = sbits_kv_attention_cut(ctx, *cache, *sequences, tokens, heads, a);
+    if (need && (!aligned(ws, 256) || ws_bytes < need)) return SBITS_ERR_WORKSPACE;
+    if ((rc = need_device(ctx))) return rc;
     a.cache = pages_of(*cache);
     a.sequences = sequences_of(*sequences);
     a.q = {q_bf16, ld_q, hd_q}; a.out = {out_bf16, ld_out, hd_out};
     a.lse = lse;
     a.tokens = tokens;
     a.heads = heads; a.group = heads / cache->kv_heads;
-    a.scale = scale; a.causal = causal; a.window = window;
+    a.scale = (float)(scale * 1.4426950408889634); a.causal = causal; a.window = window;
+    a.part = static_cast<float *>(ws);
     return sbits_launch_kv_attention(ctx, a);
 }
 

@@ -140,11 +140,17 @@ struct AttentionArgs {
     float *lse;
     int64_t tokens;
     int heads, group;                        // of queries; to a key's
-    float scale;
+    float scale;                             // of scores as powers of two: scale * log2(e)
     int causal, window;
+    // few rows: tiles of 16 rows of a sequence that have workgroups of their own, parts of its keys, rows of a sequence from which on it is not this kernel's
+    int tiles, splits;
+    int64_t most_rows;
+    float *part;                             // [sequence][tile][kv_head][part][16][dim], then the same of pairs (largest score, sum)
+    int64_t first;                           // workgroups ahead of this launch
 };
+constexpr int64_t KV_LAUNCH = (int64_t)1 << 22;      // workgroups of a launch
 
-// the keys that a row sees: positions first .. last - 1
+// the keys that a row at a position sees: first .. last - 1
 __device__ __forceinline__ void seen_keys(const AttentionArgs &a, int64_t length, int64_t position, int64_t &first, int64_t &last)
 {
     const int64_t there = (int64_t)a.sequences.max_pages << a.cache.shift;
@@ -161,4 +167,6 @@ __device__ __forceinline__ void seen_keys(const AttentionArgs &a, int64_t length
 int sbits_launch_rotate(sbits_ctx *ctx, const sbits::RotateArgs &a, bool bf16, bool wide);
 int sbits_launch_kv_store(sbits_ctx *ctx, const sbits::StoreArgs &a, bool bf16);
 int sbits_launch_kv_load(sbits_ctx *ctx, const sbits::LoadArgs &a, bool bf16);
-int sbits_launch_kv_attention(sbits_ctx *ctx, const sbits::AttentionArgs &a);
+// how an attention is cut up: tiles, splits, most_rows; the workspace of its parts in bytes
+size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache, const sbits_sequences &sequences, int64_t tokens, int heads, sbits::AttentionArgs &a);
+int sbits_launch_kv_attention(sbits_ctx *ctx, sbits::AttentionArgs &a);
