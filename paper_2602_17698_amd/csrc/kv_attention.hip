@@ -6,13 +6,7 @@
 
 namespace sbits {
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x6 __attribute__((ext_vector_type(6)));
-typedef float f32x32 __attribute__((ext_vector_type(32)));
-
-constexpr int FEW_ROWS = 16, FEW_KEYS = 64, FEW_WAVES = 4, FEW_LEAST = 8;     // FEW_LEAST: tiles of keys of a part, at least
-constexpr int Q_TERMS = 4;
-constexpr float LN2F = 0x1.62e43p-1f;
+constexpr int FEW_WAVES = 4;
 
 // largest or sum over the lanes with the same lane % 16
 template <class Op>
@@ -22,71 +16,9 @@ __device__ __forceinline__ float across_rows(float v, Op op)
     return op_halves(v, op, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
 }
 
-// A block of 32 values of q as Q_TERMS blocks of 6-bit codes (E2M3) whose powers of two are 4, 6 and 6 steps apart.  The matrix instruction multiplies 4-bit by 6-bit
-// codes at twice the rate of bf16 and without a conversion of k.  A code has 4 bits, bf16 8: what the first term leaves of elements down to 1/4
-// of the block's largest is exact in the second, of those down to 2^-8 of it in the third, of those down to 2^-14 in the fourth; of smaller ones less than 2^-18
-// of the largest is left out.
-struct QBlock { u32x6 codes[Q_TERMS]; int scale; };                           // scale: the first term's byte
-constexpr int Q_STEP[4] = {0, 4, 10, 16};
-__device__ __forceinline__ QBlock split_q(const float (&x)[32])
-{
-    f32x16 a, b;
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        a[i] = x[2 * i];
-        b[i] = x[2 * i + 1];
-        top = max(top, __float_as_uint(b[i]) & 0x7fffffffu);
-        top = max(top, __float_as_uint(a[i]) & 0x7fffffffu);
-    }
-    QBlock q;
-    q.scale = max((int)(top >> 23) - 2, 17);
-#pragma unroll
-    for (int t = 0; t < Q_TERMS; ++t) {
-        const float scale = __uint_as_float((uint32_t)(q.scale - Q_STEP[t]) << 23);
-        q.codes[t] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(a, b, scale);
-        const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q.codes[t], scale);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            a[i] -= back[2 * i];
-            b[i] -= back[2 * i + 1];
-        }
-    }
-    return q;
-}
-
-// ---- few rows of a sequence ------------------------------------------------------------
-// How a tile of rows goes over a sequence's keys.
-struct FewPlan {
-    int64_t start, end, rows;                 // the sequence's rows; times heads of a key's head
-    int64_t tiles;                            // of rows, in all
-    int64_t first, last, keys;                // keys of this tile of rows, from a multiple of 64 on; tiles of them
-    int64_t each;                             // of a part
-    int parts;
-};
-__device__ __forceinline__ bool few_plan(const AttentionArgs &a, int sequence, int64_t tile, FewPlan &p)
-{
-    const int start = a.sequences.starts[sequence], end = a.sequences.starts[sequence + 1];
-    p.start = start > 0 ? start : 0;
-    p.end = end < a.tokens ? end : a.tokens;
-    p.rows = (p.end - p.start) * a.group;
-    p.tiles = (p.rows + FEW_ROWS - 1) / FEW_ROWS;
-    if (tile >= p.tiles || p.rows > a.most_rows) return false;
-    const int64_t length = a.sequences.lengths[sequence], r0 = tile * FEW_ROWS, r1 = std::min(r0 + FEW_ROWS, p.rows) - 1;
-    int64_t none;
-    seen_keys(a, length, length - end + p.start + r0 / a.group, p.first, none);
-    seen_keys(a, length, length - end + p.start + r1 / a.group, none, p.last);
-    p.first &= ~(int64_t)(FEW_KEYS - 1);
-    p.keys = p.last > p.first ? (p.last - p.first + FEW_KEYS - 1) / FEW_KEYS : 0;
-    const int most = p.tiles <= a.tiles ? a.splits : 1;
-    p.each = std::max<int64_t>((p.keys + most - 1) / most, FEW_LEAST);
-    p.parts = (int)std::max<int64_t>((p.keys + p.each - 1) / p.each, 1);
-    return true;
-}
-
 // A workgroup has 16 rows (tokens times the heads of a key's head) and a part of their keys, of which its four waves take 64 in turn, each by itself.
 // Scores, transposed:  k's codes go to the matrix instruction as they lie in the cache, a lane a block of 32, with q in 6-bit terms.  Lane l then has row l % 16 and the keys 16 b + 4 (l / 16) + r.
-// Sums, transposed:  v becomes bf16 (exactly) on its way to LDS, whose transposing reads give a lane one element of 8 keys; weights, in two bf16 terms, are already
+// Sums, transposed:  v becomes fp16 or bf16 (exactly) on its way to LDS, whose transposing reads give a lane one element of 8 keys; weights are already
 // where the instruction wants them, if its keys come in the order 16 (j / 4) + 4 (l / 16) + j % 4.
 // Pages' numbers are asked for two tiles of keys ahead, codes one.
 template <int DB>
@@ -96,17 +28,17 @@ template <int DB>
 __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(AttentionArgs a)
 {
     constexpr int D = 32 * DB, KS = (DB + 3) / 4, PITCH = 2 * D + 32;          // PITCH: rows 8 banks apart, mod 64 an odd multiple of 8
-    __shared__ __attribute__((aligned(16))) unsigned char smem[FEW_WAVES][FEW_KEYS * PITCH];
+    __shared__ __attribute__((aligned(16))) unsigned char smem[FEW_WAVES][KV_TILE * PITCH];
     __shared__ float2 red[FEW_WAVES][FEW_ROWS];
     const int64_t item = a.first + blockIdx.x;
-    const int split = (int)(item % a.splits), kv_head = (int)(item / a.splits % a.cache.kv_heads);
-    const int64_t place = item / a.splits / a.cache.kv_heads;                  // [sequence][tile]
-    const int sequence = (int)(place / a.tiles);
+    const int split = (int)(item % a.few.splits), kv_head = (int)(item / a.few.splits % a.cache.kv_heads);
+    const int64_t place = item / a.few.splits / a.cache.kv_heads;                  // [sequence][tile]
+    const int sequence = (int)(place / a.few.tiles);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const u32x4 zero = {0, 0, 0, 0};
-    for (int64_t tile = place % a.tiles;; tile += a.tiles) {
-        FewPlan p;
-        if (!few_plan(a, sequence, tile, p) || split >= p.parts) return;
+    for (int64_t tile = place % a.few.tiles;; tile += a.few.tiles) {
+        TilePlan p;
+        if (!tile_plan<FEW_ROWS>(a, a.few, sequence, tile, p) || split >= p.parts) return;
         const int64_t length = a.sequences.lengths[sequence], end = a.sequences.starts[sequence + 1];
         // this lane's row
         const int64_t r = tile * FEW_ROWS + n;
@@ -116,38 +48,24 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
         int64_t lo, hi;
         seen_keys(a, length, length - end + token, lo, hi);
         if (!there) lo = p.first, hi = p.last;                                 // (its sums go nowhere)
-        QBlock q[KS];
+        QBlock<4> q[KS];
         bool fine = true;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            float x[32];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (4 * s + g < DB && there) load8<true>(a.q.at, token * a.q.ld + head * a.q.hd + 32 * (4 * s + g) + 8 * i, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool ok = (__float_as_uint(v[e]) & 0x7f800000u) != 0x7f800000u;
-                    fine = fine && ok;
-                    x[8 * i + e] = ok ? v[e] : 0.0f;
-                }
-            }
-            q[s] = split_q(x);
-        }
+        for (int s = 0; s < KS; ++s) q[s] = load_q<4>(a, there && 4 * s + g < DB, token, head, 4 * s + g, fine);
         const uint64_t broken = __builtin_amdgcn_ballot_w64(!fine);
         const float scale = ((broken | broken >> 16 | broken >> 32 | broken >> 48) >> n & 1) ? NAN : a.scale;
 
         const int64_t tile0 = split * p.each, tile1 = std::min(tile0 + p.each, p.keys);
         const int32_t *const table = a.sequences.pages + sequence * a.sequences.ld_pages;
         auto page_at = [&](int64_t t) {                                        // of this lane's key of a tile
-            const int64_t key = p.first + t * FEW_KEYS + lane;
+            const int64_t key = p.first + t * KV_TILE + lane;
             if (t >= tile1 || key >= p.last) return -1;
             const int page = table[key >> a.cache.shift];
             return (uint32_t)page < (uint64_t)a.cache.pages ? page : -1;
         };
         FewTile<DB> now, next;
         auto fetch = [&](FewTile<DB> &f, int64_t t, int pages) {               // (keys that are not there: of page 0)
-            const int key0 = (int)((p.first + t * FEW_KEYS) & a.cache.mask);   // place in a page of the tile's first key, if a page has them all
+            const int key0 = (int)((p.first + t * KV_TILE) & a.cache.mask);   // place in a page of the tile's first key, if a page has them all
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int page = max(__shfl(pages, 16 * b + n), 0);
@@ -183,7 +101,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
         for (int64_t t = tile0 + wave; t < tile1; t += FEW_WAVES) {
             const int pages_ahead = page_at(t + 2 * FEW_WAVES);
             if (t + FEW_WAVES < tile1) fetch(next, t + FEW_WAVES, pages_next);
-            const int64_t key0 = p.first + t * FEW_KEYS;
+            const int64_t key0 = p.first + t * KV_TILE;
             const uint64_t valid = __builtin_amdgcn_ballot_w64(pages >= 0);
             // scores
             f32x4 s[4];
@@ -191,7 +109,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
             for (int b = 0; b < 4; ++b) {
                 s[b] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int term = Q_TERMS - 1; term >= 0; --term)
+                for (int term = 4 - 1; term >= 0; --term)
 #pragma unroll
                     for (int k = 0; k < KS; ++k) {
                         const u32x4 c = now.k[b][k];
@@ -201,23 +119,38 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                     }
             }
             // v to LDS
+            bool usual = true;                                                 // all in fp16
 #pragma unroll
             for (int i = 0; i < DB; ++i) {
-                const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
-                const bool ok = valid >> key & 1;
-                const bool bad = ok && now.vs[i] >= KV_V_LIMIT;
-                uint64_t bads = __builtin_amdgcn_ballot_w64(bad);
-                while (bads) {                                                 // (rare)
-                    const int at = __builtin_ctzll(bads), bad_piece = 64 * i + at;
-                    bads &= bads - 1;
-                    const int64_t where = key0 + bad_piece / DB;
-                    if (where >= lo && where < hi) spoiled |= 1u << bad_piece % DB;
-                }
-                const u32x4 codes = ok && !bad ? now.v[i] : zero;
-                const float sc = __uint_as_float((uint32_t)(ok && !bad ? now.vs[i] : 127) << 23);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) *reinterpret_cast<u32x4 *>(lds + key * PITCH + 64 * block + 16 * w) = mx_values8(codes[w], sc);
+                const int key = (64 * i + lane) / DB;
+                usual = usual && (!(valid >> key & 1) || (now.vs[i] >= F16_LOW && now.vs[i] <= F16_HIGH));
             }
+            const bool halves = __builtin_amdgcn_ballot_w64(!usual) == 0;
+            auto put = [&](auto f16) {
+#pragma unroll
+                for (int i = 0; i < DB; ++i) {
+                    const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
+                    bool ok = valid >> key & 1;
+                    if constexpr (!decltype(f16)::value) {
+                        const bool bad = ok && now.vs[i] >= KV_V_LIMIT;
+                        uint64_t bads = __builtin_amdgcn_ballot_w64(bad);
+                        while (bads) {
+                            const int bad_piece = 64 * i + __builtin_ctzll(bads);
+                            bads &= bads - 1;
+                            const int64_t where = key0 + bad_piece / DB;
+                            if (where >= lo && where < hi) spoiled |= 1u << bad_piece % DB;
+                        }
+                        ok = ok && !bad;
+                    }
+                    const u32x4 codes = ok ? now.v[i] : zero;
+                    const float sc = __uint_as_float((uint32_t)(ok ? now.vs[i] : 127) << 23);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+                        *reinterpret_cast<u32x4 *>(lds + key * PITCH + 64 * block + 16 * w) = decltype(f16)::value ? mx_halves8(codes[w], sc) : mx_values8(codes[w], sc);
+                }
+            };
+            if (halves) put(std::true_type{});
+            else put(std::false_type{});
             // weights
             float most = -INFINITY;
 #pragma unroll
@@ -238,32 +171,37 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                 for (int i = 0; i < 2 * DB; ++i) acc[i] *= shrink;
                 top = most;
             }
-            const float base = top == -INFINITY ? 0.0f : top;
-            bf16x8 high[2], low[2];
+            const float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT;
+            float w[2][8];
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(s[b][i] - base);
-                    sum += w;
-                    const __bf16 h = (__bf16)w;
-                    high[b / 2][b % 2 * 4 + i] = h;
-                    low[b / 2][b % 2 * 4 + i] = (__bf16)(w - (float)h);
+                    const float one = __builtin_amdgcn_exp2f(s[b][i] - base);
+                    sum += one;
+                    w[b / 2][b % 2 * 4 + i] = one;
                 }
             __builtin_amdgcn_wave_barrier();
             // sums
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int half = 0; half < 2; ++half) {
+                const unsigned char *const at = lds + (32 * half + 4 * g + n / 4) * PITCH + 8 * (n % 4);
+                if (halves) {
+                    const f16x8 p16 = weights_f16(w[half]);
 #pragma unroll
-                for (int d = 0; d < 2 * DB; ++d) {
-                    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                    typedef __attribute__((address_space(3))) unsigned char lds_u8;
-                    lds_u8 *const at = (lds_u8 *)lds + (32 * half + 4 * g + n / 4) * PITCH + 32 * d + 8 * (n % 4);
-                    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at), v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 16 * PITCH));
-                    const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, low[half], acc[d], 0, 0, 0);
-                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high[half], acc[d], 0, 0, 0);
+                    for (int d = 0; d < 2 * DB; ++d)
+                        acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, read_transposed(at + 32 * d, 16 * PITCH)), p16, acc[d], 0, 0, 0);
+                } else {
+                    bf16x8 high, low;
+                    weights_bf16(w[half], high, low);
+#pragma unroll
+                    for (int d = 0; d < 2 * DB; ++d) {
+                        const bf16x8 v = __builtin_bit_cast(bf16x8, read_transposed(at + 32 * d, 16 * PITCH));
+                        acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, low, acc[d], 0, 0, 0);
+                        acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high, acc[d], 0, 0, 0);
+                    }
                 }
+            }
             __builtin_amdgcn_wave_barrier();
             now = next;
             pages = pages_next;
@@ -275,7 +213,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
             if (spoiled >> d / 2 & 1) acc[d] = f32x4{NAN, NAN, NAN, NAN};
             *reinterpret_cast<f32x4 *>(lds + (n * (D + 4) + 16 * d + 4 * g) * 4) = acc[d];
         }
-        if (g == 0) red[wave][n] = make_float2(top, sum);
+        if (g == 0) red[wave][n] = make_float2(top - WEIGHT_LIFT, sum);
         __syncthreads();
         // the waves' sums: 8 elements of a row a thread
         for (int unit = tid; unit < 4 * DB * FEW_ROWS; unit += 64 * FEW_WAVES) {
@@ -295,11 +233,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
             const int64_t mine = tile * FEW_ROWS + row;
             if (mine >= p.rows) continue;
             if (p.parts > 1) {
-                const int64_t slot = ((place * a.cache.kv_heads + kv_head) * a.splits + split) * FEW_ROWS + row;
-                store8<false>(a.part, slot * D + at, y);
+                const int64_t slot = ((place * a.cache.kv_heads + kv_head) * a.few.splits + split) * FEW_ROWS + row;
+                store8<false>(a.few.part, slot * D + at, y);
                 if (at == 0) {
-                    const int64_t all = (int64_t)a.sequences.count * a.tiles * a.cache.kv_heads * a.splits * FEW_ROWS;
-                    reinterpret_cast<float2 *>(a.part + all * D)[slot] = make_float2(m, l);
+                    const int64_t all = (int64_t)a.sequences.count * a.few.tiles * a.cache.kv_heads * a.few.splits * FEW_ROWS;
+                    reinterpret_cast<float2 *>(a.few.part + all * D)[slot] = make_float2(m, l);
                 }
                 continue;
             }
@@ -309,36 +247,39 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] *= over;
             store8<true>(const_cast<void *>(a.out.at), to * a.out.ld + h * a.out.hd + at, y);
-            if (a.lse && at == 0) a.lse[to * a.heads + h] = (m + __builtin_amdgcn_logf(l)) * LN2F;
+            if (a.lse && at == 0) a.lse[to * a.heads + h] = log_sum(m, l);
         }
         __syncthreads();
     }
 }
 
-// The parts of a tile of rows: a thread has 8 elements of a row.
-template <int DB>
+// The parts of 16 rows of a tile: a thread has 8 elements of a row.
+template <int DB, int ROWS>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
 {
     constexpr int D = 32 * DB;
-    const int64_t item = a.first + blockIdx.x, place = item / a.cache.kv_heads;
-    const int kv_head = (int)(item % a.cache.kv_heads), sequence = (int)(place / a.tiles);
-    const int64_t tile = place % a.tiles;
-    FewPlan p;
-    if (!few_plan(a, sequence, tile, p) || p.parts == 1) return;
-    const float2 *const pairs = reinterpret_cast<const float2 *>(a.part + (int64_t)a.sequences.count * a.tiles * a.cache.kv_heads * a.splits * FEW_ROWS * D);
-    for (int unit = threadIdx.x; unit < 4 * DB * FEW_ROWS; unit += 256) {
-        const int row = unit / (4 * DB), at = unit % (4 * DB) * 8;
-        const int64_t mine = tile * FEW_ROWS + row, slot = item * a.splits * FEW_ROWS + row;
+    const AttentionCut &cut = ROWS == FEW_ROWS ? a.few : a.many;
+    const int64_t number = a.first + blockIdx.x, item = number / (ROWS / 16), place = item / a.cache.kv_heads;
+    const int kv_head = (int)(item % a.cache.kv_heads), row0 = (int)(number % (ROWS / 16)) * 16;
+    int sequence = (int)(place / cut.tiles);
+    int64_t tile = place % cut.tiles, items = (int64_t)a.sequences.count * cut.tiles;
+    if (ROWS == MANY_ROWS) sequence = find_tile(a, place, tile), items = cut.tiles;
+    TilePlan p;
+    if (sequence < 0 || !tile_plan<ROWS>(a, cut, sequence, tile, p) || p.parts == 1) return;
+    const float2 *const pairs = reinterpret_cast<const float2 *>(cut.part + items * a.cache.kv_heads * cut.splits * ROWS * D);
+    for (int unit = threadIdx.x; unit < 4 * DB * 16; unit += 256) {
+        const int row = row0 + unit / (4 * DB), at = unit % (4 * DB) * 8;
+        const int64_t mine = tile * ROWS + row, slot = item * cut.splits * ROWS + row;
         if (mine >= p.rows) continue;
         float m = -INFINITY, l = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int s = 0; s < p.parts; ++s) m = fmaxf(m, pairs[slot + s * FEW_ROWS].x);
+        for (int s = 0; s < p.parts; ++s) m = fmaxf(m, pairs[slot + s * ROWS].x);
         const float base = m == -INFINITY ? 0.0f : m;
         for (int s = 0; s < p.parts; ++s) {
-            const float2 one = pairs[slot + s * FEW_ROWS];
+            const float2 one = pairs[slot + s * ROWS];
             const float f = __builtin_amdgcn_exp2f(one.x - base);
             l = fmaf(one.y, f, l);
             float o[8];
-            load8<false>(a.part, (slot + s * FEW_ROWS) * D + at, o);
+            load8<false>(cut.part, (slot + s * ROWS) * D + at, o);
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = fmaf(o[e], f, y[e]);
         }
@@ -348,11 +289,15 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] *= over;
         store8<true>(const_cast<void *>(a.out.at), to * a.out.ld + h * a.out.hd + at, y);
-        if (a.lse && at == 0) a.lse[to * a.heads + h] = (m + __builtin_amdgcn_logf(l)) * LN2F;
+        if (a.lse && at == 0) a.lse[to * a.heads + h] = log_sum(m, l);
     }
 }
 
 }  // namespace sbits
+
+// Which kernel takes which sequence: of several, those of up to FEW_MOST rows (tokens times heads of a key's head) go to the kernel of few rows, the others to that of many.
+// Hints of the most rows spare one of the two launches; each kernel is right for any number.
+constexpr int64_t FEW_MOST = 64;
 
 size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache, const sbits_sequences &sequences, int64_t tokens, int heads, sbits::AttentionArgs &a)
 {
@@ -360,30 +305,43 @@ size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache,
     const int64_t group = heads / cache.kv_heads, new_most = sequences.max_new ? std::min<int64_t>(sequences.max_new, tokens) : tokens;
     const int64_t there = std::min<int64_t>((int64_t)sequences.max_pages * cache.page_tokens, INT32_MAX);
     const int64_t length = sequences.max_length ? std::min<int64_t>(sequences.max_length, there) : there;
-    a.tiles = (int)std::min<int64_t>((new_most * group + FEW_ROWS - 1) / FEW_ROWS, 64);
-    a.most_rows = INT64_MAX;
-    const int64_t items = (int64_t)sequences.count * a.tiles * cache.kv_heads, parts = (length / FEW_KEYS + FEW_LEAST) / FEW_LEAST;
-    const int cus = ctx->cus ? ctx->cus : 256;
-    a.splits = (int)std::max<int64_t>(std::min<int64_t>(parts, 4 * cus / items), 1);
-    return a.splits == 1 ? 0 : (size_t)(items * a.splits) * FEW_ROWS * (cache.head_dim + 2) * 4;
+    const int64_t cus = ctx->cus ? ctx->cus : 256;
+    auto splits = [&](int64_t items, int64_t least, int64_t wanted) {
+        return (int)std::max<int64_t>(std::min<int64_t>((length / KV_TILE + least) / least, wanted / items), 1);
+    };
+    a.few = a.many = {0, 1, 0, INT64_MAX, nullptr};
+    const bool only_few = new_most * group <= FEW_MOST, only_many = !only_few && sequences.count == 1;
+    if (!only_many) {
+        a.few.tiles = (int)((std::min(new_most * group, FEW_MOST) + FEW_ROWS - 1) / FEW_ROWS);
+        a.few.splits = splits((int64_t)sequences.count * a.few.tiles * cache.kv_heads, FEW_LEAST, 4 * cus);
+        if (!only_few) a.few.most_rows = FEW_MOST;
+    }
+    if (!only_few) {
+        const int64_t tiles = tokens * group / MANY_ROWS + sequences.count;
+        a.many.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
+        a.many.splits = splits(tiles * cache.kv_heads, MANY_LEAST, 2 * cus);
+        if (!only_many) a.many.least_rows = FEW_MOST + 1;
+    }
+    return sbits_kv_attention_part(a.few, FEW_ROWS, cache, sequences.count) + sbits_kv_attention_part(a.many, MANY_ROWS, cache, sequences.count);
 }
 
 template <int DB>
 static int launch(sbits_ctx *ctx, sbits::AttentionArgs &a)
 {
     using namespace sbits;
-    const int64_t tiles = (int64_t)a.sequences.count * a.tiles * a.cache.kv_heads;
-    for (a.first = 0; a.first < tiles * a.splits; a.first += KV_LAUNCH) {
-        const dim3 grid((uint32_t)std::min(tiles * a.splits - a.first, KV_LAUNCH));
-        hipLaunchKernelGGL(kv_attention_few_kernel<DB>, grid, dim3(64 * FEW_WAVES), 0, ctx->stream, a);
-        SBITS_HIP(ctx, hipGetLastError());
-    }
-    if (a.splits == 1) return SBITS_OK;
-    for (a.first = 0; a.first < tiles; a.first += KV_LAUNCH) {
-        const dim3 grid((uint32_t)std::min(tiles - a.first, KV_LAUNCH));
-        hipLaunchKernelGGL(kv_attention_join_kernel<DB>, grid, dim3(256), 0, ctx->stream, a);
-        SBITS_HIP(ctx, hipGetLastError());
-    }
+    auto enqueue = [&](auto kernel, int64_t items, int threads) -> int {
+        for (a.first = 0; a.first < items; a.first += KV_LAUNCH) {
+            hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(items - a.first, KV_LAUNCH)), dim3(threads), 0, ctx->stream, a);
+            SBITS_HIP(ctx, hipGetLastError());
+        }
+        return SBITS_OK;
+    };
+    const int64_t few = (int64_t)a.sequences.count * a.few.tiles * a.cache.kv_heads, many = (int64_t)a.many.tiles * a.cache.kv_heads;
+    int rc;
+    if (many && (rc = sbits_launch_kv_attention_many(ctx, a))) return rc;
+    if (few && (rc = enqueue(kv_attention_few_kernel<DB>, few * a.few.splits, 64 * FEW_WAVES))) return rc;
+    if (a.many.splits > 1 && (rc = enqueue(kv_attention_join_kernel<DB, MANY_ROWS>, many * (MANY_ROWS / 16), 256))) return rc;
+    if (a.few.splits > 1 && (rc = enqueue(kv_attention_join_kernel<DB, FEW_ROWS>, few, 256))) return rc;
     return SBITS_OK;
 }
 

@@ -1,0 +1,333 @@
+// Attention of many rows of a sequence to a paged cache in the microscaled 4-bit form (formulas and the kernel of few rows: kv_attention.hip).
+#include <algorithm>
+
+#include "kv_core.hpp"
+
+namespace sbits {
+
+constexpr int MANY_WAVES = 4;
+
+// A workgroup has 128 rows (tokens times the heads of a key's head), a wave 32 of them, and goes over their keys 64 at a time.  A wave brings 16 keys of a tile: k's codes go to
+// LDS as they are, v's as fp16 (or bf16), in one of two buffers while the other is read; codes are asked for a tile ahead of that, pages' numbers two.
+// Scores, transposed: a lane has k's row and block from LDS and its row of q in 6-bit terms, and gets for row lane % 32 the keys 8 (r / 4) + 4 (lane / 32) + r % 4 of 32.
+// Sums, transposed: weights are where the instruction wants them, if 16 keys come in the order 8 (j / 4) + 4 (lane / 32) + j % 4; v's transposing reads bring them so.
+template <int DB>
+struct ManyShared {
+    static constexpr int K_PITCH = 16 * (DB | 1), V_PITCH = 64 * DB + (DB % 2 ? 0 : 64), SCALES = (DB + 3) / 4 * 4;      // pitches: neighbouring rows in other banks
+    unsigned char v[2][KV_TILE * V_PITCH];
+    unsigned char k[2][KV_TILE * K_PITCH];
+    unsigned char ks[2][KV_TILE * SCALES];
+    uint32_t kind[2][MANY_WAVES];                  // of 16 keys: 0 fp16, 1 bf16, 3 some of them not finite
+    unsigned char spoiled[2][KV_TILE];             // blocks of a key that are not finite
+};
+
+template <int DB, int TERMS>
+__global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention_many_kernel(AttentionArgs a)
+{
+    constexpr int D = 32 * DB, KS = (DB + 1) / 2, PIECES = (16 * DB + 63) / 64;
+    using Shared = ManyShared<DB>;
+    constexpr int K_PITCH = Shared::K_PITCH, V_PITCH = Shared::V_PITCH, SCALES = Shared::SCALES;
+    __shared__ __attribute__((aligned(16))) Shared sh;
+    // heads first: neighbouring workgroups, on different dies, have different keys; the last rows of a sequence, which see the most, ahead of the others
+    const int64_t item = a.first + blockIdx.x;
+    const int kv_head = (int)(item % a.cache.kv_heads), split = (int)(item / a.cache.kv_heads % a.many.splits);
+    const int64_t number = a.many.tiles - 1 - item / a.cache.kv_heads / a.many.splits;
+    int64_t tile;
+    const int sequence = find_tile(a, number, tile);
+    TilePlan p;
+    if (sequence < 0 || !tile_plan<MANY_ROWS>(a, a.many, sequence, tile, p) || split >= p.parts) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
+    const u32x4 zero = {0, 0, 0, 0};
+    const int64_t length = a.sequences.lengths[sequence], end = a.sequences.starts[sequence + 1];
+    // this lane's row
+    const int64_t r = tile * MANY_ROWS + 32 * wave + n;
+    const bool there = r < p.rows;
+    const int64_t token = p.start + (there ? r : 0) / a.group;
+    const int head = kv_head * a.group + (int)((there ? r : 0) % a.group);
+    const int64_t key_first = p.first + split * p.each * KV_TILE;              // the part's keys count from here on
+    const int tiles = (int)std::min(p.each, p.keys - split * p.each);
+    int lo, hi;                                                                // keys seen, of the part's
+    {
+        int64_t first, last;
+        seen_keys(a, length, length - end + token, first, last);
+        const int64_t all = (int64_t)tiles * KV_TILE;
+        first -= key_first; last -= key_first;
+        lo = (int)std::min(std::max<int64_t>(first, 0), all);
+        hi = (int)std::min(std::max<int64_t>(last, 0), all);
+        if (!there) lo = hi = 0;
+    }
+    // of the wave's rows that are there: the first key that one sees, that all see; the last ones
+    auto over_wave = [&](int v, auto op) {
+#pragma unroll
+        for (int i = 1; i < 64; i *= 2) v = op(v, __shfl_xor(v, i));
+        return __builtin_amdgcn_readfirstlane(v);
+    };
+    auto smaller = [](int x, int y) { return std::min(x, y); };
+    auto larger = [](int x, int y) { return std::max(x, y); };
+    const int lo_any = over_wave(there ? lo : INT32_MAX, smaller), lo_all = over_wave(lo, larger);
+    const int hi_any = over_wave(hi, larger), hi_all = over_wave(there ? hi : INT32_MAX, smaller);
+
+    QBlock<TERMS> q[KS];
+    bool fine = true;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        q[s] = load_q<TERMS>(a, there && 2 * s + h < DB, token, head, 2 * s + h, fine);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    const uint64_t broken = __builtin_amdgcn_ballot_w64(!fine);
+    const float scale = ((broken | broken >> 32) >> n & 1) ? NAN : a.scale;
+
+    const int32_t *const table = a.sequences.pages + sequence * a.sequences.ld_pages;
+    auto page_at = [&](int t) {                                                // of this lane's key of a tile
+        const int64_t key = key_first + (int64_t)t * KV_TILE + lane;
+        if (t >= tiles || key >= p.last) return -1;
+        const int page = table[key >> a.cache.shift];
+        return (uint32_t)page < (uint64_t)a.cache.pages ? page : -1;
+    };
+    // this wave's share of a tile: 16 keys, 16 DB pieces of k and of v
+    u32x4 kc[PIECES], vc[PIECES];
+    uint32_t vs[PIECES], ks;
+    auto fetch = [&](int t, int pages) {                                       // (keys that are not there: of page 0)
+        const int key0 = (int)((key_first + (int64_t)t * KV_TILE) & a.cache.mask) + 16 * wave;
+        const int64_t base = (int64_t)kv_head << a.cache.shift;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
+            const int page = std::max(__shfl(pages, (16 * wave + key) & 63), 0);         // (of all lanes: a lane that is not there would give 0)
+            if (16 * DB % 64 && key >= 16) continue;
+            const int64_t at = base + ((key0 + key) & a.cache.mask), codes = page * a.cache.ld_codes + at * (16 * DB) + 16 * block;
+            kc[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[0] + codes);
+            vc[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[1] + codes);
+            vs[i] = a.cache.scales[1][page * a.cache.ld_scales + at * SCALES + block];
+        }
+        const int page = std::max(__shfl(pages, 16 * wave + lane % 16), 0);
+        const int64_t at = base + ((key0 + lane % 16) & a.cache.mask);
+        if (lane < 16 * (SCALES / 4)) ks = *reinterpret_cast<const uint32_t *>(a.cache.scales[0] + page * a.cache.ld_scales + at * SCALES + lane / 16 * 4);
+    };
+    auto put = [&](int buffer, uint64_t valid) {
+        const uint32_t mine = (uint32_t)(valid >> 16 * wave) & 0xffffu;
+        bool usual = true;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
+            if (16 * DB % 64 && key >= 16) continue;
+            *reinterpret_cast<u32x4 *>(sh.k[buffer] + (16 * wave + key) * K_PITCH + 16 * block) = kc[i];
+            if (!(mine >> key & 1)) vc[i] = zero, vs[i] = 127;
+            usual = usual && vs[i] >= F16_LOW && vs[i] <= F16_HIGH;
+        }
+        if (lane < 16 * (SCALES / 4)) *reinterpret_cast<uint32_t *>(sh.ks[buffer] + (16 * wave + lane % 16) * SCALES + lane / 16 * 4) = ks;
+        const bool halves = __builtin_amdgcn_ballot_w64(!usual) == 0;
+        auto write = [&](auto f16) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
+                if (16 * DB % 64 && key >= 16) continue;
+                const float sc = __uint_as_float(vs[i] << 23);
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    *reinterpret_cast<u32x4 *>(sh.v[buffer] + (16 * wave + key) * V_PITCH + 64 * block + 16 * w) = decltype(f16)::value ? mx_halves8(vc[i][w], sc) : mx_values8(vc[i][w], sc);
+            }
+        };
+        uint32_t kind = 0;
+        if (halves) {
+            write(std::true_type{});
+        } else {
+            kind = 1;
+            uint64_t bad[PIECES];
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const bool is = (64 * i + lane) / DB < 16 && vs[i] >= KV_V_LIMIT;
+                bad[i] = __builtin_amdgcn_ballot_w64(is);
+                if (bad[i]) kind = 3;
+                if (is) vc[i] = zero, vs[i] = 127;
+            }
+            if (kind == 3 && lane < 16) {
+                uint32_t blocks = 0;
+                for (int b = 0; b < DB; ++b) {
+                    const int piece = lane * DB + b;
+                    uint64_t from = bad[0];
+                    if (PIECES > 1 && piece >= 64) from = bad[PIECES - 1];
+                    blocks |= (uint32_t)(from >> piece % 64 & 1) << b;
+                }
+                sh.spoiled[buffer][16 * wave + lane] = (unsigned char)blocks;
+            }
+            write(std::false_type{});
+        }
+        if (lane == 0) sh.kind[buffer][wave] = kind;
+    };
+
+    f32x16 acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
+    float top = -INFINITY, sum = 0.0f;
+    uint32_t spoiled = 0;
+    // one tile of keys; special: not all seen by all rows, or v not all in fp16
+    auto take = [&](auto special_, int buffer, int key0, uint64_t valid) {
+        constexpr bool SPECIAL = decltype(special_)::value;
+        f32x16 s[2];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[m][i] = 0.0f;
+            u32x4 c[KS];
+            int sc[KS];
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int block = 2 * k + h;
+                c[k] = zero;
+                sc[k] = 127;
+                if (DB % 2 == 0 || block < DB) {
+                    c[k] = *reinterpret_cast<const u32x4 *>(sh.k[buffer] + (32 * m + n) * K_PITCH + 16 * block);
+                    sc[k] = sh.ks[buffer][(32 * m + n) * SCALES + block];
+                }
+            }
+#pragma unroll
+            for (int term = TERMS - 1; term >= 0; --term)
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    const u32x6 x = q[k].codes[term];
+                    const i32x8 kv = {(int)c[k].x, (int)c[k].y, (int)c[k].z, (int)c[k].w, 0, 0, 0, 0}, qv = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
+                    s[m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kv, qv, s[m], 4, 2, 0, sc[k], 0, q[k].scale - Q_STEP[term]);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (SPECIAL) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int at = 32 * m + 8 * (i / 4) + 4 * h + i % 4, key = key0 + at;
+                    s[m][i] = (valid >> at & 1) && key >= lo && key < hi ? s[m][i] : -INFINITY;
+                }
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, s[m][i]);
+        most = op_halves(most, OpMax(), __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false));
+        most = fmaxf(most * scale, top);
+        if (__builtin_amdgcn_ballot_w64(most > top)) {
+            const float shrink = most > top ? __builtin_amdgcn_exp2f(top - most) : 1.0f;
+            sum *= shrink;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] *= shrink;
+            top = most;
+        }
+        const float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT;
+#pragma unroll
+        for (int step = 0; step < 4; ++step) {
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                w[j] = __builtin_amdgcn_exp2f(fmaf(s[step / 2][step % 2 * 8 + j], scale, -base));
+                sum += w[j];
+            }
+            const unsigned char *const at = sh.v[buffer] + (16 * step + 4 * h + n % 16 / 4) * V_PITCH + 32 * (n / 16) + 8 * (n % 4);
+            const uint32_t kind = SPECIAL ? __builtin_amdgcn_readfirstlane(sh.kind[buffer][step]) : 0;
+            if (!SPECIAL || kind == 0) {
+                const f16x8 p16 = weights_f16(w);
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, read_transposed(at + 64 * d, 8 * V_PITCH)), p16, acc[d], 0, 0, 0);
+            } else {
+                bf16x8 high, low;
+                weights_bf16(w, high, low);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const bf16x8 v = __builtin_bit_cast(bf16x8, read_transposed(at + 64 * d, 8 * V_PITCH));
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, low, acc[d], 0, 0, 0);
+                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, high, acc[d], 0, 0, 0);
+                }
+                if (kind == 3)
+                    for (int j = 0; j < 16; ++j)
+                        if (key0 + 16 * step + j >= lo && key0 + 16 * step + j < hi) spoiled |= sh.spoiled[buffer][16 * step + j];
+            }
+        }
+    };
+    int pages = page_at(0), pages_next = page_at(1);
+    uint64_t valid = __builtin_amdgcn_ballot_w64(pages >= 0);
+    if (tiles > 0) {
+        fetch(0, pages);
+        put(0, valid);
+        if (tiles > 1) fetch(1, pages_next);
+    }
+    __syncthreads();
+    for (int t = 0; t < tiles; ++t) {
+        const int buffer = t & 1, key0 = t * KV_TILE;
+        const int pages_ahead = page_at(t + 2);
+        const uint64_t valid_next = __builtin_amdgcn_ballot_w64(pages_next >= 0);
+        if (t + 1 < tiles) {
+            put(buffer ^ 1, valid_next);
+            if (t + 2 < tiles) fetch(t + 2, pages_ahead);
+        }
+        if (key0 < hi_any && key0 + KV_TILE > lo_any) {                        // (else none of this wave's rows sees any of it)
+            const uint32_t *const kind = sh.kind[buffer];
+            const uint32_t kinds = __builtin_amdgcn_readfirstlane(kind[0] | kind[1] | kind[2] | kind[3]);
+            if (kinds || valid != ~0ull || key0 < lo_all || key0 + KV_TILE > hi_all) take(std::true_type{}, buffer, key0, valid);
+            else take(std::false_type{}, buffer, key0, valid);
+        }
+        __syncthreads();
+        valid = valid_next;
+        pages_next = pages_ahead;
+    }
+    sum = op_halves(sum, OpAdd(), __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false));
+    top -= WEIGHT_LIFT;
+    const int64_t slot = ((number * a.cache.kv_heads + kv_head) * a.many.splits + split) * MANY_ROWS + 32 * wave + n;
+    const float over = p.parts > 1 ? 1.0f : top == -INFINITY && sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        const float f = spoiled >> d & 1 ? NAN : over;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+    }
+    if (p.parts > 1) {
+        if (!there) return;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4 *>(a.many.part + slot * D + 32 * d + 8 * i + 4 * h) = f32x4{acc[d][4 * i], acc[d][4 * i + 1], acc[d][4 * i + 2], acc[d][4 * i + 3]};
+        if (h == 0) reinterpret_cast<float2 *>(a.many.part + (int64_t)a.many.tiles * a.cache.kv_heads * a.many.splits * MANY_ROWS * D)[slot] = make_float2(top, sum);
+        return;
+    }
+    if (a.lse && there && h == 0) a.lse[token * a.heads + head] = log_sum(top, sum);
+    if (!there) return;
+    uint16_t *const out = static_cast<uint16_t *>(const_cast<void *>(a.out.at)) + token * a.out.ld + head * a.out.hd;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<u32x2 *>(out + 32 * d + 8 * i + 4 * h) = u32x2{bf16_pair(acc[d][4 * i], acc[d][4 * i + 1]), bf16_pair(acc[d][4 * i + 2], acc[d][4 * i + 3])};
+}
+
+}  // namespace sbits
+
+template <int DB>
+static int launch(sbits_ctx *ctx, sbits::AttentionArgs &a)
+{
+    using namespace sbits;
+    const int64_t items = (int64_t)a.many.tiles * a.cache.kv_heads * a.many.splits;
+    auto fn = a.lse ? kv_attention_many_kernel<DB, 4> : kv_attention_many_kernel<DB, 3>;       // (sums in fp32 want scores to its last bits)
+    for (a.first = 0; a.first < items; a.first += KV_LAUNCH) {
+        hipLaunchKernelGGL(fn, dim3((uint32_t)std::min(items - a.first, KV_LAUNCH)), dim3(64 * MANY_WAVES), 0, ctx->stream, a);
+        SBITS_HIP(ctx, hipGetLastError());
+    }
+    return SBITS_OK;
+}
+
+int sbits_launch_kv_attention_many(sbits_ctx *ctx, sbits::AttentionArgs &a)
+{
+    switch (a.cache.dim / 32) {
+    case 1: return launch<1>(ctx, a);
+    case 2: return launch<2>(ctx, a);
+    case 3: return launch<3>(ctx, a);
+    case 4: return launch<4>(ctx, a);
+    case 5: return launch<5>(ctx, a);
+    case 6: return launch<6>(ctx, a);
+    case 7: return launch<7>(ctx, a);
+    default: return launch<8>(ctx, a);
+    }
+}

@@ -133,6 +133,13 @@ struct LoadArgs {
     void *out[2];
     int64_t ld[2], hd[2], tokens;
 };
+// How the rows of a kernel are cut up: tiles of rows (few: of each sequence, workgroups of their own; many: of all), parts of the keys, and of which sequences, by
+// their rows times the heads of a key's head.  part: [tile][kv_heads][part][rows of a tile][dim], then the same of pairs (largest score, sum).
+struct AttentionCut {
+    int tiles, splits;
+    int64_t least_rows, most_rows;
+    float *part;
+};
 struct AttentionArgs {
     KvPages cache;
     KvSequences sequences;
@@ -142,13 +149,13 @@ struct AttentionArgs {
     int heads, group;                        // of queries; to a key's
     float scale;                             // of scores as powers of two: scale * log2(e)
     int causal, window;
-    // few rows: tiles of 16 rows of a sequence that have workgroups of their own, parts of its keys, rows of a sequence from which on it is not this kernel's
-    int tiles, splits;
-    int64_t most_rows;
-    float *part;                             // [sequence][tile][kv_head][part][16][dim], then the same of pairs (largest score, sum)
+    AttentionCut few, many;
     int64_t first;                           // workgroups ahead of this launch
 };
 constexpr int64_t KV_LAUNCH = (int64_t)1 << 22;      // workgroups of a launch
+
+constexpr int FEW_ROWS = 16, MANY_ROWS = 128, KV_TILE = 64;      // rows of a tile; keys of one
+constexpr int FEW_LEAST = 8, MANY_LEAST = 16;                    // tiles of keys of a part, at least
 
 // the keys that a row at a position sees: first .. last - 1
 __device__ __forceinline__ void seen_keys(const AttentionArgs &a, int64_t length, int64_t position, int64_t &first, int64_t &last)
@@ -161,12 +168,183 @@ __device__ __forceinline__ void seen_keys(const AttentionArgs &a, int64_t length
     if (last < first) last = first;
 }
 
+// How a tile of rows goes over a sequence's keys.
+struct TilePlan {
+    int64_t start, end, rows;                 // the sequence's rows; times heads of a key's head
+    int64_t tiles;                            // of rows, in all
+    int64_t first, last, keys;                // keys of this tile of rows, from a multiple of 64 on; tiles of them
+    int64_t each;                             // of a part
+    int parts;
+};
+template <int ROWS>
+__device__ __forceinline__ bool tile_plan(const AttentionArgs &a, const AttentionCut &cut, int sequence, int64_t tile, TilePlan &p)
+{
+    constexpr int LEAST = ROWS == FEW_ROWS ? FEW_LEAST : MANY_LEAST;
+    const int start = a.sequences.starts[sequence], end = a.sequences.starts[sequence + 1];
+    p.start = start > 0 ? start : 0;
+    p.end = end < a.tokens ? end : a.tokens;
+    p.rows = (p.end - p.start) * a.group;
+    p.tiles = (p.rows + ROWS - 1) / ROWS;
+    if (tile >= p.tiles || p.rows < cut.least_rows || p.rows > cut.most_rows) return false;
+    const int64_t length = a.sequences.lengths[sequence], r0 = tile * ROWS, r1 = r0 + ROWS < p.rows ? r0 + ROWS - 1 : p.rows - 1;
+    int64_t none;
+    seen_keys(a, length, length - end + p.start + r0 / a.group, p.first, none);
+    seen_keys(a, length, length - end + p.start + r1 / a.group, none, p.last);
+    p.first &= ~(int64_t)(KV_TILE - 1);
+    p.keys = p.last > p.first ? (p.last - p.first + KV_TILE - 1) / KV_TILE : 0;
+    // (more tiles of a sequence than have workgroups: these take several, each with all of its keys)
+    const int most = ROWS == MANY_ROWS || p.tiles <= cut.tiles ? cut.splits : 1;
+    const int64_t each = (p.keys + most - 1) / most;
+    p.each = each > LEAST ? each : LEAST;
+    p.parts = p.keys > p.each ? (int)((p.keys + p.each - 1) / p.each) : 1;
+    return true;
+}
+
+// The tiles of many rows of all sequences are numbered so that sequence b's begin at floor(rows ahead of it / MANY_ROWS) + b, which leaves each as many as
+// it can need.  The sequence and the tile of a number, -1 if there is none.
+__device__ __forceinline__ int64_t many_base(const AttentionArgs &a, int b)
+{
+    const int64_t start = a.sequences.starts[b];
+    return (start < 0 ? 0 : start > a.tokens ? a.tokens : start) * a.group / MANY_ROWS + b;
+}
+__device__ __forceinline__ int find_tile(const AttentionArgs &a, int64_t number, int64_t &tile)
+{
+    const int lane = threadIdx.x & 63;
+    int first = 0, left = a.sequences.count;
+    while (true) {
+        const int step = (left + 63) >> 6, i = lane * step;
+        const bool below = i < left && many_base(a, first + i) <= number;
+        const uint64_t above = ~__builtin_amdgcn_ballot_w64(below);
+        const int n = above ? __builtin_ctzll(above) : 64;
+        if (n == 0) return -1;
+        first += (n - 1) * step;
+        if (step == 1) break;
+        left = left - (n - 1) * step < step ? left - (n - 1) * step : step;
+    }
+    tile = number - many_base(a, first);
+    return first;
+}
+
+// ---- scores: k as it lies in the cache, q in 6-bit terms ------------------------------
+typedef unsigned int u32x6 __attribute__((ext_vector_type(6)));
+typedef float f32x32 __attribute__((ext_vector_type(32)));
+
+// A block of 32 values of q as blocks of 6-bit codes (E2M3) whose powers of two are 4, 6 and 6 steps apart.  The matrix instruction multiplies 4-bit by 6-bit
+// codes at twice the rate of bf16 and without a conversion of k.  A code has 4 bits, bf16 8: what the first term leaves of elements down to 1/4
+// of the block's largest is exact in the second, of those down to 2^-8 of it in the third, of those down to 2^-14 in the fourth; of smaller ones less than 2^-18
+// of the largest is left out (with three terms less than 2^-15).
+constexpr int Q_STEP[4] = {0, 4, 10, 16};
+template <int TERMS>
+struct QBlock { u32x6 codes[TERMS]; int scale; };                             // scale: the first term's byte
+template <int TERMS>
+__device__ __forceinline__ QBlock<TERMS> split_q(const float (&x)[32])
+{
+    f32x16 a, b;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        a[i] = x[2 * i];
+        b[i] = x[2 * i + 1];
+        top = max(top, __float_as_uint(a[i]) & 0x7fffffffu);
+        top = max(top, __float_as_uint(b[i]) & 0x7fffffffu);
+    }
+    QBlock<TERMS> q;
+    q.scale = max((int)(top >> 23) - 2, 17);
+#pragma unroll
+    for (int t = 0; t < TERMS; ++t) {
+        const float scale = __uint_as_float((uint32_t)(q.scale - Q_STEP[t]) << 23);
+        q.codes[t] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(a, b, scale);
+        if (t == TERMS - 1) break;
+        const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q.codes[t], scale);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            a[i] -= back[2 * i];
+            b[i] -= back[2 * i + 1];
+        }
+    }
+    return q;
+}
+// Block `block` of a row of q, zeros if it is not there; fine: whether all values are finite (others become 0).
+template <int TERMS>
+__device__ __forceinline__ QBlock<TERMS> load_q(const AttentionArgs &a, bool there, int64_t token, int head, int block, bool &fine)
+{
+    float x[32];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (there) load8<true>(a.q.at, token * a.q.ld + head * a.q.hd + 32 * block + 8 * i, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool ok = (__float_as_uint(v[e]) & 0x7f800000u) != 0x7f800000u;
+            fine = fine && ok;
+            x[8 * i + e] = ok ? v[e] : 0.0f;
+        }
+    }
+    return split_q<TERMS>(x);
+}
+
+// ---- sums: v in fp16 where that is exact, else in bf16 ----------------------------------
+// Codes times 2^(byte - 127) are fp16 numbers for the bytes 104 .. 140, and a weight in fp16 has 11 bits.  Steps of keys with other bytes take v in bf16, which is exact for
+// all, and weights in two bf16 terms.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+constexpr uint32_t F16_LOW = 104, F16_HIGH = 140;
+__device__ __forceinline__ u32x4 mx_halves8(uint32_t codes, float scale)
+{
+    u32x4 v;
+    v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0));
+    v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1));
+    v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2));
+    v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3));
+    return v;
+}
+// 8 weights, in fp16, or bf16 and what that leaves
+__device__ __forceinline__ f16x8 weights_f16(const float (&w)[8])
+{
+    f16x8 h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = (_Float16)w[i];
+    return h;
+}
+__device__ __forceinline__ void weights_bf16(const float (&w)[8], bf16x8 &high, bf16x8 &low)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        high[i] = (__bf16)w[i];
+        low[i] = (__bf16)(w[i] - (float)high[i]);
+    }
+}
+// Weights are 2^14 times what they are against the largest score: fp16 then keeps those down to 2^-28 of the largest with all its bits, and some of those down to 2^-38.
+constexpr float WEIGHT_LIFT = 14.0f;
+// The logarithm of the sum: that of weights at their own size, which loses no bits to the lift's.
+__device__ __forceinline__ float log_sum(float lowered, float sum)
+{
+    return (lowered + WEIGHT_LIFT + __builtin_amdgcn_logf(sum * 0x1p-14f)) * 0x1.62e43p-1f;
+}
+
+// 4 rows of 16 elements at `at` and `step` bytes on, transposed
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ s16x8 read_transposed(const unsigned char *at, int step)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    typedef __attribute__((address_space(3))) unsigned char lds_u8;
+    lds_u8 *const p = (lds_u8 *)at;
+    return __builtin_shufflevector(__builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p), __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + step)), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 }  // namespace sbits
 
 // ---- launchers --------------------------------------------------------------
 int sbits_launch_rotate(sbits_ctx *ctx, const sbits::RotateArgs &a, bool bf16, bool wide);
 int sbits_launch_kv_store(sbits_ctx *ctx, const sbits::StoreArgs &a, bool bf16);
 int sbits_launch_kv_load(sbits_ctx *ctx, const sbits::LoadArgs &a, bool bf16);
-// how an attention is cut up: tiles, splits, most_rows; the workspace of its parts in bytes
+// bytes of the parts of a kernel's tiles (few: tiles of each of `sequences`)
+inline size_t sbits_kv_attention_part(const sbits::AttentionCut &cut, int rows, const sbits_kv_cache &cache, int64_t sequences)
+{
+    return cut.splits <= 1 ? 0 : (size_t)(cut.tiles * (rows == sbits::FEW_ROWS ? sequences : 1) * cache.kv_heads * cut.splits) * rows * (cache.head_dim + 2) * 4;
+}
+// how an attention is cut up; the workspace of its parts in bytes
 size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache, const sbits_sequences &sequences, int64_t tokens, int heads, sbits::AttentionArgs &a);
 int sbits_launch_kv_attention(sbits_ctx *ctx, sbits::AttentionArgs &a);
+int sbits_launch_kv_attention_many(sbits_ctx *ctx, sbits::AttentionArgs &a);

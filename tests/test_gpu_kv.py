@@ -211,10 +211,12 @@ def check(ctx, b, heads, causal=True, window=0, scale=None, lse=True, pad=0, gon
         keep = ~none & ~torch.isnan(want_lse)
         assert ((s[rows] - want_lse).abs()[keep] <= off_lse[keep]).all()
     again = torch.empty_like(out)
-    ctx.kv_attention(cache, seqs, src, again, ws, scale=scale, causal=causal, window=window)
-    if not nan.any():
-        assert torch.equal(again[rows.cuda()], out[rows.cuda()]) or not lse
-    return out
+    ws.fill_(0)
+    ctx.kv_attention(cache, seqs, src, again, ws, scale=scale, causal=causal, window=window, lse=sums)
+    assert torch.equal(again[rows.cuda()].nan_to_num(nan=5.0), out[rows.cuda()].nan_to_num(nan=5.0))
+    if lse:                                                      # without the sums the same within the bounds
+        ctx.kv_attention(cache, seqs, src, again, ws, scale=scale, causal=causal, window=window)
+        assert ((again.cpu().double()[rows] - want).abs()[~nan] <= off[~nan]).all()
 
 
 @pytest.mark.parametrize("dim", [32, 64, 96, 128, 160, 192, 224, 256])
