@@ -522,7 +522,7 @@ typedef struct {
     void *k_codes, *k_scales, *v_codes, *v_scales;   /* DEVICE                          */
     int64_t pages;                                   /* 1 .. 2^31 - 1                   */
     int64_t ld_codes, ld_scales;                     /* bytes from page to page         */
-    int32_t page_tokens;                             /* a power of two, 1 .. 2^20       */
+    int32_t page_tokens;                             /* a power of two, 8 .. 2^20       */
     int32_t kv_heads, head_dim;                      /* 1 .. 1024; a multiple of 32, 32 .. 256 */
 } sbits_kv_cache;
 
@@ -594,14 +594,15 @@ int  sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequ
 
 /* Attention of the rows to their sequences' cached tokens:  out = sum_j p_j v_j,  p = softmax over the keys seen of
  * scale * q . k_j.  q, out: bf16 [tokens][heads][head_dim] by pitches as above, 16-byte aligned, pitches multiples of 8;
- * heads a multiple of kv_heads, head h reads kv_heads' number h / (heads / kv_heads).  causal: a row at position p sees the
+ * heads a multiple of kv_heads, tokens * heads < 2^31 - 255, head h reads kv_heads' number h / (heads / kv_heads).  causal: a row at position p sees the
  * positions up to p, with window > 0 (causal only) the last `window` of them; else all of the sequence's.
  * A row that sees no key gets zeros.  lse (float32[tokens][heads], may be NULL): the logarithm of the sum of
  * e^(scale * q . k_j), -infinity where no key is seen.  Only keys that a row sees have a part in it, whatever the others
  * hold; a seen value that is not finite makes its block of 32 outputs NaN (in v the bytes 253 and 254 count as 255), a seen key that is
  * not or a q that is not makes the row NaN.  Scores and sums are taken in fp32 on the matrix cores, in an order that goes with the batch's
  * sizes; a call gives the same bits again.  scale > 0.  ws: 256-byte aligned,
- * sbits_kv_attention_ws_bytes() bytes (which may be 0), asked for with the call's own arguments.  */
+ * sbits_kv_attention_ws_bytes() bytes (which may be 0), asked for with the call's own arguments.  Positions from 2^31 - 256 on
+ * are not there.  With lse, q enters the products in a term more, so that last bits of out may differ.  */
 size_t sbits_kv_attention_ws_bytes(const sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens,
                                    int heads);
 int  sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens, int heads,

@@ -29,7 +29,7 @@ static int need_device(sbits_ctx *ctx)
 static int check_cache(const sbits_kv_cache *c)
 {
     if (!c || !aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) || !aligned(c->k_scales, 4) || !aligned(c->v_scales, 4)) return SBITS_ERR_INVALID_ARG;
-    if (c->page_tokens < 1 || c->page_tokens > KV_MAX_PAGE || (c->page_tokens & (c->page_tokens - 1)) || c->kv_heads < 1 || c->kv_heads > KV_MAX_HEADS ||
+    if (c->page_tokens < KV_LEAST_PAGE || c->page_tokens > KV_MAX_PAGE || (c->page_tokens & (c->page_tokens - 1)) || c->kv_heads < 1 || c->kv_heads > KV_MAX_HEADS ||
         c->head_dim < 32 || c->head_dim > KV_MAX_DIM || c->head_dim % MX_BLOCK || c->pages < 1 || c->pages > INT32_MAX)
         return SBITS_ERR_BAD_SHAPE;
     const int64_t rows = (int64_t)c->kv_heads * c->page_tokens;
@@ -162,7 +162,7 @@ int sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_seque
 size_t sbits_kv_attention_ws_bytes(const sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens, int heads)
 {
     if (!ctx || check_cache(cache) || check_sequences(sequences) || !tokens_ok(tokens) || heads < 1 || heads > KV_MAX_QUERY_HEADS || heads % cache->kv_heads) return 0;
-    if (tokens == 0 || sequences->count == 0) return 0;
+    if (tokens == 0 || sequences->count == 0 || tokens * heads > KV_MAX_ROWS) return 0;
     AttentionArgs a;
     return sbits_kv_attention_cut(ctx, *cache, *sequences, tokens, heads, a);
 }
@@ -174,7 +174,7 @@ int sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_
     if (!ctx || !tokens_ok(tokens) || (causal & ~1) || window < 0 || (window && !causal) || !(scale > 0.0f) || !isfinite(scale)) return SBITS_ERR_INVALID_ARG;
     int rc;
     if ((rc = check_cache(cache)) || (rc = check_sequences(sequences))) return rc;
-    if (heads < 1 || heads > KV_MAX_QUERY_HEADS || heads % cache->kv_heads) return SBITS_ERR_BAD_SHAPE;
+    if (heads < 1 || heads > KV_MAX_QUERY_HEADS || heads % cache->kv_heads || tokens * heads > KV_MAX_ROWS) return SBITS_ERR_BAD_SHAPE;
     if (tokens == 0 || sequences->count == 0) return SBITS_OK;
     if (!heads_ok(q_bf16, ld_q, hd_q, SBITS_TYPE_BF16, 0) || !heads_ok(out_bf16, ld_out, hd_out, SBITS_TYPE_BF16, cache->head_dim) || (lse && !aligned(lse, 4)))
         return SBITS_ERR_INVALID_ARG;
@@ -186,8 +186,9 @@ int sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_
     a.sequences = sequences_of(*sequences);
     a.q = {q_bf16, ld_q, hd_q}; a.out = {out_bf16, ld_out, hd_out};
     a.lse = lse;
-    a.tokens = tokens;
+    a.tokens = (int)tokens;
     a.heads = heads; a.group = heads / cache->kv_heads;
+    a.there = (int)std::min<int64_t>((int64_t)sequences->max_pages * cache->page_tokens, KV_MAX_KEYS);
     a.scale = (float)(scale * 1.4426950408889634); a.causal = causal; a.window = window;
     char *const base = static_cast<char *>(ws);
     a.few.part = reinterpret_cast<float *>(base);

@@ -6,7 +6,7 @@
 
 namespace sbits {
 
-constexpr int FEW_WAVES = 4;
+constexpr int FEW_WAVES = 4, FEW_LEAST = 8, MANY_LEAST = 16;                  // .._LEAST: tiles of keys of a part, at least
 
 // largest or sum over the lanes with the same lane % 16
 template <class Op>
@@ -16,37 +16,105 @@ __device__ __forceinline__ float across_rows(float v, Op op)
     return op_halves(v, op, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
 }
 
-// A workgroup has 16 rows (tokens times the heads of a key's head) and a part of their keys, of which its four waves take 64 in turn, each by itself.
-// Scores, transposed:  k's codes go to the matrix instruction as they lie in the cache, a lane a block of 32, with q in 6-bit terms.  Lane l then has row l % 16 and the keys 16 b + 4 (l / 16) + r.
-// Sums, transposed:  v becomes fp16 or bf16 (exactly) on its way to LDS, whose transposing reads give a lane one element of 8 keys; weights are already
-// where the instruction wants them, if its keys come in the order 16 (j / 4) + 4 (l / 16) + j % 4.
-// Pages' numbers are asked for two tiles of keys ahead, codes one.
+// 8 elements of a row of the output, from `at` on: sums over the sum of weights l, which is against the largest score m
 template <int DB>
-struct FewTile { u32x4 k[4][(DB + 3) / 4], v[DB]; uint32_t ks[4][(DB + 3) / 4]; uint8_t vs[DB]; };
+__device__ __forceinline__ void put_row(const AttentionArgs &a, const TilePlan &p, int kv_head, int row, int at, float m, float l, float (&y)[8])
+{
+    const int in_row = (uint32_t)row / (uint32_t)a.group, token = p.start + in_row, head = kv_head * a.group + row - in_row * a.group;
+    const float over = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] *= over;
+    store8<true>(const_cast<void *>(a.out.at), (int64_t)token * a.out.ld + (int64_t)head * a.out.hd + at, y);
+    if (a.lse && at == 0) a.lse[(int64_t)token * a.heads + head] = log_sum(m, l);
+}
 
+// A workgroup has 16 rows (tokens times the heads of a key's head) and a part of their keys, of which its four waves take 64 in turn, each by itself.
+// Keys go by fours, neighbours in a page: a lane's loads of a tile have one address for codes of k, one for its scales, and so for v.
+// Scores, transposed:  k's codes go to the matrix instruction as they lie in the cache, a lane a block of 32, with q in 6-bit terms.  Instruction b has the keys 4 i + b, and
+// lane l then row l % 16 and the keys 16 (l / 16) + 4 r + b.
+// Sums, transposed:  v becomes fp16 or bf16 (exactly) on its way to LDS, key 16 g + 4 r + b to row 16 b + 4 g + r, where transposing reads give a lane one element of 8
+// keys, the ones whose weights it has.
+// A tile's codes are asked for when those of the one before have been used, ahead of its weights and sums; pages' numbers a tile earlier.
 template <int DB>
 __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(AttentionArgs a)
 {
     constexpr int D = 32 * DB, KS = (DB + 3) / 4, PITCH = 2 * D + 32;          // PITCH: rows 8 banks apart, mod 64 an odd multiple of 8
     __shared__ __attribute__((aligned(16))) unsigned char smem[FEW_WAVES][KV_TILE * PITCH];
     __shared__ float2 red[FEW_WAVES][FEW_ROWS];
-    const int64_t item = a.first + blockIdx.x;
-    const int split = (int)(item % a.few.splits), kv_head = (int)(item / a.few.splits % a.cache.kv_heads);
-    const int64_t place = item / a.few.splits / a.cache.kv_heads;                  // [sequence][tile]
-    const int sequence = (int)(place / a.few.tiles);
+    const int split = blockIdx.x, kv_head = blockIdx.y, place = a.first + blockIdx.z;          // place: [sequence][tile]
+    const int sequence = (uint32_t)place / (uint32_t)a.few.tiles;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const u32x4 zero = {0, 0, 0, 0};
-    for (int64_t tile = place % a.few.tiles;; tile += a.few.tiles) {
+    typedef u32x4 __attribute__((aligned(4))) u32x4_by4;
+    for (int tile = place - sequence * a.few.tiles;; tile += a.few.tiles) {
         TilePlan p;
         if (!tile_plan<FEW_ROWS>(a, a.few, sequence, tile, p) || split >= p.parts) return;
-        const int64_t length = a.sequences.lengths[sequence], end = a.sequences.starts[sequence + 1];
+        const int tile0 = split * p.each, tile1 = min(tile0 + p.each, p.keys);
+        // pages of this lane's four keys of a tile: those it multiplies, and those of v that it brings
+        const int32_t *const table = a.sequences.pages + sequence * a.sequences.ld_pages;
+        struct Pages { int k, v; };
+        auto pages_at = [&](int t) {
+            auto page_of = [&](int key) {
+                if (t >= tile1 || key >= p.last) return -1;
+                const int page = table[key >> a.cache.shift];
+                return (uint32_t)page < (uint64_t)a.cache.pages ? page : -1;
+            };
+            const int key0 = p.first + t * KV_TILE;
+            return Pages{page_of(key0 + 4 * n), page_of(key0 + 4 * (lane >> 2))};
+        };
+        u32x4 kc[4][KS], vc[DB], ks[KS], vq[KS];
+        uint8_t vb[DB];
+        const int64_t head_rows = (int64_t)kv_head << a.cache.shift;
+        auto fetch_k = [&](int t, int page) {                                  // (keys that are not there: of page 0)
+            const int64_t at = head_rows + ((p.first + t * KV_TILE + 4 * n) & a.cache.mask), from = max(page, 0);
+            const uint8_t *const c = a.cache.codes[0] + from * a.cache.ld_codes + at * (16 * DB) + 16 * g, *const sc = a.cache.scales[0] + from * a.cache.ld_scales + at * (4 * KS);
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    kc[b][s] = DB % 4 == 0 || 4 * s + g < DB ? *reinterpret_cast<const u32x4 *>(c + 16 * DB * b + 64 * s) : zero;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) ks[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
+        };
+        auto k_scale = [&](int b, int s) {                                     // of key b, block 4 s + g
+            const uint32_t word = KS == 1 ? ks[0][b] : ks[b / 2][b % 2 * 2 + s];
+            return DB % 4 == 0 || 4 * s + g < DB ? (int)(word >> 8 * g) : 127;
+        };
+        // v: piece 4 i + lane % 4 of the 4 DB pieces of four keys
+        auto v_key = [&](int i) { return DB % 4 == 0 ? 4 * i / DB : (4 * i + (lane & 3)) / DB; };
+        auto v_block = [&](int i) { return DB % 4 == 0 ? 4 * i % DB + (lane & 3) : (4 * i + (lane & 3)) % DB; };
+        auto fetch_v = [&](int t, int page) {
+            const int64_t at = head_rows + ((p.first + t * KV_TILE + 4 * (lane >> 2)) & a.cache.mask), from = max(page, 0);
+            const uint8_t *const c = a.cache.codes[1] + from * a.cache.ld_codes + at * (16 * DB) + 16 * (lane & 3), *const sc = a.cache.scales[1] + from * a.cache.ld_scales + at * (4 * KS);
+#pragma unroll
+            for (int i = 0; i < DB; ++i) vc[i] = *reinterpret_cast<const u32x4 *>(c + 64 * i);
+            if constexpr (DB % 4 == 0) {
+#pragma unroll
+                for (int s = 0; s < KS; ++s) vq[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
+            } else {
+#pragma unroll
+                for (int i = 0; i < DB; ++i) vb[i] = sc[4 * KS * v_key(i) + v_block(i)];
+            }
+        };
+        auto v_scale = [&](int i) -> uint32_t {
+            if constexpr (DB % 4 == 0) {
+                const int word = 4 * i / DB * KS + i % KS;                     // (of key 4 i / DB, blocks 4 (i % KS) on)
+                return vq[word / 4][word % 4] >> 8 * (lane & 3) & 255;
+            } else {
+                return vb[i];
+            }
+        };
+        Pages pages = pages_at(tile0 + wave), pages_next = pages_at(tile0 + wave + FEW_WAVES);
+        if (tile0 + wave < tile1) {
+            fetch_k(tile0 + wave, pages.k);
+            fetch_v(tile0 + wave, pages.v);
+        }
         // this lane's row
-        const int64_t r = tile * FEW_ROWS + n;
+        const int r = tile * FEW_ROWS + n;
         const bool there = r < p.rows;
-        const int64_t token = p.start + (there ? r : 0) / a.group;
-        const int head = kv_head * a.group + (int)((there ? r : 0) % a.group);
-        int64_t lo, hi;
-        seen_keys(a, length, length - end + token, lo, hi);
+        const int in_row = (uint32_t)(there ? r : 0) / (uint32_t)a.group, token = p.start + in_row, head = kv_head * a.group + (there ? r : 0) - in_row * a.group;
+        int lo, hi;
+        seen_keys(a, p.length, p.ahead + token, lo, hi);
         if (!there) lo = p.first, hi = p.last;                                 // (its sums go nowhere)
         QBlock<4> q[KS];
         bool fine = true;
@@ -54,116 +122,68 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
         for (int s = 0; s < KS; ++s) q[s] = load_q<4>(a, there && 4 * s + g < DB, token, head, 4 * s + g, fine);
         const uint64_t broken = __builtin_amdgcn_ballot_w64(!fine);
         const float scale = ((broken | broken >> 16 | broken >> 32 | broken >> 48) >> n & 1) ? NAN : a.scale;
+        // the keys that all rows see
+        int lo_all = lo, hi_all = hi;
+#pragma unroll
+        for (int i = 1; i < 16; i *= 2) {
+            lo_all = max(lo_all, __shfl_xor(lo_all, i));
+            hi_all = min(hi_all, __shfl_xor(hi_all, i));
+        }
+        lo_all = __builtin_amdgcn_readfirstlane(lo_all);
+        hi_all = __builtin_amdgcn_readfirstlane(hi_all);
 
-        const int64_t tile0 = split * p.each, tile1 = std::min(tile0 + p.each, p.keys);
-        const int32_t *const table = a.sequences.pages + sequence * a.sequences.ld_pages;
-        auto page_at = [&](int64_t t) {                                        // of this lane's key of a tile
-            const int64_t key = p.first + t * KV_TILE + lane;
-            if (t >= tile1 || key >= p.last) return -1;
-            const int page = table[key >> a.cache.shift];
-            return (uint32_t)page < (uint64_t)a.cache.pages ? page : -1;
-        };
-        FewTile<DB> now, next;
-        auto fetch = [&](FewTile<DB> &f, int64_t t, int pages) {               // (keys that are not there: of page 0)
-            const int key0 = (int)((p.first + t * KV_TILE) & a.cache.mask);   // place in a page of the tile's first key, if a page has them all
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int page = max(__shfl(pages, 16 * b + n), 0);
-                const int64_t at = ((int64_t)kv_head << a.cache.shift) + ((key0 + 16 * b + n) & a.cache.mask);
-                const uint8_t *const c = a.cache.codes[0] + page * a.cache.ld_codes + at * (16 * DB), *const sc = a.cache.scales[0] + page * a.cache.ld_scales + at * (4 * KS);
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    f.k[b][s] = zero;
-                    f.ks[b][s] = 0x7f7f7f7fu;
-                    if (4 * s + g < DB) {
-                        f.k[b][s] = *reinterpret_cast<const u32x4 *>(c + 16 * (4 * s + g));
-                        f.ks[b][s] = *reinterpret_cast<const uint32_t *>(sc + 4 * s);
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
-                const int page = max(__shfl(pages, key), 0);
-                const int64_t at = ((int64_t)kv_head << a.cache.shift) + ((key0 + key) & a.cache.mask);
-                f.v[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[1] + page * a.cache.ld_codes + at * (16 * DB) + 16 * block);
-                f.vs[i] = a.cache.scales[1][page * a.cache.ld_scales + at * (4 * KS) + block];
-            }
-        };
         f32x4 acc[2 * DB];
 #pragma unroll
         for (int i = 0; i < 2 * DB; ++i) acc[i] = f32x4{0, 0, 0, 0};
         float top = -INFINITY, sum = 0.0f;
         uint32_t spoiled = 0;                                                  // blocks of this lane's row with a seen value that is not finite
         unsigned char *const lds = smem[wave];
-        int pages = page_at(tile0 + wave), pages_next = page_at(tile0 + wave + FEW_WAVES);
-        if (tile0 + wave < tile1) fetch(now, tile0 + wave, pages);
-        for (int64_t t = tile0 + wave; t < tile1; t += FEW_WAVES) {
-            const int pages_ahead = page_at(t + 2 * FEW_WAVES);
-            if (t + FEW_WAVES < tile1) fetch(next, t + FEW_WAVES, pages_next);
-            const int64_t key0 = p.first + t * KV_TILE;
-            const uint64_t valid = __builtin_amdgcn_ballot_w64(pages >= 0);
-            // scores
-            f32x4 s[4];
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                s[b] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int term = 4 - 1; term >= 0; --term)
-#pragma unroll
-                    for (int k = 0; k < KS; ++k) {
-                        const u32x4 c = now.k[b][k];
-                        const u32x6 x = q[k].codes[term];
-                        const i32x8 kv = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}, qv = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
-                        s[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv, s[b], 4, 2, 0, (int)(now.ks[b][k] >> 8 * g), 0, q[k].scale - Q_STEP[term]);
-                    }
-            }
-            // v to LDS
-            bool usual = true;                                                 // all in fp16
+        // v to LDS; special: not all keys there, or other powers than fp16 has
+        auto put = [&](auto special_, auto f16_, int key0, bool v_there) {
+            constexpr bool SPECIAL = decltype(special_)::value, F16 = decltype(f16_)::value;
 #pragma unroll
             for (int i = 0; i < DB; ++i) {
-                const int key = (64 * i + lane) / DB;
-                usual = usual && (!(valid >> key & 1) || (now.vs[i] >= F16_LOW && now.vs[i] <= F16_HIGH));
-            }
-            const bool halves = __builtin_amdgcn_ballot_w64(!usual) == 0;
-            auto put = [&](auto f16) {
-#pragma unroll
-                for (int i = 0; i < DB; ++i) {
-                    const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
-                    bool ok = valid >> key & 1;
-                    if constexpr (!decltype(f16)::value) {
-                        const bool bad = ok && now.vs[i] >= KV_V_LIMIT;
+                const int key = 4 * (lane >> 2) + v_key(i), block = v_block(i);
+                u32x4 codes = vc[i];
+                uint32_t byte = v_scale(i);
+                if constexpr (SPECIAL) {
+                    bool ok = v_there && key0 + key < p.last;
+                    if constexpr (!F16) {
+                        const bool bad = ok && byte >= KV_V_LIMIT;
                         uint64_t bads = __builtin_amdgcn_ballot_w64(bad);
                         while (bads) {
-                            const int bad_piece = 64 * i + __builtin_ctzll(bads);
+                            const int from = __builtin_ctzll(bads), bad_key = __builtin_amdgcn_readlane(key, from), bad_block = __builtin_amdgcn_readlane(block, from);
                             bads &= bads - 1;
-                            const int64_t where = key0 + bad_piece / DB;
-                            if (where >= lo && where < hi) spoiled |= 1u << bad_piece % DB;
+                            if (key0 + bad_key >= lo && key0 + bad_key < hi) spoiled |= 1u << bad_block;
                         }
                         ok = ok && !bad;
                     }
-                    const u32x4 codes = ok ? now.v[i] : zero;
-                    const float sc = __uint_as_float((uint32_t)(ok ? now.vs[i] : 127) << 23);
-#pragma unroll
-                    for (int w = 0; w < 4; ++w)
-                        *reinterpret_cast<u32x4 *>(lds + key * PITCH + 64 * block + 16 * w) = decltype(f16)::value ? mx_halves8(codes[w], sc) : mx_values8(codes[w], sc);
+                    if (!ok) codes = zero, byte = 127;
                 }
-            };
-            if (halves) put(std::true_type{});
-            else put(std::false_type{});
-            // weights
+                const float sc = __uint_as_float(byte << 23);
+                unsigned char *const to = lds + (16 * (key & 3) + (key >> 2)) * PITCH + 64 * block;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) *reinterpret_cast<u32x4 *>(to + 16 * w) = F16 ? mx_halves8(codes[w], sc) : mx_values8(codes[w], sc);
+            }
+        };
+        // weights and sums of a tile
+        auto take = [&](auto special_, bool halves, f32x4 (&s)[4], int key0, uint32_t fours) {
+            constexpr bool SPECIAL = decltype(special_)::value;
+            if constexpr (SPECIAL) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = key0 + 16 * g + 4 * i + b;
+                        s[b][i] = (fours >> (4 * g + i) & 1) && key >= lo && key < hi ? s[b][i] : -INFINITY;
+                    }
+            }
             float most = -INFINITY;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t key = key0 + 16 * b + 4 * g + i;
-                    float x = s[b][i] * scale;
-                    x = (valid >> (16 * b + 4 * g + i) & 1) && key >= lo && key < hi ? x : -INFINITY;
-                    s[b][i] = x;
-                    most = fmaxf(most, x);
-                }
-            most = fmaxf(across_rows(most, OpMax()), top);
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, s[b][i]);
+            most = fmaxf(across_rows(most, OpMax()) * scale, top);
             if (__builtin_amdgcn_ballot_w64(most > top)) {
                 const float shrink = most > top ? __builtin_amdgcn_exp2f(top - most) : 1.0f;
                 sum *= shrink;
@@ -177,16 +197,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float one = __builtin_amdgcn_exp2f(s[b][i] - base);
+                    const float one = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale, -base));
                     sum += one;
                     w[b / 2][b % 2 * 4 + i] = one;
                 }
-            __builtin_amdgcn_wave_barrier();
-            // sums
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const unsigned char *const at = lds + (32 * half + 4 * g + n / 4) * PITCH + 8 * (n % 4);
-                if (halves) {
+                if (!SPECIAL || halves) {
                     const f16x8 p16 = weights_f16(w[half]);
 #pragma unroll
                     for (int d = 0; d < 2 * DB; ++d)
@@ -202,10 +220,44 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                     }
                 }
             }
+        };
+        for (int t = tile0 + wave; t < tile1; t += FEW_WAVES) {
+            const Pages ahead = pages_at(t + 2 * FEW_WAVES);
+            const int key0 = p.first + t * KV_TILE;
+            const uint32_t fours = (uint32_t)__builtin_amdgcn_ballot_w64(pages.k >= 0) & 0xffffu;
+            f32x4 s[4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                s[b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int term = 3; term >= 0; --term)
+#pragma unroll
+                    for (int k = 0; k < KS; ++k) {
+                        const u32x4 c = kc[b][k];
+                        const u32x6 x = q[k].codes[term];
+                        const i32x8 kv = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}, qv = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
+                        s[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv, s[b], 4, 2, 0, k_scale(b, k), 0, q[k].scale - Q_STEP[term]);
+                    }
+            }
+            bool usual = true;                                                 // all in fp16
+#pragma unroll
+            for (int i = 0; i < DB; ++i) usual = usual && v_scale(i) >= F16_LOW && v_scale(i) <= F16_HIGH;
+            // (keys that are not there count, too: they may make the tile a special one)
+            const bool halves = __builtin_amdgcn_ballot_w64(!usual) == 0;
+            const bool plain = halves && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all;
+            if (plain) put(std::false_type{}, std::true_type{}, key0, true);
+            else if (halves) put(std::true_type{}, std::true_type{}, key0, pages.v >= 0);
+            else put(std::true_type{}, std::false_type{}, key0, pages.v >= 0);
+            if (t + FEW_WAVES < tile1) {
+                fetch_k(t + FEW_WAVES, pages_next.k);
+                fetch_v(t + FEW_WAVES, pages_next.v);
+            }
             __builtin_amdgcn_wave_barrier();
-            now = next;
+            if (plain) take(std::false_type{}, true, s, key0, fours);
+            else take(std::true_type{}, halves, s, key0, fours);
+            __builtin_amdgcn_wave_barrier();
             pages = pages_next;
-            pages_next = pages_ahead;
+            pages_next = ahead;
         }
         sum = across_rows(sum, OpAdd());
 #pragma unroll
@@ -217,7 +269,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
         __syncthreads();
         // the waves' sums: 8 elements of a row a thread
         for (int unit = tid; unit < 4 * DB * FEW_ROWS; unit += 64 * FEW_WAVES) {
-            const int row = unit / (4 * DB), at = unit % (4 * DB) * 8;
+            const int row = unit / (4 * DB), at = unit % (4 * DB) * 8, mine = tile * FEW_ROWS + row;
+            if (mine >= p.rows) continue;
             float m = -INFINITY, l = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
             for (int w = 0; w < FEW_WAVES; ++w) m = fmaxf(m, red[w][row].x);
@@ -230,10 +283,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = fmaf(o[e], f, y[e]);
             }
-            const int64_t mine = tile * FEW_ROWS + row;
-            if (mine >= p.rows) continue;
             if (p.parts > 1) {
-                const int64_t slot = ((place * a.cache.kv_heads + kv_head) * a.few.splits + split) * FEW_ROWS + row;
+                const int64_t slot = (((int64_t)place * a.cache.kv_heads + kv_head) * a.few.splits + split) * FEW_ROWS + row;
                 store8<false>(a.few.part, slot * D + at, y);
                 if (at == 0) {
                     const int64_t all = (int64_t)a.sequences.count * a.few.tiles * a.cache.kv_heads * a.few.splits * FEW_ROWS;
@@ -241,56 +292,57 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                 }
                 continue;
             }
-            const int64_t to = p.start + mine / a.group;
-            const int h = kv_head * a.group + (int)(mine % a.group);
-            const float over = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] *= over;
-            store8<true>(const_cast<void *>(a.out.at), to * a.out.ld + h * a.out.hd + at, y);
-            if (a.lse && at == 0) a.lse[to * a.heads + h] = log_sum(m, l);
+            put_row<DB>(a, p, kv_head, mine, at, m, l, y);
         }
         __syncthreads();
     }
 }
 
-// The parts of 16 rows of a tile: a thread has 8 elements of a row.
+// The parts of a row: a thread has 8 elements of every 16th (or, with DB threads of 4 to an element's run, as many as fit 256) part.
 template <int DB, int ROWS>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
 {
-    constexpr int D = 32 * DB;
+    constexpr int D = 32 * DB, RUNS = 4 * DB, WAYS = 256 / RUNS;
+    __shared__ __attribute__((aligned(16))) float part[WAYS][RUNS][8];
+    __shared__ float sums[WAYS];
     const AttentionCut &cut = ROWS == FEW_ROWS ? a.few : a.many;
-    const int64_t number = a.first + blockIdx.x, item = number / (ROWS / 16), place = item / a.cache.kv_heads;
-    const int kv_head = (int)(item % a.cache.kv_heads), row0 = (int)(number % (ROWS / 16)) * 16;
-    int sequence = (int)(place / cut.tiles);
-    int64_t tile = place % cut.tiles, items = (int64_t)a.sequences.count * cut.tiles;
-    if (ROWS == MANY_ROWS) sequence = find_tile(a, place, tile), items = cut.tiles;
+    const int kv_head = blockIdx.y, place = a.first + blockIdx.z, row = blockIdx.x;
+    int sequence = (uint32_t)place / (uint32_t)cut.tiles, tile = place - sequence * cut.tiles;
+    int64_t places = (int64_t)a.sequences.count * cut.tiles;
+    if (ROWS == MANY_ROWS) sequence = find_tile(a, place, tile), places = cut.tiles;
     TilePlan p;
-    if (sequence < 0 || !tile_plan<ROWS>(a, cut, sequence, tile, p) || p.parts == 1) return;
-    const float2 *const pairs = reinterpret_cast<const float2 *>(cut.part + items * a.cache.kv_heads * cut.splits * ROWS * D);
-    for (int unit = threadIdx.x; unit < 4 * DB * 16; unit += 256) {
-        const int row = row0 + unit / (4 * DB), at = unit % (4 * DB) * 8;
-        const int64_t mine = tile * ROWS + row, slot = item * cut.splits * ROWS + row;
-        if (mine >= p.rows) continue;
-        float m = -INFINITY, l = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int s = 0; s < p.parts; ++s) m = fmaxf(m, pairs[slot + s * ROWS].x);
-        const float base = m == -INFINITY ? 0.0f : m;
-        for (int s = 0; s < p.parts; ++s) {
-            const float2 one = pairs[slot + s * ROWS];
+    if (sequence < 0 || !tile_plan<ROWS>(a, cut, sequence, tile, p) || p.parts == 1 || tile * ROWS + row >= p.rows) return;
+    const int64_t slot = ((int64_t)place * a.cache.kv_heads + kv_head) * cut.splits * ROWS + row;
+    const float2 *const pairs = reinterpret_cast<const float2 *>(cut.part + places * a.cache.kv_heads * cut.splits * ROWS * D) + slot;
+    const int lane = threadIdx.x & 63, way = threadIdx.x / RUNS, run = threadIdx.x - way * RUNS;
+    // (every wave finds the largest score)
+    float m = -INFINITY;
+    for (int s = lane; s < p.parts; s += 64) m = fmaxf(m, pairs[(int64_t)s * ROWS].x);
+    m = group_allreduce<64>(m, OpMax());
+    const float base = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (way < WAYS) {
+        for (int s = way; s < p.parts; s += WAYS) {
+            const float2 one = pairs[(int64_t)s * ROWS];
+            float o[8];
+            load8<false>(cut.part, (slot + (int64_t)s * ROWS) * D + 8 * run, o);
             const float f = __builtin_amdgcn_exp2f(one.x - base);
             l = fmaf(one.y, f, l);
-            float o[8];
-            load8<false>(cut.part, (slot + s * ROWS) * D + at, o);
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = fmaf(o[e], f, y[e]);
         }
-        const int64_t to = p.start + mine / a.group;
-        const int h = kv_head * a.group + (int)(mine % a.group);
-        const float over = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= over;
-        store8<true>(const_cast<void *>(a.out.at), to * a.out.ld + h * a.out.hd + at, y);
-        if (a.lse && at == 0) a.lse[to * a.heads + h] = log_sum(m, l);
+        for (int e = 0; e < 8; ++e) part[way][run][e] = y[e];
+        if (run == 0) sums[way] = l;
     }
+    __syncthreads();
+    if (way != 0) return;
+    for (int w = 1; w < WAYS && w < p.parts; ++w) {
+        l += sums[w];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] += part[w][run][e];
+    }
+    put_row<DB>(a, p, kv_head, tile * ROWS + row, 8 * run, m, l, y);
 }
 
 }  // namespace sbits
@@ -306,21 +358,24 @@ size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache,
     const int64_t there = std::min<int64_t>((int64_t)sequences.max_pages * cache.page_tokens, INT32_MAX);
     const int64_t length = sequences.max_length ? std::min<int64_t>(sequences.max_length, there) : there;
     const int64_t cus = ctx->cus ? ctx->cus : 256;
-    auto splits = [&](int64_t items, int64_t least, int64_t wanted) {
-        return (int)std::max<int64_t>(std::min<int64_t>((length / KV_TILE + least) / least, wanted / items), 1);
+    // parts of about as many tiles of keys as make `wanted` workgroups of the longest sequences there may be
+    auto cut = [&](AttentionCut &c, int64_t items, int64_t least, int64_t wanted) {
+        const int64_t keys = length / KV_TILE + 1;
+        c.each = (int)std::min(std::max(keys * items / wanted, least), std::max(keys, least));
+        c.splits = (int)std::min<int64_t>((keys + c.each - 1) / c.each, KV_MAX_PARTS);
     };
-    a.few = a.many = {0, 1, 0, INT64_MAX, nullptr};
+    a.few = a.many = {0, 1, 1, 0, INT32_MAX, nullptr};
     const bool only_few = new_most * group <= FEW_MOST, only_many = !only_few && sequences.count == 1;
     if (!only_many) {
         a.few.tiles = (int)((std::min(new_most * group, FEW_MOST) + FEW_ROWS - 1) / FEW_ROWS);
-        a.few.splits = splits((int64_t)sequences.count * a.few.tiles * cache.kv_heads, FEW_LEAST, 4 * cus);
-        if (!only_few) a.few.most_rows = FEW_MOST;
+        cut(a.few, (int64_t)sequences.count * a.few.tiles * cache.kv_heads, FEW_LEAST, 4 * cus);
+        if (!only_few) a.few.most_rows = (int)FEW_MOST;
     }
     if (!only_few) {
         const int64_t tiles = tokens * group / MANY_ROWS + sequences.count;
         a.many.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
-        a.many.splits = splits(tiles * cache.kv_heads, MANY_LEAST, 2 * cus);
-        if (!only_many) a.many.least_rows = FEW_MOST + 1;
+        cut(a.many, tiles * cache.kv_heads, MANY_LEAST, 2 * cus);
+        if (!only_many) a.many.least_rows = (int)FEW_MOST + 1;
     }
     return sbits_kv_attention_part(a.few, FEW_ROWS, cache, sequences.count) + sbits_kv_attention_part(a.many, MANY_ROWS, cache, sequences.count);
 }
@@ -329,19 +384,22 @@ template <int DB>
 static int launch(sbits_ctx *ctx, sbits::AttentionArgs &a)
 {
     using namespace sbits;
-    auto enqueue = [&](auto kernel, int64_t items, int threads) -> int {
-        for (a.first = 0; a.first < items; a.first += KV_LAUNCH) {
-            hipLaunchKernelGGL(kernel, dim3((uint32_t)std::min(items - a.first, KV_LAUNCH)), dim3(threads), 0, ctx->stream, a);
+    auto enqueue = [&](auto kernel, int x, int64_t places, int threads) -> int {
+        const int64_t most = kv_launch(x, a.cache.kv_heads);
+        for (int64_t first = 0; first < places; first += most) {
+            a.first = (int)first;
+            const dim3 grid(x, a.cache.kv_heads, (uint32_t)std::min(places - first, most));
+            hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, ctx->stream, a);
             SBITS_HIP(ctx, hipGetLastError());
         }
         return SBITS_OK;
     };
-    const int64_t few = (int64_t)a.sequences.count * a.few.tiles * a.cache.kv_heads, many = (int64_t)a.many.tiles * a.cache.kv_heads;
+    const int64_t few = (int64_t)a.sequences.count * a.few.tiles;
     int rc;
-    if (many && (rc = sbits_launch_kv_attention_many(ctx, a))) return rc;
-    if (few && (rc = enqueue(kv_attention_few_kernel<DB>, few * a.few.splits, 64 * FEW_WAVES))) return rc;
-    if (a.many.splits > 1 && (rc = enqueue(kv_attention_join_kernel<DB, MANY_ROWS>, many * (MANY_ROWS / 16), 256))) return rc;
-    if (a.few.splits > 1 && (rc = enqueue(kv_attention_join_kernel<DB, FEW_ROWS>, few, 256))) return rc;
+    if (a.many.tiles && (rc = sbits_launch_kv_attention_many(ctx, a))) return rc;
+    if (few && (rc = enqueue(kv_attention_few_kernel<DB>, a.few.splits, few, 64 * FEW_WAVES))) return rc;
+    if (a.many.splits > 1 && (rc = enqueue(kv_attention_join_kernel<DB, MANY_ROWS>, MANY_ROWS, a.many.tiles, 256))) return rc;
+    if (a.few.splits > 1 && (rc = enqueue(kv_attention_join_kernel<DB, FEW_ROWS>, FEW_ROWS, few, 256))) return rc;
     return SBITS_OK;
 }
 

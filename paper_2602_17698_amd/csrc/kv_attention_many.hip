@@ -29,32 +29,26 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     constexpr int K_PITCH = Shared::K_PITCH, V_PITCH = Shared::V_PITCH, SCALES = Shared::SCALES;
     __shared__ __attribute__((aligned(16))) Shared sh;
     // heads first: neighbouring workgroups, on different dies, have different keys; the last rows of a sequence, which see the most, ahead of the others
-    const int64_t item = a.first + blockIdx.x;
-    const int kv_head = (int)(item % a.cache.kv_heads), split = (int)(item / a.cache.kv_heads % a.many.splits);
-    const int64_t number = a.many.tiles - 1 - item / a.cache.kv_heads / a.many.splits;
-    int64_t tile;
+    const int kv_head = blockIdx.x, split = blockIdx.y, number = a.many.tiles - 1 - (a.first + (int)blockIdx.z);
+    int tile;
     const int sequence = find_tile(a, number, tile);
     TilePlan p;
     if (sequence < 0 || !tile_plan<MANY_ROWS>(a, a.many, sequence, tile, p) || split >= p.parts) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const u32x4 zero = {0, 0, 0, 0};
-    const int64_t length = a.sequences.lengths[sequence], end = a.sequences.starts[sequence + 1];
     // this lane's row
-    const int64_t r = tile * MANY_ROWS + 32 * wave + n;
+    const int r = tile * MANY_ROWS + 32 * wave + n;
     const bool there = r < p.rows;
-    const int64_t token = p.start + (there ? r : 0) / a.group;
-    const int head = kv_head * a.group + (int)((there ? r : 0) % a.group);
-    const int64_t key_first = p.first + split * p.each * KV_TILE;              // the part's keys count from here on
-    const int tiles = (int)std::min(p.each, p.keys - split * p.each);
-    int lo, hi;                                                                // keys seen, of the part's
+    const int in_row = (uint32_t)(there ? r : 0) / (uint32_t)a.group, token = p.start + in_row, head = kv_head * a.group + (there ? r : 0) - in_row * a.group;
+    const int key_first = p.first + split * p.each * KV_TILE, tiles = min(p.each, p.keys - split * p.each);    // of the part
+    int lo, hi;                                                                // keys seen, counted from the part's first
     {
-        int64_t first, last;
-        seen_keys(a, length, length - end + token, first, last);
-        const int64_t all = (int64_t)tiles * KV_TILE;
-        first -= key_first; last -= key_first;
-        lo = (int)std::min(std::max<int64_t>(first, 0), all);
-        hi = (int)std::min(std::max<int64_t>(last, 0), all);
-        if (!there) lo = hi = 0;
+        int first, last;
+        seen_keys(a, p.length, p.ahead + token, first, last);
+        const int all = tiles * KV_TILE;
+        lo = min(max(first - key_first, 0), all);
+        hi = there ? min(max(last - key_first, 0), all) : 0;
+        if (!there) lo = 0;
     }
     // of the wave's rows that are there: the first key that one sees, that all see; the last ones
     auto over_wave = [&](int v, auto op) {
@@ -79,7 +73,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
 
     const int32_t *const table = a.sequences.pages + sequence * a.sequences.ld_pages;
     auto page_at = [&](int t) {                                                // of this lane's key of a tile
-        const int64_t key = key_first + (int64_t)t * KV_TILE + lane;
+        const int key = key_first + t * KV_TILE + lane;
         if (t >= tiles || key >= p.last) return -1;
         const int page = table[key >> a.cache.shift];
         return (uint32_t)page < (uint64_t)a.cache.pages ? page : -1;
@@ -88,7 +82,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     u32x4 kc[PIECES], vc[PIECES];
     uint32_t vs[PIECES], ks;
     auto fetch = [&](int t, int pages) {                                       // (keys that are not there: of page 0)
-        const int key0 = (int)((key_first + (int64_t)t * KV_TILE) & a.cache.mask) + 16 * wave;
+        const int key0 = ((key_first + t * KV_TILE) & a.cache.mask) + 16 * wave;
         const int64_t base = (int64_t)kv_head << a.cache.shift;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -275,7 +269,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     }
     sum = op_halves(sum, OpAdd(), __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false));
     top -= WEIGHT_LIFT;
-    const int64_t slot = ((number * a.cache.kv_heads + kv_head) * a.many.splits + split) * MANY_ROWS + 32 * wave + n;
+    const int64_t slot = (((int64_t)number * a.cache.kv_heads + kv_head) * a.many.splits + split) * MANY_ROWS + 32 * wave + n;
     const float over = p.parts > 1 ? 1.0f : top == -INFINITY && sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
@@ -293,9 +287,9 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         if (h == 0) reinterpret_cast<float2 *>(a.many.part + (int64_t)a.many.tiles * a.cache.kv_heads * a.many.splits * MANY_ROWS * D)[slot] = make_float2(top, sum);
         return;
     }
-    if (a.lse && there && h == 0) a.lse[token * a.heads + head] = log_sum(top, sum);
+    if (a.lse && there && h == 0) a.lse[(int64_t)token * a.heads + head] = log_sum(top, sum);
     if (!there) return;
-    uint16_t *const out = static_cast<uint16_t *>(const_cast<void *>(a.out.at)) + token * a.out.ld + head * a.out.hd;
+    uint16_t *const out = static_cast<uint16_t *>(const_cast<void *>(a.out.at)) + (int64_t)token * a.out.ld + (int64_t)head * a.out.hd;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -309,10 +303,12 @@ template <int DB>
 static int launch(sbits_ctx *ctx, sbits::AttentionArgs &a)
 {
     using namespace sbits;
-    const int64_t items = (int64_t)a.many.tiles * a.cache.kv_heads * a.many.splits;
     auto fn = a.lse ? kv_attention_many_kernel<DB, 4> : kv_attention_many_kernel<DB, 3>;       // (sums in fp32 want scores to its last bits)
-    for (a.first = 0; a.first < items; a.first += KV_LAUNCH) {
-        hipLaunchKernelGGL(fn, dim3((uint32_t)std::min(items - a.first, KV_LAUNCH)), dim3(64 * MANY_WAVES), 0, ctx->stream, a);
+    const int64_t most = kv_launch(a.cache.kv_heads, a.many.splits);
+    for (int64_t first = 0; first < a.many.tiles; first += most) {
+        a.first = (int)first;
+        const dim3 grid(a.cache.kv_heads, a.many.splits, (uint32_t)std::min(a.many.tiles - first, most));
+        hipLaunchKernelGGL(fn, grid, dim3(64 * MANY_WAVES), 0, ctx->stream, a);
         SBITS_HIP(ctx, hipGetLastError());
     }
     return SBITS_OK;

@@ -6,7 +6,7 @@
 
 namespace sbits {
 
-constexpr int KV_MAX_DIM = 256, KV_MAX_HEADS = 1024, KV_MAX_PAGE = 1 << 20, ROTARY_MAX_PAIRS = 128;
+constexpr int KV_MAX_DIM = 256, KV_MAX_HEADS = 1024, KV_MAX_PAGE = 1 << 20, ROTARY_MAX_PAIRS = 128, KV_LEAST_PAGE = 8;
 constexpr int KV_MAX_QUERY_HEADS = 65535;
 constexpr uint32_t KV_V_LIMIT = 253;         // bytes of v from here on: a value beyond bf16's range is possible, the block counts as NaN
 
@@ -136,8 +136,8 @@ struct LoadArgs {
 // How the rows of a kernel are cut up: tiles of rows (few: of each sequence, workgroups of their own; many: of all), parts of the keys, and of which sequences, by
 // their rows times the heads of a key's head.  part: [tile][kv_heads][part][rows of a tile][dim], then the same of pairs (largest score, sum).
 struct AttentionCut {
-    int tiles, splits;
-    int64_t least_rows, most_rows;
+    int tiles, splits, each;                 // each: tiles of keys of a part, at least
+    int least_rows, most_rows;
     float *part;
 };
 struct AttentionArgs {
@@ -145,58 +145,62 @@ struct AttentionArgs {
     KvSequences sequences;
     Heads q, out;
     float *lse;
-    int64_t tokens;
-    int heads, group;                        // of queries; to a key's
+    int tokens, heads, group;                // heads of queries; of a key's head
+    int there;                               // positions that the table of pages reaches
     float scale;                             // of scores as powers of two: scale * log2(e)
     int causal, window;
     AttentionCut few, many;
-    int64_t first;                           // workgroups ahead of this launch
+    int first;                               // workgroups (of the grid's z) ahead of this launch
 };
-constexpr int64_t KV_LAUNCH = (int64_t)1 << 22;      // workgroups of a launch
+constexpr int KV_MAX_KEYS = INT32_MAX - 255, KV_MAX_ROWS = INT32_MAX - 255;    // a tile's keys or rows more are numbers still
+constexpr int KV_MAX_PARTS = 1024;
+// z of a launch: at most 2^22 workgroups, 2^30 threads
+inline int64_t kv_launch(int64_t x, int64_t y)
+{
+    const int64_t z = ((int64_t)1 << 22) / (x * y);
+    return z < 1 ? 1 : z > 32768 ? 32768 : z;
+}
 
 constexpr int FEW_ROWS = 16, MANY_ROWS = 128, KV_TILE = 64;      // rows of a tile; keys of one
-constexpr int FEW_LEAST = 8, MANY_LEAST = 16;                    // tiles of keys of a part, at least
 
 // the keys that a row at a position sees: first .. last - 1
-__device__ __forceinline__ void seen_keys(const AttentionArgs &a, int64_t length, int64_t position, int64_t &first, int64_t &last)
+__device__ __forceinline__ void seen_keys(const AttentionArgs &a, int length, int position, int &first, int &last)
 {
-    const int64_t there = (int64_t)a.sequences.max_pages << a.cache.shift;
-    first = 0;
-    last = a.causal && position + 1 < length ? position + 1 : length;
-    if (a.window && position + 1 - a.window > 0) first = position + 1 - a.window;
-    if (last > there) last = there;
-    if (last < first) last = first;
+    last = a.causal && position < length ? position + 1 : length;
+    first = a.window && position >= a.window ? position + 1 - a.window : 0;
+    last = min(last, a.there);
+    last = max(last, first);
 }
 
 // How a tile of rows goes over a sequence's keys.
 struct TilePlan {
-    int64_t start, end, rows;                 // the sequence's rows; times heads of a key's head
-    int64_t tiles;                            // of rows, in all
-    int64_t first, last, keys;                // keys of this tile of rows, from a multiple of 64 on; tiles of them
-    int64_t each;                             // of a part
-    int parts;
+    int start, end, rows;                     // the sequence's rows; times heads of a key's head
+    int ahead;                                // position of row 0 of all: a row's is that and its number
+    int length, tiles;                        // tiles of rows, in all
+    int first, last, keys;                    // keys of this tile of rows, from a multiple of 64 on; tiles of them
+    int each, parts;                          // tiles of keys of a part
 };
 template <int ROWS>
-__device__ __forceinline__ bool tile_plan(const AttentionArgs &a, const AttentionCut &cut, int sequence, int64_t tile, TilePlan &p)
+__device__ __forceinline__ bool tile_plan(const AttentionArgs &a, const AttentionCut &cut, int sequence, int tile, TilePlan &p)
 {
-    constexpr int LEAST = ROWS == FEW_ROWS ? FEW_LEAST : MANY_LEAST;
     const int start = a.sequences.starts[sequence], end = a.sequences.starts[sequence + 1];
-    p.start = start > 0 ? start : 0;
-    p.end = end < a.tokens ? end : a.tokens;
+    p.length = max(a.sequences.lengths[sequence], 0);
+    p.start = min(max(start, 0), a.tokens);
+    p.end = min(max(end, 0), a.tokens);
     p.rows = (p.end - p.start) * a.group;
     p.tiles = (p.rows + ROWS - 1) / ROWS;
     if (tile >= p.tiles || p.rows < cut.least_rows || p.rows > cut.most_rows) return false;
-    const int64_t length = a.sequences.lengths[sequence], r0 = tile * ROWS, r1 = r0 + ROWS < p.rows ? r0 + ROWS - 1 : p.rows - 1;
-    int64_t none;
-    seen_keys(a, length, length - end + p.start + r0 / a.group, p.first, none);
-    seen_keys(a, length, length - end + p.start + r1 / a.group, none, p.last);
-    p.first &= ~(int64_t)(KV_TILE - 1);
+    p.ahead = p.length - end;
+    const int r0 = tile * ROWS, r1 = min(r0 + ROWS, p.rows) - 1;
+    int none;
+    seen_keys(a, p.length, p.ahead + p.start + r0 / a.group, p.first, none);
+    seen_keys(a, p.length, p.ahead + p.start + r1 / a.group, none, p.last);
+    p.first &= ~(KV_TILE - 1);
     p.keys = p.last > p.first ? (p.last - p.first + KV_TILE - 1) / KV_TILE : 0;
     // (more tiles of a sequence than have workgroups: these take several, each with all of its keys)
     const int most = ROWS == MANY_ROWS || p.tiles <= cut.tiles ? cut.splits : 1;
-    const int64_t each = (p.keys + most - 1) / most;
-    p.each = each > LEAST ? each : LEAST;
-    p.parts = p.keys > p.each ? (int)((p.keys + p.each - 1) / p.each) : 1;
+    p.each = max((p.keys + most - 1) / most, cut.each);
+    p.parts = p.keys > p.each ? (p.keys + p.each - 1) / p.each : 1;
     return true;
 }
 
@@ -204,10 +208,9 @@ __device__ __forceinline__ bool tile_plan(const AttentionArgs &a, const Attentio
 // it can need.  The sequence and the tile of a number, -1 if there is none.
 __device__ __forceinline__ int64_t many_base(const AttentionArgs &a, int b)
 {
-    const int64_t start = a.sequences.starts[b];
-    return (start < 0 ? 0 : start > a.tokens ? a.tokens : start) * a.group / MANY_ROWS + b;
+    return (int64_t)((uint32_t)(min(max(a.sequences.starts[b], 0), a.tokens) * a.group) / MANY_ROWS) + b;
 }
-__device__ __forceinline__ int find_tile(const AttentionArgs &a, int64_t number, int64_t &tile)
+__device__ __forceinline__ int find_tile(const AttentionArgs &a, int number, int &tile)
 {
     const int lane = threadIdx.x & 63;
     int first = 0, left = a.sequences.count;
@@ -221,7 +224,7 @@ __device__ __forceinline__ int find_tile(const AttentionArgs &a, int64_t number,
         if (step == 1) break;
         left = left - (n - 1) * step < step ? left - (n - 1) * step : step;
     }
-    tile = number - many_base(a, first);
+    tile = (int)(number - many_base(a, first));
     return first;
 }
 
@@ -266,13 +269,13 @@ __device__ __forceinline__ QBlock<TERMS> split_q(const float (&x)[32])
 }
 // Block `block` of a row of q, zeros if it is not there; fine: whether all values are finite (others become 0).
 template <int TERMS>
-__device__ __forceinline__ QBlock<TERMS> load_q(const AttentionArgs &a, bool there, int64_t token, int head, int block, bool &fine)
+__device__ __forceinline__ QBlock<TERMS> load_q(const AttentionArgs &a, bool there, int token, int head, int block, bool &fine)
 {
     float x[32];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (there) load8<true>(a.q.at, token * a.q.ld + head * a.q.hd + 32 * block + 8 * i, v);
+        if (there) load8<true>(a.q.at, (int64_t)token * a.q.ld + (int64_t)head * a.q.hd + 32 * block + 8 * i, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const bool ok = (__float_as_uint(v[e]) & 0x7f800000u) != 0x7f800000u;
@@ -342,7 +345,7 @@ int sbits_launch_kv_load(sbits_ctx *ctx, const sbits::LoadArgs &a, bool bf16);
 // bytes of the parts of a kernel's tiles (few: tiles of each of `sequences`)
 inline size_t sbits_kv_attention_part(const sbits::AttentionCut &cut, int rows, const sbits_kv_cache &cache, int64_t sequences)
 {
-    return cut.splits <= 1 ? 0 : (size_t)(cut.tiles * (rows == sbits::FEW_ROWS ? sequences : 1) * cache.kv_heads * cut.splits) * rows * (cache.head_dim + 2) * 4;
+    return cut.splits <= 1 ? 0 : (size_t)((int64_t)cut.tiles * (rows == sbits::FEW_ROWS ? sequences : 1) * cache.kv_heads * cut.splits) * rows * (cache.head_dim + 2) * 4;
 }
 // how an attention is cut up; the workspace of its parts in bytes
 size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache, const sbits_sequences &sequences, int64_t tokens, int heads, sbits::AttentionArgs &a);

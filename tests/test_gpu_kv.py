@@ -87,8 +87,8 @@ SIZES = [(1, 0), (5, 3), (0, 9), (40, 100), (0, 0), (2, 64)]
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("page,kv_heads,dim,dims,interleaved,given,pad", [
-    (16, 2, 128, 128, False, False, 0), (1, 1, 32, 32, True, False, 8), (8, 3, 96, 40, False, True, 16), (64, 1, 256, 38, True, True, 0),
-    (128, 5, 64, 64, False, False, 8), (4096, 2, 160, 0, False, False, 0), (2, 4, 192, 192, False, True, 24), (32, 1, 224, 64, True, False, 0)])
+    (16, 2, 128, 128, False, False, 0), (8, 1, 32, 32, True, False, 8), (8, 3, 96, 40, False, True, 16), (64, 1, 256, 38, True, True, 0),
+    (128, 5, 64, 64, False, False, 8), (4096, 2, 160, 0, False, False, 0), (16, 4, 192, 192, False, True, 24), (32, 1, 224, 64, True, False, 0)])
 def test_store_and_load(ctx, dtype, page, kv_heads, dim, dims, interleaved, given, pad):
     b = Batch(SIZES, page, kv_heads, dim, seed=dim, lead=3, behind=2)
     cache, seqs, buffers = b.on(sb)
@@ -220,7 +220,7 @@ def check(ctx, b, heads, causal=True, window=0, scale=None, lse=True, pad=0, gon
 
 
 @pytest.mark.parametrize("dim", [32, 64, 96, 128, 160, 192, 224, 256])
-@pytest.mark.parametrize("page,kv_heads,group", [(16, 2, 4), (1, 1, 1), (64, 1, 7), (256, 3, 16)])
+@pytest.mark.parametrize("page,kv_heads,group", [(16, 2, 4), (8, 1, 1), (64, 1, 7), (256, 3, 16)])
 def test_attention_of_single_tokens(ctx, dim, page, kv_heads, group):
     b = Batch([(1, 0), (1, 1), (1, 62), (1, 63), (1, 64), (0, 70), (1, 200), (1, 400)], page, kv_heads, dim, seed=dim + page, lead=1, behind=3)
     check(ctx, b, kv_heads * group, pad=8, max_new=1, max_length=401)

@@ -69,14 +69,14 @@ def everything(ctx, c=None, s=None):
 
 def test_nothing_wrong_but_no_device(ctx):
     assert everything(ctx) == {sb.ERR_HIP}
-    assert everything(ctx, cache(page_tokens=1, kv_heads=1, head_dim=32)) != {0}
+    assert everything(ctx, cache(page_tokens=8, kv_heads=1, head_dim=32)) != {0}
     assert store(ctx, rotary=turns(), positions=A, q=A, q_heads=8, q_out=A) == sb.ERR_HIP
     assert call("rotate", ctx, turns(), A, 3, 2, 128, A, 256, 128, 1, 0, A, 256, 128) == sb.ERR_HIP
 
 
 @pytest.mark.parametrize("change,status", [
     (dict(k_codes=None), -1), (dict(v_codes=A + 8), -1), (dict(k_scales=A + 2), -1), (dict(v_scales=None), -1), (dict(pages=0), -2), (dict(pages=1 << 31), -2),
-    (dict(page_tokens=0), -2), (dict(page_tokens=24), -2), (dict(page_tokens=1 << 21), -2), (dict(kv_heads=0), -2), (dict(kv_heads=1025), -2), (dict(head_dim=48), -2),
+    (dict(page_tokens=4), -2), (dict(page_tokens=24), -2), (dict(page_tokens=1 << 21), -2), (dict(kv_heads=0), -2), (dict(kv_heads=1025), -2), (dict(head_dim=48), -2),
     (dict(head_dim=0), -2), (dict(head_dim=288), -2), (dict(ld_codes=2032), -1), (dict(ld_codes=2056), -1), (dict(ld_scales=124), -1), (dict(ld_scales=130), -1),
     (dict(ld_codes=1 << 40), -1), (dict(ld_codes=-2048), -1)])
 def test_caches_that_are_refused(ctx, change, status):
@@ -120,7 +120,7 @@ def test_store_refuses_rotations(ctx):
 
 
 @pytest.mark.parametrize("at,value,status", [
-    (2, -1, -1), (3, 7, -2), (3, 0, -2), (3, 65536, -2), (4, None, -1), (4, A + 2, -1), (5, 1020, -1), (7, 0.0, -1), (7, -1.0, -1), (7, math.nan, -1),
+    (2, -1, -1), (3, 7, -2), (3, 0, -2), (3, 65536, -2), (2, 1 << 28, -2), (4, None, -1), (4, A + 2, -1), (5, 1020, -1), (7, 0.0, -1), (7, -1.0, -1), (7, math.nan, -1),
     (7, math.inf, -1), (8, 2, -1), (9, -1, -1), (10, None, -1), (11, 64, -1), (12, 120, -1), (13, A + 2, -1)])
 def test_attention_refuses(ctx, at, value, status):
     assert attend(ctx, change=[(at, value)]) == status
