@@ -192,7 +192,7 @@ int sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_
     a.scale = (float)(scale * 1.4426950408889634); a.causal = causal; a.window = window;
     char *const base = static_cast<char *>(ws);
     a.few.part = reinterpret_cast<float *>(base);
-    a.many.part = reinterpret_cast<float *>(base + sbits_kv_attention_part(a.few, FEW_ROWS, *cache, sequences->count));
+    a.many.part = reinterpret_cast<float *>(base + sbits_kv_attention_part(a.few, FEW_ROWS, *cache));
     return sbits_launch_kv_attention(ctx, a);
 }
 

@@ -6,7 +6,7 @@
 
 namespace sbits {
 
-constexpr int FEW_WAVES = 4, FEW_LEAST = 8, MANY_LEAST = 16;                  // .._LEAST: tiles of keys of a part, at least
+constexpr int FEW_WAVES = 4, MANY_LEAST = 16;                                 // MANY_LEAST: tiles of keys of a part, at least
 
 // largest or sum over the lanes with the same lane % 16
 template <class Op>
@@ -18,9 +18,9 @@ __device__ __forceinline__ float across_rows(float v, Op op)
 
 // 8 elements of a row of the output, from `at` on: sums over the sum of weights l, which is against the largest score m
 template <int DB>
-__device__ __forceinline__ void put_row(const AttentionArgs &a, const TilePlan &p, int kv_head, int row, int at, float m, float l, float (&y)[8])
+__device__ __forceinline__ void put_row(const AttentionArgs &a, int start, int kv_head, int row, int at, float m, float l, float (&y)[8])
 {
-    const int in_row = (uint32_t)row / (uint32_t)a.group, token = p.start + in_row, head = kv_head * a.group + row - in_row * a.group;
+    const int in_row = (uint32_t)row / (uint32_t)a.group, token = start + in_row, head = kv_head * a.group + row - in_row * a.group;
     const float over = m == -INFINITY && l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] *= over;
@@ -28,94 +28,115 @@ __device__ __forceinline__ void put_row(const AttentionArgs &a, const TilePlan &
     if (a.lse && at == 0) a.lse[(int64_t)token * a.heads + head] = log_sum(m, l);
 }
 
-// A workgroup has 16 rows (tokens times the heads of a key's head) and a part of their keys, of which its four waves take 64 in turn, each by itself.
+// A workgroup has, one after the other, the items and parts of items of its share of the line; of an item's keys its four waves take 64 in turn, each by itself.
 // Keys go by fours, neighbours in a page: a lane's loads of a tile have one address for codes of k, one for its scales, and so for v.
 // Scores, transposed:  k's codes go to the matrix instruction as they lie in the cache, a lane a block of 32, with q in 6-bit terms.  Instruction b has the keys 4 i + b, and
 // lane l then row l % 16 and the keys 16 (l / 16) + 4 r + b.
-// Sums, transposed:  v becomes fp16 or bf16 (exactly) on its way to LDS, key 16 g + 4 r + b to row 16 b + 4 g + r, where transposing reads give a lane one element of 8
-// keys, the ones whose weights it has.
-// A tile's codes are asked for when those of the one before have been used, ahead of its weights and sums; pages' numbers a tile earlier.
+// Sums, transposed:  v becomes fp16 or bf16 (exactly) on its way to LDS, 32 keys at a time, key 16 g + 4 r + b to row 16 (b % 2) + 4 g + r, where transposing reads give a lane one element
+// of 8 keys, the ones whose weights it has.
+// A tile's codes of k are asked for when those of the one before have been used, of v likewise; pages' numbers a tile earlier.
 template <int DB>
 __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(AttentionArgs a)
 {
     constexpr int D = 32 * DB, KS = (DB + 3) / 4, PITCH = 2 * D + 32;          // PITCH: rows 8 banks apart, mod 64 an odd multiple of 8
-    __shared__ __attribute__((aligned(16))) unsigned char smem[FEW_WAVES][KV_TILE * PITCH];
+    __shared__ __attribute__((aligned(16))) unsigned char smem[FEW_WAVES][32 * PITCH];
     __shared__ float2 red[FEW_WAVES][FEW_ROWS];
-    const int split = blockIdx.x, kv_head = blockIdx.y, place = a.first + blockIdx.z;          // place: [sequence][tile]
-    const int sequence = (uint32_t)place / (uint32_t)a.few.tiles;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const u32x4 zero = {0, 0, 0, 0};
     typedef u32x4 __attribute__((aligned(4))) u32x4_by4;
-    for (int tile = place - sequence * a.few.tiles;; tile += a.few.tiles) {
-        TilePlan p;
-        if (!tile_plan<FEW_ROWS>(a, a.few, sequence, tile, p) || split >= p.parts) return;
-        const int tile0 = split * p.each, tile1 = min(tile0 + p.each, p.keys);
-        // pages of this lane's four keys of a tile: those it multiplies, and those of v that it brings
+    // this workgroup's share
+    int64_t none;
+    const int64_t total = few_total(a, -1, none);
+    const int workgroups = few_workgroups(a, total), workgroup = blockIdx.x;
+    if (total == 0 || workgroup >= workgroups) return;
+    int sequence = 0, item, off;
+    FewSequence f;
+    auto cut = [&](int w) {                                                    // (of the end of the line: behind the last item)
+        if (w == workgroups) return total;
+        const int64_t x = few_cut(w, workgroups, total);
+        int64_t begin;
+        sequence = __builtin_amdgcn_readfirstlane(few_find(a, x, begin));
+        f = few_sequence(a, sequence);
+        const uint64_t in = (uint64_t)(x - begin);
+        item = in >> 32 ? (int)(in / (uint32_t)f.keys) : (int)((uint32_t)in / (uint32_t)f.keys);
+        off = (int)(x - begin - (int64_t)item * f.keys);
+        const int moved = few_snap(off, f.keys), by = moved - off;
+        off = moved;
+        return x + by;
+    };
+    const int64_t stop = cut(workgroup + 1), from = cut(workgroup);
+    int64_t left = stop - from;
+    for (; left > 0; ++item, off = 0) {
+        if (off == f.keys) continue;                                           // (cut behind its last tile)
+        while (item >= f.tiles * a.cache.kv_heads) {
+            item = 0;
+            do f = few_sequence(a, ++sequence); while (f.tiles == 0);
+        }
+        const int tile = (uint32_t)item / (uint32_t)a.cache.kv_heads, kv_head = item - tile * a.cache.kv_heads;
+        const int tile0 = off, tile1 = (int)min((int64_t)f.keys, off + left);
+        left -= tile1 - tile0;
+        const bool whole = tile0 == 0 && tile1 == f.keys;
+        // the page of this lane's four keys of a tile
         const int32_t *const table = a.sequences.pages + sequence * a.sequences.ld_pages;
-        struct Pages { int k, v; };
-        auto pages_at = [&](int t) {
-            auto page_of = [&](int key) {
-                if (t >= tile1 || key >= p.last) return -1;
-                const int page = table[key >> a.cache.shift];
-                return (uint32_t)page < (uint64_t)a.cache.pages ? page : -1;
-            };
-            const int key0 = p.first + t * KV_TILE;
-            return Pages{page_of(key0 + 4 * n), page_of(key0 + 4 * (lane >> 2))};
+        auto page_at = [&](int t) {
+            const int key = f.first + t * KV_TILE + 4 * n;
+            if (t >= tile1 || key >= f.last) return -1;
+            const int page = table[key >> a.cache.shift];
+            return (uint32_t)page < (uint64_t)a.cache.pages ? page : -1;
         };
         u32x4 kc[4][KS], vc[DB], ks[KS], vq[KS];
         uint8_t vb[DB];
-        const int64_t head_rows = (int64_t)kv_head << a.cache.shift;
-        auto fetch_k = [&](int t, int page) {                                  // (keys that are not there: of page 0)
-            const int64_t at = head_rows + ((p.first + t * KV_TILE + 4 * n) & a.cache.mask), from = max(page, 0);
-            const uint8_t *const c = a.cache.codes[0] + from * a.cache.ld_codes + at * (16 * DB) + 16 * g, *const sc = a.cache.scales[0] + from * a.cache.ld_scales + at * (4 * KS);
+        const int64_t codes0 = ((int64_t)kv_head << a.cache.shift) * (16 * DB) + 16 * g, scales0 = ((int64_t)kv_head << a.cache.shift) * (4 * KS);
+        auto fetch = [&](auto which_, int t, int page) {                       // 0: k, 1: v  (keys that are not there: of page 0)
+            constexpr int WHICH = decltype(which_)::value;
+            const int at = (f.first + t * KV_TILE + 4 * n) & a.cache.mask, from = max(page, 0);
+            const uint8_t *const c = a.cache.codes[WHICH] + codes0 + from * a.cache.ld_codes + at * (16 * DB), *const sc = a.cache.scales[WHICH] + scales0 + from * a.cache.ld_scales + at * (4 * KS);
+            if constexpr (WHICH == 0) {
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+                for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int s = 0; s < KS; ++s)
-                    kc[b][s] = DB % 4 == 0 || 4 * s + g < DB ? *reinterpret_cast<const u32x4 *>(c + 16 * DB * b + 64 * s) : zero;
+                    for (int s = 0; s < KS; ++s)
+                        kc[b][s] = DB % 4 == 0 || 4 * s + g < DB ? *reinterpret_cast<const u32x4 *>(c + 16 * DB * b + 64 * s) : zero;
 #pragma unroll
-            for (int s = 0; s < KS; ++s) ks[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
+                for (int s = 0; s < KS; ++s) ks[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
+            } else {
+#pragma unroll
+                for (int i = 0; i < DB; ++i) vc[i] = *reinterpret_cast<const u32x4 *>(c + 64 * i);
+                if constexpr (DB % 4 == 0) {
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) vq[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < DB; ++i) vb[i] = sc[(4 * i + g) / DB * (4 * KS) + (4 * i + g) % DB];
+                }
+            }
         };
+        constexpr std::integral_constant<int, 0> K{};
+        constexpr std::integral_constant<int, 1> V{};
         auto k_scale = [&](int b, int s) {                                     // of key b, block 4 s + g
             const uint32_t word = KS == 1 ? ks[0][b] : ks[b / 2][b % 2 * 2 + s];
             return DB % 4 == 0 || 4 * s + g < DB ? (int)(word >> 8 * g) : 127;
         };
-        // v: piece 4 i + lane % 4 of the 4 DB pieces of four keys
-        auto v_key = [&](int i) { return DB % 4 == 0 ? 4 * i / DB : (4 * i + (lane & 3)) / DB; };
-        auto v_block = [&](int i) { return DB % 4 == 0 ? 4 * i % DB + (lane & 3) : (4 * i + (lane & 3)) % DB; };
-        auto fetch_v = [&](int t, int page) {
-            const int64_t at = head_rows + ((p.first + t * KV_TILE + 4 * (lane >> 2)) & a.cache.mask), from = max(page, 0);
-            const uint8_t *const c = a.cache.codes[1] + from * a.cache.ld_codes + at * (16 * DB) + 16 * (lane & 3), *const sc = a.cache.scales[1] + from * a.cache.ld_scales + at * (4 * KS);
-#pragma unroll
-            for (int i = 0; i < DB; ++i) vc[i] = *reinterpret_cast<const u32x4 *>(c + 64 * i);
-            if constexpr (DB % 4 == 0) {
-#pragma unroll
-                for (int s = 0; s < KS; ++s) vq[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
-            } else {
-#pragma unroll
-                for (int i = 0; i < DB; ++i) vb[i] = sc[4 * KS * v_key(i) + v_block(i)];
-            }
-        };
+        // v: piece 4 i + g of the 4 DB pieces of four keys
+        auto v_key = [&](int i, int g) { return DB % 4 == 0 ? 4 * i / DB : (4 * i + g) / DB; };
+        auto v_block = [&](int i, int g) { return DB % 4 == 0 ? 4 * i % DB + g : (4 * i + g) % DB; };
         auto v_scale = [&](int i) -> uint32_t {
             if constexpr (DB % 4 == 0) {
                 const int word = 4 * i / DB * KS + i % KS;                     // (of key 4 i / DB, blocks 4 (i % KS) on)
-                return vq[word / 4][word % 4] >> 8 * (lane & 3) & 255;
+                return vq[word / 4][word % 4] >> 8 * g & 255;
             } else {
                 return vb[i];
             }
         };
-        Pages pages = pages_at(tile0 + wave), pages_next = pages_at(tile0 + wave + FEW_WAVES);
-        if (tile0 + wave < tile1) {
-            fetch_k(tile0 + wave, pages.k);
-            fetch_v(tile0 + wave, pages.v);
-        }
+        int page = page_at(tile0 + wave), page_next = page_at(tile0 + wave + FEW_WAVES);
+        if (tile0 + wave < tile1) fetch(K, tile0 + wave, page), fetch(V, tile0 + wave, page);
         // this lane's row
         const int r = tile * FEW_ROWS + n;
-        const bool there = r < p.rows;
-        const int in_row = (uint32_t)(there ? r : 0) / (uint32_t)a.group, token = p.start + in_row, head = kv_head * a.group + (there ? r : 0) - in_row * a.group;
+        const bool there = r < f.rows;
+        const int in_row = (uint32_t)(there ? r : 0) / (uint32_t)a.group, token = f.start + in_row, head = kv_head * a.group + (there ? r : 0) - in_row * a.group;
         int lo, hi;
-        seen_keys(a, p.length, p.ahead + token, lo, hi);
-        if (!there) lo = p.first, hi = p.last;                                 // (its sums go nowhere)
+        seen_keys(a, f.length, f.ahead + token, lo, hi);
+        if (!there) lo = f.first, hi = f.last;                                 // (its sums go nowhere)
         QBlock<4> q[KS];
         bool fine = true;
 #pragma unroll
@@ -136,47 +157,51 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
 #pragma unroll
         for (int i = 0; i < 2 * DB; ++i) acc[i] = f32x4{0, 0, 0, 0};
         float top = -INFINITY, sum = 0.0f;
-        uint32_t spoiled = 0;                                                  // blocks of this lane's row with a seen value that is not finite
+        uint32_t spoil = 0;                                                    // blocks of this lane's row with a seen value that is not finite
         unsigned char *const lds = smem[wave];
-        // v to LDS; special: not all keys there, or other powers than fp16 has
-        auto put = [&](auto special_, auto f16_, int key0, bool v_there) {
+        // half of v's keys (those with the same b / 2) to LDS; special: not all keys there, or other powers than fp16 has
+        auto put = [&](auto special_, auto f16_, auto half_, int key0, bool v_there) {
             constexpr bool SPECIAL = decltype(special_)::value, F16 = decltype(f16_)::value;
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                const int key = 4 * (lane >> 2) + v_key(i), block = v_block(i);
+            constexpr int HALF = decltype(half_)::value;
+            const int g = SPECIAL ? fresh(lane >> 4) : lane >> 4, n = SPECIAL ? fresh(lane & 15) : lane & 15;
+            static_for<0, DB>([&](auto i_) {
+                constexpr int i = decltype(i_)::value;
+                if constexpr (DB % 2 == 0 && i / (DB / 2) != HALF) return;
+                const int four = v_key(i, g), key = 4 * n + four, block = v_block(i, g);
+                if (DB % 2 && four / 2 != HALF) return;
                 u32x4 codes = vc[i];
                 uint32_t byte = v_scale(i);
                 if constexpr (SPECIAL) {
-                    bool ok = v_there && key0 + key < p.last;
+                    bool ok = v_there && key0 + key < f.last;
                     if constexpr (!F16) {
                         const bool bad = ok && byte >= KV_V_LIMIT;
                         uint64_t bads = __builtin_amdgcn_ballot_w64(bad);
                         while (bads) {
                             const int from = __builtin_ctzll(bads), bad_key = __builtin_amdgcn_readlane(key, from), bad_block = __builtin_amdgcn_readlane(block, from);
                             bads &= bads - 1;
-                            if (key0 + bad_key >= lo && key0 + bad_key < hi) spoiled |= 1u << bad_block;
+                            if (key0 + bad_key >= lo && key0 + bad_key < hi) spoil |= 1u << bad_block;
                         }
                         ok = ok && !bad;
                     }
                     if (!ok) codes = zero, byte = 127;
                 }
                 const float sc = __uint_as_float(byte << 23);
-                unsigned char *const to = lds + (16 * (key & 3) + (key >> 2)) * PITCH + 64 * block;
+                unsigned char *const to = lds + (16 * (four & 1) + n) * PITCH + 64 * block;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) *reinterpret_cast<u32x4 *>(to + 16 * w) = F16 ? mx_halves8(codes[w], sc) : mx_values8(codes[w], sc);
-            }
+            });
         };
         // weights and sums of a tile
-        auto take = [&](auto special_, bool halves, f32x4 (&s)[4], int key0, uint32_t fours) {
+        auto take = [&](auto special_, bool halves, f32x4 (&s)[4], int t, uint32_t fours, int page_next) {
             constexpr bool SPECIAL = decltype(special_)::value;
+            const int key0 = f.first + t * KV_TILE;
             if constexpr (SPECIAL) {
+                const int g4 = fresh(4 * g), from = lo - key0 - 4 * g4, past = hi - key0 - 4 * g4;
+                const uint32_t mine = fours >> g4;
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = key0 + 16 * g + 4 * i + b;
-                        s[b][i] = (fours >> (4 * g + i) & 1) && key >= lo && key < hi ? s[b][i] : -INFINITY;
-                    }
+                    for (int i = 0; i < 4; ++i) s[b][i] = (mine >> i & 1) && 4 * i + b >= from && 4 * i + b < past ? s[b][i] : -INFINITY;
             }
             float most = -INFINITY;
 #pragma unroll
@@ -185,6 +210,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, s[b][i]);
             most = fmaxf(across_rows(most, OpMax()) * scale, top);
             if (__builtin_amdgcn_ballot_w64(most > top)) {
+                asm volatile("" ::: "memory");                                 // (and this)
                 const float shrink = most > top ? __builtin_amdgcn_exp2f(top - most) : 1.0f;
                 sum *= shrink;
 #pragma unroll
@@ -201,9 +227,15 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                     sum += one;
                     w[b / 2][b % 2 * 4 + i] = one;
                 }
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const unsigned char *const at = lds + (32 * half + 4 * g + n / 4) * PITCH + 8 * (n % 4);
+            static_for<0, 2>([&](auto half_) {
+                constexpr int half = decltype(half_)::value;
+                __builtin_amdgcn_wave_barrier();
+                if constexpr (!SPECIAL) put(std::false_type{}, std::true_type{}, half_, key0, true);
+                else if (halves) put(std::true_type{}, std::true_type{}, half_, key0, fours >> n & 1);
+                else put(std::true_type{}, std::false_type{}, half_, key0, fours >> n & 1);
+                if (half == 1 && t + FEW_WAVES < tile1) fetch(V, t + FEW_WAVES, page_next);
+                __builtin_amdgcn_wave_barrier();
+                const unsigned char *const at = lds + (4 * g + n / 4) * PITCH + 8 * (n % 4);
                 if (!SPECIAL || halves) {
                     const f16x8 p16 = weights_f16(w[half]);
 #pragma unroll
@@ -219,50 +251,43 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                         acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high, acc[d], 0, 0, 0);
                     }
                 }
-            }
+            });
         };
         for (int t = tile0 + wave; t < tile1; t += FEW_WAVES) {
-            const Pages ahead = pages_at(t + 2 * FEW_WAVES);
-            const int key0 = p.first + t * KV_TILE;
-            const uint32_t fours = (uint32_t)__builtin_amdgcn_ballot_w64(pages.k >= 0) & 0xffffu;
+            const int ahead = page_at(t + 2 * FEW_WAVES);
+            const int key0 = f.first + t * KV_TILE;
+            const uint32_t fours = (uint32_t)__builtin_amdgcn_ballot_w64(page >= 0) & 0xffffu;
             f32x4 s[4];
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                s[b] = f32x4{0, 0, 0, 0};
+            for (int b = 0; b < 4; ++b) s[b] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int term = 3; term >= 0; --term)
+            for (int term = 3; term >= 0; --term)
 #pragma unroll
-                    for (int k = 0; k < KS; ++k) {
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
                         const u32x4 c = kc[b][k];
                         const u32x6 x = q[k].codes[term];
                         const i32x8 kv = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}, qv = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
                         s[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv, s[b], 4, 2, 0, k_scale(b, k), 0, q[k].scale - Q_STEP[term]);
                     }
-            }
-            bool usual = true;                                                 // all in fp16
+            // (here, not where they are needed: k's registers are free from here on)
+            asm volatile("" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
+            if (t + FEW_WAVES < tile1) fetch(K, t + FEW_WAVES, page_next);
+            __builtin_amdgcn_sched_barrier(0);
+            bool usual = true;                                                 // all in fp16 (keys that are not there count, too: they may make the tile a special one)
 #pragma unroll
             for (int i = 0; i < DB; ++i) usual = usual && v_scale(i) >= F16_LOW && v_scale(i) <= F16_HIGH;
-            // (keys that are not there count, too: they may make the tile a special one)
             const bool halves = __builtin_amdgcn_ballot_w64(!usual) == 0;
-            const bool plain = halves && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all;
-            if (plain) put(std::false_type{}, std::true_type{}, key0, true);
-            else if (halves) put(std::true_type{}, std::true_type{}, key0, pages.v >= 0);
-            else put(std::true_type{}, std::false_type{}, key0, pages.v >= 0);
-            if (t + FEW_WAVES < tile1) {
-                fetch_k(t + FEW_WAVES, pages_next.k);
-                fetch_v(t + FEW_WAVES, pages_next.v);
-            }
-            __builtin_amdgcn_wave_barrier();
-            if (plain) take(std::false_type{}, true, s, key0, fours);
-            else take(std::true_type{}, halves, s, key0, fours);
-            __builtin_amdgcn_wave_barrier();
-            pages = pages_next;
-            pages_next = ahead;
+            if (halves && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all) take(std::false_type{}, true, s, t, fours, page_next);
+            else take(std::true_type{}, halves, s, t, fours, page_next);
+            page = page_next;
+            page_next = ahead;
         }
         sum = across_rows(sum, OpAdd());
 #pragma unroll
         for (int d = 0; d < 2 * DB; ++d) {
-            if (spoiled >> d / 2 & 1) acc[d] = f32x4{NAN, NAN, NAN, NAN};
+            if (spoil >> d / 2 & 1) acc[d] = f32x4{NAN, NAN, NAN, NAN};
             *reinterpret_cast<f32x4 *>(lds + (n * (D + 4) + 16 * d + 4 * g) * 4) = acc[d];
         }
         if (g == 0) red[wave][n] = make_float2(top - WEIGHT_LIFT, sum);
@@ -270,62 +295,92 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
         // the waves' sums: 8 elements of a row a thread
         for (int unit = tid; unit < 4 * DB * FEW_ROWS; unit += 64 * FEW_WAVES) {
             const int row = unit / (4 * DB), at = unit % (4 * DB) * 8, mine = tile * FEW_ROWS + row;
-            if (mine >= p.rows) continue;
+            if (mine >= f.rows) continue;
             float m = -INFINITY, l = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
             for (int w = 0; w < FEW_WAVES; ++w) m = fmaxf(m, red[w][row].x);
             const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll
             for (int w = 0; w < FEW_WAVES; ++w) {
-                const float f = __builtin_amdgcn_exp2f(red[w][row].x - base);
-                l = fmaf(red[w][row].y, f, l);
+                const float shrink = __builtin_amdgcn_exp2f(red[w][row].x - base);
+                l = fmaf(red[w][row].y, shrink, l);
                 const float *const o = reinterpret_cast<const float *>(smem[w]) + row * (D + 4) + at;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = fmaf(o[e], f, y[e]);
+                for (int e = 0; e < 8; ++e) y[e] = fmaf(o[e], shrink, y[e]);
             }
-            if (p.parts > 1) {
-                const int64_t slot = (((int64_t)place * a.cache.kv_heads + kv_head) * a.few.splits + split) * FEW_ROWS + row;
+            if (whole) {
+                put_row<DB>(a, f.start, kv_head, mine, at, m, l, y);
+            } else {                                                           // an item's first part is its workgroup's last
+                const int64_t slot = (int64_t)(2 * workgroup + (tile0 == 0)) * FEW_ROWS + row;
                 store8<false>(a.few.part, slot * D + at, y);
-                if (at == 0) {
-                    const int64_t all = (int64_t)a.sequences.count * a.few.tiles * a.cache.kv_heads * a.few.splits * FEW_ROWS;
-                    reinterpret_cast<float2 *>(a.few.part + all * D)[slot] = make_float2(m, l);
-                }
-                continue;
+                if (at == 0) reinterpret_cast<float2 *>(a.few.part + (int64_t)2 * a.few.splits * FEW_ROWS * D)[slot] = make_float2(m, l);
             }
-            put_row<DB>(a, p, kv_head, mine, at, m, l, y);
         }
         __syncthreads();
     }
 }
 
-// The parts of a row: a thread has 8 elements of every 16th (or, with DB threads of 4 to an element's run, as many as fit 256) part.
+// The parts of a row: a thread has 8 elements of some of the parts.
 template <int DB, int ROWS>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
 {
     constexpr int D = 32 * DB, RUNS = 4 * DB, WAYS = 256 / RUNS;
     __shared__ __attribute__((aligned(16))) float part[WAYS][RUNS][8];
     __shared__ float sums[WAYS];
-    const AttentionCut &cut = ROWS == FEW_ROWS ? a.few : a.many;
-    const int kv_head = blockIdx.y, place = a.first + blockIdx.z, row = blockIdx.x;
-    int sequence = (uint32_t)place / (uint32_t)cut.tiles, tile = place - sequence * cut.tiles;
-    int64_t places = (int64_t)a.sequences.count * cut.tiles;
-    if (ROWS == MANY_ROWS) sequence = find_tile(a, place, tile), places = cut.tiles;
-    TilePlan p;
-    if (sequence < 0 || !tile_plan<ROWS>(a, cut, sequence, tile, p) || p.parts == 1 || tile * ROWS + row >= p.rows) return;
-    const int64_t slot = ((int64_t)place * a.cache.kv_heads + kv_head) * cut.splits * ROWS + row;
-    const float2 *const pairs = reinterpret_cast<const float2 *>(cut.part + places * a.cache.kv_heads * cut.splits * ROWS * D) + slot;
-    const int lane = threadIdx.x & 63, way = threadIdx.x / RUNS, run = threadIdx.x - way * RUNS;
+    const int kv_head = blockIdx.y, place = a.first + blockIdx.z, lane = threadIdx.x & 63;
+    int parts, start, row = blockIdx.x;
+    int64_t slot0, slot1, step, slots;                                         // of the first part, the second; from then on; of all
+    if constexpr (ROWS == FEW_ROWS) {
+        const int sequence = (uint32_t)place / (uint32_t)a.few.tiles;
+        const FewSequence f = few_sequence(a, sequence);
+        const int tile = place - sequence * a.few.tiles;
+        if (tile * ROWS + row >= f.rows || f.keys <= FEW_WHOLE) return;
+        int64_t begin;
+        const int64_t total = few_total(a, sequence, begin);
+        begin += ((int64_t)tile * a.cache.kv_heads + kv_head) * f.keys;
+        const int workgroups = few_workgroups(a, total);
+        // the cuts inside: from the first that is behind the item's begin and stays there on
+        int w = (int)((double)begin / ((double)total / (double)workgroups));
+        w = max(w - 1, 0);
+        while (w < workgroups && few_cut(w, workgroups, total) - begin < FEW_EDGE) ++w;
+        int past = min((int)((double)(begin + f.keys - FEW_EDGE) / ((double)total / (double)workgroups)) + 2, workgroups);
+        while (past > w && few_cut(past - 1, workgroups, total) - begin > f.keys - FEW_EDGE) --past;
+        parts = 1 + past - w;
+        slot0 = (int64_t)(2 * (w - 1) + 1) * ROWS + row;
+        slot1 = (int64_t)(2 * w) * ROWS + row;
+        step = 2 * ROWS;
+        slots = (int64_t)2 * a.few.splits * ROWS;
+        start = f.start;
+        row += tile * ROWS;
+    } else {
+        int tile;
+        const int sequence = find_tile(a, place, tile);
+        TilePlan p;
+        if (sequence < 0 || !tile_plan(a, sequence, tile, p) || tile * ROWS + row >= p.rows) return;
+        parts = p.parts;
+        slot0 = ((int64_t)place * a.cache.kv_heads + kv_head) * a.many.splits * ROWS + row;
+        slot1 = slot0 + ROWS;
+        step = ROWS;
+        slots = (int64_t)a.many.tiles * a.cache.kv_heads * a.many.splits * ROWS;
+        start = p.start;
+        row += tile * ROWS;
+    }
+    if (parts == 1) return;
+    const float *const from = ROWS == FEW_ROWS ? a.few.part : a.many.part;
+    const float2 *const pairs = reinterpret_cast<const float2 *>(from + slots * D);
+    auto slot = [&](int s) { return s == 0 ? slot0 : slot1 + (s - 1) * step; };
+    const int way = threadIdx.x / RUNS, run = threadIdx.x - way * RUNS;
     // (every wave finds the largest score)
     float m = -INFINITY;
-    for (int s = lane; s < p.parts; s += 64) m = fmaxf(m, pairs[(int64_t)s * ROWS].x);
+    for (int s = lane; s < parts; s += 64) m = fmaxf(m, pairs[slot(s)].x);
     m = group_allreduce<64>(m, OpMax());
     const float base = m == -INFINITY ? 0.0f : m;
     float l = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (way < WAYS) {
-        for (int s = way; s < p.parts; s += WAYS) {
-            const float2 one = pairs[(int64_t)s * ROWS];
+        for (int s = way; s < parts; s += WAYS) {
+            const float2 one = pairs[slot(s)];
             float o[8];
-            load8<false>(cut.part, (slot + (int64_t)s * ROWS) * D + 8 * run, o);
+            load8<false>(from, slot(s) * D + 8 * run, o);
             const float f = __builtin_amdgcn_exp2f(one.x - base);
             l = fmaf(one.y, f, l);
 #pragma unroll
@@ -337,19 +392,19 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
     }
     __syncthreads();
     if (way != 0) return;
-    for (int w = 1; w < WAYS && w < p.parts; ++w) {
+    for (int w = 1; w < WAYS && w < parts; ++w) {
         l += sums[w];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] += part[w][run][e];
     }
-    put_row<DB>(a, p, kv_head, tile * ROWS + row, 8 * run, m, l, y);
+    put_row<DB>(a, start, kv_head, row, 8 * run, m, l, y);
 }
 
 }  // namespace sbits
 
 // Which kernel takes which sequence: of several, those of up to FEW_MOST rows (tokens times heads of a key's head) go to the kernel of few rows, the others to that of many.
 // Hints of the most rows spare one of the two launches; each kernel is right for any number.
-constexpr int64_t FEW_MOST = 64;
+static constexpr int64_t FEW_MOST = 64;
 
 size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache, const sbits_sequences &sequences, int64_t tokens, int heads, sbits::AttentionArgs &a)
 {
@@ -358,48 +413,50 @@ size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache,
     const int64_t there = std::min<int64_t>((int64_t)sequences.max_pages * cache.page_tokens, INT32_MAX);
     const int64_t length = sequences.max_length ? std::min<int64_t>(sequences.max_length, there) : there;
     const int64_t cus = ctx->cus ? ctx->cus : 256;
-    // parts of about as many tiles of keys as make `wanted` workgroups of the longest sequences there may be
-    auto cut = [&](AttentionCut &c, int64_t items, int64_t least, int64_t wanted) {
-        const int64_t keys = length / KV_TILE + 1;
-        c.each = (int)std::min(std::max(keys * items / wanted, least), std::max(keys, least));
-        c.splits = (int)std::min<int64_t>((keys + c.each - 1) / c.each, KV_MAX_PARTS);
-    };
-    a.few = a.many = {0, 1, 1, 0, INT32_MAX, nullptr};
+    const int64_t keys = (length + KV_TILE - 1) / KV_TILE;
+    a.few = a.many = {0, 0, 1, 0, 0, INT32_MAX, nullptr};
     const bool only_few = new_most * group <= FEW_MOST, only_many = !only_few && sequences.count == 1;
     if (!only_many) {
         a.few.tiles = (int)((std::min(new_most * group, FEW_MOST) + FEW_ROWS - 1) / FEW_ROWS);
-        cut(a.few, (int64_t)sequences.count * a.few.tiles * cache.kv_heads, FEW_LEAST, 4 * cus);
-        if (!only_few) a.few.most_rows = (int)FEW_MOST;
+        a.few.most_rows = (int)(only_few ? INT32_MAX : FEW_MOST);
+        a.few.rows = (int)std::min<int64_t>(FEW_ROWS, tokens * group);
+        // (as many workgroups as run at a time; their parts' join where items may be cut)
+        a.few.splits = (int)std::min(2 * cus, std::max<int64_t>(1, (int64_t)sequences.count * a.few.tiles * cache.kv_heads * keys / FEW_LEAST));
+        a.few.each = keys > FEW_WHOLE;
     }
     if (!only_few) {
         const int64_t tiles = tokens * group / MANY_ROWS + sequences.count;
         a.many.tiles = (int)std::min<int64_t>(tiles, INT32_MAX);
-        cut(a.many, tiles * cache.kv_heads, MANY_LEAST, 2 * cus);
+        // parts that make up to two workgroups a CU
+        a.many.splits = (int)std::min<int64_t>(std::max<int64_t>(std::min(2 * cus / (tiles * cache.kv_heads), keys / MANY_LEAST), 1), KV_MAX_PARTS);
+        a.many.each = a.many.splits > 1 ? (int)std::max<int64_t>((keys + a.many.splits - 1) / a.many.splits, MANY_LEAST) : 0;
         if (!only_many) a.many.least_rows = (int)FEW_MOST + 1;
     }
-    return sbits_kv_attention_part(a.few, FEW_ROWS, cache, sequences.count) + sbits_kv_attention_part(a.many, MANY_ROWS, cache, sequences.count);
+    return sbits_kv_attention_part(a.few, FEW_ROWS, cache) + sbits_kv_attention_part(a.many, MANY_ROWS, cache);
 }
 
 template <int DB>
 static int launch(sbits_ctx *ctx, sbits::AttentionArgs &a)
 {
     using namespace sbits;
-    auto enqueue = [&](auto kernel, int x, int64_t places, int threads) -> int {
+    auto join = [&](auto kernel, int x, int64_t places) -> int {
         const int64_t most = kv_launch(x, a.cache.kv_heads);
         for (int64_t first = 0; first < places; first += most) {
             a.first = (int)first;
             const dim3 grid(x, a.cache.kv_heads, (uint32_t)std::min(places - first, most));
-            hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, ctx->stream, a);
+            hipLaunchKernelGGL(kernel, grid, dim3(256), 0, ctx->stream, a);
             SBITS_HIP(ctx, hipGetLastError());
         }
         return SBITS_OK;
     };
-    const int64_t few = (int64_t)a.sequences.count * a.few.tiles;
     int rc;
     if (a.many.tiles && (rc = sbits_launch_kv_attention_many(ctx, a))) return rc;
-    if (few && (rc = enqueue(kv_attention_few_kernel<DB>, a.few.splits, few, 64 * FEW_WAVES))) return rc;
-    if (a.many.splits > 1 && (rc = enqueue(kv_attention_join_kernel<DB, MANY_ROWS>, MANY_ROWS, a.many.tiles, 256))) return rc;
-    if (a.few.splits > 1 && (rc = enqueue(kv_attention_join_kernel<DB, FEW_ROWS>, FEW_ROWS, few, 256))) return rc;
+    if (a.few.tiles) {
+        hipLaunchKernelGGL(kv_attention_few_kernel<DB>, dim3(a.few.splits), dim3(64 * FEW_WAVES), 0, ctx->stream, a);
+        SBITS_HIP(ctx, hipGetLastError());
+    }
+    if (a.many.each && (rc = join(kv_attention_join_kernel<DB, MANY_ROWS>, MANY_ROWS, a.many.tiles))) return rc;
+    if (a.few.each && (rc = join(kv_attention_join_kernel<DB, FEW_ROWS>, a.few.rows, (int64_t)a.sequences.count * a.few.tiles))) return rc;
     return SBITS_OK;
 }
 

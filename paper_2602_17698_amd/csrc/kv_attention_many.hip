@@ -33,7 +33,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     int tile;
     const int sequence = find_tile(a, number, tile);
     TilePlan p;
-    if (sequence < 0 || !tile_plan<MANY_ROWS>(a, a.many, sequence, tile, p) || split >= p.parts) return;
+    if (sequence < 0 || !tile_plan(a, sequence, tile, p) || split >= p.parts) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, h = lane >> 5;
     const u32x4 zero = {0, 0, 0, 0};
     // this lane's row
@@ -188,13 +188,16 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (SPECIAL) {
+            const int h4 = fresh(4 * h), from = lo - key0 - h4, past = hi - key0 - h4;
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < 2; ++m) {
+                const uint32_t mine = (uint32_t)(valid >> 32 * m) >> h4;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int at = 32 * m + 8 * (i / 4) + 4 * h + i % 4, key = key0 + at;
-                    s[m][i] = (valid >> at & 1) && key >= lo && key < hi ? s[m][i] : -INFINITY;
+                    const int at = 8 * (i / 4) + i % 4;
+                    s[m][i] = (mine >> at & 1) && 32 * m + at >= from && 32 * m + at < past ? s[m][i] : -INFINITY;
                 }
+            }
         }
         float most = -INFINITY;
 #pragma unroll

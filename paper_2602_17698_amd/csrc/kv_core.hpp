@@ -133,10 +133,11 @@ struct LoadArgs {
     void *out[2];
     int64_t ld[2], hd[2], tokens;
 };
-// How the rows of a kernel are cut up: tiles of rows (few: of each sequence, workgroups of their own; many: of all), parts of the keys, and of which sequences, by
-// their rows times the heads of a key's head.  part: [tile][kv_heads][part][rows of a tile][dim], then the same of pairs (largest score, sum).
+// How a kernel's work is cut up: tiles of rows (few: at most, of each sequence; many: of all), and of which sequences, by their rows times the heads of a key's head.
+// few: workgroups, among which the keys are shared out; part: [workgroup][2][rows of a tile][dim], then the same of pairs (largest score, sum)
+// many: parts of the keys, of `each` tiles of them at least; part: [tile][kv_heads][part][rows of a tile][dim], then pairs
 struct AttentionCut {
-    int tiles, splits, each;                 // each: tiles of keys of a part, at least
+    int tiles, rows, splits, each;            // rows: of a tile, at most
     int least_rows, most_rows;
     float *part;
 };
@@ -176,33 +177,124 @@ __device__ __forceinline__ void seen_keys(const AttentionArgs &a, int length, in
 struct TilePlan {
     int start, end, rows;                     // the sequence's rows; times heads of a key's head
     int ahead;                                // position of row 0 of all: a row's is that and its number
-    int length, tiles;                        // tiles of rows, in all
+    int length;
     int first, last, keys;                    // keys of this tile of rows, from a multiple of 64 on; tiles of them
     int each, parts;                          // tiles of keys of a part
 };
-template <int ROWS>
-__device__ __forceinline__ bool tile_plan(const AttentionArgs &a, const AttentionCut &cut, int sequence, int tile, TilePlan &p)
+__device__ __forceinline__ bool tile_plan(const AttentionArgs &a, int sequence, int tile, TilePlan &p)
 {
     const int start = a.sequences.starts[sequence], end = a.sequences.starts[sequence + 1];
     p.length = max(a.sequences.lengths[sequence], 0);
     p.start = min(max(start, 0), a.tokens);
     p.end = min(max(end, 0), a.tokens);
     p.rows = (p.end - p.start) * a.group;
-    p.tiles = (p.rows + ROWS - 1) / ROWS;
-    if (tile >= p.tiles || p.rows < cut.least_rows || p.rows > cut.most_rows) return false;
+    if (tile >= (p.rows + MANY_ROWS - 1) / MANY_ROWS || p.rows < a.many.least_rows || p.rows > a.many.most_rows) return false;
     p.ahead = p.length - end;
-    const int r0 = tile * ROWS, r1 = min(r0 + ROWS, p.rows) - 1;
+    const int r0 = tile * MANY_ROWS, r1 = min(r0 + MANY_ROWS, p.rows) - 1;
     int none;
     seen_keys(a, p.length, p.ahead + p.start + r0 / a.group, p.first, none);
     seen_keys(a, p.length, p.ahead + p.start + r1 / a.group, none, p.last);
     p.first &= ~(KV_TILE - 1);
     p.keys = p.last > p.first ? (p.last - p.first + KV_TILE - 1) / KV_TILE : 0;
-    // (more tiles of a sequence than have workgroups: these take several, each with all of its keys)
-    const int most = ROWS == MANY_ROWS || p.tiles <= cut.tiles ? cut.splits : 1;
-    p.each = max((p.keys + most - 1) / most, cut.each);
+    p.each = max((p.keys + a.many.splits - 1) / a.many.splits, a.many.each);
     p.parts = p.keys > p.each ? (p.keys + p.each - 1) / p.each : 1;
     return true;
 }
+
+// ---- sharing out the keys of few rows ----------------------------------------------------
+// An item is a tile of 16 rows of a sequence with a key's head; its work the tiles of keys that the sequence's rows see.  All items, sequence after sequence, a sequence's by tiles of rows,
+// then heads, make a line of W tiles of keys, of which workgroup w of G has those from cut(w) to cut(w + 1):  w (W / G), moved to the item's begin or end where that is less than FEW_EDGE tiles
+// away, and to the begin of an item of up to FEW_WHOLE tiles.  So workgroups have the same to do, whatever the lengths.
+constexpr int FEW_EDGE = 4, FEW_WHOLE = 16, FEW_LEAST = 8;       // FEW_LEAST: tiles of keys a workgroup, at least
+struct FewSequence {
+    int start, rows, ahead, length;           // as in TilePlan
+    int tiles, first, last, keys;             // of rows; keys of all rows, from a multiple of 64 on; tiles of them (an item without keys counts as one)
+};
+__device__ __forceinline__ FewSequence few_sequence(const AttentionArgs &a, int b)
+{
+    FewSequence f;
+    const int start = a.sequences.starts[b], end = a.sequences.starts[b + 1];
+    f.length = max(a.sequences.lengths[b], 0);
+    f.start = min(max(start, 0), a.tokens);
+    const int stop = min(max(end, 0), a.tokens);
+    f.rows = (stop - f.start) * a.group;
+    if (f.rows < 0 || f.rows > a.few.most_rows) f.rows = 0;
+    f.ahead = f.length - end;
+    f.tiles = (f.rows + FEW_ROWS - 1) / FEW_ROWS;
+    int none;
+    seen_keys(a, f.length, f.ahead + f.start, f.first, none);
+    seen_keys(a, f.length, f.ahead + stop - 1, none, f.last);
+    f.first &= ~(KV_TILE - 1);
+    f.keys = f.last > f.first ? (f.last - f.first + KV_TILE - 1) / KV_TILE : 1;
+    return f;
+}
+__device__ __forceinline__ int64_t few_weight(const AttentionArgs &a, const FewSequence &f) { return (int64_t)f.tiles * a.cache.kv_heads * f.keys; }
+// a number that is the same in all lanes, as one that the compiler knows to be
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+__device__ __forceinline__ int64_t lane_sum(int64_t v, int64_t &all)         // of the lanes up to this one; of all
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) {
+        const int64_t other = __shfl_up(v, i);
+        if (lane >= i) v += other;
+    }
+    all = uniform(__shfl(v, 63));
+    return v;
+}
+// W, and the place where `sequence` begins
+__device__ __forceinline__ int64_t few_total(const AttentionArgs &a, int sequence, int64_t &begin)
+{
+    begin = 0;
+    if (a.sequences.count == 1) return few_weight(a, few_sequence(a, 0));
+    int64_t total = 0;
+    for (int first = 0; first < a.sequences.count; first += 64) {
+        const int b = first + (threadIdx.x & 63);
+        int64_t all;
+        const int64_t mine = b < a.sequences.count ? few_weight(a, few_sequence(a, b)) : 0, end = lane_sum(mine, all);
+        if (sequence >= first && sequence < first + 64) begin = total + uniform(__shfl(end - mine, sequence - first));
+        total += all;
+    }
+    return total;
+}
+// the sequence that has place x of the line (x < W), and its begin
+__device__ __forceinline__ int few_find(const AttentionArgs &a, int64_t x, int64_t &begin)
+{
+    begin = 0;
+    if (a.sequences.count == 1) return 0;
+    for (int first = 0; first < a.sequences.count; first += 64) {
+        const int b = first + (threadIdx.x & 63);
+        const int64_t mine = b < a.sequences.count ? few_weight(a, few_sequence(a, b)) : 0;
+        int64_t all;
+        const int64_t end = lane_sum(mine, all);
+        const uint64_t past = __builtin_amdgcn_ballot_w64(begin + end > x);
+        if (past) {
+            const int lane = __builtin_ctzll(past);
+            begin += uniform(__shfl(end - mine, lane));
+            return first + lane;
+        }
+        begin += all;
+    }
+    return -1;
+}
+__device__ __forceinline__ int few_workgroups(const AttentionArgs &a, int64_t total)
+{
+    const int64_t most = total / FEW_LEAST;
+    return most >= a.few.splits ? a.few.splits : most < 1 ? 1 : (int)most;
+}
+// A number of a lane's that the compiler takes for a new one: what is computed from it stays where it is, and is not kept in registers over a loop.
+__device__ __forceinline__ int fresh(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+// Where cut w of G falls ahead of its move (w < G): a product in 64 bits, rounded down, which is the same wherever it is asked for.
+__device__ __forceinline__ int64_t few_cut(int w, int workgroups, int64_t total) { return (int64_t)((double)w * ((double)total / (double)workgroups)); }
+// what a cut at `off` tiles of an item of `keys` becomes
+__device__ __forceinline__ int few_snap(int off, int keys) { return off < FEW_EDGE || keys <= FEW_WHOLE ? 0 : keys - off < FEW_EDGE ? keys : off; }
 
 // The tiles of many rows of all sequences are numbered so that sequence b's begin at floor(rows ahead of it / MANY_ROWS) + b, which leaves each as many as
 // it can need.  The sequence and the tile of a number, -1 if there is none.
@@ -239,51 +331,59 @@ typedef float f32x32 __attribute__((ext_vector_type(32)));
 constexpr int Q_STEP[4] = {0, 4, 10, 16};
 template <int TERMS>
 struct QBlock { u32x6 codes[TERMS]; int scale; };                             // scale: the first term's byte
+typedef __bf16 bf16x32 __attribute__((ext_vector_type(32)));
+typedef unsigned int u32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+// (what a term leaves of bf16 is bf16: in pairs all along, as this is where a kernel would need most registers)
 template <int TERMS>
-__device__ __forceinline__ QBlock<TERMS> split_q(const float (&x)[32])
+__device__ __forceinline__ QBlock<TERMS> split_q(u32x16 x, uint32_t top)
 {
-    f32x16 a, b;
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        a[i] = x[2 * i];
-        b[i] = x[2 * i + 1];
-        top = max(top, __float_as_uint(a[i]) & 0x7fffffffu);
-        top = max(top, __float_as_uint(b[i]) & 0x7fffffffu);
-    }
     QBlock<TERMS> q;
-    q.scale = max((int)(top >> 23) - 2, 17);
+    q.scale = max((int)(top >> 7) - 2, 17);
 #pragma unroll
     for (int t = 0; t < TERMS; ++t) {
         const float scale = __uint_as_float((uint32_t)(q.scale - Q_STEP[t]) << 23);
-        q.codes[t] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(a, b, scale);
+        q.codes[t] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(__builtin_bit_cast(bf16x32, x), scale);
         if (t == TERMS - 1) break;
-        const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q.codes[t], scale);
+        const u32x16 back = __builtin_bit_cast(u32x16, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(q.codes[t], scale));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            a[i] -= back[2 * i];
-            b[i] -= back[2 * i + 1];
-        }
+        for (int i = 0; i < 16; ++i)
+            x[i] = bf16_pair(__uint_as_float(x[i] << 16) - __uint_as_float(back[i] << 16), __uint_as_float(x[i] & 0xffff0000u) - __uint_as_float(back[i] & 0xffff0000u));
     }
     return q;
+}
+__device__ __forceinline__ uint32_t largest_half(const u32x16 &x)
+{
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[i] & 0x7fff7fffu));
+    return max(top.x, top.y);
 }
 // Block `block` of a row of q, zeros if it is not there; fine: whether all values are finite (others become 0).
 template <int TERMS>
 __device__ __forceinline__ QBlock<TERMS> load_q(const AttentionArgs &a, bool there, int token, int head, int block, bool &fine)
 {
-    float x[32];
+    u32x16 x = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    if (there) {
+        const u32x4 *const from = reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q.at) + (int64_t)token * a.q.ld + (int64_t)head * a.q.hd + 32 * block);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (there) load8<true>(a.q.at, (int64_t)token * a.q.ld + (int64_t)head * a.q.hd + 32 * block + 8 * i, v);
+        for (int i = 0; i < 4; ++i) {
+            const u32x4 v = from[i];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const bool ok = (__float_as_uint(v[e]) & 0x7f800000u) != 0x7f800000u;
-            fine = fine && ok;
-            x[8 * i + e] = ok ? v[e] : 0.0f;
+            for (int e = 0; e < 4; ++e) x[4 * i + e] = v[e];
         }
     }
-    return split_q<TERMS>(x);
+    uint32_t top = largest_half(x);
+    if (top >= 0x7f80) {
+        fine = false;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if ((x[i] & 0x7f80u) == 0x7f80u) x[i] &= 0xffff0000u;
+            if ((x[i] & 0x7f800000u) == 0x7f800000u) x[i] &= 0xffffu;
+        }
+        top = largest_half(x);
+    }
+    return split_q<TERMS>(x, top);
 }
 
 // ---- sums: v in fp16 where that is exact, else in bf16 ----------------------------------
@@ -342,10 +442,11 @@ __device__ __forceinline__ s16x8 read_transposed(const unsigned char *at, int st
 int sbits_launch_rotate(sbits_ctx *ctx, const sbits::RotateArgs &a, bool bf16, bool wide);
 int sbits_launch_kv_store(sbits_ctx *ctx, const sbits::StoreArgs &a, bool bf16);
 int sbits_launch_kv_load(sbits_ctx *ctx, const sbits::LoadArgs &a, bool bf16);
-// bytes of the parts of a kernel's tiles (few: tiles of each of `sequences`)
-inline size_t sbits_kv_attention_part(const sbits::AttentionCut &cut, int rows, const sbits_kv_cache &cache, int64_t sequences)
+// bytes of a kernel's parts
+inline size_t sbits_kv_attention_part(const sbits::AttentionCut &cut, int rows, const sbits_kv_cache &cache)
 {
-    return cut.splits <= 1 ? 0 : (size_t)((int64_t)cut.tiles * (rows == sbits::FEW_ROWS ? sequences : 1) * cache.kv_heads * cut.splits) * rows * (cache.head_dim + 2) * 4;
+    if (cut.each == 0) return 0;
+    return (size_t)(rows == sbits::FEW_ROWS ? 2 * cut.splits : (int64_t)cut.tiles * cache.kv_heads * cut.splits) * rows * (cache.head_dim + 2) * 4;
 }
 // how an attention is cut up; the workspace of its parts in bytes
 size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache, const sbits_sequences &sequences, int64_t tokens, int heads, sbits::AttentionArgs &a);
