@@ -517,7 +517,7 @@ int  sbits_expert_layer(sbits_ctx *ctx, const sbits_router *r, const void *logit
  * sbits_mx_scale_pitch(head_dim) bytes of scales, of which those behind the last block may hold
  * anything.  Code row of token t and head h in page p: p * ld_codes + (h * page_tokens + t) *
  * head_dim / 2; scales likewise.  Codes 16-byte aligned, ld_codes a multiple of 16, scales
- * 4-byte aligned, ld_scales a multiple of 4; pitches at least a page long.            */
+ * 4-byte aligned, ld_scales a multiple of 4; pitches at least a page long, below 4 GiB. */
 typedef struct {
     void *k_codes, *k_scales, *v_codes, *v_scales;   /* DEVICE                          */
     int64_t pages;                                   /* 1 .. 2^31 - 1                   */
@@ -601,7 +601,7 @@ int  sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequ
  * hold; a seen value that is not finite makes its block of 32 outputs NaN (in v the bytes 253 and 254 count as 255), a seen key that is
  * not or a q that is not makes the row NaN.  Scores and sums are taken in fp32 on the matrix cores, in an order that goes with the batch's
  * sizes; a call gives the same bits again.  scale > 0.  ws: 256-byte aligned,
- * sbits_kv_attention_ws_bytes() bytes (which may be 0), asked for with the call's own arguments.  Positions from 2^31 - 256 on
+ * sbits_kv_attention_ws_bytes() bytes (which may be 0), asked for with the call's own arguments.  Positions from 2^31 - 4096 on
  * are not there.  With lse, q enters the products in a term more, so that last bits of out may differ.  */
 size_t sbits_kv_attention_ws_bytes(const sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens,
                                    int heads);

@@ -33,8 +33,8 @@ static int check_cache(const sbits_kv_cache *c)
         c->head_dim < 32 || c->head_dim > KV_MAX_DIM || c->head_dim % MX_BLOCK || c->pages < 1 || c->pages > INT32_MAX)
         return SBITS_ERR_BAD_SHAPE;
     const int64_t rows = (int64_t)c->kv_heads * c->page_tokens;
-    if (c->ld_codes < rows * (c->head_dim / 2) || c->ld_codes % 16 || c->ld_codes >= ((int64_t)1 << 40) ||
-        c->ld_scales < rows * sbits_mx_scale_pitch(c->head_dim) || c->ld_scales % 4 || c->ld_scales >= ((int64_t)1 << 40))
+    if (c->ld_codes < rows * (c->head_dim / 2) || c->ld_codes % 16 || c->ld_codes > UINT32_MAX ||
+        c->ld_scales < rows * sbits_mx_scale_pitch(c->head_dim) || c->ld_scales % 4 || c->ld_scales > UINT32_MAX)
         return SBITS_ERR_INVALID_ARG;
     return SBITS_OK;
 }

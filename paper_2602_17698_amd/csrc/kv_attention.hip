@@ -34,16 +34,21 @@ __device__ __forceinline__ void put_row(const AttentionArgs &a, int start, int k
 // lane l then row l % 16 and the keys 16 (l / 16) + 4 r + b.
 // Sums, transposed:  v becomes fp16 or bf16 (exactly) on its way to LDS, 32 keys at a time, key 16 g + 4 r + b to row 16 (b % 2) + 4 g + r, where transposing reads give a lane one element
 // of 8 keys, the ones whose weights it has.
-// A tile's codes of k are asked for when those of the one before have been used, of v likewise; pages' numbers a tile earlier.
+// A tile's codes of k are asked for when those of the one before the one ahead of it have been used, of v likewise; pages' numbers a tile earlier.
 template <int DB>
-__global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(AttentionArgs a)
+struct FewCodes { u32x4 k[4][(DB + 3) / 4], v[DB], ks[(DB + 3) / 4], vq[DB % 4 ? 1 : DB / 4]; uint8_t vb[DB]; };
+
+template <int DB>
+__global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_few_kernel(AttentionArgs a)
 {
+    constexpr int DEPTH = 1;
     constexpr int D = 32 * DB, KS = (DB + 3) / 4, PITCH = 2 * D + 32;          // PITCH: rows 8 banks apart, mod 64 an odd multiple of 8
     __shared__ __attribute__((aligned(16))) unsigned char smem[FEW_WAVES][32 * PITCH];
     __shared__ float2 red[FEW_WAVES][FEW_ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     const u32x4 zero = {0, 0, 0, 0};
     typedef u32x4 __attribute__((aligned(4))) u32x4_by4;
+    using Codes = FewCodes<DB>;
     // this workgroup's share
     int64_t none;
     const int64_t total = few_total(a, -1, none);
@@ -78,58 +83,68 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
         const bool whole = tile0 == 0 && tile1 == f.keys;
         // the page of this lane's four keys of a tile
         const int32_t *const table = a.sequences.pages + sequence * a.sequences.ld_pages;
-        auto page_at = [&](int t) {
-            const int key = f.first + t * KV_TILE + 4 * n;
-            if (t >= tile1 || key >= f.last) return -1;
-            const int page = table[key >> a.cache.shift];
-            return (uint32_t)page < (uint64_t)a.cache.pages ? page : -1;
-        };
-        u32x4 kc[4][KS], vc[DB], ks[KS], vq[KS];
-        uint8_t vb[DB];
-        const int64_t codes0 = ((int64_t)kv_head << a.cache.shift) * (16 * DB) + 16 * g, scales0 = ((int64_t)kv_head << a.cache.shift) * (4 * KS);
-        auto fetch = [&](auto which_, int t, int page) {                       // 0: k, 1: v  (keys that are not there: of page 0)
+        auto key_at = [&](int t) { return f.first + t * KV_TILE + 4 * n; };
+        // (no branch around the load and nothing done with it yet: its number is waited for a tile later, not all loads under way here)
+        auto page_at = [&](int t) { return table[max(min(key_at(t), f.last - 1), 0) >> a.cache.shift]; };
+        auto page_there = [&](int page, int t) { return key_at(t) < f.last && (uint32_t)page < (uint64_t)a.cache.pages; };
+        Codes even, odd;                                                       // odd: of the second of two tiles under way
+        auto fetch = [&](auto which_, Codes &o, int t, int page) {                   // 0: k, 1: v  (keys that are not there: of page 0)
             constexpr int WHICH = decltype(which_)::value;
-            const int at = (f.first + t * KV_TILE + 4 * n) & a.cache.mask, from = max(page, 0);
-            const uint8_t *const c = a.cache.codes[WHICH] + codes0 + from * a.cache.ld_codes + at * (16 * DB), *const sc = a.cache.scales[WHICH] + scales0 + from * a.cache.ld_scales + at * (4 * KS);
+            // (a uniform address and a lane's offset: one product and sum)
+            const uint32_t at = key_at(t) & a.cache.mask, from = (uint32_t)page < (uint64_t)a.cache.pages ? page : 0;
+            const int64_t rows = (int64_t)kv_head << a.cache.shift;
+            const uint8_t *const c = a.cache.codes[WHICH] + rows * (16 * DB) + ((uint64_t)from * (uint32_t)a.cache.ld_codes + (at * (16 * DB) + 16 * g));
+            const uint8_t *const sc = a.cache.scales[WHICH] + rows * (4 * KS) + ((uint64_t)from * (uint32_t)a.cache.ld_scales + at * (4 * KS));
             if constexpr (WHICH == 0) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int s = 0; s < KS; ++s)
-                        kc[b][s] = DB % 4 == 0 || 4 * s + g < DB ? *reinterpret_cast<const u32x4 *>(c + 16 * DB * b + 64 * s) : zero;
+                        o.k[b][s] = DB % 4 == 0 || 4 * s + g < DB ? *reinterpret_cast<const u32x4 *>(c + 16 * DB * b + 64 * s) : zero;
 #pragma unroll
-                for (int s = 0; s < KS; ++s) ks[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
+                for (int s = 0; s < KS; ++s) o.ks[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
             } else {
 #pragma unroll
-                for (int i = 0; i < DB; ++i) vc[i] = *reinterpret_cast<const u32x4 *>(c + 64 * i);
+                for (int i = 0; i < DB; ++i) o.v[i] = *reinterpret_cast<const u32x4 *>(c + 64 * i);
                 if constexpr (DB % 4 == 0) {
 #pragma unroll
-                    for (int s = 0; s < KS; ++s) vq[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
+                    for (int s = 0; s < KS; ++s) o.vq[s] = *reinterpret_cast<const u32x4_by4 *>(sc + 16 * s);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < DB; ++i) vb[i] = sc[(4 * i + g) / DB * (4 * KS) + (4 * i + g) % DB];
+                    for (int i = 0; i < DB; ++i) o.vb[i] = sc[(4 * i + g) / DB * (4 * KS) + (4 * i + g) % DB];
                 }
             }
         };
         constexpr std::integral_constant<int, 0> K{};
         constexpr std::integral_constant<int, 1> V{};
-        auto k_scale = [&](int b, int s) {                                     // of key b, block 4 s + g
-            const uint32_t word = KS == 1 ? ks[0][b] : ks[b / 2][b % 2 * 2 + s];
+        auto k_scale = [&](const Codes &o, int b, int s) {                                     // of key b, block 4 s + g
+            const uint32_t word = KS == 1 ? o.ks[0][b] : o.ks[b / 2][b % 2 * 2 + s];
             return DB % 4 == 0 || 4 * s + g < DB ? (int)(word >> 8 * g) : 127;
         };
         // v: piece 4 i + g of the 4 DB pieces of four keys
         auto v_key = [&](int i, int g) { return DB % 4 == 0 ? 4 * i / DB : (4 * i + g) / DB; };
         auto v_block = [&](int i, int g) { return DB % 4 == 0 ? 4 * i % DB + g : (4 * i + g) % DB; };
-        auto v_scale = [&](int i) -> uint32_t {
+        auto v_scale = [&](const Codes &o, int i) -> uint32_t {
             if constexpr (DB % 4 == 0) {
                 const int word = 4 * i / DB * KS + i % KS;                     // (of key 4 i / DB, blocks 4 (i % KS) on)
-                return vq[word / 4][word % 4] >> 8 * g & 255;
+                return o.vq[word / 4][word % 4] >> 8 * g & 255;
             } else {
-                return vb[i];
+                return o.vb[i];
             }
         };
-        int page = page_at(tile0 + wave), page_next = page_at(tile0 + wave + FEW_WAVES);
-        if (tile0 + wave < tile1) fetch(K, tile0 + wave, page), fetch(V, tile0 + wave, page);
+        // pages of this tile of the wave's, the next, and those behind
+        int page = page_at(tile0 + wave), page_next = page_at(tile0 + wave + FEW_WAVES), page_third = page_at(tile0 + wave + 2 * FEW_WAVES);
+        // (Loads are never in a branch: behind one the compiler would wait for all that are under way.  Where there is no tile to ask for, this one is asked for again.)
+        auto ask = [&](auto which, Codes &o, int t) {
+            const int on = t + DEPTH * FEW_WAVES;
+            fetch(which, o, on < tile1 ? on : t, on >= tile1 ? page : DEPTH == 1 ? page_next : page_third);
+        };
+        fetch(K, even, tile0 + wave, page);
+        fetch(V, even, tile0 + wave, page);
+        if constexpr (DEPTH == 2) {
+            fetch(K, odd, tile0 + wave + FEW_WAVES, page_next);
+            fetch(V, odd, tile0 + wave + FEW_WAVES, page_next);
+        }
         // this lane's row
         const int r = tile * FEW_ROWS + n;
         const bool there = r < f.rows;
@@ -160,7 +175,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
         uint32_t spoil = 0;                                                    // blocks of this lane's row with a seen value that is not finite
         unsigned char *const lds = smem[wave];
         // half of v's keys (those with the same b / 2) to LDS; special: not all keys there, or other powers than fp16 has
-        auto put = [&](auto special_, auto f16_, auto half_, int key0, bool v_there) {
+        auto put = [&](const Codes &o, auto special_, auto f16_, auto half_, int key0, bool v_there) {
             constexpr bool SPECIAL = decltype(special_)::value, F16 = decltype(f16_)::value;
             constexpr int HALF = decltype(half_)::value;
             const int g = SPECIAL ? fresh(lane >> 4) : lane >> 4, n = SPECIAL ? fresh(lane & 15) : lane & 15;
@@ -169,8 +184,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                 if constexpr (DB % 2 == 0 && i / (DB / 2) != HALF) return;
                 const int four = v_key(i, g), key = 4 * n + four, block = v_block(i, g);
                 if (DB % 2 && four / 2 != HALF) return;
-                u32x4 codes = vc[i];
-                uint32_t byte = v_scale(i);
+                u32x4 codes = o.v[i];
+                uint32_t byte = v_scale(o, i);
                 if constexpr (SPECIAL) {
                     bool ok = v_there && key0 + key < f.last;
                     if constexpr (!F16) {
@@ -189,10 +204,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                 unsigned char *const to = lds + (16 * (four & 1) + n) * PITCH + 64 * block;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) *reinterpret_cast<u32x4 *>(to + 16 * w) = F16 ? mx_halves8(codes[w], sc) : mx_values8(codes[w], sc);
+                __builtin_amdgcn_sched_barrier(0);                             // (a piece after the other: registers)
             });
         };
         // weights and sums of a tile
-        auto take = [&](auto special_, bool halves, f32x4 (&s)[4], int t, uint32_t fours, int page_next) {
+        auto take = [&](Codes &o, auto special_, bool halves, f32x4 (&s)[4], int t, uint32_t fours) {
             constexpr bool SPECIAL = decltype(special_)::value;
             const int key0 = f.first + t * KV_TILE;
             if constexpr (SPECIAL) {
@@ -230,17 +246,19 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
             static_for<0, 2>([&](auto half_) {
                 constexpr int half = decltype(half_)::value;
                 __builtin_amdgcn_wave_barrier();
-                if constexpr (!SPECIAL) put(std::false_type{}, std::true_type{}, half_, key0, true);
-                else if (halves) put(std::true_type{}, std::true_type{}, half_, key0, fours >> n & 1);
-                else put(std::true_type{}, std::false_type{}, half_, key0, fours >> n & 1);
-                if (half == 1 && t + FEW_WAVES < tile1) fetch(V, t + FEW_WAVES, page_next);
+                if constexpr (!SPECIAL) put(o, std::false_type{}, std::true_type{}, half_, key0, true);
+                else if (halves) put(o, std::true_type{}, std::true_type{}, half_, key0, fours >> n & 1);
+                else put(o, std::true_type{}, std::false_type{}, half_, key0, fours >> n & 1);
+                if (half == 1) ask(V, o, t);
                 __builtin_amdgcn_wave_barrier();
                 const unsigned char *const at = lds + (4 * g + n / 4) * PITCH + 8 * (n % 4);
                 if (!SPECIAL || halves) {
                     const f16x8 p16 = weights_f16(w[half]);
 #pragma unroll
-                    for (int d = 0; d < 2 * DB; ++d)
+                    for (int d = 0; d < 2 * DB; ++d) {
                         acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, read_transposed(at + 32 * d, 16 * PITCH)), p16, acc[d], 0, 0, 0);
+                        if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                    }
                 } else {
                     bf16x8 high, low;
                     weights_bf16(w[half], high, low);
@@ -253,10 +271,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                 }
             });
         };
-        for (int t = tile0 + wave; t < tile1; t += FEW_WAVES) {
-            const int ahead = page_at(t + 2 * FEW_WAVES);
+        auto step = [&](Codes &o, int t) {
+            const int ahead = page_at(t + 3 * FEW_WAVES);
             const int key0 = f.first + t * KV_TILE;
-            const uint32_t fours = (uint32_t)__builtin_amdgcn_ballot_w64(page >= 0) & 0xffffu;
+            const uint32_t fours = (uint32_t)__builtin_amdgcn_ballot_w64(page_there(page, t)) & 0xffffu;
             f32x4 s[4];
 #pragma unroll
             for (int b = 0; b < 4; ++b) s[b] = f32x4{0, 0, 0, 0};
@@ -266,23 +284,28 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void kv_attention_few_kernel(Att
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
-                        const u32x4 c = kc[b][k];
+                        const u32x4 c = o.k[b][k];
                         const u32x6 x = q[k].codes[term];
                         const i32x8 kv = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}, qv = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
-                        s[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv, s[b], 4, 2, 0, k_scale(b, k), 0, q[k].scale - Q_STEP[term]);
+                        s[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv, s[b], 4, 2, 0, k_scale(o, b, k), 0, q[k].scale - Q_STEP[term]);
                     }
             // (here, not where they are needed: k's registers are free from here on)
             asm volatile("" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
-            if (t + FEW_WAVES < tile1) fetch(K, t + FEW_WAVES, page_next);
+            ask(K, o, t);
             __builtin_amdgcn_sched_barrier(0);
             bool usual = true;                                                 // all in fp16 (keys that are not there count, too: they may make the tile a special one)
 #pragma unroll
-            for (int i = 0; i < DB; ++i) usual = usual && v_scale(i) >= F16_LOW && v_scale(i) <= F16_HIGH;
+            for (int i = 0; i < DB; ++i) usual = usual && v_scale(o, i) >= F16_LOW && v_scale(o, i) <= F16_HIGH;
             const bool halves = __builtin_amdgcn_ballot_w64(!usual) == 0;
-            if (halves && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all) take(std::false_type{}, true, s, t, fours, page_next);
-            else take(std::true_type{}, halves, s, t, fours, page_next);
+            if (halves && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all) take(o, std::false_type{}, true, s, t, fours);
+            else take(o, std::true_type{}, halves, s, t, fours);
             page = page_next;
-            page_next = ahead;
+            page_next = page_third;
+            page_third = ahead;
+        };
+        for (int t = tile0 + wave; t < tile1; t += DEPTH * FEW_WAVES) {
+            step(even, t);
+            if (DEPTH == 2 && t + FEW_WAVES < tile1) step(odd, t + FEW_WAVES);
         }
         sum = across_rows(sum, OpAdd());
 #pragma unroll
@@ -421,7 +444,7 @@ size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache,
         a.few.most_rows = (int)(only_few ? INT32_MAX : FEW_MOST);
         a.few.rows = (int)std::min<int64_t>(FEW_ROWS, tokens * group);
         // (as many workgroups as run at a time; their parts' join where items may be cut)
-        a.few.splits = (int)std::min(2 * cus, std::max<int64_t>(1, (int64_t)sequences.count * a.few.tiles * cache.kv_heads * keys / FEW_LEAST));
+        a.few.splits = (int)std::min((cache.head_dim <= 128 ? 2 : 1) * cus, std::max<int64_t>(1, (int64_t)sequences.count * a.few.tiles * cache.kv_heads * keys / FEW_LEAST));
         a.few.each = keys > FEW_WHOLE;
     }
     if (!only_few) {

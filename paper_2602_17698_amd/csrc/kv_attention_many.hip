@@ -72,29 +72,29 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     const float scale = ((broken | broken >> 32) >> n & 1) ? NAN : a.scale;
 
     const int32_t *const table = a.sequences.pages + sequence * a.sequences.ld_pages;
-    auto page_at = [&](int t) {                                                // of this lane's key of a tile
-        const int key = key_first + t * KV_TILE + lane;
-        if (t >= tiles || key >= p.last) return -1;
-        const int page = table[key >> a.cache.shift];
-        return (uint32_t)page < (uint64_t)a.cache.pages ? page : -1;
-    };
+    // (no branch around the load and nothing done with it yet: its number is waited for a tile later, not all loads under way here)
+    auto key_at = [&](int t) { return key_first + t * KV_TILE + lane; };       // this lane's key of a tile
+    auto page_at = [&](int t) { return table[max(min(key_at(t), p.last - 1), 0) >> a.cache.shift]; };
+    auto known = [&](int page) { return (uint32_t)page < (uint64_t)a.cache.pages ? page : 0; };
+    auto valid_at = [&](int page, int t) { return __builtin_amdgcn_ballot_w64(key_at(t) < p.last && (uint32_t)page < (uint64_t)a.cache.pages); };
     // this wave's share of a tile: 16 keys, 16 DB pieces of k and of v
     u32x4 kc[PIECES], vc[PIECES];
     uint32_t vs[PIECES], ks;
     auto fetch = [&](int t, int pages) {                                       // (keys that are not there: of page 0)
+        pages = known(pages);
         const int key0 = ((key_first + t * KV_TILE) & a.cache.mask) + 16 * wave;
         const int64_t base = (int64_t)kv_head << a.cache.shift;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
-            const int page = std::max(__shfl(pages, (16 * wave + key) & 63), 0);         // (of all lanes: a lane that is not there would give 0)
+            const int page = __shfl(pages, (16 * wave + key) & 63);         // (of all lanes: a lane that is not there would give 0)
             if (16 * DB % 64 && key >= 16) continue;
             const int64_t at = base + ((key0 + key) & a.cache.mask), codes = page * a.cache.ld_codes + at * (16 * DB) + 16 * block;
             kc[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[0] + codes);
             vc[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[1] + codes);
             vs[i] = a.cache.scales[1][page * a.cache.ld_scales + at * SCALES + block];
         }
-        const int page = std::max(__shfl(pages, 16 * wave + lane % 16), 0);
+        const int page = __shfl(pages, 16 * wave + lane % 16);
         const int64_t at = base + ((key0 + lane % 16) & a.cache.mask);
         if (lane < 16 * (SCALES / 4)) ks = *reinterpret_cast<const uint32_t *>(a.cache.scales[0] + page * a.cache.ld_scales + at * SCALES + lane / 16 * 4);
     };
@@ -245,21 +245,18 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         }
     };
     int pages = page_at(0), pages_next = page_at(1);
-    uint64_t valid = __builtin_amdgcn_ballot_w64(pages >= 0);
-    if (tiles > 0) {
-        fetch(0, pages);
-        put(0, valid);
-        if (tiles > 1) fetch(1, pages_next);
-    }
+    uint64_t valid = valid_at(pages, 0);
+    fetch(0, pages);
+    put(0, valid);
+    fetch(tiles > 1 ? 1 : 0, tiles > 1 ? pages_next : pages);
     __syncthreads();
     for (int t = 0; t < tiles; ++t) {
         const int buffer = t & 1, key0 = t * KV_TILE;
         const int pages_ahead = page_at(t + 2);
-        const uint64_t valid_next = __builtin_amdgcn_ballot_w64(pages_next >= 0);
-        if (t + 1 < tiles) {
-            put(buffer ^ 1, valid_next);
-            if (t + 2 < tiles) fetch(t + 2, pages_ahead);
-        }
+        const uint64_t valid_next = valid_at(pages_next, t + 1);
+        // (behind the last tile: the last again.  Loads are in no branch, as behind one the compiler would wait for all that are under way)
+        put(buffer ^ 1, valid_next);
+        fetch(t + 2 < tiles ? t + 2 : t, t + 2 < tiles ? pages_ahead : pages);
         if (key0 < hi_any && key0 + KV_TILE > lo_any) {                        // (else none of this wave's rows sees any of it)
             const uint32_t *const kind = sh.kind[buffer];
             const uint32_t kinds = __builtin_amdgcn_readfirstlane(kind[0] | kind[1] | kind[2] | kind[3]);
@@ -268,6 +265,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         }
         __syncthreads();
         valid = valid_next;
+        pages = pages_next;
         pages_next = pages_ahead;
     }
     sum = op_halves(sum, OpAdd(), __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false));

@@ -153,7 +153,7 @@ struct AttentionArgs {
     AttentionCut few, many;
     int first;                               // workgroups (of the grid's z) ahead of this launch
 };
-constexpr int KV_MAX_KEYS = INT32_MAX - 255, KV_MAX_ROWS = INT32_MAX - 255;    // a tile's keys or rows more are numbers still
+constexpr int KV_MAX_KEYS = INT32_MAX - 4095, KV_MAX_ROWS = INT32_MAX - 255;   // some tiles of keys, or a tile of rows, more are numbers still
 constexpr int KV_MAX_PARTS = 1024;
 // z of a launch: at most 2^22 workgroups, 2^30 threads
 inline int64_t kv_launch(int64_t x, int64_t y)

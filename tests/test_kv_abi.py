@@ -78,7 +78,7 @@ def test_nothing_wrong_but_no_device(ctx):
     (dict(k_codes=None), -1), (dict(v_codes=A + 8), -1), (dict(k_scales=A + 2), -1), (dict(v_scales=None), -1), (dict(pages=0), -2), (dict(pages=1 << 31), -2),
     (dict(page_tokens=4), -2), (dict(page_tokens=24), -2), (dict(page_tokens=1 << 21), -2), (dict(kv_heads=0), -2), (dict(kv_heads=1025), -2), (dict(head_dim=48), -2),
     (dict(head_dim=0), -2), (dict(head_dim=288), -2), (dict(ld_codes=2032), -1), (dict(ld_codes=2056), -1), (dict(ld_scales=124), -1), (dict(ld_scales=130), -1),
-    (dict(ld_codes=1 << 40), -1), (dict(ld_codes=-2048), -1)])
+    (dict(ld_codes=1 << 32), -1), (dict(ld_codes=-2048), -1)])
 def test_caches_that_are_refused(ctx, change, status):
     assert everything(ctx, cache(**change)) == {status}
     assert call("kv_attention_ws_bytes", ctx, cache(**change), seqs(), 5, 8) == 0
