@@ -224,14 +224,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, s[b][i]);
-            most = fmaxf(across_rows(most, OpMax()) * scale, top);
-            if (__builtin_amdgcn_ballot_w64(most > top)) {
+            most = across_rows(most, OpMax()) * scale;
+            if (__builtin_amdgcn_ballot_w64(most > top + WEIGHT_SLACK)) {
                 asm volatile("" ::: "memory");                                 // (and this)
-                const float shrink = most > top ? __builtin_amdgcn_exp2f(top - most) : 1.0f;
+                const float to = fmaxf(most, top), shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
                 sum *= shrink;
 #pragma unroll
                 for (int i = 0; i < 2 * DB; ++i) acc[i] *= shrink;
-                top = most;
+                top = to;
             }
             const float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT;
             float w[2][8];

@@ -417,12 +417,13 @@ __device__ __forceinline__ void weights_bf16(const float (&w)[8], bf16x8 &high, 
         low[i] = (__bf16)(w[i] - (float)high[i]);
     }
 }
-// Weights are 2^14 times what they are against the largest score: fp16 then keeps those down to 2^-28 of the largest with all its bits, and some of those down to 2^-38.
-constexpr float WEIGHT_LIFT = 14.0f;
+// Weights are 2^9 times what they are against the score that counts as the largest, which follows the largest so far only where that is more than 6 powers of two above it: sums are
+// then hardly ever taken anew, and a weight is below 2^15.  fp16 keeps weights down to 2^-23 with all its bits, and of smaller ones what is a multiple of 2^-33.
+constexpr float WEIGHT_LIFT = 9.0f, WEIGHT_SLACK = 6.0f;
 // The logarithm of the sum: that of weights at their own size, which loses no bits to the lift's.
 __device__ __forceinline__ float log_sum(float lowered, float sum)
 {
-    return (lowered + WEIGHT_LIFT + __builtin_amdgcn_logf(sum * 0x1p-14f)) * 0x1.62e43p-1f;
+    return (lowered + WEIGHT_LIFT + __builtin_amdgcn_logf(sum * 0x1p-9f)) * 0x1.62e43p-1f;
 }
 
 // 4 rows of 16 elements at `at` and `step` bytes on, transposed

@@ -101,8 +101,8 @@ def attention(batch, q, scale=None, causal=True, window=0, gone=()):
     more than dim / 32 * 4 of them plus those inside an instruction, below 256; q enters in four parts of 4 bits, less than 2^-18 of its block's largest
     value being left out (three parts: 2^-15).  With e the bound on a score (scaled), weights are off by e^(2 e) - 1 and, rounded to bf16 ahead of their product with v, by 2^-8
     each and by 2^-8 of the sum; powers of two, and the sums of weights, add 2^-20.  The output rounds
-    once more.  A weight in fp16 is 2^14 times its size against the largest, so that
-    the smallest step is 2^-24 / 2^14: rounding to it costs 2^-39 of the key's v at most (where v is in bf16, powers below 2^-126 may count as 0, which costs less)."""
+    once more.  A weight in fp16 is 2^9 times its size against a score
+    that no weight counts more than 1 by; the smallest step is 2^-24: rounding to it costs 2^-25 / 2^9 of the key's v at most, against a sum of weights of 1 or more (where v is in bf16, powers below 2^-126 may count as 0, which costs less)."""
     dim, group = batch.dim, q.shape[1] // batch.kv_heads
     scale = dim ** -0.5 if scale is None else scale
     out, lse, off, off_lse = [], [], [], []
@@ -138,7 +138,7 @@ def attention(batch, q, scale=None, causal=True, window=0, gone=()):
             size[:, i] = (w[:, i, None] @ u.abs())[:, 0]
             least[:, i] = u.abs().sum(1)
         out.append(y.transpose(0, 1))
-        off.append(((torch.expm1(2 * far.clamp(max=100.0)) + 2.0 ** -7 + 2.0 ** -20) * size + 2.0 ** -8 * y.abs() + 2.0 ** -39 * least).transpose(0, 1))
+        off.append(((torch.expm1(2 * far.clamp(max=100.0)) + 2.0 ** -7 + 2.0 ** -20) * size + 2.0 ** -8 * y.abs() + 2.0 ** -34 * least).transpose(0, 1))
         lse.append(torch.logsumexp(t, -1).transpose(0, 1))
         off_lse.append((far[..., 0] + 2.0 ** -20 + 2.0 ** -23 * lse[-1].transpose(0, 1).abs()).nan_to_num(posinf=0.0).transpose(0, 1))
     return tuple(torch.cat(part) for part in (out, lse, off, off_lse))
