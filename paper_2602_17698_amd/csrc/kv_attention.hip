@@ -278,8 +278,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             f32x4 s[4];
 #pragma unroll
             for (int b = 0; b < 4; ++b) s[b] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int term = 3; term >= 0; --term)
+            static_for<0, 4>([&](auto term_) {
+                constexpr int term = 3 - decltype(term_)::value;
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -287,8 +287,9 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                         const u32x4 c = o.k[b][k];
                         const u32x6 x = q[k].codes[term];
                         const i32x8 kv = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0}, qv = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
-                        s[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv, s[b], 4, 2, 0, k_scale(o, b, k), 0, q[k].scale - Q_STEP[term]);
+                        s[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv, s[b], 4, 2, 0, k_scale(o, b, k), term, q[k].scales);
                     }
+            });
             // (here, not where they are needed: k's registers are free from here on)
             asm volatile("" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
             ask(K, o, t);

@@ -157,86 +157,91 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
     float top = -INFINITY, sum = 0.0f;
     uint32_t spoiled = 0;
-    // 32 keys of a tile; special: not all seen by all rows, or v not all in fp16
-    auto take = [&](auto special_, auto m_, int buffer, int key0, uint64_t valid) {
+    // a tile of keys, 32 after the other (in a loop: with both halves in one piece registers do not suffice); special: not all seen by all rows, or v not all in fp16
+    auto take = [&](auto special_, int buffer, int key0, uint64_t valid) {
         constexpr bool SPECIAL = decltype(special_)::value;
-        constexpr int m = decltype(m_)::value;
+#pragma unroll 1
+        for (int m = 0; m < 2; ++m) {
         f32x16 s;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-        {
-            u32x4 c[KS];
-            int sc[KS];
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const int block = 2 * k + h;
-                c[k] = zero;
-                sc[k] = 127;
-                if (DB % 2 == 0 || block < DB) {
-                    c[k] = *reinterpret_cast<const u32x4 *>(sh.k[buffer] + (32 * m + n) * K_PITCH + 16 * block);
-                    sc[k] = sh.ks[buffer][(32 * m + n) * SCALES + block];
-                }
-            }
-#pragma unroll
-            for (int term = TERMS - 1; term >= 0; --term)
+            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+            {
+                u32x4 c[KS];
+                int sc[KS];
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
-                    const u32x6 x = q[k].codes[term];
-                    const i32x8 kv = {(int)c[k].x, (int)c[k].y, (int)c[k].z, (int)c[k].w, 0, 0, 0, 0}, qv = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
-                    s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kv, qv, s, 4, 2, 0, sc[k], 0, q[k].scale - Q_STEP[term]);
+                    const int block = 2 * k + h;
+                    c[k] = zero;
+                    sc[k] = 127;
+                    if (DB % 2 == 0 || block < DB) {
+                        c[k] = *reinterpret_cast<const u32x4 *>(sh.k[buffer] + (32 * m + n) * K_PITCH + 16 * block);
+                        sc[k] = sh.ks[buffer][(32 * m + n) * SCALES + block];
+                    }
                 }
-        }
-        if constexpr (SPECIAL) {
-            const int h4 = fresh(4 * h), from = lo - key0 - h4, past = hi - key0 - h4;
-            const uint32_t mine = (uint32_t)(valid >> 32 * m) >> h4;
+                static_for<0, TERMS>([&](auto t) {
+                    constexpr int term = TERMS - 1 - decltype(t)::value;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int at = 8 * (i / 4) + i % 4;
-                s[i] = (mine >> at & 1) && 32 * m + at >= from && 32 * m + at < past ? s[i] : -INFINITY;
+                    for (int k = 0; k < KS; ++k) {
+                        const u32x6 x = q[k].codes[term];
+                        const i32x8 kv = {(int)c[k].x, (int)c[k].y, (int)c[k].z, (int)c[k].w, 0, 0, 0, 0}, qv = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
+                        s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kv, qv, s, 4, 2, 0, sc[k], term, q[k].scales);
+                    }
+                });
             }
-        }
-        float most = -INFINITY;
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (SPECIAL) {
+                const int h4 = fresh(4 * h), from = lo - key0 - h4, past = hi - key0 - h4;
+                const uint32_t mine = (uint32_t)(valid >> 32 * m) >> h4;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i]);
-        most = op_halves(most, OpMax(), __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false));
-        most *= scale;
-        if (__builtin_amdgcn_ballot_w64(most > top + WEIGHT_SLACK)) {
-            asm volatile("" ::: "memory");                                     // (not for all tiles)
-            const float to = fmaxf(most, top), shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
-            sum *= shrink;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) acc[d] *= shrink;
-            top = to;
-        }
-        const float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int step = 2 * m + half;
-            float w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                w[j] = __builtin_amdgcn_exp2f(fmaf(s[half * 8 + j], scale, -base));
-                sum += w[j];
-            }
-            const unsigned char *const at = sh.v[buffer] + (16 * step + 4 * h + n % 16 / 4) * V_PITCH + 32 * (n / 16) + 8 * (n % 4);
-            const uint32_t kind = SPECIAL ? __builtin_amdgcn_readfirstlane(sh.kind[buffer][step]) : 0;
-            if (!SPECIAL || kind == 0) {
-                const f16x8 p16 = weights_f16(w);
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, read_transposed(at + 64 * d, 8 * V_PITCH)), p16, acc[d], 0, 0, 0);
-            } else {
-                bf16x8 high, low;
-                weights_bf16(w, high, low);
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const bf16x8 v = __builtin_bit_cast(bf16x8, read_transposed(at + 64 * d, 8 * V_PITCH));
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, low, acc[d], 0, 0, 0);
-                    acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, high, acc[d], 0, 0, 0);
+                for (int i = 0; i < 16; ++i) {
+                    const int at = 8 * (i / 4) + i % 4;
+                    s[i] = (mine >> at & 1) && 32 * m + at >= from && 32 * m + at < past ? s[i] : -INFINITY;
                 }
-                if (kind == 3)
-                    for (int j = 0; j < 16; ++j)
-                        if (key0 + 16 * step + j >= lo && key0 + 16 * step + j < hi) spoiled |= sh.spoiled[buffer][16 * step + j];
+            }
+            float most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i]);
+            most = op_halves(most, OpMax(), __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false));
+            most *= scale;
+            if (__builtin_amdgcn_ballot_w64(most > top + WEIGHT_SLACK)) {
+                asm volatile("" ::: "memory");                                     // (not for all tiles)
+                const float to = fmaxf(most, top), shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
+                sum *= shrink;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) acc[d] *= shrink;
+                top = to;
+            }
+            const float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int step = 2 * m + half;
+                __builtin_amdgcn_sched_barrier(0);
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    w[j] = __builtin_amdgcn_exp2f(fmaf(s[half * 8 + j], scale, -base));
+                    sum += w[j];
+                }
+                const unsigned char *const at = sh.v[buffer] + (16 * step + 4 * h + n % 16 / 4) * V_PITCH + 32 * (n / 16) + 8 * (n % 4);
+                const uint32_t kind = SPECIAL ? __builtin_amdgcn_readfirstlane(sh.kind[buffer][step]) : 0;
+                if (!SPECIAL || kind == 0) {
+                    const f16x8 p16 = weights_f16(w);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d)
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, read_transposed(at + 64 * d, 8 * V_PITCH)), p16, acc[d], 0, 0, 0);
+                } else {
+                    bf16x8 high, low;
+                    weights_bf16(w, high, low);
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        const bf16x8 v = __builtin_bit_cast(bf16x8, read_transposed(at + 64 * d, 8 * V_PITCH));
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, low, acc[d], 0, 0, 0);
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, high, acc[d], 0, 0, 0);
+                    }
+                    if (kind == 3)
+                        for (int j = 0; j < 16; ++j)
+                            if (key0 + 16 * step + j >= lo && key0 + 16 * step + j < hi) spoiled |= sh.spoiled[buffer][16 * step + j];
+                }
             }
         }
     };
@@ -256,8 +261,8 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         if (key0 < hi_any && key0 + KV_TILE > lo_any) {                        // (else none of this wave's rows sees any of it)
             const uint32_t *const kind = sh.kind[buffer];
             const uint32_t kinds = __builtin_amdgcn_readfirstlane(kind[0] | kind[1] | kind[2] | kind[3]);
-            if (kinds || valid != ~0ull || key0 < lo_all || key0 + KV_TILE > hi_all) static_for<0, 2>([&](auto m) { take(std::true_type{}, m, buffer, key0, valid); });
-            else static_for<0, 2>([&](auto m) { take(std::false_type{}, m, buffer, key0, valid); });
+            if (kinds || valid != ~0ull || key0 < lo_all || key0 + KV_TILE > hi_all) take(std::true_type{}, buffer, key0, valid);
+            else take(std::false_type{}, buffer, key0, valid);
         }
         __syncthreads();
         valid = valid_next;

@@ -330,7 +330,7 @@ typedef float f32x32 __attribute__((ext_vector_type(32)));
 // of the largest is left out (with three terms less than 2^-15).
 constexpr int Q_STEP[4] = {0, 4, 10, 16};
 template <int TERMS>
-struct QBlock { u32x6 codes[TERMS]; int scale; };                             // scale: the first term's byte
+struct QBlock { u32x6 codes[TERMS]; int scales; };                            // scales: the terms' bytes
 typedef __bf16 bf16x32 __attribute__((ext_vector_type(32)));
 typedef unsigned int u32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -339,10 +339,11 @@ template <int TERMS>
 __device__ __forceinline__ QBlock<TERMS> split_q(u32x16 x, uint32_t top)
 {
     QBlock<TERMS> q;
-    q.scale = max((int)(top >> 7) - 2, 17);
+    const int first = max((int)(top >> 7) - 2, 17);
+    q.scales = first | (first - Q_STEP[1]) << 8 | (first - Q_STEP[2]) << 16 | (first - Q_STEP[3]) << 24;
 #pragma unroll
     for (int t = 0; t < TERMS; ++t) {
-        const float scale = __uint_as_float((uint32_t)(q.scale - Q_STEP[t]) << 23);
+        const float scale = __uint_as_float((uint32_t)(first - Q_STEP[t]) << 23);
         q.codes[t] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(__builtin_bit_cast(bf16x32, x), scale);
         if (t == TERMS - 1) break;
         const u32x16 back = __builtin_bit_cast(u32x16, __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(q.codes[t], scale));
