@@ -579,8 +579,8 @@ int  sbits_rotate(sbits_ctx *ctx, const sbits_rotary *rotary, const int32_t *pos
 /* Writes the rows of k and v ([tokens][kv_heads][head_dim] by pitches as above, of `type`) to their sequences' places in
  * the cache, quantised as sbits_mx_quantize does.  With `rotary` (may be NULL) keys are turned
  * first, by positions[row] or, where positions is NULL, by the row's place in its sequence, in 64
- * bits, without a rounding ahead of the quantisation; and so are the rows of q (may be NULL) with q_heads
- * heads, rounded once to `type`, into q_out (which may be q).  Rows that are 16-byte aligned: pitches multiples of 8
+ * bits, without a rounding ahead of the quantisation; and the rows of q (may be NULL), with q_heads
+ * heads, are turned as sbits_rotate does into q_out (which may be q with the same pitches).  Rows that are 16-byte aligned: pitches multiples of 8
  * (bf16) or 4 (fp32).  Where a place is not there, q_out is written all the same.         */
 int  sbits_kv_store(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens,
                     const void *k, int64_t ld_k, int64_t hd_k, const void *v, int64_t ld_v, int64_t hd_v, int type,

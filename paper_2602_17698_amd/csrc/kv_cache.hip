@@ -58,39 +58,92 @@ __device__ __forceinline__ void turned8(const Turns &t, const double2 *turn, con
     }
 }
 
-template <bool BF16, bool TURN>
+// Where the rows of a workgroup go, in LDS.
+struct Places { int64_t page[KV_MANY], position[KV_MANY]; int there[KV_MANY]; };      // there: -1: not a sequence's row
+template <int R>
+__device__ __forceinline__ void find_places(const KvPages &cache, const KvSequences &sequences, int64_t row0, int64_t tokens, Places &p)
+{
+    const int lane = threadIdx.x & 63;
+    for (int i = threadIdx.x >> 6; i < R; i += 4) {
+        const int64_t row = row0 + i;
+        Row r = {-1, 0};
+        if (row < tokens) r = find_row(sequences, row);
+        if (lane == 0) {
+            p.there[i] = r.sequence;
+            p.position[i] = r.position;
+            p.page[i] = page_of(cache, sequences, r.sequence, r.position);
+        }
+    }
+}
+
+// R rows a workgroup: neighbouring tokens of a sequence fill whole lines of a head's codes and scales, which else several dies' caches would have parts of.
+template <bool BF16, bool TURN, int R>
 __global__ __launch_bounds__(256) void kv_store_kernel(StoreArgs a)
 {
-    __shared__ double2 turn[TURN ? ROTARY_MAX_PAIRS : 1];
-    const int runs = a.cache.dim / 8, kv = a.cache.kv_heads * runs, all = 2 * kv + (TURN ? a.q_heads * runs : 0);
-    for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
-        const Row r = find_row(a.sequences, row);
-        if (r.sequence < 0) continue;                            // (all threads: the row is the workgroup's)
-        const int64_t page = page_of(a.cache, a.sequences, r.sequence, r.position);
+    __shared__ double2 turn[TURN ? R : 1][TURN ? ROTARY_MAX_PAIRS : 1];
+    __shared__ float2 turn32[TURN ? R : 1][TURN ? ROTARY_MAX_PAIRS : 1];
+    __shared__ Places places;
+    const int runs = a.cache.dim / 8, pairs = a.rotary.pairs;
+    const bool wide = pairs % 8 == 0;
+    const int mine = wide ? pairs / 8 : pairs, unit_all = TURN ? mine + (wide ? (a.cache.dim - 2 * pairs) / 8 : a.cache.dim - 2 * pairs) : 1;    // units of a head of q
+    const uint32_t kv = (uint32_t)(a.cache.kv_heads * R * runs), all = 2 * kv + (TURN ? (uint32_t)(a.q_heads * R * unit_all) : 0);
+    for (int64_t row0 = (int64_t)blockIdx.x * R; row0 < a.tokens; row0 += (int64_t)gridDim.x * R) {
+        __syncthreads();
+        find_places<R>(a.cache, a.sequences, row0, a.tokens, places);
+        __syncthreads();
         if constexpr (TURN) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < a.rotary.pairs; i += 256)
-                turn_of(a.rotary, i, a.positions ? a.positions[row] : r.position, turn[i].x, turn[i].y);
+            for (int at = threadIdx.x; at < R * pairs; at += 256) {
+                const int i = at / pairs, pair = at - i * pairs;
+                if (places.there[i] < 0) continue;
+                double2 w;
+                turn_of(a.rotary, pair, a.positions ? a.positions[row0 + i] : places.position[i], w.x, w.y);
+                turn[i][pair] = w;
+                turn32[i][pair] = make_float2((float)w.x, (float)w.y);
+            }
             __syncthreads();
         }
-        for (int at = threadIdx.x; at < all; at += 256) {
+        for (uint32_t at = threadIdx.x; at < all; at += 256) {
             if (TURN && at >= 2 * kv) {
-                const int head = (at - 2 * kv) / runs, run = at - 2 * kv - head * runs;
-                if (a.q.at == a.q_out.at) continue;              // in place: below
-                double v[8];
-                turned8<BF16>(a.rotary, turn, a.q.at, row * a.q.ld + head * a.q.hd, run, v);
-                float f[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = BF16 ? sticky(v[e]) : (float)v[e];
-                store8<BF16>(const_cast<void *>(a.q_out.at), row * a.q_out.ld + head * a.q_out.hd + 8 * run, f);
+                // queries: 8 pairs (or one) a thread, in 32 bits; both of a pair, so that q_out may be q
+                const uint32_t q = at - 2 * kv, unit = q % (uint32_t)unit_all, rest = q / (uint32_t)unit_all;
+                const int i = (int)(rest % R), head = (int)(rest / R);
+                if (places.there[i] < 0) continue;
+                const int64_t row = row0 + i, from = row * a.q.ld + head * a.q.hd, to = row * a.q_out.ld + head * a.q_out.hd;
+                void *const out = const_cast<void *>(a.q_out.at);
+                const float2 *const t = turn32[i];
+                if (wide) {
+                    float v[8], w[8];
+                    if ((int)unit >= mine) {
+                        const int j = 2 * pairs + 8 * ((int)unit - mine);
+                        load8<BF16>(a.q.at, from + j, v);
+                        store8<BF16>(out, to + j, v);
+                        continue;
+                    }
+                    const int j0 = a.rotary.interleaved ? 16 * unit : 8 * unit, j1 = a.rotary.interleaved ? j0 + 8 : pairs + j0;
+                    load8<BF16>(a.q.at, from + j0, v);
+                    load8<BF16>(a.q.at, from + j1, w);
+                    rotate16(a.rotary.interleaved, t + 8 * unit, v, w);
+                    store8<BF16>(out, to + j0, v);
+                    store8<BF16>(out, to + j1, w);
+                } else if ((int)unit >= mine) {
+                    const int j = 2 * pairs + (int)unit - mine;
+                    store1<BF16>(out, to + j, load1<BF16>(a.q.at, from + j));
+                } else {
+                    const int j0 = a.rotary.interleaved ? 2 * unit : unit, j1 = a.rotary.interleaved ? j0 + 1 : pairs + unit;
+                    const float v = load1<BF16>(a.q.at, from + j0), w = load1<BF16>(a.q.at, from + j1);
+                    store1<BF16>(out, to + j0, fmaf(v, t[unit].x, -(w * t[unit].y)));
+                    store1<BF16>(out, to + j1, fmaf(w, t[unit].x, v * t[unit].y));
+                }
                 continue;
             }
-            if (page < 0) continue;
-            const int which = at >= kv, head = (at - which * kv) / runs, run = at - which * kv - head * runs;
+            const uint32_t which = at >= kv, in = at - which * kv, run = in % (uint32_t)runs, rest = in / (uint32_t)runs;
+            const int i = (int)(rest % R), head = (int)(rest / R);
+            const int64_t page = places.page[i], row = row0 + i;
+            if (page < 0) continue;                              // (of all four lanes of a block)
             float f[8];
             if (TURN && which == 0) {
                 double v[8];
-                turned8<BF16>(a.rotary, turn, a.k.at, row * a.k.ld + head * a.k.hd, run, v);
+                turned8<BF16>(a.rotary, turn[i], a.k.at, row * a.k.ld + head * a.k.hd, run, v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] = sticky(v[e]);
             } else {
@@ -103,41 +156,31 @@ __global__ __launch_bounds__(256) void kv_store_kernel(StoreArgs a)
             top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, DPP_XOR1, 0xf, 0xf, true));
             top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, DPP_XOR2, 0xf, 0xf, true));
             const uint32_t byte = mx_scale_byte(top), codes = mx_codes8(f, byte);
-            const int64_t place = ((int64_t)head << a.cache.shift) + (r.position & a.cache.mask);
+            const int64_t place = ((int64_t)head << a.cache.shift) + (places.position[i] & a.cache.mask);
             *reinterpret_cast<uint32_t *>(a.cache.codes[which] + page * a.cache.ld_codes + place * a.cache.row_codes + 4 * run) = codes;
             if ((run & 3) == 0) a.cache.scales[which][page * a.cache.ld_scales + place * a.cache.row_scales + (run >> 2)] = (uint8_t)byte;
-        }
-        if constexpr (TURN) {
-            // in place a pair is read and written by one thread
-            if (a.q.at == a.q_out.at)
-                for (int at = threadIdx.x; at < a.q_heads * a.rotary.pairs; at += 256) {
-                    const int head = at / a.rotary.pairs, i = at - head * a.rotary.pairs;
-                    const int64_t q = row * a.q.ld + head * a.q.hd, j0 = a.rotary.interleaved ? 2 * i : i, j1 = a.rotary.interleaved ? j0 + 1 : a.rotary.pairs + i;
-                    const double p = load1<BF16>(a.q.at, q + j0), s = load1<BF16>(a.q.at, q + j1);
-                    const double v = fma(p, turn[i].x, -(s * turn[i].y)), w = fma(s, turn[i].x, p * turn[i].y);
-                    store1<BF16>(const_cast<void *>(a.q_out.at), q + j0, BF16 ? sticky(v) : (float)v);
-                    store1<BF16>(const_cast<void *>(a.q_out.at), q + j1, BF16 ? sticky(w) : (float)w);
-                }
         }
     }
 }
 
-template <bool BF16>
+template <bool BF16, int R>
 __global__ __launch_bounds__(256) void kv_load_kernel(LoadArgs a)
 {
-    const int runs = a.cache.dim / 8, kv = a.cache.kv_heads * runs;
-    for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x) {
-        const Row r = find_row(a.sequences, row);
-        if (r.sequence < 0) continue;
-        const int64_t page = page_of(a.cache, a.sequences, r.sequence, r.position);
-        for (int at = threadIdx.x; at < 2 * kv; at += 256) {
-            const int which = at >= kv, head = (at - which * kv) / runs, run = at - which * kv - head * runs;
+    __shared__ Places places;
+    const uint32_t runs = a.cache.dim / 8, kv = (uint32_t)a.cache.kv_heads * R * runs;
+    for (int64_t row0 = (int64_t)blockIdx.x * R; row0 < a.tokens; row0 += (int64_t)gridDim.x * R) {
+        __syncthreads();
+        find_places<R>(a.cache, a.sequences, row0, a.tokens, places);
+        __syncthreads();
+        for (uint32_t at = threadIdx.x; at < 2 * kv; at += 256) {
+            const uint32_t which = at >= kv, in = at - which * kv, run = in % runs, rest = in / runs;
+            const int i = (int)(rest % R), head = (int)(rest / R);
             void *const out = a.out[which];
-            if (!out) continue;
-            const int64_t to = row * a.ld[which] + head * a.hd[which] + 8 * run;
+            if (!out || places.there[i] < 0) continue;
+            const int64_t page = places.page[i], to = (row0 + i) * a.ld[which] + head * a.hd[which] + 8 * run;
             uint32_t codes = 0, byte = 127;
             if (page >= 0) {
-                const int64_t place = ((int64_t)head << a.cache.shift) + (r.position & a.cache.mask);
+                const int64_t place = ((int64_t)head << a.cache.shift) + (places.position[i] & a.cache.mask);
                 codes = *reinterpret_cast<const uint32_t *>(a.cache.codes[which] + page * a.cache.ld_codes + place * a.cache.row_codes + 4 * run);
                 byte = a.cache.scales[which][page * a.cache.ld_scales + place * a.cache.row_scales + (run >> 2)];
             }
@@ -159,22 +202,35 @@ __global__ __launch_bounds__(256) void kv_load_kernel(LoadArgs a)
 
 }  // namespace sbits
 
-int sbits_launch_kv_store(sbits_ctx *ctx, const sbits::StoreArgs &a, bool bf16)
+// Rows of a workgroup: KV_MANY where there are workgroups enough for all CUs, else one.
+static bool many_rows(const sbits_ctx *ctx, int64_t tokens) { return tokens >= (int64_t)sbits::KV_MANY * 2 * (ctx->cus ? ctx->cus : 256); }
+
+template <int R>
+static int launch_store(sbits_ctx *ctx, const sbits::StoreArgs &a, bool bf16)
 {
     using namespace sbits;
-    const dim3 grid((uint32_t)(a.tokens < (1 << 20) ? a.tokens : 1 << 20));
+    const int64_t rows = (a.tokens + R - 1) / R;
     const bool turn = a.rotary.turns != nullptr;
-    auto fn = bf16 ? (turn ? kv_store_kernel<true, true> : kv_store_kernel<true, false>) : (turn ? kv_store_kernel<false, true> : kv_store_kernel<false, false>);
-    hipLaunchKernelGGL(fn, grid, dim3(256), 0, ctx->stream, a);
+    auto fn = bf16 ? (turn ? kv_store_kernel<true, true, R> : kv_store_kernel<true, false, R>) : (turn ? kv_store_kernel<false, true, R> : kv_store_kernel<false, false, R>);
+    hipLaunchKernelGGL(fn, dim3((uint32_t)(rows < (1 << 20) ? rows : 1 << 20)), dim3(256), 0, ctx->stream, a);
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;
 }
+int sbits_launch_kv_store(sbits_ctx *ctx, const sbits::StoreArgs &a, bool bf16)
+{
+    return many_rows(ctx, a.tokens) ? launch_store<sbits::KV_MANY>(ctx, a, bf16) : launch_store<1>(ctx, a, bf16);
+}
 
-int sbits_launch_kv_load(sbits_ctx *ctx, const sbits::LoadArgs &a, bool bf16)
+template <int R>
+static int launch_load(sbits_ctx *ctx, const sbits::LoadArgs &a, bool bf16)
 {
     using namespace sbits;
-    const dim3 grid((uint32_t)(a.tokens < (1 << 20) ? a.tokens : 1 << 20));
-    hipLaunchKernelGGL(bf16 ? kv_load_kernel<true> : kv_load_kernel<false>, grid, dim3(256), 0, ctx->stream, a);
+    const int64_t rows = (a.tokens + R - 1) / R;
+    hipLaunchKernelGGL((bf16 ? kv_load_kernel<true, R> : kv_load_kernel<false, R>), dim3((uint32_t)(rows < (1 << 20) ? rows : 1 << 20)), dim3(256), 0, ctx->stream, a);
     SBITS_HIP(ctx, hipGetLastError());
     return SBITS_OK;
+}
+int sbits_launch_kv_load(sbits_ctx *ctx, const sbits::LoadArgs &a, bool bf16)
+{
+    return many_rows(ctx, a.tokens) ? launch_load<sbits::KV_MANY>(ctx, a, bf16) : launch_load<1>(ctx, a, bf16);
 }

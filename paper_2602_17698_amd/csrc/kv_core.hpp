@@ -7,6 +7,7 @@
 namespace sbits {
 
 constexpr int KV_MAX_DIM = 256, KV_MAX_HEADS = 1024, KV_MAX_PAGE = 1 << 20, ROTARY_MAX_PAIRS = 128, KV_LEAST_PAGE = 8;
+constexpr int KV_MANY = 8;                   // rows of a workgroup that writes or reads many
 constexpr int KV_MAX_QUERY_HEADS = 65535;
 constexpr uint32_t KV_V_LIMIT = 253;         // bytes of v from here on: a value beyond bf16's range is possible, the block counts as NaN
 
@@ -108,6 +109,28 @@ __device__ __forceinline__ void store1(void *base, int64_t at, float v)
 {
     if constexpr (BF16) static_cast<uint16_t *>(base)[at] = (uint16_t)bf16_round(v);
     else static_cast<float *>(base)[at] = v;
+}
+
+// 8 pairs, (v[i], w[i]) or, interleaved, neighbours in v and then in w, turned by t
+__device__ __forceinline__ void rotate16(bool interleaved, const float2 *t, float (&v)[8], float (&w)[8])
+{
+    if (interleaved) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = t[i], b = t[4 + i];
+            const float p = v[2 * i], q = v[2 * i + 1], r = w[2 * i], s = w[2 * i + 1];
+            v[2 * i] = fmaf(p, a.x, -(q * a.y)); v[2 * i + 1] = fmaf(q, a.x, p * a.y);
+            w[2 * i] = fmaf(r, b.x, -(s * b.y)); w[2 * i + 1] = fmaf(s, b.x, r * b.y);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 a = t[i];
+            const float p = v[i], q = w[i];
+            v[i] = fmaf(p, a.x, -(q * a.y));
+            w[i] = fmaf(q, a.x, p * a.y);
+        }
+    }
 }
 
 struct RotateArgs {

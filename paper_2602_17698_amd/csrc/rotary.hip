@@ -39,23 +39,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a)
                 float v[8], w[8];
                 load8<BF16>(a.x, x + j0, v);
                 load8<BF16>(a.x, x + j1, w);
-                if (a.rotary.interleaved) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 t = turn[8 * unit + i], u = turn[8 * unit + 4 + i];
-                        const float p = v[2 * i], q = v[2 * i + 1], r = w[2 * i], m = w[2 * i + 1];
-                        v[2 * i] = fmaf(p, t.x, -(q * t.y)); v[2 * i + 1] = fmaf(q, t.x, p * t.y);
-                        w[2 * i] = fmaf(r, u.x, -(m * u.y)); w[2 * i + 1] = fmaf(m, u.x, r * u.y);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 t = turn[8 * unit + i];
-                        const float p = v[i], q = w[i];
-                        v[i] = fmaf(p, t.x, -(q * t.y));
-                        w[i] = fmaf(q, t.x, p * t.y);
-                    }
-                }
+                rotate16(a.rotary.interleaved, turn + 8 * unit, v, w);
                 store8<BF16>(a.out, out + j0, v);
                 store8<BF16>(a.out, out + j1, w);
             } else {

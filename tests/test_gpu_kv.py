@@ -110,9 +110,9 @@ def test_store_and_load(ctx, dtype, page, kv_heads, dim, dims, interleaved, give
         ctx.kv_store(cache, seqs, src[0], src[1], rotary=rotary_of(kv_plain.turns(dims), interleaved, 1.1), q=src[2], q_out=q_out,
                      positions=positions.cuda() if given else None)
         want_k, _ = kv_plain.turn(k[rows], at, kv_plain.turns(dims), interleaved, 1.1)
-        want_q, _ = kv_plain.turn(q[rows], at, kv_plain.turns(dims), interleaved, 1.1)
+        want_q, size = kv_plain.turn(q[rows], at, kv_plain.turns(dims), interleaved, 1.1)
         got = q_out.cpu().double()
-        assert ((got[rows] - want_q).abs() <= (2.0 ** -8 if dtype == BF16 else 2.0 ** -23) * want_q.abs() + 1e-12).all()
+        assert ((got[rows] - want_q).abs() <= 4 * 2.0 ** -24 * size + (2.0 ** -8 * want_q.abs() if dtype == BF16 else 0.0)).all()
         assert (got[:3] == 77).all() and (got[-2:] == 77).all()
     else:
         ctx.kv_store(cache, seqs, src[0], src[1])
@@ -140,6 +140,41 @@ def test_store_and_load(ctx, dtype, page, kv_heads, dim, dims, interleaved, give
     only = torch.full_like(k, 5.0, device="cuda")
     ctx.kv_load(cache, seqs, None, only)
     assert torch.equal(only.cpu()[rows].double(), want)
+
+
+@pytest.mark.parametrize("dims,interleaved", [(128, False), (40, True), (0, False)])
+def test_store_and_load_of_many_rows(ctx, dims, interleaved):
+    """Rows enough for several to a workgroup, some of them no sequence's, sequences that begin and end inside one; queries in place."""
+    sizes = [(3000, 5), (0, 3), (1, 70), (1299, 0), (13, 13)]
+    b = Batch(sizes, 32, 2, 128, seed=1, lead=5, behind=3)
+    cache, seqs, buffers = b.on(sb)
+    g = gen(dims)
+    k, v, q = (torch.randn(b.tokens, h, 128, generator=g).to(BF16) for h in (2, 2, 3))
+    rows, at = b.rows(), b.positions()
+    turned = q.cuda()
+    if dims:
+        ctx.kv_store(cache, seqs, k.cuda(), v.cuda(), rotary=rotary_of(kv_plain.turns(dims), interleaved), q=turned, q_out=turned)
+    else:
+        ctx.kv_store(cache, seqs, k.cuda(), v.cuda())
+    want_k = kv_plain.turn(k[rows], at, kv_plain.turns(dims), interleaved, 1.0)[0] if dims else k[rows].double()
+    if dims:
+        want_q, size = kv_plain.turn(q[rows], at, kv_plain.turns(dims), interleaved, 1.0)
+        got = turned.cpu().double()
+        assert ((got[rows] - want_q).abs() <= 4 * 2.0 ** -24 * size + 2.0 ** -8 * want_q.abs()).all()
+        assert torch.equal(got[:5], q[:5].double()) and torch.equal(got[-3:], q[-3:].double())
+    row = 0
+    for s, (n, p) in enumerate(sizes):
+        for i, x in enumerate((want_k, v[rows].double())):
+            b.put(i, s, p, *kv_plain.quantised(x[row:row + n]))
+        row += n
+    for t, want in zip(buffers, (b.codes[0], b.scales[0], b.codes[1], b.scales[1])):
+        assert torch.equal(t.cpu(), want)
+    out = [torch.full((b.tokens, 2, 128), 77.0, dtype=dtype, device="cuda") for dtype in (BF16, BF16)]
+    ctx.kv_load(cache, seqs, *out)
+    for i in range(2):
+        got = out[i].cpu()
+        assert (got[:5] == 77).all() and (got[-3:] == 77).all()
+        assert torch.equal(got[rows].double(), torch.cat([b.get(i, s, p, n) for s, (n, p) in enumerate(sizes)]))
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
