@@ -344,64 +344,68 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
     }
 }
 
-// The parts of a row: a thread has 8 elements of some of the parts.
-template <int DB, int ROWS>
-__global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
+// The parts of RE rows: a thread has 8 elements of some of a row's parts.  (The first wave finds out which these are: 2048 workgroups whose waves all did, a row each, took 21 us
+// for 64 sequences of up to 16384 keys.)
+struct Parts { int parts, start, rows, row0; int64_t slot0, slot1, step, slots; };   // rows: of the sequence, row0: the tile's first; slots of row0's first part, its second, from there on; of all
+template <int ROWS>
+__device__ __forceinline__ Parts find_parts(const AttentionArgs &a, int place, int kv_head)
 {
-    constexpr int D = 32 * DB, RUNS = 4 * DB, WAYS = 256 / RUNS;
-    __shared__ __attribute__((aligned(16))) float part[WAYS][RUNS][8];
-    __shared__ float sums[WAYS];
-    const int kv_head = blockIdx.y, place = a.first + blockIdx.z, lane = threadIdx.x & 63;
-    int parts, start, row = blockIdx.x;
-    int64_t slot0, slot1, step, slots;                                         // of the first part, the second; from then on; of all
+    Parts p = {};
     if constexpr (ROWS == FEW_ROWS) {
-        const int sequence = (uint32_t)place / (uint32_t)a.few.tiles;
+        const int sequence = (uint32_t)place / (uint32_t)a.few.tiles, tile = place - sequence * a.few.tiles;
         const FewSequence f = few_sequence(a, sequence);
-        const int tile = place - sequence * a.few.tiles;
-        if (tile * ROWS + row >= f.rows || f.keys <= FEW_WHOLE) return;
+        if (tile >= f.tiles || f.keys <= FEW_WHOLE) return p;
         int64_t begin;
         const int64_t total = few_total(a, sequence, begin);
         begin += ((int64_t)tile * a.cache.kv_heads + kv_head) * f.keys;
         const int workgroups = few_workgroups(a, total);
+        const double each = (double)total / (double)workgroups;
         // the cuts inside: from the first that is behind the item's begin and stays there on
-        int w = (int)((double)begin / ((double)total / (double)workgroups));
-        w = max(w - 1, 0);
+        int w = max((int)((double)begin / each) - 1, 0);
         while (w < workgroups && few_cut(w, workgroups, total) - begin < FEW_EDGE) ++w;
-        int past = min((int)((double)(begin + f.keys - FEW_EDGE) / ((double)total / (double)workgroups)) + 2, workgroups);
+        int past = min((int)((double)(begin + f.keys - FEW_EDGE) / each) + 2, workgroups);
         while (past > w && few_cut(past - 1, workgroups, total) - begin > f.keys - FEW_EDGE) --past;
-        parts = 1 + past - w;
-        slot0 = (int64_t)(2 * (w - 1) + 1) * ROWS + row;
-        slot1 = (int64_t)(2 * w) * ROWS + row;
-        step = 2 * ROWS;
-        slots = (int64_t)2 * a.few.splits * ROWS;
-        start = f.start;
-        row += tile * ROWS;
+        p = {1 + past - w, f.start, f.rows, tile * ROWS, (int64_t)(2 * (w - 1) + 1) * ROWS, (int64_t)(2 * w) * ROWS, 2 * ROWS, (int64_t)2 * a.few.splits * ROWS};
     } else {
         int tile;
         const int sequence = find_tile(a, place, tile);
-        TilePlan p;
-        if (sequence < 0 || !tile_plan(a, sequence, tile, p) || tile * ROWS + row >= p.rows) return;
-        parts = p.parts;
-        slot0 = ((int64_t)place * a.cache.kv_heads + kv_head) * a.many.splits * ROWS + row;
-        slot1 = slot0 + ROWS;
-        step = ROWS;
-        slots = (int64_t)a.many.tiles * a.cache.kv_heads * a.many.splits * ROWS;
-        start = p.start;
-        row += tile * ROWS;
+        TilePlan t;
+        if (sequence < 0 || !tile_plan(a, sequence, tile, t)) return p;
+        const int64_t slot = ((int64_t)place * a.cache.kv_heads + kv_head) * a.many.splits * ROWS;
+        p = {t.parts, t.start, t.rows, tile * ROWS, slot, slot + ROWS, ROWS, (int64_t)a.many.tiles * a.cache.kv_heads * a.many.splits * ROWS};
     }
-    if (parts == 1) return;
+    return p;
+}
+template <int DB, int ROWS, int RE>
+__global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
+{
+    constexpr int D = 32 * DB, RUNS = 4 * DB, WAYS = 256 / (RUNS * RE);
+    static_assert(WAYS >= 1, "a thread for each run of a row");
+    __shared__ __attribute__((aligned(16))) float part[WAYS][RE][RUNS][8];
+    __shared__ float sums[WAYS][RE];
+    __shared__ Parts shared;
+    const int kv_head = blockIdx.y;
+    if (threadIdx.x < 64) {
+        const Parts found = find_parts<ROWS>(a, a.first + blockIdx.z, kv_head);
+        if (threadIdx.x == 0) shared = found;
+    }
+    __syncthreads();
+    const Parts p = shared;
+    if (p.parts <= 1) return;
     const float *const from = ROWS == FEW_ROWS ? a.few.part : a.many.part;
-    const float2 *const pairs = reinterpret_cast<const float2 *>(from + slots * D);
-    auto slot = [&](int s) { return s == 0 ? slot0 : slot1 + (s - 1) * step; };
-    const int way = threadIdx.x / RUNS, run = threadIdx.x - way * RUNS;
-    // (every wave finds the largest score)
-    float m = -INFINITY;
-    for (int s = lane; s < parts; s += 64) m = fmaxf(m, pairs[slot(s)].x);
-    m = group_allreduce<64>(m, OpMax());
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (way < WAYS) {
-        for (int s = way; s < parts; s += WAYS) {
+    const float2 *const pairs = reinterpret_cast<const float2 *>(from + p.slots * D);
+    const int way = threadIdx.x / (RUNS * RE), in = threadIdx.x - way * (RUNS * RE), row = blockIdx.x * RE + in / RUNS, run = in % RUNS;
+    auto slot = [&](int s) { return (s == 0 ? p.slot0 : p.slot1 + (s - 1) * p.step) + row; };
+    const bool there = way < WAYS && row < ROWS && p.row0 + row < p.rows;
+    float m = -INFINITY, l = 0.0f, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (RE == 1) {                                                             // (one row: a lane has some of its parts)
+        for (int s = threadIdx.x & 63; s < p.parts && row < ROWS; s += 64) m = fmaxf(m, pairs[slot(s)].x);
+        m = group_allreduce<64>(m, OpMax());
+    }
+    if (there) {
+        for (int s = 0; RE > 1 && s < p.parts; ++s) m = fmaxf(m, pairs[slot(s)].x);
+        const float base = m == -INFINITY ? 0.0f : m;
+        for (int s = way; s < p.parts; s += WAYS) {
             const float2 one = pairs[slot(s)];
             float o[8];
             load8<false>(from, slot(s) * D + 8 * run, o);
@@ -411,17 +415,17 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
             for (int e = 0; e < 8; ++e) y[e] = fmaf(o[e], f, y[e]);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) part[way][run][e] = y[e];
-        if (run == 0) sums[way] = l;
+        for (int e = 0; e < 8; ++e) part[way][in / RUNS][run][e] = y[e];
+        if (run == 0) sums[way][in / RUNS] = l;
     }
     __syncthreads();
-    if (way != 0) return;
-    for (int w = 1; w < WAYS && w < parts; ++w) {
-        l += sums[w];
+    if (way != 0 || !there) return;
+    for (int w = 1; w < WAYS && w < p.parts; ++w) {
+        l += sums[w][in / RUNS];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] += part[w][run][e];
+        for (int e = 0; e < 8; ++e) y[e] += part[w][in / RUNS][run][e];
     }
-    put_row<DB>(a, start, kv_head, row, 8 * run, m, l, y);
+    put_row<DB>(a, p.start, kv_head, p.row0 + row, 8 * run, m, l, y);
 }
 
 }  // namespace sbits
@@ -479,8 +483,14 @@ static int launch(sbits_ctx *ctx, sbits::AttentionArgs &a)
         hipLaunchKernelGGL(kv_attention_few_kernel<DB>, dim3(a.few.splits), dim3(64 * FEW_WAVES), 0, ctx->stream, a);
         SBITS_HIP(ctx, hipGetLastError());
     }
-    if (a.many.each && (rc = join(kv_attention_join_kernel<DB, MANY_ROWS>, MANY_ROWS, a.many.tiles))) return rc;
-    if (a.few.each && (rc = join(kv_attention_join_kernel<DB, FEW_ROWS>, a.few.rows, (int64_t)a.sequences.count * a.few.tiles))) return rc;
+    if (a.many.each && (rc = join(kv_attention_join_kernel<DB, MANY_ROWS, 4>, MANY_ROWS / 4, a.many.tiles))) return rc;
+    // (of few sequences a workgroup a row: there are few, and each has many parts)
+    const int64_t places = (int64_t)a.sequences.count * a.few.tiles;
+    if (a.few.each && places * a.cache.kv_heads >= 128) {
+        if ((rc = join(kv_attention_join_kernel<DB, FEW_ROWS, 4>, (a.few.rows + 3) / 4, places))) return rc;
+    } else if (a.few.each && (rc = join(kv_attention_join_kernel<DB, FEW_ROWS, 1>, a.few.rows, places))) {
+        return rc;
+    }
     return SBITS_OK;
 }
 
