@@ -83,20 +83,20 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     auto fetch = [&](int t, int pages) {                                       // (keys that are not there: of page 0)
         pages = known(pages);
         const int key0 = ((key_first + t * KV_TILE) & a.cache.mask) + 16 * wave;
-        const int64_t base = (int64_t)kv_head << a.cache.shift;
+        const int64_t rows = (int64_t)kv_head << a.cache.shift;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
-            const int page = __shfl(pages, (16 * wave + key) & 63);         // (of all lanes: a lane that is not there would give 0)
+            const uint32_t page = __shfl(pages, (16 * wave + key) & 63);        // (of all lanes: a lane that is not there would give 0)
             if (16 * DB % 64 && key >= 16) continue;
-            const int64_t at = base + ((key0 + key) & a.cache.mask), codes = page * a.cache.ld_codes + at * (16 * DB) + 16 * block;
-            kc[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[0] + codes);
-            vc[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[1] + codes);
-            vs[i] = a.cache.scales[1][page * a.cache.ld_scales + at * SCALES + block];
+            const uint32_t at = (key0 + key) & a.cache.mask;
+            const uint64_t codes = (uint64_t)page * (uint32_t)a.cache.ld_codes + (at * (16 * DB) + 16 * block);
+            kc[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[0] + rows * (16 * DB) + codes);
+            vc[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[1] + rows * (16 * DB) + codes);
+            vs[i] = (a.cache.scales[1] + rows * SCALES)[(uint64_t)page * (uint32_t)a.cache.ld_scales + (at * SCALES + block)];
         }
-        const int page = __shfl(pages, 16 * wave + lane % 16);
-        const int64_t at = base + ((key0 + lane % 16) & a.cache.mask);
-        if (lane < 16 * (SCALES / 4)) ks = *reinterpret_cast<const uint32_t *>(a.cache.scales[0] + page * a.cache.ld_scales + at * SCALES + lane / 16 * 4);
+        const uint32_t page = __shfl(pages, 16 * wave + lane % 16), at = (key0 + lane % 16) & a.cache.mask;
+        if (lane < 16 * (SCALES / 4)) ks = *reinterpret_cast<const uint32_t *>(a.cache.scales[0] + rows * SCALES + ((uint64_t)page * (uint32_t)a.cache.ld_scales + (at * SCALES + lane / 16 * 4)));
     };
     auto put = [&](int buffer, uint64_t valid) {
         const uint32_t mine = (uint32_t)(valid >> 16 * wave) & 0xffffu;
@@ -157,9 +157,11 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
     float top = -INFINITY, sum = 0.0f;
     uint32_t spoiled = 0;
-    // a tile of keys, 32 after the other (in a loop: with both halves in one piece registers do not suffice); special: not all seen by all rows, or v not all in fp16
-    auto take = [&](auto special_, int buffer, int key0, uint64_t valid) {
-        constexpr bool SPECIAL = decltype(special_)::value;
+    // a tile of keys, 32 after the other (in a loop: with both halves in one piece registers do not suffice); hidden: not all seen by all rows, kinds: v not all in fp16.
+    // (What is special is done behind conditions of its own, each without an else: two ways to the sums would cost a copy of them a tile.)
+    auto take = [&](bool hidden, uint32_t kinds, int buffer, int key0, uint64_t valid) {
+        uint32_t others = kinds;
+        asm volatile("" : "+s"(others));
 #pragma unroll 1
         for (int m = 0; m < 2; ++m) {
         f32x16 s;
@@ -189,7 +191,8 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                 });
             }
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (SPECIAL) {
+            if (hidden) {
+                asm volatile("" ::: "memory");
                 const int h4 = fresh(4 * h), from = lo - key0 - h4, past = hi - key0 - h4;
                 const uint32_t mine = (uint32_t)(valid >> 32 * m) >> h4;
 #pragma unroll
@@ -223,20 +226,30 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                     sum += w[j];
                 }
                 const unsigned char *const at = sh.v[buffer] + (16 * step + 4 * h + n % 16 / 4) * V_PITCH + 32 * (n / 16) + 8 * (n % 4);
-                const uint32_t kind = SPECIAL ? __builtin_amdgcn_readfirstlane(sh.kind[buffer][step]) : 0;
-                if (!SPECIAL || kind == 0) {
+                if (kinds == 0) {
                     const f16x8 p16 = weights_f16(w);
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
                         acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, read_transposed(at + 64 * d, 8 * V_PITCH)), p16, acc[d], 0, 0, 0);
-                } else {
+                }
+                if (others) {
+                    const uint32_t kind = __builtin_amdgcn_readfirstlane(sh.kind[buffer][step]);
                     bf16x8 high, low;
                     weights_bf16(w, high, low);
+                    const f16x8 p16 = weights_f16(w);
 #pragma unroll
                     for (int d = 0; d < DB; ++d) {
-                        const bf16x8 v = __builtin_bit_cast(bf16x8, read_transposed(at + 64 * d, 8 * V_PITCH));
-                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, low, acc[d], 0, 0, 0);
-                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, high, acc[d], 0, 0, 0);
+                        const s16x8 v = read_transposed(at + 64 * d, 8 * V_PITCH);
+                        f32x16 more;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) more[i] = 0.0f;
+                        if (kind == 0) {
+                            more = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), p16, more, 0, 0, 0);
+                        } else {
+                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), low, more, 0, 0, 0);
+                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), high, more, 0, 0, 0);
+                        }
+                        acc[d] += more;
                     }
                     if (kind == 3)
                         for (int j = 0; j < 16; ++j)
@@ -261,8 +274,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         if (key0 < hi_any && key0 + KV_TILE > lo_any) {                        // (else none of this wave's rows sees any of it)
             const uint32_t *const kind = sh.kind[buffer];
             const uint32_t kinds = __builtin_amdgcn_readfirstlane(kind[0] | kind[1] | kind[2] | kind[3]);
-            if (kinds || valid != ~0ull || key0 < lo_all || key0 + KV_TILE > hi_all) take(std::true_type{}, buffer, key0, valid);
-            else take(std::false_type{}, buffer, key0, valid);
+            take(valid != ~0ull || key0 < lo_all || key0 + KV_TILE > hi_all, kinds, buffer, key0, valid);
         }
         __syncthreads();
         valid = valid_next;
