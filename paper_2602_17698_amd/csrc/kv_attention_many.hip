@@ -11,6 +11,7 @@ constexpr int MANY_WAVES = 4;
 // LDS as they are, v's as fp16 (or bf16), in one of two buffers while the other is read; codes are asked for a tile ahead of that, pages' numbers two.
 // Scores, transposed: a lane has k's row and block from LDS and its row of q in 6-bit terms, and gets for row lane % 32 the keys 8 (r / 4) + 4 (lane / 32) + r % 4 of 32.
 // Sums, transposed: weights are where the instruction wants them, if 16 keys come in the order 8 (j / 4) + 4 (lane / 32) + j % 4; v's transposing reads bring them so.
+// In LDS the 16-byte pieces w of a block of v are at w ^ (key % 4), so that a wave's writes, 16 lanes of which have 4 keys' blocks, meet all banks.
 template <int DB>
 struct ManyShared {
     static constexpr int K_PITCH = 16 * (DB | 1), V_PITCH = 64 * DB + (DB % 2 ? 0 : 64), SCALES = (DB + 3) / 4 * 4;      // pitches: neighbouring rows in other banks
@@ -27,7 +28,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     constexpr int D = 32 * DB, KS = (DB + 1) / 2, PIECES = (16 * DB + 63) / 64;
     using Shared = ManyShared<DB>;
     constexpr int K_PITCH = Shared::K_PITCH, V_PITCH = Shared::V_PITCH, SCALES = Shared::SCALES;
-    __shared__ __attribute__((aligned(16))) Shared sh;
+    __shared__ __attribute__((aligned(64))) Shared sh;
     // heads first: neighbouring workgroups, on different dies, have different keys; the last rows of a sequence, which see the most, ahead of the others
     const int kv_head = blockIdx.x, split = blockIdx.y, number = a.many.tiles - 1 - (a.first + (int)blockIdx.z);
     int tile;
@@ -117,9 +118,11 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                 const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
                 if (16 * DB % 64 && key >= 16) continue;
                 const float sc = __uint_as_float(vs[i] << 23);
+                unsigned char *const to = sh.v[buffer];
+                const uint32_t first = (16 * wave + key) * V_PITCH + 64 * block + 16 * (key & 3);
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
-                    *reinterpret_cast<u32x4 *>(sh.v[buffer] + (16 * wave + key) * V_PITCH + 64 * block + 16 * w) = decltype(f16)::value ? mx_halves8(vc[i][w], sc) : mx_values8(vc[i][w], sc);
+                    *reinterpret_cast<u32x4 *>(to + (first ^ 16u * w)) = decltype(f16)::value ? mx_halves8(vc[i][w], sc) : mx_values8(vc[i][w], sc);
             }
         };
         uint32_t kind = 0;
@@ -225,7 +228,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                     w[j] = __builtin_amdgcn_exp2f(fmaf(s[half * 8 + j], scale, -base));
                     sum += w[j];
                 }
-                const unsigned char *const at = sh.v[buffer] + (16 * step + 4 * h + n % 16 / 4) * V_PITCH + 32 * (n / 16) + 8 * (n % 4);
+                const unsigned char *const at = sh.v[buffer] + (16 * step + 4 * h + n % 16 / 4) * V_PITCH + 16 * ((n / 16 * 2 + n % 4 / 2) ^ n % 16 / 4) + 8 * (n % 2);
                 if (kinds == 0) {
                     const f16x8 p16 = weights_f16(w);
 #pragma unroll
