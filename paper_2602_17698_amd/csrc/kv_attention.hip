@@ -65,7 +65,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         const uint64_t in = (uint64_t)(x - begin);
         item = in >> 32 ? (int)(in / (uint32_t)f.keys) : (int)((uint32_t)in / (uint32_t)f.keys);
         off = (int)(x - begin - (int64_t)item * f.keys);
-        const int moved = few_snap(off, f.keys), by = moved - off;
+        const int moved = few_snap(a, f, off), by = moved - off;
         off = moved;
         return x + by;
     };
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             });
         };
         // weights and sums of a tile
-        auto take = [&](Codes &o, auto special_, bool halves, f32x4 (&s)[4], int t, uint32_t fours) {
+        auto take = [&](Codes &o, auto special_, bool halves, bool large, f32x4 (&s)[4], int t, uint32_t fours) {
             constexpr bool SPECIAL = decltype(special_)::value;
             const int key0 = f.first + t * KV_TILE;
             if constexpr (SPECIAL) {
@@ -225,9 +225,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
 #pragma unroll
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, s[b][i]);
             most = across_rows(most, OpMax()) * scale;
-            if (__builtin_amdgcn_ballot_w64(most > top + WEIGHT_SLACK)) {
+            const bool room = SPECIAL && large;
+            if (__builtin_amdgcn_ballot_w64(most > top + (room ? -WEIGHT_ROOM : WEIGHT_SLACK))) {
                 asm volatile("" ::: "memory");                                 // (and this)
-                const float to = fmaxf(most, top), shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
+                const float to = fmaxf(most + (room ? WEIGHT_ROOM : 0.0f), top), shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
                 sum *= shrink;
 #pragma unroll
                 for (int i = 0; i < 2 * DB; ++i) acc[i] *= shrink;
@@ -298,8 +299,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
 #pragma unroll
             for (int i = 0; i < DB; ++i) usual = usual && v_scale(o, i) >= F16_LOW && v_scale(o, i) <= F16_HIGH;
             const bool halves = __builtin_amdgcn_ballot_w64(!usual) == 0;
-            if (halves && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all) take(o, std::false_type{}, true, s, t, fours);
-            else take(o, std::true_type{}, halves, s, t, fours);
+            bool large = false;
+            if (!halves) {
+#pragma unroll
+                for (int i = 0; i < DB; ++i) large = large || v_scale(o, i) >= LARGE_V;
+                large = __builtin_amdgcn_ballot_w64(large) != 0;
+            }
+            if (halves && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all) take(o, std::false_type{}, true, false, s, t, fours);
+            else take(o, std::true_type{}, halves, large, s, t, fours);
             page = page_next;
             page_next = page_third;
             page_third = ahead;
@@ -354,7 +361,7 @@ __device__ __forceinline__ Parts find_parts(const AttentionArgs &a, int place, i
     if constexpr (ROWS == FEW_ROWS) {
         const int sequence = (uint32_t)place / (uint32_t)a.few.tiles, tile = place - sequence * a.few.tiles;
         const FewSequence f = few_sequence(a, sequence);
-        if (tile >= f.tiles || f.keys <= FEW_WHOLE) return p;
+        if (tile >= f.tiles || !few_cuttable(a, f)) return p;
         int64_t begin;
         const int64_t total = few_total(a, sequence, begin);
         begin += ((int64_t)tile * a.cache.kv_heads + kv_head) * f.keys;
@@ -447,7 +454,7 @@ size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache,
     if (!only_many) {
         a.few.tiles = (int)((std::min(new_most * group, FEW_MOST) + FEW_ROWS - 1) / FEW_ROWS);
         a.few.most_rows = (int)(only_few ? INT32_MAX : FEW_MOST);
-        a.few.rows = (int)std::min<int64_t>(FEW_ROWS, tokens * group);
+        a.few.rows = (int)std::min(new_most * group, FEW_MOST);
         // (as many workgroups as run at a time; their parts' join where items may be cut)
         a.few.splits = (int)std::min((cache.head_dim <= 128 ? 2 : 1) * cus, std::max<int64_t>(1, (int64_t)sequences.count * a.few.tiles * cache.kv_heads * keys / FEW_LEAST));
         a.few.each = keys > FEW_WHOLE;
@@ -487,8 +494,8 @@ static int launch(sbits_ctx *ctx, sbits::AttentionArgs &a)
     // (of few sequences a workgroup a row: there are few, and each has many parts)
     const int64_t places = (int64_t)a.sequences.count * a.few.tiles;
     if (a.few.each && places * a.cache.kv_heads >= 128) {
-        if ((rc = join(kv_attention_join_kernel<DB, FEW_ROWS, 4>, (a.few.rows + 3) / 4, places))) return rc;
-    } else if (a.few.each && (rc = join(kv_attention_join_kernel<DB, FEW_ROWS, 1>, a.few.rows, places))) {
+        if ((rc = join(kv_attention_join_kernel<DB, FEW_ROWS, 4>, (std::min(a.few.rows, FEW_ROWS) + 3) / 4, places))) return rc;
+    } else if (a.few.each && (rc = join(kv_attention_join_kernel<DB, FEW_ROWS, 1>, std::min(a.few.rows, FEW_ROWS), places))) {
         return rc;
     }
     return SBITS_OK;

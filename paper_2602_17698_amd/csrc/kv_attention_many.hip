@@ -18,7 +18,7 @@ struct ManyShared {
     unsigned char v[2][KV_TILE * V_PITCH];
     unsigned char k[2][KV_TILE * K_PITCH];
     unsigned char ks[2][KV_TILE * SCALES];
-    uint32_t kind[2][MANY_WAVES];                  // of 16 keys: 0 fp16, 1 bf16, 3 some of them not finite
+    uint32_t kind[2][MANY_WAVES];                  // of 16 keys: 0 fp16, 1 bf16, and 2 some of them not finite, 4 some large
     unsigned char spoiled[2][KV_TILE];             // blocks of a key that are not finite
 };
 
@@ -130,6 +130,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
             write(std::true_type{});
         } else {
             kind = 1;
+            bool large = false;
             uint64_t bad[PIECES];
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
@@ -137,6 +138,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                 bad[i] = __builtin_amdgcn_ballot_w64(is);
                 if (bad[i]) kind = 3;
                 if (is) vc[i] = zero, vs[i] = 127;
+                large = large || ((64 * i + lane) / DB < 16 && vs[i] >= LARGE_V);
             }
             if (kind == 3 && lane < 16) {
                 uint32_t blocks = 0;
@@ -148,6 +150,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                 }
                 sh.spoiled[buffer][16 * wave + lane] = (unsigned char)blocks;
             }
+            if (__builtin_amdgcn_ballot_w64(large)) kind |= 4;
             write(std::false_type{});
         }
         if (lane == 0) sh.kind[buffer][wave] = kind;
@@ -209,9 +212,9 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i]);
             most = op_halves(most, OpMax(), __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false));
             most *= scale;
-            if (__builtin_amdgcn_ballot_w64(most > top + WEIGHT_SLACK)) {
+            if (__builtin_amdgcn_ballot_w64(most > top + (kinds & 4 ? -WEIGHT_ROOM : WEIGHT_SLACK))) {
                 asm volatile("" ::: "memory");                                     // (not for all tiles)
-                const float to = fmaxf(most, top), shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
+                const float to = fmaxf(most + (kinds & 4 ? WEIGHT_ROOM : 0.0f), top), shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
                 sum *= shrink;
 #pragma unroll
                 for (int d = 0; d < DB; ++d) acc[d] *= shrink;
@@ -254,7 +257,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                         }
                         acc[d] += more;
                     }
-                    if (kind == 3)
+                    if (kind & 2)
                         for (int j = 0; j < 16; ++j)
                             if (key0 + 16 * step + j >= lo && key0 + 16 * step + j < hi) spoiled |= sh.spoiled[buffer][16 * step + j];
                 }

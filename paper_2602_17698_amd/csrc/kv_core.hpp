@@ -157,10 +157,10 @@ struct LoadArgs {
     int64_t ld[2], hd[2], tokens;
 };
 // How a kernel's work is cut up: tiles of rows (few: at most, of each sequence; many: of all), and of which sequences, by their rows times the heads of a key's head.
-// few: workgroups, among which the keys are shared out; part: [workgroup][2][rows of a tile][dim], then the same of pairs (largest score, sum)
+// few: workgroups, among which the keys are shared out; each: whether keys may be cut; part: [workgroup][2][rows of a tile][dim], then the same of pairs (largest score, sum)
 // many: parts of the keys, of `each` tiles of them at least; part: [tile][kv_heads][part][rows of a tile][dim], then pairs
 struct AttentionCut {
-    int tiles, rows, splits, each;            // rows: of a tile, at most
+    int tiles, rows, splits, each;            // few: rows of a sequence whose keys may be cut, at most
     int least_rows, most_rows;
     float *part;
 };
@@ -316,8 +316,14 @@ __device__ __forceinline__ int fresh(int v)
 }
 // Where cut w of G falls ahead of its move (w < G): a product in 64 bits, rounded down, which is the same wherever it is asked for.
 __device__ __forceinline__ int64_t few_cut(int w, int workgroups, int64_t total) { return (int64_t)((double)w * ((double)total / (double)workgroups)); }
-// what a cut at `off` tiles of an item of `keys` becomes
-__device__ __forceinline__ int few_snap(int off, int keys) { return off < FEW_EDGE || keys <= FEW_WHOLE ? 0 : keys - off < FEW_EDGE ? keys : off; }
+// Whether a sequence's items may be cut: not where there is no space for parts (no sequence was announced to be long enough), nor short ones, nor those of more
+// rows than were announced (which the parts' join would not reach).
+__device__ __forceinline__ bool few_cuttable(const AttentionArgs &a, const FewSequence &f) { return a.few.each && f.keys > FEW_WHOLE && f.rows <= a.few.rows; }
+// what a cut at `off` tiles of an item becomes
+__device__ __forceinline__ int few_snap(const AttentionArgs &a, const FewSequence &f, int off)
+{
+    return off < FEW_EDGE || !few_cuttable(a, f) ? 0 : f.keys - off < FEW_EDGE ? f.keys : off;
+}
 
 // The tiles of many rows of all sequences are numbered so that sequence b's begin at floor(rows ahead of it / MANY_ROWS) + b, which leaves each as many as
 // it can need.  The sequence and the tile of a number, -1 if there is none.
@@ -444,6 +450,9 @@ __device__ __forceinline__ void weights_bf16(const float (&w)[8], bf16x8 &high, 
 // Weights are 2^9 times what they are against the score that counts as the largest, which follows the largest so far only where that is more than 6 powers of two above it: sums are
 // then hardly ever taken anew, and a weight is below 2^15.  fp16 keeps weights down to 2^-23 with all its bits, and of smaller ones what is a multiple of 2^-33.
 constexpr float WEIGHT_LIFT = 9.0f, WEIGHT_SLACK = 6.0f;
+// Where a tile has values of v from 2^83 on, what counts as the largest score is 20 powers of two above it, so that sums of such values times weights stay within fp32.
+constexpr uint32_t LARGE_V = 210;
+constexpr float WEIGHT_ROOM = 20.0f;
 // The logarithm of the sum: that of weights at their own size, which loses no bits to the lift's.
 __device__ __forceinline__ float log_sum(float lowered, float sum)
 {

@@ -2,9 +2,13 @@
 single tokens, and the router is trained for balance with the gradient of its weights.
 
     python -m paper_2602_17698_amd.experts [--hidden 2048] [--inner 1024] [--experts 64] [--top-k 8] [--tokens 2048] [--steps 40] [--four-bit] [--json]
+                                           [--heads 16 --kv-heads 4]
+
+With --heads there is attention ahead of the experts: a prompt's keys, at rotary positions, and values go into a paged cache in 4 bits, and single tokens are
+decoded behind it, by a graph that is captured once.
 
 Printed for each stage: its time, and how far the layer is from the same one with the bf16 weights (relative, root mean square over some tokens), or how
-far the experts' loads are from even (coefficient of variation).  Runs on one GPU through libscalebits.so; weights and tokens are synthetic (seeded).
+far the experts' loads are from even (coefficient of variation); with attention how far its output is from the one with keys and values in 16 bits.  Runs on one GPU through libscalebits.so; weights and tokens are synthetic (seeded).
 """
 from __future__ import annotations
 
@@ -62,6 +66,55 @@ class Layer:
         return out
 
 
+class Attention:
+    """Attention of one sequence with 4-bit projections and a 4-bit cache of pages of 64 tokens."""
+
+    def __init__(self, torch, sb, ctx, hidden, heads, kv_heads, most, seed=2):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.torch, self.sb, self.ctx, self.heads, self.kv_heads, self.dim = torch, sb, ctx, heads, kv_heads, hidden // heads // 32 * 32 or 32
+        self.widths = [heads * self.dim, kv_heads * self.dim, kv_heads * self.dim]
+        self.project = quantised(torch, sb, ctx, (torch.randn(sum(self.widths), hidden, generator=g, device="cuda") * hidden ** -0.5).bfloat16())
+        self.back = quantised(torch, sb, ctx, (torch.randn(hidden, self.widths[0], generator=g, device="cuda") * self.widths[0] ** -0.5).bfloat16())
+        pages = (most + 63) // 64
+        self.cache = sb.kv_cache(*(torch.zeros(pages, kv_heads, 64, n, dtype=torch.uint8, device="cuda")
+                                   for n in (self.dim // 2, sb.mx_scale_pitch(self.dim)) * 2), self.dim)
+        self.table = torch.randperm(pages, generator=torch.Generator().manual_seed(seed)).int().cuda().view(1, pages)
+        self.length = torch.zeros(1, dtype=torch.int32, device="cuda")
+        self.rotary = sb.rotary(torch.tensor(sb.rotary_turns(self.dim, 500000.0), dtype=torch.float64, device="cuda"))
+
+    def buffers(self, tokens):
+        """What a pass over so many new tokens writes: projections, turned queries, attention, output; its descriptor and workspace."""
+        torch, sb = self.torch, self.sb
+        new = lambda n: torch.empty(tokens, n, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+        seqs = sb.sequences(torch.tensor([0, tokens], dtype=torch.int32, device="cuda"), self.length, self.table, max_new=tokens)
+        need = max(self.ctx.mx_gemm_ws_bytes(self.project, tokens), self.ctx.mx_gemm_ws_bytes(self.back, tokens),
+                   self.ctx.kv_attention_ws_bytes(self.cache, seqs, tokens, self.heads))
+        return new(sum(self.widths)), new(self.widths[0]), new(self.widths[0]), new(self.back.rows), seqs, torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+
+    def __call__(self, x, buffers):
+        """x's tokens are the sequence's next; self.length counts them already."""
+        qkv, turned, mixed, out, seqs, ws = buffers
+        self.ctx.mx_gemm(self.project, x, qkv, ws)
+        q, k, v = (t.unflatten(1, (-1, self.dim)) for t in qkv.split(self.widths, 1))
+        turned, mixed = turned.view(q.shape), mixed.view(q.shape)
+        self.ctx.kv_store(self.cache, seqs, k, v, rotary=self.rotary, q=q, q_out=turned)
+        self.ctx.kv_attention(self.cache, seqs, turned, mixed, ws)
+        self.ctx.mx_gemm(self.back, mixed.flatten(1), out, ws)
+        return out
+
+    def in_16_bits(self, qkv, rows):
+        """The mixed values of some rows with the keys and values of a prompt as they were projected."""
+        torch = self.torch
+        q, k, v = (t.float().unflatten(1, (-1, self.dim)) for t in qkv.split(self.widths, 1))
+        at = torch.arange(len(q), dtype=torch.int32, device="cuda")
+        for t in (q, k):
+            self.ctx.rotate(self.rotary, at, t, t)
+        k, v = (t.repeat_interleave(self.heads // self.kv_heads, 1).transpose(0, 1) for t in (k, v))
+        scores = q[rows].transpose(0, 1) @ k.transpose(1, 2).contiguous() * self.dim ** -0.5
+        scores.masked_fill_(at > at[rows][:, None], float("-inf"))
+        return (torch.softmax(scores, -1) @ v.contiguous()).transpose(0, 1).flatten(1)
+
+
 def main(argv=None) -> int:
     import torch
 
@@ -70,6 +123,8 @@ def main(argv=None) -> int:
     p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     for name, value in (("hidden", 2048), ("inner", 1024), ("experts", 64), ("top-k", 8), ("tokens", 2048), ("steps", 40)):
         p.add_argument("--" + name, type=int, default=value)
+    p.add_argument("--heads", type=int, default=0, help="attention ahead of the experts, with so many heads of queries")
+    p.add_argument("--kv-heads", type=int, default=4)
     p.add_argument("--four-bit", action="store_true", help="activations in 4 bits, too")
     p.add_argument("--json", action="store_true")
     a = p.parse_args(argv)
@@ -89,6 +144,43 @@ def main(argv=None) -> int:
         out = layer(x, logits)
         torch.cuda.synchronize()
         return out, (time.perf_counter() - t0) * 1e6
+
+    if a.heads:
+        steps = 8
+        attention = Attention(torch, sb, ctx, a.hidden, a.heads, a.kv_heads, a.tokens + steps + 1)
+        x = torch.randn(a.tokens, a.hidden, generator=g, device="cuda").bfloat16()
+        buffers = attention.buffers(a.tokens)
+        attention.length.fill_(a.tokens)
+        attention(x, buffers)
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        attention(x, buffers)
+        torch.cuda.synchronize()
+        us = (time.perf_counter() - t0) * 1e6
+        rows = slice(max(0, a.tokens - 64), a.tokens)
+        want = attention.in_16_bits(buffers[0], rows)
+        say(stage="attention, prompt", tokens=a.tokens, us=us, error=float((buffers[2][rows].float() - want).norm() / want.norm()))
+        # single tokens: a graph of the whole pass, replayed with the sequence's new length
+        side = torch.cuda.Stream()
+        own = attention.ctx = sb.Context(0, side.cuda_stream)
+        one, buffers = x[:1].clone(), attention.buffers(1)
+        attention.length.add_(1)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            attention(one, buffers)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            attention(one, buffers)
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(steps):
+            attention.length.add_(1)
+            graph.replay()
+            one.copy_(buffers[3])
+        torch.cuda.synchronize()
+        say(stage="attention, one token", tokens=1, us=(time.perf_counter() - t0) * 1e6 / steps, length=int(attention.length))
+        own.close()
 
     for stage, tokens in (("prompt", a.tokens), ("16 tokens", 16), ("one token", 1)):
         x = torch.randn(tokens, a.hidden, generator=g, device="cuda").bfloat16()
