@@ -171,7 +171,7 @@ int sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_
                        int64_t ld_q, int64_t hd_q, float scale, int causal, int window, void *out_bf16, int64_t ld_out, int64_t hd_out, float *lse,
                        void *ws, size_t ws_bytes)
 {
-    if (!ctx || !tokens_ok(tokens) || (causal & ~1) || window < 0 || (window && !causal) || !(scale > 0.0f) || !isfinite(scale)) return SBITS_ERR_INVALID_ARG;
+    if (!ctx || !tokens_ok(tokens) || (causal & ~1) || window < 0 || (window && !causal) || !(scale > 0.0f) || !isfinite((float)(scale * 1.4426950408889634))) return SBITS_ERR_INVALID_ARG;
     int rc;
     if ((rc = check_cache(cache)) || (rc = check_sequences(sequences))) return rc;
     if (heads < 1 || heads > KV_MAX_QUERY_HEADS || heads % cache->kv_heads || tokens * heads > KV_MAX_ROWS) return SBITS_ERR_BAD_SHAPE;

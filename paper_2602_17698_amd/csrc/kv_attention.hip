@@ -34,14 +34,16 @@ __device__ __forceinline__ void put_row(const AttentionArgs &a, int start, int k
 // lane l then row l % 16 and the keys 16 (l / 16) + 4 r + b.
 // Sums, transposed:  v becomes fp16 or bf16 (exactly) on its way to LDS, 32 keys at a time, key 16 g + 4 r + b to row 16 (b % 2) + 4 g + r, where transposing reads give a lane one element
 // of 8 keys, the ones whose weights it has.
-// A tile's codes of k are asked for when those of the one before the one ahead of it have been used, of v likewise; pages' numbers a tile earlier.
+// A tile's codes of k are asked for when those of the one before have been used, of v likewise; pages' numbers two tiles earlier.  (Codes of two tiles under way took registers
+// that are not there: 171 us where this takes 138.)
+// Reading the cache bounds it: 64 sequences of 1638 to 16384 tokens, 8 heads of 128, 642 MB, 135 .. 138 us or 4.7 TB/s (the same loads without the arithmetic reach 5.8); 131072 tokens of
+// one sequence, 143 MB, 28 us.  Each wave has its chain of scores, weights and sums, two waves a SIMD; a third of the time a SIMD issues vector instructions.
 template <int DB>
 struct FewCodes { u32x4 k[4][(DB + 3) / 4], v[DB], ks[(DB + 3) / 4], vq[DB % 4 ? 1 : DB / 4]; uint8_t vb[DB]; };
 
 template <int DB>
 __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_few_kernel(AttentionArgs a)
 {
-    constexpr int DEPTH = 1;
     constexpr int D = 32 * DB, KS = (DB + 3) / 4, PITCH = 2 * D + 32;          // PITCH: rows 8 banks apart, mod 64 an odd multiple of 8
     __shared__ __attribute__((aligned(16))) unsigned char smem[FEW_WAVES][32 * PITCH];
     __shared__ float2 red[FEW_WAVES][FEW_ROWS];
@@ -60,7 +62,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         if (w == workgroups) return total;
         const int64_t x = few_cut(w, workgroups, total);
         int64_t begin;
-        sequence = __builtin_amdgcn_readfirstlane(few_find(a, x, begin));
+        sequence = __builtin_amdgcn_readfirstlane(max(few_find(a, x, begin), 0));
         f = few_sequence(a, sequence);
         const uint64_t in = (uint64_t)(x - begin);
         item = in >> 32 ? (int)(in / (uint32_t)f.keys) : (int)((uint32_t)in / (uint32_t)f.keys);
@@ -75,7 +77,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         if (off == f.keys) continue;                                           // (cut behind its last tile)
         while (item >= f.tiles * a.cache.kv_heads) {
             item = 0;
-            do f = few_sequence(a, ++sequence); while (f.tiles == 0);
+            do {
+                if (++sequence >= a.sequences.count) return;                   // (only if lengths changed meanwhile)
+                f = few_sequence(a, sequence);
+            } while (f.tiles == 0);
         }
         const int tile = (uint32_t)item / (uint32_t)a.cache.kv_heads, kv_head = item - tile * a.cache.kv_heads;
         const int tile0 = off, tile1 = (int)min((int64_t)f.keys, off + left);
@@ -87,7 +92,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         // (no branch around the load and nothing done with it yet: its number is waited for a tile later, not all loads under way here)
         auto page_at = [&](int t) { return table[max(min(key_at(t), f.last - 1), 0) >> a.cache.shift]; };
         auto page_there = [&](int page, int t) { return key_at(t) < f.last && (uint32_t)page < (uint64_t)a.cache.pages; };
-        Codes even, odd;                                                       // odd: of the second of two tiles under way
+        Codes codes;
         auto fetch = [&](auto which_, Codes &o, int t, int page) {                   // 0: k, 1: v  (keys that are not there: of page 0)
             constexpr int WHICH = decltype(which_)::value;
             // (a uniform address and a lane's offset: one product and sum)
@@ -136,15 +141,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         int page = page_at(tile0 + wave), page_next = page_at(tile0 + wave + FEW_WAVES), page_third = page_at(tile0 + wave + 2 * FEW_WAVES);
         // (Loads are never in a branch: behind one the compiler would wait for all that are under way.  Where there is no tile to ask for, this one is asked for again.)
         auto ask = [&](auto which, Codes &o, int t) {
-            const int on = t + DEPTH * FEW_WAVES;
-            fetch(which, o, on < tile1 ? on : t, on >= tile1 ? page : DEPTH == 1 ? page_next : page_third);
+            const int on = t + FEW_WAVES;
+            fetch(which, o, on < tile1 ? on : t, on < tile1 ? page_next : page);
         };
-        fetch(K, even, tile0 + wave, page);
-        fetch(V, even, tile0 + wave, page);
-        if constexpr (DEPTH == 2) {
-            fetch(K, odd, tile0 + wave + FEW_WAVES, page_next);
-            fetch(V, odd, tile0 + wave + FEW_WAVES, page_next);
-        }
+        fetch(K, codes, tile0 + wave, page);
+        fetch(V, codes, tile0 + wave, page);
         // this lane's row
         const int r = tile * FEW_ROWS + n;
         const bool there = r < f.rows;
@@ -311,10 +312,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             page_next = page_third;
             page_third = ahead;
         };
-        for (int t = tile0 + wave; t < tile1; t += DEPTH * FEW_WAVES) {
-            step(even, t);
-            if (DEPTH == 2 && t + FEW_WAVES < tile1) step(odd, t + FEW_WAVES);
-        }
+        for (int t = tile0 + wave; t < tile1; t += FEW_WAVES) step(codes, t);
         sum = across_rows(sum, OpAdd());
 #pragma unroll
         for (int d = 0; d < 2 * DB; ++d) {

@@ -121,7 +121,7 @@ def test_store_refuses_rotations(ctx):
 
 @pytest.mark.parametrize("at,value,status", [
     (2, -1, -1), (3, 7, -2), (3, 0, -2), (3, 65536, -2), (2, 1 << 28, -2), (4, None, -1), (4, A + 2, -1), (5, 1020, -1), (7, 0.0, -1), (7, -1.0, -1), (7, math.nan, -1),
-    (7, math.inf, -1), (8, 2, -1), (9, -1, -1), (10, None, -1), (11, 64, -1), (12, 120, -1), (13, A + 2, -1)])
+    (7, math.inf, -1), (7, 3e38, -1), (8, 2, -1), (9, -1, -1), (10, None, -1), (11, 64, -1), (12, 120, -1), (13, A + 2, -1)])
 def test_attention_refuses(ctx, at, value, status):
     assert attend(ctx, change=[(at, value)]) == status
     assert attend(ctx, change=[(8, 0), (9, 5)]) == -1                    # a window needs an order
