@@ -1,7 +1,8 @@
 // Rotary positions: pairs (a, b) of a head to (a cos - b sin, b cos + a sin) * amplitude, angles from a table of turns a position.
 //
 // Memory bounds it: 2 or 4 bytes read and written for each element; the angles of a row, in 64 bits, are computed once for all its heads.  A workgroup
-// has a row: its first threads make the cosines and sines, in LDS, then a thread takes 8 pairs (two 16-byte loads each way) or elements that stay.
+// has a row: its first threads make the cosines and sines, in LDS, then a thread takes 8 pairs (two 16-byte loads each way) or elements that stay;
+// one where pairs, pitches or addresses are no multiples of 16 bytes.  8192 rows of 40 heads of 128 in bf16: 32 us, 5.2 TB/s, what a copy reaches; one row 2.7.
 #include "kv_core.hpp"
 
 namespace sbits {
