@@ -158,7 +158,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = load_q<4>(a, there && 4 * s + g < DB, token, head, 4 * s + g, fine);
         const uint64_t broken = __builtin_amdgcn_ballot_w64(!fine);
-        const float scale = ((broken | broken >> 16 | broken >> 32 | broken >> 48) >> n & 1) ? NAN : a.scale;
+        const bool row_broken = (broken | broken >> 16 | broken >> 32 | broken >> 48) >> n & 1;
+        const float scale = a.scale;
         // the keys that all rows see
         int lo_all = lo, hi_all = hi;
 #pragma unroll
@@ -314,6 +315,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         };
         for (int t = tile0 + wave; t < tile1; t += FEW_WAVES) step(codes, t);
         sum = across_rows(sum, OpAdd());
+        // (of one row's lanes some may have had none of the pieces that are not finite; a q that is not makes a row NaN that has seen a key)
+        spoil |= __shfl_xor(spoil, 16);
+        spoil |= __shfl_xor(spoil, 32);
+        if (row_broken && sum != 0.0f) spoil = ~0u, sum = NAN;
 #pragma unroll
         for (int d = 0; d < 2 * DB; ++d) {
             if (spoil >> d / 2 & 1) acc[d] = f32x4{NAN, NAN, NAN, NAN};

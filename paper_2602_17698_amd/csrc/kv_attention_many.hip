@@ -73,7 +73,8 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         __builtin_amdgcn_sched_barrier(0);
     }
     const uint64_t broken = __builtin_amdgcn_ballot_w64(!fine);
-    const float scale = ((broken | broken >> 32) >> n & 1) ? NAN : a.scale;
+    const bool row_broken = (broken | broken >> 32) >> n & 1;
+    const float scale = a.scale;
 
     const int32_t *const table = a.sequences.pages + sequence * a.sequences.ld_pages;
     // (no branch around the load and nothing done with it yet: its number is waited for a tile later, not all loads under way here)
@@ -291,6 +292,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         pages_next = pages_ahead;
     }
     sum = op_halves(sum, OpAdd(), __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false));
+    if (row_broken && sum != 0.0f) spoiled = ~0u, sum = NAN;                   // (a q that is not finite, of a row that has seen a key)
     top -= WEIGHT_LIFT;
     const int64_t slot = (((int64_t)number * a.cache.kv_heads + kv_head) * a.many.splits + split) * MANY_ROWS + 32 * wave + n;
     const float over = p.parts > 1 ? 1.0f : top == -INFINITY && sum == 0.0f ? 0.0f : 1.0f / sum;

@@ -347,6 +347,33 @@ def test_attention_only_what_is_seen_counts(ctx, sizes):
     assert ((got - want).abs() <= off)[~torch.isnan(want)].all()
 
 
+@pytest.mark.parametrize("dim", [32, 96, 160, 224, 64, 256])
+@pytest.mark.parametrize("new", [1, 70])
+def test_attention_values_that_are_not_finite_of_other_heads(ctx, dim, new):
+    b = Batch([(new, 90), (new, 3)], 16, 1, dim, seed=dim)
+    page, at = b.places(0, 0, new + 90)
+    for position in (0, 1, 2, 3, 17, 50, 63, 64, 88):
+        b.scales[1][page[position], 0, at[position], position % (dim // 32)] = 255
+    check(ctx, b, 3)
+    check(ctx, b, 3, window=20, max_new=new)
+
+
+@pytest.mark.parametrize("new", [2, 80])
+def test_attention_rows_that_see_nothing_with_a_query_that_is_not_finite(ctx, new):
+    """Fewer tokens than rows: the first rows lie ahead of the sequence and see nothing."""
+    b = Batch([(new, 0)], 16, 1, 64, seed=3)
+    b.lengths[0] = new - 1
+    q = torch.randn(new, 4, 64, generator=gen(1)).to(BF16)
+    q[0, 1, 5], q[1, 2, 0] = math.inf, math.nan
+    cache, seqs, _ = b.on(sb)
+    out, sums = torch.ones(new, 4, 64, dtype=BF16, device="cuda"), torch.ones(new, 4, device="cuda")
+    ws = torch.empty(ctx.kv_attention_ws_bytes(cache, seqs, new, 4), dtype=torch.uint8, device="cuda")
+    ctx.kv_attention(cache, seqs, q.cuda(), out, ws, lse=sums)
+    assert (out[0] == 0).all() and (sums[0] == -math.inf).all()
+    nan = torch.isnan(out[1:]).cpu()
+    assert nan[0, 2].all() and int(nan.sum()) == 64
+
+
 def test_attention_sequences_that_share_pages(ctx):
     """A prompt's pages in two sequences, which go on in pages of their own."""
     b = Batch([(1, 39), (1, 39)], 8, 2, 64, seed=2)
