@@ -174,7 +174,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         asm volatile("" : "+s"(others));
 #pragma unroll 1
         for (int m = 0; m < 2; ++m) {
-        f32x16 s;
+            f32x16 s;
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = 0.0f;
             {

@@ -420,7 +420,6 @@ __device__ __forceinline__ QBlock<TERMS> load_q(const AttentionArgs &a, bool the
 // Codes times 2^(byte - 127) are fp16 numbers for the bytes 104 .. 140, and a weight in fp16 has 11 bits.  Steps of keys with other bytes take v in bf16, which is exact for
 // all, and weights in two bf16 terms.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 constexpr uint32_t F16_LOW = 104, F16_HIGH = 140;
 __device__ __forceinline__ u32x4 mx_halves8(uint32_t codes, float scale)
 {

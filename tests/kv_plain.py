@@ -102,7 +102,8 @@ def attention(batch, q, scale=None, causal=True, window=0, gone=()):
     value being left out (three parts: 2^-15).  With e the bound on a score (scaled), weights are off by e^(2 e) - 1 and, rounded to bf16 ahead of their product with v, by 2^-8
     each and by 2^-8 of the sum; powers of two, and the sums of weights, add 2^-20.  The output rounds
     once more.  A weight in fp16 is 2^9 times its size against a score
-    that no weight counts more than 1 by; the smallest step is 2^-24: rounding to it costs 2^-25 / 2^9 of the key's v at most, against a sum of weights of 1 or more (where v is in bf16, powers below 2^-126 may count as 0, which costs less)."""
+    that no weight counts more than 1 by; the smallest step is 2^-24: rounding to it costs 2^-25 / 2^9 of the key's v at most, against a sum of weights of 1 or more
+    (where v is in bf16, powers below 2^-126 may count as 0, which costs less)."""
     dim, group = batch.dim, q.shape[1] // batch.kv_heads
     scale = dim ** -0.5 if scale is None else scale
     out, lse, off, off_lse = [], [], [], []
