@@ -2,6 +2,7 @@
 // kv_attention.hip) and entry points (kv.hip), and device helpers.  These sources are compiled with NaN and infinities honoured.
 #pragma once
 
+#include "kv_split.hpp"
 #include "mx_core.hpp"
 
 namespace sbits {
@@ -190,10 +191,9 @@ constexpr int FEW_ROWS = 16, MANY_ROWS = 128, KV_TILE = 64;      // rows of a ti
 // the keys that a row at a position sees: first .. last - 1
 __device__ __forceinline__ void seen_keys(const AttentionArgs &a, int length, int position, int &first, int &last)
 {
-    last = a.causal && position < length ? position + 1 : length;
-    first = a.window && position >= a.window ? position + 1 - a.window : 0;
-    last = min(last, a.there);
-    last = max(last, first);
+    const KeyRange r = seen_keys(a.causal, a.window, a.there, length, position);
+    first = r.first;
+    last = r.last;
 }
 
 // How a tile of rows goes over a sequence's keys.

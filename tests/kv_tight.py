@@ -1,0 +1,64 @@
+"""Attention to the microscaled cache in 64 bits from what lies in its buffers (pages by the table, lengths and starts as they are), with bounds that count each rounding
+of the kernels once, and inputs for which a single lost or misplaced key is far outside of them."""
+import math
+
+import torch
+
+import kv_plain
+import mx_plain
+
+
+def sequence(b, s):
+    """Which positions of sequence s are there, and their keys and values [kv_heads, positions, dim] (values with bytes from 253 on: NaN)."""
+    length = max(int(b.lengths[s]), 0)
+    at = torch.arange(min(length, b.table.shape[1] * b.page))
+    page = b.table[s].long()[at // b.page] if len(at) else at
+    at, page = at[(page >= 0) & (page < b.pages)], page[(page >= 0) & (page < b.pages)]
+    out = []
+    for i in range(2):
+        code = mx_plain.unpack(b.codes[i][page, :, at % b.page].reshape(-1, b.dim // 2)).view(len(at), b.kv_heads, b.dim)
+        byte = b.scales[i][page, :, at % b.page, :b.dim // 32]
+        x = kv_plain.values(code, byte)
+        if i:
+            x = torch.where((byte >= 253).repeat_interleave(32, -1), math.nan, x)
+        out.append(x.transpose(0, 1))
+    return at, *out
+
+
+def attention(b, q, scale=None, causal=True, window=0, terms=3):
+    """out and lse [rows of sequences, heads, ..] and how far they may be off.
+
+    A score: sums in fp32 of products that are exact, each addition off by 2^-23 of the magnitudes' sum, of which there are no more than terms * dim / 32 and 256 inside
+    instructions; of q what the terms leave out, 2^-15 of its block's largest value with three of them and 2^-18 with four.  A weight: the power of two is off by a unit in the last
+    place, its argument by 2^-23 of its own and the largest score's size; rounded to fp16 2^-11 and, where it is small, by 2^-25 against a sum of 2^9.  Sums of keys by 16 or 32:
+    2^-23 each.  The output: bf16, 2^-8."""
+    dim, group = b.dim, q.shape[1] // b.kv_heads
+    scale = dim ** -0.5 if scale is None else scale
+    parts = []
+    for s in range(len(b.lengths)):
+        first, end = int(b.starts[s]), int(b.starts[s + 1])
+        key, k, v = sequence(b, s)
+        at = int(b.lengths[s]) - end + torch.arange(first, end)[:, None]
+        seen = torch.ones(end - first, len(key), dtype=torch.bool)
+        if causal:
+            seen = (key <= at) & (key > at - window) if window else key <= at
+        x = q[first:end].double().unflatten(1, (b.kv_heads, group))                 # [rows, kv_heads, group, dim]
+        t = scale * torch.einsum("nhgd,hkd->nhgk", x, k)
+        largest = x.unflatten(-1, (-1, 32)).abs().amax(-1, keepdim=True).expand(*x.shape[:-1], -1, 32).flatten(-2)
+        far = scale * torch.einsum("nhgd,hkd->nhgk", (terms * dim / 32 + 256) * 2.0 ** -23 * x.abs() + 2.0 ** (-15 if terms == 3 else -18) * largest, k.abs())
+        hide = ~seen[:, None, None, :]
+        t, far = t.masked_fill(hide, -math.inf), far.masked_fill(hide, 0.0)
+        size_t = t.masked_fill(hide, 0.0).abs()
+        far, size_t = (z.amax(-1, keepdim=True) if len(key) else z.sum(-1, keepdim=True) for z in (far, size_t))
+        lse = torch.logsumexp(t, -1)
+        w = torch.where(seen.any(-1)[:, None, None, None], torch.softmax(t, -1), 0.0)
+        y, size, least = (torch.zeros_like(x) for _ in range(3))
+        for i in range(end - first):                                              # (what a row does not see takes no part, whatever it is)
+            u = v.masked_fill(~seen[i][None, :, None], 0.0)
+            y[i], size[i] = torch.einsum("hgk,hkd->hgd", w[i], u), torch.einsum("hgk,hkd->hgd", w[i], u.abs())
+            least[i] = u.abs().sum(1)[:, None]
+        power = (1 + size_t) * 2.0 ** -22
+        off = (torch.expm1(2 * (far + power).clamp(max=100.0)) + 2.0 ** -11 + (len(key) / 16 + 64) * 2.0 ** -23) * size + 2.0 ** -8 * y.abs() + 2.0 ** -34 * least
+        off_lse = (far + power)[..., 0] + 2.0 ** -22 * (1 + lse.abs().nan_to_num(posinf=0.0))
+        parts.append([z.flatten(1, 2) for z in (y, lse, off, off_lse)])
+    return tuple(torch.cat(p) for p in zip(*parts))
