@@ -572,7 +572,8 @@ int  sbits_rotary_turns(int pairs, double base, int scaling, double factor, doub
 /* out = x with each row turned by its position (int32[tokens], any sign); inverse: by the opposite angle, the
  * amplitude as it is, which is the gradient with respect to x given that with respect to out.
  * x, out: element j of head h of row t at t * ld + h * hd + j, of `type`; x and out may be the same with the same pitches, else they must
- * not overlap.  head_dim 2 .. 256, 2 * pairs <= head_dim.  tokens may be 0.              */
+ * not overlap.  head_dim 2 .. 256, 2 * pairs <= head_dim.  tokens may be 0.  Here and below, no two heads of any rows of
+ * a tensor that is written may have elements in common (of one that is read they may, pitches of 0 included). */
 int  sbits_rotate(sbits_ctx *ctx, const sbits_rotary *rotary, const int32_t *positions, int64_t tokens, int heads, int head_dim,
                   const void *x, int64_t ld_x, int64_t hd_x, int type, int inverse, void *out, int64_t ld_out, int64_t hd_out);
 

@@ -10,7 +10,7 @@ using namespace sbits;
 static bool aligned(const void *p, size_t to) { return p && (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 static bool type_ok(int t) { return t == SBITS_TYPE_FP32 || t == SBITS_TYPE_BF16; }
 static bool tokens_ok(int64_t tokens) { return tokens >= 0 && tokens <= INT32_MAX; }
-// pitches of a tensor [tokens][heads][dim]; of one that is written, rows and heads may not lie in each other
+// pitches of a tensor [tokens][heads][dim]
 static bool pitches_ok(int64_t ld, int64_t hd, int64_t step, int64_t least)
 {
     return ld >= least && hd >= least && ld % step == 0 && hd % step == 0 && ld < ((int64_t)1 << 40) && hd < ((int64_t)1 << 40);
@@ -18,6 +18,17 @@ static bool pitches_ok(int64_t ld, int64_t hd, int64_t step, int64_t least)
 static bool heads_ok(const void *at, int64_t ld, int64_t hd, int type, int64_t least)
 {
     return aligned(at, 16) && pitches_ok(ld, hd, type == SBITS_TYPE_BF16 ? 8 : 4, least);
+}
+// Whether no two heads of any rows have elements in common, of a tensor that is written (pitches of dim at least): mostly all heads of a row lie ahead of the next row, or all rows of
+// a head ahead of the next head.
+static bool apart(int64_t tokens, int64_t heads, int64_t ld, int64_t hd, int64_t dim)
+{
+    if (tokens <= 1 || heads <= 1 || (ld - dim) / hd >= heads - 1 || (hd - dim) / ld >= tokens - 1) return true;
+    for (int64_t h = 1; h < heads; ++h) {
+        const int64_t before = h * hd / ld, rest = h * hd % ld;                // rows that begin up to a head that is h further on
+        if ((before < tokens && rest < dim) || (before + 1 < tokens && ld - rest < dim)) return false;
+    }
+    return true;
 }
 static int need_device(sbits_ctx *ctx)
 {
@@ -108,6 +119,7 @@ int sbits_rotate(sbits_ctx *ctx, const sbits_rotary *rotary, const int32_t *posi
         (x == out && (ld_x != ld_out || hd_x != hd_out)))
         return SBITS_ERR_INVALID_ARG;
     if ((rc = need_device(ctx))) return rc;
+    if (!apart(tokens, heads, ld_out, hd_out, head_dim)) return SBITS_ERR_INVALID_ARG;
     RotateArgs a;
     a.rotary = turns_of(*rotary);
     a.positions = positions;
@@ -134,6 +146,7 @@ int sbits_kv_store(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequ
               (q == q_out && (ld_q != ld_q_out || hd_q != hd_q_out))))
         return SBITS_ERR_INVALID_ARG;
     if ((rc = need_device(ctx))) return rc;
+    if (q && !apart(tokens, q_heads, ld_q_out, hd_q_out, cache->head_dim)) return SBITS_ERR_INVALID_ARG;
     StoreArgs a = {};
     a.cache = pages_of(*cache);
     a.sequences = sequences_of(*sequences);
@@ -155,6 +168,7 @@ int sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_seque
     if (tokens == 0 || sequences->count == 0 || (!k && !v)) return SBITS_OK;
     if ((k && !heads_ok(k, ld_k, hd_k, type, cache->head_dim)) || (v && !heads_ok(v, ld_v, hd_v, type, cache->head_dim))) return SBITS_ERR_INVALID_ARG;
     if ((rc = need_device(ctx))) return rc;
+    if ((k && !apart(tokens, cache->kv_heads, ld_k, hd_k, cache->head_dim)) || (v && !apart(tokens, cache->kv_heads, ld_v, hd_v, cache->head_dim))) return SBITS_ERR_INVALID_ARG;
     const LoadArgs a = {pages_of(*cache), sequences_of(*sequences), {k, v}, {ld_k, ld_v}, {hd_k, hd_v}, tokens};
     return sbits_launch_kv_load(ctx, a, type == SBITS_TYPE_BF16);
 }
@@ -182,6 +196,7 @@ int sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_
     const size_t need = sbits_kv_attention_cut(ctx, *cache, *sequences, tokens, heads, a);
     if (need && (!aligned(ws, 256) || ws_bytes < need)) return SBITS_ERR_WORKSPACE;
     if ((rc = need_device(ctx))) return rc;
+    if (!apart(tokens, heads, ld_out, hd_out, cache->head_dim)) return SBITS_ERR_INVALID_ARG;
     a.cache = pages_of(*cache);
     a.sequences = sequences_of(*sequences);
     a.q = {q_bf16, ld_q, hd_q}; a.out = {out_bf16, ld_out, hd_out};
