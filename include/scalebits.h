@@ -603,7 +603,7 @@ int  sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequ
  * not or a q that is not makes the row NaN.  Scores and sums are taken in fp32 on the matrix cores, in an order that goes with the batch's
  * sizes; a call gives the same bits again.  scale > 0.  ws: 256-byte aligned,
  * sbits_kv_attention_ws_bytes() bytes (which may be 0), asked for with the call's own arguments.  Positions from 2^31 - 4096 on
- * are not there.  With lse, q enters the products in a term more, so that last bits of out may differ.  */
+ * are not there.  At most 2^24 sequences.  With lse, q enters the products in a term more, so that last bits of out may differ.  */
 size_t sbits_kv_attention_ws_bytes(const sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens,
                                    int heads);
 int  sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens, int heads,

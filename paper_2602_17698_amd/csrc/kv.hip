@@ -176,7 +176,7 @@ int sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_seque
 size_t sbits_kv_attention_ws_bytes(const sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens, int heads)
 {
     if (!ctx || check_cache(cache) || check_sequences(sequences) || !tokens_ok(tokens) || heads < 1 || heads > KV_MAX_QUERY_HEADS || heads % cache->kv_heads) return 0;
-    if (tokens == 0 || sequences->count == 0 || tokens * heads > KV_MAX_ROWS) return 0;
+    if (tokens == 0 || sequences->count == 0 || sequences->count > KV_MAX_SEQUENCES || tokens * heads > KV_MAX_ROWS) return 0;
     AttentionArgs a;
     return sbits_kv_attention_cut(ctx, *cache, *sequences, tokens, heads, a);
 }
@@ -188,7 +188,8 @@ int sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_
     if (!ctx || !tokens_ok(tokens) || (causal & ~1) || window < 0 || (window && !causal) || !(scale > 0.0f) || !isfinite((float)(scale * 1.4426950408889634))) return SBITS_ERR_INVALID_ARG;
     int rc;
     if ((rc = check_cache(cache)) || (rc = check_sequences(sequences))) return rc;
-    if (heads < 1 || heads > KV_MAX_QUERY_HEADS || heads % cache->kv_heads || tokens * heads > KV_MAX_ROWS) return SBITS_ERR_BAD_SHAPE;
+    if (heads < 1 || heads > KV_MAX_QUERY_HEADS || heads % cache->kv_heads || tokens * heads > KV_MAX_ROWS || sequences->count > KV_MAX_SEQUENCES)
+        return SBITS_ERR_BAD_SHAPE;
     if (tokens == 0 || sequences->count == 0) return SBITS_OK;
     if (!heads_ok(q_bf16, ld_q, hd_q, SBITS_TYPE_BF16, 0) || !heads_ok(out_bf16, ld_out, hd_out, SBITS_TYPE_BF16, cache->head_dim) || (lse && !aligned(lse, 4)))
         return SBITS_ERR_INVALID_ARG;

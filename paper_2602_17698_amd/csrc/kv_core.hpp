@@ -179,6 +179,7 @@ struct AttentionArgs {
 };
 constexpr int KV_MAX_KEYS = INT32_MAX - 4095, KV_MAX_ROWS = INT32_MAX - 255;   // some tiles of keys, or a tile of rows, more are numbers still
 constexpr int KV_MAX_PARTS = 1024;
+constexpr int KV_MAX_SEQUENCES = 1 << 24;    // of an attention: numbers of tiles and of joined items stay within 31 bits
 // z of a launch: at most 2^22 workgroups, 2^30 threads
 inline int64_t kv_launch(int64_t x, int64_t y)
 {

@@ -57,3 +57,21 @@ LARGE = [(1 << 30, 2, 32, 1 << 35, True), (1 << 30, 2, 32, (1 << 35) - 32, False
 def test_large_outputs(tmp_path):
     got = record(tmp_path, SCRIPT + "answer([rotate(*a[:4]) for a in %r])" % (LARGE,))
     assert got == [sb.OK if a[4] else sb.ERR_INVALID_ARG for a in LARGE]
+
+
+def test_attention_of_more_sequences_than_its_numbers_hold_is_refused(tmp_path):
+    """Items to be joined are counted in 31 bits: four tiles of rows a sequence, and those of many rows beside them."""
+    got = record(tmp_path, SCRIPT + """
+out = []
+for count in (1 << 24, (1 << 24) + 1, 1 << 30, (1 << 31) - 2):
+    seqs = sb.Sequences(A, A, A, 32, count, 32, 0, 0)
+    cache = sb.KvCache(A, A, A, A, 8, 64 * 16, 64 * 4, 64, 1, 32)
+    need = call("kv_attention_ws_bytes", cache, seqs, 100000, 8)
+    log()
+    rc = call("kv_attention", cache, seqs, 100000, 8, A, 256, 32, 0.1, 1, 0, A, 256, 32, None, A, 1 << 40)
+    lines = [line.split() for line in log()]
+    out.append((need > 0, rc, sum(int(line[3].split(",")[2]) for line in lines if "join" in line[1]), sum(int(line[3].split(",")[2]) for line in lines if "many_kernel" in line[1])))
+answer(out)
+""")
+    tiles = 100000 * 8 // 128 + (1 << 24)
+    assert got == [[True, sb.OK, 4 << 24, tiles]] + [[False, sb.ERR_BAD_SHAPE, 0, 0]] * 3
