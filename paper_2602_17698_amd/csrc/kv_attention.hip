@@ -176,7 +176,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         float top = -INFINITY, sum = 0.0f;
         uint32_t spoil = 0;                                                    // blocks of this lane's row with a seen value that is not finite
         unsigned char *const lds = smem[wave];
-        // half of v's keys (those with the same b / 2) to LDS; special: not all keys there, or other powers than fp16 has
+        // Half of v's keys (those with the same b / 2) to LDS, in fp16 or bf16; special: not all keys are there, or their powers others than fp16 has.  Fp16 then has the pieces with its powers, bf16 the
+        // others, and zeros are where the other's pieces are.
         auto put = [&](const Codes &o, auto special_, auto f16_, auto half_, int key0, bool v_there) {
             constexpr bool SPECIAL = decltype(special_)::value, F16 = decltype(f16_)::value;
             constexpr int HALF = decltype(half_)::value;
@@ -188,20 +189,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                 if (DB % 2 && four / 2 != HALF) return;
                 u32x4 codes = o.v[i];
                 uint32_t byte = v_scale(o, i);
-                if constexpr (SPECIAL) {
-                    bool ok = v_there && key0 + key < f.last;
-                    if constexpr (!F16) {
-                        const bool bad = ok && byte >= KV_V_LIMIT;
-                        uint64_t bads = __builtin_amdgcn_ballot_w64(bad);
-                        while (bads) {
-                            const int from = __builtin_ctzll(bads), bad_key = __builtin_amdgcn_readlane(key, from), bad_block = __builtin_amdgcn_readlane(block, from);
-                            bads &= bads - 1;
-                            if (key0 + bad_key >= lo && key0 + bad_key < hi) spoil |= 1u << bad_block;
-                        }
-                        ok = ok && !bad;
-                    }
-                    if (!ok) codes = zero, byte = 127;
-                }
+                if constexpr (SPECIAL)
+                    if (!v_there || key0 + key >= f.last || f16_power(byte) != F16 || byte >= KV_V_LIMIT) codes = zero, byte = 127;
                 const float sc = __uint_as_float(byte << 23);
                 unsigned char *const to = lds + (16 * (four & 1) + n) * PITCH + 64 * block;
 #pragma unroll
@@ -210,9 +199,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             });
         };
         // weights and sums of a tile
-        auto take = [&](Codes &o, auto special_, bool halves, bool large, f32x4 (&s)[4], int t, uint32_t fours) {
+        auto take = [&](Codes &o, auto special_, f32x4 (&s)[4], int t, uint32_t fours) {
             constexpr bool SPECIAL = decltype(special_)::value;
             const int key0 = f.first + t * KV_TILE;
+            bool others = false, room = false;                                 // pieces that fp16 does not have; whether this lane's row sees large values
             if constexpr (SPECIAL) {
                 const int g4 = fresh(4 * g), from = lo - key0 - 4 * g4, past = hi - key0 - 4 * g4;
                 const uint32_t mine = fours >> g4;
@@ -220,6 +210,41 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[b][i] = (mine >> i & 1) && 4 * i + b >= from && 4 * i + b < past ? s[b][i] : -INFINITY;
+                // of the keys that are there: what v has beside the powers of fp16
+                const int g = fresh(lane >> 4), n = fresh(lane & 15);
+                auto is_there = [&](int i) { return (fours >> n & 1) && key0 + 4 * n + v_key(i, g) < f.last; };
+                uint32_t highest = 0;
+#pragma unroll
+                for (int i = 0; i < DB; ++i)
+                    if (is_there(i) && !f16_power(v_scale(o, i))) others = true, highest = max(highest, v_scale(o, i));
+                others = __builtin_amdgcn_ballot_w64(others) != 0;
+                if (__builtin_amdgcn_ballot_w64(highest >= LARGE_V)) {
+                    uint32_t large[4] = {0, 0, 0, 0};                          // of the keys 4 n + b those with large values, a bit each
+                    static_for<0, DB>([&](auto i_) {
+                        constexpr int i = decltype(i_)::value;
+                        const bool ok = is_there(i);
+                        const uint32_t byte = v_scale(o, i);
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            const uint64_t are = __builtin_amdgcn_ballot_w64(ok && byte >= LARGE_V && byte < KV_V_LIMIT && v_key(i, g) == b);
+                            large[b] |= (uint32_t)(are | are >> 16 | are >> 32 | are >> 48) & 0xffffu;
+                        }
+                        uint64_t bads = __builtin_amdgcn_ballot_w64(ok && byte >= KV_V_LIMIT);
+                        const int key = 4 * n + v_key(i, g), block = v_block(i, g);
+                        while (bads) {
+                            const int from = __builtin_ctzll(bads), bad_key = __builtin_amdgcn_readlane(key, from), bad_block = __builtin_amdgcn_readlane(block, from);
+                            bads &= bads - 1;
+                            if (key0 + bad_key >= lo && key0 + bad_key < hi) spoil |= 1u << bad_block;
+                        }
+                    });
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) room = room || ((large[b] >> 4 * g >> i & 1) && s[b][i] > -INFINITY);
+                    uint64_t rows = __builtin_amdgcn_ballot_w64(room);
+                    rows |= rows >> 32;
+                    room = (rows | rows >> 16) >> n & 1;
+                }
             }
             float most = -INFINITY;
 #pragma unroll
@@ -227,10 +252,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
 #pragma unroll
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, s[b][i]);
             most = across_rows(most, OpMax()) * scale;
-            const bool room = SPECIAL && large;
-            if (__builtin_amdgcn_ballot_w64(most > top + (room ? -WEIGHT_ROOM : WEIGHT_SLACK))) {
+            // (each row by itself: what one sees does not move another's)
+            const bool grown = most > top + (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
+            if (__builtin_amdgcn_ballot_w64(grown)) {
                 asm volatile("" ::: "memory");                                 // (and this)
-                const float to = fmaxf(most + (room ? WEIGHT_ROOM : 0.0f), top), shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
+                const float to = grown ? most + (room ? WEIGHT_ROOM : 0.0f) : top, shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
                 sum *= shrink;
 #pragma unroll
                 for (int i = 0; i < 2 * DB; ++i) acc[i] *= shrink;
@@ -249,28 +275,31 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             static_for<0, 2>([&](auto half_) {
                 constexpr int half = decltype(half_)::value;
                 __builtin_amdgcn_wave_barrier();
-                if constexpr (!SPECIAL) put(o, std::false_type{}, std::true_type{}, half_, key0, true);
-                else if (halves) put(o, std::true_type{}, std::true_type{}, half_, key0, fours >> n & 1);
-                else put(o, std::true_type{}, std::false_type{}, half_, key0, fours >> n & 1);
-                if (half == 1) ask(V, o, t);
+                put(o, special_, std::true_type{}, half_, key0, fours >> n & 1);
+                if (!SPECIAL && half == 1) ask(V, o, t);
                 __builtin_amdgcn_wave_barrier();
                 const unsigned char *const at = lds + (4 * g + n / 4) * PITCH + 8 * (n % 4);
-                if (!SPECIAL || halves) {
-                    const f16x8 p16 = weights_f16(w[half]);
+                const f16x8 p16 = weights_f16(w[half]);
 #pragma unroll
-                    for (int d = 0; d < 2 * DB; ++d) {
-                        acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, read_transposed(at + 32 * d, 16 * PITCH)), p16, acc[d], 0, 0, 0);
-                        if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                    }
-                } else {
-                    bf16x8 high, low;
-                    weights_bf16(w[half], high, low);
+                for (int d = 0; d < 2 * DB; ++d) {
+                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, read_transposed(at + 32 * d, 16 * PITCH)), p16, acc[d], 0, 0, 0);
+                    if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (SPECIAL) {
+                    if (others) {
+                        __builtin_amdgcn_wave_barrier();
+                        put(o, special_, std::false_type{}, half_, key0, fours >> n & 1);
+                        __builtin_amdgcn_wave_barrier();
+                        bf16x8 high, low;
+                        weights_bf16(w[half], high, low);
 #pragma unroll
-                    for (int d = 0; d < 2 * DB; ++d) {
-                        const bf16x8 v = __builtin_bit_cast(bf16x8, read_transposed(at + 32 * d, 16 * PITCH));
-                        acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, low, acc[d], 0, 0, 0);
-                        acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high, acc[d], 0, 0, 0);
+                        for (int d = 0; d < 2 * DB; ++d) {
+                            const bf16x8 v = __builtin_bit_cast(bf16x8, read_transposed(at + 32 * d, 16 * PITCH));
+                            acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, low, acc[d], 0, 0, 0);
+                            acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high, acc[d], 0, 0, 0);
+                        }
                     }
+                    if (half == 1) ask(V, o, t);
                 }
             });
         };
@@ -297,18 +326,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             asm volatile("" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
             ask(K, o, t);
             __builtin_amdgcn_sched_barrier(0);
-            bool usual = true;                                                 // all in fp16 (keys that are not there count, too: they may make the tile a special one)
+            bool usual = true;                                                 // all in fp16 (keys that are not there count, too: they may make the tile a special one, which finds out)
 #pragma unroll
-            for (int i = 0; i < DB; ++i) usual = usual && v_scale(o, i) >= F16_LOW && v_scale(o, i) <= F16_HIGH;
-            const bool halves = __builtin_amdgcn_ballot_w64(!usual) == 0;
-            bool large = false;
-            if (!halves) {
-#pragma unroll
-                for (int i = 0; i < DB; ++i) large = large || v_scale(o, i) >= LARGE_V;
-                large = __builtin_amdgcn_ballot_w64(large) != 0;
-            }
-            if (halves && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all) take(o, std::false_type{}, true, false, s, t, fours);
-            else take(o, std::true_type{}, halves, large, s, t, fours);
+            for (int i = 0; i < DB; ++i) usual = usual && f16_power(v_scale(o, i));
+            if (__builtin_amdgcn_ballot_w64(!usual) == 0 && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all) take(o, std::false_type{}, s, t, fours);
+            else take(o, std::true_type{}, s, t, fours);
             page = page_next;
             page_next = page_third;
             page_third = ahead;

@@ -21,9 +21,24 @@ struct ManyShared {
     unsigned char v[2][KV_TILE * V_PITCH];
     unsigned char k[2][KV_TILE * K_PITCH];
     unsigned char ks[2][KV_TILE * SCALES];
-    uint32_t kind[2][MANY_WAVES];                  // of 16 keys: 0 fp16, 1 bf16, and 2 some of them not finite, 4 some large
+    uint32_t kind[2][MANY_WAVES];                  // of 16 keys: 0 all in fp16, 1 some blocks in bf16, and 2 some of them not finite, 4 some large
+    uint16_t others[2][MANY_WAVES][DB];            // of a block those of 16 keys that are in bf16
+    uint16_t large[2][MANY_WAVES];                 // keys with large values
     unsigned char spoiled[2][KV_TILE];             // blocks of a key that are not finite
 };
+
+// of the 8 elements of the keys 8 (j / 4) + 4 h + j % 4 those whose bit is set, else 0
+__device__ __forceinline__ s16x8 only_keys(s16x8 v, uint32_t keys, int h)
+{
+    const uint32_t mine = keys >> 4 * h;
+    u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int at = 8 * (i / 2) + 2 * (i % 2);
+        x[i] &= (0u - (mine >> at & 1)) & 0xffffu | (0u - (mine >> at >> 1 & 1)) & 0xffff0000u;
+    }
+    return __builtin_bit_cast(s16x8, x);
+}
 
 template <int DB, int TERMS>
 __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention_many_kernel(AttentionArgs a)
@@ -112,11 +127,10 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
             if (16 * DB % 64 && key >= 16) continue;
             *reinterpret_cast<u32x4 *>(sh.k[buffer] + (16 * wave + key) * K_PITCH + 16 * block) = kc[i];
             if (!(mine >> key & 1)) vc[i] = zero, vs[i] = 127;
-            usual = usual && vs[i] >= F16_LOW && vs[i] <= F16_HIGH;
+            usual = usual && f16_power(vs[i]);
         }
         if (lane < 16 * (SCALES / 4)) *reinterpret_cast<uint32_t *>(sh.ks[buffer] + (16 * wave + lane % 16) * SCALES + lane / 16 * 4) = ks;
-        const bool halves = __builtin_amdgcn_ballot_w64(!usual) == 0;
-        auto write = [&](auto f16) {
+        auto write = [&](auto all_f16) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
@@ -126,35 +140,44 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                 const uint32_t first = (16 * wave + key) * V_PITCH + 64 * block + 16 * (key & 3);
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
-                    *reinterpret_cast<u32x4 *>(to + (first ^ 16u * w)) = decltype(f16)::value ? mx_halves8(vc[i][w], sc) : mx_values8(vc[i][w], sc);
+                    *reinterpret_cast<u32x4 *>(to + (first ^ 16u * w)) = decltype(all_f16)::value || f16_power(vs[i]) ? mx_halves8(vc[i][w], sc) : mx_values8(vc[i][w], sc);
             }
         };
         uint32_t kind = 0;
-        if (halves) {
+        if (__builtin_amdgcn_ballot_w64(!usual) == 0) {
             write(std::true_type{});
         } else {
-            kind = 1;
-            bool large = false;
-            uint64_t bad[PIECES];
+            // a lane a key: its blocks of which something is so, a bit each
+            auto blocks_where = [&](auto is) {
+                uint64_t are[PIECES];
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) {
-                const bool is = (64 * i + lane) / DB < 16 && vs[i] >= KV_V_LIMIT;
-                bad[i] = __builtin_amdgcn_ballot_w64(is);
-                if (bad[i]) kind = 3;
-                if (is) vc[i] = zero, vs[i] = 127;
-                large = large || ((64 * i + lane) / DB < 16 && vs[i] >= LARGE_V);
-            }
-            if (kind == 3 && lane < 16) {
+                for (int i = 0; i < PIECES; ++i) are[i] = __builtin_amdgcn_ballot_w64((64 * i + lane) / DB < 16 && is(vs[i]));
                 uint32_t blocks = 0;
                 for (int b = 0; b < DB; ++b) {
-                    const int piece = lane * DB + b;
-                    uint64_t from = bad[0];
-                    if (PIECES > 1 && piece >= 64) from = bad[PIECES - 1];
+                    const int piece = lane % 16 * DB + b;
+                    uint64_t from = are[0];
+                    if (PIECES > 1 && piece >= 64) from = are[PIECES - 1];
                     blocks |= (uint32_t)(from >> piece % 64 & 1) << b;
                 }
-                sh.spoiled[buffer][16 * wave + lane] = (unsigned char)blocks;
+                return blocks;
+            };
+            const uint32_t bad = blocks_where([](uint32_t byte) { return byte >= KV_V_LIMIT; });
+            if (__builtin_amdgcn_ballot_w64(bad != 0)) {
+                kind |= 2;
+                if (lane < 16) sh.spoiled[buffer][16 * wave + lane] = (unsigned char)bad;
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i)
+                    if (vs[i] >= KV_V_LIMIT) vc[i] = zero, vs[i] = 127;
             }
-            if (__builtin_amdgcn_ballot_w64(large)) kind |= 4;
+            const uint32_t others = blocks_where([](uint32_t byte) { return !f16_power(byte); });
+            if (__builtin_amdgcn_ballot_w64(others != 0)) kind |= 1;
+            for (int b = 0; b < DB; ++b) {
+                const uint32_t keys = (uint32_t)__builtin_amdgcn_ballot_w64(others >> b & 1) & 0xffffu;
+                if (lane == 0) sh.others[buffer][wave][b] = (uint16_t)keys;
+            }
+            const uint32_t large = (uint32_t)__builtin_amdgcn_ballot_w64(blocks_where([](uint32_t byte) { return byte >= LARGE_V; }) != 0) & 0xffffu;
+            if (large) kind |= 4;
+            if (lane == 0) sh.large[buffer][wave] = (uint16_t)large;
             write(std::false_type{});
         }
         if (lane == 0) sh.kind[buffer][wave] = kind;
@@ -216,9 +239,20 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i]);
             most = op_halves(most, OpMax(), __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false));
             most *= scale;
-            if (__builtin_amdgcn_ballot_w64(most > top + (kinds & 4 ? -WEIGHT_ROOM : WEIGHT_SLACK))) {
+            bool room = false;                                                     // whether this lane's row sees large values
+            if (kinds & 4) {
+                const uint32_t *const kind = sh.kind[buffer] + 2 * m;
+                const uint32_t low = kind[0] & 4 ? sh.large[buffer][2 * m] : 0, high = kind[1] & 4 ? sh.large[buffer][2 * m + 1] : 0, mine = (low | high << 16) >> 4 * h;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) room = room || ((mine >> (8 * (i / 4) + i % 4) & 1) && s[i] > -INFINITY);
+                const uint64_t rows = __builtin_amdgcn_ballot_w64(room);
+                room = (rows | rows >> 32) >> n & 1;
+            }
+            // (each row by itself: what one sees does not move another's)
+            const bool grown = most > top + (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
+            if (__builtin_amdgcn_ballot_w64(grown)) {
                 asm volatile("" ::: "memory");                                     // (not for all tiles)
-                const float to = fmaxf(most + (kinds & 4 ? WEIGHT_ROOM : 0.0f), top), shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
+                const float to = grown ? most + (room ? WEIGHT_ROOM : 0.0f) : top, shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
                 sum *= shrink;
 #pragma unroll
                 for (int d = 0; d < DB; ++d) acc[d] *= shrink;
@@ -243,6 +277,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                         acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, read_transposed(at + 64 * d, 8 * V_PITCH)), p16, acc[d], 0, 0, 0);
                 }
                 if (others) {
+                    // (a row's sums are the same whichever way a tile goes that it sees nothing unusual of: fp16 as above, and zeros added)
                     const uint32_t kind = __builtin_amdgcn_readfirstlane(sh.kind[buffer][step]);
                     bf16x8 high, low;
                     weights_bf16(w, high, low);
@@ -250,16 +285,17 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
 #pragma unroll
                     for (int d = 0; d < DB; ++d) {
                         const s16x8 v = read_transposed(at + 64 * d, 8 * V_PITCH);
-                        f32x16 more;
+                        const uint32_t keys = kind & 1 ? __builtin_amdgcn_readfirstlane(sh.others[buffer][step][d]) : 0;
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, only_keys(v, ~keys, h)), p16, acc[d], 0, 0, 0);
+                        if (keys) {
+                            const bf16x8 b = __builtin_bit_cast(bf16x8, only_keys(v, keys, h));
+                            f32x16 more;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) more[i] = 0.0f;
-                        if (kind == 0) {
-                            more = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), p16, more, 0, 0, 0);
-                        } else {
-                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), low, more, 0, 0, 0);
-                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), high, more, 0, 0, 0);
+                            for (int i = 0; i < 16; ++i) more[i] = 0.0f;
+                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, low, more, 0, 0, 0);
+                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, high, more, 0, 0, 0);
+                            acc[d] += more;
                         }
-                        acc[d] += more;
                     }
                     if (kind & 2)
                         for (int j = 0; j < 16; ++j)

@@ -418,10 +418,12 @@ __device__ __forceinline__ QBlock<TERMS> load_q(const AttentionArgs &a, bool the
 }
 
 // ---- sums: v in fp16 where that is exact, else in bf16 ----------------------------------
-// Codes times 2^(byte - 127) are fp16 numbers for the bytes 104 .. 140, and a weight in fp16 has 11 bits.  Steps of keys with other bytes take v in bf16, which is exact for
-// all, and weights in two bf16 terms.
+// Codes times 2^(byte - 127) are fp16 numbers for the bytes 104 .. 140, and a weight in fp16 has 11 bits.  Blocks with other bytes enter in bf16, which is exact for
+// all, with weights in two bf16 terms, in products of their own, in which the blocks of fp16 are zeros (and the other way round).  So what a row does not see, with its weight of 0, adds
+// zeros whichever way its block goes: not a bit of the row's sums goes with it.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr uint32_t F16_LOW = 104, F16_HIGH = 140;
+__device__ __forceinline__ bool f16_power(uint32_t byte) { return byte >= F16_LOW && byte <= F16_HIGH; }
 __device__ __forceinline__ u32x4 mx_halves8(uint32_t codes, float scale)
 {
     u32x4 v;

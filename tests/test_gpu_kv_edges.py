@@ -59,3 +59,71 @@ def test_a_window_behind_the_end_of_the_table(ctx, window, sizes, pages):
     if window and sizes[0][1] == 900 or sizes[0][0] == 1 and window:
         assert (out[1] == 0).all() and (sums[1] == -math.inf).all()
     check(ctx, b, queries(b, 4), window=window, lse=False, hints=dict(max_new=max(n for n, _ in sizes)))
+
+
+# ---- what a row does not see ------------------------------------------------------------------------
+def scribble(b, which, page, at, g, junk):
+    """Places of the cache, all heads of them, with other codes and bytes."""
+    if len(page) == 0:
+        return
+    b.codes[which][page, :, at] = torch.randint(0, 256, (len(page), b.kv_heads, b.dim // 2), generator=g).to(torch.uint8)
+    bytes_ = torch.full((len(page), b.kv_heads, b.row), junk) if junk >= 0 else torch.randint(0, 256, (len(page), b.kv_heads, b.row), generator=g)
+    b.scales[which][page, :, at] = bytes_.to(torch.uint8)
+
+
+def unused(b):
+    """Places that no sequence has."""
+    free = torch.ones(b.pages, b.page, dtype=torch.bool)
+    for s in range(len(b.sizes)):
+        page, at = b.places(s, 0, int(b.lengths[s]))
+        free[page, at] = False
+    return free.nonzero(as_tuple=True)
+
+
+SEEN = [[(1, 0), (1, 62), (1, 63), (1, 200), (2, 1500)], [(9, 70), (16, 300), (5, 3)], [(150, 40), (70, 0)]]
+
+
+@pytest.mark.parametrize("junk", [0, 2, 103, 120, 141, 215, 252, 253, 255, -1])
+@pytest.mark.parametrize("sizes", SEEN)
+@pytest.mark.parametrize("dim", [64, 96, 128, 160])
+def test_places_of_no_token_do_not_change_a_bit(ctx, junk, sizes, dim):
+    """Behind the last tokens, on pages of no sequence, on page 0, which stands in for pages that are not there: whatever these hold."""
+    b = Batch(sizes, 16, 2, dim, seed=dim, junk=127, lead=1)
+    b.table[0, -1] = b.pages + 5
+    q = queries(b, 4)
+    want = attend(ctx, b, q)
+    g = torch.Generator().manual_seed(junk + 2)
+    for which in range(2):
+        scribble(b, which, *unused(b), g, junk)
+    for x, y in zip(attend(ctx, b, q), want):
+        assert torch.equal(x, y)
+    check(ctx, b, q)
+
+
+@pytest.mark.parametrize("junk", [2, 100, 150, 215, 250, 255, -1])
+@pytest.mark.parametrize("sizes", SEEN[1:])
+@pytest.mark.parametrize("window", [0, 30])
+@pytest.mark.parametrize("dim", [128, 96])
+def test_hidden_keys_and_other_rows_do_not_change_a_bit(ctx, junk, sizes, window, dim):
+    """Later tokens, with other keys, values and queries; and tokens ahead of all windows of the rows that are looked at."""
+    b = Batch(sizes, 16, 1, dim, seed=dim + window)
+    q = queries(b, 3)
+    want = attend(ctx, b, q, window=window)
+    g = torch.Generator().manual_seed(junk + 2)
+    keep = []                                                    # rows from one on, up to one
+    for s, (n, past) in enumerate(sizes):
+        first, last = n // 3 if window else 0, n // 3 + (n + 2) // 3
+        page, at = b.places(s, past + last, n - last)
+        for which in range(2):
+            scribble(b, which, page, at, g, junk)
+        ahead = max(0, past + first - window + 1) if window else 0
+        page, at = b.places(s, 0, ahead)
+        for which in range(2):
+            scribble(b, which, page, at, g, junk)
+        keep.append(torch.arange(int(b.starts[s]) + first, int(b.starts[s]) + last))
+    keep = torch.cat(keep)
+    others = torch.ones(b.tokens, dtype=torch.bool)
+    others[keep] = False
+    q[others] = (q[others].float() * 3.7).to(BF16).flip(-1)
+    for x, y in zip(attend(ctx, b, q, window=window), want):
+        assert torch.equal(x[keep], y[keep])
