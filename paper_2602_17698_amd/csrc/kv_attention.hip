@@ -175,6 +175,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         for (int i = 0; i < 2 * DB; ++i) acc[i] = f32x4{0, 0, 0, 0};
         float top = -INFINITY, sum = 0.0f;
         uint32_t spoil = 0;                                                    // blocks of this lane's row with a seen value that is not finite
+        uint64_t far = 0;                                                      // lanes of rows with far scores
         unsigned char *const lds = smem[wave];
         // Half of v's keys (those with the same b / 2) to LDS, in fp16 or bf16; special: not all keys are there, or their powers others than fp16 has.  Fp16 then has the pieces with its powers, bf16 the
         // others, and zeros are where the other's pieces are.
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, s[b][i]);
             most = across_rows(most, OpMax()) * scale;
             // (each row by itself: what one sees does not move another's)
-            const bool grown = most > top + (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
+            const bool grown = most - top > (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
             if (__builtin_amdgcn_ballot_w64(grown)) {
                 asm volatile("" ::: "memory");                                 // (and this)
                 const float to = grown ? most + (room ? WEIGHT_ROOM : 0.0f) : top, shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
@@ -261,14 +262,26 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
 #pragma unroll
                 for (int i = 0; i < 2 * DB; ++i) acc[i] *= shrink;
                 top = to;
+                far = __builtin_amdgcn_ballot_w64(far_score(top));
             }
-            const float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT;
+            float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT, mul = scale;
+            if (far) {                                                         // (of rows with far scores the difference to the largest one first)
+                asm volatile("" ::: "memory");
+                if (far_score(top)) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[b][i] = s[b][i] * scale - top;
+                    base = -WEIGHT_LIFT;
+                    mul = 1.0f;
+                }
+            }
             float w[2][8];
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float one = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale, -base));
+                    const float one = __builtin_amdgcn_exp2f(fmaf(s[b][i], mul, -base));
                     sum += one;
                     w[b / 2][b % 2 * 4 + i] = one;
                 }

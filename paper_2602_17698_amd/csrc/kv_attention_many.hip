@@ -190,6 +190,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
     float top = -INFINITY, sum = 0.0f;
     uint32_t spoiled = 0;
+    uint64_t far = 0;                              // lanes of rows with far scores
     // a tile of keys, 32 after the other (in a loop: with both halves in one piece registers do not suffice); hidden: not all seen by all rows, kinds: v not all in fp16.
     // (What is special is done behind conditions of its own, each without an else: two ways to the sums would cost a copy of them a tile.)
     auto take = [&](bool hidden, uint32_t kinds, int buffer, int key0, uint64_t valid) {
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                 room = (rows | rows >> 32) >> n & 1;
             }
             // (each row by itself: what one sees does not move another's)
-            const bool grown = most > top + (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
+            const bool grown = most - top > (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
             if (__builtin_amdgcn_ballot_w64(grown)) {
                 asm volatile("" ::: "memory");                                     // (not for all tiles)
                 const float to = grown ? most + (room ? WEIGHT_ROOM : 0.0f) : top, shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
@@ -257,8 +258,18 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
 #pragma unroll
                 for (int d = 0; d < DB; ++d) acc[d] *= shrink;
                 top = to;
+                far = __builtin_amdgcn_ballot_w64(far_score(top));
             }
-            const float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT;
+            float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT, mul = scale;
+            if (far) {                                                             // (of rows with far scores the difference to the largest one first)
+                asm volatile("" ::: "memory");
+                if (far_score(top)) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = s[i] * scale - top;
+                    base = -WEIGHT_LIFT;
+                    mul = 1.0f;
+                }
+            }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int step = 2 * m + half;
@@ -266,7 +277,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                 float w[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    w[j] = __builtin_amdgcn_exp2f(fmaf(s[half * 8 + j], scale, -base));
+                    w[j] = __builtin_amdgcn_exp2f(fmaf(s[half * 8 + j], mul, -base));
                     sum += w[j];
                 }
                 const unsigned char *const at = sh.v[buffer] + (16 * step + 4 * h + n % 16 / 4) * V_PITCH + 16 * ((n / 16 * 2 + n % 4 / 2) ^ n % 16 / 4) + 8 * (n % 2);

@@ -452,6 +452,9 @@ __device__ __forceinline__ void weights_bf16(const float (&w)[8], bf16x8 &high, 
 // Weights are 2^9 times what they are against the score that counts as the largest, which follows the largest so far only where that is more than 6 powers of two above it: sums are
 // then hardly ever taken anew, and a weight is below 2^15.  fp16 keeps weights down to 2^-23 with all its bits, and of smaller ones what is a multiple of 2^-33.
 constexpr float WEIGHT_LIFT = 9.0f, WEIGHT_SLACK = 6.0f;
+// A weight's power is s scale - (top - 9), rounded once.  Where the largest score is so far from 0 that top - 9 and the product have no bits behind the point, that could be more than 15, which
+// fp16 does not hold: from 2^20 on the difference to the largest score is taken first, which is exact next to it.
+__device__ __forceinline__ bool far_score(float top) { return fabsf(top) >= 0x1p20f && top != -INFINITY; }
 // Where a tile has values of v from 2^83 on, what counts as the largest score is 20 powers of two above it, so that sums of such values times weights stay within fp32.
 constexpr uint32_t LARGE_V = 210;
 constexpr float WEIGHT_ROOM = 20.0f;

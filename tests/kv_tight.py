@@ -31,7 +31,8 @@ def attention(b, q, scale=None, causal=True, window=0, terms=3):
     A score: sums in fp32 of products that are exact, each addition off by 2^-23 of the magnitudes' sum, of which there are no more than terms * dim / 32 and 256 inside
     instructions; of q what the terms leave out, 2^-15 of its block's largest value with three of them and 2^-18 with four.  A weight: the power of two is off by a unit in the last
     place, its argument by 2^-23 of its own and the largest score's size; rounded to fp16 2^-11 and, where it is small, by 2^-25 against a sum of 2^9.  Sums of keys by 16 or 32:
-    2^-23 each.  The output: bf16, 2^-8."""
+    2^-23 each.  The output: bf16, 2^-8.  Below 2^-126 steps are no longer relative: bf16 rounds by up to 2^-134, and a product of a weight with v that the matrix cores may count as 0 is
+    below 2^-126, against a sum of weights of 2^9."""
     dim, group = b.dim, q.shape[1] // b.kv_heads
     scale = dim ** -0.5 if scale is None else scale
     parts = []
@@ -58,7 +59,8 @@ def attention(b, q, scale=None, causal=True, window=0, terms=3):
             y[i], size[i] = torch.einsum("hgk,hkd->hgd", w[i], u), torch.einsum("hgk,hkd->hgd", w[i], u.abs())
             least[i] = u.abs().sum(1)[:, None]
         power = (1 + size_t) * 2.0 ** -22
-        off = (torch.expm1(2 * (far + power).clamp(max=100.0)) + 2.0 ** -11 + (len(key) / 16 + 64) * 2.0 ** -23) * size + 2.0 ** -8 * y.abs() + 2.0 ** -34 * least
+        off = (torch.expm1(2 * (far + power).clamp(max=100.0)) + 2.0 ** -11 + (len(key) / 16 + 64) * 2.0 ** -23) * size + 2.0 ** -8 * y.abs() + 2.0 ** -34 * least \
+            + 2.0 ** -134 + len(key) * 2.0 ** -135
         off_lse = (far + power)[..., 0] + 2.0 ** -22 * (1 + lse.abs().nan_to_num(posinf=0.0))
         parts.append([z.flatten(1, 2) for z in (y, lse, off, off_lse)])
     return tuple(torch.cat(p) for p in zip(*parts))

@@ -127,3 +127,37 @@ def test_hidden_keys_and_other_rows_do_not_change_a_bit(ctx, junk, sizes, window
     q[others] = (q[others].float() * 3.7).to(BF16).flip(-1)
     for x, y in zip(attend(ctx, b, q, window=window), want):
         assert torch.equal(x[keep], y[keep])
+    if 0 <= junk <= 215:                                         # (of larger keys scores leave fp32)
+        check(ctx, b, q, window=window)
+
+
+# ---- scores far from 0 -----------------------------------------------------------------------------
+@pytest.mark.parametrize("power", [16, 19, 20, 21, 22, 23, 24, 25, 27, 30, 40, 60])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("sizes", [[(1, 700), (3, 100)], [(100, 300)]])
+@pytest.mark.parametrize("scale", [1.0, 0.7])
+def test_scores_far_from_zero(ctx, power, sign, sizes, scale):
+    """Scores that are whole multiples of 2^power, exact in 32 bits: only keys with the largest one count (the next is e^20000 times less), alike."""
+    b = Batch(sizes, 16, 1, 64, seed=power)
+    g = torch.Generator().manual_seed(power)
+    for s, (n, past) in enumerate(sizes):
+        page, at = b.places(s, 0, n + past)
+        b.codes[0][page, :, at] = 0
+        b.codes[0][page, 0, at, 0] = torch.randint(0, 8, (n + past,), generator=g).to(torch.uint8)          # an element of k: 0 .. 6
+        b.scales[0][page, :, at] = 127
+    q = torch.zeros(b.tokens, 2, 64, dtype=BF16)
+    q[:, 0, 0], q[:, 1, 0] = sign * 2.0 ** power, sign * 1.5 * 2.0 ** power
+    out, sums = attend(ctx, b, q, scale=scale)
+    for s, (n, past) in enumerate(sizes):
+        at, k, v = kv_tight.sequence(b, s)
+        for i in range(n):
+            seen = slice(0, past + i + 1)
+            t = sign * k[0, seen, 0]
+            best = t == t.max()
+            want = v[0, seen][best].mean(0)
+            for h, f in enumerate((1.0, 1.5)):
+                row = int(b.starts[s]) + i
+                # weights are alike, 2^9 times a power of the score's rounding: fp16 rounds them by 2^-11 of their size, which their sum does not have; then a product and bf16
+                assert ((out[row, h].double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -18) * v[0, seen][best].abs().mean(0)).all()
+                lse = scale * f * 2.0 ** power * float(t.max()) + math.log(int(best.sum()))
+                assert abs(float(sums[row, h]) - lse) <= 2.0 ** -20 * max(1.0, abs(lse))
