@@ -176,10 +176,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         float top = -INFINITY, sum = 0.0f;
         uint32_t spoil = 0;                                                    // blocks of this lane's row with a seen value that is not finite
         uint64_t far = 0;                                                      // lanes of rows with far scores
+        uint64_t raised = 0;                                                   // of rows that have taken room
         unsigned char *const lds = smem[wave];
-        // Half of v's keys (those with the same b / 2) to LDS, in fp16 or bf16; special: not all keys are there, or their powers others than fp16 has.  Fp16 then has the pieces with its powers, bf16 the
-        // others, and zeros are where the other's pieces are.
-        auto put = [&](const Codes &o, auto special_, auto f16_, auto half_, int key0, bool v_there) {
+        // Half of v's keys (those with the same b / 2) to LDS, in fp16 or bf16; special: not all keys are there, or their powers others than fp16 has.  Then only the pieces whose
+        // powers are of fp16, or are not, and zeros where the others are.
+        auto put = [&](const Codes &o, auto special_, auto f16_, auto half_, bool powers, int key0, bool v_there) {
             constexpr bool SPECIAL = decltype(special_)::value, F16 = decltype(f16_)::value;
             constexpr int HALF = decltype(half_)::value;
             const int g = SPECIAL ? fresh(lane >> 4) : lane >> 4, n = SPECIAL ? fresh(lane & 15) : lane & 15;
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                 u32x4 codes = o.v[i];
                 uint32_t byte = v_scale(o, i);
                 if constexpr (SPECIAL)
-                    if (!v_there || key0 + key >= f.last || f16_power(byte) != F16 || byte >= KV_V_LIMIT) codes = zero, byte = 127;
+                    if (!v_there || key0 + key >= f.last || f16_power(byte) != powers || byte >= KV_V_LIMIT) codes = zero, byte = 127;
                 const float sc = __uint_as_float(byte << 23);
                 unsigned char *const to = lds + (16 * (four & 1) + n) * PITCH + 64 * block;
 #pragma unroll
@@ -262,6 +263,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
 #pragma unroll
                 for (int i = 0; i < 2 * DB; ++i) acc[i] *= shrink;
                 top = to;
+                raised = (raised & ~__builtin_amdgcn_ballot_w64(grown)) | __builtin_amdgcn_ballot_w64(grown && room);
                 far = __builtin_amdgcn_ballot_w64(far_score(top));
             }
             float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT, mul = scale;
@@ -288,23 +290,28 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             static_for<0, 2>([&](auto half_) {
                 constexpr int half = decltype(half_)::value;
                 __builtin_amdgcn_wave_barrier();
-                put(o, special_, std::true_type{}, half_, key0, fours >> n & 1);
+                put(o, special_, std::true_type{}, half_, true, key0, fours >> n & 1);
                 if (!SPECIAL && half == 1) ask(V, o, t);
                 __builtin_amdgcn_wave_barrier();
                 const unsigned char *const at = lds + (4 * g + n / 4) * PITCH + 8 * (n % 4);
-                const f16x8 p16 = weights_f16(w[half]);
+                f16x8 p16 = weights_f16(w[half]);
+                if (SPECIAL && (raised >> lane & 1)) p16 = f16x8{};
 #pragma unroll
                 for (int d = 0; d < 2 * DB; ++d) {
                     acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, read_transposed(at + 32 * d, 16 * PITCH)), p16, acc[d], 0, 0, 0);
                     if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
                 if constexpr (SPECIAL) {
-                    if (others) {
+                    // in bf16: the other pieces, and for rows that have taken room those of fp16
+#pragma unroll 1
+                    for (int pass = 0; pass < 2; ++pass) {
+                        if (!(pass ? raised != 0 : others)) continue;
                         __builtin_amdgcn_wave_barrier();
-                        put(o, special_, std::false_type{}, half_, key0, fours >> n & 1);
+                        put(o, special_, std::false_type{}, half_, pass, key0, fours >> n & 1);
                         __builtin_amdgcn_wave_barrier();
                         bf16x8 high, low;
                         weights_bf16(w[half], high, low);
+                        if (pass && !(raised >> lane & 1)) high = low = bf16x8{};
 #pragma unroll
                         for (int d = 0; d < 2 * DB; ++d) {
                             const bf16x8 v = __builtin_bit_cast(bf16x8, read_transposed(at + 32 * d, 16 * PITCH));
@@ -342,7 +349,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             bool usual = true;                                                 // all in fp16 (keys that are not there count, too: they may make the tile a special one, which finds out)
 #pragma unroll
             for (int i = 0; i < DB; ++i) usual = usual && f16_power(v_scale(o, i));
-            if (__builtin_amdgcn_ballot_w64(!usual) == 0 && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all) take(o, std::false_type{}, s, t, fours);
+            if (__builtin_amdgcn_ballot_w64(!usual) == 0 && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all && !raised) take(o, std::false_type{}, s, t, fours);
             else take(o, std::true_type{}, s, t, fours);
             page = page_next;
             page_next = page_third;

@@ -39,6 +39,14 @@ __device__ __forceinline__ s16x8 only_keys(s16x8 v, uint32_t keys, int h)
     }
     return __builtin_bit_cast(s16x8, x);
 }
+__device__ __forceinline__ s16x8 to_bf16(s16x8 v)                              // of fp16
+{
+    const f16x8 x = __builtin_bit_cast(f16x8, v);
+    bf16x8 y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = (__bf16)(float)x[i];
+    return __builtin_bit_cast(s16x8, y);
+}
 
 template <int DB, int TERMS>
 __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention_many_kernel(AttentionArgs a)
@@ -191,10 +199,12 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     float top = -INFINITY, sum = 0.0f;
     uint32_t spoiled = 0;
     uint64_t far = 0;                              // lanes of rows with far scores
+    uint32_t raised = 0;                           // rows that have taken room
     // a tile of keys, 32 after the other (in a loop: with both halves in one piece registers do not suffice); hidden: not all seen by all rows, kinds: v not all in fp16.
     // (What is special is done behind conditions of its own, each without an else: two ways to the sums would cost a copy of them a tile.)
     auto take = [&](bool hidden, uint32_t kinds, int buffer, int key0, uint64_t valid) {
-        uint32_t others = kinds;
+        const uint32_t unusual = kinds | __builtin_amdgcn_readfirstlane(raised);
+        uint32_t others = unusual;
         asm volatile("" : "+s"(others));
 #pragma unroll 1
         for (int m = 0; m < 2; ++m) {
@@ -258,6 +268,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
 #pragma unroll
                 for (int d = 0; d < DB; ++d) acc[d] *= shrink;
                 top = to;
+                raised = (raised & ~(uint32_t)__builtin_amdgcn_ballot_w64(grown)) | (uint32_t)__builtin_amdgcn_ballot_w64(grown && room);
                 far = __builtin_amdgcn_ballot_w64(far_score(top));
             }
             float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT, mul = scale;
@@ -281,7 +292,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                     sum += w[j];
                 }
                 const unsigned char *const at = sh.v[buffer] + (16 * step + 4 * h + n % 16 / 4) * V_PITCH + 16 * ((n / 16 * 2 + n % 4 / 2) ^ n % 16 / 4) + 8 * (n % 2);
-                if (kinds == 0) {
+                if (unusual == 0) {
                     const f16x8 p16 = weights_f16(w);
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
@@ -292,21 +303,24 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                     const uint32_t kind = __builtin_amdgcn_readfirstlane(sh.kind[buffer][step]);
                     bf16x8 high, low;
                     weights_bf16(w, high, low);
-                    const f16x8 p16 = weights_f16(w);
+                    const bool mine = raised >> n & 1;
+                    const f16x8 p16 = mine ? f16x8{} : weights_f16(w);
 #pragma unroll
                     for (int d = 0; d < DB; ++d) {
                         const s16x8 v = read_transposed(at + 64 * d, 8 * V_PITCH);
                         const uint32_t keys = kind & 1 ? __builtin_amdgcn_readfirstlane(sh.others[buffer][step][d]) : 0;
                         acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, only_keys(v, ~keys, h)), p16, acc[d], 0, 0, 0);
-                        if (keys) {
-                            const bf16x8 b = __builtin_bit_cast(bf16x8, only_keys(v, keys, h));
+                        // in bf16: the other keys, and for rows that have taken room those of fp16
+                        auto add = [&](s16x8 x, bf16x8 high, bf16x8 low) {
                             f32x16 more;
 #pragma unroll
                             for (int i = 0; i < 16; ++i) more[i] = 0.0f;
-                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, low, more, 0, 0, 0);
-                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, high, more, 0, 0, 0);
+                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), low, more, 0, 0, 0);
+                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), high, more, 0, 0, 0);
                             acc[d] += more;
-                        }
+                        };
+                        if (keys) add(only_keys(v, keys, h), high, low);
+                        if (raised) add(only_keys(to_bf16(v), ~keys, h), mine ? high : bf16x8{}, mine ? low : bf16x8{});
                     }
                     if (kind & 2)
                         for (int j = 0; j < 16; ++j)

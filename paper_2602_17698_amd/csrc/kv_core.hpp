@@ -455,7 +455,8 @@ constexpr float WEIGHT_LIFT = 9.0f, WEIGHT_SLACK = 6.0f;
 // A weight's power is s scale - (top - 9), rounded once.  Where the largest score is so far from 0 that top - 9 and the product have no bits behind the point, that could be more than 15, which
 // fp16 does not hold: from 2^20 on the difference to the largest score is taken first, which is exact next to it.
 __device__ __forceinline__ bool far_score(float top) { return fabsf(top) >= 0x1p20f && top != -INFINITY; }
-// Where a tile has values of v from 2^83 on, what counts as the largest score is 20 powers of two above it, so that sums of such values times weights stay within fp32.
+// Where a row sees values of v from 2^83 on, what counts as its largest score is 20 powers of two above it, so that sums of such values times weights stay within fp32.  Weights are then too
+// small for fp16: until a larger score counts, all of the row's blocks enter in bf16.
 constexpr uint32_t LARGE_V = 210;
 constexpr float WEIGHT_ROOM = 20.0f;
 // The logarithm of the sum: that of weights at their own size, which loses no bits to the lift's.

@@ -161,3 +161,32 @@ def test_scores_far_from_zero(ctx, power, sign, sizes, scale):
                 assert ((out[row, h].double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -11 + 2.0 ** -18) * v[0, seen][best].abs().mean(0)).all()
                 lse = scale * f * 2.0 ** power * float(t.max()) + math.log(int(best.sum()))
                 assert abs(float(sums[row, h]) - lse) <= 2.0 ** -20 * max(1.0, abs(lse))
+
+
+# ---- large values ------------------------------------------------------------------------------------
+def peaked(b, seed, others=0):
+    """k of which only one element is not 0: code 7 (6) for one key in 997, `others` else."""
+    for s in range(len(b.sizes)):
+        page, at = b.places(s, 0, int(b.lengths[s]))
+        b.codes[0][page, :, at] = 0
+        code = torch.full((len(page),), others)
+        code[seed % 13::997] = 7
+        b.codes[0][page, 0, at, 0] = code.to(torch.uint8)
+        b.scales[0][page, :, at] = 127
+
+
+@pytest.mark.parametrize("byte", [199, 200, 209, 210, 230, 250])
+@pytest.mark.parametrize("sizes", [[(1, 4000), (2, 2500)], [(100, 3000)]])
+@pytest.mark.parametrize("dim", [64, 128, 160])
+def test_large_values_of_one_block_leave_the_others_as_they_are(ctx, byte, sizes, dim):
+    """A key of a sequence's first with large values in one block; most of the weight lies on thousands of keys behind it, each 2^-10 of the largest."""
+    b = Batch(sizes, 16, 1, dim, seed=byte)
+    peaked(b, byte)
+    b.codes[1] &= 0x77                                           # (no signs: an output is as large as what it is a sum of)
+    for s in range(len(sizes)):
+        page, at = b.places(s, 3, 1)
+        b.scales[1][page, 0, at, 1] = byte
+    q = torch.zeros(b.tokens, 2, dim, dtype=BF16)
+    q[:, :, 0] = 1.0
+    check(ctx, b, q, scale=1.2)
+    check(ctx, b, q, scale=1.2, lse=False)
