@@ -173,7 +173,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         f32x4 acc[2 * DB];
 #pragma unroll
         for (int i = 0; i < 2 * DB; ++i) acc[i] = f32x4{0, 0, 0, 0};
-        float top = -INFINITY, sum = 0.0f;
+        float top = -INFINITY, sum = 0.0f, base = weight_base(top);
         uint32_t spoil = 0;                                                    // blocks of this lane's row with a seen value that is not finite
         uint64_t far = 0;                                                      // lanes of rows with far scores
         uint64_t raised = 0;                                                   // of rows that have taken room
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         auto take = [&](Codes &o, auto special_, f32x4 (&s)[4], int t, uint32_t fours) {
             constexpr bool SPECIAL = decltype(special_)::value;
             const int key0 = f.first + t * KV_TILE;
-            bool others = false, room = false;                                 // pieces that fp16 does not have; whether this lane's row sees large values
+            bool others = false, large = false;                                // pieces that fp16 does not have; with large values
             if constexpr (SPECIAL) {
                 const int g4 = fresh(4 * g), from = lo - key0 - 4 * g4, past = hi - key0 - 4 * g4;
                 const uint32_t mine = fours >> g4;
@@ -221,17 +221,9 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                     if (is_there(i) && !f16_power(v_scale(o, i))) others = true, highest = max(highest, v_scale(o, i));
                 others = __builtin_amdgcn_ballot_w64(others) != 0;
                 if (__builtin_amdgcn_ballot_w64(highest >= LARGE_V)) {
-                    uint32_t large[4] = {0, 0, 0, 0};                          // of the keys 4 n + b those with large values, a bit each
                     static_for<0, DB>([&](auto i_) {
                         constexpr int i = decltype(i_)::value;
-                        const bool ok = is_there(i);
-                        const uint32_t byte = v_scale(o, i);
-#pragma unroll
-                        for (int b = 0; b < 4; ++b) {
-                            const uint64_t are = __builtin_amdgcn_ballot_w64(ok && byte >= LARGE_V && byte < KV_V_LIMIT && v_key(i, g) == b);
-                            large[b] |= (uint32_t)(are | are >> 16 | are >> 32 | are >> 48) & 0xffffu;
-                        }
-                        uint64_t bads = __builtin_amdgcn_ballot_w64(ok && byte >= KV_V_LIMIT);
+                        uint64_t bads = __builtin_amdgcn_ballot_w64(is_there(i) && v_scale(o, i) >= KV_V_LIMIT);
                         const int key = 4 * n + v_key(i, g), block = v_block(i, g);
                         while (bads) {
                             const int from = __builtin_ctzll(bads), bad_key = __builtin_amdgcn_readlane(key, from), bad_block = __builtin_amdgcn_readlane(block, from);
@@ -239,13 +231,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                             if (key0 + bad_key >= lo && key0 + bad_key < hi) spoil |= 1u << bad_block;
                         }
                     });
-#pragma unroll
-                    for (int b = 0; b < 4; ++b)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) room = room || ((large[b] >> 4 * g >> i & 1) && s[b][i] > -INFINITY);
-                    uint64_t rows = __builtin_amdgcn_ballot_w64(room);
-                    rows |= rows >> 32;
-                    room = (rows | rows >> 16) >> n & 1;
+                    large = true;
                 }
             }
             float most = -INFINITY;
@@ -254,36 +240,58 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
 #pragma unroll
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, s[b][i]);
             most = across_rows(most, OpMax()) * scale;
-            // (each row by itself: what one sees does not move another's)
-            const bool grown = most - top > (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
-            if (__builtin_amdgcn_ballot_w64(grown)) {
-                asm volatile("" ::: "memory");                                 // (and this)
-                const float to = grown ? most + (room ? WEIGHT_ROOM : 0.0f) : top, shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
-                sum *= shrink;
-#pragma unroll
-                for (int i = 0; i < 2 * DB; ++i) acc[i] *= shrink;
-                top = to;
-                raised = (raised & ~__builtin_amdgcn_ballot_w64(grown)) | __builtin_amdgcn_ballot_w64(grown && room);
-                far = __builtin_amdgcn_ballot_w64(far_score(top));
-            }
-            float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT, mul = scale;
-            if (far) {                                                         // (of rows with far scores the difference to the largest one first)
+            // (what happens to few tiles, in one place)
+            if (__builtin_expect((__builtin_amdgcn_ballot_w64(most - top > WEIGHT_SLACK) | large) != 0, 0)) {
                 asm volatile("" ::: "memory");
-                if (far_score(top)) {
+                bool room = false;                                             // whether this lane's row sees large values
+                if (SPECIAL && large) {
+                    const int g = fresh(lane >> 4), n = fresh(lane & 15);
+                    uint32_t keys[4] = {0, 0, 0, 0};                           // of the keys 4 n + b those with large values, a bit each
+                    static_for<0, DB>([&](auto i_) {
+                        constexpr int i = decltype(i_)::value;
+                        const bool is = (fours >> n & 1) && key0 + 4 * n + v_key(i, g) < f.last && v_scale(o, i) >= LARGE_V && v_scale(o, i) < KV_V_LIMIT;
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            const uint64_t are = __builtin_amdgcn_ballot_w64(is && v_key(i, g) == b);
+                            keys[b] |= (uint32_t)(are | are >> 16 | are >> 32 | are >> 48) & 0xffffu;
+                        }
+                    });
 #pragma unroll
                     for (int b = 0; b < 4; ++b)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) s[b][i] = s[b][i] * scale - top;
-                    base = -WEIGHT_LIFT;
-                    mul = 1.0f;
+                        for (int i = 0; i < 4; ++i) room = room || ((keys[b] >> 4 * g >> i & 1) && s[b][i] > -INFINITY);
+                    uint64_t rows = __builtin_amdgcn_ballot_w64(room);
+                    rows |= rows >> 32;
+                    room = (rows | rows >> 16) >> n & 1;
                 }
+                // (each row by itself: what one sees does not move another's)
+                const bool grown = most - top > (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
+                if (__builtin_amdgcn_ballot_w64(grown)) {
+                    const float to = grown ? most + (room ? WEIGHT_ROOM : 0.0f) : top, shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
+                    sum *= shrink;
+#pragma unroll
+                    for (int i = 0; i < 2 * DB; ++i) acc[i] *= shrink;
+                    top = to;
+                    raised = (raised & ~__builtin_amdgcn_ballot_w64(grown)) | __builtin_amdgcn_ballot_w64(grown && room);
+                    far = __builtin_amdgcn_ballot_w64(far_score(top));
+                    base = weight_base(top);
+                }
+            }
+            if (__builtin_expect(far != 0, 0)) {
+                asm volatile("" ::: "memory");
+                const float over = __builtin_amdgcn_rcpf(__int_as_float(fresh(__float_as_int(scale))));
+                const bool is = far_score(top);
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[b][i] = is ? (s[b][i] * scale - top) * over : s[b][i];
             }
             float w[2][8];
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float one = __builtin_amdgcn_exp2f(fmaf(s[b][i], mul, -base));
+                    const float one = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale, -base));
                     sum += one;
                     w[b / 2][b % 2 * 4 + i] = one;
                 }
@@ -295,7 +303,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                 __builtin_amdgcn_wave_barrier();
                 const unsigned char *const at = lds + (4 * g + n / 4) * PITCH + 8 * (n % 4);
                 f16x8 p16 = weights_f16(w[half]);
-                if (SPECIAL && (raised >> lane & 1)) p16 = f16x8{};
+                if (SPECIAL && (raised >> fresh(lane) & 1)) p16 = f16x8{};
 #pragma unroll
                 for (int d = 0; d < 2 * DB; ++d) {
                     acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, read_transposed(at + 32 * d, 16 * PITCH)), p16, acc[d], 0, 0, 0);
@@ -303,15 +311,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                 }
                 if constexpr (SPECIAL) {
                     // in bf16: the other pieces, and for rows that have taken room those of fp16
-#pragma unroll 1
-                    for (int pass = 0; pass < 2; ++pass) {
-                        if (!(pass ? raised != 0 : others)) continue;
+                    for (int pass = others ? 0 : 1; pass < (raised ? 2 : 1); ++pass) {
+                        asm volatile("" ::: "memory");
                         __builtin_amdgcn_wave_barrier();
                         put(o, special_, std::false_type{}, half_, pass, key0, fours >> n & 1);
                         __builtin_amdgcn_wave_barrier();
                         bf16x8 high, low;
                         weights_bf16(w[half], high, low);
-                        if (pass && !(raised >> lane & 1)) high = low = bf16x8{};
+                        if (pass && !(raised >> fresh(lane) & 1)) high = low = bf16x8{};
 #pragma unroll
                         for (int d = 0; d < 2 * DB; ++d) {
                             const bf16x8 v = __builtin_bit_cast(bf16x8, read_transposed(at + 32 * d, 16 * PITCH));

@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
-    float top = -INFINITY, sum = 0.0f;
+    float top = -INFINITY, sum = 0.0f, base = weight_base(top);
     uint32_t spoiled = 0;
     uint64_t far = 0;                              // lanes of rows with far scores
     uint32_t raised = 0;                           // rows that have taken room
@@ -250,36 +250,38 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[i]);
             most = op_halves(most, OpMax(), __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false));
             most *= scale;
-            bool room = false;                                                     // whether this lane's row sees large values
-            if (kinds & 4) {
-                const uint32_t *const kind = sh.kind[buffer] + 2 * m;
-                const uint32_t low = kind[0] & 4 ? sh.large[buffer][2 * m] : 0, high = kind[1] & 4 ? sh.large[buffer][2 * m + 1] : 0, mine = (low | high << 16) >> 4 * h;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) room = room || ((mine >> (8 * (i / 4) + i % 4) & 1) && s[i] > -INFINITY);
-                const uint64_t rows = __builtin_amdgcn_ballot_w64(room);
-                room = (rows | rows >> 32) >> n & 1;
-            }
-            // (each row by itself: what one sees does not move another's)
-            const bool grown = most - top > (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
-            if (__builtin_amdgcn_ballot_w64(grown)) {
-                asm volatile("" ::: "memory");                                     // (not for all tiles)
-                const float to = grown ? most + (room ? WEIGHT_ROOM : 0.0f) : top, shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
-                sum *= shrink;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) acc[d] *= shrink;
-                top = to;
-                raised = (raised & ~(uint32_t)__builtin_amdgcn_ballot_w64(grown)) | (uint32_t)__builtin_amdgcn_ballot_w64(grown && room);
-                far = __builtin_amdgcn_ballot_w64(far_score(top));
-            }
-            float base = (top == -INFINITY ? 0.0f : top) - WEIGHT_LIFT, mul = scale;
-            if (far) {                                                             // (of rows with far scores the difference to the largest one first)
+            // (what happens to few tiles, in one place)
+            if (__builtin_expect((__builtin_amdgcn_ballot_w64(most - top > WEIGHT_SLACK) | (kinds & 4)) != 0, 0)) {
                 asm volatile("" ::: "memory");
-                if (far_score(top)) {
+                bool room = false;                                                 // whether this lane's row sees large values
+                if (kinds & 4) {
+                    const int h = fresh(lane >> 5), n = fresh(lane & 31);
+                    const uint32_t *const kind = sh.kind[buffer] + 2 * m;
+                    const uint32_t low = kind[0] & 4 ? sh.large[buffer][2 * m] : 0, high = kind[1] & 4 ? sh.large[buffer][2 * m + 1] : 0, mine = (low | high << 16) >> 4 * h;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = s[i] * scale - top;
-                    base = -WEIGHT_LIFT;
-                    mul = 1.0f;
+                    for (int i = 0; i < 16; ++i) room = room || ((mine >> (8 * (i / 4) + i % 4) & 1) && s[i] > -INFINITY);
+                    const uint64_t rows = __builtin_amdgcn_ballot_w64(room);
+                    room = (rows | rows >> 32) >> n & 1;
                 }
+                // (each row by itself: what one sees does not move another's)
+                const bool grown = most - top > (room ? -WEIGHT_ROOM : WEIGHT_SLACK);
+                if (__builtin_amdgcn_ballot_w64(grown)) {
+                    const float to = grown ? most + (room ? WEIGHT_ROOM : 0.0f) : top, shrink = to > top ? __builtin_amdgcn_exp2f(top - to) : 1.0f;
+                    sum *= shrink;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) acc[d] *= shrink;
+                    top = to;
+                    raised = (raised & ~(uint32_t)__builtin_amdgcn_ballot_w64(grown)) | (uint32_t)__builtin_amdgcn_ballot_w64(grown && room);
+                    far = __builtin_amdgcn_ballot_w64(far_score(top));
+                    base = weight_base(top);
+                }
+            }
+            if (__builtin_expect(far != 0, 0)) {
+                asm volatile("" ::: "memory");
+                const float over = __builtin_amdgcn_rcpf(__int_as_float(fresh(__float_as_int(scale))));
+                const bool is = far_score(top);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = is ? (s[i] * scale - top) * over : s[i];
             }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -288,17 +290,19 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                 float w[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    w[j] = __builtin_amdgcn_exp2f(fmaf(s[half * 8 + j], mul, -base));
+                    w[j] = __builtin_amdgcn_exp2f(fmaf(s[half * 8 + j], scale, -base));
                     sum += w[j];
                 }
                 const unsigned char *const at = sh.v[buffer] + (16 * step + 4 * h + n % 16 / 4) * V_PITCH + 16 * ((n / 16 * 2 + n % 4 / 2) ^ n % 16 / 4) + 8 * (n % 2);
-                if (unusual == 0) {
+                if (__builtin_expect(unusual == 0, 1)) {
                     const f16x8 p16 = weights_f16(w);
 #pragma unroll
                     for (int d = 0; d < DB; ++d)
                         acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, read_transposed(at + 64 * d, 8 * V_PITCH)), p16, acc[d], 0, 0, 0);
                 }
-                if (others) {
+                if (__builtin_expect(others != 0, 0)) {
+                    asm volatile("" ::: "memory");
+                    const int h = fresh(lane >> 5), n = fresh(lane & 31);
                     // (a row's sums are the same whichever way a tile goes that it sees nothing unusual of: fp16 as above, and zeros added)
                     const uint32_t kind = __builtin_amdgcn_readfirstlane(sh.kind[buffer][step]);
                     bf16x8 high, low;
@@ -312,12 +316,8 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                         acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, only_keys(v, ~keys, h)), p16, acc[d], 0, 0, 0);
                         // in bf16: the other keys, and for rows that have taken room those of fp16
                         auto add = [&](s16x8 x, bf16x8 high, bf16x8 low) {
-                            f32x16 more;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) more[i] = 0.0f;
-                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), low, more, 0, 0, 0);
-                            more = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), high, more, 0, 0, 0);
-                            acc[d] += more;
+                            acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), low, acc[d], 0, 0, 0);
+                            acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), high, acc[d], 0, 0, 0);
                         };
                         if (keys) add(only_keys(v, keys, h), high, low);
                         if (raised) add(only_keys(to_bf16(v), ~keys, h), mine ? high : bf16x8{}, mine ? low : bf16x8{});

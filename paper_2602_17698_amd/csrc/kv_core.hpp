@@ -453,8 +453,11 @@ __device__ __forceinline__ void weights_bf16(const float (&w)[8], bf16x8 &high, 
 // then hardly ever taken anew, and a weight is below 2^15.  fp16 keeps weights down to 2^-23 with all its bits, and of smaller ones what is a multiple of 2^-33.
 constexpr float WEIGHT_LIFT = 9.0f, WEIGHT_SLACK = 6.0f;
 // A weight's power is s scale - (top - 9), rounded once.  Where the largest score is so far from 0 that top - 9 and the product have no bits behind the point, that could be more than 15, which
-// fp16 does not hold: from 2^20 on the difference to the largest score is taken first, which is exact next to it.
+// fp16 does not hold: from 2^20 on the difference to the largest score is taken first, which is exact next to it (and
+// divided by scale again, so that one formula does for all rows).
 __device__ __forceinline__ bool far_score(float top) { return fabsf(top) >= 0x1p20f && top != -INFINITY; }
+// what a weight's power has taken off, or where the difference has been taken has too much
+__device__ __forceinline__ float weight_base(float top) { return (top == -INFINITY || far_score(top) ? 0.0f : top) - WEIGHT_LIFT; }
 // Where a row sees values of v from 2^83 on, what counts as its largest score is 20 powers of two above it, so that sums of such values times weights stay within fp32.  Weights are then too
 // small for fp16: until a larger score counts, all of the row's blocks enter in bf16.
 constexpr uint32_t LARGE_V = 210;
