@@ -458,10 +458,11 @@ constexpr float WEIGHT_LIFT = 9.0f, WEIGHT_SLACK = 6.0f;
 __device__ __forceinline__ bool far_score(float top) { return fabsf(top) >= 0x1p20f && top != -INFINITY; }
 // what a weight's power has taken off, or where the difference has been taken has too much
 __device__ __forceinline__ float weight_base(float top) { return (top == -INFINITY || far_score(top) ? 0.0f : top) - WEIGHT_LIFT; }
-// Where a row sees values of v from 2^83 on, what counts as its largest score is 20 powers of two above it, so that sums of such values times weights stay within fp32.  Weights are then too
-// small for fp16: until a larger score counts, all of the row's blocks enter in bf16.
-constexpr uint32_t LARGE_V = 210;
-constexpr float WEIGHT_ROOM = 20.0f;
+// Where a row sees values of v from 2^73 on, what counts as its largest score is 40 powers of two above it, so that sums stay within fp32 whatever the number of keys, which is below 2^31: a weight
+// is then at most 2^-31, a value below 2^127.6; of smaller values 2^15 times 2^75.6 (weights of scores from 2^28 on have no bits for this).  Such weights are too small for fp16: until a larger
+// score counts, all of the row's blocks enter in bf16.
+constexpr uint32_t LARGE_V = 200;
+constexpr float WEIGHT_ROOM = 40.0f;
 // The logarithm of the sum: that of weights at their own size, which loses no bits to the lift's.
 __device__ __forceinline__ float log_sum(float lowered, float sum)
 {

@@ -190,3 +190,17 @@ def test_large_values_of_one_block_leave_the_others_as_they_are(ctx, byte, sizes
     q[:, :, 0] = 1.0
     check(ctx, b, q, scale=1.2)
     check(ctx, b, q, scale=1.2, lse=False)
+
+
+@pytest.mark.parametrize("byte", [199, 205, 240, 252])
+@pytest.mark.parametrize("sizes", [[(1, 9000), (2, 6000)], [(100, 9000)]])
+def test_means_of_thousands_of_the_largest_values_are_finite(ctx, byte, sizes):
+    """Equal scores, so that each key counts; some elements with the largest value in all keys, some with both signs of it."""
+    b = Batch(sizes, 64, 1, 64, seed=byte)
+    b.scales[1][:] = byte
+    b.codes[1][..., :8] = 0x77
+    b.codes[1][..., 8:12] = 0x7f
+    q = torch.zeros(b.tokens, 2, 64, dtype=BF16)
+    out, _ = check(ctx, b, q)
+    assert torch.isfinite(out).all() and (out[..., :16] == 6.0 * 2.0 ** (byte - 127)).all()
+    check(ctx, b, queries(b, 2), scale=0.3)
