@@ -141,7 +141,9 @@ struct RotateArgs {
     void *out;
     int64_t tokens, ld_x, hd_x, ld_out, hd_out;
     int heads, dim, back;
+    int units, rows;                         // pieces of a head, rows of a workgroup (the launch sets them)
 };
+constexpr int ROTATE_MAX_TURNS = 2048;       // of the rows of a workgroup
 struct StoreArgs {
     KvPages cache;
     KvSequences sequences;
@@ -483,7 +485,7 @@ __device__ __forceinline__ s16x8 read_transposed(const unsigned char *at, int st
 }  // namespace sbits
 
 // ---- launchers --------------------------------------------------------------
-int sbits_launch_rotate(sbits_ctx *ctx, const sbits::RotateArgs &a, bool bf16, bool wide);
+int sbits_launch_rotate(sbits_ctx *ctx, sbits::RotateArgs &a, bool bf16, bool wide);
 int sbits_launch_kv_store(sbits_ctx *ctx, const sbits::StoreArgs &a, bool bf16);
 int sbits_launch_kv_load(sbits_ctx *ctx, const sbits::LoadArgs &a, bool bf16);
 // bytes of a kernel's parts
