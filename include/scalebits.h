@@ -559,8 +559,8 @@ typedef struct {
  *   SBITS_ROTARY_LINEAR   f / (2 pi factor)
  *   SBITS_ROTARY_TURNS    by the turns n = context * f / 2 pi of a pair: f where n >= high,
  *                         f / factor where n <= low, between them in proportion to n
- *   SBITS_ROTARY_INDEX    by the pair's number: f up to the floor of the index that turns high times over the context, f / factor
- *                         from the ceiling of the one that turns low times on, between them in proportion to the index
+ *   SBITS_ROTARY_INDEX    by the pair's number: f up to the floor of the index that turns high times over the context (0 at least), f / factor
+ *                         from the ceiling of the one that turns low times on (2 pairs - 1 at most), between them in proportion to the index
  * low < high and context >= 1 are read by the last two only.                             */
 #define SBITS_ROTARY_PLAIN  0
 #define SBITS_ROTARY_LINEAR 1

@@ -99,7 +99,7 @@ int sbits_rotary_turns(int pairs, double base, int scaling, double factor, doubl
         double kept = 1.0;                                     // share of the frequency as it is
         if (scaling == SBITS_ROTARY_LINEAR) kept = 0.0;
         if (scaling == SBITS_ROTARY_TURNS) kept = (context * f / whole - low) / (high - low);
-        if (scaling == SBITS_ROTARY_INDEX) kept = 1.0 - (i - from) / std::max(to - from, 0.001);
+        if (scaling == SBITS_ROTARY_INDEX) kept = to <= 0.0 ? 0.0 : 1.0 - (i - from) / std::max(to - from, 0.001);   // (to <= 0: none turns low times)
         kept = std::min(1.0, std::max(0.0, kept));
         turns[i] = (scaling == SBITS_ROTARY_PLAIN ? f : kept * f + (1.0 - kept) * f / factor) / whole;
     }
