@@ -64,3 +64,52 @@ def attention(b, q, scale=None, causal=True, window=0, terms=3):
         off_lse = (far + power)[..., 0] + 2.0 ** -22 * (1 + lse.abs().nan_to_num(posinf=0.0))
         parts.append([z.flatten(1, 2) for z in (y, lse, off, off_lse)])
     return tuple(torch.cat(p) for p in zip(*parts))
+
+
+class Counted:
+    """A batch whose outputs show each key by itself: key j's value is 1 in the elements d with d % period == j % period, 0 in others, and its weight one of three powers of two
+    (by j % 3), so that an element is a sum of few weights, of which the least is far above what the output's rounding takes.  Scores are whole multiples of log 2."""
+
+    def __init__(self, batch, heads):
+        self.b, dim = batch, batch.dim
+        for s, length in enumerate(batch.lengths.tolist()):
+            key = torch.arange(length)
+            page, at = batch.places(s, 0, length)
+            # k: the first element 0, 1 or 2 (codes 0, 2, 4), v: code 2 is 1
+            code = torch.zeros(length, batch.kv_heads, dim, dtype=torch.uint8)
+            code[:, :, 0] = (2 * (key % 3))[:, None].to(torch.uint8)
+            one = 2 * (torch.arange(dim)[None, None, :] == self.element(key, batch.kv_heads)[..., None]).to(torch.uint8)
+            byte = torch.full((length, batch.kv_heads, dim // 32), 127, dtype=torch.uint8)
+            batch.put(0, s, 0, code, byte)
+            batch.put(1, s, 0, one, byte)
+        self.q = torch.zeros(batch.tokens, heads, dim, dtype=torch.bfloat16)
+        self.q[:, :, 0] = 1.0
+        self.scale = math.log(2.0)
+
+    def element(self, key, kv_heads):
+        return (key[:, None] + 7 * torch.arange(kv_heads)) % self.b.dim
+
+    def expected(self, causal=True, window=0, lost=()):
+        """Sums of weights by element and their quotient, without the keys in `lost` (of each sequence; to see what that makes)."""
+        b, group = self.b, self.q.shape[1] // self.b.kv_heads
+        out = []
+        for s, (n, past) in enumerate(b.sizes):
+            key = torch.arange(n + past)
+            w = 2.0 ** (key % 3).double()
+            for i in range(n):
+                last = past + i + 1 if causal else n + past
+                first = max(0, last - window) if window else 0
+                seen = (key >= first) & (key < last)
+                total = (w * seen).sum()
+                kept = seen.clone()
+                kept[[k for k in lost if k < len(key)]] = False
+                y = torch.zeros(b.kv_heads, b.dim, dtype=torch.float64)
+                for h in range(b.kv_heads):
+                    y[h].index_add_(0, self.element(key, b.kv_heads)[:, h], w * kept)
+                out.append((y / total).repeat_interleave(group, 0))
+        return torch.stack(out)
+
+    @staticmethod
+    def bound(want):
+        """Weights: their power's argument is off by 2^-20 (scores below 2 in magnitude, and what is taken off, below 32), fp16 rounds by 2^-11; the output by 2^-8."""
+        return want * (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -18)

@@ -204,3 +204,46 @@ def test_means_of_thousands_of_the_largest_values_are_finite(ctx, byte, sizes):
     out, _ = check(ctx, b, q)
     assert torch.isfinite(out).all() and (out[..., :16] == 6.0 * 2.0 ** (byte - 127)).all()
     check(ctx, b, queries(b, 2), scale=0.3)
+
+
+# ---- each key by itself --------------------------------------------------------------------------------
+@pytest.mark.parametrize("sizes,kv_heads,group,page,dim,window", [
+    ([(1, 5000)], 1, 4, 64, 128, 0), ([(1, 5000)], 2, 1, 8, 64, 0), ([(17, 3000), (1, 9)], 1, 2, 16, 128, 0), ([(17, 3000), (1, 9)], 2, 4, 32, 96, 700),
+    ([(3, 4000), (1, 63), (5, 1100), (2, 1023), (1, 0), (16, 2047)], 3, 1, 16, 160, 0), ([(1, 20000)], 1, 8, 256, 256, 0), ([(1, 9000)], 1, 16, 64, 224, 5000),
+    ([(100, 5000)], 1, 2, 64, 128, 0), ([(100, 5000), (40, 3000), (1, 800)], 2, 2, 16, 64, 0), ([(65, 7000)], 1, 1, 128, 192, 0), ([(129, 2000)], 1, 1, 8, 32, 1500),
+    ([(200, 0), (70, 60)], 2, 3, 64, 96, 33), ([(1, 1000 + 7 * i) for i in range(40)], 1, 2, 16, 64, 0)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_each_key_by_itself(ctx, sizes, kv_heads, group, page, dim, window, causal):
+    """Outputs that count keys: one that is lost, taken twice or multiplied with another's weight is outside of the bound (see kv_tight.Counted)."""
+    window = window if causal else 0
+    c = kv_tight.Counted(Batch(sizes, page, kv_heads, dim, seed=dim, lead=1), kv_heads * group)
+    want = c.expected(causal, window)
+    rows = c.b.rows()
+    for hints in ((), dict(max_new=max(n for n, _ in sizes), max_length=max(n + p for n, p in sizes)), dict(max_new=1, max_length=1)):
+        for lse in (True, False):
+            out, sums = attend(ctx, c.b, c.q, lse, hints, scale=c.scale, causal=causal, window=window)
+            got = out[rows].double()
+            assert ((got - want).abs() <= c.bound(want)).all(), float(((got - want).abs() / c.bound(want).clamp(min=1e-30)).max())
+            if lse:                                              # an element's share of the sum, in all elements together, is all of it
+                total = torch.tensor([float(sum(2.0 ** (k % 3) for k in range(max(0, p + i + 1 - window) if window else 0, p + i + 1 if causal else n + p)))
+                                      for n, p in sizes for i in range(n)], dtype=torch.float64)
+                assert ((sums[rows].double() - torch.log(total)[:, None]).abs() <= 2.0 ** -18).all()
+
+
+# ---- bytes read back -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+def test_all_bytes_and_codes_read_back(ctx, dtype):
+    """Each byte with each code: 255 is NaN, values above the type's range are infinite, bytes below 2 give subnormals, in bf16 rounded below 2^-133."""
+    b = Batch([(256, 0)], 64, 1, 32, seed=1)
+    page, at = b.places(0, 0, 256)
+    b.codes[0][page, 0, at] = (torch.arange(16).repeat(2)[0::2] | torch.arange(16).repeat(2)[1::2] << 4).to(torch.uint8)
+    b.scales[0][page, 0, at, 0] = torch.arange(256).to(torch.uint8)
+    cache, seqs, _ = b.on(sb)
+    out = torch.zeros(256, 1, 32, dtype=dtype, device="cuda")
+    ctx.kv_load(cache, seqs, out, None)
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64)
+    grid = torch.cat([grid, -grid])[torch.arange(16).repeat(2)]
+    want = grid[None] * torch.tensor([2.0 ** (e - 127) for e in range(255)], dtype=torch.float64)[:, None]
+    got = out.cpu()[:, 0]
+    assert torch.isnan(got[255]).all()
+    assert torch.equal(got[:255], want.to(dtype))                # (both roundings to nearest even, and to infinity)
