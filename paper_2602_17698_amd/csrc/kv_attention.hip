@@ -67,7 +67,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         const uint64_t in = (uint64_t)(x - begin);
         item = in >> 32 ? (int)(in / (uint32_t)f.keys) : (int)((uint32_t)in / (uint32_t)f.keys);
         off = (int)(x - begin - (int64_t)item * f.keys);
-        const int moved = few_snap(a, f, off), by = moved - off;
+        const int moved = few_snap(few_cuttable(a, f), f.keys, off), by = moved - off;
         off = moved;
         return x + by;
     };
@@ -418,13 +418,9 @@ __device__ __forceinline__ Parts find_parts(const AttentionArgs &a, int place, i
         const int64_t total = few_total(a, sequence, begin);
         begin += ((int64_t)tile * a.cache.kv_heads + kv_head) * f.keys;
         const int workgroups = few_workgroups(a, total);
-        const double each = (double)total / (double)workgroups;
-        // the cuts inside: from the first that is behind the item's begin and stays there on
-        int w = max((int)((double)begin / each) - 1, 0);
-        while (w < workgroups && few_cut(w, workgroups, total) - begin < FEW_EDGE) ++w;
-        int past = min((int)((double)(begin + f.keys - FEW_EDGE) / each) + 2, workgroups);
-        while (past > w && few_cut(past - 1, workgroups, total) - begin > f.keys - FEW_EDGE) --past;
-        p = {1 + past - w, f.start, f.rows, tile * ROWS, (int64_t)(2 * (w - 1) + 1) * ROWS, (int64_t)(2 * w) * ROWS, 2 * ROWS, (int64_t)2 * a.few.splits * ROWS};
+        const FewCuts cuts = few_cuts(begin, f.keys, workgroups, total);
+        const int w = cuts.first;
+        p = {1 + cuts.past - w, f.start, f.rows, tile * ROWS, (int64_t)(2 * (w - 1) + 1) * ROWS, (int64_t)(2 * w) * ROWS, 2 * ROWS, (int64_t)2 * a.few.splits * ROWS};
     } else {
         int tile;
         const int sequence = find_tile(a, place, tile);

@@ -227,11 +227,7 @@ __device__ __forceinline__ bool tile_plan(const AttentionArgs &a, int sequence, 
     return true;
 }
 
-// ---- sharing out the keys of few rows ----------------------------------------------------
-// An item is a tile of 16 rows of a sequence with a key's head; its work the tiles of keys that the sequence's rows see.  All items, sequence after sequence, a sequence's by tiles of rows,
-// then heads, make a line of W tiles of keys, of which workgroup w of G has those from cut(w) to cut(w + 1):  w (W / G), moved to the item's begin or end where that is less than FEW_EDGE tiles
-// away, and to the begin of an item of up to FEW_WHOLE tiles.  So workgroups have the same to do, whatever the lengths.
-constexpr int FEW_EDGE = 4, FEW_WHOLE = 16, FEW_LEAST = 8;       // FEW_LEAST: tiles of keys a workgroup, at least
+// ---- sharing out the keys of few rows (see kv_split.hpp) ----------------------------------
 struct FewSequence {
     int start, rows, ahead, length;           // as in TilePlan
     int tiles, first, last, keys;             // of rows; keys of all rows, from a multiple of 64 on; tiles of them (an item without keys counts as one)
@@ -306,27 +302,14 @@ __device__ __forceinline__ int few_find(const AttentionArgs &a, int64_t x, int64
     }
     return -1;
 }
-__device__ __forceinline__ int few_workgroups(const AttentionArgs &a, int64_t total)
-{
-    const int64_t most = total / FEW_LEAST;
-    return most >= a.few.splits ? a.few.splits : most < 1 ? 1 : (int)most;
-}
+__device__ __forceinline__ int few_workgroups(const AttentionArgs &a, int64_t total) { return few_workgroups(a.few.splits, total); }
 // A number of a lane's that the compiler takes for a new one: what is computed from it stays where it is, and is not kept in registers over a loop.
 __device__ __forceinline__ int fresh(int v)
 {
     asm volatile("" : "+v"(v));
     return v;
 }
-// Where cut w of G falls ahead of its move (w < G): a product in 64 bits, rounded down, which is the same wherever it is asked for.
-__device__ __forceinline__ int64_t few_cut(int w, int workgroups, int64_t total) { return (int64_t)((double)w * ((double)total / (double)workgroups)); }
-// Whether a sequence's items may be cut: not where there is no space for parts (no sequence was announced to be long enough), nor short ones, nor those of more
-// rows than were announced (which the parts' join would not reach).
-__device__ __forceinline__ bool few_cuttable(const AttentionArgs &a, const FewSequence &f) { return a.few.each && f.keys > FEW_WHOLE && f.rows <= a.few.rows; }
-// what a cut at `off` tiles of an item becomes
-__device__ __forceinline__ int few_snap(const AttentionArgs &a, const FewSequence &f, int off)
-{
-    return off < FEW_EDGE || !few_cuttable(a, f) ? 0 : f.keys - off < FEW_EDGE ? f.keys : off;
-}
+__device__ __forceinline__ bool few_cuttable(const AttentionArgs &a, const FewSequence &f) { return few_cuttable(a.few.each, a.few.rows, f.rows, f.keys); }
 
 // The tiles of many rows of all sequences are numbered so that sequence b's begin at floor(rows ahead of it / MANY_ROWS) + b, which leaves each as many as
 // it can need.  The sequence and the tile of a number, -1 if there is none.
