@@ -178,21 +178,19 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
         uint64_t far = 0;                                                      // lanes of rows with far scores
         uint64_t raised = 0;                                                   // of rows that have taken room
         unsigned char *const lds = smem[wave];
-        // Half of v's keys (those with the same b / 2) to LDS, in fp16 or bf16; special: not all keys are there, or their powers others than fp16 has.  Then only the pieces whose
-        // powers are of fp16, or are not, and zeros where the others are.
-        auto put = [&](const Codes &o, auto special_, auto f16_, auto half_, bool powers, int key0, bool v_there) {
+        // Half of v's keys (those with the same b / 2) to LDS, in fp16 or bf16; special: zeros but for some pieces (a lane's piece i has bit i).
+        auto put = [&](const Codes &o, auto special_, auto f16_, auto half_, uint32_t pieces) {
             constexpr bool SPECIAL = decltype(special_)::value, F16 = decltype(f16_)::value;
             constexpr int HALF = decltype(half_)::value;
             const int g = SPECIAL ? fresh(lane >> 4) : lane >> 4, n = SPECIAL ? fresh(lane & 15) : lane & 15;
             static_for<0, DB>([&](auto i_) {
                 constexpr int i = decltype(i_)::value;
                 if constexpr (DB % 2 == 0 && i / (DB / 2) != HALF) return;
-                const int four = v_key(i, g), key = 4 * n + four, block = v_block(i, g);
+                const int four = v_key(i, g), block = v_block(i, g);
                 if (DB % 2 && four / 2 != HALF) return;
                 u32x4 codes = o.v[i];
                 uint32_t byte = v_scale(o, i);
-                if constexpr (SPECIAL)
-                    if (!v_there || key0 + key >= f.last || f16_power(byte) != powers || byte >= KV_V_LIMIT) codes = zero, byte = 127;
+                if (SPECIAL && !(pieces >> i & 1)) codes = zero, byte = 127;
                 const float sc = __uint_as_float(byte << 23);
                 unsigned char *const to = lds + (16 * (four & 1) + n) * PITCH + 64 * block;
 #pragma unroll
@@ -201,10 +199,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             });
         };
         // weights and sums of a tile
-        auto take = [&](Codes &o, auto special_, f32x4 (&s)[4], int t, uint32_t fours) {
+        auto take = [&](Codes &o, auto special_, bool usual, f32x4 (&s)[4], int t, uint32_t fours) {
             constexpr bool SPECIAL = decltype(special_)::value;
             const int key0 = f.first + t * KV_TILE;
-            bool others = false, large = false;                                // pieces that fp16 does not have; with large values
+            uint32_t pieces = 0, others = 0;                                   // of v that are there: with powers of fp16, with others
+            bool any_others = false, large = false;                            // of all lanes; with large values
             if constexpr (SPECIAL) {
                 const int g4 = fresh(4 * g), from = lo - key0 - 4 * g4, past = hi - key0 - 4 * g4;
                 const uint32_t mine = fours >> g4;
@@ -212,26 +211,36 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[b][i] = (mine >> i & 1) && 4 * i + b >= from && 4 * i + b < past ? s[b][i] : -INFINITY;
-                // of the keys that are there: what v has beside the powers of fp16
-                const int g = fresh(lane >> 4), n = fresh(lane & 15);
-                auto is_there = [&](int i) { return (fours >> n & 1) && key0 + 4 * n + v_key(i, g) < f.last; };
-                uint32_t highest = 0;
+                const int left = fours >> fresh(n) & 1 ? f.last - key0 - 4 * fresh(n) : 0, g = fresh(lane >> 4);
 #pragma unroll
-                for (int i = 0; i < DB; ++i)
-                    if (is_there(i) && !f16_power(v_scale(o, i))) others = true, highest = max(highest, v_scale(o, i));
-                others = __builtin_amdgcn_ballot_w64(others) != 0;
-                if (__builtin_amdgcn_ballot_w64(highest >= LARGE_V)) {
-                    static_for<0, DB>([&](auto i_) {
-                        constexpr int i = decltype(i_)::value;
-                        uint64_t bads = __builtin_amdgcn_ballot_w64(is_there(i) && v_scale(o, i) >= KV_V_LIMIT);
-                        const int key = 4 * n + v_key(i, g), block = v_block(i, g);
-                        while (bads) {
-                            const int from = __builtin_ctzll(bads), bad_key = __builtin_amdgcn_readlane(key, from), bad_block = __builtin_amdgcn_readlane(block, from);
-                            bads &= bads - 1;
-                            if (key0 + bad_key >= lo && key0 + bad_key < hi) spoil |= 1u << bad_block;
+                for (int i = 0; i < DB; ++i) pieces |= (uint32_t)(v_key(i, g) < left) << i;
+                if (!usual) {
+                    asm volatile("" ::: "memory");
+                    uint32_t highest = 0;
+#pragma unroll
+                    for (int i = 0; i < DB; ++i)
+                        if (!f16_power(v_scale(o, i))) {
+                            others |= pieces & 1u << i;
+                            highest = max(highest, pieces >> i & 1 ? v_scale(o, i) : 0);
                         }
-                    });
-                    large = true;
+                    pieces &= ~others;
+                    any_others = __builtin_amdgcn_ballot_w64(others != 0) != 0;
+                    if (__builtin_amdgcn_ballot_w64(highest >= LARGE_V)) {
+                        const int n = fresh(lane & 15);
+                        static_for<0, DB>([&](auto i_) {
+                            constexpr int i = decltype(i_)::value;
+                            const bool is = (others >> i & 1) && v_scale(o, i) >= KV_V_LIMIT;
+                            uint64_t bads = __builtin_amdgcn_ballot_w64(is);
+                            if (is) others &= ~(1u << i);
+                            const int key = 4 * n + v_key(i, g), block = v_block(i, g);
+                            while (bads) {
+                                const int from = __builtin_ctzll(bads), bad_key = __builtin_amdgcn_readlane(key, from), bad_block = __builtin_amdgcn_readlane(block, from);
+                                bads &= bads - 1;
+                                if (key0 + bad_key >= lo && key0 + bad_key < hi) spoil |= 1u << bad_block;
+                            }
+                        });
+                        large = true;
+                    }
                 }
             }
             float most = -INFINITY;
@@ -249,7 +258,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                     uint32_t keys[4] = {0, 0, 0, 0};                           // of the keys 4 n + b those with large values, a bit each
                     static_for<0, DB>([&](auto i_) {
                         constexpr int i = decltype(i_)::value;
-                        const bool is = (fours >> n & 1) && key0 + 4 * n + v_key(i, g) < f.last && v_scale(o, i) >= LARGE_V && v_scale(o, i) < KV_V_LIMIT;
+                        const bool is = (others >> i & 1) && v_scale(o, i) >= LARGE_V;
 #pragma unroll
                         for (int b = 0; b < 4; ++b) {
                             const uint64_t are = __builtin_amdgcn_ballot_w64(is && v_key(i, g) == b);
@@ -297,24 +306,13 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                 }
             static_for<0, 2>([&](auto half_) {
                 constexpr int half = decltype(half_)::value;
-                __builtin_amdgcn_wave_barrier();
-                put(o, special_, std::true_type{}, half_, true, key0, fours >> n & 1);
-                if (!SPECIAL && half == 1) ask(V, o, t);
-                __builtin_amdgcn_wave_barrier();
                 const unsigned char *const at = lds + (4 * g + n / 4) * PITCH + 8 * (n % 4);
-                f16x8 p16 = weights_f16(w[half]);
-                if (SPECIAL && (raised >> fresh(lane) & 1)) p16 = f16x8{};
-#pragma unroll
-                for (int d = 0; d < 2 * DB; ++d) {
-                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, read_transposed(at + 32 * d, 16 * PITCH)), p16, acc[d], 0, 0, 0);
-                    if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-                }
                 if constexpr (SPECIAL) {
                     // in bf16: the other pieces, and for rows that have taken room those of fp16
-                    for (int pass = others ? 0 : 1; pass < (raised ? 2 : 1); ++pass) {
+                    for (int pass = any_others ? 0 : 1; pass < (raised ? 2 : 1); ++pass) {
                         asm volatile("" ::: "memory");
                         __builtin_amdgcn_wave_barrier();
-                        put(o, special_, std::false_type{}, half_, pass, key0, fours >> n & 1);
+                        put(o, special_, std::false_type{}, half_, pass ? pieces : others);
                         __builtin_amdgcn_wave_barrier();
                         bf16x8 high, low;
                         weights_bf16(w[half], high, low);
@@ -326,7 +324,20 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
                             acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, high, acc[d], 0, 0, 0);
                         }
                     }
-                    if (half == 1) ask(V, o, t);
+                }
+                __builtin_amdgcn_wave_barrier();
+                put(o, special_, std::true_type{}, half_, pieces);
+                if (half == 1) ask(V, o, t);
+                __builtin_amdgcn_wave_barrier();
+                f16x8 p16 = weights_f16(w[half]);
+                if (SPECIAL && raised) {
+                    asm volatile("" ::: "memory");
+                    if (raised >> fresh(lane) & 1) p16 = f16x8{};
+                }
+#pragma unroll
+                for (int d = 0; d < 2 * DB; ++d) {
+                    acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, read_transposed(at + 32 * d, 16 * PITCH)), p16, acc[d], 0, 0, 0);
+                    if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
             });
         };
@@ -353,11 +364,12 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DB <= 4 ? 2 : 1) void kv_attention_
             asm volatile("" : "+v"(s[0]), "+v"(s[1]), "+v"(s[2]), "+v"(s[3]));
             ask(K, o, t);
             __builtin_amdgcn_sched_barrier(0);
-            bool usual = true;                                                 // all in fp16 (keys that are not there count, too: they may make the tile a special one, which finds out)
+            bool usual = true;                                                 // all in fp16 (keys that are not there count, too: the tile is then a special one, which finds out)
 #pragma unroll
             for (int i = 0; i < DB; ++i) usual = usual && f16_power(v_scale(o, i));
-            if (__builtin_amdgcn_ballot_w64(!usual) == 0 && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all && !raised) take(o, std::false_type{}, s, t, fours);
-            else take(o, std::true_type{}, s, t, fours);
+            usual = __builtin_amdgcn_ballot_w64(!usual) == 0;
+            if (usual && fours == 0xffffu && key0 >= lo_all && key0 + KV_TILE <= hi_all && !raised) take(o, std::false_type{}, true, s, t, fours);
+            else take(o, std::true_type{}, usual, s, t, fours);
             page = page_next;
             page_next = page_third;
             page_third = ahead;
@@ -503,9 +515,10 @@ size_t sbits_kv_attention_cut(const sbits_ctx *ctx, const sbits_kv_cache &cache,
         a.few.tiles = (int)((std::min(new_most * group, FEW_MOST) + FEW_ROWS - 1) / FEW_ROWS);
         a.few.most_rows = (int)(only_few ? INT32_MAX : FEW_MOST);
         a.few.rows = (int)std::min(new_most * group, FEW_MOST);
-        // (as many workgroups as run at a time; their parts' join where items may be cut)
-        a.few.splits = (int)std::min((cache.head_dim <= 128 ? 2 : 1) * cus, std::max<int64_t>(1, (int64_t)sequences.count * a.few.tiles * cache.kv_heads * keys / FEW_LEAST));
+        // (as many workgroups as run at a time, if there are items or tiles of keys enough; their parts' join where items may be cut)
+        const int64_t items = (int64_t)sequences.count * a.few.tiles * cache.kv_heads;
         a.few.each = keys > FEW_WHOLE;
+        a.few.splits = (int)std::min((cache.head_dim <= 128 ? 2 : 1) * cus, std::max<int64_t>(a.few.each ? 1 : items, items * keys / FEW_LEAST));
     }
     if (!only_few) {
         const int64_t tiles = tokens * group / MANY_ROWS + sequences.count;

@@ -302,7 +302,7 @@ __device__ __forceinline__ int few_find(const AttentionArgs &a, int64_t x, int64
     }
     return -1;
 }
-__device__ __forceinline__ int few_workgroups(const AttentionArgs &a, int64_t total) { return few_workgroups(a.few.splits, total); }
+__device__ __forceinline__ int few_workgroups(const AttentionArgs &a, int64_t total) { return few_workgroups(a.few.splits, a.few.each, total); }
 // A number of a lane's that the compiler takes for a new one: what is computed from it stays where it is, and is not kept in registers over a loop.
 __device__ __forceinline__ int fresh(int v)
 {

@@ -23,10 +23,11 @@ constexpr KeyRange seen_keys(bool causal, int window, int there, int length, int
 // then heads, make a line of W tiles of keys, of which workgroup w of G has those from cut(w) to cut(w + 1):  w (W / G), moved to the item's begin or end where that is less than FEW_EDGE tiles
 // away, and to the begin of an item of up to FEW_WHOLE tiles.  So workgroups have the same to do, whatever the lengths.  A part of an item goes to slot 2 w + 1 of its workgroup if it is the item's
 // first, else to 2 w: a workgroup's last part is an item's first, and of others it has no more than one.
-constexpr int FEW_EDGE = 4, FEW_WHOLE = 16, FEW_LEAST = 8;       // FEW_LEAST: tiles of keys a workgroup, at least
-constexpr int few_workgroups(int most, int64_t total)
+constexpr int FEW_EDGE = 4, FEW_WHOLE = 16, FEW_LEAST = 8;       // FEW_LEAST: tiles of keys a workgroup, at least, where items may be cut
+// (Where none may be, a workgroup for each of them costs nothing: 87 sequences of up to 29 tokens, 16 heads of 128: 48 us with eight items in a row a workgroup, 27 with up to three; 8 tokens of one sequence, 16 heads of 256 on 2: 79 and 13.)
+constexpr int few_workgroups(int most, bool space, int64_t total)
 {
-    const int64_t all = total / FEW_LEAST;
+    const int64_t all = space ? total / FEW_LEAST : total;
     return all >= most ? most : all < 1 ? 1 : (int)all;
 }
 // Where cut w of G falls ahead of its move (w < G): a product in 64 bits, rounded down, which is the same wherever it is asked for.

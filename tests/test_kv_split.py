@@ -66,7 +66,7 @@ int main()
             begin[b + 1] = begin[b] + (int64_t)tiles[b] * kv * keys[b];
         }
         const int64_t total = begin[n];
-        const int workgroups = few_workgroups(most, total);
+        const int workgroups = few_workgroups(most, space, total);
         int at, item, off;
         auto cuttable = [&](int b) { return few_cuttable(space, announced, rows[b], keys[b]); };
         auto cut = [&](int w) {
