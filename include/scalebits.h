@@ -580,7 +580,7 @@ int  sbits_rotate(sbits_ctx *ctx, const sbits_rotary *rotary, const int32_t *pos
 /* Writes the rows of k and v ([tokens][kv_heads][head_dim] by pitches as above, of `type`) to their sequences' places in
  * the cache, quantised as sbits_mx_quantize does.  With `rotary` (may be NULL) keys are turned
  * first, by positions[row] or, where positions is NULL, by the row's place in its sequence, in 64
- * bits, without a rounding ahead of the quantisation; and the rows of q (may be NULL), with q_heads
+ * bits, without a rounding ahead of the quantisation (beyond fp32's range its largest number); and the rows of q (may be NULL), with q_heads
  * heads, are turned as sbits_rotate does into q_out (which may be q with the same pitches).  Rows that are 16-byte aligned: pitches multiples of 8
  * (bf16) or 4 (fp32).  Where a place is not there, q_out is written all the same.         */
 int  sbits_kv_store(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens,
@@ -599,11 +599,13 @@ int  sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequ
  * positions up to p, with window > 0 (causal only) the last `window` of them; else all of the sequence's.
  * A row that sees no key gets zeros.  lse (float32[tokens][heads], may be NULL): the logarithm of the sum of
  * e^(scale * q . k_j), -infinity where no key is seen.  Only keys that a row sees have a part in it, whatever the others
- * hold; a seen value that is not finite makes its block of 32 outputs NaN (in v the bytes 253 and 254 count as 255), a seen key that is
- * not or a q that is not makes the row NaN.  Scores and sums are taken in fp32 on the matrix cores, in an order that goes with the batch's
- * sizes; a call gives the same bits again.  scale > 0.  ws: 256-byte aligned,
+ * hold: not a bit goes with them, nor with other rows.  A seen value that is not finite makes its block of 32 outputs NaN (in v the bytes 253 and 254 count as 255), a seen key that is
+ * not or a q that is not makes the row NaN; so does a score above fp32's range, while one below it counts for nothing.  Scores, sums of weights and of their products are taken in fp32 on the
+ * matrix cores, in an order that goes with the batch's sizes; a call gives the same bits again.  A weight enters its product with 11 bits (fp16), or with 16 beside
+ * blocks of v whose bytes are not 104 .. 140, and below 2^-33 of the largest as a multiple of that.  q enters in 6-bit terms, which leave out less than 2^-15 of the largest value of a block of 32,
+ * with lse less than 2^-18 (and of blocks below 2^-108 what is below 2^-124).  scale > 0.  ws: 256-byte aligned,
  * sbits_kv_attention_ws_bytes() bytes (which may be 0), asked for with the call's own arguments.  Positions from 2^31 - 4096 on
- * are not there.  At most 2^24 sequences.  With lse, q enters the products in a term more, so that last bits of out may differ.  */
+ * are not there.  At most 2^24 sequences.  */
 size_t sbits_kv_attention_ws_bytes(const sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens,
                                    int heads);
 int  sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequences *sequences, int64_t tokens, int heads,

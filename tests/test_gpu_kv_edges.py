@@ -247,3 +247,44 @@ def test_all_bytes_and_codes_read_back(ctx, dtype):
     got = out.cpu()[:, 0]
     assert torch.isnan(got[255]).all()
     assert torch.equal(got[:255], want.to(dtype))                # (both roundings to nearest even, and to infinity)
+
+
+# ---- beyond fp32 -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("sizes", [[(1, 300)], [(100, 60)]])
+def test_scores_beyond_fp32(ctx, sizes):
+    """Above the range: NaN for the rows that see the key; below it: as if it were not there."""
+    b = Batch(sizes, 16, 1, 64, seed=4)
+    n, past = sizes[0]
+    q = queries(b, 2)
+    q[:, :, 0] = 2.0 ** 20
+    page, at = b.places(0, 0, n + past)
+    b.codes[0][page, 0, at, 0] &= 0xf0                           # k's first element: 0
+    want = attend(ctx, b, q)
+    key = past // 2
+    b.codes[0][page[key], 0, at[key]] = 0
+    for code in (0xf, 0x7):                                      # -6 and 6 times 2^125, and 2^20 in q
+        b.codes[0][page[key], 0, at[key], 0] = code
+        b.scales[0][page[key], 0, at[key], 0] = 252
+        out, sums = attend(ctx, b, q)
+        if code == 0x7:
+            assert torch.isnan(out).all()
+            continue
+        b2 = Batch(sizes, 16, 1, 64, seed=4)
+        b2.codes, b2.scales = [c.clone() for c in b.codes], [s.clone() for s in b.scales]
+        b2.codes[0][page[key], 0, at[key]] = 0
+        b2.codes[0][page[key], 0, at[key], 0], b2.scales[0][page[key], 0, at[key], 0] = 0xf, 140      # -6 * 2^13 * 2^20 / 8: e^-6e9
+        other, other_sums = attend(ctx, b2, q)
+        assert torch.equal(out, other) and torch.equal(sums, other_sums)
+        assert torch.isfinite(out).all() and want[0].shape == out.shape
+
+
+def test_keys_turned_beyond_fp32_are_its_largest_number(ctx):
+    b = Batch([(1, 0)], 16, 1, 32)
+    cache, seqs, buffers = b.on(sb)
+    k = torch.full((1, 1, 32), 3e38)
+    k[..., 16:] = -3e38
+    turn = torch.full((16,), 0.125, dtype=torch.float64, device="cuda")                  # at position 1 an eighth of a turn: (a, -a) to (1.41 a, 0)
+    ctx.kv_store(cache, seqs, k.cuda(), k.cuda(), rotary=sb.rotary(turn), positions=torch.ones(1, dtype=torch.int32, device="cuda"))
+    out = torch.zeros(1, 1, 32, device="cuda")
+    ctx.kv_load(cache, seqs, out, None)
+    assert (out[..., :16] == 6.0 * 2.0 ** 125).all() and (out[..., 16:].abs() <= 2.0 ** 123).all()
