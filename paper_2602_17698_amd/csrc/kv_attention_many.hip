@@ -108,15 +108,19 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
     // this wave's share of a tile: 16 keys, 16 DB pieces of k and of v
     u32x4 kc[PIECES], vc[PIECES];
     uint32_t vs[PIECES], ks;
+    // (Of heads up to 96 lanes behind the last piece do that one again: prompts of 8192 tokens, heads of 96 581 us, 589 where they wait; of 160 and 192, where they would be half of a
+    // second round, 1597 and 1617 us, 1519 and 1472 where they wait.)
+    constexpr bool AGAIN = DB < 4;
+    auto piece_of = [&](int i) { return AGAIN ? min(64 * i + lane, 16 * DB - 1) : 64 * i + lane; };
     auto fetch = [&](int t, int pages) {                                       // (keys that are not there: of page 0)
         pages = known(pages);
         const int key0 = ((key_first + t * KV_TILE) & a.cache.mask) + 16 * wave;
         const int64_t rows = (int64_t)kv_head << a.cache.shift;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
+            const int piece = piece_of(i), key = piece / DB, block = piece % DB;
             const uint32_t page = __shfl(pages, (16 * wave + key) & 63);        // (of all lanes: a lane that is not there would give 0)
-            if (16 * DB % 64 && key >= 16) continue;
+            if (!AGAIN && key >= 16) continue;
             const uint32_t at = (key0 + key) & a.cache.mask;
             const uint64_t codes = (uint64_t)page * (uint32_t)a.cache.ld_codes + (at * (16 * DB) + 16 * block);
             kc[i] = *reinterpret_cast<const u32x4 *>(a.cache.codes[0] + rows * (16 * DB) + codes);
@@ -131,8 +135,8 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         bool usual = true;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
-            if (16 * DB % 64 && key >= 16) continue;
+            const int piece = piece_of(i), key = piece / DB, block = piece % DB;
+            if (!AGAIN && key >= 16) continue;
             *reinterpret_cast<u32x4 *>(sh.k[buffer] + (16 * wave + key) * K_PITCH + 16 * block) = kc[i];
             if (!(mine >> key & 1)) vc[i] = zero, vs[i] = 127;
             usual = usual && f16_power(vs[i]);
@@ -141,8 +145,8 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
         auto write = [&](auto all_f16) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const int piece = 64 * i + lane, key = piece / DB, block = piece % DB;
-                if (16 * DB % 64 && key >= 16) continue;
+                const int piece = piece_of(i), key = piece / DB, block = piece % DB;
+                if (!AGAIN && key >= 16) continue;
                 const float sc = __uint_as_float(vs[i] << 23);
                 unsigned char *const to = sh.v[buffer];
                 const uint32_t first = (16 * wave + key) * V_PITCH + 64 * block + 16 * (key & 3);
@@ -152,7 +156,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
             }
         };
         uint32_t kind = 0;
-        if (__builtin_amdgcn_ballot_w64(!usual) == 0) {
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!usual) == 0, 1)) {
             write(std::true_type{});
         } else {
             // a lane a key: its blocks of which something is so, a bit each
@@ -235,7 +239,7 @@ __global__ __launch_bounds__(64 * MANY_WAVES, DB <= 4 ? 2 : 1) void kv_attention
                 });
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (hidden) {
+            if (__builtin_expect(hidden, 0)) {
                 asm volatile("" ::: "memory");
                 const int h4 = fresh(4 * h), from = lo - key0 - h4, past = hi - key0 - h4;
                 const uint32_t mine = (uint32_t)(valid >> 32 * m) >> h4;
