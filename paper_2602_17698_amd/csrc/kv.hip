@@ -206,6 +206,9 @@ int sbits_kv_attention(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_
     a.heads = heads; a.group = heads / cache->kv_heads;
     a.there = (int)std::min<int64_t>((int64_t)sequences->max_pages * cache->page_tokens, KV_MAX_KEYS);
     a.scale = (float)(scale * 1.4426950408889634); a.causal = causal; a.window = window;
+    // (of rows with a window of few keys no item is long enough to be cut)
+    const int64_t new_most = sequences->max_new ? std::min<int64_t>(sequences->max_new, tokens) : tokens;
+    if (window && window + new_most <= (FEW_WHOLE - 2) * KV_TILE) a.few.each = 0;
     char *const base = static_cast<char *>(ws);
     a.few.part = reinterpret_cast<float *>(base);
     a.many.part = reinterpret_cast<float *>(base + sbits_kv_attention_part(a.few, FEW_ROWS, *cache));

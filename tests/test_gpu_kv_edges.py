@@ -211,7 +211,7 @@ def test_means_of_thousands_of_the_largest_values_are_finite(ctx, byte, sizes):
     ([(1, 5000)], 1, 4, 64, 128, 0), ([(1, 5000)], 2, 1, 8, 64, 0), ([(17, 3000), (1, 9)], 1, 2, 16, 128, 0), ([(17, 3000), (1, 9)], 2, 4, 32, 96, 700),
     ([(3, 4000), (1, 63), (5, 1100), (2, 1023), (1, 0), (16, 2047)], 3, 1, 16, 160, 0), ([(1, 20000)], 1, 8, 256, 256, 0), ([(1, 9000)], 1, 16, 64, 224, 5000),
     ([(100, 5000)], 1, 2, 64, 128, 0), ([(100, 5000), (40, 3000), (1, 800)], 2, 2, 16, 64, 0), ([(65, 7000)], 1, 1, 128, 192, 0), ([(129, 2000)], 1, 1, 8, 32, 1500),
-    ([(200, 0), (70, 60)], 2, 3, 64, 96, 33), ([(1, 1000 + 7 * i) for i in range(40)], 1, 2, 16, 64, 0)])
+    ([(200, 0), (70, 60)], 2, 3, 64, 96, 33), ([(3, 9000), (1, 63), (5, 1100), (1, 5), (16, 2047)], 2, 1, 32, 64, 800), ([(1, 1000 + 7 * i) for i in range(40)], 1, 2, 16, 64, 0)])
 @pytest.mark.parametrize("causal", [True, False])
 def test_each_key_by_itself(ctx, sizes, kv_heads, group, page, dim, window, causal):
     """Outputs that count keys: one that is lost, taken twice or multiplied with another's weight is outside of the bound (see kv_tight.Counted)."""
