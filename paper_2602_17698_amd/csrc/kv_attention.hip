@@ -36,7 +36,7 @@ __device__ __forceinline__ void put_row(const AttentionArgs &a, int start, int k
 // of 8 keys, the ones whose weights it has.
 // A tile's codes of k are asked for when those of the one before have been used, of v likewise; pages' numbers two tiles earlier.  (Codes of two tiles under way took registers
 // that are not there: 171 us where this takes 138.)
-// Reading the cache bounds it: 64 sequences of 1638 to 16384 tokens, 8 heads of 128, 642 MB, 135 .. 138 us or 4.7 TB/s (the same loads without the arithmetic reach 5.8); 131072 tokens of
+// Reading the cache bounds it: 64 sequences of 1638 to 16384 tokens, 8 heads of 128, 642 MB, 137 us or 4.7 TB/s (the same loads without the arithmetic reach 5.8); 131072 tokens of
 // one sequence, 143 MB, 28 us.  Each wave has its chain of scores, weights and sums, two waves a SIMD; a third of the time a SIMD issues vector instructions.
 template <int DB>
 struct FewCodes { u32x4 k[4][(DB + 3) / 4], v[DB], ks[(DB + 3) / 4], vq[DB % 4 ? 1 : DB / 4]; uint8_t vb[DB]; };

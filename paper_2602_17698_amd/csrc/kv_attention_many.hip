@@ -8,13 +8,14 @@ namespace sbits {
 constexpr int MANY_WAVES = 4;
 
 // A workgroup has 128 rows (tokens times the heads of a key's head), a wave 32 of them, and goes over their keys 64 at a time.  A wave brings 16 keys of a tile: k's codes go to
-// LDS as they are, v's as fp16 (or bf16), in one of two buffers while the other is read; codes are asked for a tile ahead of that, pages' numbers two.
+// LDS as they are, each block of v as fp16 or bf16, in one of two buffers while the other is read; codes are asked for a tile ahead of that, pages' numbers two.
 // Scores, transposed: a lane has k's row and block from LDS and its row of q in 6-bit terms, and gets for row lane % 32 the keys 8 (r / 4) + 4 (lane / 32) + r % 4 of 32.
 // Sums, transposed: weights are where the instruction wants them, if 16 keys come in the order 8 (j / 4) + 4 (lane / 32) + j % 4; v's transposing reads bring them so.
 // In LDS the 16-byte pieces w of a block of v are at w ^ (key % 4), so that a wave's writes, 16 lanes of which have 4 keys' blocks, meet all banks.
 // Measured: a prompt of 8192 tokens, 32 heads on 8 of 128: 585 us, 0.94 PFLOP/s.  The matrix cores are busy a third of that, vector instructions are issued half of it (a tile of a wave: 28 matrix
 // and 280 vector instructions, 32 of them powers of two), LDS is busy two fifths.  On the way: 903 us with q spilled to scratch, whose reloads wait for all loads under way; 821 with
-// sums taken anew only where the largest score has grown by 2^6; 651 without spills; 617 with one way to the sums; 585 with writes to LDS that meet all banks.
+// sums taken anew only where the largest score has grown by 2^6; 651 without spills; 617 with one way to the sums; 585 with writes to LDS that meet all banks.  What happens to few tiles is
+// marked unlikely: in the way of the usual it cost 3 %.
 template <int DB>
 struct ManyShared {
     static constexpr int K_PITCH = 16 * (DB | 1), V_PITCH = 64 * DB + (DB % 2 ? 0 : 64), SCALES = (DB + 3) / 4 * 4;      // pitches: neighbouring rows in other banks

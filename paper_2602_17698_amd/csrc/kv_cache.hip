@@ -3,7 +3,7 @@
 // Keys that are turned on the way are turned in 64 bits and quantised from there: the codes are those of the exact product, without a rounding between.
 // Memory bounds both: 2 or 4 bytes read and 17/32 written for each value, or the other way round.  A workgroup has a row, or eight where there are many; a thread takes 8 values,
 // four lanes a block of 32.  16384 tokens of 8 heads of 128, 32 of queries beside them, written and read back: 114 us, 3.8 TB/s (180 with a workgroup a row and queries in
-// 64 bits); 17916 tokens of 16 heads read: 55 us, 3.4 TB/s (63).  64 rows written: 8 us, of which the search for the sequence, its page and the angles, one after the
+// 64 bits); 17916 tokens of 16 heads read: 55 us, 3.4 TB/s (63).  64 rows written: 6.4 us, of which the search for the sequence, its page and the angles, one after the
 // other, are most.
 #include "kv_core.hpp"
 

@@ -342,7 +342,8 @@ typedef float f32x32 __attribute__((ext_vector_type(32)));
 // A block of 32 values of q as blocks of 6-bit codes (E2M3) whose powers of two are 4, 6 and 6 steps apart.  The matrix instruction multiplies 4-bit by 6-bit
 // codes at twice the rate of bf16 and without a conversion of k.  A code has 4 bits, bf16 8: what the first term leaves of elements down to 1/4
 // of the block's largest is exact in the second, of those down to 2^-8 of it in the third, of those down to 2^-14 in the fourth; of smaller ones less than 2^-18
-// of the largest is left out (with three terms less than 2^-15).
+// of the largest is left out (with three terms less than 2^-15); of blocks whose largest is below 2^-108, whose first power is that of 2^-110, what is below 2^-124 with
+// three terms, 2^-129 with four.
 constexpr int Q_STEP[4] = {0, 4, 10, 16};
 template <int TERMS>
 struct QBlock { u32x6 codes[TERMS]; int scales; };                            // scales: the terms' bytes
