@@ -602,7 +602,8 @@ int  sbits_kv_load(sbits_ctx *ctx, const sbits_kv_cache *cache, const sbits_sequ
  * hold: not a bit goes with them, nor with other rows.  A seen value that is not finite makes its block of 32 outputs NaN (in v the bytes 253 and 254 count as 255), a seen key that is
  * not or a q that is not makes the row NaN; so does a score above fp32's range, while one below it counts for nothing.  Scores, sums of weights and of their products are taken in fp32 on the
  * matrix cores, in an order that goes with the batch's sizes; a call gives the same bits again.  A weight enters its product with 11 bits (fp16), or with 16 beside
- * blocks of v whose bytes are not 104 .. 140, and below 2^-33 of the largest as a multiple of that.  q enters in 6-bit terms, which leave out less than 2^-15 of the largest value of a block of 32,
+ * blocks of v whose bytes are not 104 .. 140, and below 2^-33 of the largest as a multiple of that; in a row that sees
+ * values from 2^73 on, what is below 2^-95 may be lost.  q enters in 6-bit terms, which leave out less than 2^-15 of the largest value of a block of 32,
  * with lse less than 2^-18 (and of blocks below 2^-108 what is below 2^-124).  scale > 0.  ws: 256-byte aligned,
  * sbits_kv_attention_ws_bytes() bytes (which may be 0), asked for with the call's own arguments.  Positions from 2^31 - 4096 on
  * are not there.  At most 2^24 sequences.  */

@@ -30,9 +30,9 @@ def attention(b, q, scale=None, causal=True, window=0, terms=3):
 
     A score: sums in fp32 of products that are exact, each addition off by 2^-23 of the magnitudes' sum, of which there are no more than terms * dim / 32 and 256 inside
     instructions; of q what the terms leave out, 2^-15 of its block's largest value with three of them and 2^-18 with four.  A weight: the power of two is off by a unit in the last
-    place, its argument by 2^-23 of its own and the largest score's size; rounded to fp16 2^-11 and, where it is small, by 2^-25 against a sum of 2^9.  Sums of keys by 16 or 32:
-    2^-23 each.  The output: bf16, 2^-8.  Below 2^-126 steps are no longer relative: bf16 rounds by up to 2^-134, and a product of a weight with v that the matrix cores may count as 0 is
-    below 2^-126, against a sum of weights of 2^9."""
+    place, 2^-23; its argument, 9 to 15 and the largest score's size, by half a unit of numbers below 16, 2^-21, and 2^-23 of that size; rounded to fp16 2^-11 and, where it is small, by 2^-25 against a
+    sum of 2^9.  Sums of weights: 2^-24 for each key, and for what joins them; of products, 16 or 32 at a time, 2^-23 each.  The output: bf16, 2^-8.  Below 2^-126 steps are no longer relative: bf16 rounds by up to
+    2^-134, and a product of a weight with v that the matrix cores may count as 0 is below 2^-126, against a sum of weights of 2^9, or where the row sees values from 2^73 on, of 2^-31."""
     dim, group = b.dim, q.shape[1] // b.kv_heads
     scale = dim ** -0.5 if scale is None else scale
     parts = []
@@ -54,13 +54,17 @@ def attention(b, q, scale=None, causal=True, window=0, terms=3):
         lse = torch.logsumexp(t, -1)
         w = torch.where(seen.any(-1)[:, None, None, None], torch.softmax(t, -1), 0.0)
         y, size, least = (torch.zeros_like(x) for _ in range(3))
+        largest_v = torch.zeros(end - first, b.kv_heads, dtype=torch.float64)
         for i in range(end - first):                                              # (what a row does not see takes no part, whatever it is)
             u = v.masked_fill(~seen[i][None, :, None], 0.0)
             y[i], size[i] = torch.einsum("hgk,hkd->hgd", w[i], u), torch.einsum("hgk,hkd->hgd", w[i], u.abs())
             least[i] = u.abs().sum(1)[:, None]
-        power = (1 + size_t) * 2.0 ** -22
+            if len(key):
+                largest_v[i] = u.abs().nan_to_num(nan=0.0).amax((1, 2))
+        power = (3 + size_t) * 2.0 ** -22 + (len(key) + 64) * 2.0 ** -24
+        lost = 2.0 ** -134 + len(key) * torch.where((largest_v >= 2.0 ** 72)[:, :, None, None], 2.0 ** -95, 2.0 ** -135)
         off = (torch.expm1(2 * (far + power).clamp(max=100.0)) + 2.0 ** -11 + (len(key) / 16 + 64) * 2.0 ** -23) * size + 2.0 ** -8 * y.abs() + 2.0 ** -34 * least \
-            + 2.0 ** -134 + len(key) * 2.0 ** -135
+            + lost
         off_lse = (far + power)[..., 0] + 2.0 ** -22 * (1 + lse.abs().nan_to_num(posinf=0.0))
         parts.append([z.flatten(1, 2) for z in (y, lse, off, off_lse)])
     return tuple(torch.cat(p) for p in zip(*parts))
