@@ -449,6 +449,8 @@ class Context:
             if positions.shape != (tokens,) or not positions.is_contiguous():
                 raise ValueError("positions is not [%d]" % tokens)
         queries, heads, turned = (None, 0, 0), 0, (None, 0, 0)
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
         if q is not None:
             _is(q, kind, "q")
             _is(q_out, kind, "q_out")

@@ -1,4 +1,8 @@
 """Outputs of the cache's reading and writing, of rotary positions and of attention whose rows and heads lie in each other are refused, on a device that need not be there."""
+import pytest
+import torch
+
+import kv_plain
 from paper_2602_17698_amd import binding as sb
 from recording_runtime import record
 
@@ -75,3 +79,13 @@ answer(out)
 """)
     tiles = 100000 * 8 // 128 + (1 << 24)
     assert got == [[True, sb.OK, 4 << 24, tiles]] + [[False, sb.ERR_BAD_SHAPE, 0, 0]] * 3
+
+
+def test_queries_and_what_they_become_go_together():
+    ctx = sb.Context(device=-1)
+    cache, seqs, _ = kv_plain.Batch([(2, 3), (1, 0)], 8, 2, 64).on(sb, dev="cpu")
+    k, turn = torch.zeros(3, 2, 64), sb.rotary(torch.zeros(32, dtype=torch.float64))
+    for other in (dict(q=k), dict(q_out=k)):
+        with pytest.raises(ValueError):
+            ctx.kv_store(cache, seqs, k, k, rotary=turn, **other)
+    ctx.close()
